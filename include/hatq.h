@@ -520,6 +520,97 @@ hatq_status hatq_prepare_gdn(int c, const double *beta, const double *gamma, flo
  * Stream-ordered; device errors surface through hatq_sync_status(). */
 hatq_status hatq_gdn(const int8_t *z, int n, int h, int w, const hatq_prepared_gdn *g, int8_t *y, hatq_stream stream);
 
+/*
+ * Token layers: the DH layer (Eq. double_hadamard_quantization) for row-major
+ * token matrices, with one activation scale per token (row) taken from the row
+ * itself, one weight scale per output channel, and one weight matrix per
+ * expert. The paper states tensor-wise activation scales; the scale per token
+ * is Eq. symmetric_q applied to each row of its operand.
+ */
+typedef enum { HATQ_F32 = 0, HATQ_F16 = 1, HATQ_BF16 = 2 } hatq_type;
+/* How INT8 codes are held: as int8, or as fp16 (every code is exact). */
+typedef enum { HATQ_CODES_I8 = 0, HATQ_CODES_F16 = 1 } hatq_codes;
+
+/* Per-token transform and quantization. For every row r < rows, with
+ * v = x[index[r]] (index NULL: x[r]), all in fp32:
+ *   u = act(v), or act(v[0..c)) * v[c..2c) when gated
+ *   t = H~_hb u on consecutive blocks of hb (unnormalized), a = max|t|
+ *   codes[r] = clamp(round(t min(127 / a, 2^126)), -127, 127)
+ *   scales[r] = max(a / 127, 2^-126) / sqrt(hb)
+ * so codes * scale is the operand H~ u / sqrt(hb). A row with a = 0 gets codes 0
+ * and scale 1; a row with an infinity or a NaN in t gets codes 0 and scale NaN
+ * (its outputs are NaN, no other row's). An index outside [0, src_rows) is an
+ * empty row: v = 0 without activation, codes 0, scale 1.
+ *   x        device, type x_type, src_rows rows of c (2 c when gated) values at
+ *            a pitch of ldx elements; index device int32 [rows] or NULL (then
+ *            src_rows >= rows)
+ *   c        1 .. 32768; hb a power of two <= 256 that divides c (1: no transform)
+ *   act      hatq_act (SiLU: v / (1 + exp(-v)), GELU: with erf)
+ *   codes    device, hatq_codes format, pitch ldc >= c; behind c nothing is written
+ *   scales   device float [rows]
+ * Any element alignment works; 16-byte aligned rows are read and written in
+ * 16-byte pieces. x and codes must not overlap. */
+hatq_status hatq_quantize_tokens(const void *x, int x_type, long long ldx, long long src_rows, const int32_t *index,
+                                 long long rows, int c, int hb, int act, int gated, int format, void *codes,
+                                 long long ldc, float *scales, hatq_stream stream);
+
+/* The weights of a token layer, laid out for hatq_linear / hatq_grouped_linear. */
+typedef struct {
+    int experts;          /* 1 .. 1024; 1 for a dense layer */
+    int n, k;             /* output channels, reduction length (k <= 65536) */
+    int reserved;
+    uint8_t *codes;       /* device, hatq_linear_sizes bytes, 16-byte aligned; written by hatq_linear_layout */
+    int32_t *windows;     /* device [experts]; written by hatq_linear_layout */
+    float *s_w;           /* device [experts][n], the channels' scales; the caller's */
+    float *bias;          /* device [experts][n] or NULL; the caller's */
+} hatq_linear_weights;
+
+/* Bytes of hatq_linear_weights.codes: experts * n * k, n padded to 128, k to 64. */
+hatq_status hatq_linear_sizes(int experts, int n, int k, size_t *code_bytes);
+
+/* Lays out INT8 weight codes w (device [experts][n] rows of k codes at a pitch
+ * of ldw; the whole int8 range is allowed) into L->codes and L->windows. The
+ * codes of a floating-point weight matrix are those of hatq_quantize_tokens on
+ * its rows (I8 format), with the layer's hb. Stream-ordered. */
+hatq_status hatq_linear_layout(const int8_t *w, long long ldw, const hatq_linear_weights *L, hatq_stream stream);
+
+/* y[r][n] = (sum_k x[r][k] w[n][k]) s_w[n] s_x[r] + bias[n] for r < rows: an
+ * exact integer sum (int32), converted to fp32, scaled, rounded once to y_type.
+ *   x          device codes in hatq_codes format, rows at a pitch of ldx >= k
+ *   s_x        device float [rows]
+ *   y          device, hatq_type y_type, pitch ldy >= n; must not overlap x
+ *   workspace  device scratch, 16-byte aligned, of the bytes that
+ *              hatq_linear_workspace returns for the same x, format, ldx, rows
+ *              and experts (0: may be NULL); calls in flight at the same time
+ *              need one each
+ * Fp16 codes must be integers in [-128, 127]. Weights are read once per call
+ * for up to a few hundred rows. Stream-ordered; an expired device wait surfaces
+ * through hatq_sync_status(). */
+hatq_status hatq_linear_workspace(const void *x, int format, long long ldx, long long rows,
+                                  const hatq_linear_weights *L, size_t *bytes);
+hatq_status hatq_linear(const void *x, int format, long long ldx, const float *s_x, long long rows,
+                        const hatq_linear_weights *L, int y_type, void *y, long long ldy, void *workspace,
+                        size_t workspace_bytes, hatq_stream stream);
+
+/* hatq_linear with the weights of the expert that holds the row: expert e holds
+ * rows offsets[e] .. offsets[e + 1] - 1 (device int32 [experts + 1], ascending,
+ * within [0, rows]; experts may hold no row). Rows that no expert holds are not
+ * written. Offsets are read on the device only; values outside [0, rows] are
+ * clamped to it, and an expert whose end lies before its start holds nothing. */
+hatq_status hatq_grouped_linear(const void *x, int format, long long ldx, const float *s_x, long long rows,
+                                const int32_t *offsets, const hatq_linear_weights *L, int y_type, void *y,
+                                long long ldy, void *workspace, size_t workspace_bytes, hatq_stream stream);
+
+/* out[t] = sum_{j < topk} weights[t][j] y[index[t][j]], j ascending, in fp32,
+ * rounded once; an index outside [0, rows) contributes nothing (a token whose
+ * indices all do gets zeros).
+ *   y, out   device, hatq_type type, rows of c values at pitches ldy, ldo >= c
+ *   index    device int32 [tokens][topk], weights device float [tokens][topk]
+ *   topk     1 .. 64 */
+hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
+                              const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
+                              hatq_stream stream);
+
 /* Failure-detection self test (the paper has no counterpart): launches one
  * thread that waits, through the same bounded mbarrier wait the convolution
  * pipeline uses, on a barrier nothing arrives at. The wait expires after

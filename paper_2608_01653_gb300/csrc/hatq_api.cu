@@ -17,6 +17,7 @@
 
 #include "hatq.h"
 #include "hatq_internal.h"
+#include "hatq_tokens.h"
 
 namespace {
 
@@ -529,6 +530,19 @@ hatq_status prepare_core(const hatq_conv_desc *d, const float *w_ohwi, const flo
 }  // namespace
 
 hatq_status hatq::report(hatq_status st, const char *msg) { return fail(st, "%s", msg); }
+
+int *hatq::device_error_word() { return err_word(); }
+
+CUresult hatq::encode_tiled_2d(CUtensorMap *tm, CUtensorMapDataType type, const void *base, unsigned long long inner,
+                               unsigned long long outer, unsigned long long pitch_bytes, unsigned box_inner,
+                               unsigned box_outer) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return CUDA_ERROR_NOT_SUPPORTED;
+    const cuuint64_t dims[2] = {inner, outer}, strides[1] = {pitch_bytes};
+    const cuuint32_t box[2] = {box_inner, box_outer}, estr[2] = {1, 1};
+    return enc(tm, type, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
 
 extern "C" {
 

@@ -1,0 +1,571 @@
+// The token layers' product on the 5th-generation tensor cores: for every row r
+// of a group and every output channel n
+//   y[r][n] = (sum_k x[r][k] w[n][k]) s_w[n] s_x[r] + bias[n],
+// x and w integers of 8 bits and the sum an exact integer. The groups are the
+// experts of a mixture (row ranges read from device offsets) or one dense layer.
+//
+// sm_103a has no 8-bit integer tensor-core kind, so codes enter as fp16 (exact)
+// and fp32 accumulators hold exact integers as long as no partial sum passes
+// 2^24. The layout pass measured, per expert, up to which window length
+// 128 sum |w| stays below that (trained weights: usually 4096 codes and more,
+// where the blind bound allows 1024); past a window the epilogue warps add the
+// accumulator into int32 registers while the next window fills the other one.
+//
+// The WEIGHTS are the M side (128 channels, the tensor-memory lanes) and the
+// tokens the N side. So the weights stay one byte in memory - what a decode step
+// is bound by - and are widened on their way into tensor memory, and a tile of
+// few tokens wastes no lanes. The tokens' codes are fp16 in memory (few bytes
+// next to the weights, or next to the arithmetic when there are many) and go
+// from the copy engine to the tensor cores untouched.
+//
+// Roles of a CTA's 20 warps: 0 copies (8 KB weight blocks by bulk copy, token
+// boxes by TMA), 1 issues the MMAs, 4-11 widen weights (two warpgroups, every
+// other 64-code block: prmt puts code + 128 into the mantissa of 1024.0, one
+// subtraction leaves the code), 12-19 are the epilogue (half of the tile's
+// tokens per warpgroup). Two accumulators alternate, so the epilogue of one
+// window or tile runs under the MMAs of the next.
+//
+// kPair: two CTAs (one cluster) compute 256 channels x kT tokens with
+// cta_group::2; each widens its own 128 channels and holds half of the tokens,
+// which halves the shared-memory traffic per product. split > 1: the CTAs of a
+// cluster share one tile's reduction and add their int32 sums through
+// distributed shared memory (integers: the order does not matter).
+// Every wait is bounded, as in the other tensor-core kernels.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hatq_tc.h"
+#include "hatq_tokens.h"
+
+namespace hatq {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 640;
+// registers per thread of the five warpgroups: copies and MMAs, two of converters, two of the epilogue
+constexpr int kRegsIssue = 40, kRegsWiden = 72, kRegsOut = 144;
+constexpr int kRegShares = kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut;
+constexpr int kRasterN = 8;            // channel tiles that share a sweep over the token tiles
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// mbar_wait for barriers that the other CTA of a cluster may arrive at
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t spin = 1;; ++spin) {
+        if (mbar_try_wait_cluster(bar, parity)) return true;
+        if ((spin & 63) == 0) {
+            if (*abort_flag) return false;
+            if (*reinterpret_cast<volatile int *>(err) != 0) { *abort_flag = 1; return false; }
+            if (clock64() - t0 > kWaitLimitCycles) {
+                *abort_flag = 1;
+                atomicExch(err, kErrWaitTimeout);
+                return false;
+            }
+        }
+    }
+}
+// without regard to the abort flag: before the CTA leaves, what it has in flight has to land
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait_cluster(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+    }
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+            "r"(a), "l"(b), "r"(idesc), "r"(acc)
+            : "memory");
+    else
+        umma_f16_ts(d, a, b, idesc, acc);
+}
+// arrives at the barrier of this CTA (of both CTAs of a pair) when the MMAs issued so far are done
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        umma_commit(bar);
+}
+
+__device__ __forceinline__ uint32_t prmt(uint32_t x, uint32_t y, uint32_t sel) {
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(y), "r"(sel));
+    return d;
+}
+__device__ __forceinline__ uint32_t hsub2(uint32_t x, uint32_t y) {
+    uint32_t d;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y));
+    return d;
+}
+
+template <int REGS> __device__ __forceinline__ void regs_dec() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
+}
+template <int REGS> __device__ __forceinline__ void regs_inc() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS));
+}
+
+__device__ __forceinline__ void put(void *y, int type, long long at, float v) {
+    if (type == HATQ_BF16) reinterpret_cast<__nv_bfloat16 *>(y)[at] = __float2bfloat16_rn(v);
+    else if (type == HATQ_F16) reinterpret_cast<__half *>(y)[at] = __float2half_rn(v);
+    else reinterpret_cast<float *>(y)[at] = v;
+}
+
+template <int T, bool PAIR>
+struct Config {
+    static constexpr int kCtas = PAIR ? 2 : 1;
+    static constexpr int kXBytes = T / kCtas * 128;
+    static constexpr int kStageBytes = kXBytes + kBlockBytes;
+    static constexpr int kFit = 200 * 1024 / kStageBytes;
+    static constexpr int kStages = kFit < 16 ? kFit : 16;
+    static constexpr int kFree = (512 - 2 * T) / 32;                   // 32 columns: one widened block
+    static constexpr int kSlots = kFree < 8 ? kFree : 8;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + (kMaxExperts + 1) * 4 + 64;
+    static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
+    static_assert(kSlots >= 2 && kStages >= kSlots, "a slot's last use is found at its stage's barrier");
+    static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
+};
+
+struct Tile {
+    int e, row, rows, ch;              // expert, first row, rows of the tile, first channel tile
+};
+
+template <int T, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearArgs a) {
+    using C = Config<T, PAIR>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *bar_area = smem + C::kStages * C::kStageBytes;
+    const uint32_t bar0 = smem_addr(bar_area);
+    auto full = [&](int s) { return bar0 + 8u * s; };
+    auto empty = [&](int s) { return bar0 + 8u * (C::kStages + s); };
+    auto wide = [&](int s) { return bar0 + 8u * (2 * C::kStages + s); };
+    auto dfull = [&](int d) { return bar0 + 8u * (3 * C::kStages + d); };
+    auto dempty = [&](int d) { return bar0 + 8u * (3 * C::kStages + 2 + d); };
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (3 * C::kStages + 4));
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    int *tile_start = reinterpret_cast<int *>(bar_area + 1024);
+    __shared__ int warp_sums[kThreads / 32];
+    __shared__ int s_skip;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool clustered = PAIR || a.split > 1;
+    const uint32_t rank = clustered ? cluster_rank() : 0u;
+    const uint32_t in_pair = PAIR ? rank : 0u;
+    const int part = PAIR ? 0 : (int)rank, parts = PAIR ? 1 : a.split;
+
+    if (threadIdx.x == 0) {
+        s_skip = *reinterpret_cast<volatile int *>(a.err);
+        *abort_flag = 0;
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+            mbar_init(wide(s), 4 * C::kCtas);
+        }
+        for (int d = 0; d < 2; ++d) {
+            mbar_init(dfull(d), 1);
+            mbar_init(dempty(d), 8 * C::kCtas);
+        }
+        fence_barrier_init();
+    }
+    if (warp == 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_holder)),
+                         "r"(512)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_holder)),
+                         "r"(512)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    // token tiles before each expert's: two experts per thread, then the warps' sums
+    if (a.offsets) {
+        int c[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = 2 * threadIdx.x + i;
+            c[i] = 0;
+            if (e < a.experts) {
+                const int lo = min(max(a.offsets[e], 0), a.rows), hi = min(max(a.offsets[e + 1], 0), a.rows);
+                c[i] = hi > lo ? (hi - lo + T - 1) / T : 0;
+            }
+        }
+        int sum = c[0] + c[1];
+        for (int m = 1; m < 32; m <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, sum, m);
+            if (lane >= m) sum += o;
+        }
+        if (lane == 31) warp_sums[warp] = sum;
+        __syncthreads();
+        int before = sum - c[0] - c[1];
+        for (int w = 0; w < warp; ++w) before += warp_sums[w];
+        if (2 * threadIdx.x < a.experts) tile_start[2 * threadIdx.x + 1] = before + c[0];
+        if (2 * threadIdx.x + 1 < a.experts) tile_start[2 * threadIdx.x + 2] = before + c[0] + c[1];
+        if (threadIdx.x == 0) tile_start[0] = 0;
+    } else if (threadIdx.x == 0) {
+        tile_start[0] = 0;
+        tile_start[1] = (a.rows + T - 1) / T;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (clustered) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;
+    const bool skip = s_skip != 0;
+
+    const int pairs_n = (a.n_tiles + C::kCtas - 1) / C::kCtas;          // channel tiles of a cluster
+    const int total = skip ? 0 : tile_start[a.experts] * pairs_n;
+    const int per = PAIR ? 2 : a.split;
+    const int first = (int)blockIdx.x / per, step = (int)gridDim.x / per;
+    const int kb0 = (int)((long long)a.kb * part / parts), kb1 = (int)((long long)a.kb * (part + 1) / parts);
+
+    auto decode = [&](int t) {
+        int lo = 0, hi = a.experts;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (tile_start[mid] * pairs_n <= t) lo = mid;
+            else hi = mid;
+        }
+        const int tokens = tile_start[lo + 1] - tile_start[lo];
+        const int local = t - tile_start[lo] * pairs_n;
+        const int sweep = local / (kRasterN * tokens), rest = local - sweep * kRasterN * tokens;
+        const int width = min(kRasterN, pairs_n - sweep * kRasterN);
+        const int mt = rest / width;
+        int r0 = 0, r1 = a.rows;
+        if (a.offsets) {
+            r0 = min(max(a.offsets[lo], 0), a.rows);
+            r1 = min(max(a.offsets[lo + 1], 0), a.rows);
+        }
+        Tile tile;
+        tile.e = lo;
+        tile.row = r0 + mt * T;
+        tile.rows = min(T, r1 - tile.row);
+        tile.ch = (sweep * kRasterN + rest - mt * width) * C::kCtas;
+        return tile;
+    };
+    // 64-code blocks of an exact fp32 window of this expert
+    auto window = [&](int e) {
+        const int bits = a.windows[e];
+        int j = 6;
+        while (j > 0 && (bits >> j & 1)) --j;
+        return 16 << j;
+    };
+
+    bool ok = true;
+    if (warp < 4) {
+        regs_dec<kRegsIssue>();
+        if (warp == 0 && lane == 0) {
+            int it = 0;
+            for (int t = first; t < total && ok; t += step) {
+                const Tile tile = decode(t);
+                // a pair's second half may lie behind the last channel tile: any block does, nothing of it is stored
+                const int ct = min(tile.ch + (int)in_pair, a.n_tiles - 1);
+                const uint8_t *w = a.w + ((long long)tile.e * a.n_tiles + ct) * a.kb * kBlockBytes;
+                const int row = tile.row + (int)in_pair * (T / C::kCtas);
+                for (int b = kb0; b < kb1; ++b, ++it) {
+                    const int s = it % C::kStages;
+                    ok = mbar_wait_cluster(empty(s), (uint32_t)((it / C::kStages) & 1) ^ 1u, abort_flag, a.err);
+                    if (!ok) break;
+                    const uint32_t st = smem_addr(smem + s * C::kStageBytes);
+                    mbar_expect_tx(full(s), C::kStageBytes);
+                    bulk_load(st + C::kXBytes, w + (long long)b * kBlockBytes, kBlockBytes, full(s));
+                    tma_load_2d(st, &tmX, full(s), b * 64, row);
+                }
+            }
+            if (!ok)
+                for (int i = max(0, it - C::kStages); i < it; ++i) mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
+        } else if (warp == 1 && lane == 0 && in_pair == 0) {
+            const uint32_t idesc = (1u << 4) | ((uint32_t)(T >> 3) << 17) | ((uint32_t)(C::kCtas * 128 >> 4) << 24);
+            int it = 0, cc = 0;
+            for (int t = first; t < total && ok; t += step) {
+                const int win = window(decode(t).e);
+                uint32_t acc = 0, d = 0;
+                for (int b = kb0; b < kb1; ++b, ++it) {
+                    if (acc == 0) {
+                        ok = mbar_wait_cluster(dempty(cc & 1), (uint32_t)((cc >> 1) & 1) ^ 1u, abort_flag, a.err);
+                        if (!ok) break;
+                        d = tmem + (uint32_t)((cc & 1) * T);
+                    }
+                    const int s = it % C::kStages;
+                    const uint32_t ph = (uint32_t)((it / C::kStages) & 1);
+                    ok = mbar_wait_cluster(full(s), ph, abort_flag, a.err) && mbar_wait_cluster(wide(s), ph, abort_flag, a.err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t bd = sdesc_sw128(smem_addr(smem + s * C::kStageBytes));
+                    const uint32_t at = tmem + (uint32_t)(2 * T + (it % C::kSlots) * 32);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_ts<PAIR>(d, at + 8 * q, bd + 2 * q, idesc, acc | (uint32_t)q);
+                    commit<PAIR>(empty(s));
+                    acc = 1;
+                    if (b + 1 == kb1 || (b + 1) % win == 0) {
+                        commit<PAIR>(dfull(cc & 1));
+                        ++cc;
+                        acc = 0;
+                    }
+                }
+            }
+            if (!ok && it > 0) mbar_drain(empty((it - 1) % C::kStages), (uint32_t)(((it - 1) / C::kStages) & 1));
+        }
+        __syncwarp();
+        if (!PAIR && parts > 1) {
+            cluster_sync();
+            cluster_sync();
+        }
+    } else if (warp < 12) {
+        regs_dec<kRegsWiden>();
+        const int set = (warp >> 2) - 1;                                // takes the blocks with it % 2 == set
+        const int m = (warp & 3) * 32 + lane;                           // channel of the tile = tensor-memory lane
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T;
+        int it = 0;
+        for (int t = first; t < total && ok; t += step) {
+            for (int b = kb0; b < kb1; ++b, ++it) {
+                if ((it & 1) != set) continue;
+                const int s = it % C::kStages;
+                ok = mbar_wait_cluster(full(s), (uint32_t)((it / C::kStages) & 1), abort_flag, a.err);
+                if (ok && it >= C::kSlots) {
+                    const int p = it - C::kSlots;                       // the slot's last user
+                    ok = mbar_wait_cluster(empty(p % C::kStages), (uint32_t)((p / C::kStages) & 1), abort_flag, a.err);
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint8_t *src = smem + s * C::kStageBytes + C::kXBytes + m * 16;
+                uint32_t h[32];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + j * 2048);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        h[8 * j + 2 * q] = hsub2(prmt(w[q], 0x64646464u, 0x4140u), 0x64806480u);
+                        h[8 * j + 2 * q + 1] = hsub2(prmt(w[q], 0x64646464u, 0x4342u), 0x64806480u);
+                    }
+                }
+                tc_fence_after();
+                tmem_st32(t_lane + (uint32_t)((it % C::kSlots) * 32), h);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_remote(map_shared(wide(s), 0));
+                    else mbar_arrive(wide(s));
+                }
+            }
+        }
+        __syncwarp();
+        if (!PAIR && parts > 1) {
+            cluster_sync();
+            cluster_sync();
+        }
+    } else {
+        regs_inc<kRegsOut>();
+        constexpr int kHalf = T / 2;
+        const int half = (warp >> 2) - 3;
+        const int m = (warp & 3) * 32 + lane;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kHalf);
+        int cc = 0;
+        auto release = [&](int d) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_remote(map_shared(dempty(d), 0));
+                else mbar_arrive(dempty(d));
+            }
+        };
+        for (int t = first; t < total && ok; t += step) {
+            const Tile tile = decode(t);
+            const int win = window(tile.e);
+            const int ch = (tile.ch + (int)in_pair) * kRowTile + m;
+            const bool live = ch < a.n;
+            const float sw = live ? a.s_w[(long long)tile.e * a.n + ch] : 0.0f;
+            const float bias = live && a.bias ? a.bias[(long long)tile.e * a.n + ch] : 0.0f;
+            const int chunks = (kb1 - 1) / win - kb0 / win + 1;
+            // 16 tokens' values of this channel, c0 the first one's column
+            auto emit = [&](const float (&v)[16], int c0) {
+                const int c = c0 + (lane & 15);
+                const float mine = c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
+                long long at = (long long)(tile.row + c0) * a.ldy + ch;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float sx = __shfl_sync(0xffffffffu, mine, i);
+                    const float r = v[i] * sw * sx;
+                    if (live && c0 + i < tile.rows) put(a.y, a.y_type, at, a.bias ? r + bias : r);
+                    at += a.ldy;
+                }
+            };
+            if (chunks == 1 && parts == 1) {
+                ok = mbar_wait_cluster(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int g = 0; g < kHalf; g += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(t_lane + (uint32_t)((cc & 1) * T + g), r);
+                    tmem_wait_ld();
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+                    emit(v, half * kHalf + g);
+                }
+                release(cc & 1);
+                ++cc;
+            } else {
+                int acc[kHalf];
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) acc[i] = 0;
+                for (int q = 0; q < chunks; ++q, ++cc) {
+                    ok = mbar_wait_cluster(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int g = 0; g < kHalf; g += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(t_lane + (uint32_t)((cc & 1) * T + g), r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[g + i] += __float2int_rn(__uint_as_float(r[i]));
+                    }
+                    release(cc & 1);
+                }
+                if (!ok) break;
+                if (parts == 1) {
+#pragma unroll
+                    for (int g = 0; g < kHalf; g += 16) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = (float)acc[g + i];
+                        emit(v, half * kHalf + g);
+                    }
+                } else {
+                    // every MMA of this CTA is done: the stages hold its sums, [token][channel]
+                    int *sums = reinterpret_cast<int *>(smem);
+#pragma unroll
+                    for (int i = 0; i < kHalf; ++i) sums[(half * kHalf + i) * kRowTile + m] = acc[i];
+                }
+            }
+        }
+        __syncwarp();
+        if (!PAIR && parts > 1) {
+            cluster_sync();
+            if (ok && first < total) {
+                const Tile tile = decode(first);
+                const int ch = tile.ch * kRowTile + m;
+                if (ch < a.n) {
+                    const float sw = a.s_w[(long long)tile.e * a.n + ch];
+                    const float bias = a.bias ? a.bias[(long long)tile.e * a.n + ch] : 0.0f;
+                    const uint32_t mine = smem_addr(smem) + 4u * (uint32_t)m;
+                    for (int c = part + parts * half; c < tile.rows; c += 2 * parts) {
+                        int sum = 0;
+                        for (int q = 0; q < parts; ++q) {
+                            int v;
+                            asm volatile("ld.shared::cluster.s32 %0, [%1];"
+                                         : "=r"(v)
+                                         : "r"(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q)));
+                            sum += v;
+                        }
+                        float r = (float)sum * sw * a.s_x[tile.row + c];
+                        if (a.bias) r += bias;
+                        put(a.y, a.y_type, (long long)(tile.row + c) * a.ldy + ch, r);
+                    }
+                }
+            }
+            cluster_sync();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();
+    tc_fence_after();
+    if (warp == 1) {
+        if (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+template <int T, bool PAIR>
+cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cudaStream_t s) {
+    using C = Config<T, PAIR>;
+    // the roles' register shares have to fit what the launch brings, or the increase would wait for ever
+    static const int regs = [] {
+        cudaFuncAttributes fa{};
+        return cudaFuncGetAttributes(&fa, linear_tc_kernel<T, PAIR>) == cudaSuccess ? fa.numRegs : 0;
+    }();
+    if (regs * kThreads < kRegShares * 128) return cudaErrorInvalidConfiguration;
+    cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) return e;
+    const int width = PAIR ? 2 : a.split;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * width));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)width;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = width > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, linear_tc_kernel<T, PAIR>, tm, a);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
+                             cudaStream_t s) {
+    if (pair) return tile == 192 ? launch<192, true>(tm, a, clusters, s) : launch<224, true>(tm, a, clusters, s);
+    switch (tile) {
+        case 32: return launch<32, false>(tm, a, clusters, s);
+        case 64: return launch<64, false>(tm, a, clusters, s);
+        default: return launch<128, false>(tm, a, clusters, s);
+    }
+}
+
+}  // namespace hatq

@@ -1,0 +1,74 @@
+// Internal interface of the token operators (quantize_tokens, linear,
+// grouped_linear, combine_rows) between the host side (hatq_tokens_api.cu) and
+// the kernels. Not part of the public ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "hatq.h"
+
+namespace hatq {
+
+constexpr int kRowTile = 128;          // output channels per block of the weight layout
+constexpr int kBlockBytes = 8192;      // one block: 128 channels x 64 codes
+constexpr int kMaxExperts = 1024;
+constexpr int kMaxTokenWidth = 32768;  // values per row of quantize_tokens
+constexpr int kMaxDepth = 65536;       // reduction length of a product: 128 * 128 * 65536 < 2^31
+
+struct TokenQuantArgs {
+    const void *x;
+    long long ldx, src_rows;
+    const int32_t *index;
+    long long rows;
+    int c, hb, act, gated;
+    float inv_norm;                    // 1 / sqrt(hb)
+    void *codes;
+    long long ldc;
+    float *scales;
+};
+cudaError_t launch_quantize_tokens(const TokenQuantArgs &a, int x_type, int format, bool vec, cudaStream_t s);
+
+cudaError_t launch_linear_layout(const int8_t *w, long long ldw, int experts, int n, int k, uint8_t *codes,
+                                 int32_t *windows, cudaStream_t s);
+// codes of either format and any pitch -> fp16 codes [rows][k_pad], zero behind k
+cudaError_t launch_pack_codes(const void *x, int format, long long ldx, long long rows, int k, int k_pad, void *out,
+                              cudaStream_t s);
+
+struct LinearArgs {
+    const void *x;                     // codes
+    int format;
+    long long ldx;
+    const float *s_x;
+    int rows;
+    const int32_t *offsets;            // [experts + 1], or null: one group of all rows
+    int experts, n, k, kb;             // kb: 64-wide blocks of the reduction
+    int n_tiles;                       // 128-channel tiles
+    const uint8_t *w;
+    const float *s_w, *bias;
+    const int32_t *windows;
+    void *y;
+    long long ldy;
+    int y_type;
+    int split;                         // CTAs of a cluster that share one tile's reduction
+    int slots;                         // one-token kernel: groups the grid has room for
+    int *err;
+};
+// few rows per group: integer dot products on the CUDA cores
+cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s);
+// the tensor-core kernel; tile: tokens per tile, pair: two CTAs per tile
+cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
+                             cudaStream_t s);
+
+cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
+                                const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
+                                bool vec, cudaStream_t s);
+
+// host services of hatq_api.cu
+int *device_error_word();
+CUresult encode_tiled_2d(CUtensorMap *tm, CUtensorMapDataType type, const void *base, unsigned long long inner,
+                         unsigned long long outer, unsigned long long pitch_bytes, unsigned box_inner,
+                         unsigned box_outer);
+
+}  // namespace hatq

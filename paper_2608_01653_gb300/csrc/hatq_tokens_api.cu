@@ -1,0 +1,304 @@
+// Host side of the token operators: argument checks and the choice of kernel.
+#include <cstdarg>
+#include <cstdio>
+#include <climits>
+#include <cmath>
+
+#include "hatq_internal.h"
+#include "hatq_tokens.h"
+
+namespace {
+
+using hatq::LinearArgs;
+
+hatq_status fail(hatq_status st, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return hatq::report(st, buf);
+}
+hatq_status cuda_fail(cudaError_t e, const char *what) {
+    return fail(HATQ_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+size_t type_size(int t) { return t == HATQ_F32 ? 4 : 2; }
+bool is_type(int t) { return t == HATQ_F32 || t == HATQ_F16 || t == HATQ_BF16; }
+size_t codes_size(int f) { return f == HATQ_CODES_F16 ? 2 : 1; }
+bool is_codes(int f) { return f == HATQ_CODES_I8 || f == HATQ_CODES_F16; }
+int round_up(int v, int m) { return (v + m - 1) / m * m; }
+
+// bytes of rows x width elements at a pitch, as far as they are touched
+bool overlap(const void *p, long long p_rows, long long p_pitch, long long p_width, size_t p_size, const void *q,
+             long long q_rows, long long q_pitch, long long q_width, size_t q_size) {
+    if (p_rows == 0 || q_rows == 0) return false;
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), q0 = reinterpret_cast<uintptr_t>(q);
+    const uintptr_t p1 = p0 + (uintptr_t)((p_rows - 1) * p_pitch + p_width) * p_size;
+    const uintptr_t q1 = q0 + (uintptr_t)((q_rows - 1) * q_pitch + q_width) * q_size;
+    return p0 < q1 && q0 < p1;
+}
+
+constexpr long long kMaxRows = (1LL << 31) - 1024;
+constexpr long long kMaxPitch = 1LL << 32;
+
+struct Plan {
+    bool few;        // the dot-product kernel
+    int tokens;      // rows per pass of it, or per tile of the tensor-core kernel
+    bool pair;
+};
+
+// Which kernel: see hatq_tokens.cu and hatq_linear.cu for both.
+Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped) {
+    Plan p{};
+    const int k_pad = round_up(L->k, 64);
+    const int tokens = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    p.few = rows <= 8 && tokens * k_pad <= 96 * 1024;
+    if (p.few) {
+        p.tokens = tokens;
+        return p;
+    }
+    const long long per = grouped ? (rows + L->experts - 1) / L->experts : rows;
+    p.tokens = per <= 32 ? 32 : per <= 64 ? 64 : 128;
+    return p;
+}
+
+int sm_count() {
+    static int counts[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (!counts[dev]) {
+        int v = 0;
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        counts[dev] = v;
+    }
+    return counts[dev];
+}
+
+hatq_status check_weights(const hatq_linear_weights *L) {
+    if (!L) return fail(HATQ_ERR_INVALID_ARG, "null weights");
+    if (L->experts < 1 || L->experts > hatq::kMaxExperts)
+        return fail(HATQ_ERR_INVALID_ARG, "experts must be in 1..%d", hatq::kMaxExperts);
+    if (L->n < 1 || L->k < 1) return fail(HATQ_ERR_INVALID_ARG, "n and k must be positive");
+    if (L->k > hatq::kMaxDepth) return fail(HATQ_ERR_UNSUPPORTED, "k must be at most %d", hatq::kMaxDepth);
+    if ((long long)L->experts * ((L->n + 127LL) / 128) > (1LL << 30))
+        return fail(HATQ_ERR_UNSUPPORTED, "too many output channels");
+    return HATQ_OK;
+}
+
+// where x can go to the tensor cores as it lies: fp16 at a pitch and a base that TMA takes
+bool direct(const void *x, int format, long long ldx) {
+    return format == HATQ_CODES_F16 && ldx % 8 == 0 && aligned(x, 16);
+}
+
+hatq_status workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L,
+                         bool grouped, size_t *bytes) {
+    const Plan p = plan_of(rows, L, grouped);
+    *bytes = rows == 0 || p.few || direct(x, format, ldx) ? 0 : (size_t)rows * (size_t)round_up(L->k, 64) * 2;
+    return HATQ_OK;
+}
+
+hatq_status product(const void *x, int format, long long ldx, const float *s_x, long long rows, const int32_t *offsets,
+                    bool grouped, const hatq_linear_weights *L, int y_type, void *y, long long ldy, void *workspace,
+                    size_t workspace_bytes, hatq_stream stream) {
+    const hatq_status st = check_weights(L);
+    if (st != HATQ_OK) return st;
+    if (!is_codes(format)) return fail(HATQ_ERR_INVALID_ARG, "unknown code format %d", format);
+    if (!is_type(y_type)) return fail(HATQ_ERR_INVALID_ARG, "unknown output type %d", y_type);
+    if (rows < 0) return fail(HATQ_ERR_INVALID_ARG, "negative row count");
+    if (rows > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows per call");
+    if (ldx < L->k || ldy < L->n) return fail(HATQ_ERR_INVALID_ARG, "a pitch is smaller than its row");
+    if (ldx > kMaxPitch || ldy > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
+    if (!grouped && L->experts != 1) return fail(HATQ_ERR_INVALID_ARG, "a layer with experts needs hatq_grouped_linear");
+    if (rows == 0) return HATQ_OK;
+    if (!x || !s_x || !y || !L->codes || !L->windows || !L->s_w || (grouped && !offsets))
+        return fail(HATQ_ERR_INVALID_ARG, "null tensor");
+    if (!aligned(L->codes, 16)) return fail(HATQ_ERR_INVALID_ARG, "the weight codes must be 16-byte aligned");
+    if (!aligned(x, codes_size(format)) || !aligned(y, type_size(y_type)) || !aligned(s_x, 4) || !aligned(L->s_w, 4) ||
+        !aligned(L->bias, 4) || !aligned(L->windows, 4) || !aligned(offsets, 4))
+        return fail(HATQ_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+    if (overlap(x, rows, ldx, L->k, codes_size(format), y, rows, ldy, L->n, type_size(y_type)))
+        return fail(HATQ_ERR_INVALID_ARG, "x and y overlap");
+    const int sms = sm_count();
+    LinearArgs a{};
+    a.err = hatq::device_error_word();
+    if (!sms || !a.err) return fail(HATQ_ERR_CUDA, "no CUDA device");
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    a.x = x;
+    a.format = format;
+    a.ldx = ldx;
+    a.s_x = s_x;
+    a.rows = (int)rows;
+    a.offsets = offsets;
+    a.experts = L->experts;
+    a.n = L->n;
+    a.k = L->k;
+    a.kb = (L->k + 63) / 64;
+    a.n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
+    a.w = L->codes;
+    a.s_w = L->s_w;
+    a.bias = L->bias;
+    a.windows = L->windows;
+    a.y = y;
+    a.ldy = ldy;
+    a.y_type = y_type;
+    a.split = 1;
+    a.slots = (int)(rows < L->experts ? rows : L->experts);
+    const Plan p = plan_of(rows, L, grouped);
+    cudaError_t e;
+    if (p.few) {
+        if ((e = hatq::launch_linear_few(a, p.tokens, s)) != cudaSuccess) return cuda_fail(e, "product launch");
+        return HATQ_OK;
+    }
+    if (!direct(x, format, ldx)) {
+        size_t need = 0;
+        workspace_of(x, format, ldx, rows, L, grouped, &need);
+        if (!workspace || workspace_bytes < need)
+            return fail(HATQ_ERR_INVALID_ARG, "the product needs a workspace of %zu bytes", need);
+        if (!aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+        if ((e = hatq::launch_pack_codes(x, format, ldx, rows, L->k, a.kb * 64, workspace, s)) != cudaSuccess)
+            return cuda_fail(e, "code packing launch");
+        a.x = workspace;
+        a.ldx = a.kb * 64;
+        a.format = HATQ_CODES_F16;
+    }
+    const int ctas = p.pair ? 2 : 1;
+    const long long token_tiles = (rows + p.tokens - 1) / p.tokens + (grouped ? a.slots : 0);
+    const long long tiles = token_tiles * ((a.n_tiles + ctas - 1) / ctas);
+    if (tiles > INT_MAX / 2) return fail(HATQ_ERR_UNSUPPORTED, "too many output tiles");
+    CUtensorMap tm;
+    const CUresult r = hatq::encode_tiled_2d(&tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, (unsigned long long)a.k,
+                                             (unsigned long long)rows, (unsigned long long)a.ldx * 2, 64,
+                                             (unsigned)(p.tokens / ctas));
+    if (r != CUDA_SUCCESS) return fail(HATQ_ERR_CUDA, "code tensor map encoding failed (%d)", (int)r);
+    if (!p.pair)
+        while (a.split < 8 && tiles * a.split * 2 <= sms && a.kb / (a.split * 2) >= 4) a.split *= 2;
+    const int room = sms / (p.pair ? 2 : 1);
+    const int clusters = a.split > 1 ? (int)tiles : (int)(tiles < room ? tiles : room);
+    if ((e = hatq::launch_linear_tc(tm, a, p.tokens, p.pair, clusters, s)) != cudaSuccess)
+        return cuda_fail(e, "product launch");
+    return HATQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hatq_status hatq_quantize_tokens(const void *x, int x_type, long long ldx, long long src_rows, const int32_t *index,
+                                 long long rows, int c, int hb, int act, int gated, int format, void *codes,
+                                 long long ldc, float *scales, hatq_stream stream) {
+    if (!is_type(x_type)) return fail(HATQ_ERR_INVALID_ARG, "unknown input type %d", x_type);
+    if (!is_codes(format)) return fail(HATQ_ERR_INVALID_ARG, "unknown code format %d", format);
+    if (act < HATQ_ACT_NONE || act > HATQ_ACT_GELU) return fail(HATQ_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (gated != 0 && gated != 1) return fail(HATQ_ERR_INVALID_ARG, "gated is 0 or 1");
+    if (rows < 0 || src_rows < 0 || c < 1) return fail(HATQ_ERR_INVALID_ARG, "negative or empty shape");
+    if (c > hatq::kMaxTokenWidth) return fail(HATQ_ERR_UNSUPPORTED, "at most %d values per row", hatq::kMaxTokenWidth);
+    if (rows > kMaxRows || src_rows > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows per call");
+    if (hb < 1 || hb > 256 || (hb & (hb - 1)) || c % hb)
+        return fail(HATQ_ERR_INVALID_ARG, "hb must be a power of two <= 256 that divides c");
+    const long long width = (long long)c * (gated ? 2 : 1);
+    if (ldx < width || ldc < c) return fail(HATQ_ERR_INVALID_ARG, "a pitch is smaller than its row");
+    if (ldx > kMaxPitch || ldc > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
+    if (!index && src_rows < rows) return fail(HATQ_ERR_INVALID_ARG, "fewer source rows than rows and no index");
+    if (rows == 0) return HATQ_OK;
+    if ((!x && src_rows > 0) || !codes || !scales) return fail(HATQ_ERR_INVALID_ARG, "null tensor");
+    const size_t xs = type_size(x_type), cs = codes_size(format);
+    if (!aligned(x, xs) || !aligned(codes, cs) || !aligned(scales, 4) || !aligned(index, 4))
+        return fail(HATQ_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+    if (overlap(x, src_rows, ldx, width, xs, codes, rows, ldc, c, cs))
+        return fail(HATQ_ERR_INVALID_ARG, "x and codes overlap");
+    hatq::TokenQuantArgs a{};
+    a.x = x;
+    a.ldx = ldx;
+    a.src_rows = src_rows;
+    a.index = index;
+    a.rows = rows;
+    a.c = c;
+    a.hb = hb;
+    a.act = act;
+    a.gated = gated;
+    a.inv_norm = (float)(1.0 / std::sqrt((double)hb));
+    a.codes = codes;
+    a.ldc = ldc;
+    a.scales = scales;
+    const bool vec = aligned(x, 16) && ldx * xs % 16 == 0 && (!gated || (size_t)c * xs % 16 == 0) && aligned(codes, 16) &&
+                     ldc * cs % 16 == 0;
+    const cudaError_t e = hatq::launch_quantize_tokens(a, x_type, format, vec, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "token quantization launch");
+}
+
+hatq_status hatq_linear_sizes(int experts, int n, int k, size_t *code_bytes) {
+    hatq_linear_weights L{};
+    L.experts = experts;
+    L.n = n;
+    L.k = k;
+    const hatq_status st = check_weights(&L);
+    if (st != HATQ_OK) return st;
+    if (!code_bytes) return fail(HATQ_ERR_INVALID_ARG, "null output");
+    *code_bytes = (size_t)experts * ((size_t)(n + 127) / 128 * 128) * (size_t)round_up(k, 64);
+    return HATQ_OK;
+}
+
+hatq_status hatq_linear_layout(const int8_t *w, long long ldw, const hatq_linear_weights *L, hatq_stream stream) {
+    const hatq_status st = check_weights(L);
+    if (st != HATQ_OK) return st;
+    if (ldw < L->k) return fail(HATQ_ERR_INVALID_ARG, "a pitch is smaller than its row");
+    if (ldw > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
+    if (!w || !L->codes || !L->windows) return fail(HATQ_ERR_INVALID_ARG, "null tensor");
+    if (!aligned(L->codes, 16) || !aligned(L->windows, 4))
+        return fail(HATQ_ERR_INVALID_ARG, "the weight codes must be 16-byte aligned");
+    const cudaError_t e = hatq::launch_linear_layout(w, ldw, L->experts, L->n, L->k, L->codes, L->windows,
+                                                     reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "weight layout launch");
+}
+
+hatq_status hatq_linear_workspace(const void *x, int format, long long ldx, long long rows,
+                                  const hatq_linear_weights *L, size_t *bytes) {
+    const hatq_status st = check_weights(L);
+    if (st != HATQ_OK) return st;
+    if (!bytes) return fail(HATQ_ERR_INVALID_ARG, "null output");
+    if (!is_codes(format)) return fail(HATQ_ERR_INVALID_ARG, "unknown code format %d", format);
+    if (rows < 0) return fail(HATQ_ERR_INVALID_ARG, "negative row count");
+    // the larger of what the dense and the grouped product want
+    size_t dense = 0, grouped = 0;
+    workspace_of(x, format, ldx, rows, L, false, &dense);
+    workspace_of(x, format, ldx, rows, L, true, &grouped);
+    *bytes = dense > grouped ? dense : grouped;
+    return HATQ_OK;
+}
+
+hatq_status hatq_linear(const void *x, int format, long long ldx, const float *s_x, long long rows,
+                        const hatq_linear_weights *L, int y_type, void *y, long long ldy, void *workspace,
+                        size_t workspace_bytes, hatq_stream stream) {
+    return product(x, format, ldx, s_x, rows, nullptr, false, L, y_type, y, ldy, workspace, workspace_bytes, stream);
+}
+
+hatq_status hatq_grouped_linear(const void *x, int format, long long ldx, const float *s_x, long long rows,
+                                const int32_t *offsets, const hatq_linear_weights *L, int y_type, void *y,
+                                long long ldy, void *workspace, size_t workspace_bytes, hatq_stream stream) {
+    return product(x, format, ldx, s_x, rows, offsets, true, L, y_type, y, ldy, workspace, workspace_bytes, stream);
+}
+
+hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
+                              const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
+                              hatq_stream stream) {
+    if (!is_type(type)) return fail(HATQ_ERR_INVALID_ARG, "unknown type %d", type);
+    if (rows < 0 || tokens < 0 || c < 1) return fail(HATQ_ERR_INVALID_ARG, "negative or empty shape");
+    if (topk < 1 || topk > 64) return fail(HATQ_ERR_INVALID_ARG, "topk must be in 1..64");
+    if (rows > kMaxRows || tokens > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows per call");
+    if (ldy < c || ldo < c) return fail(HATQ_ERR_INVALID_ARG, "a pitch is smaller than its row");
+    if (ldy > kMaxPitch || ldo > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
+    if (tokens == 0) return HATQ_OK;
+    if ((!y && rows > 0) || !index || !weights || !out) return fail(HATQ_ERR_INVALID_ARG, "null tensor");
+    const size_t ts = type_size(type);
+    if (!aligned(y, ts) || !aligned(out, ts) || !aligned(index, 4) || !aligned(weights, 4))
+        return fail(HATQ_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+    if (overlap(y, rows, ldy, c, ts, out, tokens, ldo, c, ts)) return fail(HATQ_ERR_INVALID_ARG, "y and out overlap");
+    const bool vec = aligned(y, 16) && aligned(out, 16) && ldy * ts % 16 == 0 && ldo * ts % 16 == 0 && c * ts % 16 == 0;
+    const cudaError_t e = hatq::launch_combine_rows(y, type, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec,
+                                                    reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "combine launch");
+}
+
+}  // extern "C"
