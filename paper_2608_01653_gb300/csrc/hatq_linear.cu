@@ -53,6 +53,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+// One lane of the warp. The issuing warps run their loops with all lanes and pick the lane only around the
+// asynchronous instructions: their operands then stay warp-uniform for the compiler (with the loops under a
+// lane == 0 branch a 64-code block cost about 800 cycles of issue, whatever the tile).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
@@ -61,40 +69,15 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// Arrival at the pair leader's barrier. What it announces is tensor memory, ordered by the tcgen05 fences on
+// both sides; a release and an acquire at cluster scope would add memory barriers to every 64-code block.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-        " selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-// mbar_wait for barriers that the other CTA of a cluster may arrive at
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (uint32_t spin = 1;; ++spin) {
-        if (mbar_try_wait_cluster(bar, parity)) return true;
-        if ((spin & 63) == 0) {
-            if (*abort_flag) return false;
-            if (*reinterpret_cast<volatile int *>(err) != 0) { *abort_flag = 1; return false; }
-            if (clock64() - t0 > kWaitLimitCycles) {
-                *abort_flag = 1;
-                atomicExch(err, kErrWaitTimeout);
-                return false;
-            }
-        }
-    }
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // without regard to the abort flag: before the CTA leaves, what it has in flight has to land
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
-    while (!mbar_try_wait_cluster(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+    while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
     }
 }
 
@@ -154,15 +137,21 @@ __device__ __forceinline__ void put(void *y, int type, long long at, float v) {
 template <int T, bool PAIR>
 struct Config {
     static constexpr int kCtas = PAIR ? 2 : 1;
-    static constexpr int kXBytes = T / kCtas * 128;
-    static constexpr int kStageBytes = kXBytes + kBlockBytes;
+    // 64-code blocks per pipeline stage: with few tokens a block's MMAs are short and its hand-offs count
+    static constexpr int kSub = T / kCtas <= 64 ? 2 : 1;
+    static constexpr int kXBytes = T / kCtas * 128;                    // one block's token codes
+    static constexpr int kWOffset = kSub * kXBytes;
+    static constexpr int kStageBytes = kSub * (kXBytes + kBlockBytes);
     static constexpr int kFit = 200 * 1024 / kStageBytes;
     static constexpr int kStages = kFit < 16 ? kFit : 16;
-    static constexpr int kFree = (512 - 2 * T) / 32;                   // 32 columns: one widened block
-    static constexpr int kSlots = kFree < 8 ? kFree : 8;
+    static constexpr int kSlotCols = 32 * kSub;                        // a widened block takes 32 columns
+    static constexpr int kFree = (512 - 2 * T) / kSlotCols;
+    static constexpr int kSlots = kFree < kStages ? (kFree < 8 ? kFree : 8) : (kStages < 8 ? kStages : 8);
+    // warps that announce a widened stage: one set (the sets take turns) or both (a block each)
+    static constexpr int kWideWarps = (kSub == 2 ? 8 : 4) * kCtas;
     static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + (kMaxExperts + 1) * 4 + 64;
     static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
-    static_assert(kSlots >= 2 && kStages >= kSlots, "a slot's last use is found at its stage's barrier");
+    static_assert(kSlots >= 2 && kStages >= kSlots, "the barrier of a slot's last stage still has that phase");
     static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
 };
 
@@ -189,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ int warp_sums[kThreads / 32];
     __shared__ int s_skip;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const bool clustered = PAIR || a.split > 1;
     const uint32_t rank = clustered ? cluster_rank() : 0u;
     const uint32_t in_pair = PAIR ? rank : 0u;
@@ -201,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            mbar_init(wide(s), 4 * C::kCtas);
+            mbar_init(wide(s), C::kWideWarps);
         }
         for (int d = 0; d < 2; ++d) {
             mbar_init(dfull(d), 1);
@@ -261,7 +250,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int total = skip ? 0 : tile_start[a.experts] * pairs_n;
     const int per = PAIR ? 2 : a.split;
     const int first = (int)blockIdx.x / per, step = (int)gridDim.x / per;
-    const int kb0 = (int)((long long)a.kb * part / parts), kb1 = (int)((long long)a.kb * (part + 1) / parts);
+    // this CTA's blocks of the reduction, whole stages but for the last
+    const int units = (a.kb + C::kSub - 1) / C::kSub;
+    const int kb0 = (int)((long long)units * part / parts) * C::kSub;
+    const int kb1 = min((int)((long long)units * (part + 1) / parts) * C::kSub, a.kb);
 
     auto decode = [&](int t) {
         int lo = 0, hi = a.experts;
@@ -296,59 +288,87 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
 
     bool ok = true;
+    int issued = 0;
+    const uint32_t stage0 = smem_addr(smem);
     if (warp < 4) {
         regs_dec<kRegsIssue>();
-        if (warp == 0 && lane == 0) {
-            int it = 0;
+        if (warp == 0) {
+            int s = 0;
+            uint32_t ph = 1;                                            // parity of the stage's previous release
             for (int t = first; t < total && ok; t += step) {
                 const Tile tile = decode(t);
                 // a pair's second half may lie behind the last channel tile: any block does, nothing of it is stored
                 const int ct = min(tile.ch + (int)in_pair, a.n_tiles - 1);
-                const uint8_t *w = a.w + ((long long)tile.e * a.n_tiles + ct) * a.kb * kBlockBytes;
+                const uint8_t *w = a.w + (((long long)tile.e * a.n_tiles + ct) * a.kb + kb0) * kBlockBytes;
                 const int row = tile.row + (int)in_pair * (T / C::kCtas);
-                for (int b = kb0; b < kb1; ++b, ++it) {
-                    const int s = it % C::kStages;
-                    ok = mbar_wait_cluster(empty(s), (uint32_t)((it / C::kStages) & 1) ^ 1u, abort_flag, a.err);
+                for (int b = kb0; b < kb1; b += C::kSub) {
+                    ok = mbar_wait(empty(s), ph, abort_flag, a.err);
+                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    const uint32_t st = smem_addr(smem + s * C::kStageBytes);
-                    mbar_expect_tx(full(s), C::kStageBytes);
-                    bulk_load(st + C::kXBytes, w + (long long)b * kBlockBytes, kBlockBytes, full(s));
-                    tma_load_2d(st, &tmX, full(s), b * 64, row);
+                    if (elect_one()) {
+                        const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
+                        const bool both = C::kSub == 2 && b + 1 < kb1;
+                        mbar_expect_tx(full(s), both ? C::kStageBytes : C::kXBytes + kBlockBytes);
+                        bulk_load(st + C::kWOffset, w, both ? 2 * kBlockBytes : kBlockBytes, full(s));
+                        tma_load_2d(st, &tmX, full(s), b * 64, row);
+                        if (both) tma_load_2d(st + C::kXBytes, &tmX, full(s), b * 64 + 64, row);
+                    }
+                    __syncwarp();
+                    w += C::kSub * kBlockBytes;
+                    ++issued;
+                    if (++s == C::kStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
                 }
             }
             if (!ok)
-                for (int i = max(0, it - C::kStages); i < it; ++i) mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
-        } else if (warp == 1 && lane == 0 && in_pair == 0) {
+                for (int i = max(0, issued - C::kStages); i < issued; ++i)
+                    mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
+        } else if (warp == 1 && in_pair == 0) {
             const uint32_t idesc = (1u << 4) | ((uint32_t)(T >> 3) << 17) | ((uint32_t)(C::kCtas * 128 >> 4) << 24);
-            int it = 0, cc = 0;
+            const uint64_t bd0 = sdesc_sw128(stage0);
+            int s = 0, slot = 0, cc = 0;
+            uint32_t ph = 0;
             for (int t = first; t < total && ok; t += step) {
                 const int win = window(decode(t).e);
-                uint32_t acc = 0, d = 0;
-                for (int b = kb0; b < kb1; ++b, ++it) {
-                    if (acc == 0) {
-                        ok = mbar_wait_cluster(dempty(cc & 1), (uint32_t)((cc >> 1) & 1) ^ 1u, abort_flag, a.err);
+                for (int b = kb0; b < kb1 && ok;) {
+                    const int end = min(kb1, (b / win + 1) * win);      // one exact window, one accumulator
+                    const int d = cc & 1;
+                    ok = mbar_wait(dempty(d), (uint32_t)((cc >> 1) & 1) ^ 1u, abort_flag, a.err);
+                    ok = __all_sync(0xffffffffu, ok);
+                    uint32_t acc = 0;
+                    for (; b < end && ok; b += C::kSub) {
+                        ok = mbar_wait(full(s), ph, abort_flag, a.err) && mbar_wait(wide(s), ph, abort_flag, a.err);
+                        ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
-                        d = tmem + (uint32_t)((cc & 1) * T);
-                    }
-                    const int s = it % C::kStages;
-                    const uint32_t ph = (uint32_t)((it / C::kStages) & 1);
-                    ok = mbar_wait_cluster(full(s), ph, abort_flag, a.err) && mbar_wait_cluster(wide(s), ph, abort_flag, a.err);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t bd = sdesc_sw128(smem_addr(smem + s * C::kStageBytes));
-                    const uint32_t at = tmem + (uint32_t)(2 * T + (it % C::kSlots) * 32);
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t bd = bd0 + (uint64_t)(s * (C::kStageBytes >> 4));
+                            const uint32_t at = tmem + (uint32_t)(2 * T + slot * C::kSlotCols);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) mma_ts<PAIR>(d, at + 8 * q, bd + 2 * q, idesc, acc | (uint32_t)q);
-                    commit<PAIR>(empty(s));
-                    acc = 1;
-                    if (b + 1 == kb1 || (b + 1) % win == 0) {
-                        commit<PAIR>(dfull(cc & 1));
-                        ++cc;
-                        acc = 0;
+                            for (int q = 0; q < 4; ++q) mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 8 * q, bd + 2 * q, idesc, acc | (uint32_t)q);
+                            if (C::kSub == 2 && b + 1 < end) {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 32 + 8 * q, bd + (C::kXBytes >> 4) + 2 * q, idesc, 1);
+                            }
+                            commit<PAIR>(empty(s));
+                            if (b + C::kSub >= end) commit<PAIR>(dfull(d));
+                        }
+                        __syncwarp();
+                        acc = 1;
+                        ++issued;
+                        if (++slot == C::kSlots) slot = 0;
+                        if (++s == C::kStages) {
+                            s = 0;
+                            ph ^= 1u;
+                        }
                     }
+                    ++cc;
                 }
             }
-            if (!ok && it > 0) mbar_drain(empty((it - 1) % C::kStages), (uint32_t)(((it - 1) / C::kStages) & 1));
+            if (!ok && issued > 0) mbar_drain(empty((issued - 1) % C::kStages), (uint32_t)(((issued - 1) / C::kStages) & 1));
         }
         __syncwarp();
         if (!PAIR && parts > 1) {
@@ -360,19 +380,38 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int set = (warp >> 2) - 1;                                // takes the blocks with it % 2 == set
         const int m = (warp & 3) * 32 + lane;                           // channel of the tile = tensor-memory lane
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T;
-        int it = 0;
-        for (int t = first; t < total && ok; t += step) {
-            for (int b = kb0; b < kb1; ++b, ++it) {
-                if ((it & 1) != set) continue;
-                const int s = it % C::kStages;
-                ok = mbar_wait_cluster(full(s), (uint32_t)((it / C::kStages) & 1), abort_flag, a.err);
-                if (ok && it >= C::kSlots) {
-                    const int p = it - C::kSlots;                       // the slot's last user
-                    ok = mbar_wait_cluster(empty(p % C::kStages), (uint32_t)((p / C::kStages) & 1), abort_flag, a.err);
-                }
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                const uint8_t *src = smem + s * C::kStageBytes + C::kXBytes + m * 16;
+        // One block per stage: this set's stages are it = set, set + 2, ..; two: every stage, and of each this set's
+        // block. ps is the stage that used the slot before, it - kSlots.
+        constexpr int kTurn = C::kSub == 2 ? 1 : 2;
+        auto ahead = [](int &x, uint32_t &phase, int by, int size) {
+            x += by;
+            if (x >= size) {
+                x -= size;
+                phase ^= 1u;
+            }
+        };
+        const int tiles = total > first ? (total - first + step - 1) / step : 0;
+        const int per_tile = (kb1 - kb0 + C::kSub - 1) / C::kSub;
+        const bool odd = C::kSub == 2 && (kb1 - kb0) % 2 != 0;           // a tile's last stage has one block
+        const long long stages = (long long)tiles * per_tile;
+        const int start = C::kSub == 2 ? 0 : set;
+        int s = start, slot = start, ps = C::kSub == 2 ? 0 : (set + C::kSlots) & 1, left = per_tile;
+        uint32_t ph = 0, pph = 0, unused = 0;
+        for (long long it = start; it < stages; it += kTurn) {
+            ok = mbar_wait(full(s), ph, abort_flag, a.err);
+            if (ok && it >= C::kSlots) {
+                ok = mbar_wait(empty(ps), pph, abort_flag, a.err);
+                ahead(ps, pph, kTurn, C::kStages);
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            bool mine = true;
+            if (C::kSub == 2) {
+                mine = !(odd && left == 1 && set == 1);
+                if (--left == 0) left = per_tile;
+            }
+            if (mine) {
+                const uint8_t *src = smem + s * C::kStageBytes + C::kWOffset + (C::kSub == 2 ? set * kBlockBytes : 0) + m * 16;
                 uint32_t h[32];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -385,15 +424,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 tc_fence_after();
-                tmem_st32(t_lane + (uint32_t)((it % C::kSlots) * 32), h);
+                tmem_st32(t_lane + (uint32_t)(slot * C::kSlotCols + (C::kSub == 2 ? set * 32 : 0)), h);
                 tmem_wait_st();
                 tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) mbar_arrive_remote(map_shared(wide(s), 0));
-                    else mbar_arrive(wide(s));
-                }
             }
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_remote(map_shared(wide(s), 0));
+                else mbar_arrive(wide(s));
+            }
+            ahead(s, ph, kTurn, C::kStages);
+            ahead(slot, unused, kTurn, C::kSlots);
         }
         __syncwarp();
         if (!PAIR && parts > 1) {
@@ -437,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             };
             if (chunks == 1 && parts == 1) {
-                ok = mbar_wait_cluster(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
+                ok = mbar_wait(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -458,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int i = 0; i < kHalf; ++i) acc[i] = 0;
                 for (int q = 0; q < chunks; ++q, ++cc) {
-                    ok = mbar_wait_cluster(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
+                    ok = mbar_wait(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_fence_after();
@@ -560,7 +601,7 @@ cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cud
 
 cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
                              cudaStream_t s) {
-    if (pair) return tile == 192 ? launch<192, true>(tm, a, clusters, s) : launch<224, true>(tm, a, clusters, s);
+    if (pair) return tile == 128 ? launch<128, true>(tm, a, clusters, s) : launch<192, true>(tm, a, clusters, s);
     switch (tile) {
         case 32: return launch<32, false>(tm, a, clusters, s);
         case 64: return launch<64, false>(tm, a, clusters, s);

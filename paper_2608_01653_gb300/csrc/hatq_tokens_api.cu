@@ -60,7 +60,8 @@ Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped) {
         return p;
     }
     const long long per = grouped ? (rows + L->experts - 1) / L->experts : rows;
-    p.tokens = per <= 32 ? 32 : per <= 64 ? 64 : 128;
+    p.pair = per > 128;
+    p.tokens = per <= 32 ? 32 : per <= 64 ? 64 : per <= 128 ? 128 : 192;
     return p;
 }
 
