@@ -46,6 +46,7 @@ constexpr int kThreads = 640;
 // registers per thread of the five warpgroups: copies and MMAs, two of converters, two of the epilogue
 constexpr int kRegsIssue = 40, kRegsWiden = 72, kRegsOut = 144;
 constexpr int kRegShares = kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut;
+constexpr int kMaxSplit = 8;           // CTAs of one portable cluster
 constexpr int kRasterN = 8;            // channel tiles that share a sweep over the token tiles
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -81,6 +82,11 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     }
 }
 
+__device__ __forceinline__ int4 load_cluster(uint32_t addr) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(src), "r"(bytes), "r"(bar)
@@ -185,6 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int part = PAIR ? 0 : (int)rank, parts = PAIR ? 1 : a.split;
 
     if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
         s_skip = *reinterpret_cast<volatile int *>(a.err);
         *abort_flag = 0;
         for (int s = 0; s < C::kStages; ++s) {
@@ -241,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (clustered) cluster_sync();
+    if (PAIR) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *tmem_holder;
     const bool skip = s_skip != 0;
@@ -464,18 +471,25 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float sw = live ? a.s_w[(long long)tile.e * a.n + ch] : 0.0f;
             const float bias = live && a.bias ? a.bias[(long long)tile.e * a.n + ch] : 0.0f;
             const int chunks = (kb1 - 1) / win - kb0 / win + 1;
-            // 16 tokens' values of this channel, c0 the first one's column
-            auto emit = [&](const float (&v)[16], int c0) {
-                const int c = c0 + (lane & 15);
-                const float mine = c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
+            // the scales of 16 of this warpgroup's columns, one per lane (twice); asked for a group ahead
+            auto scales_of = [&](int g) {
+                const int c = half * kHalf + g + (lane & 15);
+                return g < kHalf && c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
+            };
+            float sx_now = scales_of(0);
+            // 16 tokens' values of this channel, from column half * kHalf + g
+            auto emit = [&](const float (&v)[16], int g) {
+                const float sx_next = scales_of(g + 16);
+                const int c0 = half * kHalf + g;
                 long long at = (long long)(tile.row + c0) * a.ldy + ch;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float sx = __shfl_sync(0xffffffffu, mine, i);
+                    const float sx = __shfl_sync(0xffffffffu, sx_now, i);
                     const float r = v[i] * sw * sx;
                     if (live && c0 + i < tile.rows) put(a.y, a.y_type, at, a.bias ? r + bias : r);
                     at += a.ldy;
                 }
+                sx_now = sx_next;
             };
             if (chunks == 1 && parts == 1) {
                 ok = mbar_wait(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
@@ -490,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-                    emit(v, half * kHalf + g);
+                    emit(v, g);
                 }
                 release(cc & 1);
                 ++cc;
@@ -520,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         float v[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] = (float)acc[g + i];
-                        emit(v, half * kHalf + g);
+                        emit(v, g);
                     }
                 } else {
                     // every MMA of this CTA is done: the stages hold its sums, [token][channel]
@@ -534,24 +548,39 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!PAIR && parts > 1) {
             cluster_sync();
             if (ok && first < total) {
+                // this CTA finishes every parts-th token: a warp takes a token, a lane four channels, the parts'
+                // sums all loaded before the first is added
                 const Tile tile = decode(first);
-                const int ch = tile.ch * kRowTile + m;
-                if (ch < a.n) {
-                    const float sw = a.s_w[(long long)tile.e * a.n + ch];
-                    const float bias = a.bias ? a.bias[(long long)tile.e * a.n + ch] : 0.0f;
-                    const uint32_t mine = smem_addr(smem) + 4u * (uint32_t)m;
-                    for (int c = part + parts * half; c < tile.rows; c += 2 * parts) {
-                        int sum = 0;
-                        for (int q = 0; q < parts; ++q) {
-                            int v;
-                            asm volatile("ld.shared::cluster.s32 %0, [%1];"
-                                         : "=r"(v)
-                                         : "r"(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q)));
-                            sum += v;
+                const int ch = tile.ch * kRowTile + 4 * lane;
+                float sw[4], bias[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool live = ch + i < a.n;
+                    sw[i] = live ? a.s_w[(long long)tile.e * a.n + ch + i] : 0.0f;
+                    bias[i] = live && a.bias ? a.bias[(long long)tile.e * a.n + ch + i] : 0.0f;
+                }
+                const uint32_t mine = smem_addr(smem) + 16u * (uint32_t)lane;
+                for (int c = part + parts * (warp - 12); c < tile.rows; c += 8 * parts) {
+                    int4 v[kMaxSplit];
+#pragma unroll
+                    for (int q = 0; q < kMaxSplit; ++q)
+                        if (q < parts) v[q] = load_cluster(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q));
+                    const float sx = a.s_x[tile.row + c];
+                    int4 sum = v[0];
+#pragma unroll
+                    for (int q = 1; q < kMaxSplit; ++q)
+                        if (q < parts) {
+                            sum.x += v[q].x;
+                            sum.y += v[q].y;
+                            sum.z += v[q].z;
+                            sum.w += v[q].w;
                         }
-                        float r = (float)sum * sw * a.s_x[tile.row + c];
-                        if (a.bias) r += bias;
-                        put(a.y, a.y_type, (long long)(tile.row + c) * a.ldy + ch, r);
+                    const int part4[4] = {sum.x, sum.y, sum.z, sum.w};
+                    const long long at = (long long)(tile.row + c) * a.ldy + ch;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float r = (float)part4[i] * sw[i] * sx;
+                        if (ch + i < a.n) put(a.y, a.y_type, at + i, a.bias ? r + bias[i] : r);
                     }
                 }
             }

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include <climits>
+#include <type_traits>
 
 #include "hatq_tokens.h"
 
@@ -20,171 +21,463 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// max that keeps a NaN
-__device__ __forceinline__ float max_nan(float a, float b) {
+// max of the magnitudes that keeps a NaN
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// two fp32 values in one register pair: one instruction for both, each rounded as alone
+using pair32 = unsigned long long;
+__device__ __forceinline__ pair32 pack2(float a, float b) {
+    pair32 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(pair32 v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ pair32 add2(pair32 a, pair32 b) {
+    pair32 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ pair32 sub2(pair32 a, pair32 b) {
+    pair32 r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ pair32 fma2(pair32 a, pair32 b, pair32 c) {
+    pair32 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 
 // ------------------------------------------------------------ quantize_tokens
 //
 // u = act(x) (times the row's second half where gated), t = H~_hb u,
-// a = max |t|, code = clamp(rint(t * min(127 / a, 2^126))), scale =
-// max(a / 127, 2^-126) / sqrt(hb). fp32 throughout, one rounding to the code.
+// a = max |t|, code = round(t * min(127 / a, 2^126)), scale =
+// max(a / 127, 2^-126) / sqrt(hb). fp32 throughout, one rounding to the code;
+// |t| (127 / a) stays below 127.5, so nothing has to be clamped.
+//
+// Memory-bound: bytes of x and codes. Two kernels:
+//  * many rows: CTAs stay and walk the rows. A thread owns 32 consecutive
+//    values, so that blocks up to 32 are transformed without leaving the thread
+//    and wider ones cost one lane exchange per doubling. A warp keeps its part
+//    of the next rows on their way into shared memory (cp.async, 16-byte pieces
+//    of 32 lanes next to each other) while it works on one, and the codes leave
+//    through the same buffer; the pieces of a lane are XOR-swizzled, which keeps
+//    both sides of the exchange free of bank conflicts.
+//  * few rows: a thread owns 8 values, four times the threads per row, one row
+//    per thread: latency counts there.
 
-constexpr int kPer = 32;               // consecutive values of one thread
-
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_values(const T *p, int have, float (&v)[kPer]) {
-    if (VEC && have >= kPer) {
-        constexpr int kVec = 16 / sizeof(T);
-#pragma unroll
-        for (int i = 0; i < kPer / kVec; ++i) {
-            const uint4 w = reinterpret_cast<const uint4 *>(p)[i];
-            const T *e = reinterpret_cast<const T *>(&w);
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) v[i * kVec + j] = to_f32(e[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = i < have ? to_f32(p[i]) : 0.0f;
-    }
-}
-
-template <int ACT>
-__device__ __forceinline__ float activate(float v) {
-    if (ACT == HATQ_ACT_RELU) return max_nan(v, 0.0f);
-    if (ACT == HATQ_ACT_SILU) return v / (1.0f + expf(-v));
-    if (ACT == HATQ_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-    return v;
-}
-
-// tpr threads per row: a power of two below a warp, or whole warps; blockDim.x / tpr rows per CTA
-template <typename T, int ACT, bool VEC, bool F16>
-__global__ void __launch_bounds__(1024) quantize_tokens_kernel(const TokenQuantArgs a, int tpr) {
-    __shared__ float warp_max[32];
-    const int rl = threadIdx.x / tpr, t = threadIdx.x - rl * tpr;
-    const long long row = (long long)blockIdx.x * (blockDim.x / tpr) + rl;
-    const int have = row < a.rows ? min(kPer, max(0, a.c - t * kPer)) : 0;
-    long long src = row;
-    if (a.index && row < a.rows) src = a.index[row];
-    float v[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = 0.0f;
-    if (have > 0 && src >= 0 && src < a.src_rows) {
-        const T *p = reinterpret_cast<const T *>(a.x) + src * a.ldx + t * kPer;
-        load_values<T, VEC>(p, have, v);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = activate<ACT>(v[i]);
-        if (a.gated) {
-            float u[kPer];
-            load_values<T, VEC>(p + a.c, have, u);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) v[i] *= u[i];
-        }
-    }
-    // blocks of hb consecutive values: up to 32 in the thread, wider ones across hb / 32 lanes
-#pragma unroll
-    for (int h = 1; h < kPer; h <<= 1) {
-        if (h < a.hb) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (i & h) continue;
-                const float x = v[i], y = v[i + h];
-                v[i] = x + y;
-                v[i + h] = x - y;
-            }
-        }
-    }
-    for (int m = 1; m * kPer < a.hb; m <<= 1) {
-        const bool upper = (t & m) != 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float o = __shfl_xor_sync(0xffffffffu, v[i], m);
-            v[i] = upper ? o - v[i] : v[i] + o;
-        }
-    }
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) amax = max_nan(amax, fabsf(v[i]));
-    for (int m = min(tpr, 32) / 2; m > 0; m >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, m));
-    if (tpr > 32) {
-        const int warps = tpr / 32, w0 = rl * warps;
-        if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = amax;
-        __syncthreads();
-        for (int w = 0; w < warps; ++w) amax = max_nan(amax, warp_max[w0 + w]);
-    }
-    if (have <= 0) return;
-    const bool fine = amax <= 3.402823466e38f;                          // false for infinity and NaN
-    // 127 / a overflows below 127 / 2^128: the step stays at the smallest normal number there
-    const float inv = !fine || amax == 0.0f ? 0.0f : fminf(127.0f / amax, 0x1p126f);
-    if (t == 0)
-        a.scales[row] = !fine ? __int_as_float(0x7fc00000)
-                              : (amax == 0.0f ? 1.0f : fmaxf(amax / 127.0f, 0x1p-126f) * a.inv_norm);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = fine ? fminf(fmaxf(rintf(v[i] * inv), -127.0f), 127.0f) : 0.0f;
-    if (F16) {
-        __half *q = reinterpret_cast<__half *>(a.codes) + row * a.ldc + t * kPer;
-        if (VEC && have >= kPer) {
-#pragma unroll
-            for (int i = 0; i < kPer / 8; ++i) {
-                uint4 w;
-                __half2 *h = reinterpret_cast<__half2 *>(&w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = __floats2half2_rn(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
-                reinterpret_cast<uint4 *>(q)[i] = w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < have) q[i] = __float2half_rn(v[i]);
-        }
-    } else {
-        int8_t *q = reinterpret_cast<int8_t *>(a.codes) + row * a.ldc + t * kPer;
-        if (VEC && have >= kPer) {
-#pragma unroll
-            for (int i = 0; i < kPer / 16; ++i) {
-                uint4 w;
-                int8_t *b = reinterpret_cast<int8_t *>(&w);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) b[j] = (int8_t)(int)v[16 * i + j];
-                reinterpret_cast<uint4 *>(q)[i] = w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < have) q[i] = (int8_t)(int)v[i];
-        }
-    }
-}
-
-template <typename T, int ACT>
-cudaError_t quantize_launch(const TokenQuantArgs &a, int format, bool vec, cudaStream_t s) {
-    const int need = (a.c + kPer - 1) / kPer;
-    int tpr = 1;
-    if (need > 32) tpr = (need + 31) & ~31;
-    else
-        while (tpr < need) tpr <<= 1;
-    const int per_cta = tpr >= 256 ? 1 : 256 / tpr;
-    const long long grid = (a.rows + per_cta - 1) / per_cta;
-    const int threads = ((per_cta * tpr + 31) / 32) * 32;
-    if (grid > INT_MAX) return cudaErrorInvalidValue;
-    void (*k)(TokenQuantArgs, int) =
-        format == HATQ_CODES_F16 ? (vec ? quantize_tokens_kernel<T, ACT, true, true> : quantize_tokens_kernel<T, ACT, false, true>)
-                                 : (vec ? quantize_tokens_kernel<T, ACT, true, false> : quantize_tokens_kernel<T, ACT, false, false>);
-    k<<<(unsigned)grid, threads, 0, s>>>(a, tpr);
-    return cudaGetLastError();
+template <int PIECES>
+__device__ __forceinline__ int swizzle(int owner, int piece) {
+    // the 8 lanes of one 128-byte pass sit in different 16-byte columns
+    return owner * PIECES + (piece ^ (PIECES == 8 ? owner & 7 : PIECES == 4 ? (owner >> 1) & 3 : PIECES == 2 ? (owner >> 2) & 1 : 0));
 }
 
 template <typename T>
-cudaError_t quantize_act(const TokenQuantArgs &a, int format, bool vec, cudaStream_t s) {
-    switch (a.act) {
-        case HATQ_ACT_NONE: return quantize_launch<T, HATQ_ACT_NONE>(a, format, vec, s);
-        case HATQ_ACT_RELU: return quantize_launch<T, HATQ_ACT_RELU>(a, format, vec, s);
-        case HATQ_ACT_SILU: return quantize_launch<T, HATQ_ACT_SILU>(a, format, vec, s);
-        default: return quantize_launch<T, HATQ_ACT_GELU>(a, format, vec, s);
+__device__ __forceinline__ pair32 widen2(uint32_t w);
+template <> __device__ __forceinline__ pair32 widen2<__nv_bfloat16>(uint32_t w) {
+    return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <> __device__ __forceinline__ pair32 widen2<__half>(uint32_t w) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    return pack2(f.x, f.y);
+}
+
+__device__ __forceinline__ float activate(float v, int act) {
+    if (act == HATQ_ACT_RELU) return v < 0.0f ? 0.0f : v;               // keeps a NaN
+    if (act == HATQ_ACT_SILU) return v / (1.0f + expf(-v));
+    return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+}
+
+// A row's threads: tpr, a power of two below a warp (a warp then holds 32 / tpr rows) or whole warps.
+struct Lanes {
+    int tpr, lane, t;                  // threads per row, lane, thread within the row
+    long long row;                     // the thread's row
+};
+
+// One 16-byte piece, or its first `have` values where it is cut off or not aligned.
+template <typename E, int IN>
+__device__ __forceinline__ uint4 load_piece(const E *p, int have, bool vec) {
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (vec && have >= IN) return *reinterpret_cast<const uint4 *>(p);
+    E *e = reinterpret_cast<E *>(&w);
+#pragma unroll
+    for (int j = 0; j < IN; ++j)
+        if (j < have) e[j] = p[j];
+    return w;
+}
+template <typename E, int IN>
+__device__ __forceinline__ void store_piece(E *p, int have, bool vec, const uint4 &w) {
+    if (vec && have >= IN) {
+        if (sizeof(E) * IN == 16) *reinterpret_cast<uint4 *>(p) = w;
+        else *reinterpret_cast<uint2 *>(p) = make_uint2(w.x, w.y);
+        return;
     }
+    const E *e = reinterpret_cast<const E *>(&w);
+#pragma unroll
+    for (int j = 0; j < IN; ++j)
+        if (j < have) p[j] = e[j];
+}
+
+// Where piece i of the warp's values lies: {row of the owner lane, first element}, and its place in the buffer.
+template <int PER, int IN>
+__device__ __forceinline__ int piece_first(const Lanes &l, int i) {
+    constexpr int kPieces = PER / IN;
+    const int at = i * 32 + l.lane;
+    return l.tpr >= 32 ? (l.t - l.lane) * PER + at * IN : ((at / kPieces) & (l.tpr - 1)) * PER + (at % kPieces) * IN;
+}
+template <int PER, int IN>
+__device__ __forceinline__ int piece_at(const Lanes &l, int i) {
+    constexpr int kPieces = PER / IN;
+    return swizzle<kPieces>((i * 32 + l.lane) / kPieces, (i * 32 + l.lane) % kPieces);
+}
+
+template <typename T, int PIECES>
+__device__ __forceinline__ void widen(const uint4 (&w)[PIECES], pair32 (&v)[PIECES * 16 / sizeof(T) / 2]) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const uint32_t e[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 2) v[4 * i + j] = widen2<T>(e[j]);
+            else if (j % 2 == 0) v[2 * i + j / 2] = pack2(__uint_as_float(e[j]), __uint_as_float(e[j + 1]));
+        }
+    }
+}
+
+template <int PER>
+__device__ __forceinline__ void activate_all(pair32 (&v)[PER / 2], int act) {
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i) {
+        float x, y;
+        unpack2(v[i], x, y);
+        v[i] = pack2(activate(x, act), activate(y, act));
+    }
+}
+template <int PER>
+__device__ __forceinline__ void gate_all(pair32 (&v)[PER / 2], const pair32 (&u)[PER / 2]) {
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i) {
+        float x, y, p, q;
+        unpack2(v[i], x, y);
+        unpack2(u[i], p, q);
+        v[i] = pack2(x * p, y * q);
+    }
+}
+
+// H~_hb on blocks of hb consecutive values: up to PER in the thread, wider ones across hb / PER lanes
+template <int PER>
+__device__ __forceinline__ void transform(pair32 (&v)[PER / 2], int hb, int t) {
+    if (hb > 1) {
+#pragma unroll
+        for (int i = 0; i < PER / 2; ++i) {
+            float x, y;
+            unpack2(v[i], x, y);
+            v[i] = pack2(x + y, x - y);
+        }
+    }
+#pragma unroll
+    for (int h = 1; h < PER / 2; h <<= 1) {
+        if (2 * h < hb) {
+#pragma unroll
+            for (int i = 0; i < PER / 2; ++i) {
+                if (i & h) continue;
+                const pair32 x = v[i], y = v[i + h];
+                v[i] = add2(x, y);
+                v[i + h] = sub2(x, y);
+            }
+        }
+    }
+    for (int m = 1; m * PER < hb; m <<= 1) {
+        const float sign = (t & m) != 0 ? -1.0f : 1.0f;
+        const pair32 sign2 = pack2(sign, sign);
+#pragma unroll
+        for (int i = 0; i < PER / 2; ++i) {
+            float x, y;
+            unpack2(v[i], x, y);
+            x = __shfl_xor_sync(0xffffffffu, x, m);
+            y = __shfl_xor_sync(0xffffffffu, y, m);
+            v[i] = fma2(sign2, v[i], pack2(x, y));                      // exact product: one rounding, that of the sum
+        }
+    }
+}
+
+// max |v| of the thread's lanes of the row (the warp, or tpr lanes of it)
+template <int PER>
+__device__ __forceinline__ float lane_max(const pair32 (&v)[PER / 2], int tpr) {
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i) {
+        float x, y;
+        unpack2(v[i], x, y);
+        amax = max_abs(amax, x, y);
+    }
+    for (int m = min(tpr, 32) / 2; m > 0; m >>= 1) amax = max_abs(amax, __shfl_xor_sync(0xffffffffu, amax, m), 0.0f);
+    return amax;
+}
+// of the row's warps, whose maxima lie at m[0 .. warps)
+__device__ __forceinline__ float warps_max(const float *m, int warps, int lane) {
+    float amax = 0.0f;
+    if (warps <= 8) {
+        for (int w = 0; w < warps; ++w) amax = max_abs(amax, m[w], 0.0f);
+    } else {
+        amax = lane < warps ? m[lane] : 0.0f;
+        for (int h = 16; h > 0; h >>= 1) amax = max_abs(amax, __shfl_xor_sync(0xffffffffu, amax, h), 0.0f);
+    }
+    return amax;
+}
+
+__device__ __forceinline__ bool is_fine(float amax) { return amax <= 3.402823466e38f; }   // no infinity, no NaN
+// 127 / a overflows below 127 / 2^128: the step stays at the smallest normal number there
+__device__ __forceinline__ float step_inverse(float amax) {
+    return !is_fine(amax) || amax == 0.0f ? 0.0f : fminf(127.0f / amax, 0x1p126f);
+}
+__device__ __forceinline__ float step_of(float amax, float inv_norm) {
+    if (!is_fine(amax)) return __int_as_float(0x7fc00000);
+    return amax == 0.0f ? 1.0f : fmaxf(amax / 127.0f, 0x1p-126f) * inv_norm;
+}
+
+// fma(t, inv, 1.5 2^23 + c) rounds t inv to an integer (half to even) and leaves it, plus c, in the low bits.
+// c = 0x6480 makes the low half-word the fp16 number 1152 + code.
+template <bool F16, int PER>
+__device__ __forceinline__ void encode(const pair32 (&v)[PER / 2], float amax, uint32_t (&w)[F16 ? PER / 2 : PER / 4]) {
+    const bool fine = is_fine(amax);
+    const float inv = step_inverse(amax), base = 12582912.0f + (F16 ? 25728.0f : 0.0f);
+    const pair32 inv2 = pack2(inv, inv), base2 = pack2(base, base);
+    if constexpr (F16) {
+#pragma unroll
+        for (int i = 0; i < PER / 2; ++i) {
+            float x, y;
+            unpack2(fma2(v[i], inv2, base2), x, y);
+            uint32_t h;
+            asm("sub.f16x2 %0, %1, %2;"
+                : "=r"(h)
+                : "r"(__byte_perm(__float_as_uint(x), __float_as_uint(y), 0x5410)), "r"(0x64806480u));
+            w[i] = fine ? h : 0u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER / 4; ++i) {
+            float x, y, z, q;
+            unpack2(fma2(v[2 * i], inv2, base2), x, y);
+            unpack2(fma2(v[2 * i + 1], inv2, base2), z, q);
+            const uint32_t c = __byte_perm(__byte_perm(__float_as_uint(x), __float_as_uint(y), 0x0040),
+                                           __byte_perm(__float_as_uint(z), __float_as_uint(q), 0x0040), 0x5410);
+            w[i] = fine ? c : 0u;
+        }
+    }
+}
+
+// ---- few rows: 8 values per thread, one CTA per row or more rows per CTA
+
+template <typename T, bool F16>
+__global__ void __launch_bounds__(1024) quantize_few_kernel(const __grid_constant__ TokenQuantArgs a, int tpr) {
+    using E = typename std::conditional<F16, __half, int8_t>::type;
+    constexpr int kPer = 8, kIn = 16 / sizeof(T), kPieces = kPer / kIn;
+    __shared__ float warp_max[32];
+    const int rl = threadIdx.x / tpr, lane = threadIdx.x & 31, t = threadIdx.x - rl * tpr;
+    const long long row = (long long)blockIdx.x * (blockDim.x / tpr) + rl;
+    int src = row < a.rows ? (a.index ? a.index[row] : (int)row) : -1;
+    if (src >= a.src_rows) src = -1;
+    const int have = src < 0 ? 0 : a.c - t * kPer;
+    const T *p = reinterpret_cast<const T *>(a.x) + (long long)max(src, 0) * a.ldx + t * kPer;
+    uint4 w[kPieces], g[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        w[i] = load_piece<T, kIn>(p + i * kIn, have - i * kIn, a.vec);
+        if (a.gated) g[i] = load_piece<T, kIn>(p + a.c + i * kIn, have - i * kIn, a.vec);
+    }
+    pair32 v[kPer / 2];
+    widen<T, kPieces>(w, v);
+    if (a.act != HATQ_ACT_NONE && src >= 0) activate_all<kPer>(v, a.act);
+    if (a.gated) {
+        pair32 u[kPer / 2];
+        widen<T, kPieces>(g, u);
+        gate_all<kPer>(v, u);
+    }
+    transform<kPer>(v, a.hb, t);
+    float amax = lane_max<kPer>(v, tpr);
+    if (tpr > 32) {
+        if (lane == 0) warp_max[threadIdx.x >> 5] = amax;
+        __syncthreads();
+        amax = warps_max(warp_max + rl * (tpr / 32), tpr / 32, lane);
+    }
+    if (row >= a.rows) return;
+    if (t == 0) a.scales[row] = step_of(amax, a.inv_norm);
+    uint32_t out[4] = {0, 0, 0, 0};
+    encode<F16, kPer>(v, amax, reinterpret_cast<uint32_t(&)[F16 ? 4 : 2]>(out));
+    store_piece<E, kPer>(reinterpret_cast<E *>(a.codes) + row * a.ldc + t * kPer, a.c - t * kPer, a.vec,
+                         make_uint4(out[0], out[1], out[2], out[3]));
+}
+
+// ---- many rows
+
+constexpr int kPer = 32;
+
+__device__ __forceinline__ void copy_async(uint4 *dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src)
+                 : "memory");
+}
+template <int AHEAD> __device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+}
+
+// STAGES buffers per warp, so STAGES - 1 rows on their way. With one buffer (wide rows, whose buffers would not
+// all fit) the two halves of a gated row pass through it one after the other.
+template <typename T, bool F16, int THREADS, int STAGES>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
+    quantize_rows_kernel(const __grid_constant__ TokenQuantArgs a, int tpr) {
+    using E = typename std::conditional<F16, __half, int8_t>::type;
+    constexpr int kIn = 16 / sizeof(T), kPieces = kPer / kIn;            // pieces per thread
+    constexpr int kOutIn = 16 / sizeof(E), kOutPieces = kPer / kOutIn;
+    __shared__ float warp_max[2][32];
+    extern __shared__ __align__(16) uint4 buffers[];
+    constexpr bool kAlone = STAGES == 1;
+    const int halves = a.gated && !kAlone ? 2 : 1, stage_pieces = 32 * kPieces * halves;
+    uint4 *stages = buffers + (threadIdx.x >> 5) * STAGES * stage_pieces;
+    const int rl = threadIdx.x / tpr, per_cta = blockDim.x / tpr;
+    Lanes l;
+    l.tpr = tpr;
+    l.lane = threadIdx.x & 31;
+    l.t = threadIdx.x - rl * tpr;
+    const long long step = (long long)gridDim.x * per_cta;
+    const long long base = (long long)blockIdx.x * per_cta;
+    auto source = [&](long long row) {
+        int src = row < a.rows ? (a.index ? a.index[row] : (int)row) : -1;
+        return src >= a.src_rows ? -1 : src;
+    };
+    auto issue = [&](int src, uint4 *buffer, int half) {
+#pragma unroll 1
+        for (int h = half; h < half + halves; ++h) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int first = piece_first<kPer, kIn>(l, i);
+                const int from = l.tpr >= 32 ? src : __shfl_sync(0xffffffffu, src, (i * 32 + l.lane) / kPieces);
+                const T *p = reinterpret_cast<const T *>(a.x) + (long long)max(from, 0) * a.ldx + h * a.c + first;
+                const int have = from < 0 ? 0 : a.c - first;
+                uint4 *dst = buffer + (h - half) * 32 * kPieces + piece_at<kPer, kIn>(l, i);
+                if (a.vec && have >= kIn) copy_async(dst, p);
+                else *dst = load_piece<T, kIn>(p, have, false);
+            }
+        }
+    };
+    int srcs[STAGES];
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        srcs[s] = source(base + s * step + rl);
+        issue(srcs[s], stages + s * stage_pieces, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    srcs[STAGES - 1] = source(base + (STAGES - 1) * step + rl);
+    int at = 0, ahead = STAGES - 1, turn = 0;
+    for (long long first = base; first < a.rows; first += step) {
+        issue(srcs[STAGES - 1], stages + ahead * stage_pieces, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        const int src = srcs[0];
+#pragma unroll
+        for (int s = 0; s + 1 < STAGES; ++s) srcs[s] = srcs[s + 1];
+        srcs[STAGES - 1] = source(first + STAGES * step + rl);
+        l.row = first + rl;
+        copies_wait<STAGES - 1>();
+        __syncwarp();
+        uint4 *stage = stages + at * stage_pieces;
+        uint4 w[kPieces];
+        pair32 v[kPer / 2];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) w[i] = stage[swizzle<kPieces>(l.lane, i)];
+        widen<T, kPieces>(w, v);
+        if (a.act != HATQ_ACT_NONE && src >= 0) activate_all<kPer>(v, a.act);
+        if (a.gated) {
+            pair32 u[kPer / 2];
+            if (kAlone) {
+                __syncwarp();
+                issue(src, stage, 1);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                copies_wait<0>();
+                __syncwarp();
+            }
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) w[i] = stage[(kAlone ? 0 : 32 * kPieces) + swizzle<kPieces>(l.lane, i)];
+            widen<T, kPieces>(w, u);
+            gate_all<kPer>(v, u);
+        }
+        transform<kPer>(v, a.hb, l.t);
+        float amax = lane_max<kPer>(v, tpr);
+        if (tpr > 32) {
+            if (l.lane == 0) warp_max[turn][threadIdx.x >> 5] = amax;
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + rl), "r"(tpr) : "memory");
+            amax = warps_max(warp_max[turn] + rl * (tpr / 32), tpr / 32, l.lane);
+            turn ^= 1;                                                   // the next row's maxima have a place of their own
+        }
+        if (l.t == 0 && l.row < a.rows) a.scales[l.row] = step_of(amax, a.inv_norm);
+        union { uint4 p[kOutPieces]; uint32_t w[F16 ? kPer / 2 : kPer / 4]; } out;
+        encode<F16, kPer>(v, amax, out.w);
+        __syncwarp();                                                    // every lane has read the buffer
+#pragma unroll
+        for (int i = 0; i < kOutPieces; ++i) stage[swizzle<kOutPieces>(l.lane, i)] = out.p[i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kOutPieces; ++i) {
+            const int from = piece_first<kPer, kOutIn>(l, i);
+            const long long row = l.tpr >= 32 ? l.row : l.row - l.lane / l.tpr + (i * 32 + l.lane) / kOutPieces / l.tpr;
+            store_piece<E, kOutIn>(reinterpret_cast<E *>(a.codes) + row * a.ldc + from, row < a.rows ? a.c - from : 0, a.vec,
+                                   stage[piece_at<kPer, kOutIn>(l, i)]);
+        }
+        __syncwarp();                                                    // the buffer is free for the next copies
+        at = at + 1 == STAGES ? 0 : at + 1;
+        ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+    }
+    copies_wait<0>();
+}
+
+int threads_per_row(int c, int per) {
+    const int need = (c + per - 1) / per;
+    if (need > 32) return (need + 31) & ~31;
+    int tpr = 1;
+    while (tpr < need) tpr <<= 1;
+    return tpr;
+}
+
+template <typename T, bool F16, int THREADS, int STAGES>
+cudaError_t quantize_rows_launch(const TokenQuantArgs &a, cudaStream_t s) {
+    const int tpr = threads_per_row(a.c, kPer);
+    const int per_cta = tpr >= 256 ? 1 : 256 / tpr;
+    const int threads = per_cta * tpr;                                   // whole warps
+    auto k = quantize_rows_kernel<T, F16, THREADS, STAGES>;
+    const int smem = threads * kPer * (int)sizeof(T) * STAGES * (a.gated && STAGES > 1 ? 2 : 1);
+    static const int regs = [] {
+        cudaFuncAttributes fa{};
+        return cudaFuncGetAttributes(&fa, quantize_rows_kernel<T, F16, THREADS, STAGES>) == cudaSuccess ? fa.numRegs : 128;
+    }();
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    // as many CTAs as are resident at once: they walk the rows
+    const int fit = max(1, min(min(2048 / threads, 220 * 1024 / (smem + 1024)), 65536 / (regs * threads)));
+    const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * fit;
+    k<<<(unsigned)(ctas < room ? ctas : room), threads, smem, s>>>(a, tpr);
+    return cudaGetLastError();
+}
+
+template <typename T, bool F16>
+cudaError_t quantize_size(const TokenQuantArgs &a, cudaStream_t s) {
+    // few rows: as long as one CTA wave of 8-value threads holds them
+    if (a.c <= 8192 && a.rows * a.c <= (long long)a.sms * 1024 * 8) {
+        const int tpr = threads_per_row(a.c, 8), per_cta = tpr >= 256 ? 1 : 256 / tpr;
+        quantize_few_kernel<T, F16><<<(unsigned)((a.rows + per_cta - 1) / per_cta), per_cta * tpr, 0, s>>>(a, tpr);
+        return cudaGetLastError();
+    }
+    if (a.c > 8192) {
+        if (sizeof(T) == 4 || a.gated) return quantize_rows_launch<T, F16, 1024, 1>(a, s);
+        return quantize_rows_launch<T, F16, 1024, sizeof(T) == 4 ? 1 : 2>(a, s);
+    }
+    return quantize_rows_launch<T, F16, 256, sizeof(T) == 4 ? 2 : 3>(a, s);
 }
 
 // ------------------------------------------------------------ weight layout
@@ -291,33 +584,19 @@ template <int MT>
 __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArgs a) {
     extern __shared__ __align__(16) uint8_t xs[];                       // [MT][k_pad] codes
     __shared__ int part[kFewThreads / 32][kFewCh][MT];
-    __shared__ int s_group, s_count;
     const int k_pad = a.kb * 64;
     int e = 0, r0 = 0, r1 = a.rows;
     if (a.offsets) {
-        // the blockIdx.y-th group that holds rows
-        if (threadIdx.x == 0) { s_group = -1; s_count = 0; }
-        __syncthreads();
-        for (int g0 = 0; g0 < a.experts; g0 += kFewThreads) {
-            const int g = g0 + threadIdx.x;
-            const bool holds = g < a.experts && min(a.offsets[g + 1], a.rows) > max(a.offsets[g], 0);
-            const unsigned ball = __ballot_sync(0xffffffffu, holds);
-            __shared__ int warps[kFewThreads / 32];
-            if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = __popc(ball);
-            __syncthreads();
-            int before = s_count;
-            for (int w = 0; w < (int)(threadIdx.x >> 5); ++w) before += warps[w];
-            before += __popc(ball & ((1u << (threadIdx.x & 31)) - 1));
-            if (holds && before == (int)blockIdx.y) s_group = g;
-            __syncthreads();
-            if (threadIdx.x == 0)
-                for (int w = 0; w < kFewThreads / 32; ++w) s_count += warps[w];
-            __syncthreads();
-        }
-        e = s_group;
-        if (e < 0) return;
-        r0 = max(a.offsets[e], 0);
-        r1 = min(a.offsets[e + 1], a.rows);
+        // the expert of row blockIdx.y: as many experts end at or before it. The CTA takes the row and the next
+        // MT - 1 of its expert; the other rows' CTAs leave.
+        for (int g = 0; g < a.experts; g += kFewThreads)
+            e += __syncthreads_count(g + (int)threadIdx.x < a.experts &&
+                                     a.offsets[g + threadIdx.x + 1] <= (int)blockIdx.y);
+        if (e >= a.experts) return;
+        const int lo = min(max(a.offsets[e], 0), a.rows);
+        r0 = (int)blockIdx.y;
+        r1 = min(min(max(a.offsets[e + 1], 0), a.rows), r0 + MT);
+        if (r0 < lo || (r0 - lo) % MT != 0) return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ch_l = lane & 7, j = lane >> 3;
@@ -403,11 +682,14 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
 
 // ------------------------------------------------------------ combine_rows
 
+// A thread owns 16 bytes of a token's row; the rows of up to eight slots are on their way at a time.
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) combine_rows_kernel(const T *y, long long ldy, long long rows, const int32_t *index,
                                                            const float *weights, long long tokens, int topk, int c, T *out,
                                                            long long ldo) {
     constexpr int kVec = VEC ? 16 / sizeof(T) : 1;
+    constexpr int kAhead = 8;
     const int per_row = (c + kVec - 1) / kVec;
     const long long total = tokens * per_row;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
@@ -416,17 +698,27 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const T *y, long long
         float acc[kVec];
 #pragma unroll
         for (int q = 0; q < kVec; ++q) acc[q] = 0.0f;
-        for (int j = 0; j < topk; ++j) {
-            const long long r = index[t * topk + j];
-            if (r < 0 || r >= rows) continue;
-            const float w = weights[t * topk + j];
-            if (VEC) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(y + r * ldy + at);
-                const T *e = reinterpret_cast<const T *>(&v);
+        for (int j0 = 0; j0 < topk; j0 += kAhead) {
+            uint4 v[kAhead];
+            float w[kAhead];
+            bool have[kAhead];
 #pragma unroll
-                for (int q = 0; q < kVec; ++q) acc[q] += w * to_f32(e[q]);
-            } else {
-                acc[0] += w * to_f32(y[r * ldy + at]);
+            for (int j = 0; j < kAhead; ++j) {
+                const long long r = j0 + j < topk ? index[t * topk + j0 + j] : -1;
+                have[j] = r >= 0 && r < rows;
+                w[j] = have[j] ? weights[t * topk + j0 + j] : 0.0f;
+                if (have[j]) {
+                    if (VEC) v[j] = *reinterpret_cast<const uint4 *>(y + r * ldy + at);
+                    else *reinterpret_cast<T *>(&v[j]) = y[r * ldy + at];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (have[j]) {
+                    const T *e = reinterpret_cast<const T *>(&v[j]);
+#pragma unroll
+                    for (int q = 0; q < kVec; ++q) acc[q] += w[j] * to_f32(e[q]);
+                }
             }
         }
         if (VEC) {
@@ -456,11 +748,12 @@ cudaError_t combine_launch(const void *y, long long ldy, long long rows, const i
 
 }  // namespace
 
-cudaError_t launch_quantize_tokens(const TokenQuantArgs &a, int x_type, int format, bool vec, cudaStream_t s) {
+cudaError_t launch_quantize_tokens(const TokenQuantArgs &a, int x_type, int format, cudaStream_t s) {
+    const bool f16 = format == HATQ_CODES_F16;
     switch (x_type) {
-        case HATQ_F32: return quantize_act<float>(a, format, vec, s);
-        case HATQ_F16: return quantize_act<__half>(a, format, vec, s);
-        default: return quantize_act<__nv_bfloat16>(a, format, vec, s);
+        case HATQ_F32: return f16 ? quantize_size<float, true>(a, s) : quantize_size<float, false>(a, s);
+        case HATQ_F16: return f16 ? quantize_size<__half, true>(a, s) : quantize_size<__half, false>(a, s);
+        default: return f16 ? quantize_size<__nv_bfloat16, true>(a, s) : quantize_size<__nv_bfloat16, false>(a, s);
     }
 }
 
@@ -482,7 +775,7 @@ cudaError_t launch_pack_codes(const void *x, int format, long long ldx, long lon
 }
 
 cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
-    const dim3 grid((a.n + kFewCh - 1) / kFewCh, a.offsets ? a.slots : 1);
+    const dim3 grid((a.n + kFewCh - 1) / kFewCh, a.offsets ? a.rows : 1);
     const int smem = tokens * a.kb * 64;
     void (*k)(LinearArgs) = tokens == 1   ? linear_few_kernel<1>
                             : tokens == 2 ? linear_few_kernel<2>

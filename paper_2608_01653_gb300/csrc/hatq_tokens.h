@@ -23,12 +23,14 @@ struct TokenQuantArgs {
     const int32_t *index;
     long long rows;
     int c, hb, act, gated;
+    int sms;                           // of the device
+    bool vec;                          // rows of x and codes lie on 16-byte boundaries
     float inv_norm;                    // 1 / sqrt(hb)
     void *codes;
     long long ldc;
     float *scales;
 };
-cudaError_t launch_quantize_tokens(const TokenQuantArgs &a, int x_type, int format, bool vec, cudaStream_t s);
+cudaError_t launch_quantize_tokens(const TokenQuantArgs &a, int x_type, int format, cudaStream_t s);
 
 cudaError_t launch_linear_layout(const int8_t *w, long long ldw, int experts, int n, int k, uint8_t *codes,
                                  int32_t *windows, cudaStream_t s);

@@ -223,9 +223,11 @@ hatq_status hatq_quantize_tokens(const void *x, int x_type, long long ldx, long 
     a.codes = codes;
     a.ldc = ldc;
     a.scales = scales;
-    const bool vec = aligned(x, 16) && ldx * xs % 16 == 0 && (!gated || (size_t)c * xs % 16 == 0) && aligned(codes, 16) &&
+    a.sms = sm_count();
+    if (!a.sms) return fail(HATQ_ERR_CUDA, "no CUDA device");
+    a.vec = aligned(x, 16) && ldx * xs % 16 == 0 && (!gated || (size_t)c * xs % 16 == 0) && aligned(codes, 16) &&
                      ldc * cs % 16 == 0;
-    const cudaError_t e = hatq::launch_quantize_tokens(a, x_type, format, vec, reinterpret_cast<cudaStream_t>(stream));
+    const cudaError_t e = hatq::launch_quantize_tokens(a, x_type, format, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "token quantization launch");
 }
 

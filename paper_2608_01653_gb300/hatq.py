@@ -779,60 +779,74 @@ CODES_I8, CODES_F16 = 0, 1
 _CODE_FORMATS = {"i8": CODES_I8, "f16": CODES_F16}
 _TOKEN_TYPES = {}                                   # torch dtype -> hatq_type / hatq_codes, filled on first use
 _CODE_TYPES = {}
+_TORCH = None
 
+
+# A decode step's kernels run for a few microseconds, so the checks of a call are kept to what takes tens of
+# nanoseconds each: no tensor is made, no device object compared, no symbol imported.
 
 def _token_torch():
-    """torch, with the dtype tables filled (the module itself imports without torch)."""
-    import torch
-    if not _TOKEN_TYPES:
+    """torch, with the dtype tables filled (this module imports without torch)."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
         _CODE_TYPES.update({torch.int8: CODES_I8, torch.float16: CODES_F16})
         _TOKEN_TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
-    return torch
+        _TORCH = torch
+    return _TORCH
 
 
-def _rows_of(t, name, types, width=None):
-    """Checks a [rows][width] device tensor with contiguous rows; returns its type code."""
+def _rows_of(t, name, types, width, device):
+    """Checks a [rows][width] tensor on `device` with contiguous rows that do not overlap; returns its type code,
+    its rows and its pitch in elements."""
     code = types.get(t.dtype)
     if code is None:
         raise ValueError(f"{name}: dtype {t.dtype} is none of {[str(d) for d in types]}")
     shape = t.shape
     if len(shape) != 2 or (width is not None and shape[1] != width):
         raise ValueError(f"{name}: shape {tuple(shape)}, expected [rows, {'width' if width is None else width}]")
-    if shape[1] > 1 and t.stride(1) != 1:
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
+    rows, values = shape
+    pitch, inner = t.stride()
+    if inner != 1 and values > 1:
         raise ValueError(f"{name}: the values of a row must be contiguous")
-    return code
+    if rows <= 1:
+        pitch = values                              # a single row may carry any stride
+    elif pitch < values:
+        raise ValueError(f"{name}: rows overlap (stride {pitch} for {values} values)")
+    return code, rows, pitch
 
 
-def _pitch(t):
-    """Elements from row to row. A single row, or rows of a tensor without elements, may carry any stride."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+def _apart(t):
+    """The input t, copied where its rows are one row (expand) or overlap: the library takes pitches of a row or more."""
+    return t.contiguous() if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1] else t
 
 
-def _flat(t, name, dtype, shape, like):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}")
-
-
-def _no_broadcast(t, name):
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)} for {t.shape[1]} values)")
+def _flat(t, name, dtype, shape, device):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def _launch_stream(t, stream):
-    """The raw stream of a call: `stream`, or the tensor's device's current one. The device must be the current one."""
+    """(device index, raw stream) of a call: `stream`, or the device's current one. The device must be the current one."""
     torch = _token_torch()
-    index = t.device.index
-    if t.device.type != "cuda":
+    device = t.get_device()
+    if device < 0:
         raise ValueError(f"expected CUDA tensors, got {t.device}")
-    if index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return device, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _on(stream):
-    """Allocations of a call belong to the stream that it runs on."""
-    import contextlib
-    return contextlib.nullcontext() if stream is None else _token_torch().cuda.stream(stream)
+def _empty(like, shape, dtype, stream):
+    """A tensor of a call's own; it belongs to the stream that the call runs on."""
+    if stream is None:
+        return _TORCH.empty(shape, dtype=dtype, device=like.device)
+    with _TORCH.cuda.stream(stream):
+        return _TORCH.empty(shape, dtype=dtype, device=like.device)
 
 
 class LinearWeights:
@@ -841,6 +855,7 @@ class LinearWeights:
     def __init__(self, experts, n, k, codes, windows, s_w, bias, grouped):
         self.experts, self.n, self.k, self.grouped = experts, n, k, grouped
         self.codes, self.windows, self.s_w, self.bias = codes, windows, s_w, bias
+        self.device = codes.get_device()
         self.struct = LinearWeightsStruct(experts, n, k, 0, codes.data_ptr(), windows.data_ptr(), s_w.data_ptr(),
                                           None if bias is None else bias.data_ptr())
         self.ref = ctypes.byref(self.struct)
@@ -862,26 +877,25 @@ def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeight
     e, n, k = w.shape if grouped else (1, *w.shape)
     size = ctypes.c_size_t()
     _check(load().hatq_linear_sizes(e, n, k, ctypes.byref(size)))
-    raw = _launch_stream(w, stream)
-    with _on(stream):
+    device, raw = _launch_stream(w, stream)
+    with torch.cuda.stream(stream):                 # None: the current one
         rows = w.reshape(e * n, k)
+        rows = _apart(rows if k == 1 or rows.stride(1) == 1 else rows.contiguous())
         if w.dtype == torch.int8:
             if scales is None or hb != 1:
                 raise ValueError("int8 weights need their scales, and are not transformed")
-            codes = rows if k == 1 or rows.stride(1) == 1 else rows.contiguous()
             s_w = scales.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
         else:
             if scales is not None:
                 raise ValueError("scales belong to int8 weights")
-            codes, s_w = quantize_tokens(rows if k == 1 or rows.stride(1) == 1 else rows.contiguous(), hb=hb,
-                                         codes="i8", stream=stream)
+            rows, s_w = quantize_tokens(rows, hb=hb, codes="i8", stream=stream)
         b = None if bias is None else bias.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
         if s_w.numel() != e * n or (b is not None and b.numel() != e * n):
             raise ValueError(f"scales and bias need one value per output channel ({e * n})")
-        _no_broadcast(codes, "w")
+        _, _, pitch = _rows_of(rows, "w", {torch.int8: 0}, k, device)
         L = LinearWeights(e, n, k, torch.empty(size.value, dtype=torch.uint8, device=w.device),
                           torch.empty(e, dtype=torch.int32, device=w.device), s_w, b, grouped)
-        _check(load().hatq_linear_layout(codes.data_ptr(), _pitch(codes), L.ref, raw))
+        _check(load().hatq_linear_layout(rows.data_ptr(), pitch, L.ref, raw))
     return L
 
 
@@ -892,80 +906,68 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
     codes: "i8", "f16", or "auto": int8 for up to 8 rows (the dot-product kernel
     reads them as they are), fp16 above (the tensor cores do). out / scales:
     tensors to write into; new codes come with a pitch that suits the products."""
-    torch = _token_torch()
-    kind = _rows_of(x, "x", _TOKEN_TYPES)
-    if act not in _ACTS:
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(x, stream)
+    x = _apart(x)
+    kind, src_rows, pitch = _rows_of(x, "x", _TOKEN_TYPES, None, device)
+    code = _ACTS.get(act)
+    if code is None:
         raise ValueError(f"unknown activation {act!r}")
-    c = x.shape[1] // 2 if gated else x.shape[1]
-    if gated and x.shape[1] % 2:
-        raise ValueError("a gated row holds two halves")
-    raw = _launch_stream(x, stream)
-    n = x.shape[0] if rows is None else rows.shape[0]
-    if rows is not None:
-        _flat(rows, "rows", torch.int32, (n,), x)
+    c = x.shape[1]
+    if gated:
+        if c % 2:
+            raise ValueError("a gated row holds two halves")
+        c //= 2
+    n = src_rows if rows is None else rows.shape[0]
+    index = None if rows is None else _flat(rows, "rows", torch.int32, (n,), device)
     if codes == "auto":
         codes = "i8" if n <= 8 else "f16"
-    if out is None or scales is None:
-        with _on(stream):
-            if out is None:
-                pad = 16 if codes == "i8" else 8
-                out = torch.empty((n, -(-c // pad) * pad), dtype=torch.int8 if codes == "i8" else torch.float16,
-                                  device=x.device)
-                out = out if out.shape[1] == c else out[:, :c]
-            if scales is None:
-                scales = torch.empty(n, dtype=torch.float32, device=x.device)
-    fmt = _rows_of(out, "out", _CODE_TYPES, c)
-    if out.shape[0] != n or out.device != x.device or _CODE_FORMATS.get(codes) != fmt:
-        raise ValueError(f"out: expected {n} rows of {codes} codes on {x.device}")
-    _no_broadcast(out, "out")
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-        x = x.contiguous()                          # expanded rows: the library takes pitches of at least a row
-    _flat(scales, "scales", torch.float32, (n,), x)
-    st = load().hatq_quantize_tokens(x.data_ptr(), kind, _pitch(x), x.shape[0], None if rows is None else rows.data_ptr(),
-                                     n, c, hb, _ACTS[act], int(bool(gated)), fmt, out.data_ptr(), _pitch(out),
-                                     scales.data_ptr(), raw)
+    if out is None:
+        pad = 16 if codes == "i8" else 8
+        out = _empty(x, (n, -(-c // pad) * pad), torch.int8 if codes == "i8" else torch.float16, stream)
+        if out.shape[1] != c:
+            out = out[:, :c]
+    if scales is None:
+        scales = _empty(x, (n,), torch.float32, stream)
+    fmt, out_rows, out_pitch = _rows_of(out, "out", _CODE_TYPES, c, device)
+    if out_rows != n or _CODE_FORMATS.get(codes) != fmt:
+        raise ValueError(f"out: expected {n} rows of {codes} codes, got {out_rows} of {out.dtype}")
+    st = (_LIB or load()).hatq_quantize_tokens(x.data_ptr(), kind, pitch, src_rows, index, n, c, hb, code, 1 if gated else 0,
+                                               fmt, out.data_ptr(), out_pitch,
+                                               _flat(scales, "scales", torch.float32, (n,), device), raw)
     if st:
         _check(st)
     return out, scales
 
 
 def _product(x, scales, offsets, layer, dtype, out, stream):
-    torch = _token_torch()
-    fmt = _rows_of(x, "x", _CODE_TYPES, layer.k)
-    raw = _launch_stream(x, stream)
-    if layer.codes.device != x.device:
-        raise ValueError(f"the weights are on {layer.codes.device}, x on {x.device}")
-    n = x.shape[0]
-    _flat(scales, "scales", torch.float32, (n,), x)
-    if offsets is not None:
-        _flat(offsets, "offsets", torch.int32, (layer.experts + 1,), x)
-    if n > 1 and x.stride(0) < layer.k:
-        x = x.contiguous()
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(x, stream)
+    x = _apart(x)
+    fmt, n, pitch = _rows_of(x, "x", _CODE_TYPES, layer.k, device)
+    if layer.device != device:
+        raise ValueError(f"the weights are on cuda:{layer.device}, x on cuda:{device}")
+    s_x = _flat(scales, "scales", torch.float32, (n,), device)
     if out is None:
-        if stream is None:
-            out = torch.empty((n, layer.n), dtype=dtype, device=x.device)
-        else:
-            with _on(stream):
-                out = torch.empty((n, layer.n), dtype=dtype, device=x.device)
-    kind = _rows_of(out, "out", _TOKEN_TYPES, layer.n)
-    if out.shape[0] != n or out.device != x.device:
-        raise ValueError(f"out: expected {n} rows on {x.device}")
-    _no_broadcast(out, "out")
-    lib, px, pitch = load(), x.data_ptr(), _pitch(x)
+        out = _empty(x, (n, layer.n), dtype or torch.bfloat16, stream)
+    kind, out_rows, out_pitch = _rows_of(out, "out", _TOKEN_TYPES, layer.n, device)
+    if out_rows != n:
+        raise ValueError(f"out: expected {n} rows, got {out_rows}")
+    lib, px = _LIB or load(), x.data_ptr()
     ws, size = None, 0
-    if n > 8 and (fmt == CODES_I8 or pitch % 8 or px % 16) or n <= 8:
+    if n > 8 and not (fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0) or n * layer.k > 65536:
         need = ctypes.c_size_t()
         _check(lib.hatq_linear_workspace(px, fmt, pitch, n, layer.ref, ctypes.byref(need)))
-        if need.value:
-            with _on(stream):
-                ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-            size = need.value
+        size = need.value
+        if size:
+            scratch = _empty(x, (size,), torch.uint8, stream)
+            ws = scratch.data_ptr()
     if offsets is None:
-        st = lib.hatq_linear(px, fmt, pitch, scales.data_ptr(), n, layer.ref, kind, out.data_ptr(), _pitch(out),
-                             None if ws is None else ws.data_ptr(), size, raw)
+        st = lib.hatq_linear(px, fmt, pitch, s_x, n, layer.ref, kind, out.data_ptr(), out_pitch, ws, size, raw)
     else:
-        st = lib.hatq_grouped_linear(px, fmt, pitch, scales.data_ptr(), n, offsets.data_ptr(), layer.ref, kind,
-                                     out.data_ptr(), _pitch(out), None if ws is None else ws.data_ptr(), size, raw)
+        st = lib.hatq_grouped_linear(px, fmt, pitch, s_x, n,
+                                     _flat(offsets, "offsets", torch.int32, (layer.experts + 1,), device), layer.ref,
+                                     kind, out.data_ptr(), out_pitch, ws, size, raw)
     if st:
         _check(st)
     return out
@@ -976,7 +978,7 @@ def linear(x, scales, layer, dtype=None, out=None, stream=None):
     in `dtype` (float32, float16, bfloat16 - the default) or into `out`."""
     if layer.grouped:
         raise ValueError("a layer with experts needs grouped_linear")
-    return _product(x, scales, None, layer, dtype or _token_torch().bfloat16, out, stream)
+    return _product(x, scales, None, layer, dtype, out, stream)
 
 
 def grouped_linear(x, scales, offsets, layer, dtype=None, out=None, stream=None):
@@ -984,31 +986,29 @@ def grouped_linear(x, scales, offsets, layer, dtype=None, out=None, stream=None)
     (offsets int32 [experts + 1] on the device). Rows that no expert holds are not written."""
     if offsets is None:
         raise ValueError("offsets are missing")
-    return _product(x, scales, offsets, layer, dtype or _token_torch().bfloat16, out, stream)
+    return _product(x, scales, offsets, layer, dtype, out, stream)
 
 
 def combine_rows(y, index, weights, out=None, stream=None):
     """hatq_combine_rows: out[t] = sum_j weights[t][j] y[index[t][j]] (int32 index, float32 weights,
     both [tokens][topk]; an index outside y contributes nothing)."""
-    torch = _token_torch()
-    kind = _rows_of(y, "y", _TOKEN_TYPES)
-    raw = _launch_stream(y, stream)
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(y, stream)
+    y = _apart(y)
+    kind, rows, pitch = _rows_of(y, "y", _TOKEN_TYPES, None, device)
     if index.dim() != 2:
         raise ValueError(f"index: shape {tuple(index.shape)}, expected [tokens, topk]")
     t, topk = index.shape
-    _flat(index, "index", torch.int32, (t, topk), y)
-    _flat(weights, "weights", torch.float32, (t, topk), y)
     c = y.shape[1]
     if out is None:
-        with _on(stream):
-            out = torch.empty((t, c), dtype=y.dtype, device=y.device)
-    if _rows_of(out, "out", _TOKEN_TYPES, c) != kind or out.shape[0] != t or out.device != y.device:
-        raise ValueError(f"out: expected {t} rows of {y.dtype} on {y.device}")
-    _no_broadcast(out, "out")
-    if y.shape[0] > 1 and y.stride(0) < c:
-        y = y.contiguous()
-    st = load().hatq_combine_rows(y.data_ptr(), kind, _pitch(y), y.shape[0], index.data_ptr(), weights.data_ptr(), t,
-                                  topk, c, out.data_ptr(), _pitch(out), raw)
+        out = _empty(y, (t, c), y.dtype, stream)
+    out_kind, out_rows, out_pitch = _rows_of(out, "out", _TOKEN_TYPES, c, device)
+    if out_kind != kind or out_rows != t:
+        raise ValueError(f"out: expected {t} rows of {y.dtype}, got {out_rows} of {out.dtype}")
+    st = (_LIB or load()).hatq_combine_rows(y.data_ptr(), kind, pitch, rows,
+                                            _flat(index, "index", torch.int32, (t, topk), device),
+                                            _flat(weights, "weights", torch.float32, (t, topk), device), t, topk, c,
+                                            out.data_ptr(), out_pitch, raw)
     if st:
         _check(st)
     return out

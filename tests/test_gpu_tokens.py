@@ -354,6 +354,34 @@ def test_quantize_activations(act, gated, rows, c, hb):
         check_quantized(x, q, s, hb, act, gated)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,c,hb", [(3, 32768, 256), (2, 9000, 8), (700, 8192, 128), (900, 2050, 2)])
+def test_quantize_wide_gated_rows(dtype, rows, c, hb):
+    x = torch.randn(rows, 2 * c, generator=gen(69), device="cuda").to(TYPES[dtype])
+    q, s = H.quantize_tokens(x, hb=hb, act="silu", gated=True)
+    finish()
+    check_quantized(x, q, s, hb, "silu", True)
+
+
+@pytest.mark.parametrize("rows,c,hb", [(20_000, 64, 64), (9_001, 200, 8), (5_000, 1000, 8), (3_001, 4096, 256), (2_000, 8192, 32),
+                                       (500, 16384, 128)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_quantize_many_rows(rows, c, hb, dtype):
+    """More rows than the GPU holds at once, gathered in part, a few of them empty or not finite."""
+    x = torch.randn(rows, c, generator=gen(75), device="cuda").to(TYPES[dtype])
+    x[7], x[rows - 2, 0] = 0, math.nan
+    index = torch.randint(-1, rows + 1, (rows,), generator=gen(76), device="cuda").to(torch.int32)
+    for at in (None, index):
+        for kind in CODES:
+            q, s = H.quantize_tokens(x, hb=hb, codes=kind, rows=at)
+            finish()
+            bad = s.isnan()
+            source = torch.arange(rows, device="cuda") if at is None else at.long()
+            assert torch.equal(bad, source == rows - 2) and bool((q[bad] == 0).all())
+            keep = torch.where(~bad)[0]
+            check_quantized(x, q[keep], s[keep], hb, rows=source[keep])
+
+
 @pytest.mark.parametrize("gated", [False, True])
 def test_quantize_gathers_rows(gated):
     x = torch.randn(50, 256 * (1 + gated), generator=gen(63), device="cuda").bfloat16()
