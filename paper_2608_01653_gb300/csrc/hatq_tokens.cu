@@ -88,11 +88,9 @@ template <> __device__ __forceinline__ pair32 widen2<__half>(uint32_t w) {
     return pack2(f.x, f.y);
 }
 
-__device__ __forceinline__ float activate(float v, int act) {
-    if (act == HATQ_ACT_RELU) return v < 0.0f ? 0.0f : v;               // keeps a NaN
-    if (act == HATQ_ACT_SILU) return v / (1.0f + expf(-v));
-    return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-}
+__device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }               // keeps a NaN
+__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + expf(-v)); }    // the quotient within 2 ulp
+__device__ __forceinline__ float gelu(float v) { return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f)); }
 
 // A row's threads: tpr, a power of two below a warp (a warp then holds 32 / tpr rows) or whole warps.
 struct Lanes {
@@ -124,17 +122,17 @@ __device__ __forceinline__ void store_piece(E *p, int have, bool vec, const uint
         if (j < have) p[j] = e[j];
 }
 
-// Where piece i of the warp's values lies: {row of the owner lane, first element}, and its place in the buffer.
+// Piece i of the warp's values, IN of them: the first one's place in the row, and the piece's in the buffer.
 template <int PER, int IN>
 __device__ __forceinline__ int piece_first(const Lanes &l, int i) {
     constexpr int kPieces = PER / IN;
     const int at = i * 32 + l.lane;
     return l.tpr >= 32 ? (l.t - l.lane) * PER + at * IN : ((at / kPieces) & (l.tpr - 1)) * PER + (at % kPieces) * IN;
 }
-template <int PER, int IN>
-__device__ __forceinline__ int piece_at(const Lanes &l, int i) {
-    constexpr int kPieces = PER / IN;
-    return swizzle<kPieces>((i * 32 + l.lane) / kPieces, (i * 32 + l.lane) % kPieces);
+// swizzle() of piece i * 32 + lane, from that of piece `lane`
+template <int PIECES>
+__device__ __forceinline__ int piece_at(int at0, int i) {
+    return i * 32 + (PIECES == 8 && (i & 1) ? at0 ^ 4 : at0);
 }
 
 template <typename T, int PIECES>
@@ -150,14 +148,20 @@ __device__ __forceinline__ void widen(const uint4 (&w)[PIECES], pair32 (&v)[PIEC
     }
 }
 
-template <int PER>
-__device__ __forceinline__ void activate_all(pair32 (&v)[PER / 2], int act) {
+template <int PER, typename F>
+__device__ __forceinline__ void map_all(pair32 (&v)[PER / 2], F f) {
 #pragma unroll
     for (int i = 0; i < PER / 2; ++i) {
         float x, y;
         unpack2(v[i], x, y);
-        v[i] = pack2(activate(x, act), activate(y, act));
+        v[i] = pack2(f(x), f(y));
     }
+}
+template <int PER>
+__device__ __forceinline__ void activate_all(pair32 (&v)[PER / 2], int act) {
+    if (act == HATQ_ACT_SILU) map_all<PER>(v, silu);
+    else if (act == HATQ_ACT_GELU) map_all<PER>(v, gelu);
+    else map_all<PER>(v, relu);
 }
 template <int PER>
 __device__ __forceinline__ void gate_all(pair32 (&v)[PER / 2], const pair32 (&u)[PER / 2]) {
@@ -193,7 +197,9 @@ __device__ __forceinline__ void transform(pair32 (&v)[PER / 2], int hb, int t) {
             }
         }
     }
-    for (int m = 1; m * PER < hb; m <<= 1) {
+#pragma unroll
+    for (int m = 1; m <= 128 / PER; m <<= 1) {
+        if (m * PER >= hb) break;
         const float sign = (t & m) != 0 ? -1.0f : 1.0f;
         const pair32 sign2 = pack2(sign, sign);
 #pragma unroll
@@ -323,6 +329,12 @@ __device__ __forceinline__ void copy_async(uint4 *dst, const void *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src)
                  : "memory");
 }
+// the first `bytes` of the 16, zeros behind them
+__device__ __forceinline__ void copy_async_part(uint4 *dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "r"(bytes)
+                 : "memory");
+}
 template <int AHEAD> __device__ __forceinline__ void copies_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
 }
@@ -351,19 +363,45 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
         int src = row < a.rows ? (a.index ? a.index[row] : (int)row) : -1;
         return src >= a.src_rows ? -1 : src;
     };
+    // a warp whose values are all there, in 16-byte pieces, needs no look at a piece
+    const int warp_first = (l.t - l.lane) * kPer;
+    const bool wide = a.vec && tpr >= 32, whole = wide && warp_first + 32 * kPer <= a.c;
+    const int in_at = swizzle<kPieces>(l.lane / kPieces, l.lane % kPieces);
+    const int out_at = swizzle<kOutPieces>(l.lane / kOutPieces, l.lane % kOutPieces);
     auto issue = [&](int src, uint4 *buffer, int half) {
+        if (wide) {
+            // pieces of one row, 32 lanes next to each other; behind its end (or in an empty row) they are zeros
+            const T *p = reinterpret_cast<const T *>(a.x) + (long long)max(src, 0) * a.ldx + half * a.c;
+            const int first = warp_first + l.lane * kIn;
 #pragma unroll 1
-        for (int h = half; h < half + halves; ++h) {
+            for (int h = 0; h < halves; ++h) {
+                if (whole && src >= 0) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int first = piece_first<kPer, kIn>(l, i);
-                const int from = l.tpr >= 32 ? src : __shfl_sync(0xffffffffu, src, (i * 32 + l.lane) / kPieces);
-                const T *p = reinterpret_cast<const T *>(a.x) + (long long)max(from, 0) * a.ldx + h * a.c + first;
-                const int have = from < 0 ? 0 : a.c - first;
-                uint4 *dst = buffer + (h - half) * 32 * kPieces + piece_at<kPer, kIn>(l, i);
-                if (a.vec && have >= kIn) copy_async(dst, p);
-                else *dst = load_piece<T, kIn>(p, have, false);
+                    for (int i = 0; i < kPieces; ++i)
+                        copy_async(buffer + piece_at<kPieces>(in_at, i), p + first + i * 32 * kIn);
+                } else {
+                    const int end = src >= 0 ? a.c : 0;
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int at = first + i * 32 * kIn, have = min(max(end - at, 0), kIn);
+                        copy_async_part(buffer + piece_at<kPieces>(in_at, i), p + min(at, a.c - 1), have * (int)sizeof(T));
+                    }
+                }
+                buffer += 32 * kPieces;
+                p += a.c;
             }
+            return;
+        }
+#pragma unroll 1
+        for (int hi = 0; hi < halves * kPieces; ++hi) {
+            const int h = hi / kPieces, i = hi % kPieces;
+            const int first = piece_first<kPer, kIn>(l, i);
+            const int from = l.tpr >= 32 ? src : __shfl_sync(0xffffffffu, src, (i * 32 + l.lane) / kPieces);
+            const T *p = reinterpret_cast<const T *>(a.x) + (long long)max(from, 0) * a.ldx + (half + h) * a.c + first;
+            const int have = from < 0 ? 0 : a.c - first;
+            uint4 *dst = buffer + h * 32 * kPieces + piece_at<kPieces>(in_at, i);
+            if (a.vec && have >= kIn) copy_async(dst, p);
+            else *dst = load_piece<T, kIn>(p, have, false);
         }
     };
     int srcs[STAGES];
@@ -421,12 +459,32 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
 #pragma unroll
         for (int i = 0; i < kOutPieces; ++i) stage[swizzle<kOutPieces>(l.lane, i)] = out.p[i];
         __syncwarp();
+        E *codes = reinterpret_cast<E *>(a.codes);
+        if (wide) {
+            const int first = warp_first + l.lane * kOutIn;
+            E *p = codes + l.row * a.ldc + first;
+            if (l.row < a.rows) {
 #pragma unroll
-        for (int i = 0; i < kOutPieces; ++i) {
-            const int from = piece_first<kPer, kOutIn>(l, i);
-            const long long row = l.tpr >= 32 ? l.row : l.row - l.lane / l.tpr + (i * 32 + l.lane) / kOutPieces / l.tpr;
-            store_piece<E, kOutIn>(reinterpret_cast<E *>(a.codes) + row * a.ldc + from, row < a.rows ? a.c - from : 0, a.vec,
-                                   stage[piece_at<kPer, kOutIn>(l, i)]);
+                for (int i = 0; i < kOutPieces; ++i)
+                    if (first + i * 32 * kOutIn + kOutIn <= a.c)
+                        *reinterpret_cast<uint4 *>(p + i * 32 * kOutIn) = stage[piece_at<kOutPieces>(out_at, i)];
+                if (!whole && a.c % kOutIn != 0) {
+                    // the row's last values fill no piece: the lane that has it stores them one by one
+#pragma unroll 1
+                    for (int i = 0; i < kOutPieces; ++i)
+                        if (first + i * 32 * kOutIn < a.c)
+                            store_piece<E, kOutIn>(p + i * 32 * kOutIn, min(a.c - first - i * 32 * kOutIn, kOutIn - 1), false,
+                                                   stage[piece_at<kOutPieces>(out_at, i)]);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < kOutPieces; ++i) {
+                const int from = piece_first<kPer, kOutIn>(l, i);
+                const long long row = l.tpr >= 32 ? l.row : l.row - l.lane / l.tpr + (i * 32 + l.lane) / kOutPieces / l.tpr;
+                store_piece<E, kOutIn>(codes + row * a.ldc + from, row < a.rows ? a.c - from : 0, a.vec,
+                                       stage[piece_at<kOutPieces>(out_at, i)]);
+            }
         }
         __syncwarp();                                                    // the buffer is free for the next copies
         at = at + 1 == STAGES ? 0 : at + 1;
@@ -477,7 +535,7 @@ cudaError_t quantize_size(const TokenQuantArgs &a, cudaStream_t s) {
         if (sizeof(T) == 4 || a.gated) return quantize_rows_launch<T, F16, 1024, 1>(a, s);
         return quantize_rows_launch<T, F16, 1024, sizeof(T) == 4 ? 1 : 2>(a, s);
     }
-    return quantize_rows_launch<T, F16, 256, sizeof(T) == 4 ? 2 : 3>(a, s);
+    return quantize_rows_launch<T, F16, 256, 2>(a, s);
 }
 
 // ------------------------------------------------------------ weight layout
