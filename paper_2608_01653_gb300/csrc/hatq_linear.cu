@@ -75,6 +75,16 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// whether the phase is over, without a wait
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 // without regard to the abort flag: before the CTA leaves, what it has in flight has to land
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
@@ -143,19 +153,17 @@ __device__ __forceinline__ void put(void *y, int type, long long at, float v) {
 template <int T, bool PAIR>
 struct Config {
     static constexpr int kCtas = PAIR ? 2 : 1;
-    // 64-code blocks per pipeline stage: with few tokens a block's MMAs are short and its hand-offs count
-    static constexpr int kSub = T / kCtas <= 64 ? 2 : 1;
+    // 64-code blocks per pipeline stage. The MMA warp's wait, fence and commit take about 300 cycles, so a stage
+    // holds enough blocks for its MMAs to take longer: one block per stage cost 480 cycles a block at any tile width.
+    static constexpr int kSub = T <= 64 ? 4 : 2;
     static constexpr int kXBytes = T / kCtas * 128;                    // one block's token codes
     static constexpr int kWOffset = kSub * kXBytes;
     static constexpr int kStageBytes = kSub * (kXBytes + kBlockBytes);
-    static constexpr int kFit = 200 * 1024 / kStageBytes;
-    static constexpr int kStages = kFit < 16 ? kFit : 16;
+    static constexpr int kStages = 204 * 1024 / kStageBytes;
     static constexpr int kSlotCols = 32 * kSub;                        // a widened block takes 32 columns
     static constexpr int kFree = (512 - 2 * T) / kSlotCols;
-    static constexpr int kSlots = kFree < kStages ? (kFree < 8 ? kFree : 8) : (kStages < 8 ? kStages : 8);
-    // warps that announce a widened stage: one set (the sets take turns) or both (a block each)
-    static constexpr int kWideWarps = (kSub == 2 ? 8 : 4) * kCtas;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + (kMaxExperts + 1) * 4 + 64;
+    static constexpr int kSlots = kFree < kStages ? kFree : kStages;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + (4 * kMaxExperts + 1) * 4 + 64;
     static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
     static_assert(kSlots >= 2 && kStages >= kSlots, "the barrier of a slot's last stage still has that phase");
     static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
@@ -180,7 +188,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto dempty = [&](int d) { return bar0 + 8u * (3 * C::kStages + 2 + d); };
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (3 * C::kStages + 4));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
-    int *tile_start = reinterpret_cast<int *>(bar_area + 1024);
+    // per expert: token tiles before it, its rows, its exact window
+    int *tile_start = reinterpret_cast<int *>(bar_area + 1024), *first_row = tile_start + kMaxExperts + 1,
+        *end_row = first_row + kMaxExperts, *window_of = end_row + kMaxExperts;
     __shared__ int warp_sums[kThreads / 32];
     __shared__ int s_skip;
 
@@ -197,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            mbar_init(wide(s), C::kWideWarps);
+            mbar_init(wide(s), 8 * C::kCtas);
         }
         for (int d = 0; d < 2; ++d) {
             mbar_init(dfull(d), 1);
@@ -218,15 +228,29 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
-    // token tiles before each expert's: two experts per thread, then the warps' sums
-    if (a.offsets) {
-        int c[2];
+    // two experts per thread, then the warps' sums
+    if (2 * threadIdx.x < a.experts) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = 2 * threadIdx.x + i;
-            c[i] = 0;
+            if (e < a.experts) {
+                // 64-code blocks of the longest window length that no channel's weights pass 2^24 in
+                const int bits = a.windows[e];
+                int j = 6;
+                while (j > 0 && (bits >> j & 1)) --j;
+                window_of[e] = 16 << j;
+            }
+        }
+    }
+    if (a.offsets) {
+        int c[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = 2 * threadIdx.x + i;
             if (e < a.experts) {
                 const int lo = min(max(a.offsets[e], 0), a.rows), hi = min(max(a.offsets[e + 1], 0), a.rows);
+                first_row[e] = lo;
+                end_row[e] = hi;
                 c[i] = hi > lo ? (hi - lo + T - 1) / T : 0;
             }
         }
@@ -243,8 +267,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (2 * threadIdx.x + 1 < a.experts) tile_start[2 * threadIdx.x + 2] = before + c[0] + c[1];
         if (threadIdx.x == 0) tile_start[0] = 0;
     } else if (threadIdx.x == 0) {
-        tile_start[0] = 0;
+        tile_start[0] = first_row[0] = 0;
         tile_start[1] = (a.rows + T - 1) / T;
+        end_row[0] = a.rows;
     }
     tc_fence_before();
     __syncthreads();
@@ -262,36 +287,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int kb0 = (int)((long long)units * part / parts) * C::kSub;
     const int kb1 = min((int)((long long)units * (part + 1) / parts) * C::kSub, a.kb);
 
+    // A CTA's tiles come in order, so each role walks the experts along with them. Within an expert: all its token
+    // tiles under kRasterN channel tiles, then the next channel tiles, so that weights and codes are taken from L2.
+    int expert = 0;
     auto decode = [&](int t) {
-        int lo = 0, hi = a.experts;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (tile_start[mid] * pairs_n <= t) lo = mid;
-            else hi = mid;
-        }
-        const int tokens = tile_start[lo + 1] - tile_start[lo];
-        const int local = t - tile_start[lo] * pairs_n;
+        while (tile_start[expert + 1] * pairs_n <= t) ++expert;
+        const int tokens = tile_start[expert + 1] - tile_start[expert];
+        const int local = t - tile_start[expert] * pairs_n;
         const int sweep = local / (kRasterN * tokens), rest = local - sweep * kRasterN * tokens;
         const int width = min(kRasterN, pairs_n - sweep * kRasterN);
         const int mt = rest / width;
-        int r0 = 0, r1 = a.rows;
-        if (a.offsets) {
-            r0 = min(max(a.offsets[lo], 0), a.rows);
-            r1 = min(max(a.offsets[lo + 1], 0), a.rows);
-        }
         Tile tile;
-        tile.e = lo;
-        tile.row = r0 + mt * T;
-        tile.rows = min(T, r1 - tile.row);
+        tile.e = expert;
+        tile.row = first_row[expert] + mt * T;
         tile.ch = (sweep * kRasterN + rest - mt * width) * C::kCtas;
+        tile.rows = min(T, end_row[expert] - tile.row);
         return tile;
-    };
-    // 64-code blocks of an exact fp32 window of this expert
-    auto window = [&](int e) {
-        const int bits = a.windows[e];
-        int j = 6;
-        while (j > 0 && (bits >> j & 1)) --j;
-        return 16 << j;
     };
 
     bool ok = true;
@@ -314,11 +325,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!ok) break;
                     if (elect_one()) {
                         const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
-                        const bool both = C::kSub == 2 && b + 1 < kb1;
-                        mbar_expect_tx(full(s), both ? C::kStageBytes : C::kXBytes + kBlockBytes);
-                        bulk_load(st + C::kWOffset, w, both ? 2 * kBlockBytes : kBlockBytes, full(s));
-                        tma_load_2d(st, &tmX, full(s), b * 64, row);
-                        if (both) tma_load_2d(st + C::kXBytes, &tmX, full(s), b * 64 + 64, row);
+                        const int blocks = min(C::kSub, kb1 - b);
+                        mbar_expect_tx(full(s), (uint32_t)(blocks * (C::kXBytes + kBlockBytes)));
+                        bulk_load(st + C::kWOffset, w, (uint32_t)(blocks * kBlockBytes), full(s));
+#pragma unroll
+                        for (int q = 0; q < C::kSub; ++q)
+                            if (q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
                     }
                     __syncwarp();
                     w += C::kSub * kBlockBytes;
@@ -337,8 +349,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t bd0 = sdesc_sw128(stage0);
             int s = 0, slot = 0, cc = 0;
             uint32_t ph = 0;
+            bool ready = false;
             for (int t = first; t < total && ok; t += step) {
-                const int win = window(decode(t).e);
+                const int win = window_of[decode(t).e];
                 for (int b = kb0; b < kb1 && ok;) {
                     const int end = min(kb1, (b / win + 1) * win);      // one exact window, one accumulator
                     const int d = cc & 1;
@@ -346,31 +359,37 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ok = __all_sync(0xffffffffu, ok);
                     uint32_t acc = 0;
                     for (; b < end && ok; b += C::kSub) {
-                        ok = mbar_wait(full(s), ph, abort_flag, a.err) && mbar_wait(wide(s), ph, abort_flag, a.err);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t bd = bd0 + (uint64_t)(s * (C::kStageBytes >> 4));
-                            const uint32_t at = tmem + (uint32_t)(2 * T + slot * C::kSlotCols);
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 8 * q, bd + 2 * q, idesc, acc | (uint32_t)q);
-                            if (C::kSub == 2 && b + 1 < end) {
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 32 + 8 * q, bd + (C::kXBytes >> 4) + 2 * q, idesc, 1);
-                            }
-                            commit<PAIR>(empty(s));
-                            if (b + C::kSub >= end) commit<PAIR>(dfull(d));
+                        // The widening warps waited for the stage's copies, so their arrival speaks for both operands.
+                        if (!ready) {
+                            ok = mbar_wait(wide(s), ph, abort_flag, a.err);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (!ok) break;
                         }
-                        __syncwarp();
-                        acc = 1;
-                        ++issued;
+                        const int now = s, at_slot = slot;
                         if (++slot == C::kSlots) slot = 0;
                         if (++s == C::kStages) {
                             s = 0;
                             ph ^= 1u;
                         }
+                        const bool next = mbar_test(wide(s), ph);       // looked at early: its answer takes a while
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t bd = bd0 + (uint64_t)(now * (C::kStageBytes >> 4));
+                            const uint32_t at = tmem + (uint32_t)(2 * T + at_slot * C::kSlotCols);
+#pragma unroll
+                            for (int j = 0; j < C::kSub; ++j) {
+                                if (j > 0 && b + j >= end) break;
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 32 * j + 8 * q,
+                                                 bd + (uint64_t)(j * (C::kXBytes >> 4) + 2 * q), idesc, acc | (uint32_t)(j + q));
+                            }
+                            commit<PAIR>(empty(now));
+                            if (b + C::kSub >= end) commit<PAIR>(dfull(d));
+                        }
+                        ready = __all_sync(0xffffffffu, next);
+                        acc = 1;
+                        ++issued;
                     }
                     ++cc;
                 }
@@ -384,64 +403,61 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp < 12) {
         regs_dec<kRegsWiden>();
-        const int set = (warp >> 2) - 1;                                // takes the blocks with it % 2 == set
+        const int set = (warp >> 2) - 1;                                // takes every other block of a stage
         const int m = (warp & 3) * 32 + lane;                           // channel of the tile = tensor-memory lane
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T;
-        // One block per stage: this set's stages are it = set, set + 2, ..; two: every stage, and of each this set's
-        // block. ps is the stage that used the slot before, it - kSlots.
-        constexpr int kTurn = C::kSub == 2 ? 1 : 2;
-        auto ahead = [](int &x, uint32_t &phase, int by, int size) {
-            x += by;
-            if (x >= size) {
-                x -= size;
-                phase ^= 1u;
-            }
-        };
         const int tiles = total > first ? (total - first + step - 1) / step : 0;
-        const int per_tile = (kb1 - kb0 + C::kSub - 1) / C::kSub;
-        const bool odd = C::kSub == 2 && (kb1 - kb0) % 2 != 0;           // a tile's last stage has one block
+        const int per_tile = (kb1 - kb0 + C::kSub - 1) / C::kSub, last = kb1 - kb0 - (per_tile - 1) * C::kSub;
         const long long stages = (long long)tiles * per_tile;
-        const int start = C::kSub == 2 ? 0 : set;
-        int s = start, slot = start, ps = C::kSub == 2 ? 0 : (set + C::kSlots) & 1, left = per_tile;
-        uint32_t ph = 0, pph = 0, unused = 0;
-        for (long long it = start; it < stages; it += kTurn) {
+        int s = 0, slot = 0, prior = 0, left = per_tile;                // prior: the stage that used the slot before
+        uint32_t ph = 0, prior_ph = 0;
+        for (long long it = 0; it < stages; ++it) {
+            int blocks = C::kSub;
+            if (--left == 0) {
+                left = per_tile;
+                blocks = last;
+            }
             ok = mbar_wait(full(s), ph, abort_flag, a.err);
             if (ok && it >= C::kSlots) {
-                ok = mbar_wait(empty(ps), pph, abort_flag, a.err);
-                ahead(ps, pph, kTurn, C::kStages);
+                ok = mbar_wait(empty(prior), prior_ph, abort_flag, a.err);
+                if (++prior == C::kStages) {
+                    prior = 0;
+                    prior_ph ^= 1u;
+                }
             }
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            bool mine = true;
-            if (C::kSub == 2) {
-                mine = !(odd && left == 1 && set == 1);
-                if (--left == 0) left = per_tile;
-            }
-            if (mine) {
-                const uint8_t *src = smem + s * C::kStageBytes + C::kWOffset + (C::kSub == 2 ? set * kBlockBytes : 0) + m * 16;
+            tc_fence_after();
+#pragma unroll
+            for (int j = 0; j < C::kSub / 2; ++j) {
+                const int block = 2 * j + set;
+                if (block >= blocks) break;
+                const uint8_t *src = smem + s * C::kStageBytes + C::kWOffset + block * kBlockBytes + m * 16;
                 uint32_t h[32];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(src + j * 2048);
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + i * 2048);
                     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        h[8 * j + 2 * q] = hsub2(prmt(w[q], 0x64646464u, 0x4140u), 0x64806480u);
-                        h[8 * j + 2 * q + 1] = hsub2(prmt(w[q], 0x64646464u, 0x4342u), 0x64806480u);
+                        h[8 * i + 2 * q] = hsub2(prmt(w[q], 0x64646464u, 0x4140u), 0x64806480u);
+                        h[8 * i + 2 * q + 1] = hsub2(prmt(w[q], 0x64646464u, 0x4342u), 0x64806480u);
                     }
                 }
-                tc_fence_after();
-                tmem_st32(t_lane + (uint32_t)(slot * C::kSlotCols + (C::kSub == 2 ? set * 32 : 0)), h);
-                tmem_wait_st();
-                tc_fence_before();
+                tmem_st32(t_lane + (uint32_t)(slot * C::kSlotCols + block * 32), h);
             }
+            tmem_wait_st();
+            tc_fence_before();
             __syncwarp();
             if (lane == 0) {
                 if (PAIR) mbar_arrive_remote(map_shared(wide(s), 0));
                 else mbar_arrive(wide(s));
             }
-            ahead(s, ph, kTurn, C::kStages);
-            ahead(slot, unused, kTurn, C::kSlots);
+            if (++slot == C::kSlots) slot = 0;
+            if (++s == C::kStages) {
+                s = 0;
+                ph ^= 1u;
+            }
         }
         __syncwarp();
         if (!PAIR && parts > 1) {
@@ -465,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         for (int t = first; t < total && ok; t += step) {
             const Tile tile = decode(t);
-            const int win = window(tile.e);
+            const int win = window_of[tile.e];
             const int ch = (tile.ch + (int)in_pair) * kRowTile + m;
             const bool live = ch < a.n;
             const float sw = live ? a.s_w[(long long)tile.e * a.n + ch] : 0.0f;
