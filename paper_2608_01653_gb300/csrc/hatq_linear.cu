@@ -171,6 +171,8 @@ struct Config {
 
 struct Tile {
     int e, row, rows, ch;              // expert, first row, rows of the tile, first channel tile
+    // columns that are multiplied: an expert's last tile may hold few rows
+    __device__ __forceinline__ int columns() const { return (rows + 31) & ~31; }
 };
 
 template <int T, bool PAIR>
@@ -202,7 +204,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (threadIdx.x == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
-        s_skip = *reinterpret_cast<volatile int *>(a.err);
         *abort_flag = 0;
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
@@ -228,6 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
+    after_prior_kernels();
+    if (threadIdx.x == 0) s_skip = *reinterpret_cast<volatile int *>(a.err);
     // two experts per thread, then the warps' sums
     if (2 * threadIdx.x < a.experts) {
 #pragma unroll
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // a pair's second half may lie behind the last channel tile: any block does, nothing of it is stored
                 const int ct = min(tile.ch + (int)in_pair, a.n_tiles - 1);
                 const uint8_t *w = a.w + (((long long)tile.e * a.n_tiles + ct) * a.kb + kb0) * kBlockBytes;
-                const int row = tile.row + (int)in_pair * (T / C::kCtas);
+                const int row = tile.row + (int)in_pair * (tile.columns() / 2);      // a pair's second half of the tokens
                 for (int b = kb0; b < kb1; b += C::kSub) {
                     ok = mbar_wait(empty(s), ph, abort_flag, a.err);
                     ok = __all_sync(0xffffffffu, ok);
@@ -345,13 +348,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = max(0, issued - C::kStages); i < issued; ++i)
                     mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
         } else if (warp == 1 && in_pair == 0) {
-            const uint32_t idesc = (1u << 4) | ((uint32_t)(T >> 3) << 17) | ((uint32_t)(C::kCtas * 128 >> 4) << 24);
             const uint64_t bd0 = sdesc_sw128(stage0);
             int s = 0, slot = 0, cc = 0;
             uint32_t ph = 0;
             bool ready = false;
             for (int t = first; t < total && ok; t += step) {
-                const int win = window_of[decode(t).e];
+                const Tile tile = decode(t);
+                const int win = window_of[tile.e];
+                const uint32_t idesc =
+                    (1u << 4) | ((uint32_t)(tile.columns() >> 3) << 17) | ((uint32_t)(C::kCtas * 128 >> 4) << 24);
                 for (int b = kb0; b < kb1 && ok;) {
                     const int end = min(kb1, (b / win + 1) * win);      // one exact window, one accumulator
                     const int d = cc & 1;
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll 1
-                for (int g = 0; g < kHalf; g += 16) {
+                for (int g = 0; g < kHalf && half * kHalf + g < tile.rows; g += 16) {
                     uint32_t r[16];
                     tmem_ld16(t_lane + (uint32_t)((cc & 1) * T + g), r);
                     tmem_wait_ld();
@@ -632,13 +637,14 @@ cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cud
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::kSmem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)width;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0] = early_start();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)width;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = width > 1 ? 1 : 0;
+    cfg.numAttrs = width > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, linear_tc_kernel<T, PAIR>, tm, a);
 }
 

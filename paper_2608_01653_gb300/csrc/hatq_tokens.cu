@@ -288,6 +288,7 @@ __global__ void __launch_bounds__(1024) quantize_few_kernel(const __grid_constan
     __shared__ float warp_max[32];
     const int rl = threadIdx.x / tpr, lane = threadIdx.x & 31, t = threadIdx.x - rl * tpr;
     const long long row = (long long)blockIdx.x * (blockDim.x / tpr) + rl;
+    after_prior_kernels();
     int src = row < a.rows ? (a.index ? a.index[row] : (int)row) : -1;
     if (src >= a.src_rows) src = -1;
     const int have = src < 0 ? 0 : a.c - t * kPer;
@@ -404,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
             else *dst = load_piece<T, kIn>(p, have, false);
         }
     };
+    after_prior_kernels();
     int srcs[STAGES];
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
@@ -519,8 +521,7 @@ cudaError_t quantize_rows_launch(const TokenQuantArgs &a, cudaStream_t s) {
     // as many CTAs as are resident at once: they walk the rows
     const int fit = max(1, min(min(2048 / threads, 220 * 1024 / (smem + 1024)), 65536 / (regs * threads)));
     const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * fit;
-    k<<<(unsigned)(ctas < room ? ctas : room), threads, smem, s>>>(a, tpr);
-    return cudaGetLastError();
+    return launch_early(k, dim3((unsigned)(ctas < room ? ctas : room)), threads, smem, s, a, tpr);
 }
 
 template <typename T, bool F16>
@@ -528,8 +529,8 @@ cudaError_t quantize_size(const TokenQuantArgs &a, cudaStream_t s) {
     // few rows: as long as one CTA wave of 8-value threads holds them
     if (a.c <= 8192 && a.rows * a.c <= (long long)a.sms * 1024 * 8) {
         const int tpr = threads_per_row(a.c, 8), per_cta = tpr >= 256 ? 1 : 256 / tpr;
-        quantize_few_kernel<T, F16><<<(unsigned)((a.rows + per_cta - 1) / per_cta), per_cta * tpr, 0, s>>>(a, tpr);
-        return cudaGetLastError();
+        return launch_early(quantize_few_kernel<T, F16>, dim3((unsigned)((a.rows + per_cta - 1) / per_cta)), per_cta * tpr, 0, s,
+                            a, tpr);
     }
     if (a.c > 8192) {
         if (sizeof(T) == 4 || a.gated) return quantize_rows_launch<T, F16, 1024, 1>(a, s);
@@ -598,6 +599,7 @@ __global__ void __launch_bounds__(256) pack_codes_kernel(const void *x, int form
                                                          int k_pad, __half *out) {
     const int per_row = k_pad / 8;
     const long long total = rows * per_row;
+    after_prior_kernels();
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
         const long long r = i / per_row;
         const int c = (int)(i - r * per_row) * 8;
@@ -643,6 +645,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
     extern __shared__ __align__(16) uint8_t xs[];                       // [MT][k_pad] codes
     __shared__ int part[kFewThreads / 32][kFewCh][MT];
     const int k_pad = a.kb * 64;
+    after_prior_kernels();
     int e = 0, r0 = 0, r1 = a.rows;
     if (a.offsets) {
         // the expert of row blockIdx.y: as many experts end at or before it. The CTA takes the row and the next
@@ -750,6 +753,7 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const T *y, long long
     constexpr int kAhead = 8;
     const int per_row = (c + kVec - 1) / kVec;
     const long long total = tokens * per_row;
+    after_prior_kernels();
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
         const long long t = i / per_row;
         const int at = (int)(i - t * per_row) * kVec;
@@ -797,11 +801,8 @@ cudaError_t combine_launch(const void *y, long long ldy, long long rows, const i
     const int kvec = vec ? 16 / (int)sizeof(T) : 1;
     const long long blocks = (tokens * ((c + kvec - 1) / kvec) + 255) / 256;
     const unsigned grid = (unsigned)(blocks < (1LL << 30) ? blocks : (1LL << 30));
-    if (vec)
-        combine_rows_kernel<T, true><<<grid, 256, 0, s>>>((const T *)y, ldy, rows, index, weights, tokens, topk, c, (T *)out, ldo);
-    else
-        combine_rows_kernel<T, false><<<grid, 256, 0, s>>>((const T *)y, ldy, rows, index, weights, tokens, topk, c, (T *)out, ldo);
-    return cudaGetLastError();
+    return launch_early(vec ? combine_rows_kernel<T, true> : combine_rows_kernel<T, false>, dim3(grid), 256, 0, s, (const T *)y,
+                        ldy, rows, index, weights, tokens, topk, c, (T *)out, ldo);
 }
 
 }  // namespace
@@ -827,9 +828,8 @@ cudaError_t launch_linear_layout(const int8_t *w, long long ldw, int experts, in
 cudaError_t launch_pack_codes(const void *x, int format, long long ldx, long long rows, int k, int k_pad, void *out,
                               cudaStream_t s) {
     const long long blocks = (rows * (k_pad / 8) + 255) / 256;
-    pack_codes_kernel<<<(unsigned)(blocks < 152 * 32 ? blocks : 152 * 32), 256, 0, s>>>(x, format, ldx, rows, k, k_pad,
-                                                                                     (__half *)out);
-    return cudaGetLastError();
+    return launch_early(pack_codes_kernel, dim3((unsigned)(blocks < 152 * 32 ? blocks : 152 * 32)), 256, 0, s, x, format, ldx,
+                        rows, k, k_pad, (__half *)out);
 }
 
 cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
@@ -843,8 +843,7 @@ cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
         const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
     }
-    k<<<grid, kFewThreads, smem, s>>>(a);
-    return cudaGetLastError();
+    return launch_early(k, grid, kFewThreads, smem, s, a);
 }
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,

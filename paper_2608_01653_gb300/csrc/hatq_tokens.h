@@ -67,6 +67,35 @@ cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long lon
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
                                 bool vec, cudaStream_t s);
 
+// A kernel of this file's operators may be started while the one before it in
+// the stream is ending: it sets itself up and then waits here, before its first
+// access to global memory, until everything before it in the stream is done and
+// visible. From then on its own successor may be started the same way.
+#ifdef __CUDACC__
+__device__ __forceinline__ void after_prior_kernels() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+#endif
+inline cudaLaunchAttribute early_start() {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    return attr;
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t s, Args... args) {
+    cudaLaunchAttribute attr = early_start();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 // host services of hatq_api.cu
 int *device_error_word();
 CUresult encode_tiled_2d(CUtensorMap *tm, CUtensorMapDataType type, const void *base, unsigned long long inner,

@@ -46,22 +46,47 @@ constexpr long long kMaxPitch = 1LL << 32;
 struct Plan {
     bool few;        // the dot-product kernel
     int tokens;      // rows per pass of it, or per tile of the tensor-core kernel
-    bool pair;
+    bool pair;       // two CTAs per tile
+    int split;       // CTAs that share a tile's reduction
+    long long tiles;
 };
 
-// Which kernel: see hatq_tokens.cu and hatq_linear.cu for both.
-Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped) {
+// Which kernel (hatq_tokens.cu, hatq_linear.cu) and which tile. Up to 8 rows the dot-product kernel needs no
+// pipeline to fill: one row at 4096 x 4096 takes 3.8 us, the tensor-core kernel 8.1 us. Beyond, the tile with the
+// least estimated time: waves of tiles x blocks of the reduction x time per block, the last measured with every SM
+// at work (a wider tile costs more per block and less per product), and about 0.8 us to join a split reduction.
+Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms) {
     Plan p{};
-    const int k_pad = round_up(L->k, 64);
-    const int tokens = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
-    p.few = rows <= 8 && tokens * k_pad <= 96 * 1024;
+    const int k_pad = round_up(L->k, 64), kb = k_pad / 64, n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
+    const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    p.split = 1;
+    p.few = rows <= 8 && few * k_pad <= 96 * 1024;
     if (p.few) {
-        p.tokens = tokens;
+        p.tokens = few;
         return p;
     }
-    const long long per = grouped ? (rows + L->experts - 1) / L->experts : rows;
-    p.pair = per > 128;
-    p.tokens = per <= 32 ? 32 : per <= 64 ? 64 : per <= 128 ? 128 : 192;
+    static const struct { int tokens; bool pair; int ns; } options[] = {
+        {32, false, 127}, {64, false, 156}, {128, false, 230}, {128, true, 190}, {192, true, 255}};
+    const long long held = rows < L->experts ? rows : L->experts;
+    long long best = LLONG_MAX;
+    for (const auto &o : options) {
+        const int ctas = o.pair ? 2 : 1, room = sms / ctas;
+        // experts leave half a tile over each, and one tile at least
+        const long long full = (rows + o.tokens - 1) / o.tokens, ragged = rows / o.tokens + held / 2;
+        const long long tiles = (!grouped ? full : ragged > held ? ragged : held) * ((n_tiles + ctas - 1) / ctas);
+        for (int split = 1; split <= (o.pair ? 1 : 8); split *= 2) {
+            if (split > 1 && (tiles * split > room || kb / split < 4)) break;
+            const long long ns = (tiles * split + room - 1) / room * ((kb + split - 1) / split) * o.ns + (split > 1 ? 800 : 0);
+            if (ns < best) {
+                best = ns;
+                p.tokens = o.tokens;
+                p.pair = o.pair;
+                p.split = split;
+                // what the grid has to hold: every tile there may be, where a cluster takes only one
+                p.tiles = (full + (grouped ? held : 0)) * ((n_tiles + ctas - 1) / ctas);
+            }
+        }
+    }
     return p;
 }
 
@@ -93,11 +118,9 @@ bool direct(const void *x, int format, long long ldx) {
     return format == HATQ_CODES_F16 && ldx % 8 == 0 && aligned(x, 16);
 }
 
-hatq_status workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L,
-                         bool grouped, size_t *bytes) {
-    const Plan p = plan_of(rows, L, grouped);
-    *bytes = rows == 0 || p.few || direct(x, format, ldx) ? 0 : (size_t)rows * (size_t)round_up(L->k, 64) * 2;
-    return HATQ_OK;
+size_t workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L, bool grouped) {
+    if (rows == 0 || plan_of(rows, L, grouped, 152).few || direct(x, format, ldx)) return 0;
+    return (size_t)rows * (size_t)round_up(L->k, 64) * 2;
 }
 
 hatq_status product(const void *x, int format, long long ldx, const float *s_x, long long rows, const int32_t *offsets,
@@ -146,15 +169,14 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
     a.y_type = y_type;
     a.split = 1;
     a.slots = (int)(rows < L->experts ? rows : L->experts);
-    const Plan p = plan_of(rows, L, grouped);
+    const Plan p = plan_of(rows, L, grouped, sms);
     cudaError_t e;
     if (p.few) {
         if ((e = hatq::launch_linear_few(a, p.tokens, s)) != cudaSuccess) return cuda_fail(e, "product launch");
         return HATQ_OK;
     }
     if (!direct(x, format, ldx)) {
-        size_t need = 0;
-        workspace_of(x, format, ldx, rows, L, grouped, &need);
+        const size_t need = workspace_of(x, format, ldx, rows, L, grouped);
         if (!workspace || workspace_bytes < need)
             return fail(HATQ_ERR_INVALID_ARG, "the product needs a workspace of %zu bytes", need);
         if (!aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -165,18 +187,15 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
         a.format = HATQ_CODES_F16;
     }
     const int ctas = p.pair ? 2 : 1;
-    const long long token_tiles = (rows + p.tokens - 1) / p.tokens + (grouped ? a.slots : 0);
-    const long long tiles = token_tiles * ((a.n_tiles + ctas - 1) / ctas);
-    if (tiles > INT_MAX / 2) return fail(HATQ_ERR_UNSUPPORTED, "too many output tiles");
+    if (p.tiles > INT_MAX / 16) return fail(HATQ_ERR_UNSUPPORTED, "too many output tiles");
+    a.split = p.split;
     CUtensorMap tm;
     const CUresult r = hatq::encode_tiled_2d(&tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, (unsigned long long)a.k,
                                              (unsigned long long)rows, (unsigned long long)a.ldx * 2, 64,
                                              (unsigned)(p.tokens / ctas));
     if (r != CUDA_SUCCESS) return fail(HATQ_ERR_CUDA, "code tensor map encoding failed (%d)", (int)r);
-    if (!p.pair)
-        while (a.split < 8 && tiles * a.split * 2 <= sms && a.kb / (a.split * 2) >= 4) a.split *= 2;
-    const int room = sms / (p.pair ? 2 : 1);
-    const int clusters = a.split > 1 ? (int)tiles : (int)(tiles < room ? tiles : room);
+    const int room = sms / ctas;
+    const int clusters = a.split > 1 ? (int)p.tiles : (int)(p.tiles < room ? p.tiles : room);
     if ((e = hatq::launch_linear_tc(tm, a, p.tokens, p.pair, clusters, s)) != cudaSuccess)
         return cuda_fail(e, "product launch");
     return HATQ_OK;
@@ -264,9 +283,7 @@ hatq_status hatq_linear_workspace(const void *x, int format, long long ldx, long
     if (!is_codes(format)) return fail(HATQ_ERR_INVALID_ARG, "unknown code format %d", format);
     if (rows < 0) return fail(HATQ_ERR_INVALID_ARG, "negative row count");
     // the larger of what the dense and the grouped product want
-    size_t dense = 0, grouped = 0;
-    workspace_of(x, format, ldx, rows, L, false, &dense);
-    workspace_of(x, format, ldx, rows, L, true, &grouped);
+    const size_t dense = workspace_of(x, format, ldx, rows, L, false), grouped = workspace_of(x, format, ldx, rows, L, true);
     *bytes = dense > grouped ? dense : grouped;
     return HATQ_OK;
 }
