@@ -46,7 +46,7 @@ constexpr int kThreads = 640;
 // registers per thread of the five warpgroups: copies and MMAs, two of converters, two of the epilogue
 constexpr int kRegsIssue = 40, kRegsWiden = 72, kRegsOut = 144;
 constexpr int kRegShares = kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut;
-constexpr int kMaxSplit = 8;           // CTAs of one portable cluster
+constexpr int kMaxSplit = 4;           // CTAs that share a reduction at most
 constexpr int kRasterN = 8;            // channel tiles that share a sweep over the token tiles
 
 __device__ __forceinline__ uint32_t cluster_rank() {

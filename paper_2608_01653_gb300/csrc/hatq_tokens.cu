@@ -627,12 +627,16 @@ __global__ void __launch_bounds__(256) pack_codes_kernel(const void *x, int form
 
 // ------------------------------------------------------------ a few rows
 //
-// A CTA owns 8 channels of one group and the whole reduction; a warp takes
-// every 8th 64-code block, a lane 16 codes of one channel (8 lanes read 128
-// consecutive bytes). The weights' loads are issued before the rows' codes are
-// brought to shared memory, so both latencies run together. Sums are int32.
+// Bound by the weights' bytes and by latency: every load of weights that a
+// thread makes is on its way before the rows' codes are brought to shared
+// memory and before the first is used. A CTA owns 8 R channels of one group and
+// the whole reduction; a warp takes every 8th 64-code block, a lane 16 codes of
+// R channels (8 lanes read 128 consecutive bytes). Sums are int32 dot products
+// of four codes; this GPU issues them at a fraction of its other integer
+// instructions, so from three rows on they, not the bytes, are the bound, and
+// larger weights go to the tensor cores then (see plan_of).
 
-constexpr int kFewThreads = 256, kFewCh = 8;
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 
 __device__ __forceinline__ void store_y(void *y, int type, long long at, float v) {
     if (type == HATQ_F32) reinterpret_cast<float *>(y)[at] = v;
@@ -640,10 +644,19 @@ __device__ __forceinline__ void store_y(void *y, int type, long long at, float v
     else reinterpret_cast<__nv_bfloat16 *>(y)[at] = __float2bfloat16_rn(v);
 }
 
-template <int MT>
-__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArgs a) {
+// four fp16 codes as bytes: 1152 + code has code + 128 in its low byte
+__device__ __forceinline__ uint32_t narrow4(uint32_t x, uint32_t y) {
+    uint32_t a, b;
+    asm("add.f16x2 %0, %1, %2;" : "=r"(a) : "r"(x), "r"(0x64806480u));
+    asm("add.f16x2 %0, %1, %2;" : "=r"(b) : "r"(y), "r"(0x64806480u));
+    return __byte_perm(a, b, 0x6420) ^ 0x80808080u;
+}
+
+template <int MT, int R>
+__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_constant__ LinearArgs a) {
+    constexpr int kCh = 8 * R, kAhead = 8 / R;                          // channels of the CTA, blocks on their way
     extern __shared__ __align__(16) uint8_t xs[];                       // [MT][k_pad] codes
-    __shared__ int part[kFewThreads / 32][kFewCh][MT];
+    __shared__ int part[kFewWarps][kCh][MT];
     const int k_pad = a.kb * 64;
     after_prior_kernels();
     int e = 0, r0 = 0, r1 = a.rows;
@@ -659,84 +672,86 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
         r1 = min(min(max(a.offsets[e + 1], 0), a.rows), r0 + MT);
         if (r0 < lo || (r0 - lo) % MT != 0) return;
     }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int ch_l = lane & 7, j = lane >> 3;
-    const int ch0 = blockIdx.x * kFewCh;
-    const uint8_t *wp = a.w + ((long long)e * a.n_tiles + ch0 / kRowTile) * a.kb * kBlockBytes + j * 2048 +
-                        ((ch0 % kRowTile) + ch_l) * 16;
-    constexpr int kAhead = 8;
-    for (int base = r0; base < r1; base += MT) {
-        int acc[MT];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ch_l = lane & 7, j = lane >> 3;
+    const int ch0 = blockIdx.x * kCh;
+    const uint8_t *wp = a.w + (((long long)e * a.n_tiles + ch0 / kRowTile) * a.kb + warp) * kBlockBytes + j * 2048 +
+                        (ch0 % kRowTile + ch_l) * 16;
+    uint4 w[kAhead][R];
+    auto load = [&](int b, uint4 (&v)[R]) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = 0;
-        uint4 w[kAhead];
+        for (int r = 0; r < R; ++r)
+            v[r] = b < a.kb ? *reinterpret_cast<const uint4 *>(wp + (long long)(b - warp) * kBlockBytes + r * 128)
+                            : make_uint4(0, 0, 0, 0);
+    };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int b = warp + 8 * i;
-            w[i] = b < a.kb ? *reinterpret_cast<const uint4 *>(wp + (long long)b * kBlockBytes) : make_uint4(0, 0, 0, 0);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < MT * (k_pad / 16); i += kFewThreads) {
-            const int t = i / (k_pad / 16), c = (i - t * (k_pad / 16)) * 16;
-            const long long r = base + t;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            int8_t *b = reinterpret_cast<int8_t *>(&v);
-            if (r < r1) {
-                if (a.format == HATQ_CODES_I8) {
-                    const int8_t *p = reinterpret_cast<const int8_t *>(a.x) + r * a.ldx + c;
-                    if (c + 16 <= a.k && (reinterpret_cast<uintptr_t>(p) & 15) == 0) v = *reinterpret_cast<const uint4 *>(p);
-                    else
-                        for (int q = 0; q < 16; ++q) b[q] = c + q < a.k ? p[q] : 0;
+    for (int i = 0; i < kAhead; ++i) load(warp + i * kFewWarps, w[i]);
+    for (int i = threadIdx.x; i < MT * (k_pad / 16); i += kFewThreads) {
+        const int t = i / (k_pad / 16), c = (i - t * (k_pad / 16)) * 16;
+        const long long r = r0 + t;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        int8_t *b = reinterpret_cast<int8_t *>(&v);
+        if (r < r1) {
+            if (a.format == HATQ_CODES_I8) {
+                const int8_t *p = reinterpret_cast<const int8_t *>(a.x) + r * a.ldx + c;
+                if (c + 16 <= a.k && (reinterpret_cast<uintptr_t>(p) & 15) == 0) v = *reinterpret_cast<const uint4 *>(p);
+                else
+                    for (int q = 0; q < 16; ++q) b[q] = c + q < a.k ? p[q] : 0;
+            } else {
+                const __half *p = reinterpret_cast<const __half *>(a.x) + r * a.ldx + c;
+                if (c + 16 <= a.k && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+                    const uint4 lo = reinterpret_cast<const uint4 *>(p)[0], hi = reinterpret_cast<const uint4 *>(p)[1];
+                    v = make_uint4(narrow4(lo.x, lo.y), narrow4(lo.z, lo.w), narrow4(hi.x, hi.y), narrow4(hi.z, hi.w));
                 } else {
-                    const __half *p = reinterpret_cast<const __half *>(a.x) + r * a.ldx + c;
                     for (int q = 0; q < 16; ++q) b[q] = c + q < a.k ? (int8_t)__half2int_rn(p[q]) : 0;
                 }
             }
-            *reinterpret_cast<uint4 *>(xs + t * k_pad + c) = v;
         }
-        __syncthreads();
-        for (int b0 = warp;; ) {
+        *reinterpret_cast<uint4 *>(xs + t * k_pad + c) = v;
+    }
+    __syncthreads();
+    int acc[R][MT];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int b = b0 + 8 * i;
-                if (b < a.kb) {
-                    const uint32_t q[4] = {w[i].x ^ 0x80808080u, w[i].y ^ 0x80808080u, w[i].z ^ 0x80808080u,
-                                           w[i].w ^ 0x80808080u};
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(xs + t * k_pad + b * 64 + j * 16);
-                        acc[t] = __dp4a((int)q[0], (int)x.x, acc[t]);
-                        acc[t] = __dp4a((int)q[1], (int)x.y, acc[t]);
-                        acc[t] = __dp4a((int)q[2], (int)x.z, acc[t]);
-                        acc[t] = __dp4a((int)q[3], (int)x.w, acc[t]);
+        for (int t = 0; t < MT; ++t) acc[r][t] = 0;
+    for (int b0 = warp; b0 < a.kb; b0 += kFewWarps * kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int b = b0 + i * kFewWarps;
+            if (b < a.kb) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(xs + t * k_pad + b * 64 + j * 16);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        acc[r][t] = __dp4a((int)(w[i][r].x ^ 0x80808080u), (int)x.x, acc[r][t]);
+                        acc[r][t] = __dp4a((int)(w[i][r].y ^ 0x80808080u), (int)x.y, acc[r][t]);
+                        acc[r][t] = __dp4a((int)(w[i][r].z ^ 0x80808080u), (int)x.z, acc[r][t]);
+                        acc[r][t] = __dp4a((int)(w[i][r].w ^ 0x80808080u), (int)x.w, acc[r][t]);
                     }
                 }
-            }
-            b0 += 8 * kAhead;
-            if (b0 - warp >= a.kb) break;
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int b = b0 + 8 * i;
-                if (b < a.kb) w[i] = *reinterpret_cast<const uint4 *>(wp + (long long)b * kBlockBytes);
+                if (b + kFewWarps * kAhead < a.kb) load(b + kFewWarps * kAhead, w[i]);
             }
         }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            acc[t] += __shfl_xor_sync(0xffffffffu, acc[t], 8);
-            acc[t] += __shfl_xor_sync(0xffffffffu, acc[t], 16);
-            if (j == 0) part[warp][ch_l][t] = acc[t];
+            acc[r][t] += __shfl_xor_sync(0xffffffffu, acc[r][t], 8);
+            acc[r][t] += __shfl_xor_sync(0xffffffffu, acc[r][t], 16);
+            if (j == 0) part[warp][8 * r + ch_l][t] = acc[r][t];
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < kFewCh * MT; i += kFewThreads) {
-            const int t = i / kFewCh, c = i % kFewCh;
-            if (base + t < r1 && ch0 + c < a.n) {
-                int sum = 0;
-                for (int q = 0; q < kFewThreads / 32; ++q) sum += part[q][c][t];
-                const long long ch = (long long)e * a.n + ch0 + c;
-                float v = (float)sum * a.s_w[ch] * a.s_x[base + t];
-                if (a.bias) v += a.bias[ch];
-                store_y(a.y, a.y_type, (base + t) * a.ldy + ch0 + c, v);
-            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kCh * MT; i += kFewThreads) {
+        const int t = i / kCh, c = i % kCh;
+        if (r0 + t < r1 && ch0 + c < a.n) {
+            int sum = 0;
+            for (int q = 0; q < kFewWarps; ++q) sum += part[q][c][t];
+            const long long ch = (long long)e * a.n + ch0 + c;
+            float v = (float)sum * a.s_w[ch] * a.s_x[r0 + t];
+            if (a.bias) v += a.bias[ch];
+            store_y(a.y, a.y_type, (r0 + t) * a.ldy + ch0 + c, v);
         }
     }
 }
@@ -832,18 +847,28 @@ cudaError_t launch_pack_codes(const void *x, int format, long long ldx, long lon
                         rows, k, k_pad, (__half *)out);
 }
 
-cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
-    const dim3 grid((a.n + kFewCh - 1) / kFewCh, a.offsets ? a.rows : 1);
-    const int smem = tokens * a.kb * 64;
-    void (*k)(LinearArgs) = tokens == 1   ? linear_few_kernel<1>
-                            : tokens == 2 ? linear_few_kernel<2>
-                            : tokens == 4 ? linear_few_kernel<4>
-                                          : linear_few_kernel<8>;
+namespace {
+template <int MT, int R>
+cudaError_t few_launch(const LinearArgs &a, cudaStream_t s) {
+    const dim3 grid((a.n + 8 * R - 1) / (8 * R), a.offsets ? a.rows : 1);
+    const int smem = MT * a.kb * 64;
     if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        const cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<MT, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
     }
-    return launch_early(k, grid, kFewThreads, smem, s, a);
+    return launch_early(linear_few_kernel<MT, R>, grid, kFewThreads, smem, s, a);
+}
+}  // namespace
+
+// rows per pass: `tokens`. A short reduction leaves a thread few loads, so it takes two channels there.
+cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
+    const bool two = a.kb <= 4 * kFewWarps && (long long)a.n * (a.offsets ? a.rows : 1) >= 152 * 32;
+    switch (tokens) {
+        case 1: return two ? few_launch<1, 2>(a, s) : few_launch<1, 1>(a, s);
+        case 2: return two ? few_launch<2, 2>(a, s) : few_launch<2, 1>(a, s);
+        case 4: return few_launch<4, 1>(a, s);
+        default: return few_launch<8, 1>(a, s);
+    }
 }
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,

@@ -51,16 +51,21 @@ struct Plan {
     long long tiles;
 };
 
-// Which kernel (hatq_tokens.cu, hatq_linear.cu) and which tile. Up to 8 rows the dot-product kernel needs no
-// pipeline to fill: one row at 4096 x 4096 takes 3.8 us, the tensor-core kernel 8.1 us. Beyond, the tile with the
-// least estimated time: waves of tiles x blocks of the reduction x time per block, the last measured with every SM
-// at work (a wider tile costs more per block and less per product), and about 0.8 us to join a split reduction.
+// Which kernel (hatq_tokens.cu, hatq_linear.cu) and which tile. The dot-product kernel has no pipeline to fill, but
+// its instructions are slow and every CTA brings in all rows. Measured, against the tensor-core kernel: 4096 x 4096
+// with 1 / 4 / 8 rows 3.6 / 6.7 / 10.9 us against 8.1 .. 8.9; 4096 x 16384 with 2 / 4 rows 15 / 21 against 18.5;
+// 16384 x 4096 with 1 / 2 rows 14 / 23 against 16.6; experts of 2048 x 1536 with a row each, 8 / 16 / 24 of them,
+// 5.5 / 12 / 15 against 12 / 19 / 19. Of the tensor-core kernel's tiles the one with the least estimated time: waves
+// of tiles x blocks of the reduction x time per block, the last measured with every SM at work (a wider tile costs
+// more per block and less per product), and about 0.8 us to join a split reduction.
 Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms) {
     Plan p{};
     const int k_pad = round_up(L->k, 64), kb = k_pad / 64, n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
     const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
     p.split = 1;
-    p.few = rows <= 8 && few * k_pad <= 96 * 1024;
+    const long long weights = (long long)L->n * L->k;
+    p.few = few * k_pad <= 24 * 1024 &&
+            (grouped ? rows <= 24 : rows <= 2 || (rows <= 4 && weights <= 28'000'000) || (rows <= 8 && weights <= 13'000'000));
     if (p.few) {
         p.tokens = few;
         return p;
@@ -74,8 +79,9 @@ Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms
         // experts leave half a tile over each, and one tile at least
         const long long full = (rows + o.tokens - 1) / o.tokens, ragged = rows / o.tokens + held / 2;
         const long long tiles = (!grouped ? full : ragged > held ? ragged : held) * ((n_tiles + ctas - 1) / ctas);
-        for (int split = 1; split <= (o.pair ? 1 : 8); split *= 2) {
-            if (split > 1 && (tiles * split > room || kb / split < 4)) break;
+        // clusters of four leave a few SMs of each group of SMs idle, clusters of eight too many
+        for (int split = 1; split <= (o.pair ? 1 : 4); split *= 2) {
+            if (split > 1 && (tiles * split > (split == 4 ? room * 15 / 16 : room) || kb / split < 4)) break;
             const long long ns = (tiles * split + room - 1) / room * ((kb + split - 1) / split) * o.ns + (split > 1 ? 800 : 0);
             if (ns < best) {
                 best = ns;

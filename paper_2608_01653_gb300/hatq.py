@@ -903,7 +903,7 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
     """hatq_quantize_tokens: (codes, scales) of the rows of x ([rows][c], or [rows][2 c] when gated).
 
     rows: int32 [n], the source row of each output row (outside x: an empty row).
-    codes: "i8", "f16", or "auto": int8 for up to 8 rows (the dot-product kernel
+    codes: "i8", "f16", or "auto": int8 for up to 2 rows (the dot-product kernel
     reads them as they are), fp16 above (the tensor cores do). out / scales:
     tensors to write into; new codes come with a pitch that suits the products."""
     torch = _TORCH or _token_torch()
@@ -921,7 +921,7 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
     n = src_rows if rows is None else rows.shape[0]
     index = None if rows is None else _flat(rows, "rows", torch.int32, (n,), device)
     if codes == "auto":
-        codes = "i8" if n <= 8 else "f16"
+        codes = "i8" if n <= 2 else "f16"
     if out is None:
         pad = 16 if codes == "i8" else 8
         out = _empty(x, (n, -(-c // pad) * pad), torch.int8 if codes == "i8" else torch.float16, stream)
@@ -955,7 +955,7 @@ def _product(x, scales, offsets, layer, dtype, out, stream):
         raise ValueError(f"out: expected {n} rows, got {out_rows}")
     lib, px = _LIB or load(), x.data_ptr()
     ws, size = None, 0
-    if n > 8 and not (fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0) or n * layer.k > 65536:
+    if n > 2 and not (fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0):
         need = ctypes.c_size_t()
         _check(lib.hatq_linear_workspace(px, fmt, pitch, n, layer.ref, ctypes.byref(need)))
         size = need.value
