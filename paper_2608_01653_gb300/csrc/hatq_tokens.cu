@@ -89,7 +89,8 @@ template <> __device__ __forceinline__ pair32 widen2<__half>(uint32_t w) {
 }
 
 __device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }               // keeps a NaN
-__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + expf(-v)); }    // the quotient within 2 ulp
+// exp(-v) is off by about |v| + 2 ulp and counts with sigma (1 - sigma), so the product stays within a few ulp of |v|
+__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
 __device__ __forceinline__ float gelu(float v) { return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f)); }
 
 // A row's threads: tpr, a power of two below a warp (a warp then holds 32 / tpr rows) or whole warps.
@@ -925,66 +926,96 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
 
 // ------------------------------------------------------------ combine_rows
 
-// A thread owns 16 bytes of a token's row; the rows of up to eight slots are on their way at a time.
+// Bound by the rows' bytes. A thread owns 16 bytes of a token's row; the rows
+// of up to kAhead slots are on their way at a time, and the next token's indices
+// and weights before this one's rows are added up. Fewer slots leave room for
+// more threads.
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) combine_rows_kernel(const T *y, long long ldy, long long rows, const int32_t *index,
-                                                           const float *weights, long long tokens, int topk, int c, T *out,
-                                                           long long ldo) {
+constexpr int combine_ctas(int ahead) { return ahead == 8 ? 3 : ahead == 4 ? 4 : 6; }
+
+template <typename T, bool VEC, int kAhead>
+__global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel(const T *y, long long ldy, long long rows, const int32_t *index,
+                                                              const float *weights, long long tokens, int topk, int c, T *out,
+                                                              long long ldo, int width) {
     constexpr int kVec = VEC ? 16 / sizeof(T) : 1;
-    constexpr int kAhead = 8;
-    const int per_row = (c + kVec - 1) / kVec;
-    const long long total = tokens * per_row;
+    // width threads (a power of two) for a token, or for a part of its row
+    const int per_row = (c + kVec - 1) / kVec, parts = (per_row + width - 1) / width, per_cta = 256 / width;
+    const int slot = threadIdx.x / width, lane = threadIdx.x - slot * width;
+    const long long items = (tokens + per_cta - 1) / per_cta * parts;
+    int at_next = 0;
+    long long t_next = 0;
+    int idx[kAhead];
+    float w[kAhead];
+    auto fetch = [&](long long item, int j0) {
+        t_next = item / parts * per_cta + slot;
+        at_next = (int)(item % parts) * width + lane;
+        const bool live = item < items && t_next < tokens && at_next < per_row;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            idx[j] = live && j0 + j < topk ? index[t_next * topk + j0 + j] : -1;
+            w[j] = idx[j] >= 0 ? weights[t_next * topk + j0 + j] : 0.0f;
+        }
+    };
     after_prior_kernels();
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long t = i / per_row;
-        const int at = (int)(i - t * per_row) * kVec;
+    fetch(blockIdx.x, 0);
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const long long t = t_next;
+        const int at = at_next * kVec;
         float acc[kVec];
 #pragma unroll
         for (int q = 0; q < kVec; ++q) acc[q] = 0.0f;
         for (int j0 = 0; j0 < topk; j0 += kAhead) {
             uint4 v[kAhead];
-            float w[kAhead];
+            float p[kAhead];
             bool have[kAhead];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
-                const long long r = j0 + j < topk ? index[t * topk + j0 + j] : -1;
-                have[j] = r >= 0 && r < rows;
-                w[j] = have[j] ? weights[t * topk + j0 + j] : 0.0f;
+                have[j] = idx[j] >= 0 && idx[j] < rows;
+                p[j] = w[j];
                 if (have[j]) {
-                    if (VEC) v[j] = *reinterpret_cast<const uint4 *>(y + r * ldy + at);
-                    else *reinterpret_cast<T *>(&v[j]) = y[r * ldy + at];
+                    const T *from = y + (long long)idx[j] * ldy + at;
+                    if (VEC) v[j] = *reinterpret_cast<const uint4 *>(from);
+                    else *reinterpret_cast<T *>(&v[j]) = *from;
                 }
             }
+            if (j0 + kAhead < topk) fetch(item, j0 + kAhead);
+            else fetch(item + gridDim.x, 0);
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 if (have[j]) {
                     const T *e = reinterpret_cast<const T *>(&v[j]);
 #pragma unroll
-                    for (int q = 0; q < kVec; ++q) acc[q] += w[j] * to_f32(e[q]);
+                    for (int q = 0; q < kVec; ++q) acc[q] += p[j] * to_f32(e[q]);
                 }
             }
         }
-        if (VEC) {
-            uint4 v;
-            T *e = reinterpret_cast<T *>(&v);
+        if (t < tokens && at < c) {
+            if (VEC) {
+                uint4 v;
+                T *e = reinterpret_cast<T *>(&v);
 #pragma unroll
-            for (int q = 0; q < kVec; ++q) e[q] = from_f32<T>(acc[q]);
-            *reinterpret_cast<uint4 *>(out + t * ldo + at) = v;
-        } else {
-            out[t * ldo + at] = from_f32<T>(acc[0]);
+                for (int q = 0; q < kVec; ++q) e[q] = from_f32<T>(acc[q]);
+                *reinterpret_cast<uint4 *>(out + t * ldo + at) = v;
+            } else {
+                out[t * ldo + at] = from_f32<T>(acc[0]);
+            }
         }
     }
 }
 
 template <typename T>
 cudaError_t combine_launch(const void *y, long long ldy, long long rows, const int32_t *index, const float *weights,
-                           long long tokens, int topk, int c, void *out, long long ldo, bool vec, cudaStream_t s) {
-    const int kvec = vec ? 16 / (int)sizeof(T) : 1;
-    const long long blocks = (tokens * ((c + kvec - 1) / kvec) + 255) / 256;
-    const unsigned grid = (unsigned)(blocks < (1LL << 30) ? blocks : (1LL << 30));
-    return launch_early(vec ? combine_rows_kernel<T, true> : combine_rows_kernel<T, false>, dim3(grid), 256, 0, s, (const T *)y,
-                        ldy, rows, index, weights, tokens, topk, c, (T *)out, ldo);
+                           long long tokens, int topk, int c, void *out, long long ldo, bool vec, int sms, cudaStream_t s) {
+    const int per_row = vec ? (c * (int)sizeof(T) + 15) / 16 : c, ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
+    int width = 4;
+    while (width < per_row && width < 256) width *= 2;
+    const long long items = (tokens + 256 / width - 1) / (256 / width) * ((per_row + width - 1) / width);
+    const long long room = (long long)combine_ctas(ahead) * sms;
+    auto k = ahead == 2   ? (vec ? combine_rows_kernel<T, true, 2> : combine_rows_kernel<T, false, 2>)
+             : ahead == 4 ? (vec ? combine_rows_kernel<T, true, 4> : combine_rows_kernel<T, false, 4>)
+                          : (vec ? combine_rows_kernel<T, true, 8> : combine_rows_kernel<T, false, 8>);
+    return launch_early(k, dim3((unsigned)(items < room ? items : room)), 256, 0, s, (const T *)y, ldy, rows, index, weights,
+                        tokens, topk, c, (T *)out, ldo, width);
 }
 
 }  // namespace
@@ -1040,11 +1071,11 @@ cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
-                                bool vec, cudaStream_t s) {
+                                bool vec, int sms, cudaStream_t s) {
     switch (type) {
-        case HATQ_F32: return combine_launch<float>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, s);
-        case HATQ_F16: return combine_launch<__half>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, s);
-        default: return combine_launch<__nv_bfloat16>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, s);
+        case HATQ_F32: return combine_launch<float>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
+        case HATQ_F16: return combine_launch<__half>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
+        default: return combine_launch<__nv_bfloat16>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
     }
 }
 

@@ -65,7 +65,7 @@ cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int til
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
-                                bool vec, cudaStream_t s);
+                                bool vec, int sms, cudaStream_t s);
 
 // A kernel of this file's operators may be started while the one before it in
 // the stream is ending: it sets itself up and then waits here, before its first
