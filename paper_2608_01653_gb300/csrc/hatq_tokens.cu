@@ -934,22 +934,25 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
 constexpr int combine_ctas(int ahead) { return ahead == 8 ? 3 : ahead == 4 ? 4 : 6; }
 
 template <typename T, bool VEC, int kAhead>
-__global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel(const T *y, long long ldy, long long rows, const int32_t *index,
-                                                              const float *weights, long long tokens, int topk, int c, T *out,
-                                                              long long ldo, int width) {
-    constexpr int kVec = VEC ? 16 / sizeof(T) : 1;
+__global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel(const T *y, long long ldy, long long rows,
+                                                                                 const int32_t *index, const float *weights,
+                                                                                 long long tokens, int topk, int c, T *out,
+                                                                                 long long ldo, int width) {
+    // rows that are not on 16-byte boundaries: four values per thread, `width` apart
+    constexpr int kVec = VEC ? 16 / sizeof(T) : 4;
     // width threads (a power of two) for a token, or for a part of its row
     const int per_row = (c + kVec - 1) / kVec, parts = (per_row + width - 1) / width, per_cta = 256 / width;
-    const int slot = threadIdx.x / width, lane = threadIdx.x - slot * width;
+    const int slot = threadIdx.x / width, lane = threadIdx.x - slot * width, apart = VEC ? 1 : width;
     const long long items = (tokens + per_cta - 1) / per_cta * parts;
     int at_next = 0;
     long long t_next = 0;
     int idx[kAhead];
     float w[kAhead];
     auto fetch = [&](long long item, int j0) {
+        const int part = (int)(item % parts);
         t_next = item / parts * per_cta + slot;
-        at_next = (int)(item % parts) * width + lane;
-        const bool live = item < items && t_next < tokens && at_next < per_row;
+        at_next = VEC ? (part * width + lane) * kVec : part * width * kVec + lane;
+        const bool live = item < items && t_next < tokens && at_next < c;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             idx[j] = live && j0 + j < topk ? index[t_next * topk + j0 + j] : -1;
@@ -960,7 +963,7 @@ __global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel
     fetch(blockIdx.x, 0);
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         const long long t = t_next;
-        const int at = at_next * kVec;
+        const int at = at_next;
         float acc[kVec];
 #pragma unroll
         for (int q = 0; q < kVec; ++q) acc[q] = 0.0f;
@@ -974,8 +977,13 @@ __global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel
                 p[j] = w[j];
                 if (have[j]) {
                     const T *from = y + (long long)idx[j] * ldy + at;
-                    if (VEC) v[j] = *reinterpret_cast<const uint4 *>(from);
-                    else *reinterpret_cast<T *>(&v[j]) = *from;
+                    if (VEC) {
+                        v[j] = *reinterpret_cast<const uint4 *>(from);
+                    } else {
+                        T *e = reinterpret_cast<T *>(&v[j]);
+#pragma unroll
+                        for (int q = 0; q < kVec; ++q) e[q] = at + q * apart < c ? from[q * apart] : from_f32<T>(0.0f);
+                    }
                 }
             }
             if (j0 + kAhead < topk) fetch(item, j0 + kAhead);
@@ -990,14 +998,17 @@ __global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel
             }
         }
         if (t < tokens && at < c) {
+            T *to = out + t * ldo + at;
             if (VEC) {
                 uint4 v;
                 T *e = reinterpret_cast<T *>(&v);
 #pragma unroll
                 for (int q = 0; q < kVec; ++q) e[q] = from_f32<T>(acc[q]);
-                *reinterpret_cast<uint4 *>(out + t * ldo + at) = v;
+                *reinterpret_cast<uint4 *>(to) = v;
             } else {
-                out[t * ldo + at] = from_f32<T>(acc[0]);
+#pragma unroll
+                for (int q = 0; q < kVec; ++q)
+                    if (at + q * apart < c) to[q * apart] = from_f32<T>(acc[q]);
             }
         }
     }
@@ -1006,7 +1017,7 @@ __global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel
 template <typename T>
 cudaError_t combine_launch(const void *y, long long ldy, long long rows, const int32_t *index, const float *weights,
                            long long tokens, int topk, int c, void *out, long long ldo, bool vec, int sms, cudaStream_t s) {
-    const int per_row = vec ? (c * (int)sizeof(T) + 15) / 16 : c, ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
+    const int per_row = vec ? (c * (int)sizeof(T) + 15) / 16 : (c + 3) / 4, ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
     int width = 4;
     while (width < per_row && width < 256) width *= 2;
     const long long items = (tokens + 256 / width - 1) / (256 / width) * ((per_row + width - 1) / width);
