@@ -796,31 +796,31 @@ def _token_torch():
     return _TORCH
 
 
-def _rows_of(t, name, types, width, device):
-    """Checks a [rows][width] tensor on `device` with contiguous rows that do not overlap; returns its type code,
-    its rows and its pitch in elements."""
+def _rows_of(t, name, types, device):
+    """Checks a [rows][values] tensor on `device` with contiguous rows; returns its type code, its rows, the values of
+    a row and the pitch in elements (below the values where rows overlap or are one row, as expand makes them)."""
     code = types.get(t.dtype)
     if code is None:
         raise ValueError(f"{name}: dtype {t.dtype} is none of {[str(d) for d in types]}")
-    shape = t.shape
-    if len(shape) != 2 or (width is not None and shape[1] != width):
-        raise ValueError(f"{name}: shape {tuple(shape)}, expected [rows, {'width' if width is None else width}]")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected two dimensions")
     if t.get_device() != device:
         raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
-    rows, values = shape
+    rows, values = t.shape
     pitch, inner = t.stride()
     if inner != 1 and values > 1:
         raise ValueError(f"{name}: the values of a row must be contiguous")
-    if rows <= 1:
-        pitch = values                              # a single row may carry any stride
-    elif pitch < values:
-        raise ValueError(f"{name}: rows overlap (stride {pitch} for {values} values)")
-    return code, rows, pitch
+    return code, rows, values, pitch if rows > 1 else values     # a single row may carry any stride
 
 
-def _apart(t):
-    """The input t, copied where its rows are one row (expand) or overlap: the library takes pitches of a row or more."""
-    return t.contiguous() if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1] else t
+def _out_of(t, types, rows, values, device):
+    """Checks a tensor to write [rows][values] into; returns its type code and its pitch."""
+    code, r, v, pitch = _rows_of(t, "out", types, device)
+    if r != rows or v != values:
+        raise ValueError(f"out: shape {(r, v)}, expected {(rows, values)}")
+    if pitch < values:
+        raise ValueError(f"out: rows overlap (stride {pitch} for {values} values)")
+    return code, pitch
 
 
 def _flat(t, name, dtype, shape, device):
@@ -856,6 +856,7 @@ class LinearWeights:
         self.experts, self.n, self.k, self.grouped = experts, n, k, grouped
         self.codes, self.windows, self.s_w, self.bias = codes, windows, s_w, bias
         self.device = codes.get_device()
+        self.row_bytes = 2 * (-(-k // 64) * 64)     # of hatq_linear's workspace
         self.struct = LinearWeightsStruct(experts, n, k, 0, codes.data_ptr(), windows.data_ptr(), s_w.data_ptr(),
                                           None if bias is None else bias.data_ptr())
         self.ref = ctypes.byref(self.struct)
@@ -880,7 +881,8 @@ def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeight
     device, raw = _launch_stream(w, stream)
     with torch.cuda.stream(stream):                 # None: the current one
         rows = w.reshape(e * n, k)
-        rows = _apart(rows if k == 1 or rows.stride(1) == 1 else rows.contiguous())
+        if k > 1 and rows.stride(1) != 1 or rows.stride(0) < k:
+            rows = rows.contiguous()
         if w.dtype == torch.int8:
             if scales is None or hb != 1:
                 raise ValueError("int8 weights need their scales, and are not transformed")
@@ -892,7 +894,7 @@ def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeight
         b = None if bias is None else bias.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
         if s_w.numel() != e * n or (b is not None and b.numel() != e * n):
             raise ValueError(f"scales and bias need one value per output channel ({e * n})")
-        _, _, pitch = _rows_of(rows, "w", {torch.int8: 0}, k, device)
+        pitch = rows.stride(0) if e * n > 1 else k
         L = LinearWeights(e, n, k, torch.empty(size.value, dtype=torch.uint8, device=w.device),
                           torch.empty(e, dtype=torch.int32, device=w.device), s_w, b, grouped)
         _check(load().hatq_linear_layout(rows.data_ptr(), pitch, L.ref, raw))
@@ -908,33 +910,42 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
     tensors to write into; new codes come with a pitch that suits the products."""
     torch = _TORCH or _token_torch()
     device, raw = _launch_stream(x, stream)
-    x = _apart(x)
-    kind, src_rows, pitch = _rows_of(x, "x", _TOKEN_TYPES, None, device)
+    kind, src_rows, c, pitch = _rows_of(x, "x", _TOKEN_TYPES, device)
+    if pitch < c:
+        x, pitch = x.contiguous(), c                # the library takes rows that are apart
     code = _ACTS.get(act)
     if code is None:
         raise ValueError(f"unknown activation {act!r}")
-    c = x.shape[1]
     if gated:
         if c % 2:
             raise ValueError("a gated row holds two halves")
         c //= 2
-    n = src_rows if rows is None else rows.shape[0]
-    index = None if rows is None else _flat(rows, "rows", torch.int32, (n,), device)
+    if rows is None:
+        n, index = src_rows, None
+    else:
+        n = rows.shape[0]
+        index = _flat(rows, "rows", torch.int32, (n,), device)
     if codes == "auto":
         codes = "i8" if n <= 2 else "f16"
+    fmt = _CODE_FORMATS.get(codes)
+    if fmt is None:
+        raise ValueError(f"unknown code format {codes!r}")
     if out is None:
-        pad = 16 if codes == "i8" else 8
-        out = _empty(x, (n, -(-c // pad) * pad), torch.int8 if codes == "i8" else torch.float16, stream)
-        if out.shape[1] != c:
+        out_pitch = -(-c // 16) * 16 if fmt == CODES_I8 else -(-c // 8) * 8
+        out = _empty(x, (n, out_pitch), torch.int8 if fmt == CODES_I8 else torch.float16, stream)
+        if out_pitch != c:
             out = out[:, :c]
+    else:
+        kept, out_pitch = _out_of(out, _CODE_TYPES, n, c, device)
+        if kept != fmt:
+            raise ValueError(f"out: {out.dtype} does not hold {codes} codes")
     if scales is None:
         scales = _empty(x, (n,), torch.float32, stream)
-    fmt, out_rows, out_pitch = _rows_of(out, "out", _CODE_TYPES, c, device)
-    if out_rows != n or _CODE_FORMATS.get(codes) != fmt:
-        raise ValueError(f"out: expected {n} rows of {codes} codes, got {out_rows} of {out.dtype}")
+        ps = scales.data_ptr()
+    else:
+        ps = _flat(scales, "scales", torch.float32, (n,), device)
     st = (_LIB or load()).hatq_quantize_tokens(x.data_ptr(), kind, pitch, src_rows, index, n, c, hb, code, 1 if gated else 0,
-                                               fmt, out.data_ptr(), out_pitch,
-                                               _flat(scales, "scales", torch.float32, (n,), device), raw)
+                                               fmt, out.data_ptr(), out_pitch, ps, raw)
     if st:
         _check(st)
     return out, scales
@@ -943,22 +954,30 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
 def _product(x, scales, offsets, layer, dtype, out, stream):
     torch = _TORCH or _token_torch()
     device, raw = _launch_stream(x, stream)
-    x = _apart(x)
-    fmt, n, pitch = _rows_of(x, "x", _CODE_TYPES, layer.k, device)
+    fmt, n, k, pitch = _rows_of(x, "x", _CODE_TYPES, device)
+    if k != layer.k:
+        raise ValueError(f"x: rows of {k} codes, the weights take {layer.k}")
+    if pitch < k:
+        x, pitch = x.contiguous(), k                # the library takes rows that are apart
     if layer.device != device:
         raise ValueError(f"the weights are on cuda:{layer.device}, x on cuda:{device}")
     s_x = _flat(scales, "scales", torch.float32, (n,), device)
     if out is None:
-        out = _empty(x, (n, layer.n), dtype or torch.bfloat16, stream)
-    kind, out_rows, out_pitch = _rows_of(out, "out", _TOKEN_TYPES, layer.n, device)
-    if out_rows != n:
-        raise ValueError(f"out: expected {n} rows, got {out_rows}")
+        kind, out_pitch = _TOKEN_TYPES.get(dtype), layer.n
+        if kind is None:
+            raise ValueError(f"dtype {dtype} is none of {[str(d) for d in _TOKEN_TYPES]}")
+        out = _empty(x, (n, out_pitch), dtype, stream)
+    else:
+        kind, out_pitch = _out_of(out, _TOKEN_TYPES, n, layer.n, device)
     lib, px = _LIB or load(), x.data_ptr()
     ws, size = None, 0
     if n > 2 and not (fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0):
-        need = ctypes.c_size_t()
-        _check(lib.hatq_linear_workspace(px, fmt, pitch, n, layer.ref, ctypes.byref(need)))
-        size = need.value
+        if n <= 64:                                 # few rows mostly need no workspace
+            need = ctypes.c_size_t()
+            _check(lib.hatq_linear_workspace(px, fmt, pitch, n, layer.ref, ctypes.byref(need)))
+            size = need.value
+        else:
+            size = n * layer.row_bytes
         if size:
             scratch = _empty(x, (size,), torch.uint8, stream)
             ws = scratch.data_ptr()
@@ -978,7 +997,7 @@ def linear(x, scales, layer, dtype=None, out=None, stream=None):
     in `dtype` (float32, float16, bfloat16 - the default) or into `out`."""
     if layer.grouped:
         raise ValueError("a layer with experts needs grouped_linear")
-    return _product(x, scales, None, layer, dtype, out, stream)
+    return _product(x, scales, None, layer, dtype or _token_torch().bfloat16, out, stream)
 
 
 def grouped_linear(x, scales, offsets, layer, dtype=None, out=None, stream=None):
@@ -986,7 +1005,7 @@ def grouped_linear(x, scales, offsets, layer, dtype=None, out=None, stream=None)
     (offsets int32 [experts + 1] on the device). Rows that no expert holds are not written."""
     if offsets is None:
         raise ValueError("offsets are missing")
-    return _product(x, scales, offsets, layer, dtype, out, stream)
+    return _product(x, scales, offsets, layer, dtype or _token_torch().bfloat16, out, stream)
 
 
 def combine_rows(y, index, weights, out=None, stream=None):
@@ -994,20 +1013,20 @@ def combine_rows(y, index, weights, out=None, stream=None):
     both [tokens][topk]; an index outside y contributes nothing)."""
     torch = _TORCH or _token_torch()
     device, raw = _launch_stream(y, stream)
-    y = _apart(y)
-    kind, rows, pitch = _rows_of(y, "y", _TOKEN_TYPES, None, device)
+    kind, rows, c, pitch = _rows_of(y, "y", _TOKEN_TYPES, device)
+    if pitch < c:
+        y, pitch = y.contiguous(), c                # the library takes rows that are apart
     if index.dim() != 2:
         raise ValueError(f"index: shape {tuple(index.shape)}, expected [tokens, topk]")
-    t, topk = index.shape
-    c = y.shape[1]
+    t, topk = shape = index.shape
     if out is None:
-        out = _empty(y, (t, c), y.dtype, stream)
-    out_kind, out_rows, out_pitch = _rows_of(out, "out", _TOKEN_TYPES, c, device)
-    if out_kind != kind or out_rows != t:
-        raise ValueError(f"out: expected {t} rows of {y.dtype}, got {out_rows} of {out.dtype}")
-    st = (_LIB or load()).hatq_combine_rows(y.data_ptr(), kind, pitch, rows,
-                                            _flat(index, "index", torch.int32, (t, topk), device),
-                                            _flat(weights, "weights", torch.float32, (t, topk), device), t, topk, c,
+        out, out_pitch = _empty(y, (t, c), y.dtype, stream), c
+    else:
+        out_kind, out_pitch = _out_of(out, _TOKEN_TYPES, t, c, device)
+        if out_kind != kind:
+            raise ValueError(f"out: {out.dtype}, expected {y.dtype}")
+    st = (_LIB or load()).hatq_combine_rows(y.data_ptr(), kind, pitch, rows, _flat(index, "index", torch.int32, shape, device),
+                                            _flat(weights, "weights", torch.float32, shape, device), t, topk, c,
                                             out.data_ptr(), out_pitch, raw)
     if st:
         _check(st)
