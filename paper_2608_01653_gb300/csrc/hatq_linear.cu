@@ -144,6 +144,12 @@ template <int REGS> __device__ __forceinline__ void regs_inc() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
+    uint32_t r;
+    if (bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 __device__ __forceinline__ void put(void *y, int type, long long at, float v) {
     if (type == HATQ_BF16) reinterpret_cast<__nv_bfloat16 *>(y)[at] = __float2bfloat16_rn(v);
     else if (type == HATQ_F16) reinterpret_cast<__half *>(y)[at] = __float2half_rn(v);
@@ -159,11 +165,12 @@ struct Config {
     static constexpr int kXBytes = T / kCtas * 128;                    // one block's token codes
     static constexpr int kWOffset = kSub * kXBytes;
     static constexpr int kStageBytes = kSub * (kXBytes + kBlockBytes);
-    static constexpr int kStages = 204 * 1024 / kStageBytes;
+    static constexpr int kStages = 202 * 1024 / kStageBytes;
     static constexpr int kSlotCols = 32 * kSub;                        // a widened block takes 32 columns
     static constexpr int kFree = (512 - 2 * T) / kSlotCols;
     static constexpr int kSlots = kFree < kStages ? kFree : kStages;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + (4 * kMaxExperts + 1) * 4 + 64;
+    static constexpr int kTables = ((4 * kMaxExperts + 1) * 4 + 15) & ~15;   // the experts' tables
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + kTables + 8 * (T / 2) * 4;
     static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
     static_assert(kSlots >= 2 && kStages >= kSlots, "the barrier of a slot's last stage still has that phase");
     static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
@@ -475,6 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int half = (warp >> 2) - 3;
         const int m = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kHalf);
+        float *scales = reinterpret_cast<float *>(bar_area + 1024 + C::kTables) + (warp - 12) * kHalf;
         int cc = 0;
         auto release = [&](int d) {
             tc_fence_before();
@@ -492,39 +500,80 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float sw = live ? a.s_w[(long long)tile.e * a.n + ch] : 0.0f;
             const float bias = live && a.bias ? a.bias[(long long)tile.e * a.n + ch] : 0.0f;
             const int chunks = (kb1 - 1) / win - kb0 / win + 1;
-            // the scales of 16 of this warpgroup's columns, one per lane (twice); asked for a group ahead
-            auto scales_of = [&](int g) {
-                const int c = half * kHalf + g + (lane & 15);
-                return g < kHalf && c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
-            };
-            float sx_now = scales_of(0);
-            // 16 tokens' values of this channel, from column half * kHalf + g
-            auto emit = [&](const float (&v)[16], int g) {
-                const float sx_next = scales_of(g + 16);
+            // the tokens' scales of this warpgroup's columns, the warp's own copy
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kHalf; i += 32) {
+                const int c = half * kHalf + i + lane;
+                if (i + lane < kHalf) scales[i + lane] = c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
+            }
+            __syncwarp();
+            const bool warp_live = (tile.ch + (int)in_pair) * kRowTile + (int)(warp & 3) * 32 + 32 <= a.n;
+            // 16 tokens' sums of this channel, from column half * kHalf + g
+            auto emit = [&](float (&v)[16], int g) {
                 const int c0 = half * kHalf + g;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 sx = reinterpret_cast<const float4 *>(scales + g)[i];
+                    v[4 * i] = v[4 * i] * sw * sx.x;
+                    v[4 * i + 1] = v[4 * i + 1] * sw * sx.y;
+                    v[4 * i + 2] = v[4 * i + 2] * sw * sx.z;
+                    v[4 * i + 3] = v[4 * i + 3] * sw * sx.w;
+                }
+                if (a.bias) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += bias;
+                }
+                if (warp_live && c0 + 16 <= tile.rows && (a.y_type == HATQ_F32 || a.y_even)) {
+                    const long long row = tile.row + c0;
+                    if (a.y_type == HATQ_F32) {
+                        float *y = reinterpret_cast<float *>(a.y) + row * a.ldy + ch;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i, y += a.ldy) *y = v[i];
+                        return;
+                    }
+                    // Lanes 2i and 2i + 1 swap halves: the even one then has both channels of the first eight tokens,
+                    // the odd one of the others, and 16 stores of 2 bytes become 8 of 4.
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], a.y_type == HATQ_BF16);
+                    const bool odd = (lane & 1) != 0;
+                    char *y = reinterpret_cast<char *>(a.y) + ((row + (odd ? 8 : 0)) * a.ldy + (ch & ~1)) * 2;
+                    const long long pitch = a.ldy * 2;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t mine = odd ? w[4 + i] : w[i];
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? w[i] : w[4 + i], 1);
+                        const uint32_t lo = odd ? other : mine, hi = odd ? mine : other;
+                        *reinterpret_cast<uint32_t *>(y) = prmt(lo, hi, 0x5410u);
+                        *reinterpret_cast<uint32_t *>(y + pitch) = prmt(lo, hi, 0x7632u);
+                        y += 2 * pitch;
+                    }
+                    return;
+                }
                 long long at = (long long)(tile.row + c0) * a.ldy + ch;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float sx = __shfl_sync(0xffffffffu, sx_now, i);
-                    const float r = v[i] * sw * sx;
-                    if (live && c0 + i < tile.rows) put(a.y, a.y_type, at, a.bias ? r + bias : r);
+                    if (live && c0 + i < tile.rows) put(a.y, a.y_type, at, v[i]);
                     at += a.ldy;
                 }
-                sx_now = sx_next;
             };
             if (chunks == 1 && parts == 1) {
                 ok = mbar_wait(dfull(cc & 1), (uint32_t)((cc >> 1) & 1), abort_flag, a.err);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t from = t_lane + (uint32_t)((cc & 1) * T);
+                const int end = min(kHalf, tile.rows - half * kHalf);
+                uint32_t r[16];
+                if (end > 0) tmem_ld16(from, r);
 #pragma unroll 1
-                for (int g = 0; g < kHalf && half * kHalf + g < tile.rows; g += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(t_lane + (uint32_t)((cc & 1) * T + g), r);
+                for (int g = 0; g < end; g += 16) {
                     tmem_wait_ld();
                     float v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+                    if (g + 16 < end) tmem_ld16(from + (uint32_t)(g + 16), r);    // while these are stored
                     emit(v, g);
                 }
                 release(cc & 1);

@@ -53,6 +53,7 @@ struct LinearArgs {
     void *y;
     long long ldy;
     int y_type;
+    bool y_even;                       // 16-bit outputs: pairs of an even channel and the next lie on 4-byte boundaries
     int split;                         // CTAs of a cluster that share one tile's reduction
     int slots;                         // one-token kernel: groups the grid has room for
     int *err;
