@@ -166,13 +166,20 @@ struct Config {
     static constexpr int kWOffset = kSub * kXBytes;
     static constexpr int kStageBytes = kSub * (kXBytes + kBlockBytes);
     static constexpr int kStages = 202 * 1024 / kStageBytes;
-    static constexpr int kSlotCols = 32 * kSub;                        // a widened block takes 32 columns
+    // Blocks per hand-off from the widening warps to the MMA warp and back: all of a stage, or one where the
+    // accumulators leave room for four blocks only. Widening takes about 1000 cycles from a freed slot to the MMAs:
+    // the MMAs of three other blocks cover that, those of one other stage (770 cycles) do not.
+    static constexpr int kGroup = T > 128 ? 1 : kSub;
+    static constexpr int kHands = kSub / kGroup;                       // hand-offs per stage
+    static constexpr int kSlotCols = 32 * kGroup;                      // a widened block takes 32 columns
     static constexpr int kFree = (512 - 2 * T) / kSlotCols;
-    static constexpr int kSlots = kFree < kStages ? kFree : kStages;
+    static constexpr int kSlots = kFree < 8 ? kFree : 8;
+    static constexpr int kWideWarps = (kGroup == 1 ? 4 : 8) * kCtas;   // one set widens a hand-off, or both
     static constexpr int kTables = ((4 * kMaxExperts + 1) * 4 + 15) & ~15;   // the experts' tables
     static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + kTables + 8 * (T / 2) * 4;
     static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
-    static_assert(kSlots >= 2 && kStages >= kSlots, "the barrier of a slot's last stage still has that phase");
+    static_assert(kSlots >= 2 && (kGroup > 1 || kSlots % 2 == 0), "slots of a hand-off");
+    static_assert(8 * (kStages * (2 + kHands) + kSlots + 5) + 8 <= 1024, "barriers");
     static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
 };
 
@@ -192,10 +199,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t bar0 = smem_addr(bar_area);
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (C::kStages + s); };
-    auto wide = [&](int s) { return bar0 + 8u * (2 * C::kStages + s); };
-    auto dfull = [&](int d) { return bar0 + 8u * (3 * C::kStages + d); };
-    auto dempty = [&](int d) { return bar0 + 8u * (3 * C::kStages + 2 + d); };
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (3 * C::kStages + 4));
+    auto wide = [&](int s, int h) { return bar0 + 8u * (2 * C::kStages + s * C::kHands + h); };
+    auto slot_free = [&](int q) { return bar0 + 8u * (C::kStages * (2 + C::kHands) + q); };
+    auto dfull = [&](int d) { return bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + d); };
+    auto dempty = [&](int d) { return bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + 2 + d); };
+    const uint32_t tail = bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + 4);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (C::kStages * (2 + C::kHands) + C::kSlots + 5));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     // per expert: token tiles before it, its rows, its exact window
     int *tile_start = reinterpret_cast<int *>(bar_area + 1024), *first_row = tile_start + kMaxExperts + 1,
@@ -215,8 +224,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            mbar_init(wide(s), 8 * C::kCtas);
+            for (int h = 0; h < C::kHands; ++h) mbar_init(wide(s, h), C::kWideWarps);
         }
+        for (int q = 0; q < C::kSlots; ++q) mbar_init(slot_free(q), 1);
+        mbar_init(tail, 1);
         for (int d = 0; d < 2; ++d) {
             mbar_init(dfull(d), 1);
             mbar_init(dempty(d), 8 * C::kCtas);
@@ -372,41 +383,55 @@ __global__ void __launch_bounds__(kThreads, 1)
                     uint32_t acc = 0;
                     for (; b < end && ok; b += C::kSub) {
                         // The widening warps waited for the stage's copies, so their arrival speaks for both operands.
-                        if (!ready) {
-                            ok = mbar_wait(wide(s), ph, abort_flag, a.err);
-                            ok = __all_sync(0xffffffffu, ok);
-                            if (!ok) break;
-                        }
-                        const int now = s, at_slot = slot;
-                        if (++slot == C::kSlots) slot = 0;
+                        const int now = s;
+                        const uint32_t now_ph = ph;
                         if (++s == C::kStages) {
                             s = 0;
                             ph ^= 1u;
                         }
-                        const bool next = mbar_test(wide(s), ph);       // looked at early: its answer takes a while
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t bd = bd0 + (uint64_t)(now * (C::kStageBytes >> 4));
-                            const uint32_t at = tmem + (uint32_t)(2 * T + at_slot * C::kSlotCols);
+                        const uint64_t bd = bd0 + (uint64_t)(now * (C::kStageBytes >> 4));
 #pragma unroll
-                            for (int j = 0; j < C::kSub; ++j) {
-                                if (j > 0 && b + j >= end) break;
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 32 * j + 8 * q,
-                                                 bd + (uint64_t)(j * (C::kXBytes >> 4) + 2 * q), idesc, acc | (uint32_t)(j + q));
+                        for (int h = 0; h < C::kHands; ++h) {
+                            if (!ready) {
+                                ok = mbar_wait(wide(now, h), now_ph, abort_flag, a.err);
+                                ok = __all_sync(0xffffffffu, ok);
+                                if (!ok) break;
                             }
-                            commit<PAIR>(empty(now));
-                            if (b + C::kSub >= end) commit<PAIR>(dfull(d));
+                            // the next hand-off is looked at early: the answer takes a while
+                            const bool next = h + 1 < C::kHands ? mbar_test(wide(now, h + 1), now_ph) : mbar_test(wide(s, 0), ph);
+                            tc_fence_after();
+                            if (elect_one()) {
+                                const uint32_t at = tmem + (uint32_t)(2 * T + slot * C::kSlotCols);
+#pragma unroll
+                                for (int j = 0; j < C::kGroup; ++j) {
+                                    const int block = h * C::kGroup + j;
+                                    if (block > 0 && b + block >= end) break;
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q)
+                                        mma_ts<PAIR>(tmem + (uint32_t)(d * T), at + 32 * j + 8 * q,
+                                                     bd + (uint64_t)(block * (C::kXBytes >> 4) + 2 * q), idesc,
+                                                     acc | (uint32_t)(block + q));
+                                }
+                                commit<PAIR>(slot_free(slot));
+                                if (h + 1 == C::kHands) {
+                                    commit<PAIR>(empty(now));
+                                    if (b + C::kSub >= end) commit<PAIR>(dfull(d));
+                                }
+                            }
+                            ready = __all_sync(0xffffffffu, next);
+                            if (++slot == C::kSlots) slot = 0;
                         }
-                        ready = __all_sync(0xffffffffu, next);
+                        if (!ok) break;
                         acc = 1;
-                        ++issued;
                     }
                     ++cc;
                 }
             }
-            if (!ok && issued > 0) mbar_drain(empty((issued - 1) % C::kStages), (uint32_t)(((issued - 1) / C::kStages) & 1));
+            if (!ok) {
+                if (elect_one()) commit<PAIR>(tail);                    // after all MMAs that are on their way
+                __syncwarp();
+                mbar_drain(tail, 0);
+            }
         }
         __syncwarp();
         if (!PAIR && parts > 1) {
@@ -421,29 +446,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int tiles = total > first ? (total - first + step - 1) / step : 0;
         const int per_tile = (kb1 - kb0 + C::kSub - 1) / C::kSub, last = kb1 - kb0 - (per_tile - 1) * C::kSub;
         const long long stages = (long long)tiles * per_tile;
-        int s = 0, slot = 0, prior = 0, left = per_tile;                // prior: the stage that used the slot before
-        uint32_t ph = 0, prior_ph = 0;
+        // hand-offs are numbered it * kHands + h, their slots in turn; with one block each, a set takes every other one
+        int s = 0, left = per_tile, slot = C::kGroup == 1 ? set : 0;
+        uint32_t ph = 0, slot_ph = 1;                                   // the first use of a slot waits for nothing
         for (long long it = 0; it < stages; ++it) {
             int blocks = C::kSub;
             if (--left == 0) {
                 left = per_tile;
                 blocks = last;
             }
-            ok = mbar_wait(full(s), ph, abort_flag, a.err);
-            if (ok && it >= C::kSlots) {
-                ok = mbar_wait(empty(prior), prior_ph, abort_flag, a.err);
-                if (++prior == C::kStages) {
-                    prior = 0;
-                    prior_ph ^= 1u;
-                }
-            }
+            ok = mbar_wait(full(s), ph, abort_flag, a.err) && mbar_wait(slot_free(slot), slot_ph, abort_flag, a.err);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
-            for (int j = 0; j < C::kSub / 2; ++j) {
+            for (int j = 0; j < (C::kGroup == 1 ? 1 : C::kGroup / 2); ++j) {
                 const int block = 2 * j + set;
-                if (block >= blocks) break;
+                if (block >= blocks) break;                             // a tile's last stage may hold fewer
                 const uint8_t *src = smem + s * C::kStageBytes + C::kWOffset + block * kBlockBytes + m * 16;
                 uint32_t h[32];
 #pragma unroll
@@ -456,16 +475,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                         h[8 * i + 2 * q + 1] = hsub2(prmt(w[q], 0x64646464u, 0x4342u), 0x64806480u);
                     }
                 }
-                tmem_st32(t_lane + (uint32_t)(slot * C::kSlotCols + block * 32), h);
+                tmem_st32(t_lane + (uint32_t)(slot * C::kSlotCols + (C::kGroup == 1 ? 0 : block * 32)), h);
             }
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (PAIR) mbar_arrive_remote(map_shared(wide(s), 0));
-                else mbar_arrive(wide(s));
+                const uint32_t bar = wide(s, C::kGroup == 1 ? set : 0);
+                if (PAIR) mbar_arrive_remote(map_shared(bar, 0));
+                else mbar_arrive(bar);
             }
-            if (++slot == C::kSlots) slot = 0;
+            slot += C::kGroup == 1 ? 2 : 1;
+            if (slot >= C::kSlots) {
+                slot -= C::kSlots;
+                slot_ph ^= 1u;
+            }
             if (++s == C::kStages) {
                 s = 0;
                 ph ^= 1u;
