@@ -247,7 +247,65 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
+    const int pairs_n = (a.n_tiles + C::kCtas - 1) / C::kCtas;          // channel tiles of a cluster
+    const int per = PAIR ? 2 : a.split;
+    const int first = (int)blockIdx.x / per, step = (int)gridDim.x / per;
+    // this CTA's blocks of the reduction, whole stages but for the last
+    const int units = (a.kb + C::kSub - 1) / C::kSub;
+    const int kb0 = (int)((long long)units * part / parts) * C::kSub;
+    const int kb1 = min((int)((long long)units * (part + 1) / parts) * C::kSub, a.kb);
+
+    // A CTA's tiles come in order, so each role walks the experts along with them. Within an expert: all its token
+    // tiles under kRasterN channel tiles, then the next channel tiles, so that weights and codes are taken from L2.
+    int expert = 0;
+    auto decode = [&](int t) {
+        while (tile_start[expert + 1] * pairs_n <= t) ++expert;
+        const int tokens = tile_start[expert + 1] - tile_start[expert];
+        const int local = t - tile_start[expert] * pairs_n;
+        const int sweep = local / (kRasterN * tokens), rest = local - sweep * kRasterN * tokens;
+        const int width = min(kRasterN, pairs_n - sweep * kRasterN);
+        const int mt = rest / width;
+        Tile tile;
+        tile.e = expert;
+        tile.row = first_row[expert] + mt * T;
+        tile.ch = (sweep * kRasterN + rest - mt * width) * C::kCtas;
+        tile.rows = min(T, end_row[expert] - tile.row);
+        return tile;
+    };
+    // copies of the stage that begins at block b
+    const uint32_t stage0 = smem_addr(smem);
+    auto copy_stage = [&](const Tile &tile, int b, int s) {
+        // a pair's second half may lie behind the last channel tile: any block does, nothing of it is stored
+        const int ct = min(tile.ch + (int)in_pair, a.n_tiles - 1);
+        const uint8_t *w = a.w + (((long long)tile.e * a.n_tiles + ct) * a.kb + b) * kBlockBytes;
+        const int row = tile.row + (int)in_pair * (tile.columns() / 2);              // a pair's second half of the tokens
+        if (elect_one()) {
+            const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
+            const int blocks = min(C::kSub, kb1 - b);
+            mbar_expect_tx(full(s), (uint32_t)(blocks * (C::kXBytes + kBlockBytes)));
+            bulk_load(st + C::kWOffset, w, (uint32_t)(blocks * kBlockBytes), full(s));
+#pragma unroll
+            for (int q = 0; q < C::kSub; ++q)
+                if (q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
+        }
+        __syncwarp();
+    };
+
     after_prior_kernels();
+    int issued = 0;                                                     // stages that warp 0 asked for
+    if (!a.offsets && warp == 0) {
+        // one group: its table needs no memory, and the first copies wait for no other warp
+        if (lane == 0) {
+            tile_start[0] = first_row[0] = 0;
+            tile_start[1] = (a.rows + T - 1) / T;
+            end_row[0] = a.rows;
+        }
+        __syncwarp();
+        if (first < tile_start[1] * pairs_n) {
+            const Tile tile = decode(first);
+            for (int b = kb0; b < kb1 && issued < C::kStages; b += C::kSub) copy_stage(tile, b, issued++);
+        }
+    }
     if (threadIdx.x == 0) s_skip = *reinterpret_cast<volatile int *>(a.err);
     // two experts per thread, then the warps' sums
     if (2 * threadIdx.x < a.experts) {
@@ -287,10 +345,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (2 * threadIdx.x < a.experts) tile_start[2 * threadIdx.x + 1] = before + c[0];
         if (2 * threadIdx.x + 1 < a.experts) tile_start[2 * threadIdx.x + 2] = before + c[0] + c[1];
         if (threadIdx.x == 0) tile_start[0] = 0;
-    } else if (threadIdx.x == 0) {
-        tile_start[0] = first_row[0] = 0;
-        tile_start[1] = (a.rows + T - 1) / T;
-        end_row[0] = a.rows;
     }
     tc_fence_before();
     __syncthreads();
@@ -299,70 +353,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = *tmem_holder;
     const bool skip = s_skip != 0;
 
-    const int pairs_n = (a.n_tiles + C::kCtas - 1) / C::kCtas;          // channel tiles of a cluster
     const int total = skip ? 0 : tile_start[a.experts] * pairs_n;
-    const int per = PAIR ? 2 : a.split;
-    const int first = (int)blockIdx.x / per, step = (int)gridDim.x / per;
-    // this CTA's blocks of the reduction, whole stages but for the last
-    const int units = (a.kb + C::kSub - 1) / C::kSub;
-    const int kb0 = (int)((long long)units * part / parts) * C::kSub;
-    const int kb1 = min((int)((long long)units * (part + 1) / parts) * C::kSub, a.kb);
-
-    // A CTA's tiles come in order, so each role walks the experts along with them. Within an expert: all its token
-    // tiles under kRasterN channel tiles, then the next channel tiles, so that weights and codes are taken from L2.
-    int expert = 0;
-    auto decode = [&](int t) {
-        while (tile_start[expert + 1] * pairs_n <= t) ++expert;
-        const int tokens = tile_start[expert + 1] - tile_start[expert];
-        const int local = t - tile_start[expert] * pairs_n;
-        const int sweep = local / (kRasterN * tokens), rest = local - sweep * kRasterN * tokens;
-        const int width = min(kRasterN, pairs_n - sweep * kRasterN);
-        const int mt = rest / width;
-        Tile tile;
-        tile.e = expert;
-        tile.row = first_row[expert] + mt * T;
-        tile.ch = (sweep * kRasterN + rest - mt * width) * C::kCtas;
-        tile.rows = min(T, end_row[expert] - tile.row);
-        return tile;
-    };
-
     bool ok = true;
-    int issued = 0;
-    const uint32_t stage0 = smem_addr(smem);
     if (warp < 4) {
         regs_dec<kRegsIssue>();
         if (warp == 0) {
-            int s = 0;
-            uint32_t ph = 1;                                            // parity of the stage's previous release
+            // what was asked for before the roles began: the first stages of the first tile
+            int s = issued % C::kStages, done = issued;
+            uint32_t ph = issued == C::kStages ? 0u : 1u;               // parity of the stage's previous release
             for (int t = first; t < total && ok; t += step) {
                 const Tile tile = decode(t);
-                // a pair's second half may lie behind the last channel tile: any block does, nothing of it is stored
-                const int ct = min(tile.ch + (int)in_pair, a.n_tiles - 1);
-                const uint8_t *w = a.w + (((long long)tile.e * a.n_tiles + ct) * a.kb + kb0) * kBlockBytes;
-                const int row = tile.row + (int)in_pair * (tile.columns() / 2);      // a pair's second half of the tokens
-                for (int b = kb0; b < kb1; b += C::kSub) {
+                for (int b = kb0 + done * C::kSub; b < kb1; b += C::kSub) {
                     ok = mbar_wait(empty(s), ph, abort_flag, a.err);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    if (elect_one()) {
-                        const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
-                        const int blocks = min(C::kSub, kb1 - b);
-                        mbar_expect_tx(full(s), (uint32_t)(blocks * (C::kXBytes + kBlockBytes)));
-                        bulk_load(st + C::kWOffset, w, (uint32_t)(blocks * kBlockBytes), full(s));
-#pragma unroll
-                        for (int q = 0; q < C::kSub; ++q)
-                            if (q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
-                    }
-                    __syncwarp();
-                    w += C::kSub * kBlockBytes;
+                    copy_stage(tile, b, s);
                     ++issued;
                     if (++s == C::kStages) {
                         s = 0;
                         ph ^= 1u;
                     }
                 }
+                done = 0;
             }
-            if (!ok)
+            if (!ok || skip)
                 for (int i = max(0, issued - C::kStages); i < issued; ++i)
                     mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
         } else if (warp == 1 && in_pair == 0) {
@@ -640,26 +654,37 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (!PAIR && parts > 1) {
-            cluster_sync();
-            if (ok && first < total) {
-                // this CTA finishes every parts-th token: a warp takes a token, a lane four channels, the parts'
-                // sums all loaded before the first is added
-                const Tile tile = decode(first);
-                const int ch = tile.ch * kRowTile + 4 * lane;
-                float sw[4], bias[4];
+            // this CTA finishes every parts-th token: a warp takes a token, a lane four channels; scales are on their way
+            // while the others' sums are waited for, and the parts' sums all loaded before the first is added
+            constexpr int kOwn = T / 16 < 8 ? T / 16 : 8;               // tokens of a warp, at two parts
+            float sw[4], bias[4], sx[kOwn];
+            Tile tile{};
+            if (first < total) tile = decode(first);
+            const int ch = tile.ch * kRowTile + 4 * lane, c0 = part + parts * (warp - 12);
+            if (first < total) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool live = ch + i < a.n;
                     sw[i] = live ? a.s_w[(long long)tile.e * a.n + ch + i] : 0.0f;
                     bias[i] = live && a.bias ? a.bias[(long long)tile.e * a.n + ch + i] : 0.0f;
                 }
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    const int c = c0 + 8 * parts * i;
+                    sx[i] = c < tile.rows ? a.s_x[tile.row + c] : 0.0f;
+                }
+            }
+            cluster_sync();
+            if (ok && first < total) {
                 const uint32_t mine = smem_addr(smem) + 16u * (uint32_t)lane;
-                for (int c = part + parts * (warp - 12); c < tile.rows; c += 8 * parts) {
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    const int c = c0 + 8 * parts * i;
+                    if (c >= tile.rows) break;
                     int4 v[kMaxSplit];
 #pragma unroll
                     for (int q = 0; q < kMaxSplit; ++q)
                         if (q < parts) v[q] = load_cluster(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q));
-                    const float sx = a.s_x[tile.row + c];
                     int4 sum = v[0];
 #pragma unroll
                     for (int q = 1; q < kMaxSplit; ++q)
@@ -672,9 +697,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int part4[4] = {sum.x, sum.y, sum.z, sum.w};
                     const long long at = (long long)(tile.row + c) * a.ldy + ch;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float r = (float)part4[i] * sw[i] * sx;
-                        if (ch + i < a.n) put(a.y, a.y_type, at + i, a.bias ? r + bias[i] : r);
+                    for (int q = 0; q < 4; ++q) {
+                        const float r = (float)part4[q] * sw[q] * sx[i];
+                        if (ch + q < a.n) put(a.y, a.y_type, at + q, a.bias ? r + bias[q] : r);
                     }
                 }
             }

@@ -71,7 +71,7 @@ Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms
         return p;
     }
     static const struct { int tokens; bool pair; int ns; } options[] = {
-        {32, false, 127}, {64, false, 156}, {128, false, 230}, {128, true, 190}, {192, true, 255}};
+        {32, false, 115}, {64, false, 140}, {128, false, 202}, {128, true, 165}, {192, true, 224}};
     const long long held = rows < L->experts ? rows : L->experts;
     long long best = LLONG_MAX;
     for (const auto &o : options) {
