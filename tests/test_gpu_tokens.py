@@ -498,3 +498,39 @@ def test_float_weights_follow_the_float_layer():
         bound = math.sqrt(k) * (sx * w.double().norm(dim=1)[None] + sw * x.double().norm(dim=1)[:, None]) / 2 + k * sx * sw / 4
         assert bool(((y.double() - ref).abs() <= 1.001 * bound).all())
         assert float((y - ref).norm() / ref.norm()) < 0.05
+
+
+# ------------------------------------------------------------------ refusals of the binding
+
+def test_binding_refuses():
+    x, w = codes(4, 64, 90), codes(32, 64, 91)
+    one = torch.ones(64, device="cuda")
+    L = H.prepare_linear(w, scales=one[:32])
+    G = H.prepare_linear(w.view(2, 16, 64), scales=one[:32].view(2, 16))
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    s = one[:4].contiguous()
+    bad = [lambda: H.linear(x.float(), s, L), lambda: H.linear(x[:, :32], s, L), lambda: H.linear(x.T, s, L),
+           lambda: H.linear(x.cpu(), s, L), lambda: H.linear(x, one, L), lambda: H.linear(x, s.double(), L),
+           lambda: H.linear(x, s.cpu(), L), lambda: H.linear(x, s, L, dtype=torch.float64), lambda: H.linear(x, s, G),
+           lambda: H.linear(x, s, L, out=torch.empty(4, 31, device="cuda")),
+           lambda: H.linear(x, s, L, out=torch.empty(1, 32, device="cuda").expand(4, 32)),
+           lambda: H.linear(x, s, L, out=torch.empty(32, 4, device="cuda").T),
+           lambda: H.grouped_linear(x, s, None, G), lambda: H.grouped_linear(x, s, off[:2], G),
+           lambda: H.grouped_linear(x, s, off.long(), G), lambda: H.prepare_linear(w), lambda: H.prepare_linear(w, hb=2, scales=one[:32]),
+           lambda: H.prepare_linear(w, scales=one), lambda: H.prepare_linear(w.half(), scales=one[:32]),
+           lambda: H.prepare_linear(w[0], scales=one[:32]), lambda: H.prepare_linear(w, scales=one[:32], bias=one),
+           lambda: H.quantize_tokens(x), lambda: H.quantize_tokens(x.half(), act="tanh"), lambda: H.quantize_tokens(x.half(), codes="i4"),
+           lambda: H.quantize_tokens(x.half()[:, :63], gated=True), lambda: H.quantize_tokens(x.half(), rows=off.long()),
+           lambda: H.quantize_tokens(x.half(), codes="i8", out=torch.empty(4, 64, dtype=torch.float16, device="cuda")),
+           lambda: H.quantize_tokens(x.half(), scales=one), lambda: H.combine_rows(x, off.view(1, 3), one[:3].view(1, 3)),
+           lambda: H.combine_rows(x.half(), off.view(1, 3), one[:2].view(1, 2)), lambda: H.combine_rows(x.half(), off, one[:3]),
+           lambda: H.combine_rows(x.half(), off.view(1, 3), one[:3].contiguous().view(1, 3), out=torch.empty(1, 64, device="cuda"))]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was accepted")
+    for call in (lambda: H.quantize_tokens(x.half(), hb=3), lambda: H.quantize_tokens(x.half(), hb=128),
+                 lambda: H.prepare_linear(w.half(), hb=48)):
+        with pytest.raises(H.HatqError):
+            call()
+    finish()
