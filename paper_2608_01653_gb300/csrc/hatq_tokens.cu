@@ -342,17 +342,18 @@ template <int AHEAD> __device__ __forceinline__ void copies_wait() {
 }
 
 // STAGES buffers per warp, so STAGES - 1 rows on their way. With one buffer (wide rows, whose buffers would not
-// all fit) the two halves of a gated row pass through it one after the other.
-template <typename T, bool F16, int THREADS, int STAGES>
+// all fit) the two halves of a gated row pass through it one after the other. PLAIN: no activation and no gate (their
+// code, not run, costs 5 to 7 %).
+template <typename T, bool F16, int THREADS, int STAGES, bool PLAIN>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
     quantize_rows_kernel(const __grid_constant__ TokenQuantArgs a, int tpr) {
     using E = typename std::conditional<F16, __half, int8_t>::type;
     constexpr int kIn = 16 / sizeof(T), kPieces = kPer / kIn;            // pieces per thread
     constexpr int kOutIn = 16 / sizeof(E), kOutPieces = kPer / kOutIn;
     __shared__ float warp_max[2][32];
-    extern __shared__ __align__(16) uint4 buffers[];
+    extern __shared__ __align__(128) uint4 buffers[];
     constexpr bool kAlone = STAGES == 1;
-    const int halves = a.gated && !kAlone ? 2 : 1, stage_pieces = 32 * kPieces * halves;
+    const int halves = !PLAIN && a.gated && !kAlone ? 2 : 1, stage_pieces = 32 * kPieces * halves;
     uint4 *stages = buffers + (threadIdx.x >> 5) * STAGES * stage_pieces;
     const int rl = threadIdx.x / tpr, per_cta = blockDim.x / tpr;
     Lanes l;
@@ -432,8 +433,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) w[i] = stage[swizzle<kPieces>(l.lane, i)];
         widen<T, kPieces>(w, v);
-        if (a.act != HATQ_ACT_NONE && src >= 0) activate_all<kPer>(v, a.act);
-        if (a.gated) {
+        if (!PLAIN && a.act != HATQ_ACT_NONE && src >= 0) activate_all<kPer>(v, a.act);
+        if (!PLAIN && a.gated) {
             pair32 u[kPer / 2];
             if (kAlone) {
                 __syncwarp();
@@ -524,13 +525,13 @@ __device__ __forceinline__ void product16(float (&c)[4], const uint32_t (&a)[4],
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <typename T, bool F16>
-__global__ void __launch_bounds__(256, 4) quantize_blocks_kernel(const __grid_constant__ TokenQuantArgs a, int tpr) {
+template <typename T, bool F16, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_blocks_kernel(const __grid_constant__ TokenQuantArgs a, int tpr) {
     using E = typename std::conditional<F16, __half, int8_t>::type;
     constexpr int kStages = 2, kPieces = 4, kIn = 8, kOutIn = 16 / sizeof(E), kOutPieces = kPer / kOutIn;
-    __shared__ float warp_max[2][8];
-    __shared__ __align__(128) uint4 buffers[8][kStages][32 * kPieces];
-    uint4(*stages)[32 * kPieces] = buffers[threadIdx.x >> 5];
+    __shared__ float warp_max[2][32];
+    extern __shared__ __align__(128) uint4 buffers[];
+    uint4(*stages)[32 * kPieces] = reinterpret_cast<uint4(*)[32 * kPieces]>(buffers) + (threadIdx.x >> 5) * kStages;
     const int rl = threadIdx.x / tpr, per_cta = blockDim.x / tpr, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
     const int t0 = threadIdx.x - rl * tpr, warp_first = (t0 - lane) * kPer;
     const long long step = (long long)gridDim.x * per_cta, base = (long long)blockIdx.x * per_cta;
@@ -663,16 +664,16 @@ int threads_per_row(int c, int per) {
     return tpr;
 }
 
-template <typename T, bool F16, int THREADS, int STAGES>
+template <typename T, bool F16, int THREADS, int STAGES, bool PLAIN>
 cudaError_t quantize_rows_launch(const TokenQuantArgs &a, cudaStream_t s) {
     const int tpr = threads_per_row(a.c, kPer);
     const int per_cta = tpr >= 256 ? 1 : 256 / tpr;
     const int threads = per_cta * tpr;                                   // whole warps
-    auto k = quantize_rows_kernel<T, F16, THREADS, STAGES>;
+    auto k = quantize_rows_kernel<T, F16, THREADS, STAGES, PLAIN>;
     const int smem = threads * kPer * (int)sizeof(T) * STAGES * (a.gated && STAGES > 1 ? 2 : 1);
     static const int regs = [] {
         cudaFuncAttributes fa{};
-        return cudaFuncGetAttributes(&fa, quantize_rows_kernel<T, F16, THREADS, STAGES>) == cudaSuccess ? fa.numRegs : 128;
+        return cudaFuncGetAttributes(&fa, quantize_rows_kernel<T, F16, THREADS, STAGES, PLAIN>) == cudaSuccess ? fa.numRegs : 128;
     }();
     if (smem > 40 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -681,6 +682,19 @@ cudaError_t quantize_rows_launch(const TokenQuantArgs &a, cudaStream_t s) {
     // as many CTAs as are resident at once: they walk the rows
     const int fit = max(1, min(min(2048 / threads, 220 * 1024 / (smem + 1024)), 65536 / (regs * threads)));
     const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * fit;
+    return launch_early(k, dim3((unsigned)(ctas < room ? ctas : room)), threads, smem, s, a, tpr);
+}
+
+template <typename T, bool F16, int THREADS>
+cudaError_t quantize_blocks_launch(const TokenQuantArgs &a, cudaStream_t s) {
+    const int tpr = threads_per_row(a.c, kPer), per_cta = tpr >= 256 ? 1 : 256 / tpr, threads = per_cta * tpr;
+    const int smem = threads * 2 * kPer * 2;
+    auto k = quantize_blocks_kernel<T, F16, THREADS>;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * (1024 / threads);
     return launch_early(k, dim3((unsigned)(ctas < room ? ctas : room)), threads, smem, s, a, tpr);
 }
 
@@ -693,18 +707,15 @@ cudaError_t quantize_size(const TokenQuantArgs &a, cudaStream_t s) {
                             a, tpr);
     }
     if constexpr (sizeof(T) == 2) {
-        const int tpr = threads_per_row(a.c, kPer);
-        if (a.c <= 8192 && tpr >= 32 && a.vec && !a.gated && a.act == HATQ_ACT_NONE && a.hb >= 16) {
-            const int per_cta = tpr >= 256 ? 1 : 256 / tpr, threads = per_cta * tpr;
-            const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * (1024 / threads);
-            return launch_early(quantize_blocks_kernel<T, F16>, dim3((unsigned)(ctas < room ? ctas : room)), threads, 0, s, a, tpr);
-        }
+        if (threads_per_row(a.c, kPer) >= 32 && a.vec && !a.gated && a.act == HATQ_ACT_NONE && a.hb >= 16)
+            return a.c <= 8192 ? quantize_blocks_launch<T, F16, 256>(a, s) : quantize_blocks_launch<T, F16, 1024>(a, s);
     }
     if (a.c > 8192) {
-        if (sizeof(T) == 4 || a.gated) return quantize_rows_launch<T, F16, 1024, 1>(a, s);
-        return quantize_rows_launch<T, F16, 1024, sizeof(T) == 4 ? 1 : 2>(a, s);
+        if (sizeof(T) == 4 || a.gated) return quantize_rows_launch<T, F16, 1024, 1, false>(a, s);
+        return quantize_rows_launch<T, F16, 1024, sizeof(T) == 4 ? 1 : 2, false>(a, s);
     }
-    return quantize_rows_launch<T, F16, 256, 2>(a, s);
+    if (a.act == HATQ_ACT_NONE && !a.gated) return quantize_rows_launch<T, F16, 256, 2, true>(a, s);
+    return quantize_rows_launch<T, F16, 256, 2, false>(a, s);
 }
 
 // ------------------------------------------------------------ weight layout

@@ -55,12 +55,11 @@ struct LinearArgs {
     int y_type;
     bool y_even;                       // 16-bit outputs: pairs of an even channel and the next lie on 4-byte boundaries
     int split;                         // CTAs of a cluster that share one tile's reduction
-    int slots;                         // one-token kernel: groups the grid has room for
     int *err;
 };
 // few rows per group: integer dot products on the CUDA cores
 cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s);
-// the tensor-core kernel; tile: tokens per tile, pair: two CTAs per tile
+// the tensor-core kernel; tile: tokens per tile, pair: two CTAs per tile; clusters (of a.split CTAs, or pairs) in the grid
 cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
                              cudaStream_t s);
 

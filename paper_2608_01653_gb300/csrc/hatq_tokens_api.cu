@@ -175,7 +175,6 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
     a.y_type = y_type;
     a.y_even = ldy % 2 == 0 && aligned(y, 4);
     a.split = 1;
-    a.slots = (int)(rows < L->experts ? rows : L->experts);
     const Plan p = plan_of(rows, L, grouped, sms);
     cudaError_t e;
     if (p.few) {

@@ -823,6 +823,14 @@ def _out_of(t, types, rows, values, device):
     return code, pitch
 
 
+def _apart(t, stream):
+    """A copy whose rows lie apart, as the library takes them, made on the stream that the call runs on."""
+    if stream is None:
+        return t.contiguous()
+    with _TORCH.cuda.stream(stream):
+        return t.contiguous()
+
+
 def _flat(t, name, dtype, shape, device):
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, "
@@ -912,7 +920,7 @@ def quantize_tokens(x, hb=1, act="none", gated=False, rows=None, codes="auto", o
     device, raw = _launch_stream(x, stream)
     kind, src_rows, c, pitch = _rows_of(x, "x", _TOKEN_TYPES, device)
     if pitch < c:
-        x, pitch = x.contiguous(), c                # the library takes rows that are apart
+        x, pitch = _apart(x, stream), c
     code = _ACTS.get(act)
     if code is None:
         raise ValueError(f"unknown activation {act!r}")
@@ -958,7 +966,7 @@ def _product(x, scales, offsets, layer, dtype, out, stream):
     if k != layer.k:
         raise ValueError(f"x: rows of {k} codes, the weights take {layer.k}")
     if pitch < k:
-        x, pitch = x.contiguous(), k                # the library takes rows that are apart
+        x, pitch = _apart(x, stream), k
     if layer.device != device:
         raise ValueError(f"the weights are on cuda:{layer.device}, x on cuda:{device}")
     s_x = _flat(scales, "scales", torch.float32, (n,), device)
@@ -1015,7 +1023,7 @@ def combine_rows(y, index, weights, out=None, stream=None):
     device, raw = _launch_stream(y, stream)
     kind, rows, c, pitch = _rows_of(y, "y", _TOKEN_TYPES, device)
     if pitch < c:
-        y, pitch = y.contiguous(), c                # the library takes rows that are apart
+        y, pitch = _apart(y, stream), c
     if index.dim() != 2:
         raise ValueError(f"index: shape {tuple(index.shape)}, expected [tokens, topk]")
     t, topk = shape = index.shape
