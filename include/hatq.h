@@ -579,10 +579,13 @@ hatq_status hatq_linear_layout(const int8_t *w, long long ldw, const hatq_linear
  *   x          device codes in hatq_codes format, rows at a pitch of ldx >= k
  *   s_x        device float [rows]
  *   y          device, hatq_type y_type, pitch ldy >= n; must not overlap x
- *   workspace  device scratch, 16-byte aligned, of the bytes that
- *              hatq_linear_workspace returns for the same x, format, ldx, rows
- *              and experts (0: may be NULL); calls in flight at the same time
- *              need one each
+ *   workspace  device scratch, 16-byte aligned, or NULL. Codes that are int8, or
+ *              whose rows are off 16-byte boundaries, are taken as they lie by
+ *              the tensor-core kernel, or packed first where that pays (many
+ *              rows) and a workspace of the bytes that hatq_linear_workspace
+ *              returns for the same x, format, ldx, rows and weights is given;
+ *              results are the same. Calls in flight at the same time need one
+ *              each
  * Fp16 codes must be integers in [-128, 127]. Weights are read once per call
  * for up to a few hundred rows. Stream-ordered; an expired device wait surfaces
  * through hatq_sync_status(). */

@@ -44,8 +44,8 @@ using namespace tc;
 
 constexpr int kThreads = 640;
 // registers per thread of the five warpgroups: copies and MMAs, two of converters, two of the epilogue
-constexpr int kRegsIssue = 40, kRegsWiden = 72, kRegsOut = 144;
-constexpr int kRegShares = kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut;
+constexpr int kRegsIssue = 40;
+constexpr int kRegShares = 472;
 constexpr int kMaxSplit = 4;           // CTAs that share a reduction at most
 constexpr int kRasterN = 8;            // channel tiles that share a sweep over the token tiles
 
@@ -137,6 +137,46 @@ __device__ __forceinline__ uint32_t hsub2(uint32_t x, uint32_t y) {
     return d;
 }
 
+// 16 codes of row r from k0 < k on as bytes, zeros behind k
+__device__ __forceinline__ uint4 loose_codes(const LinearArgs &a, int r, int k0) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (a.format == HATQ_CODES_I8) {
+        const int8_t *p = reinterpret_cast<const int8_t *>(a.x) + (long long)r * a.ldx + k0;
+        if (k0 + 16 <= a.k) {
+            const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p);
+            if ((off & 15) == 0) return *reinterpret_cast<const uint4 *>(p);
+            if ((off & 7) == 0) {
+                const uint2 lo = reinterpret_cast<const uint2 *>(p)[0], hi = reinterpret_cast<const uint2 *>(p)[1];
+                return make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+            if ((off & 3) == 0) {
+                const uint32_t *q = reinterpret_cast<const uint32_t *>(p);
+                return make_uint4(q[0], q[1], q[2], q[3]);
+            }
+        }
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k0 + i < a.k) w[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    const __half *p = reinterpret_cast<const __half *>(a.x) + (long long)r * a.ldx + k0;
+    uint32_t h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (k0 + 16 <= a.k && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k0 + i < a.k) h[i >> 1] |= (uint32_t)__half_as_ushort(p[i]) << (16 * (i & 1));
+    }
+    v.x = narrow_codes(h[0], h[1]);
+    v.y = narrow_codes(h[2], h[3]);
+    v.z = narrow_codes(h[4], h[5]);
+    v.w = narrow_codes(h[6], h[7]);
+    return v;
+}
+
 template <int REGS> __device__ __forceinline__ void regs_dec() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
 }
@@ -156,14 +196,17 @@ __device__ __forceinline__ void put(void *y, int type, long long at, float v) {
     else reinterpret_cast<float *>(y)[at] = v;
 }
 
-template <int T, bool PAIR>
+template <int T, bool PAIR, bool LOOSE>
 struct Config {
     static constexpr int kCtas = PAIR ? 2 : 1;
+    static constexpr int kRegsWiden = LOOSE ? 88 : 72, kRegsOut = LOOSE ? 128 : 144;
+    static_assert(kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut <= kRegShares && !(LOOSE && PAIR), "register shares");
     // 64-code blocks per pipeline stage. The MMA warp's wait, fence and commit take about 300 cycles, so a stage
     // holds enough blocks for its MMAs to take longer: one block per stage cost 480 cycles a block at any tile width.
     static constexpr int kSub = T <= 64 ? 4 : 2;
     static constexpr int kXBytes = T / kCtas * 128;                    // one block's token codes
     static constexpr int kWOffset = kSub * kXBytes;
+    static constexpr int kChunks = T * kSub * 4 / 256;                 // LOOSE: 16-code pieces of a stage per widening thread
     static constexpr int kStageBytes = kSub * (kXBytes + kBlockBytes);
     static constexpr int kStages = 202 * 1024 / kStageBytes;
     // Blocks per hand-off from the widening warps to the MMA warp and back: all of a stage, or one where the
@@ -189,10 +232,12 @@ struct Tile {
     __device__ __forceinline__ int columns() const { return (rows + 31) & ~31; }
 };
 
-template <int T, bool PAIR>
+// LOOSE: token codes of any format, pitch and alignment, brought in and widened by the widening warps themselves
+// (their next stage's pieces on the way while one is worked on) instead of by TMA from packed fp16 codes.
+template <int T, bool PAIR, bool LOOSE>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearArgs a) {
-    using C = Config<T, PAIR>;
+    using C = Config<T, PAIR, LOOSE>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *bar_area = smem + C::kStages * C::kStageBytes;
@@ -219,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int part = PAIR ? 0 : (int)rank, parts = PAIR ? 1 : a.split;
 
     if (threadIdx.x == 0) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+        if (!LOOSE) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
         *abort_flag = 0;
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
@@ -282,11 +327,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (elect_one()) {
             const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
             const int blocks = min(C::kSub, kb1 - b);
-            mbar_expect_tx(full(s), (uint32_t)(blocks * (C::kXBytes + kBlockBytes)));
+            mbar_expect_tx(full(s), (uint32_t)(blocks * (LOOSE ? kBlockBytes : C::kXBytes + kBlockBytes)));
             bulk_load(st + C::kWOffset, w, (uint32_t)(blocks * kBlockBytes), full(s));
 #pragma unroll
             for (int q = 0; q < C::kSub; ++q)
-                if (q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
+                if (!LOOSE && q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
         }
         __syncwarp();
     };
@@ -453,13 +498,36 @@ __global__ void __launch_bounds__(kThreads, 1)
             cluster_sync();
         }
     } else if (warp < 12) {
-        regs_dec<kRegsWiden>();
+        regs_dec<C::kRegsWiden>();
         const int set = (warp >> 2) - 1;                                // takes every other block of a stage
         const int m = (warp & 3) * 32 + lane;                           // channel of the tile = tensor-memory lane
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T;
         const int tiles = total > first ? (total - first + step - 1) / step : 0;
         const int per_tile = (kb1 - kb0 + C::kSub - 1) / C::kSub, last = kb1 - kb0 - (per_tile - 1) * C::kSub;
         const long long stages = (long long)tiles * per_tile;
+        // LOOSE: this thread's pieces of the next stage (block xb of tile xtile)
+        uint4 x[C::kChunks];
+        Tile xtile{};
+        int xt = first, xb = kb0;
+        const int u = (int)threadIdx.x - 128;
+        auto fetch = [&] {
+#pragma unroll
+            for (int i = 0; i < C::kChunks; ++i) {
+                const int c = u + 256 * i, row = c / (4 * C::kSub), piece = c % (4 * C::kSub), k0 = xb * 64 + piece * 16;
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (row < xtile.rows && k0 < a.k) x[i] = loose_codes(a, xtile.row + row, k0);
+            }
+            xb += C::kSub;
+            if (xb >= kb1) {
+                xb = kb0;
+                xt += step;
+                if (xt < total) xtile = decode(xt);
+            }
+        };
+        if (LOOSE && first < total) {
+            xtile = decode(first);
+            fetch();
+        }
         // hand-offs are numbered it * kHands + h, their slots in turn; with one block each, a set takes every other one
         int s = 0, left = per_tile, slot = C::kGroup == 1 ? set : 0;
         uint32_t ph = 0, slot_ph = 1;                                   // the first use of a slot waits for nothing
@@ -473,6 +541,27 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
+            if (LOOSE) {
+                // into the layout that TMA leaves: rows of 128 bytes, 16-byte pieces swizzled by the row
+                uint8_t *xs = smem + s * C::kStageBytes;
+#pragma unroll
+                for (int i = 0; i < C::kChunks; ++i) {
+                    const int c = u + 256 * i, row = c / (4 * C::kSub), piece = c % (4 * C::kSub);
+                    uint8_t *to = xs + (piece >> 2) * C::kXBytes + row * 128;
+                    const int at = (piece & 3) * 2;
+                    const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
+                    uint32_t h[8];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        h[2 * q] = hsub2(prmt(w[q], 0x64646464u, 0x4140u), 0x64806480u);
+                        h[2 * q + 1] = hsub2(prmt(w[q], 0x64646464u, 0x4342u), 0x64806480u);
+                    }
+                    *reinterpret_cast<uint4 *>(to + ((at ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    *reinterpret_cast<uint4 *>(to + (((at + 1) ^ (row & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                if (it + 1 < stages) fetch();
+            }
 #pragma unroll
             for (int j = 0; j < (C::kGroup == 1 ? 1 : C::kGroup / 2); ++j) {
                 const int block = 2 * j + set;
@@ -515,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             cluster_sync();
         }
     } else {
-        regs_inc<kRegsOut>();
+        regs_inc<C::kRegsOut>();
         constexpr int kHalf = T / 2;
         const int half = (warp >> 2) - 3;
         const int m = (warp & 3) * 32 + lane;
@@ -718,16 +807,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-template <int T, bool PAIR>
+template <int T, bool PAIR, bool LOOSE = false>
 cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cudaStream_t s) {
-    using C = Config<T, PAIR>;
+    using C = Config<T, PAIR, LOOSE>;
     // the roles' register shares have to fit what the launch brings, or the increase would wait for ever
     static const int regs = [] {
         cudaFuncAttributes fa{};
-        return cudaFuncGetAttributes(&fa, linear_tc_kernel<T, PAIR>) == cudaSuccess ? fa.numRegs : 0;
+        return cudaFuncGetAttributes(&fa, linear_tc_kernel<T, PAIR, LOOSE>) == cudaSuccess ? fa.numRegs : 0;
     }();
     if (regs * kThreads < kRegShares * 128) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<T, PAIR, LOOSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) return e;
     const int width = PAIR ? 2 : a.split;
     cudaLaunchConfig_t cfg{};
@@ -743,13 +832,17 @@ cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cud
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = width > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, linear_tc_kernel<T, PAIR>, tm, a);
+    return cudaLaunchKernelEx(&cfg, linear_tc_kernel<T, PAIR, LOOSE>, tm, a);
 }
 
 }  // namespace
 
-cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
+cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, bool loose, int clusters,
                              cudaStream_t s) {
+    if (loose)
+        return tile == 32   ? launch<32, false, true>(tm, a, clusters, s)
+               : tile == 64 ? launch<64, false, true>(tm, a, clusters, s)
+                            : launch<128, false, true>(tm, a, clusters, s);
     if (pair) return tile == 128 ? launch<128, true>(tm, a, clusters, s) : launch<192, true>(tm, a, clusters, s);
     switch (tile) {
         case 32: return launch<32, false>(tm, a, clusters, s);

@@ -823,14 +823,6 @@ __device__ __forceinline__ void store_y(void *y, int type, long long at, float v
     else reinterpret_cast<__nv_bfloat16 *>(y)[at] = __float2bfloat16_rn(v);
 }
 
-// four fp16 codes as bytes: 1152 + code has code + 128 in its low byte
-__device__ __forceinline__ uint32_t narrow4(uint32_t x, uint32_t y) {
-    uint32_t a, b;
-    asm("add.f16x2 %0, %1, %2;" : "=r"(a) : "r"(x), "r"(0x64806480u));
-    asm("add.f16x2 %0, %1, %2;" : "=r"(b) : "r"(y), "r"(0x64806480u));
-    return __byte_perm(a, b, 0x6420) ^ 0x80808080u;
-}
-
 template <int MT, int R>
 __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_constant__ LinearArgs a) {
     constexpr int kCh = 8 * R, kAhead = 8 / R;                          // channels of the CTA, blocks on their way
@@ -879,7 +871,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
                 const __half *p = reinterpret_cast<const __half *>(a.x) + r * a.ldx + c;
                 if (c + 16 <= a.k && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
                     const uint4 lo = reinterpret_cast<const uint4 *>(p)[0], hi = reinterpret_cast<const uint4 *>(p)[1];
-                    v = make_uint4(narrow4(lo.x, lo.y), narrow4(lo.z, lo.w), narrow4(hi.x, hi.y), narrow4(hi.z, hi.w));
+                    v = make_uint4(narrow_codes(lo.x, lo.y), narrow_codes(lo.z, lo.w), narrow_codes(hi.x, hi.y), narrow_codes(hi.z, hi.w));
                 } else {
                     for (int q = 0; q < 16; ++q) b[q] = c + q < a.k ? (int8_t)__half2int_rn(p[q]) : 0;
                 }

@@ -59,8 +59,9 @@ struct LinearArgs {
 };
 // few rows per group: integer dot products on the CUDA cores
 cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s);
-// the tensor-core kernel; tile: tokens per tile, pair: two CTAs per tile; clusters (of a.split CTAs, or pairs) in the grid
-cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, int clusters,
+// the tensor-core kernel; tile: tokens per tile, pair: two CTAs per tile, loose: token codes as they lie (no tensor map);
+// clusters (of a.split CTAs, or pairs) in the grid
+cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int tile, bool pair, bool loose, int clusters,
                              cudaStream_t s);
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
@@ -72,6 +73,13 @@ cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long lon
 // access to global memory, until everything before it in the stream is done and
 // visible. From then on its own successor may be started the same way.
 #ifdef __CUDACC__
+// four fp16 codes as bytes: 1152 + code has code + 128 in its low byte
+__device__ __forceinline__ uint32_t narrow_codes(uint32_t x, uint32_t y) {
+    uint32_t a, b;
+    asm("add.f16x2 %0, %1, %2;" : "=r"(a) : "r"(x), "r"(0x64806480u));
+    asm("add.f16x2 %0, %1, %2;" : "=r"(b) : "r"(y), "r"(0x64806480u));
+    return __byte_perm(a, b, 0x6420) ^ 0x80808080u;
+}
 __device__ __forceinline__ void after_prior_kernels() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -48,8 +48,13 @@ struct Plan {
     int tokens;      // rows per pass of it, or per tile of the tensor-core kernel
     bool pair;       // two CTAs per tile
     int split;       // CTAs that share a tile's reduction
+    bool pack;       // codes are packed as TMA takes them first
     long long tiles;
 };
+
+// How the tensor cores may take x: as it lies (fp16 at a pitch and a base that TMA takes), by the widening warps
+// (anything else), or that or packed into a workspace first.
+enum Operand { kDirect, kLoose, kEither };
 
 // Which kernel (hatq_tokens.cu, hatq_linear.cu) and which tile. The dot-product kernel has no pipeline to fill, but
 // its instructions are slow and every CTA brings in all rows. Measured, against the tensor-core kernel: 4096 x 4096
@@ -57,8 +62,10 @@ struct Plan {
 // 16384 x 4096 with 1 / 2 rows 14 / 23 against 16.6; experts of 2048 x 1536 with a row each, 8 / 16 / 24 of them,
 // 5.5 / 12 / 15 against 12 / 19 / 19. Of the tensor-core kernel's tiles the one with the least estimated time: waves
 // of tiles x blocks of the reduction x time per block, the last measured with every SM at work (a wider tile costs
-// more per block and less per product), and about 0.8 us to join a split reduction.
-Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms) {
+// more per block and less per product), and about 0.8 us to join a split reduction. Codes that TMA cannot take are
+// brought in by the widening warps, with single-CTA tiles only (48 rows, 4096 -> 8192: 16.8 us against 12.0; 512 rows,
+// 4096 -> 4096: 36 against 16.5), or packed first: a launch of about 3 us and 3 bytes a code.
+Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms, Operand operand) {
     Plan p{};
     const int k_pad = round_up(L->k, 64), kb = k_pad / 64, n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
     const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
@@ -76,6 +83,7 @@ Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms
     long long best = LLONG_MAX;
     for (const auto &o : options) {
         const int ctas = o.pair ? 2 : 1, room = sms / ctas;
+        if (o.pair && operand == kLoose) continue;
         // experts leave half a tile over each, and one tile at least
         const long long full = (rows + o.tokens - 1) / o.tokens, ragged = rows / o.tokens + held / 2;
         const long long tiles = (!grouped ? full : ragged > held ? ragged : held) * ((n_tiles + ctas - 1) / ctas);
@@ -83,8 +91,12 @@ Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms
         for (int split = 1; split <= (o.pair ? 1 : 4); split *= 2) {
             if (split > 1 && (tiles * split > (split == 4 ? room * 15 / 16 : room) || kb / split < 4)) break;
             const long long ns = (tiles * split + room - 1) / room * ((kb + split - 1) / split) * o.ns + (split > 1 ? 800 : 0);
-            if (ns < best) {
-                best = ns;
+            const long long loose = o.pair ? LLONG_MAX : ns * 185 / 100;
+            const long long packed = operand == kLoose ? LLONG_MAX : ns + 3000 + rows * k_pad * 3 / 5000;
+            const long long cost = operand == kDirect ? ns : loose < packed ? loose : packed;
+            if (cost < best) {
+                best = cost;
+                p.pack = operand == kEither && packed <= loose;
                 p.tokens = o.tokens;
                 p.pair = o.pair;
                 p.split = split;
@@ -124,8 +136,9 @@ bool direct(const void *x, int format, long long ldx) {
     return format == HATQ_CODES_F16 && ldx % 8 == 0 && aligned(x, 16);
 }
 
+// what packing takes; it is used where it pays
 size_t workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L, bool grouped) {
-    if (rows == 0 || plan_of(rows, L, grouped, 152).few || direct(x, format, ldx)) return 0;
+    if (rows == 0 || direct(x, format, ldx) || plan_of(rows, L, grouped, 152, kEither).few) return 0;
     return (size_t)rows * (size_t)round_up(L->k, 64) * 2;
 }
 
@@ -175,34 +188,36 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
     a.y_type = y_type;
     a.y_even = ldy % 2 == 0 && aligned(y, 4);
     a.split = 1;
-    const Plan p = plan_of(rows, L, grouped, sms);
+    const bool as_it_lies = direct(x, format, ldx);
+    const bool room_to_pack = workspace && workspace_bytes >= (size_t)rows * (size_t)round_up(L->k, 64) * 2;
+    if (workspace && !aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const Plan p = plan_of(rows, L, grouped, sms, as_it_lies ? kDirect : room_to_pack ? kEither : kLoose);
     cudaError_t e;
     if (p.few) {
         if ((e = hatq::launch_linear_few(a, p.tokens, s)) != cudaSuccess) return cuda_fail(e, "product launch");
         return HATQ_OK;
     }
-    if (!direct(x, format, ldx)) {
-        const size_t need = workspace_of(x, format, ldx, rows, L, grouped);
-        if (!workspace || workspace_bytes < need)
-            return fail(HATQ_ERR_INVALID_ARG, "the product needs a workspace of %zu bytes", need);
-        if (!aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    if (p.pack) {
         if ((e = hatq::launch_pack_codes(x, format, ldx, rows, L->k, a.kb * 64, workspace, s)) != cudaSuccess)
             return cuda_fail(e, "code packing launch");
         a.x = workspace;
         a.ldx = a.kb * 64;
         a.format = HATQ_CODES_F16;
     }
+    const bool loose = !as_it_lies && !p.pack;
     const int ctas = p.pair ? 2 : 1;
     if (p.tiles > INT_MAX / 16) return fail(HATQ_ERR_UNSUPPORTED, "too many output tiles");
     a.split = p.split;
-    CUtensorMap tm;
-    const CUresult r = hatq::encode_tiled_2d(&tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, (unsigned long long)a.k,
-                                             (unsigned long long)rows, (unsigned long long)a.ldx * 2, 64,
-                                             (unsigned)(p.tokens / ctas));
-    if (r != CUDA_SUCCESS) return fail(HATQ_ERR_CUDA, "code tensor map encoding failed (%d)", (int)r);
+    CUtensorMap tm{};
+    if (!loose) {
+        const CUresult r = hatq::encode_tiled_2d(&tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, (unsigned long long)a.k,
+                                                 (unsigned long long)rows, (unsigned long long)a.ldx * 2, 64,
+                                                 (unsigned)(p.tokens / ctas));
+        if (r != CUDA_SUCCESS) return fail(HATQ_ERR_CUDA, "code tensor map encoding failed (%d)", (int)r);
+    }
     const int room = sms / ctas;
     const int clusters = a.split > 1 ? (int)p.tiles : (int)(p.tiles < room ? p.tiles : room);
-    if ((e = hatq::launch_linear_tc(tm, a, p.tokens, p.pair, clusters, s)) != cudaSuccess)
+    if ((e = hatq::launch_linear_tc(tm, a, p.tokens, p.pair, loose, clusters, s)) != cudaSuccess)
         return cuda_fail(e, "product launch");
     return HATQ_OK;
 }

@@ -864,7 +864,7 @@ class LinearWeights:
         self.experts, self.n, self.k, self.grouped = experts, n, k, grouped
         self.codes, self.windows, self.s_w, self.bias = codes, windows, s_w, bias
         self.device = codes.get_device()
-        self.row_bytes = 2 * (-(-k // 64) * 64)     # of hatq_linear's workspace
+        self.size, self.row_bytes = n * k, 2 * (-(-k // 64) * 64)    # products per row; hatq_linear's workspace
         self.struct = LinearWeightsStruct(experts, n, k, 0, codes.data_ptr(), windows.data_ptr(), s_w.data_ptr(),
                                           None if bias is None else bias.data_ptr())
         self.ref = ctypes.byref(self.struct)
@@ -979,16 +979,14 @@ def _product(x, scales, offsets, layer, dtype, out, stream):
         kind, out_pitch = _out_of(out, _TOKEN_TYPES, n, layer.n, device)
     lib, px = _LIB or load(), x.data_ptr()
     ws, size = None, 0
-    if n > 2 and not (fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0):
-        if n <= 64:                                 # few rows mostly need no workspace
-            need = ctypes.c_size_t()
-            _check(lib.hatq_linear_workspace(px, fmt, pitch, n, layer.ref, ctypes.byref(need)))
-            size = need.value
-        else:
-            size = n * layer.row_bytes
-        if size:
-            scratch = _empty(x, (size,), torch.uint8, stream)
-            ws = scratch.data_ptr()
+    if max(n, 32 * min(n, layer.experts)) * layer.size > 1_500_000_000 and not (
+            fmt == CODES_F16 and pitch % 8 == 0 and px % 16 == 0):
+        # More than about ten microseconds of products, or of weights to read: packing the codes may pay. Below, the
+        # workspace and the second launch cost the host more than the GPU gains (777 rows, 1000 -> 1234: 20.6 us a
+        # call with them, 12.6 us without).
+        size = n * layer.row_bytes
+        scratch = _empty(x, (size,), torch.uint8, stream)
+        ws = scratch.data_ptr()
     if offsets is None:
         st = lib.hatq_linear(px, fmt, pitch, s_x, n, layer.ref, kind, out.data_ptr(), out_pitch, ws, size, raw)
     else:

@@ -134,6 +134,20 @@ def test_linear_weights_from_strided_and_float_tensors():
     assert torch.equal(y, ref) and torch.equal(z, ref)
 
 
+@pytest.mark.parametrize("kind,k", [("i8", 2000), ("i8", 2001), ("f16", 2003), ("f16", 1024)])
+def test_linear_of_many_rows_in_any_format(kind, k):
+    rows, n = 3500, 4000
+    x, w = codes(rows, k, 23, kind), codes(n, k, 24)
+    one = torch.ones(n, device="cuda")
+    L = H.prepare_linear(w, scales=one)
+    y = H.linear(x, one[:rows].contiguous(), L, dtype=torch.float32)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    z = H.grouped_linear(x, one[:rows].contiguous(), off, H.prepare_linear(w[None], scales=one[None]), dtype=torch.float32)
+    finish()
+    ref = integer_sums(x, w).float()
+    assert torch.equal(y, ref) and torch.equal(z, ref)
+
+
 @pytest.mark.parametrize("rows", [2, 20, 150, 400])
 def test_a_nan_scale_stays_in_its_row(rows):
     x, w = codes(rows, 128, 15, "f16"), codes(64, 128, 16)
