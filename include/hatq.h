@@ -599,7 +599,7 @@ hatq_status hatq_linear(const void *x, int format, long long ldx, const float *s
  * rows offsets[e] .. offsets[e + 1] - 1 (device int32 [experts + 1], ascending,
  * within [0, rows]; experts may hold no row). Rows that no expert holds are not
  * written. Offsets are read on the device only; values outside [0, rows] are
- * clamped to it, and an expert whose end lies before its start holds nothing. */
+ * clamped to it, and one below an earlier one counts as the earlier one. */
 hatq_status hatq_grouped_linear(const void *x, int format, long long ldx, const float *s_x, long long rows,
                                 const int32_t *offsets, const hatq_linear_weights *L, int y_type, void *y,
                                 long long ldy, void *workspace, size_t workspace_bytes, hatq_stream stream);

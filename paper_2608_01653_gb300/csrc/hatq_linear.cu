@@ -25,11 +25,19 @@
 // tokens per warpgroup). Two accumulators alternate, so the epilogue of one
 // window or tile runs under the MMAs of the next.
 //
-// kPair: two CTAs (one cluster) compute 256 channels x kT tokens with
+// PAIR: two CTAs (one cluster) compute 256 channels x T tokens with
 // cta_group::2; each widens its own 128 channels and holds half of the tokens,
 // which halves the shared-memory traffic per product. split > 1: the CTAs of a
 // cluster share one tile's reduction and add their int32 sums through
-// distributed shared memory (integers: the order does not matter).
+// distributed shared memory (integers: the order does not matter). LOOSE: token
+// codes of any format, pitch and alignment, brought in and widened by the
+// widening warps (their next stage's pieces on the way while one is worked on)
+// instead of by TMA.
+//
+// Bound by the tensor cores where rows are many (8192 x 4096 -> 16384: 545 us,
+// 2019 TFLOP/s, the tensor pipe 0.91 active), by the weights' bytes where they
+// are few per expert (256 rows, 61 experts of 2048 x 2048: 45 us, 5.7 TB/s), by
+// latency in between (48 rows, 4096 -> 8192: 12 us against 5.1 us of bytes).
 // Every wait is bounded, as in the other tensor-core kernels.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -232,8 +240,6 @@ struct Tile {
     __device__ __forceinline__ int columns() const { return (rows + 31) & ~31; }
 };
 
-// LOOSE: token codes of any format, pitch and alignment, brought in and widened by the widening warps themselves
-// (their next stage's pieces on the way while one is worked on) instead of by TMA from packed fp16 codes.
 template <int T, bool PAIR, bool LOOSE>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ LinearArgs a) {
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // per expert: token tiles before it, its rows, its exact window
     int *tile_start = reinterpret_cast<int *>(bar_area + 1024), *first_row = tile_start + kMaxExperts + 1,
         *end_row = first_row + kMaxExperts, *window_of = end_row + kMaxExperts;
-    __shared__ int warp_sums[kThreads / 32];
+    __shared__ int warp_sums[kThreads / 32], warp_tops[kThreads / 32];
     __shared__ int s_skip;
 
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -367,15 +373,31 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     }
     if (a.offsets) {
+        // An expert's rows begin at the largest offset up to its own, so that no offsets, ascending or not, give a row
+        // to two experts: first the running maximum, then the running sum of the token tiles.
+        const int e0 = 2 * threadIdx.x;
+        int o[3], top = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) o[i] = e0 + i <= a.experts ? min(max(a.offsets[e0 + i], 0), a.rows) : 0;
+        top = max(o[0], o[1]);
+        for (int m = 1; m < 32; m <<= 1) {
+            const int other = __shfl_up_sync(0xffffffffu, top, m);
+            if (lane >= m) top = max(top, other);
+        }
+        if (lane == 31) warp_tops[warp] = top;
+        top = __shfl_up_sync(0xffffffffu, top, 1);
+        if (lane == 0) top = 0;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) top = max(top, warp_tops[w]);
         int c[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int e = 2 * threadIdx.x + i;
-            if (e < a.experts) {
-                const int lo = min(max(a.offsets[e], 0), a.rows), hi = min(max(a.offsets[e + 1], 0), a.rows);
-                first_row[e] = lo;
-                end_row[e] = hi;
-                c[i] = hi > lo ? (hi - lo + T - 1) / T : 0;
+            const int lo = max(top, o[i]), hi = max(lo, o[i + 1]);
+            top = lo;
+            if (e0 + i < a.experts) {
+                first_row[e0 + i] = lo;
+                end_row[e0 + i] = hi;
+                c[i] = (hi - lo + T - 1) / T;
             }
         }
         int sum = c[0] + c[1];

@@ -832,16 +832,21 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
     after_prior_kernels();
     int e = 0, r0 = 0, r1 = a.rows;
     if (a.offsets) {
-        // the expert of row blockIdx.y: as many experts end at or before it. The CTA takes the row and the next
-        // MT - 1 of its expert; the other rows' CTAs leave.
-        for (int g = 0; g < a.experts; g += kFewThreads)
-            e += __syncthreads_count(g + (int)threadIdx.x < a.experts &&
-                                     a.offsets[g + threadIdx.x + 1] <= (int)blockIdx.y);
-        if (e >= a.experts) return;
-        const int lo = min(max(a.offsets[e], 0), a.rows);
+        // row blockIdx.y, of the expert before the first offset above it (one row per CTA: MT is 1)
+        __shared__ int above[kFewWarps];
         r0 = (int)blockIdx.y;
-        r1 = min(min(max(a.offsets[e + 1], 0), a.rows), r0 + MT);
-        if (r0 < lo || (r0 - lo) % MT != 0) return;
+        r1 = r0 + 1;
+        int mine = INT_MAX;
+        for (int g = threadIdx.x; g <= a.experts; g += kFewThreads)
+            if (a.offsets[g] > r0) mine = min(mine, g);
+        mine = __reduce_min_sync(0xffffffffu, mine);
+        if ((threadIdx.x & 31) == 0) above[threadIdx.x >> 5] = mine;
+        __syncthreads();
+        int to = INT_MAX;
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) to = min(to, above[w]);
+        if (to == 0 || to > a.experts) return;                          // no expert holds the row
+        e = to - 1;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ch_l = lane & 7, j = lane >> 3;
     const int ch0 = blockIdx.x * kCh;

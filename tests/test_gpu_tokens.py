@@ -260,6 +260,22 @@ def test_offsets_are_clamped_to_the_rows(rows):
     assert torch.equal(y, grouped_reference(x, w, fine))
 
 
+@pytest.mark.parametrize("rows", [7, 20, 60, 700])
+def test_offsets_that_step_back(rows):
+    """One below an earlier one counts as the earlier one: no row belongs to two experts."""
+    e = 70
+    x, w = codes(rows, 64, 41, "f16"), codes(e * 32, 64, 42).view(e, 32, 64)
+    off = torch.randint(-3, rows + 3, (e + 1,), generator=gen(43), device="cuda", dtype=torch.int32)
+    off[0], off[5], off[6], off[-1] = 1, rows // 2, 0, rows // 3
+    fine = torch.cummax(off.clamp(0, rows), 0)[0]
+    out = torch.full((rows, 32), -7.0, device="cuda")
+    H.grouped_linear(x, torch.ones(rows, device="cuda"), off, H.prepare_linear(w, scales=torch.ones(e, 32, device="cuda")), out=out)
+    finish()
+    ref = grouped_reference(x, w, fine.int())
+    held = ~ref[:, 0].isnan()
+    assert bool(held.any()) and torch.equal(out[held], ref[held]) and bool((out[~held] == -7).all())
+
+
 def test_grouped_scales_and_bias_belong_to_the_expert():
     counts, k, n = [3, 0, 90, 41], 192, 100
     rows = sum(counts)
