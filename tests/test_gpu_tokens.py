@@ -202,6 +202,26 @@ def test_linear_offsets_past_32_bits():
         assert torch.equal(y[r], integer_sums(x[r:r + 1], w)[0].bfloat16())
 
 
+@pytest.mark.parametrize("rows,k,n,kind", [(20, 2048, 512, "f16"), (60, 700, 300, "i8"), (600, 1024, 600, "f16"),
+                                           (2000, 4096, 4096, "f16")])
+def test_linear_behind_an_expired_wait(rows, k, n, kind):
+    """A product enqueued behind a wait that ran out leaves its output alone; after the status was read all is as before."""
+    x, w = codes(rows, k, 25, kind), codes(n, k, 26)
+    one = torch.ones(max(rows, n), device="cuda")
+    L, s = H.prepare_linear(w, scales=one[:n]), one[:rows].contiguous()
+    finish()
+    out = torch.full((rows, n), 3.0, device="cuda")
+    H.selftest_wait(1000)
+    H.linear(x, s, L, out=out)
+    torch.cuda.synchronize()
+    with pytest.raises(H.HatqError) as e:
+        H.sync_status()
+    assert e.value.status == H.ERR_TIMEOUT and bool((out == 3).all())
+    H.linear(x, s, L, out=out)
+    finish()
+    assert torch.equal(out, integer_sums(x, w).float())
+
+
 # ------------------------------------------------------------------ grouped_linear
 
 def offsets_of(counts):
