@@ -838,7 +838,8 @@ cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cud
         return cudaFuncGetAttributes(&fa, linear_tc_kernel<T, PAIR, LOOSE>) == cudaSuccess ? fa.numRegs : 0;
     }();
     if (regs * kThreads < kRegShares * 128) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<T, PAIR, LOOSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear_tc_kernel<T, PAIR, LOOSE>), C::kSmem, allowed);
     if (e != cudaSuccess) return e;
     const int width = PAIR ? 2 : a.split;
     cudaLaunchConfig_t cfg{};

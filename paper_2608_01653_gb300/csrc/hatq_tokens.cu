@@ -675,10 +675,9 @@ cudaError_t quantize_rows_launch(const TokenQuantArgs &a, cudaStream_t s) {
         cudaFuncAttributes fa{};
         return cudaFuncGetAttributes(&fa, quantize_rows_kernel<T, F16, THREADS, STAGES, PLAIN>) == cudaSuccess ? fa.numRegs : 128;
     }();
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(k), smem, allowed);
+    if (e != cudaSuccess) return e;
     // as many CTAs as are resident at once: they walk the rows
     const int fit = max(1, min(min(2048 / threads, 220 * 1024 / (smem + 1024)), 65536 / (regs * threads)));
     const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * fit;
@@ -690,10 +689,9 @@ cudaError_t quantize_blocks_launch(const TokenQuantArgs &a, cudaStream_t s) {
     const int tpr = threads_per_row(a.c, kPer), per_cta = tpr >= 256 ? 1 : 256 / tpr, threads = per_cta * tpr;
     const int smem = threads * 2 * kPer * 2;
     auto k = quantize_blocks_kernel<T, F16, THREADS>;
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(k), smem, allowed);
+    if (e != cudaSuccess) return e;
     const long long ctas = (a.rows + per_cta - 1) / per_cta, room = (long long)a.sms * (1024 / threads);
     return launch_early(k, dim3((unsigned)(ctas < room ? ctas : room)), threads, smem, s, a, tpr);
 }
@@ -1069,10 +1067,9 @@ template <int MT, int R>
 cudaError_t few_launch(const LinearArgs &a, cudaStream_t s) {
     const dim3 grid((a.n + 8 * R - 1) / (8 * R), a.offsets ? a.rows : 1);
     const int smem = MT * a.kb * 64;
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<MT, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-    }
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear_few_kernel<MT, R>), smem, allowed);
+    if (e != cudaSuccess) return e;
     return launch_early(linear_few_kernel<MT, R>, grid, kFewThreads, smem, s, a);
 }
 }  // namespace

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "hatq.h"
 
 namespace hatq {
@@ -102,6 +104,19 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, int 
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+// Lets `kernel` have `bytes` of dynamic shared memory: asked of the driver once per device and size, not per launch.
+// `allowed` is the caller's static array; host threads that race ask twice.
+inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<int> (&allowed)[64]) {
+    if (bytes <= 40 * 1024) return cudaSuccess;                          // what every launch may have (48 KB), less static arrays
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && allowed[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(bytes, std::memory_order_relaxed);
+    return e;
 }
 
 // host services of hatq_api.cu
