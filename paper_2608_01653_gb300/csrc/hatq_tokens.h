@@ -106,7 +106,7 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, int 
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
-// Lets `kernel` have `bytes` of dynamic shared memory: asked of the driver once per device and size, not per launch.
+// Lets `kernel` have `bytes` of dynamic shared memory: asked of CUDA once per device and size, not per launch.
 // `allowed` is the caller's static array; host threads that race ask twice.
 inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<int> (&allowed)[64]) {
     if (bytes <= 40 * 1024) return cudaSuccess;                          // what every launch may have (48 KB), less static arrays
