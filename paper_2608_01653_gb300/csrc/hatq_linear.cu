@@ -52,8 +52,9 @@ using namespace tc;
 
 constexpr int kThreads = 640;
 // registers per thread of the five warpgroups: copies and MMAs, two of converters, two of the epilogue
+constexpr int kLaunchRegs = 96;         // what __launch_bounds__ gives 640 threads
 constexpr int kRegsIssue = 40;
-constexpr int kRegShares = 472;
+constexpr int kRegShares = 472;         // of 5 * 96
 constexpr int kMaxSplit = 4;           // CTAs that share a reduction at most
 constexpr int kRasterN = 8;            // channel tiles that share a sweep over the token tiles
 
@@ -185,11 +186,11 @@ __device__ __forceinline__ uint4 loose_codes(const LinearArgs &a, int r, int k0)
     return v;
 }
 
-template <int REGS> __device__ __forceinline__ void regs_dec() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
-}
-template <int REGS> __device__ __forceinline__ void regs_inc() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS));
+// a warpgroup's share, from the launch's: fewer or more, each has its own instruction
+template <int REGS> __device__ __forceinline__ void set_regs() {
+    static_assert(REGS != kLaunchRegs && REGS % 8 == 0, "register share");
+    if constexpr (REGS < kLaunchRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
 __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
@@ -207,8 +208,9 @@ __device__ __forceinline__ void put(void *y, int type, long long at, float v) {
 template <int T, bool PAIR, bool LOOSE>
 struct Config {
     static constexpr int kCtas = PAIR ? 2 : 1;
-    static constexpr int kRegsWiden = LOOSE ? 88 : 72, kRegsOut = LOOSE ? 128 : 144;
-    static_assert(kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut <= kRegShares && !(LOOSE && PAIR), "register shares");
+    static constexpr int kRegsWiden = LOOSE ? 104 : 72, kRegsOut = LOOSE ? 112 : 144;
+    static_assert(kRegsIssue + 2 * kRegsWiden + 2 * kRegsOut <= kRegShares && kRegShares <= 5 * kLaunchRegs, "register shares");
+    static_assert(!(LOOSE && PAIR), "loose codes: single CTAs");
     // 64-code blocks per pipeline stage. The MMA warp's wait, fence and commit take about 300 cycles, so a stage
     // holds enough blocks for its MMAs to take longer: one block per stage cost 480 cycles a block at any tile width.
     static constexpr int kSub = T <= 64 ? 4 : 2;
@@ -423,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int total = skip ? 0 : tile_start[a.experts] * pairs_n;
     bool ok = true;
     if (warp < 4) {
-        regs_dec<kRegsIssue>();
+        set_regs<kRegsIssue>();
         if (warp == 0) {
             // what was asked for before the roles began: the first stages of the first tile
             int s = issued % C::kStages, done = issued;
@@ -520,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             cluster_sync();
         }
     } else if (warp < 12) {
-        regs_dec<C::kRegsWiden>();
+        set_regs<C::kRegsWiden>();
         const int set = (warp >> 2) - 1;                                // takes every other block of a stage
         const int m = (warp & 3) * 32 + lane;                           // channel of the tile = tensor-memory lane
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T;
@@ -626,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             cluster_sync();
         }
     } else {
-        regs_inc<C::kRegsOut>();
+        set_regs<C::kRegsOut>();
         constexpr int kHalf = T / 2;
         const int half = (warp >> 2) - 3;
         const int m = (warp & 3) * 32 + lane;
@@ -832,12 +834,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <int T, bool PAIR, bool LOOSE = false>
 cudaError_t launch(const CUtensorMap &tm, const LinearArgs &a, int clusters, cudaStream_t s) {
     using C = Config<T, PAIR, LOOSE>;
-    // the roles' register shares have to fit what the launch brings, or the increase would wait for ever
+    // the roles' shares go by what the launch brings: a decrease below it, increases that fit its sum
     static const int regs = [] {
         cudaFuncAttributes fa{};
         return cudaFuncGetAttributes(&fa, linear_tc_kernel<T, PAIR, LOOSE>) == cudaSuccess ? fa.numRegs : 0;
     }();
-    if (regs * kThreads < kRegShares * 128) return cudaErrorInvalidConfiguration;
+    if (regs != kLaunchRegs) return cudaErrorInvalidConfiguration;
     static std::atomic<int> allowed[64];
     const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear_tc_kernel<T, PAIR, LOOSE>), C::kSmem, allowed);
     if (e != cudaSuccess) return e;
