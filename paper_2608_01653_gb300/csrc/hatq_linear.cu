@@ -37,7 +37,7 @@
 // Bound by the tensor cores where rows are many (8192 x 4096 -> 16384: 545 us,
 // 2019 TFLOP/s, the tensor pipe 0.91 active), by the weights' bytes where they
 // are few per expert (256 rows, 61 experts of 2048 x 2048: 45 us, 5.7 TB/s), by
-// latency in between (48 rows, 4096 -> 8192: 12 us against 5.1 us of bytes).
+// latency in between (48 rows, 4096 -> 8192: 11.8 us against 5.1 us of bytes).
 // Every wait is bounded, as in the other tensor-core kernels.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -788,35 +788,47 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             cluster_sync();
-            if (ok && first < total) {
-                const uint32_t mine = smem_addr(smem) + 16u * (uint32_t)lane;
+            // the parts' sums are all asked for before the first is used, and the others may leave once they are here:
+            // the second barrier completes while the outputs are written
+            constexpr int kBatch = kOwn < 4 ? kOwn : 4;
+            const bool finish = ok && first < total;
+            const uint32_t mine = smem_addr(smem) + 16u * (uint32_t)lane;
 #pragma unroll
-                for (int i = 0; i < kOwn; ++i) {
-                    const int c = c0 + 8 * parts * i;
-                    if (c >= tile.rows) break;
-                    int4 v[kMaxSplit];
+            for (int i0 = 0; i0 < kOwn; i0 += kBatch) {
+                int4 v[kBatch][kMaxSplit];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const int c = c0 + 8 * parts * (i0 + i);
 #pragma unroll
                     for (int q = 0; q < kMaxSplit; ++q)
-                        if (q < parts) v[q] = load_cluster(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q));
-                    int4 sum = v[0];
+                        if (finish && c < tile.rows && q < parts)
+                            v[i][q] = load_cluster(map_shared(mine + (uint32_t)c * (kRowTile * 4), (uint32_t)q));
+                        else v[i][q] = make_int4(0, 0, 0, 0);
+                }
 #pragma unroll
-                    for (int q = 1; q < kMaxSplit; ++q)
-                        if (q < parts) {
-                            sum.x += v[q].x;
-                            sum.y += v[q].y;
-                            sum.z += v[q].z;
-                            sum.w += v[q].w;
-                        }
-                    const int part4[4] = {sum.x, sum.y, sum.z, sum.w};
+                for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+                    for (int q = 1; q < kMaxSplit; ++q) {
+                        v[i][0].x += v[i][q].x;
+                        v[i][0].y += v[i][q].y;
+                        v[i][0].z += v[i][q].z;
+                        v[i][0].w += v[i][q].w;
+                    }
+                if (i0 + kBatch >= kOwn) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const int c = c0 + 8 * parts * (i0 + i);
+                    if (!finish || c >= tile.rows) break;
+                    const int part4[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w};
                     const long long at = (long long)(tile.row + c) * a.ldy + ch;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float r = (float)part4[q] * sw[q] * sx[i];
+                        const float r = (float)part4[q] * sw[q] * sx[i0 + i];
                         if (ch + q < a.n) put(a.y, a.y_type, at + q, a.bias ? r + bias[q] : r);
                     }
                 }
             }
-            cluster_sync();
+            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         }
     }
     tc_fence_before();

@@ -63,7 +63,7 @@ enum Operand { kDirect, kLoose, kEither };
 // 5.5 / 12 / 15 against 12 / 19 / 19. Of the tensor-core kernel's tiles the one with the least estimated time: waves
 // of tiles x blocks of the reduction x time per block, the last measured with every SM at work (a wider tile costs
 // more per block and less per product), and about 0.8 us to join a split reduction. Codes that TMA cannot take are
-// brought in by the widening warps, with single-CTA tiles only (48 rows, 4096 -> 8192: 16.8 us against 12.0; 512 rows,
+// brought in by the widening warps, with single-CTA tiles only (48 rows, 4096 -> 8192: 16.8 us against 11.8; 512 rows,
 // 4096 -> 4096: 36 against 16.5), or packed first: a launch of about 3 us and 3 bytes a code.
 Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms, Operand operand) {
     Plan p{};

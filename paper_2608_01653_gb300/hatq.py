@@ -873,9 +873,9 @@ class LinearWeights:
 def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeights:
     """The weights of linear (w [n][k]) or grouped_linear (w [experts][n][k]), on the device.
 
-    w in float32 / float16 / bfloat16 is transformed along k in blocks of hb and
-    quantized with one scale per output channel, as hatq_quantize_tokens does
-    with a row; quantize_tokens must be called with the same hb. w in int8 is
+    w in float32 / float16 / bfloat16 (k <= 32768) is transformed along k in blocks
+    of hb and quantized with one scale per output channel, as hatq_quantize_tokens
+    does with a row; quantize_tokens must be called with the same hb. w in int8 is
     taken as it is, with `scales` ([n] or [experts][n], float32). bias: [n] or
     [experts][n], any floating type."""
     torch = _token_torch()
