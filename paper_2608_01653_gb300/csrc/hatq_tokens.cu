@@ -943,102 +943,139 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
 // Bound by the rows' bytes. A thread owns 16 bytes of a token's row; the rows
 // of up to kAhead slots are on their way at a time, and the next token's indices
 // and weights before this one's rows are added up. Fewer slots leave room for
-// more threads. 8192 tokens x 8 rows of 2048 bf16: 50 us, 6.1 TB/s.
+// more threads. 8192 tokens x 8 rows of 2048 bf16: 48 us, 6.3 TB/s.
 
 constexpr int combine_ctas(int ahead) { return ahead == 8 ? 3 : ahead == 4 ? 4 : 6; }
 
-template <typename T, bool VEC, int kAhead>
+// UNIT: bytes that a load or a store takes. Rows on 16-byte boundaries: one of 16 per thread and row; else four of 4 or
+// of 2, `width` units apart, so that the lanes of each lie next to each other.
+template <typename T, int UNIT, int kAhead>
 __global__ void __launch_bounds__(256, combine_ctas(kAhead)) combine_rows_kernel(const T *y, long long ldy, long long rows,
                                                                                  const int32_t *index, const float *weights,
                                                                                  long long tokens, int topk, int c, T *out,
                                                                                  long long ldo, int width) {
-    // rows that are not on 16-byte boundaries: four values per thread, `width` apart
-    constexpr int kVec = VEC ? 16 / sizeof(T) : 4;
+    constexpr int kEach = UNIT / sizeof(T), kUnits = UNIT == 16 ? 1 : 4, kVec = kUnits * kEach;
+    using U = typename std::conditional<UNIT == 16, uint4, typename std::conditional<UNIT == 4, uint32_t, uint16_t>::type>::type;
     // width threads (a power of two) for a token, or for a part of its row
     const int per_row = (c + kVec - 1) / kVec, parts = (per_row + width - 1) / width, per_cta = 256 / width;
-    const int slot = threadIdx.x / width, lane = threadIdx.x - slot * width, apart = VEC ? 1 : width;
-    const long long items = (tokens + per_cta - 1) / per_cta * parts;
-    int at_next = 0;
-    long long t_next = 0;
+    const int slot = threadIdx.x / width, lane = threadIdx.x - slot * width, apart = width * kEach;
+    const long long groups = (tokens + per_cta - 1) / per_cta;           // of per_cta tokens; an item is a part of one
+    const int step_part = gridDim.x % parts;
+    const long long step_group = gridDim.x / parts;
+    long long group = blockIdx.x / parts, t_next = 0;
+    int part = blockIdx.x % parts, at_next = 0;
+    const bool quads = topk % 4 == 0 && ((reinterpret_cast<uintptr_t>(index) | reinterpret_cast<uintptr_t>(weights)) & 15) == 0;
     int idx[kAhead];
     float w[kAhead];
-    auto fetch = [&](long long item, int j0) {
-        const int part = (int)(item % parts);
-        t_next = item / parts * per_cta + slot;
-        at_next = VEC ? (part * width + lane) * kVec : part * width * kVec + lane;
-        const bool live = item < items && t_next < tokens && at_next < c;
+    auto fetch = [&](int j0) {
+        t_next = group * per_cta + slot;
+        at_next = part * width * kVec + lane * kEach;
+        const bool live = t_next < tokens && at_next < c;
+        const int32_t *from = index + t_next * topk + j0;
+        const float *by = weights + t_next * topk + j0;
+        if (kAhead % 4 == 0 && quads) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            idx[j] = live && j0 + j < topk ? index[t_next * topk + j0 + j] : -1;
-            w[j] = idx[j] >= 0 ? weights[t_next * topk + j0 + j] : 0.0f;
+            for (int j = 0; j + 3 < kAhead; j += 4) {
+                int4 i4 = make_int4(-1, -1, -1, -1);
+                float4 w4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (live && j0 + j < topk) {
+                    i4 = *reinterpret_cast<const int4 *>(from + j);
+                    w4 = *reinterpret_cast<const float4 *>(by + j);
+                }
+                idx[j] = i4.x, idx[j + 1] = i4.y, idx[j + 2] = i4.z, idx[j + 3] = i4.w;
+                w[j] = w4.x, w[j + 1] = w4.y, w[j + 2] = w4.z, w[j + 3] = w4.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                idx[j] = live && j0 + j < topk ? from[j] : -1;
+                w[j] = live && j0 + j < topk ? by[j] : 0.0f;
+            }
         }
     };
     after_prior_kernels();
-    fetch(blockIdx.x, 0);
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    fetch(0);
+    while (group < groups) {
         const long long t = t_next;
         const int at = at_next;
         float acc[kVec];
 #pragma unroll
         for (int q = 0; q < kVec; ++q) acc[q] = 0.0f;
         for (int j0 = 0; j0 < topk; j0 += kAhead) {
-            uint4 v[kAhead];
+            U v[kAhead][kUnits];
             float p[kAhead];
             bool have[kAhead];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 have[j] = idx[j] >= 0 && idx[j] < rows;
                 p[j] = w[j];
-                if (have[j]) {
-                    const T *from = y + (long long)idx[j] * ldy + at;
-                    if (VEC) {
-                        v[j] = *reinterpret_cast<const uint4 *>(from);
-                    } else {
-                        T *e = reinterpret_cast<T *>(&v[j]);
+                const T *from = y + (long long)idx[j] * ldy + at;
 #pragma unroll
-                        for (int q = 0; q < kVec; ++q) e[q] = at + q * apart < c ? from[q * apart] : from_f32<T>(0.0f);
-                    }
-                }
+                for (int u = 0; u < kUnits; ++u)
+                    if (have[j] && (kUnits == 1 || at + u * apart < c)) v[j][u] = *reinterpret_cast<const U *>(from + u * apart);
             }
-            if (j0 + kAhead < topk) fetch(item, j0 + kAhead);
-            else fetch(item + gridDim.x, 0);
+            if (j0 + kAhead < topk) {
+                fetch(j0 + kAhead);
+            } else {
+                group += step_group;
+                part += step_part;
+                if (part >= parts) {
+                    part -= parts;
+                    ++group;
+                }
+                fetch(0);
+            }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 if (have[j]) {
-                    const T *e = reinterpret_cast<const T *>(&v[j]);
 #pragma unroll
-                    for (int q = 0; q < kVec; ++q) acc[q] += p[j] * to_f32(e[q]);
+                    for (int u = 0; u < kUnits; ++u) {
+                        const T *e = reinterpret_cast<const T *>(&v[j][u]);
+#pragma unroll
+                        for (int q = 0; q < kEach; ++q) acc[u * kEach + q] += p[j] * to_f32(e[q]);
+                    }
                 }
             }
         }
-        if (t < tokens && at < c) {
-            T *to = out + t * ldo + at;
-            if (VEC) {
-                uint4 v;
+        if (t < tokens) {
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                U v;
                 T *e = reinterpret_cast<T *>(&v);
 #pragma unroll
-                for (int q = 0; q < kVec; ++q) e[q] = from_f32<T>(acc[q]);
-                *reinterpret_cast<uint4 *>(to) = v;
-            } else {
-#pragma unroll
-                for (int q = 0; q < kVec; ++q)
-                    if (at + q * apart < c) to[q * apart] = from_f32<T>(acc[q]);
+                for (int q = 0; q < kEach; ++q) e[q] = from_f32<T>(acc[u * kEach + q]);
+                if (at + u * apart < c) *reinterpret_cast<U *>(out + t * ldo + at + u * apart) = v;
             }
         }
     }
 }
 
 template <typename T>
+auto combine_kernel(int unit, int ahead) {
+    constexpr int kSmall = sizeof(T) == 2 ? 2 : 4;
+    if (unit == 16)
+        return ahead == 2   ? combine_rows_kernel<T, 16, 2>
+               : ahead == 4 ? combine_rows_kernel<T, 16, 4>
+                            : combine_rows_kernel<T, 16, 8>;
+    if (unit == 4)
+        return ahead == 2   ? combine_rows_kernel<T, 4, 2>
+               : ahead == 4 ? combine_rows_kernel<T, 4, 4>
+                            : combine_rows_kernel<T, 4, 8>;
+    return ahead == 2   ? combine_rows_kernel<T, kSmall, 2>
+           : ahead == 4 ? combine_rows_kernel<T, kSmall, 4>
+                        : combine_rows_kernel<T, kSmall, 8>;
+}
+
+template <typename T>
 cudaError_t combine_launch(const void *y, long long ldy, long long rows, const int32_t *index, const float *weights,
-                           long long tokens, int topk, int c, void *out, long long ldo, bool vec, int sms, cudaStream_t s) {
-    const int per_row = vec ? (c * (int)sizeof(T) + 15) / 16 : (c + 3) / 4, ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
+                           long long tokens, int topk, int c, void *out, long long ldo, int unit, int sms, cudaStream_t s) {
+    const int per_thread = unit == 16 ? 16 : 4 * unit, per_row = (c * (int)sizeof(T) + per_thread - 1) / per_thread;
+    const int ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
     int width = 4;
     while (width < per_row && width < 256) width *= 2;
     const long long items = (tokens + 256 / width - 1) / (256 / width) * ((per_row + width - 1) / width);
     const long long room = (long long)combine_ctas(ahead) * sms;
-    auto k = ahead == 2   ? (vec ? combine_rows_kernel<T, true, 2> : combine_rows_kernel<T, false, 2>)
-             : ahead == 4 ? (vec ? combine_rows_kernel<T, true, 4> : combine_rows_kernel<T, false, 4>)
-                          : (vec ? combine_rows_kernel<T, true, 8> : combine_rows_kernel<T, false, 8>);
+    auto k = combine_kernel<T>(unit, ahead);
     return launch_early(k, dim3((unsigned)(items < room ? items : room)), 256, 0, s, (const T *)y, ldy, rows, index, weights,
                         tokens, topk, c, (T *)out, ldo, width);
 }
@@ -1095,11 +1132,11 @@ cudaError_t launch_linear_few(const LinearArgs &a, int tokens, cudaStream_t s) {
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
-                                bool vec, int sms, cudaStream_t s) {
+                                int unit, int sms, cudaStream_t s) {
     switch (type) {
-        case HATQ_F32: return combine_launch<float>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
-        case HATQ_F16: return combine_launch<__half>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
-        default: return combine_launch<__nv_bfloat16>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms, s);
+        case HATQ_F32: return combine_launch<float>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, unit, sms, s);
+        case HATQ_F16: return combine_launch<__half>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, unit, sms, s);
+        default: return combine_launch<__nv_bfloat16>(y, ldy, rows, index, weights, tokens, topk, c, out, ldo, unit, sms, s);
     }
 }
 

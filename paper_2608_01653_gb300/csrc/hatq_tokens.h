@@ -68,7 +68,7 @@ cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int til
 
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
-                                bool vec, int sms, cudaStream_t s);
+                                int unit, int sms, cudaStream_t s);   // unit: bytes that all rows are aligned to, 16, 4 or 2
 
 // A kernel of this file's operators may be started while the one before it in
 // the stream is ending: it sets itself up and then waits here, before its first

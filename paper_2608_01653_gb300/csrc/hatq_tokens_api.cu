@@ -336,10 +336,13 @@ hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long 
     if (!aligned(y, ts) || !aligned(out, ts) || !aligned(index, 4) || !aligned(weights, 4))
         return fail(HATQ_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
     if (overlap(y, rows, ldy, c, ts, out, tokens, ldo, c, ts)) return fail(HATQ_ERR_INVALID_ARG, "y and out overlap");
-    const bool vec = aligned(y, 16) && aligned(out, 16) && ldy * ts % 16 == 0 && ldo * ts % 16 == 0 && c * ts % 16 == 0;
+    auto all = [&](size_t u) {
+        return aligned(y, u) && aligned(out, u) && ldy * ts % u == 0 && ldo * ts % u == 0 && c * ts % u == 0;
+    };
+    const int unit = all(16) ? 16 : all(4) ? 4 : 2;
     const int sms = sm_count();
     if (!sms) return fail(HATQ_ERR_CUDA, "no CUDA device");
-    const cudaError_t e = hatq::launch_combine_rows(y, type, ldy, rows, index, weights, tokens, topk, c, out, ldo, vec, sms,
+    const cudaError_t e = hatq::launch_combine_rows(y, type, ldy, rows, index, weights, tokens, topk, c, out, ldo, unit, sms,
                                                     reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "combine launch");
 }

@@ -516,6 +516,25 @@ def test_combine(tokens, topk, c, dtype):
         assert bool((out[1] == 0).all())
 
 
+@pytest.mark.parametrize("topk", [2, 4, 8, 12])
+@pytest.mark.parametrize("c", [6, 34, 256, 1030])
+def test_combine_off_the_usual_boundaries(topk, c):
+    """Rows on 4-byte boundaries, and indices and weights that begin off 16-byte ones."""
+    tokens = 50
+    index = torch.randint(-1, 90, (tokens * topk + 1,), generator=gen(77), device="cuda").to(torch.int32)[1:].view(tokens, topk)
+    weights = torch.rand(tokens * topk + 1, generator=gen(78), device="cuda")[1:].view(tokens, topk)
+    for dtype in TYPES.values():
+        y = torch.randn(88, c, generator=gen(79), device="cuda").to(dtype)
+        out = H.combine_rows(y, index, weights)
+        finish()
+        i = index.long()
+        valid = (i >= 0) & (i < 88)
+        z = torch.where(valid[:, :, None], y.double()[i.clamp(0, 87)] * weights.double()[:, :, None], 0.0)
+        ref = z.sum(1)
+        tol = (topk + 1) * 1.01 * U * z.abs().sum(1) + HALF_ULP[dtype] * 1.01 * ref.abs() + 2.0 ** -25
+        assert bool(((out.double() - ref).abs() <= tol).all())
+
+
 def test_combine_strides():
     wide = torch.randn(60, 211, generator=gen(73), device="cuda").half()
     index = torch.randint(0, 30, (20, 2), generator=gen(74), device="cuda").to(torch.int32)
