@@ -334,7 +334,7 @@ __device__ __forceinline__ void copy_async(uint4 *dst, const void *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src)
                  : "memory");
 }
-// the first `bytes` of the 16, zeros behind them
+// the first `bytes` (at least one) of the 16, zeros behind them; the source is aligned to 16 all the same
 __device__ __forceinline__ void copy_async_part(uint4 *dst, const void *src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
                  "r"(bytes)
@@ -389,8 +389,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
                     const int end = src >= 0 ? a.c : 0;
 #pragma unroll
                     for (int i = 0; i < kPieces; ++i) {
-                        const int at = first + i * 32 * kIn, have = min(max(end - at, 0), kIn);
-                        copy_async_part(buffer + piece_at<kPieces>(in_at, i), p + min(at, a.c - 1), have * (int)sizeof(T));
+                        const int at = first + i * 32 * kIn, have = min(end - at, kIn);
+                        uint4 *dst = buffer + piece_at<kPieces>(in_at, i);
+                        if (have > 0) copy_async_part(dst, p + at, have * (int)sizeof(T));
+                        else *dst = make_uint4(0, 0, 0, 0);              // nothing to copy from, nor an aligned address to name
                     }
                 }
                 buffer += 32 * kPieces;
@@ -563,7 +565,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_blocks_kerne
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int at = first + i * 32 * kIn;
-                copy_async_part(buffer + spread<16>(i * 32 + lane), p + min(at, a.c - kIn), at < end ? 16 : 0);
+                uint4 *dst = buffer + spread<16>(i * 32 + lane);
+                if (at < end) copy_async(dst, p + at);
+                else *dst = make_uint4(0, 0, 0, 0);                      // nothing to copy from
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
