@@ -27,7 +27,8 @@
 //
 // PAIR: two CTAs (one cluster) compute 256 channels x T tokens with
 // cta_group::2; each widens its own 128 channels and holds half of the tokens,
-// which halves the shared-memory traffic per product. split > 1: the CTAs of a
+// which halves the shared-memory traffic per product. The peer's token copies
+// complete on the leader's barriers, whose MMAs read them. split > 1: the CTAs of a
 // cluster share one tile's reduction and add their int32 sums through
 // distributed shared memory (integers: the order does not matter). LOOSE: token
 // codes of any format, pitch and alignment, brought in and widened by the
@@ -79,20 +80,49 @@ __device__ __forceinline__ uint32_t map_shared(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// Arrival at the pair leader's barrier. What it announces is tensor memory, ordered by the tcgen05 fences on
-// both sides; a release and an acquire at cluster scope would add memory barriers to every 64-code block.
+// The peer's arrival at the pair leader's barrier. What it announces is tensor memory alone, ordered by the tcgen05
+// fences on both sides. A release at cluster scope here, which would speak for shared memory as well, costs a memory
+// barrier per hand-off: 8192 x 4096 -> 16384 1142 us a call instead of 620.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// whether the phase is over, without a wait
+// arrival at the leader's barrier that announces copies of `bytes` on their way to the peer's shared memory
+__device__ __forceinline__ void mbar_expect_tx_remote(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// a box into this CTA's shared memory whose bytes complete on a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *tm, uint32_t bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+        "[%2];" ::"r"(dst),
+        "l"(tm), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+}
+// Whether the phase is over, without a wait. PAIR: with an acquire of what the other CTA of the pair (or its copies)
+// announced.
+template <bool PAIR>
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
     return ok != 0;
+}
+// mbar_wait; PAIR: with that acquire, made when the phase is known to be over
+template <bool PAIR>
+__device__ __forceinline__ bool wait_acquire(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    if (!mbar_wait(bar, parity, abort_flag, err)) return false;
+    return !PAIR || mbar_test<PAIR>(bar, parity);
 }
 // without regard to the abort flag: before the CTA leaves, what it has in flight has to land
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
@@ -232,7 +262,7 @@ struct Config {
     static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024 + kTables + 8 * (T / 2) * 4;
     static_assert(T % 32 == 0 && T / kCtas % 8 == 0, "token tile");
     static_assert(kSlots >= 2 && (kGroup > 1 || kSlots % 2 == 0), "slots of a hand-off");
-    static_assert(8 * (kStages * (2 + kHands) + kSlots + 5) + 8 <= 1024, "barriers");
+    static_assert(8 * (kStages * (3 + kHands) + kSlots + 5) + 12 <= 1024, "barriers");
     static_assert(kStages * kStageBytes >= T * 512, "the int32 sums of a split tile reuse the stages");
 };
 
@@ -257,8 +287,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto dfull = [&](int d) { return bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + d); };
     auto dempty = [&](int d) { return bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + 2 + d); };
     const uint32_t tail = bar0 + 8u * (C::kStages * (2 + C::kHands) + C::kSlots + 4);
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (C::kStages * (2 + C::kHands) + C::kSlots + 5));
+    auto peer_full = [&](int s) { return tail + 8u * (1 + s); };        // in a pair's leader: the peer's token codes
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bar_area + 8 * (C::kStages * (3 + C::kHands) + C::kSlots + 5));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    uint32_t *peer_issued = tmem_holder + 2;                            // in a pair's leader: stages that the peer asked for
     // per expert: token tiles before it, its rows, its exact window
     int *tile_start = reinterpret_cast<int *>(bar_area + 1024), *first_row = tile_start + kMaxExperts + 1,
         *end_row = first_row + kMaxExperts, *window_of = end_row + kMaxExperts;
@@ -277,7 +309,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            for (int h = 0; h < C::kHands; ++h) mbar_init(wide(s, h), C::kWideWarps);
+            for (int h = 0; h < C::kHands; ++h) mbar_init(wide(s, h), C::kWideWarps + (PAIR && h == 0 ? 1 : 0));
+            if (PAIR) mbar_init(peer_full(s), 1);
         }
         for (int q = 0; q < C::kSlots; ++q) mbar_init(slot_free(q), 1);
         mbar_init(tail, 1);
@@ -300,6 +333,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
+    // a pair's barriers and tensor memory are there once every thread of both CTAs has come by
+    if (PAIR) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     const int pairs_n = (a.n_tiles + C::kCtas - 1) / C::kCtas;          // channel tiles of a cluster
     const int per = PAIR ? 2 : a.split;
     const int first = (int)blockIdx.x / per, step = (int)gridDim.x / per;
@@ -335,11 +370,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (elect_one()) {
             const uint32_t st = stage0 + (uint32_t)(s * C::kStageBytes);
             const int blocks = min(C::kSub, kb1 - b);
-            mbar_expect_tx(full(s), (uint32_t)(blocks * (LOOSE ? kBlockBytes : C::kXBytes + kBlockBytes)));
+            // The leader's MMAs read the peer's token codes, so those complete on the leader's barrier.
+            const bool here = !LOOSE && in_pair == 0;
+            mbar_expect_tx(full(s), (uint32_t)(blocks * (here ? C::kXBytes + kBlockBytes : kBlockBytes)));
             bulk_load(st + C::kWOffset, w, (uint32_t)(blocks * kBlockBytes), full(s));
+            if (here) {
 #pragma unroll
-            for (int q = 0; q < C::kSub; ++q)
-                if (!LOOSE && q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
+                for (int q = 0; q < C::kSub; ++q)
+                    if (q < blocks) tma_load_2d(st + q * C::kXBytes, &tmX, full(s), (b + q) * 64, row);
+            } else if (PAIR) {
+                const uint32_t bar = map_shared(peer_full(s), 0);
+                mbar_expect_tx_remote(bar, (uint32_t)(blocks * C::kXBytes));
+#pragma unroll
+                for (int q = 0; q < C::kSub; ++q)
+                    if (q < blocks) tma_load_2d_pair(st + q * C::kXBytes, &tmX, bar, (b + q) * 64, row);
+            }
         }
         __syncwarp();
     };
@@ -354,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             end_row[0] = a.rows;
         }
         __syncwarp();
+        if (PAIR) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (first < tile_start[1] * pairs_n) {
             const Tile tile = decode(first);
             for (int b = kb0; b < kb1 && issued < C::kStages; b += C::kSub) copy_stage(tile, b, issued++);
@@ -417,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync();
+    if (PAIR && (a.offsets || warp != 0)) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     tc_fence_after();
     const uint32_t tmem = *tmem_holder;
     const bool skip = s_skip != 0;
@@ -461,11 +507,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int b = kb0; b < kb1 && ok;) {
                     const int end = min(kb1, (b / win + 1) * win);      // one exact window, one accumulator
                     const int d = cc & 1;
-                    ok = mbar_wait(dempty(d), (uint32_t)((cc >> 1) & 1) ^ 1u, abort_flag, a.err);
+                    ok = wait_acquire<PAIR>(dempty(d), (uint32_t)((cc >> 1) & 1) ^ 1u, abort_flag, a.err);
                     ok = __all_sync(0xffffffffu, ok);
                     uint32_t acc = 0;
                     for (; b < end && ok; b += C::kSub) {
-                        // The widening warps waited for the stage's copies, so their arrival speaks for both operands.
+                        // The widening warps waited for this CTA's copies, and warp 2 for the peer's, so their arrival
+                        // speaks for both operands.
                         const int now = s;
                         const uint32_t now_ph = ph;
                         if (++s == C::kStages) {
@@ -476,12 +523,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int h = 0; h < C::kHands; ++h) {
                             if (!ready) {
-                                ok = mbar_wait(wide(now, h), now_ph, abort_flag, a.err);
+                                ok = wait_acquire<PAIR>(wide(now, h), now_ph, abort_flag, a.err);
                                 ok = __all_sync(0xffffffffu, ok);
                                 if (!ok) break;
                             }
                             // the next hand-off is looked at early: the answer takes a while
-                            const bool next = h + 1 < C::kHands ? mbar_test(wide(now, h + 1), now_ph) : mbar_test(wide(s, 0), ph);
+                            const bool next = h + 1 < C::kHands ? mbar_test<PAIR>(wide(now, h + 1), now_ph)
+                                                                : mbar_test<PAIR>(wide(s, 0), ph);
                             tc_fence_after();
                             if (elect_one()) {
                                 const uint32_t at = tmem + (uint32_t)(2 * T + slot * C::kSlotCols);
@@ -514,6 +562,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (elect_one()) commit<PAIR>(tail);                    // after all MMAs that are on their way
                 __syncwarp();
                 mbar_drain(tail, 0);
+            }
+        } else if (PAIR && warp == 2 && in_pair == 0) {
+            // The peer's token codes of each stage: this idle warp waits for them and joins the arrivals of the stage's
+            // first hand-off, so that the MMA warp has no second barrier to wait for.
+            const int tiles = total > first ? (total - first + step - 1) / step : 0;
+            const long long stages = (long long)tiles * ((kb1 - kb0 + C::kSub - 1) / C::kSub);
+            int s = 0;
+            uint32_t ph = 0;
+            for (long long it = 0; it < stages; ++it) {
+                ok = wait_acquire<PAIR>(peer_full(s), ph, abort_flag, a.err);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) mbar_arrive(wide(s, 0));
+                if (++s == C::kStages) {
+                    s = 0;
+                    ph ^= 1u;
+                }
             }
         }
         __syncwarp();
@@ -609,8 +674,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (lane == 0) {
                 const uint32_t bar = wide(s, C::kGroup == 1 ? set : 0);
-                if (PAIR) mbar_arrive_remote(map_shared(bar, 0));
-                else mbar_arrive(bar);
+                if (PAIR && in_pair != 0) mbar_arrive_remote(map_shared(bar, 0));
+                else mbar_arrive(bar);                                  // a release: speaks for the token codes, too
             }
             slot += C::kGroup == 1 ? 2 : 1;
             if (slot >= C::kSlots) {
@@ -831,9 +896,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         }
     }
+    if (PAIR && in_pair != 0 && threadIdx.x == 0)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_shared(smem_addr(peer_issued), 0)), "r"(issued) : "memory");
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync();
+    if (PAIR) {
+        cluster_sync();
+        // The peer stays until its token copies, which only the leader's barriers know of, have landed. (Waited for
+        // already unless a wait expired.)
+        if (in_pair == 0 && warp == 0) {
+            const int asked = (int)*reinterpret_cast<volatile uint32_t *>(peer_issued);
+            for (int i = max(0, asked - C::kStages); i < asked; ++i)
+                mbar_drain(peer_full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
+        }
+        cluster_sync();
+    }
     tc_fence_after();
     if (warp == 1) {
         if (PAIR)
