@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <thread>
 
 #include "hatq.h"
 
@@ -106,16 +107,23 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, int 
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
-// Lets `kernel` have `bytes` of dynamic shared memory: asked of CUDA once per device and size, not per launch.
-// `allowed` is the caller's static array; host threads that race ask twice.
+// Lets `kernel` have `bytes` of dynamic shared memory: asked of CUDA where no call on this device has had as many, not
+// per launch. `allowed` is the caller's static array. A call sets the limit, to less than it was if so asked, so host
+// threads ask one at a time and look again when it is their turn. (A flag, held for one driver call: a mutex may throw.)
 inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<int> (&allowed)[64]) {
     if (bytes <= 40 * 1024) return cudaSuccess;                          // what every launch may have (48 KB), less static arrays
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64 && allowed[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(bytes, std::memory_order_relaxed);
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (allowed[dev].load(std::memory_order_acquire) >= bytes) return cudaSuccess;
+    static std::atomic_flag busy = ATOMIC_FLAG_INIT;
+    while (busy.test_and_set(std::memory_order_acquire)) std::this_thread::yield();
+    if (allowed[dev].load(std::memory_order_relaxed) < bytes) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) allowed[dev].store(bytes, std::memory_order_release);
+    }
+    busy.clear(std::memory_order_release);
     return e;
 }
 
