@@ -557,7 +557,7 @@ hatq_status hatq_quantize_tokens(const void *x, int x_type, long long ldx, long 
 /* The weights of a token layer, laid out for hatq_linear / hatq_grouped_linear. */
 typedef struct {
     int experts;          /* 1 .. 1024; 1 for a dense layer */
-    int n, k;             /* output channels, reduction length (k <= 65536) */
+    int n, k;             /* output channels (n <= 2^31 - 1024), reduction length (k <= 65536) */
     int reserved;
     uint8_t *codes;       /* device, hatq_linear_sizes bytes, 16-byte aligned; written by hatq_linear_layout */
     int32_t *windows;     /* device [experts]; written by hatq_linear_layout */
@@ -609,7 +609,7 @@ hatq_status hatq_grouped_linear(const void *x, int format, long long ldx, const 
  * indices all do gets zeros).
  *   y, out   device, hatq_type type, rows of c values at pitches ldy, ldo >= c
  *   index    device int32 [tokens][topk], weights device float [tokens][topk]
- *   topk     1 .. 64 */
+ *   topk     1 .. 64; c at most 2^31 - 4096 */
 hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                               const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
                               hatq_stream stream);

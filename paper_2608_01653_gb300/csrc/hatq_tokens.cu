@@ -1073,7 +1073,7 @@ auto combine_kernel(int unit, int ahead) {
 template <typename T>
 cudaError_t combine_launch(const void *y, long long ldy, long long rows, const int32_t *index, const float *weights,
                            long long tokens, int topk, int c, void *out, long long ldo, int unit, int sms, cudaStream_t s) {
-    const int per_thread = unit == 16 ? 16 : 4 * unit, per_row = (c * (int)sizeof(T) + per_thread - 1) / per_thread;
+    const int per_thread = (unit == 16 ? 16 : 4 * unit) / (int)sizeof(T), per_row = (c + per_thread - 1) / per_thread;
     const int ahead = topk <= 2 ? 2 : topk <= 4 ? 4 : 8;
     int width = 4;
     while (width < per_row && width < 256) width *= 2;

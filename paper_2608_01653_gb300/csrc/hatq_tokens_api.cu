@@ -42,6 +42,8 @@ bool overlap(const void *p, long long p_rows, long long p_pitch, long long p_wid
 
 constexpr long long kMaxRows = (1LL << 31) - 1024;
 constexpr long long kMaxPitch = 1LL << 32;
+constexpr int kMaxChannels = INT_MAX - 1023;    // the last tiles of 128 (of 256 on a pair) still count in int
+constexpr int kMaxCombined = INT_MAX - 4095;    // and so does a row's end in whole steps of a CTA
 
 struct Plan {
     bool few;        // the dot-product kernel
@@ -126,7 +128,7 @@ hatq_status check_weights(const hatq_linear_weights *L) {
         return fail(HATQ_ERR_INVALID_ARG, "experts must be in 1..%d", hatq::kMaxExperts);
     if (L->n < 1 || L->k < 1) return fail(HATQ_ERR_INVALID_ARG, "n and k must be positive");
     if (L->k > hatq::kMaxDepth) return fail(HATQ_ERR_UNSUPPORTED, "k must be at most %d", hatq::kMaxDepth);
-    if ((long long)L->experts * ((L->n + 127LL) / 128) > (1LL << 30))
+    if (L->n > kMaxChannels || (long long)L->experts * ((L->n + 127LL) / 128) > (1LL << 30))
         return fail(HATQ_ERR_UNSUPPORTED, "too many output channels");
     return HATQ_OK;
 }
@@ -328,6 +330,7 @@ hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long 
     if (rows < 0 || tokens < 0 || c < 1) return fail(HATQ_ERR_INVALID_ARG, "negative or empty shape");
     if (topk < 1 || topk > 64) return fail(HATQ_ERR_INVALID_ARG, "topk must be in 1..64");
     if (rows > kMaxRows || tokens > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows per call");
+    if (c > kMaxCombined) return fail(HATQ_ERR_UNSUPPORTED, "at most %d values per row", kMaxCombined);
     if (ldy < c || ldo < c) return fail(HATQ_ERR_INVALID_ARG, "a pitch is smaller than its row");
     if (ldy > kMaxPitch || ldo > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
     if (tokens == 0) return HATQ_OK;

@@ -93,3 +93,17 @@ def test_grouped_products_on_pairs_behind_an_expired_wait():
     H.grouped_linear(x, one, off, L, out=out)
     finish()
     assert torch.equal(out, grouped_reference(x, w, off))
+
+
+# ------------------------------------------------------------------ combine_rows
+
+@pytest.mark.parametrize("dtype,c", [("f32", (1 << 29) + 1), ("f16", (1 << 30) + 8), ("bf16", (1 << 30) + 3)])
+def test_combine_rows_of_more_than_2_gb(dtype, c):
+    """A row whose bytes do not count in 32 bits; one row with weight 1 is the row itself."""
+    y = torch.empty(1, c, dtype=TYPES[dtype], device="cuda")
+    step = 1 << 27
+    for at in range(0, c, step):
+        y[0, at:at + step].normal_(generator=gen(at // step))
+    out = H.combine_rows(y, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, 1, device="cuda"))
+    finish()
+    assert torch.equal(out, y)
