@@ -153,13 +153,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
     else
         umma_f16_ts(d, a, b, idesc, acc);
 }
-// arrives at the barrier of this CTA (of both CTAs of a pair) when the MMAs issued so far are done
+// arrives at the barrier of this CTA (of a pair's CTAs in `ctas`) when the MMAs issued so far are done
 template <bool PAIR>
-__device__ __forceinline__ void commit(uint32_t bar) {
+__device__ __forceinline__ void commit(uint32_t bar, uint16_t ctas = 3) {
     if (PAIR)
         asm volatile(
             "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-            "h"((uint16_t)3)
+            "h"(ctas)
             : "memory");
     else
         umma_commit(bar);
@@ -491,6 +491,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 done = 0;
             }
+            // The last MMAs' arrivals come to this CTA's shared memory, from a pair's leader too: it does not leave before.
+            if (ok && !skip) {
+                const int hands = issued * C::kHands;
+                for (int i = max(0, issued - C::kStages); i < issued && ok; ++i)
+                    ok = mbar_wait(empty(i % C::kStages), (uint32_t)((i / C::kStages) & 1), abort_flag, a.err);
+                for (int i = max(0, hands - C::kSlots); i < hands && ok; ++i)
+                    ok = mbar_wait(slot_free(i % C::kSlots), (uint32_t)((i / C::kSlots) & 1), abort_flag, a.err);
+                ok = __all_sync(0xffffffffu, ok);
+            }
+            // nor before its copies have landed: those that no one waited for, where a wait expired
             if (!ok || skip)
                 for (int i = max(0, issued - C::kStages); i < issued; ++i)
                     mbar_drain(full(i % C::kStages), (uint32_t)((i / C::kStages) & 1));
@@ -558,11 +568,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ++cc;
                 }
             }
-            if (!ok) {
-                if (elect_one()) commit<PAIR>(tail);                    // after all MMAs that are on their way
-                __syncwarp();
-                mbar_drain(tail, 0);
-            }
+            // all MMAs that are on their way, whether or not another role gave up, before tensor memory is handed back
+            if (elect_one()) commit<PAIR>(tail, 1);
+            __syncwarp();
+            mbar_drain(tail, 0);
         } else if (PAIR && warp == 2 && in_pair == 0) {
             // The peer's token codes of each stage: this idle warp waits for them and joins the arrivals of the stage's
             // first hand-off, so that the MMA warp has no second barrier to wait for.

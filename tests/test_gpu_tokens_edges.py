@@ -95,6 +95,21 @@ def test_grouped_products_on_pairs_behind_an_expired_wait():
     assert torch.equal(out, grouped_reference(x, w, off))
 
 
+def test_products_of_every_kind_follow_one_another():
+    """Kernels with other tiles and barriers start on the same SMs at once: nothing of the one before may still arrive."""
+    calls = []
+    for i, (rows, k, n, kind) in enumerate([(2500, 64, 4096, "f16"), (40, 4096, 300, "f16"), (60, 700, 300, "i8"),
+                                            (1300, 1024, 4224, "f16"), (2, 512, 100, "i8"), (300, 256, 2100, "f16")]):
+        x, w, one = codes(rows, k, 20 + i, kind), codes(n, k, 30 + i), torch.ones(max(rows, n), device="cuda")
+        calls.append((x, one[:rows].contiguous(), H.prepare_linear(w, scales=one[:n]), integer_sums(x, w).float()))
+    ys = []
+    for turn in range(12):
+        order = calls[turn % 6:] + calls[:turn % 6]
+        ys += [(H.linear(x, s, L, dtype=torch.float32), ref) for x, s, L, ref in (order if turn % 2 else order[::-1])]
+    finish()
+    assert all(torch.equal(y, ref) for y, ref in ys)
+
+
 # ------------------------------------------------------------------ combine_rows
 
 @pytest.mark.parametrize("dtype,c", [("f32", (1 << 29) + 1), ("f16", (1 << 30) + 8), ("bf16", (1 << 30) + 3)])
