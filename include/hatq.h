@@ -289,8 +289,10 @@ const char *hatq_last_error(void);
 /* Synchronizes `stream`, then reads and clears the device error word of the
  * current device: HATQ_ERR_TIMEOUT if a bounded wait expired, HATQ_ERR_CUDA
  * on an asynchronous CUDA error, HATQ_OK otherwise. The error word is sticky:
- * while it is set, convolution blocks that have not started return at once,
- * so work enqueued after a failure produces no output until it is read. */
+ * while it is set, the blocks of convolutions, GDN transitions and products
+ * (hatq_linear, hatq_grouped_linear) that have not started write nothing until
+ * it is read. Quantizers and hatq_combine_rows, which wait for nothing, run on
+ * whatever their inputs then hold. */
 hatq_status hatq_sync_status(hatq_stream stream);
 
 /* Range-expansion profiling for the layer-wise DH/WH selection

@@ -110,6 +110,30 @@ def test_products_of_every_kind_follow_one_another():
     assert all(torch.equal(y, ref) for y, ref in ys)
 
 
+# ------------------------------------------------------------------ products of a few rows
+
+@pytest.mark.parametrize("rows,k,n,kind", [(1, 4096, 4096, "i8"), (2, 300, 77, "f16"), (8, 512, 256, "i8")])
+def test_a_few_rows_behind_an_expired_wait(rows, k, n, kind):
+    """As with many rows: the output is left alone until the status was read."""
+    x, w, one = codes(rows, k, 40, kind), codes(n, k, 41), torch.ones(n, device="cuda")
+    L, G, off = H.prepare_linear(w, scales=one), H.prepare_linear(w[None], scales=one[None]), offsets_of([rows])
+    s = one[:rows].contiguous()
+    finish()
+    a, b = torch.full((rows, n), 3.0, device="cuda"), torch.full((rows, n), 3.0, device="cuda")
+    H.selftest_wait(1000)
+    H.linear(x, s, L, out=a)
+    H.grouped_linear(x, s, off, G, out=b)
+    torch.cuda.synchronize()
+    with pytest.raises(H.HatqError) as error:
+        H.sync_status()
+    assert error.value.status == H.ERR_TIMEOUT and bool((a == 3).all()) and bool((b == 3).all())
+    H.linear(x, s, L, out=a)
+    H.grouped_linear(x, s, off, G, out=b)
+    finish()
+    ref = integer_sums(x, w).float()
+    assert torch.equal(a, ref) and torch.equal(b, ref)
+
+
 # ------------------------------------------------------------------ combine_rows
 
 @pytest.mark.parametrize("dtype,c", [("f32", (1 << 29) + 1), ("f16", (1 << 30) + 8), ("bf16", (1 << 30) + 3)])
