@@ -551,7 +551,8 @@ typedef enum { HATQ_CODES_I8 = 0, HATQ_CODES_F16 = 1 } hatq_codes;
  *   codes    device, hatq_codes format, pitch ldc >= c; behind c nothing is written
  *   scales   device float [rows]
  * Any element alignment works; 16-byte aligned rows are read and written in
- * 16-byte pieces. x and codes must not overlap. */
+ * 16-byte pieces. x and codes must not share an element; they may be columns of
+ * one buffer, with the same pitch in bytes. */
 hatq_status hatq_quantize_tokens(const void *x, int x_type, long long ldx, long long src_rows, const int32_t *index,
                                  long long rows, int c, int hb, int act, int gated, int format, void *codes,
                                  long long ldc, float *scales, hatq_stream stream);
@@ -580,7 +581,8 @@ hatq_status hatq_linear_layout(const int8_t *w, long long ldw, const hatq_linear
  * exact integer sum (int32), converted to fp32, scaled, rounded once to y_type.
  *   x          device codes in hatq_codes format, rows at a pitch of ldx >= k
  *   s_x        device float [rows]
- *   y          device, hatq_type y_type, pitch ldy >= n; must not overlap x
+ *   y          device, hatq_type y_type, pitch ldy >= n; shares no element with x
+ *              (columns of one buffer, with the same pitch in bytes, do not)
  *   workspace  device scratch, 16-byte aligned, or NULL. Codes that are int8, or
  *              whose rows are off 16-byte boundaries, are taken as they lie by
  *              the tensor-core kernel, or packed first where that pays (many
@@ -609,7 +611,8 @@ hatq_status hatq_grouped_linear(const void *x, int format, long long ldx, const 
 /* out[t] = sum_{j < topk} weights[t][j] y[index[t][j]], j ascending, in fp32,
  * rounded once; an index outside [0, rows) contributes nothing (a token whose
  * indices all do gets zeros).
- *   y, out   device, hatq_type type, rows of c values at pitches ldy, ldo >= c
+ *   y, out   device, hatq_type type, rows of c values at pitches ldy, ldo >= c;
+ *            they share no element (columns of one buffer, at one pitch, do not)
  *   index    device int32 [tokens][topk], weights device float [tokens][topk]
  *   topk     1 .. 64; c at most 2^31 - 4096 */
 hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,

@@ -30,14 +30,20 @@ size_t codes_size(int f) { return f == HATQ_CODES_F16 ? 2 : 1; }
 bool is_codes(int f) { return f == HATQ_CODES_I8 || f == HATQ_CODES_F16; }
 int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
-// bytes of rows x width elements at a pitch, as far as they are touched
+// Whether rows of width elements at a pitch share memory with others. Rows between one another, as the columns of one
+// buffer, do not: where both have the same pitch, their places within it are compared. (A single row has any pitch.)
 bool overlap(const void *p, long long p_rows, long long p_pitch, long long p_width, size_t p_size, const void *q,
              long long q_rows, long long q_pitch, long long q_width, size_t q_size) {
     if (p_rows == 0 || q_rows == 0) return false;
     const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), q0 = reinterpret_cast<uintptr_t>(q);
-    const uintptr_t p1 = p0 + (uintptr_t)((p_rows - 1) * p_pitch + p_width) * p_size;
-    const uintptr_t q1 = q0 + (uintptr_t)((q_rows - 1) * q_pitch + q_width) * q_size;
-    return p0 < q1 && q0 < p1;
+    const uintptr_t p_bytes = (uintptr_t)p_width * p_size, q_bytes = (uintptr_t)q_width * q_size;
+    const uintptr_t p_step = (uintptr_t)p_pitch * p_size, q_step = (uintptr_t)q_pitch * q_size;
+    const uintptr_t p1 = p0 + (uintptr_t)(p_rows - 1) * p_step + p_bytes, q1 = q0 + (uintptr_t)(q_rows - 1) * q_step + q_bytes;
+    if (!(p0 < q1 && q0 < p1)) return false;
+    if (p_rows > 1 && q_rows > 1 ? p_step != q_step : p_rows == 1 && q_rows == 1) return true;
+    const uintptr_t step = p_rows > 1 ? p_step : q_step;
+    const uintptr_t at = q0 >= p0 ? (q0 - p0) % step : (step - (p0 - q0) % step) % step;   // q's place, p's is 0
+    return at < p_bytes || at + q_bytes > step;
 }
 
 constexpr long long kMaxRows = (1LL << 31) - 1024;

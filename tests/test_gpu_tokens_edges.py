@@ -146,3 +146,51 @@ def test_combine_rows_of_more_than_2_gb(dtype, c):
     out = H.combine_rows(y, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, 1, device="cuda"))
     finish()
     assert torch.equal(out, y)
+
+
+# ------------------------------------------------------------------ columns of one buffer
+
+@pytest.mark.parametrize("rows", [1, 2, 40, 700])
+@pytest.mark.parametrize("left", [False, True])
+def test_operands_and_results_in_columns_of_one_buffer(rows, left):
+    """Rows that lie between one another share no element: codes beside values, results beside operands."""
+    c, n = 64, 96
+    buffer = torch.zeros(rows, 4 * c + n, dtype=torch.float16, device="cuda")
+    values, result = (buffer[:, c:2 * c], buffer[:, :c]) if left else (buffer[:, :c], buffer[:, c:2 * c])
+    values.normal_(generator=gen(50))
+    x = values.clone()
+    _, s = H.quantize_tokens(values, hb=32, codes="f16", out=result)
+    finish()
+    assert torch.equal(values, x)
+    check_quantized(x, result, s, 32)
+    w, one = codes(n, c, 51), torch.ones(max(n, rows), device="cuda")
+    y = buffer[:, 2 * c:2 * c + n]
+    H.linear(result, one[:rows].contiguous(), H.prepare_linear(w, scales=0.001 * one[:n]), out=y)
+    finish()
+    ref = integer_sums(result, w) * 0.001
+    assert bool(((y.double() - ref).abs() <= (3.01 * 2.0 ** -24 + 1.01 * 2.0 ** -11) * ref.abs() + 2.0 ** -25).all())
+    index = torch.arange(rows, dtype=torch.int32, device="cuda").flip(0)[:, None].contiguous()
+    H.combine_rows(values, index, one[:rows, None].contiguous(), out=result)
+    finish()
+    assert torch.equal(result, x.flip(0))
+    H.combine_rows(values, index[:1].contiguous(), one[:1, None].contiguous(), out=result[rows // 2:rows // 2 + 1])
+    finish()
+    assert torch.equal(result[rows // 2], x[rows - 1])
+
+
+def test_columns_that_share_an_element_are_refused():
+    buffer = torch.zeros(40, 256, dtype=torch.float16, device="cuda")
+    w, one = codes(96, 64, 52), torch.ones(96, device="cuda")
+    L, index = H.prepare_linear(w, scales=one), torch.zeros(40, 1, dtype=torch.int32, device="cuda")
+    s, x = one[:40].contiguous(), buffer[:, 96:160]
+    for call in (lambda: H.quantize_tokens(x, out=buffer[:, 159:223], codes="f16"), lambda: H.quantize_tokens(x, out=buffer[:, 33:97], codes="f16"),
+                 lambda: H.linear(x, s, L, out=buffer[:, 159:255]), lambda: H.linear(x, s, L, out=buffer[:, 1:97]),
+                 lambda: H.combine_rows(x, index, s[:, None].contiguous(), out=buffer[:, 100:164]),
+                 lambda: H.combine_rows(x, index, s[:, None].contiguous(), out=x),
+                 lambda: H.combine_rows(x, index[:1].contiguous(), s[:1, None].contiguous(), out=buffer[3:4, 95:159])):
+        with pytest.raises(H.HatqError):
+            call()
+    # the last row's end reaches into the buffer's next row
+    wrapped = buffer.view(-1)[200:200 + 39 * 256].view(39, 256)[:, :64]
+    with pytest.raises(H.HatqError):
+        H.quantize_tokens(buffer[:39, :64], out=wrapped, codes="f16")
