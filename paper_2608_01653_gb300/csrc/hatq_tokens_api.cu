@@ -64,11 +64,19 @@ struct Plan {
 // (anything else), or that or packed into a workspace first.
 enum Operand { kDirect, kLoose, kEither };
 
-// Which kernel (hatq_tokens.cu, hatq_linear.cu) and which tile. The dot-product kernel has no pipeline to fill, but
-// its instructions are slow and every CTA brings in all rows. Measured, against the tensor-core kernel: 4096 x 4096
-// with 1 / 4 / 8 rows 3.6 / 6.7 / 10.9 us against 8.1 .. 8.9; 4096 x 16384 with 2 / 4 rows 15 / 21 against 18.5;
-// 16384 x 4096 with 1 / 2 rows 14 / 23 against 16.6; experts of 2048 x 1536 with a row each, 8 / 16 / 24 of them,
-// 5.5 / 12 / 15 against 12 / 19 / 19. Of the tensor-core kernel's tiles the one with the least estimated time: waves
+// Rows per pass of the dot-product kernel (hatq_tokens.cu), or 0 for the tensor-core kernel (hatq_linear.cu). The
+// former has no pipeline to fill, but its instructions are slow and every CTA brings in all rows. Measured, against the
+// latter: 4096 x 4096 with 1 / 4 / 8 rows 3.6 / 6.7 / 10.9 us against 8.1 .. 8.9; 4096 x 16384 with 2 / 4 rows 15 / 21
+// against 18.5; 16384 x 4096 with 1 / 2 rows 14 / 23 against 16.6; experts of 2048 x 1536 with a row each, 8 / 16 / 24
+// of them, 5.5 / 12 / 15 against 12 / 19 / 19.
+int few_rows(long long rows, const hatq_linear_weights *L, bool grouped) {
+    const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    const long long weights = (long long)L->n * L->k;
+    const bool take = grouped ? rows <= 24 : rows <= 2 || (rows <= 4 && weights <= 28'000'000) || (rows <= 8 && weights <= 13'000'000);
+    return take && few * round_up(L->k, 64) <= 24 * 1024 ? few : 0;
+}
+
+// Which kernel and which tile. Of the tensor-core kernel's tiles the one with the least estimated time: waves
 // of tiles x blocks of the reduction x time per block, the last measured with every SM at work (a wider tile costs
 // more per block and less per product), and about 0.8 us to join a split reduction. Codes that TMA cannot take are
 // brought in by the widening warps, with single-CTA tiles only (48 rows, 4096 -> 8192: 16.8 us against 11.8; 512 rows,
@@ -76,15 +84,10 @@ enum Operand { kDirect, kLoose, kEither };
 Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms, Operand operand) {
     Plan p{};
     const int k_pad = round_up(L->k, 64), kb = k_pad / 64, n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
-    const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
     p.split = 1;
-    const long long weights = (long long)L->n * L->k;
-    p.few = few * k_pad <= 24 * 1024 &&
-            (grouped ? rows <= 24 : rows <= 2 || (rows <= 4 && weights <= 28'000'000) || (rows <= 8 && weights <= 13'000'000));
-    if (p.few) {
-        p.tokens = few;
-        return p;
-    }
+    p.tokens = few_rows(rows, L, grouped);
+    p.few = p.tokens > 0;
+    if (p.few) return p;
     static const struct { int tokens; bool pair; int ns; } options[] = {
         {32, false, 115}, {64, false, 140}, {128, false, 202}, {128, true, 165}, {192, true, 224}};
     const long long held = rows < L->experts ? rows : L->experts;
@@ -146,7 +149,7 @@ bool direct(const void *x, int format, long long ldx) {
 
 // what packing takes; it is used where it pays
 size_t workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L, bool grouped) {
-    if (rows == 0 || direct(x, format, ldx) || plan_of(rows, L, grouped, 152, kEither).few) return 0;
+    if (rows == 0 || direct(x, format, ldx) || few_rows(rows, L, grouped) > 0) return 0;
     return (size_t)rows * (size_t)round_up(L->k, 64) * 2;
 }
 
