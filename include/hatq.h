@@ -599,6 +599,16 @@ hatq_status hatq_linear(const void *x, int format, long long ldx, const float *s
                         const hatq_linear_weights *L, int y_type, void *y, long long ldy, void *workspace,
                         size_t workspace_bytes, hatq_stream stream);
 
+/* Which kernel hatq_linear (grouped 0) or hatq_grouped_linear (1) takes on the
+ * current device for these arguments, for tests and profiles; rows >= 1:
+ *   plan[0]  1: dot products on the CUDA cores, 0: tensor cores
+ *   plan[1]  rows per pass, or tokens per tile
+ *   plan[2]  CTAs that compute a tile together (256 channels where 2)
+ *   plan[3]  CTAs that share a tile's reduction
+ *   plan[4]  codes taken as they lie (0), widened by the kernel (1), packed first (2) */
+hatq_status hatq_linear_plan(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L,
+                             int grouped, size_t workspace_bytes, int plan[5]);
+
 /* hatq_linear with the weights of the expert that holds the row: expert e holds
  * rows offsets[e] .. offsets[e + 1] - 1 (device int32 [experts + 1], ascending,
  * within [0, rows]; experts may hold no row). Rows that no expert holds are not

@@ -147,6 +147,12 @@ bool direct(const void *x, int format, long long ldx) {
     return format == HATQ_CODES_F16 && ldx % 8 == 0 && aligned(x, 16);
 }
 
+Plan plan_for(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L, bool grouped,
+              size_t workspace_bytes, int sms) {
+    const bool room_to_pack = workspace_bytes >= (size_t)rows * (size_t)round_up(L->k, 64) * 2;
+    return plan_of(rows, L, grouped, sms, direct(x, format, ldx) ? kDirect : room_to_pack ? kEither : kLoose);
+}
+
 // what packing takes; it is used where it pays
 size_t workspace_of(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L, bool grouped) {
     if (rows == 0 || direct(x, format, ldx) || few_rows(rows, L, grouped) > 0) return 0;
@@ -199,10 +205,8 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
     a.y_type = y_type;
     a.y_even = ldy % 2 == 0 && aligned(y, 4);
     a.split = 1;
-    const bool as_it_lies = direct(x, format, ldx);
-    const bool room_to_pack = workspace && workspace_bytes >= (size_t)rows * (size_t)round_up(L->k, 64) * 2;
     if (workspace && !aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-    const Plan p = plan_of(rows, L, grouped, sms, as_it_lies ? kDirect : room_to_pack ? kEither : kLoose);
+    const Plan p = plan_for(x, format, ldx, rows, L, grouped, workspace ? workspace_bytes : 0, sms);
     cudaError_t e;
     if (p.few) {
         if ((e = hatq::launch_linear_few(a, p.tokens, s)) != cudaSuccess) return cuda_fail(e, "product launch");
@@ -215,7 +219,7 @@ hatq_status product(const void *x, int format, long long ldx, const float *s_x, 
         a.ldx = a.kb * 64;
         a.format = HATQ_CODES_F16;
     }
-    const bool loose = !as_it_lies && !p.pack;
+    const bool loose = !direct(x, format, ldx) && !p.pack;
     const int ctas = p.pair ? 2 : 1;
     if (p.tiles > INT_MAX / 16) return fail(HATQ_ERR_UNSUPPORTED, "too many output tiles");
     a.split = p.split;
@@ -317,6 +321,25 @@ hatq_status hatq_linear_workspace(const void *x, int format, long long ldx, long
     // the larger of what the dense and the grouped product want
     const size_t dense = workspace_of(x, format, ldx, rows, L, false), grouped = workspace_of(x, format, ldx, rows, L, true);
     *bytes = dense > grouped ? dense : grouped;
+    return HATQ_OK;
+}
+
+hatq_status hatq_linear_plan(const void *x, int format, long long ldx, long long rows, const hatq_linear_weights *L,
+                             int grouped, size_t workspace_bytes, int plan[5]) {
+    const hatq_status st = check_weights(L);
+    if (st != HATQ_OK) return st;
+    if (!plan) return fail(HATQ_ERR_INVALID_ARG, "null output");
+    if (!is_codes(format)) return fail(HATQ_ERR_INVALID_ARG, "unknown code format %d", format);
+    if (rows < 1) return fail(HATQ_ERR_INVALID_ARG, "no rows");
+    if (rows > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows per call");
+    const int sms = sm_count();
+    if (!sms) return fail(HATQ_ERR_CUDA, "no CUDA device");
+    const Plan p = plan_for(x, format, ldx, rows, L, grouped != 0, workspace_bytes, sms);
+    plan[0] = p.few;
+    plan[1] = p.tokens;
+    plan[2] = p.pair ? 2 : 1;
+    plan[3] = p.split;
+    plan[4] = p.few || direct(x, format, ldx) ? 0 : p.pack ? 2 : 1;
     return HATQ_OK;
 }
 

@@ -136,6 +136,7 @@ def load(build: bool = True) -> ctypes.CDLL:
             "hatq_linear_layout": (_I, [_P, _L, ctypes.POINTER(LinearWeightsStruct), _P]),
             "hatq_linear_workspace": (_I, [_P, _I, _L, _L, ctypes.POINTER(LinearWeightsStruct),
                                            ctypes.POINTER(ctypes.c_size_t)]),
+            "hatq_linear_plan": (_I, [_P, _I, _L, _L, ctypes.POINTER(LinearWeightsStruct), _I, ctypes.c_size_t, _P]),
             "hatq_linear": (_I, [_P, _I, _L, _P, _L, ctypes.POINTER(LinearWeightsStruct), _I, _P, _L, _P,
                                  ctypes.c_size_t, _P]),
             "hatq_grouped_linear": (_I, [_P, _I, _L, _P, _L, _P, ctypes.POINTER(LinearWeightsStruct), _I, _P, _L, _P,

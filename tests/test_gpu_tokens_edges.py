@@ -42,6 +42,19 @@ def test_quantize_rows_that_end_inside_a_warp(dtype, gated, c):
         check_quantized(x, q, s, 1, act, gated, at)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("rows,c,hb", [(400, 9000, 8), (333, 12345, 1), (160, 32768, 256), (2000, 1000, 4), (40_000, 40, 8)])
+def test_quantize_many_rows_with_an_activation(dtype, act, rows, c, hb):
+    """More rows than are at work at a time, on and off 16-byte boundaries, wider and narrower than a warp's values."""
+    x = (4 * torch.randn(rows, c, generator=gen(12), device="cuda")).to(TYPES[dtype])
+    index = torch.randint(-1, rows + 1, (rows,), generator=gen(13), device="cuda").to(torch.int32)
+    for at, kind in ((None, "i8"), (index, "f16")):
+        q, s = H.quantize_tokens(x, hb=hb, act=act, rows=at, codes=kind)
+        finish()
+        check_quantized(x, q, s, hb, act, rows=at)
+
+
 # ------------------------------------------------------------------ products on pairs of CTAs
 
 def padded(rows, k, seed):

@@ -39,3 +39,10 @@ def test_as_many_channels_as_an_index_holds(lib):
 def test_combine_rows_wider_than_an_index(lib, kind, c):
     assert lib.hatq_combine_rows(1 << 40, kind, c, 1, P, 2 * P, 1, 1, c, 1 << 45, c, None) == H.ERR_UNSUPPORTED
     assert H.last_error()
+
+
+def test_linear_plan_refuses(lib):
+    plan, L = (ctypes.c_int * 5)(), weights(64)
+    ask = lambda x=P, fmt=0, rows=4, L=ctypes.byref(L), out=plan: lib.hatq_linear_plan(x, fmt, 64, rows, L, 0, 0, out)
+    assert ask(fmt=2) == ask(rows=0) == ask(rows=-1) == ask(L=None) == ask(out=None) == H.ERR_INVALID_ARG
+    assert ask(rows=1 << 31) == H.ERR_UNSUPPORTED
