@@ -871,6 +871,14 @@ class LinearWeights:
         self.ref = ctypes.byref(self.struct)
 
 
+def _per_channel(t, name, e, n, device):
+    """A float32 copy of one value per output channel: [experts][n] (dense: or [n]), flat, or with a reduced k kept."""
+    shape = tuple(t.shape)
+    if t.numel() != e * n or not (t.dim() <= 1 or shape[:2] == (e, n) or e == 1 and shape[0] == n):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected one value per output channel, {(e, n)}")
+    return t.to(device=device, dtype=_TORCH.float32).reshape(-1).clone()
+
+
 def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeights:
     """The weights of linear (w [n][k]) or grouped_linear (w [experts][n][k]), on the device.
 
@@ -895,14 +903,12 @@ def prepare_linear(w, hb=1, scales=None, bias=None, stream=None) -> LinearWeight
         if w.dtype == torch.int8:
             if scales is None or hb != 1:
                 raise ValueError("int8 weights need their scales, and are not transformed")
-            s_w = scales.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
+            s_w = _per_channel(scales, "scales", e, n, w.device)
         else:
             if scales is not None:
                 raise ValueError("scales belong to int8 weights")
             rows, s_w = quantize_tokens(rows, hb=hb, codes="i8", stream=stream)
-        b = None if bias is None else bias.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
-        if s_w.numel() != e * n or (b is not None and b.numel() != e * n):
-            raise ValueError(f"scales and bias need one value per output channel ({e * n})")
+        b = None if bias is None else _per_channel(bias, "bias", e, n, w.device)
         pitch = rows.stride(0) if e * n > 1 else k
         L = LinearWeights(e, n, k, torch.empty(size.value, dtype=torch.uint8, device=w.device),
                           torch.empty(e, dtype=torch.int32, device=w.device), s_w, b, grouped)

@@ -147,6 +147,28 @@ def test_a_few_rows_behind_an_expired_wait(rows, k, n, kind):
     assert torch.equal(a, ref) and torch.equal(b, ref)
 
 
+# ------------------------------------------------------------------ weights
+
+def test_scales_and_bias_in_another_order_are_refused():
+    """[n][experts] holds as many values as [experts][n], in the wrong order."""
+    w, one = codes(4 * 6, 32, 60).view(4, 6, 32), torch.ones(4, 6, device="cuda")
+    for bad in (one.T, one.T.contiguous(), one.view(2, 12), one.view(3, 8), one[:, None]):
+        with pytest.raises(ValueError):
+            H.prepare_linear(w, scales=bad)
+        with pytest.raises(ValueError):
+            H.prepare_linear(w, scales=one, bias=bad)
+    with pytest.raises(ValueError):
+        H.prepare_linear(w[0], scales=one[0].view(2, 3))
+    x, s, off = codes(9, 32, 61), one.new_ones(9), offsets_of([1, 4, 0, 4])
+    scales = torch.rand(4, 6, generator=gen(62), device="cuda")
+    ys = [H.grouped_linear(x, s, off, H.prepare_linear(w, scales=v), dtype=torch.float32)
+          for v in (scales, scales.view(24), scales[:, :, None], scales.double())]
+    zs = [H.linear(x, s, H.prepare_linear(w[1], scales=v), dtype=torch.float32) for v in (scales[1], scales[1:2], scales[1][:, None])]
+    finish()
+    assert all(torch.equal(y, ys[0]) for y in ys) and all(torch.equal(z, zs[0]) for z in zs)
+    assert torch.equal(zs[0][1:5], ys[0][1:5])
+
+
 # ------------------------------------------------------------------ combine_rows
 
 @pytest.mark.parametrize("dtype,c", [("f32", (1 << 29) + 1), ("f16", (1 << 30) + 8), ("bf16", (1 << 30) + 3)])
