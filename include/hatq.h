@@ -539,7 +539,10 @@ typedef enum { HATQ_CODES_I8 = 0, HATQ_CODES_F16 = 1 } hatq_codes;
  *   t = H~_hb u on consecutive blocks of hb (unnormalized), a = max|t|
  *   codes[r] = clamp(round(t min(127 / a, 2^126)), -127, 127)
  *   scales[r] = max(a / 127, 2^-126) / sqrt(hb)
- * so codes * scale is the operand H~ u / sqrt(hb). A row with a = 0 gets codes 0
+ * so codes * scale is the operand H~ u / sqrt(hb). The sums of t are fp32 in an
+ * order of the kernel's own; many plain 16-bit rows take their 16-value sums from
+ * the tensor cores, whose rounding differs in the last bits, so a value that lies
+ * at the middle of two codes may get either, by type, size and alignment. A row with a = 0 gets codes 0
  * and scale 1; a row with an infinity or a NaN in t gets codes 0 and scale NaN
  * (its outputs are NaN, no other row's). An index outside [0, src_rows) is an
  * empty row: v = 0 without activation, codes 0, scale 1.
@@ -547,7 +550,9 @@ typedef enum { HATQ_CODES_I8 = 0, HATQ_CODES_F16 = 1 } hatq_codes;
  *            a pitch of ldx elements; index device int32 [rows] or NULL (then
  *            src_rows >= rows)
  *   c        1 .. 32768; hb a power of two <= 256 that divides c (1: no transform)
- *   act      hatq_act (SiLU: v / (1 + exp(-v)), GELU: with erf)
+ *   act      hatq_act (SiLU: v / (1 + exp(-v)) with the fast exponential and
+ *            division: off by at most a few fp32 ulp of |v|, 0 for v below
+ *            -87.3; GELU: with erf)
  *   codes    device, hatq_codes format, pitch ldc >= c; behind c nothing is written
  *   scales   device float [rows]
  * Any element alignment works; 16-byte aligned rows are read and written in
@@ -578,7 +583,8 @@ hatq_status hatq_linear_sizes(int experts, int n, int k, size_t *code_bytes);
 hatq_status hatq_linear_layout(const int8_t *w, long long ldw, const hatq_linear_weights *L, hatq_stream stream);
 
 /* y[r][n] = (sum_k x[r][k] w[n][k]) s_w[n] s_x[r] + bias[n] for r < rows: an
- * exact integer sum (int32), converted to fp32, scaled, rounded once to y_type.
+ * exact integer sum (int32), in fp32 from there on (rounded by the conversion, by
+ * each scale and by the bias), then rounded to y_type.
  *   x          device codes in hatq_codes format, rows at a pitch of ldx >= k
  *   s_x        device float [rows]
  *   y          device, hatq_type y_type, pitch ldy >= n; shares no element with x

@@ -35,10 +35,11 @@
 // widening warps (their next stage's pieces on the way while one is worked on)
 // instead of by TMA.
 //
-// Bound by the tensor cores where rows are many (8192 x 4096 -> 16384: 545 us,
-// 2019 TFLOP/s, the tensor pipe 0.91 active), by the weights' bytes where they
-// are few per expert (256 rows, 61 experts of 2048 x 2048: 45 us, 5.7 TB/s), by
-// latency in between (48 rows, 4096 -> 8192: 11.8 us against 5.1 us of bytes).
+// Bound by the tensor cores where rows are many (8192 x 4096 -> 16384: 557 us at
+// 2070 MHz, 600 us once the power cap takes clocks away, the tensor pipe 0.89
+// active), by the weights' bytes where they are few per expert (256 rows, 61
+// experts of 2048 x 2048: 45.5 us, 5.7 TB/s), by latency in between (48 rows,
+// 4096 -> 8192: 11.8 us against 5.1 us of bytes).
 // Every wait is bounded, as in the other tensor-core kernels.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

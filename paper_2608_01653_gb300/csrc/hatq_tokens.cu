@@ -71,9 +71,9 @@ __device__ __forceinline__ pair32 fma2(pair32 a, pair32 b, pair32 c) {
 //    both sides of the exchange free of bank conflicts.
 //  * few rows: a thread owns 8 values, four times the threads per row, one row
 //    per thread: latency counts there.
-// Measured: 8192 x 4096 fp32 in blocks of 128 34 us (5.9 TB/s), 16384 gathered
-// fp32 rows of 2000 25.8 us (instruction issue), 8192 gated rows of 2048 bf16
-// 22 us, one gated row of 8192 3.6 us (latency).
+// Measured: 8192 x 4096 fp32 in blocks of 128 32 us (6.3 TB/s), 16384 gathered
+// fp32 rows of 2000 26.2 us (instruction issue), 8192 gated rows of 2048 bf16
+// 21.4 us, one gated row of 8192 3.7 us (latency).
 
 template <int PIECES>
 __device__ __forceinline__ int swizzle(int owner, int piece) {
@@ -92,7 +92,9 @@ template <> __device__ __forceinline__ pair32 widen2<__half>(uint32_t w) {
 }
 
 __device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }               // keeps a NaN
-// exp(-v) is off by about |v| + 2 ulp and counts with sigma (1 - sigma), so the product stays within a few ulp of |v|
+// The fast exp(-v) is off by about |v| + 2 ulp and counts with sigma (1 - sigma), so the product stays within a few ulp
+// of |v|. Relative to the product itself that is up to |v| ulp in the lower tail, about 1e-5, a thousandth of a code's step
+// at 127. Divisors above 2^126 (v below -87.3) give 0.
 __device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
 __device__ __forceinline__ float gelu(float v) { return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f)); }
 
@@ -510,7 +512,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
 // values 2j, 2j + 1 and 2j + 8, 2j + 9 of blocks 8g .. 8g + 7, i.e. of a whole
 // block of 128, so only blocks of 256 need a lane exchange. With butterflies
 // alone the kernel above is bound by instruction issue: 8192 x 4096 bf16 in
-// blocks of 128 took 30.7 us there and takes 22.6 us (5.9 TB/s) here.
+// blocks of 128 took 30.7 us there and takes 22.3 us (6.0 TB/s) here.
 
 // Place of 16-byte piece p in a buffer: 8 pieces that lie 16 apart (or, for INT8 codes, 8 apart) on different banks.
 template <int APART>

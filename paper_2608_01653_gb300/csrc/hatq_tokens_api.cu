@@ -66,9 +66,10 @@ enum Operand { kDirect, kLoose, kEither };
 
 // Rows per pass of the dot-product kernel (hatq_tokens.cu), or 0 for the tensor-core kernel (hatq_linear.cu). The
 // former has no pipeline to fill, but its instructions are slow and every CTA brings in all rows. Measured, against the
-// latter: 4096 x 4096 with 1 / 4 / 8 rows 3.6 / 6.7 / 10.9 us against 8.1 .. 8.9; 4096 x 16384 with 2 / 4 rows 15 / 21
+// latter: 4096 x 4096 with 1 / 4 / 8 rows 3.5 / 5.4 / 10.9 us against 8.1 .. 9.1; 4096 x 16384 with 2 / 4 rows 15 / 21
 // against 18.5; 16384 x 4096 with 1 / 2 rows 14 / 23 against 16.6; experts of 2048 x 1536 with a row each, 8 / 16 / 24
-// of them, 5.5 / 12 / 15 against 12 / 19 / 19.
+// of them, 5.6 / 12 / 15 against 12 / 19 / 19. Of grouped products only such small experts were measured: the kernel
+// reads the weights once per row, so that with few and large experts the tensor-core kernel may be the faster one.
 int few_rows(long long rows, const hatq_linear_weights *L, bool grouped) {
     const int few = grouped ? 1 : rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
     const long long weights = (long long)L->n * L->k;
@@ -80,7 +81,7 @@ int few_rows(long long rows, const hatq_linear_weights *L, bool grouped) {
 // of tiles x blocks of the reduction x time per block, the last measured with every SM at work (a wider tile costs
 // more per block and less per product), and about 0.8 us to join a split reduction. Codes that TMA cannot take are
 // brought in by the widening warps, with single-CTA tiles only (48 rows, 4096 -> 8192: 16.8 us against 11.8; 512 rows,
-// 4096 -> 4096: 36 against 16.5), or packed first: a launch of about 3 us and 3 bytes a code.
+// 4096 -> 4096: 36 against 16.9), or packed first: a launch of about 3 us and 3 bytes a code.
 Plan plan_of(long long rows, const hatq_linear_weights *L, bool grouped, int sms, Operand operand) {
     Plan p{};
     const int k_pad = round_up(L->k, 64), kb = k_pad / 64, n_tiles = (L->n + hatq::kRowTile - 1) / hatq::kRowTile;
