@@ -635,6 +635,92 @@ hatq_status hatq_combine_rows(const void *y, int type, long long ldy, long long 
                               const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
                               hatq_stream stream);
 
+/*
+ * The 4-bit cache of an attention layer, and its attention. Keys and values are
+ * transformed along the head in Sylvester blocks of hb (orthonormal), quantized
+ * as Eq. symmetric_q does with 4 bits (the paper states 8-bit tensors; here each
+ * token and head has its own scale) and kept in pages that sequences own through
+ * a table. Attention reads the codes as they lie: queries are transformed
+ * instead of keys, and the result is transformed back.
+ *
+ * A page holds page consecutive tokens of one sequence. Its bytes, per head:
+ * page * width / 2 of key codes, token after token, as many of value codes, page
+ * float32 key scales, page float32 value scales. A byte holds the codes + 8 of
+ * two neighbouring transformed values, the first in its low half; value = code *
+ * scale in the orthonormal basis. Codes are in [-8, 7] (append writes -7 .. 7);
+ * scales are not negative, or NaN.
+ */
+typedef struct {
+    uint8_t *data;        /* device [pages][heads][page * (width + 8)], 16-byte aligned */
+    int pages, page;      /* page: 16, 32 or 64 tokens */
+    int heads, width;     /* heads: 1 .. 1024; width: 64, 128, 192 or 256 */
+    int hb;               /* a power of two <= 256 that divides width (1: no transform) */
+    int reserved;
+} hatq_token_cache;
+
+/* The sequences of a call, common to append and attend, all int32 on the device
+ * and read there only:
+ *   table    [seqs] rows of table_width page numbers at a pitch of ldt: token j of
+ *            sequence b lies in page table[b][j / page]. A page number outside
+ *            [0, pages) is no page: nothing is written to it, and attention passes
+ *            over its tokens. table_width * page <= 2^30
+ *   lengths  [seqs] tokens of each sequence, the call's new ones included; clamped
+ *            to [0, table_width * page]
+ *   starts   [seqs + 1] ascending: sequence b has the rows starts[b] .. starts[b + 1]
+ *            - 1, its newest tokens in order, so that the last row is token
+ *            lengths[b] - 1. NULL: one row each (rows == seqs). Offsets are clamped to
+ *            [0, rows], one below an earlier one counts as the earlier one; rows that
+ *            no sequence holds are neither read nor written
+ *   seqs     at most 65536
+ *
+ * hatq_append_tokens writes the new tokens' keys and values, all in fp32: per row
+ * and head
+ *   t = H~_hb x (unnormalized, sums and differences, shortest distances first),
+ *   a = max|t|, codes = rint(7 t / a), scale = a / 7 / sqrt(hb)
+ * Zeros get codes 0 and scale 1 / sqrt(hb). Where 7 a is not finite (an infinity or
+ * a NaN in the row, or a above 4.8e37) codes are 0 and the scale is NaN. A row
+ * whose token would lie before the sequence's first (more new rows than tokens) or
+ * in no page is not stored.
+ *   k, v     device, type hatq_type, [rows][heads][width] at pitches of ldk, ldv
+ *            (rows) and hk, hv (heads) elements, values contiguous
+ *   kept_k, kept_v   device, or both NULL: what the cache now stands for,
+ *            H~_hb codes * scale / sqrt(hb) rounded to `type`, contiguous
+ *            [rows][heads][width], 16-byte aligned; for every row that a sequence
+ *            holds, stored or not
+ * No element of k or v lies in the cache or in what is written. No two rows of a
+ * call may have the same place in the cache (two entries of the table that name
+ * one page, where both are written): either may be stored. */
+hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, long long ldk, long long hk, const void *v,
+                               long long ldv, long long hv, int type, long long rows, const int32_t *table,
+                               long long ldt, int table_width, const int32_t *lengths, const int32_t *starts, int seqs,
+                               void *kept_k, void *kept_v, hatq_stream stream);
+
+/* Causal softmax attention over the cache. For every row, the token at position p
+ * of its sequence, and query head h, with keys and values of head h / (q_heads /
+ * heads):
+ *   out = sum_{j <= p} w_j v_j / sum_{j <= p} w_j,  w_j = exp(scale q k_j)
+ * A row that sees no token (before the sequence's first, or none of its pages is
+ * one) gets zeros. Tokens that a row does not see do not reach it, whatever their
+ * scales are. q and the weights times the value scales enter the products as fp16
+ * brought into range by powers of two (for fp16 queries as two fp16 each, about 22
+ * bits); sums, maxima and norms are fp32. An infinity or a NaN in a query makes
+ * that head of that row NaN.
+ *   q, out   device, both HATQ_F16 or HATQ_BF16, [rows][q_heads][width] at pitches
+ *            of rows and heads; they share no element, and out none with the cache
+ *   q_heads  a multiple of the cache's heads, rows * q_heads < 2^31 - 1024
+ *   workspace  device scratch of the bytes that hatq_attend_workspace returns for
+ *            the same sizes (starts: whether there are any), 16-byte aligned.
+ *            Calls in flight at the same time need one each
+ * Results do not depend on timing; they may differ in the last bits with the
+ * number of SMs and with what else is in the call. Stream-ordered; an expired
+ * device wait surfaces through hatq_sync_status(). */
+hatq_status hatq_attend_workspace(const hatq_token_cache *cache, int q_heads, long long rows, int seqs, int starts,
+                                  int table_width, size_t *bytes);
+hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long hq, int q_heads, long long rows,
+                               const hatq_token_cache *cache, const int32_t *table, long long ldt, int table_width,
+                               const int32_t *lengths, const int32_t *starts, int seqs, float scale, void *out,
+                               long long ldo, long long ho, void *workspace, size_t workspace_bytes, hatq_stream stream);
+
 /* Failure-detection self test (the paper has no counterpart): launches one
  * thread that waits, through the same bounded mbarrier wait the convolution
  * pipeline uses, on a barrier nothing arrives at. The wait expires after

@@ -1,0 +1,815 @@
+// Attention over the 4-bit cache.
+#include <type_traits>
+
+#include "hatq_cache.h"
+#include "hatq_tc.h"
+
+namespace hatq {
+namespace {
+
+using tc::mbar_init;
+using tc::mbar_expect_tx;
+using tc::smem_addr;
+
+// For query column c of a kv head (token i and head h of the group: c = i * group + h) and keys j:
+//   s_j = f_c k_j sum_d n_jd q_cd, p_j = 2^(s_j - m_c), o_cd = sum_j p_j v_j n'_jd / sum_j p_j
+// with the codes n, n' and the scales k, v of the keys and values, q transformed as the keys were and f the constant
+// factors (softmax scale, log2 e, the transform's norm). o is transformed back when the pieces are joined.
+//
+// Both products run as S^T = K Q^T and O^T = V^T P^T in m16n8k16 steps: codes are the A operand, so that 8 columns
+// cost no more than one. For bf16 queries widening a code is a mask: a nibble x at bits 0-3 of a 16-bit half is the
+// subnormal fp16 number x 2^-24, at bits 4-7 x 2^-20. The latter's factor of 16 goes into q (keys: the value is in the
+// reduction) and into the result (values: it is a row). Codes are stored + 8; that is subtracted once per sum, 8 * 2^-24
+// sum_d q_d as the accumulators' first value, 8 * 2^-24 sum_j p_j by one step with constant A. The scales of keys
+// multiply s, those of values p: no code is ever multiplied by a scale.
+//
+// Rounded to fewer than 32 bits: q and p v, to fp16, both brought into its range by powers of two (q per column, p v
+// by the largest v so far). For fp16 queries, whose outputs would show it, both go through in two parts, high and low,
+// and codes are widened whole: the tensor cores align a subnormal's product as if it were a normal one's, and what they
+// then drop left sums off by up to 2^-14 of their terms.
+// m_c is raised only when some s_j exceeds it by 8: p stays below 2^8, sums are in fp32.
+//
+// Memory-bound for few queries. A warp works by itself: its own ring of chunks (64 keys of one head, brought in by one
+// bulk copy per page), its own maxima and sums; no barrier between warps. The chunks of all sequences and heads are
+// laid in a row and every warp takes an equal part of it, whatever the lengths; what a warp finds of a (sequence, head,
+// column tile) goes to a piece in memory, and a second kernel joins the pieces. Where a CTA's whole part lies in one
+// (sequence, head, tile) its warps are joined first.
+
+__host__ __device__ constexpr int kWarps(int d) { return d == 256 ? 6 : 8; }
+__host__ __device__ constexpr int kStages(int d) { return d == 64 ? 4 : d == 128 ? 3 : 2; }
+__host__ __device__ constexpr int stage_bytes(int d) { return kChunk * (d + 8); }
+__host__ __device__ constexpr int piece_floats(int d, int cols) { return cols * (d + 2); }
+__host__ __device__ constexpr int warp_smem(int d) {       // ring, chunk descriptions, barriers, q, factors; in whole 128 bytes, as bulk copies take 16
+    return (kStages(d) * (stage_bytes(d) + 32 + 8) + 8 * d * 2 + 64 + 127) / 128 * 128;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t at, uint32_t (&w)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
+                         : "r"(at + 4 * i));
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[i]), "=r"(w[i + 1]) : "r"(at + 4 * i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i));
+    }
+}
+__device__ __forceinline__ float load_float(uint32_t at) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float low_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x & 0xffff))); }
+__device__ __forceinline__ float high_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x >> 16))); }
+
+// The codes of a word at bits 0-3 (ODD: 4-7) of its halves, as A operands: bare, subnormal numbers (code + 8) 2^-24 and
+// 2^-20, or (WHOLE) the codes themselves: 1024 + x and 1024 + 16 x are fp16 numbers whose last bits are x.
+template <bool WHOLE, bool ODD>
+__device__ __forceinline__ uint32_t codes_of(uint32_t w) {
+    if constexpr (!WHOLE) return w & (ODD ? 0x00f000f0u : 0x000f000fu);
+    uint32_t x = (w & (ODD ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    if constexpr (ODD)
+        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x) : "r"(0x2c002c00u), "r"(0xd480d480u));      // x / 16 - 72
+    else
+        asm("add.rn.f16x2 %0, %0, %1;" : "+r"(x) : "r"(0xe408e408u));                            // x - 1032
+    return x;
+}
+
+// The row of chunks: sequence after sequence, in it head after head, in it tile after tile of the columns.
+struct Sequence {
+    int b, begin, m, len;              // its index, first row, new tokens, length
+    int tiles, chunks;                 // column tiles of a head, chunks of 64 keys
+    long long unit, segment;           // units and segments (head, tile) of the sequences before it
+    __device__ long long units(int heads) const { return (long long)heads * tiles * chunks; }
+    __device__ long long segments(int heads) const { return chunks ? (long long)heads * tiles : 0; }
+};
+
+template <int COLS>
+__device__ __forceinline__ void measure(const CacheArgs &c, int group, Sequence &s, int b, int most_before, int next) {
+    s.b = b;
+    s.begin = min(max(most_before, 0), c.rows);
+    s.m = min(max(next, 0), c.rows) - s.begin;
+    if (s.m < 0) s.m = 0;
+    s.len = length_of(c, b);
+    s.tiles = (int)(((long long)s.m * group + COLS - 1) / COLS);
+    s.chunks = (s.len + kChunk - 1) / kChunk;
+}
+
+__device__ __forceinline__ long long scan_add(long long v, int lane) {
+#pragma unroll
+    for (int h = 1; h < 32; h *= 2) {
+        const long long o = __shfl_up_sync(0xffffffffu, v, h);
+        if (lane >= h) v += o;
+    }
+    return v;
+}
+
+// All units, or, where `unit` is one of them, the sequence that holds it. A whole warp calls this.
+template <int COLS>
+__device__ __forceinline__ long long find_unit(const CacheArgs &c, int group, int lane, long long unit, Sequence &found) {
+    long long units = 0, segments = 0;
+    int most = 0;                                            // of the offsets so far
+    for (int b0 = 0; b0 < c.seqs; b0 += 32) {
+        const int b = b0 + lane;
+        Sequence s{};
+        if (c.starts) {
+            int here = b < c.seqs ? c.starts[b] : 0, next = b < c.seqs ? c.starts[b + 1] : 0;
+            here = max(here, most);
+#pragma unroll
+            for (int h = 1; h < 32; h *= 2) here = max(here, __shfl_up_sync(0xffffffffu, here, h));   // (lane < h: its own)
+            next = max(next, here);
+            if (b < c.seqs) measure<COLS>(c, group, s, b, here, next);
+            most = __shfl_sync(0xffffffffu, next, 31);
+        } else if (b < c.seqs) {
+            measure<COLS>(c, group, s, b, b, b + 1);
+        }
+        const long long mine = s.units(c.heads), segs = s.segments(c.heads);
+        const long long up_to = scan_add(mine, lane);
+        if (unit >= 0) {
+            const bool here = unit < units + up_to;
+            const unsigned who = __ballot_sync(0xffffffffu, here);
+            if (who) {
+                const int from = __ffs(who) - 1;
+                const long long before = units + up_to - mine, before_segs = segments + scan_add(segs, lane) - segs;
+                found.b = __shfl_sync(0xffffffffu, s.b, from);
+                found.begin = __shfl_sync(0xffffffffu, s.begin, from);
+                found.m = __shfl_sync(0xffffffffu, s.m, from);
+                found.len = __shfl_sync(0xffffffffu, s.len, from);
+                found.tiles = __shfl_sync(0xffffffffu, s.tiles, from);
+                found.chunks = __shfl_sync(0xffffffffu, s.chunks, from);
+                found.unit = __shfl_sync(0xffffffffu, before, from);
+                found.segment = __shfl_sync(0xffffffffu, before_segs, from);
+                return 0;
+            }
+            segments += __shfl_sync(0xffffffffu, scan_add(segs, lane), 31);
+        }
+        units += __shfl_sync(0xffffffffu, up_to, 31);
+    }
+    return units;
+}
+
+// What a warp knows of a chunk between asking for it and working on it.
+struct alignas(16) Chunk {
+    int begin, m, len;                 // of its sequence
+    int head, tile, chunk;
+    int pages;                         // bit i: its page i holds keys
+    int first_last;                    // of the warp's part of the segment: bit 0 first, bit 1 last
+};
+static_assert(sizeof(Chunk) == 32, "two 16-byte loads");
+
+template <int D, typename T, int NT>
+__global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendArgs a) {
+    constexpr int COLS = 8 * NT, WARPS = kWarps(D), STAGES = kStages(D), STAGE = stage_bytes(D);
+    constexpr int WORDS = D / 32, VW = D / 64, STEPS = D / 16, E = D / 32;
+    constexpr bool kTwo = std::is_same<T, __half>::value;      // q and p in two parts
+    constexpr int PARTS = kTwo ? 2 : 1;
+    constexpr float kOdd = kTwo ? 1.0f : 0.0625f, kUnit = kTwo ? 1.0f : 0x1p24f;     // of a code at an odd place; of a sum
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int s_abort;
+    const CacheArgs &c = a.c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    uint8_t *mine = smem + warp * warp_smem(D);
+    Chunk *chunks = reinterpret_cast<Chunk *>(mine + STAGES * STAGE);
+    __half *q_smem = reinterpret_cast<__half *>(mine + STAGES * (STAGE + 32));
+    float *factors = reinterpret_cast<float *>(mine + STAGES * (STAGE + 32) + 16 * D);      // 8 offsets, 8 factors
+    const uint32_t ring = smem_addr(mine), bars = smem_addr(mine + STAGES * (STAGE + 32) + 16 * D + 64);
+    volatile int *abort_flag = &s_abort;
+
+    if (lane < STAGES) mbar_init(bars + 8 * lane, 1);
+    tc::fence_barrier_init();
+    if (threadIdx.x == 0) s_abort = 0;
+    __syncthreads();
+    after_prior_kernels();
+    if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
+
+    // ---- this warp's part
+    Sequence seq{};
+    const long long total = find_unit<COLS>(c, a.group, lane, -1, seq);
+    const long long workers = (long long)gridDim.x * WARPS, worker = (long long)blockIdx.x * WARPS + warp;
+    const long long cta_from = blockIdx.x * WARPS * total / workers, cta_to = (blockIdx.x + 1LL) * WARPS * total / workers;
+    const long long from = worker * total / workers, to = (worker + 1) * total / workers;
+    if (cta_from == cta_to) return;
+    find_unit<COLS>(c, a.group, lane, cta_from, seq);
+    const long long in_cta = (cta_from - seq.unit) / seq.chunks;
+    const bool joined = cta_to <= seq.unit + (in_cta + 1) * seq.chunks;      // the CTA's part lies in one segment
+    if (from < to && from >= seq.unit + seq.units(c.heads)) find_unit<COLS>(c, a.group, lane, from, seq);
+    const int size = 1 << c.page_bits, pages_of_chunk = kChunk >> c.page_bits;
+    const uint32_t record = (uint32_t)size * (D + 8);
+
+    // ---- asking for chunks
+    long long unit = from;                                   // the next one to ask for
+    int segment = 0, chunk = 0, asked = 0;                   // segment within the sequence
+    if (from < to) {
+        segment = (int)((from - seq.unit) / seq.chunks);
+        chunk = (int)((from - seq.unit) % seq.chunks);
+    }
+    int entry = -1, entries_from = -1;                       // 32 entries of the sequence's row of the table, one a lane
+    auto ask = [&]() {
+        if (unit >= to) return;
+        const int stage = asked % STAGES;
+        const int first_page = chunk * pages_of_chunk;
+        if (entries_from < 0 || first_page < entries_from || first_page >= entries_from + 32) {
+            entries_from = first_page;
+            entry = first_page + lane < c.table_width ? c.table[seq.b * c.ldt + first_page + lane] : -1;
+        }
+        const int page = __shfl_sync(0xffffffffu, entry, (first_page - entries_from + lane) & 31);
+        const int head = segment / seq.tiles;
+        const bool take = lane < pages_of_chunk && chunk * kChunk + lane * size < seq.len && page >= 0 && page < c.pages;
+        const unsigned pages = __ballot_sync(0xffffffffu, take);
+        if (lane == 0) {
+            Chunk k;
+            k.begin = seq.begin;
+            k.m = seq.m;
+            k.len = seq.len;
+            k.head = head;
+            k.tile = segment - head * seq.tiles;
+            k.chunk = chunk;
+            k.pages = (int)pages;
+            const bool first = unit == from || chunk == 0, last = unit + 1 == to || chunk + 1 == seq.chunks;
+            k.first_last = (first ? 1 : 0) | (last ? 2 : 0);
+            chunks[stage] = k;
+            mbar_expect_tx(bars + 8 * stage, (uint32_t)__popc(pages) * record);
+        }
+        __syncwarp();
+        if (take)
+            bulk_load(ring + stage * STAGE + lane * record, c.data + ((long long)page * c.heads + head) * record, record, bars + 8 * stage);
+        ++asked;
+        ++unit;
+        if (++chunk == seq.chunks) {
+            chunk = 0;
+            if (entries_from != 0) entries_from = -1;
+            if (++segment == c.heads * seq.tiles && unit < to) {
+                // the next sequence that has units
+                Sequence next = seq;
+                do {
+                    const long long u = next.unit + next.units(c.heads), sg = next.segment + next.segments(c.heads);
+                    const int end = next.begin + next.m, b = next.b + 1;
+                    measure<COLS>(c, a.group, next, b, c.starts ? end : b, c.starts ? max(end, c.starts[b + 1]) : b + 1);
+                    next.unit = u;
+                    next.segment = sg;
+                } while (next.units(c.heads) == 0 && next.b + 1 < c.seqs);
+                seq = next;
+                segment = 0;
+                entries_from = -1;
+            }
+        }
+    };
+    // Where the pieces go: one that begins its segment has the segment's place, any other (a worker has at most one, its
+    // first) the worker's.
+    long long piece = 0;
+    if (from < to)
+        piece = from == seq.unit + (long long)segment * seq.chunks ? seq.segment + segment : a.segments + worker;
+    long long next_piece = from < to ? seq.segment + segment + 1 : 0;
+    for (int i = 0; i < STAGES; ++i) ask();
+
+    float o[NT][STEPS][4], off[NT][4], m[NT][2], l[NT][2];
+    uint32_t qf[PARTS][NT][STEPS][2];
+    float q_off[NT][2], q_f[NT][2];
+    int lim[NT][2];
+    float rinv = 0x1p100f;
+    bool sound = true;
+    const int units = (int)(to - from);
+    const int near = (g & 1) ? 7 - (g >> 1) : g >> 1;        // the key of the tile that row g of A is; row g + 8: + 8
+    const uint32_t ones[4] = {0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u};       // 8 * 2^-24
+
+    for (int i = 0; i < units; ++i) {
+        const int stage = i % STAGES;
+        sound = tc::mbar_wait(bars + 8 * stage, (uint32_t)(i / STAGES) & 1u, abort_flag, a.err);
+        sound = __all_sync(0xffffffffu, sound);
+        if (!sound) break;
+        const Chunk k = chunks[stage];
+
+        if (k.first_last & 1) {
+            // ---- a new segment: its queries, 8 columns at a time
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float v[8][E];
+#pragma unroll
+                for (int col = 0; col < 8; ++col) {
+                    const int x = k.tile * COLS + nt * 8 + col, token = x / a.group, h = x - token * a.group;
+                    const T *p = static_cast<const T *>(a.q) + (long long)(k.begin + token) * a.ldq +
+                                 (long long)(k.head * a.group + h) * a.hq + lane;
+                    const bool live = token < k.m;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[col][e] = live ? to_f32<T>(p[32 * e]) : 0.0f;
+                }
+#pragma unroll
+                for (int col = 0; col < 8; ++col) {
+#pragma unroll
+                    for (int h = 1; h < 32; h *= 2)
+                        if (h < c.hb)
+#pragma unroll
+                            for (int e = 0; e < E; ++e) {
+                                const float other = __shfl_xor_sync(0xffffffffu, v[col][e], h);
+                                v[col][e] = lane & h ? other - v[col][e] : v[col][e] + other;
+                            }
+#pragma unroll
+                    for (int h = 1; h < E; h *= 2)
+                        if (32 * h < c.hb)
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                if (!(e & h) && e + h < E) {
+                                    const float x = v[col][e], y = v[col][e + h];
+                                    v[col][e] = x + y;
+                                    v[col][e + h] = x - y;
+                                }
+                    unsigned bits = 0;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) bits = max(bits, __float_as_uint(v[col][e]) & 0x7fffffffu);
+                    bits = __reduce_max_sync(0xffffffffu, bits);
+                    // |q| below 2^10, by a power of two; an infinity or a NaN makes the whole column NaN
+                    const unsigned ex = max(bits >> 23, 10u);
+                    const float by = ex == 255u ? __int_as_float(0x7fffffff) : __uint_as_float((263u - ex) << 23);
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[col][e] *= by;
+                    // values at odd places meet codes of 16-fold value
+                    const float part = lane & 1 ? kOdd : 1.0f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const __half h = __float2half_rn(v[col][e] * part);
+                        q_smem[col * D + 32 * e + (lane & 24) + ((lane & 3) << 1) + ((lane >> 2) & 1)] = h;
+                        const float back = __half2float(h) * (lane & 1 ? 1.0f / kOdd : 1.0f);
+                        sum += back;
+                        v[col][e] -= back;
+                    }
+#pragma unroll
+                    for (int h = 1; h < 32; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
+                    if (lane == 0) {
+                        factors[col] = kTwo ? 0.0f : -0x1p-21f * sum;
+                        factors[8 + col] = a.scale * c.inv_norm * kUnit * __uint_as_float((min(ex, 254u) - 9u) << 23);
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    if (part) {
+                        __syncwarp();
+#pragma unroll
+                        for (int col = 0; col < 8; ++col)
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                q_smem[col * D + 32 * e + (lane & 24) + ((lane & 3) << 1) + ((lane >> 2) & 1)] =
+                                    __float2half_rn(v[col][e]);
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int j = 0; j < WORDS; ++j) {
+                        uint32_t w[4];
+                        load_words<4>(smem_addr(q_smem + g * D + (t * WORDS + j) * 8), w);
+                        qf[part][nt][2 * j][0] = w[0];
+                        qf[part][nt][2 * j][1] = w[1];
+                        qf[part][nt][2 * j + 1][0] = w[2];
+                        qf[part][nt][2 * j + 1][1] = w[3];
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int x = k.tile * COLS + nt * 8 + 2 * t + y, token = x / a.group;
+                    q_off[nt][y] = factors[2 * t + y];
+                    q_f[nt][y] = factors[8 + 2 * t + y];
+                    lim[nt][y] = token < k.m ? k.len - k.m + token : -1;
+                    m[nt][y] = -1e30f;
+                    l[nt][y] = 0.0f;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) o[nt][s][y] = 0.0f;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) off[nt][y] = 0.0f;
+            }
+            rinv = 0x1p100f;
+        }
+
+        // ---- S^T of the chunk's 64 keys
+        const uint32_t base = ring + stage * STAGE;
+        const int key0 = k.chunk * kChunk, left = min(k.len - key0, kChunk);
+        const bool whole = key0 + kChunk <= k.len - k.m + k.tile * COLS / a.group + 1 && k.pages == (1 << pages_of_chunk) - 1;
+        float s[NT][4][4], vs[4][2], most[NT][2], largest = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) most[nt][0] = most[nt][1] = -1e30f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int in_page = (16 * j) >> c.page_bits, token = (16 * j) & (size - 1);
+            const uint32_t rec = base + in_page * record, krow = rec + (token + near) * (D / 2);
+            if (16 * j < left) {
+                uint32_t w0[WORDS], w1[WORDS];
+                load_words<WORDS>(krow + t * (WORDS * 4), w0);
+                load_words<WORDS>(krow + 8 * (D / 2) + t * (WORDS * 4), w1);
+                const uint32_t sc = rec + size * D + 4 * (token + near);
+                float k0 = load_float(sc), k1 = load_float(sc + 32);
+                vs[j][0] = load_float(sc + 4 * size);
+                vs[j][1] = load_float(sc + 4 * size + 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    s[nt][j][0] = s[nt][j][2] = q_off[nt][0];
+                    s[nt][j][1] = s[nt][j][3] = q_off[nt][1];
+                }
+#pragma unroll
+                for (int x = 0; x < WORDS; ++x) {
+                    const uint32_t u0 = w0[x] >> 8, u1 = w1[x] >> 8;
+                    const uint32_t A[4] = {codes_of<kTwo, false>(w0[x]), codes_of<kTwo, false>(w1[x]), codes_of<kTwo, true>(w0[x]),
+                                           codes_of<kTwo, true>(w1[x])};
+                    const uint32_t B[4] = {codes_of<kTwo, false>(u0), codes_of<kTwo, false>(u1), codes_of<kTwo, true>(u0),
+                                           codes_of<kTwo, true>(u1)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) {
+                            mma(s[nt][j], A, qf[part][nt][2 * x][0], qf[part][nt][2 * x][1]);
+                            mma(s[nt][j], B, qf[part][nt][2 * x + 1][0], qf[part][nt][2 * x + 1][1]);
+                        }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    s[nt][j][0] *= k0 * q_f[nt][0];
+                    s[nt][j][1] *= k0 * q_f[nt][1];
+                    s[nt][j][2] *= k1 * q_f[nt][0];
+                    s[nt][j][3] *= k1 * q_f[nt][1];
+                }
+                if (!whole) {
+                    const int key = key0 + 16 * j + near;
+                    const bool held = (k.pages >> in_page) & 1;
+                    const bool in0 = held && key < k.len, in1 = held && key + 8 < k.len;
+                    if (!in0) vs[j][0] = 0.0f;
+                    if (!in1) vs[j][1] = 0.0f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            if (!in0 || key > lim[nt][y]) s[nt][j][y] = -INFINITY;
+                            if (!in1 || key + 8 > lim[nt][y]) s[nt][j][2 + y] = -INFINITY;
+                        }
+                }
+            } else {
+                vs[j][0] = vs[j][1] = 0.0f;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[nt][j][0] = s[nt][j][1] = s[nt][j][2] = s[nt][j][3] = -INFINITY;
+            }
+            largest = fmaxf(largest, fmaxf(vs[j][0], vs[j][1]));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                most[nt][0] = fmaxf(most[nt][0], fmaxf(s[nt][j][0], s[nt][j][2]));
+                most[nt][1] = fmaxf(most[nt][1], fmaxf(s[nt][j][1], s[nt][j][3]));
+            }
+        }
+
+        // ---- raise the maxima where a weight would leave the range
+        bool raise = largest * rinv > 128.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) raise |= most[nt][0] > m[nt][0] + 8.0f || most[nt][1] > m[nt][1] + 8.0f;
+        if (__any_sync(0xffffffffu, raise)) {
+            float ratio = 1.0f;
+            largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));
+            if (largest * rinv > 128.0f) {
+                const int ex = (int)(__float_as_uint(largest) >> 23);
+                const float now = __uint_as_float((uint32_t)min(max(260 - ex, 1), 247) << 23);      // largest * now in [2^6, 2^7)
+                ratio = now / rinv;
+                rinv = now;
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float by[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    float x = most[nt][y];
+#pragma unroll
+                    for (int h = 4; h < 32; h *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, h));
+                    x = fmaxf(x, m[nt][y]);
+                    by[y] = exp2_fast(m[nt][y] - x);
+                    m[nt][y] = x;
+                    l[nt][y] *= by[y];
+                    by[y] *= ratio;
+                    off[nt][y] *= by[y];
+                }
+#pragma unroll
+                for (int x = 0; x < STEPS; ++x) {
+                    o[nt][x][0] *= by[0];
+                    o[nt][x][1] *= by[1];
+                    o[nt][x][2] *= by[0];
+                    o[nt][x][3] *= by[1];
+                }
+            }
+        }
+
+        // ---- weights, and O^T
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (16 * j >= left) break;
+            uint32_t pf[PARTS][NT][2];
+            const float v0 = vs[j][0] * rinv, v1 = vs[j][1] * rinv;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float p[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) p[y] = exp2_fast(s[nt][j][y] - m[nt][y & 1]);
+                l[nt][0] += p[0] + p[2];
+                l[nt][1] += p[1] + p[3];
+                // (a weight of 0 stays 0, whatever the scale of a value that this query does not see)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) p[y] = whole || p[y] != 0.0f ? p[y] * (y < 2 ? v0 : v1) : 0.0f;
+                const uint32_t x = pack_half(p[0], p[1]), y = pack_half(p[2], p[3]);
+                pf[0][nt][0] = transposed(x);
+                pf[0][nt][1] = transposed(y);
+                if constexpr (kTwo) {
+                    pf[1][nt][0] = transposed(pack_half(p[0] - low_half(x), p[1] - high_half(x)));
+                    pf[1][nt][1] = transposed(pack_half(p[2] - low_half(y), p[3] - high_half(y)));
+                }
+                if constexpr (!kTwo) mma(off[nt], ones, pf[0][nt][0], pf[0][nt][1]);
+            }
+            const int in_page = (16 * j) >> c.page_bits, token = (16 * j) & (size - 1);
+            const uint32_t row = base + in_page * record + (size + token) * (D / 2) + g * (VW * 4);
+            uint32_t w[4][VW];
+            load_words<VW>(row + t * (D / 2), w[0]);
+            load_words<VW>(row + (7 - t) * (D / 2), w[1]);
+            load_words<VW>(row + (8 + t) * (D / 2), w[2]);
+            load_words<VW>(row + (15 - t) * (D / 2), w[3]);
+#pragma unroll
+            for (int x = 0; x < VW; ++x)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t n0 = __byte_perm(w[0][x], w[1][x], half ? 0x7632 : 0x5410);
+                    const uint32_t n1 = __byte_perm(w[2][x], w[3][x], half ? 0x7632 : 0x5410);
+                    const uint32_t u0 = n0 >> 8, u1 = n1 >> 8;
+                    const uint32_t A[4] = {codes_of<kTwo, false>(n0), codes_of<kTwo, true>(n0), codes_of<kTwo, false>(n1),
+                                           codes_of<kTwo, true>(n1)};
+                    const uint32_t B[4] = {codes_of<kTwo, false>(u0), codes_of<kTwo, true>(u0), codes_of<kTwo, false>(u1),
+                                           codes_of<kTwo, true>(u1)};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) {
+                            mma(o[nt][4 * x + 2 * half], A, pf[part][nt][0], pf[part][nt][1]);
+                            mma(o[nt][4 * x + 2 * half + 1], B, pf[part][nt][0], pf[part][nt][1]);
+                        }
+                }
+        }
+        __syncwarp();
+
+        if (k.first_last & 2) {
+            // ---- the warp's part of the segment is done: m, l and o of every column to its piece
+            float *to_piece = joined ? reinterpret_cast<float *>(mine) : a.pieces + piece * piece_floats(D, COLS);
+            const float up = 1.0f / rinv;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    float x = l[nt][y];
+#pragma unroll
+                    for (int h = 4; h < 32; h *= 2) x += __shfl_xor_sync(0xffffffffu, x, h);
+                    const int col = nt * 8 + 2 * t + y;
+                    if (g == 0) {
+                        to_piece[col] = m[nt][y];
+                        to_piece[COLS + col] = x;
+                    }
+                    float *p = to_piece + 2 * COLS + col * D + g * (D / 8);
+#pragma unroll
+                    for (int x = 0; x < STEPS; ++x)
+                        *reinterpret_cast<float2 *>(p + 2 * x) =
+                            make_float2((o[nt][x][y] - off[nt][y]) * kUnit * up,
+                                        (o[nt][x][2 + y] * kOdd - off[nt][y]) * kUnit * up);
+                }
+            piece = next_piece++;
+        }
+        if (!joined || i + STAGES < units) ask();
+    }
+    if (!sound) {
+        // copies still on their way have to land before the CTA leaves
+        const long long t0 = clock64();
+        for (int i = 0; i < STAGES; ++i)
+            if (i < asked) {
+                const int last = (asked - 1 - i) / STAGES, stage = (asked - 1 - i) % STAGES;
+                while (!tc::mbar_try_wait(bars + 8 * stage, (uint32_t)last & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
+            }
+    }
+    if (!joined) return;
+
+    // ---- one segment: the warps' parts become one piece
+    if (from == to && lane < COLS) {
+        float *p = reinterpret_cast<float *>(mine);
+        p[lane] = -1e30f;
+        p[COLS + lane] = 0.0f;
+    }
+    __syncthreads();
+    if (s_abort) return;
+    Sequence first{};
+    find_unit<COLS>(c, a.group, lane, cta_from, first);
+    const long long seg = (cta_from - first.unit) / first.chunks;
+    float *out = a.pieces + (cta_from == first.unit + seg * first.chunks ? first.segment + seg
+                                                                         : a.segments + blockIdx.x * (long long)WARPS) * piece_floats(D, COLS);
+    for (int x = threadIdx.x; x < COLS * D; x += WARPS * 32) {
+        const int col = x / D;
+        float most = -1e30f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) most = fmaxf(most, reinterpret_cast<const float *>(smem + w * warp_smem(D))[col]);
+        float sum = 0.0f, o_sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float *p = reinterpret_cast<const float *>(smem + w * warp_smem(D));
+            if (p[COLS + col] != 0.0f) {
+                const float by = exp2_fast(p[col] - most);
+                sum += by * p[COLS + col];
+                o_sum += by * p[2 * COLS + x];
+            }
+        }
+        out[2 * COLS + x] = o_sum;
+        if (x % D == 0) {
+            out[col] = most;
+            out[COLS + col] = sum;
+        }
+    }
+}
+
+// Joins the pieces of every row and head: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p, transformed back. A CTA has
+// one row and the heads of one kv head; where these are fewer than its warps, several warps share a head's pieces.
+template <int D, typename T, int NT>
+__global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas) {
+    constexpr int COLS = 8 * NT, WARPS = kWarps(D), E = D / 32;
+    __shared__ float s_m[8], s_l[8], s_o[8][D];
+    after_prior_kernels();
+    if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
+    const CacheArgs &c = a.c;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = (int)(blockIdx.x / c.heads), head = (int)(blockIdx.x % c.heads);
+    int b, begin, end;
+    if (!sequence_of(c, r, lane, b, begin, end)) return;
+    // units and segments of the sequences before, and all units
+    long long before = 0, total = 0, segs = 0;
+    int most = 0;
+    for (int b0 = 0; b0 < c.seqs; b0 += 32) {
+        const int x = b0 + lane;
+        Sequence s{};
+        if (c.starts) {
+            int here = x < c.seqs ? c.starts[x] : 0, next = x < c.seqs ? c.starts[x + 1] : 0;
+            here = max(here, most);
+#pragma unroll
+            for (int h = 1; h < 32; h *= 2) here = max(here, __shfl_up_sync(0xffffffffu, here, h));
+            next = max(next, here);
+            if (x < c.seqs) measure<COLS>(c, a.group, s, x, here, next);
+            most = __shfl_sync(0xffffffffu, next, 31);
+        } else if (x < c.seqs) {
+            measure<COLS>(c, a.group, s, x, x, x + 1);
+        }
+        const long long u = s.units(c.heads);
+        total += u;
+        if (x < b) {
+            before += u;
+            segs += s.segments(c.heads);
+        }
+    }
+#pragma unroll
+    for (int h = 1; h < 32; h *= 2) {
+        total += __shfl_xor_sync(0xffffffffu, total, h);
+        before += __shfl_xor_sync(0xffffffffu, before, h);
+        segs += __shfl_xor_sync(0xffffffffu, segs, h);
+    }
+    Sequence s{};
+    measure<COLS>(c, a.group, s, b, begin, end);
+    const int token = r - begin, ways = a.group >= 8 ? 1 : 8 / a.group;       // warps that share a head
+    const long long workers = (long long)ctas * WARPS;
+    for (int h0 = 0; h0 < a.group; h0 += 8) {
+        const int h = h0 + (ways > 1 ? warp % a.group : warp), way = ways > 1 ? warp / a.group : 0;
+        const bool live = h < a.group && way < ways;
+        const int x = token * a.group + h, tile = x / COLS, col = x % COLS;
+        float mx = -1e30f, l = 0.0f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.0f;
+        if (live && s.chunks > 0) {
+            const long long seg = (long long)head * s.tiles + tile, u0 = before + seg * s.chunks, u1 = u0 + s.chunks;
+            long long at = u0;
+            for (int i = 0; at < u1; ++i) {
+                const long long w = ((at + 1) * workers - 1) / total;         // the worker that has unit `at`
+                const long long cta = w / WARPS, from = cta * WARPS * total / workers, to = (cta + 1) * WARPS * total / workers;
+                long long place, next;
+                if (from >= u0 && to <= u1) {
+                    place = from == u0 ? segs + seg : a.segments + cta * WARPS;
+                    next = to;
+                } else {
+                    place = at == u0 ? segs + seg : a.segments + w;
+                    next = (w + 1) * total / workers;
+                }
+                at = next;
+                if (i % ways != way) continue;
+                const float *p = a.pieces + place * piece_floats(D, COLS);
+                const float pm = p[col], pl = p[COLS + col];
+                if (pl == 0.0f) continue;
+                const float now = fmaxf(mx, pm), by = exp2_fast(mx - now), add = exp2_fast(pm - now);
+                mx = now;
+                l = l * by + pl * add;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = o[e] * by + p[2 * COLS + col * D + 32 * e + lane] * add;
+            }
+        }
+        if (ways > 1) {
+            if (lane == 0) {
+                s_m[warp] = mx;
+                s_l[warp] = l;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) s_o[warp][32 * e + lane] = o[e];
+            __syncthreads();
+            if (live && way == 0)
+                for (int y = 1; y < ways; ++y) {
+                    const int other = warp + y * a.group;
+                    const float pm = s_m[other], pl = s_l[other];
+                    if (pl == 0.0f) continue;
+                    const float now = fmaxf(mx, pm), by = exp2_fast(mx - now), add = exp2_fast(pm - now);
+                    mx = now;
+                    l = l * by + pl * add;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = o[e] * by + s_o[other][32 * e + lane] * add;
+                }
+            __syncthreads();
+        }
+        if (!live || way) continue;
+        const float by = l == 0.0f ? 0.0f : c.inv_norm / l;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2)
+            if (d < c.hb)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float other = __shfl_xor_sync(0xffffffffu, o[e], d);
+                    o[e] = lane & d ? other - o[e] : o[e] + other;
+                }
+#pragma unroll
+        for (int d = 1; d < E; d *= 2)
+            if (32 * d < c.hb)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(e & d) && e + d < E) {
+                        const float x = o[e], y = o[e + d];
+                        o[e] = x + y;
+                        o[e + d] = x - y;
+                    }
+        T *out = static_cast<T *>(a.out) + (long long)r * a.ldo + (long long)(head * a.group + h) * a.ho + lane;
+#pragma unroll
+        for (int e = 0; e < E; ++e) out[32 * e] = from_f32<T>(o[e] * by);
+    }
+}
+
+template <int D, typename T, int NT>
+cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
+    static std::atomic<int> allowed[64];
+    const int bytes = kWarps(D) * warp_smem(D);
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(attend_kernel<D, T, NT>), bytes, allowed);
+    if (e != cudaSuccess) return e;
+    if ((e = launch_early(attend_kernel<D, T, NT>, dim3((unsigned)a.sms), kWarps(D) * 32, bytes, s, a)) != cudaSuccess) return e;
+    return launch_early(join_kernel<D, T, NT>, dim3((unsigned)((long long)a.c.rows * a.c.heads)), 256, 0, s, a, a.sms);
+}
+template <int D, typename T>
+cudaError_t launch_columns(const AttendArgs &a, cudaStream_t s) {
+    if constexpr (D <= 128)
+        if (a.columns == 16) return launch<D, T, 2>(a, s);
+    return launch<D, T, 1>(a, s);
+}
+template <typename T>
+cudaError_t launch_type(const AttendArgs &a, cudaStream_t s) {
+    switch (a.c.width) {
+        case 64: return launch_columns<64, T>(a, s);
+        case 128: return launch_columns<128, T>(a, s);
+        case 192: return launch_columns<192, T>(a, s);
+        default: return launch_columns<256, T>(a, s);
+    }
+}
+
+}  // namespace
+
+int attend_columns(int width, int group, bool one_each) { return width <= 128 && (group > 8 || !one_each) ? 16 : 8; }
+int attend_workers(int width, int sms) { return sms * kWarps(width); }
+cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s) {
+    return type == HATQ_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);
+}
+
+}  // namespace hatq

@@ -10,6 +10,11 @@
 #include <atomic>
 #include <thread>
 
+#ifdef __CUDACC__
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#endif
+
 #include "hatq.h"
 
 namespace hatq {
@@ -70,6 +75,17 @@ cudaError_t launch_linear_tc(const CUtensorMap &tm, const LinearArgs &a, int til
 cudaError_t launch_combine_rows(const void *y, int type, long long ldy, long long rows, const int32_t *index,
                                 const float *weights, long long tokens, int topk, int c, void *out, long long ldo,
                                 int unit, int sms, cudaStream_t s);   // unit: bytes that all rows are aligned to, 16, 4 or 2
+
+#ifdef __CUDACC__
+template <typename T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+#endif
 
 // A kernel of this file's operators may be started while the one before it in
 // the stream is ending: it sets itself up and then waits here, before its first

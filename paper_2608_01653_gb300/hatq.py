@@ -72,6 +72,11 @@ class LinearWeightsStruct(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+class TokenCacheStruct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int), ("page", ctypes.c_int), ("heads", ctypes.c_int),
+                ("width", ctypes.c_int), ("hb", ctypes.c_int), ("reserved", ctypes.c_int)]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -142,6 +147,12 @@ def load(build: bool = True) -> ctypes.CDLL:
             "hatq_grouped_linear": (_I, [_P, _I, _L, _P, _L, _P, ctypes.POINTER(LinearWeightsStruct), _I, _P, _L, _P,
                                          ctypes.c_size_t, _P]),
             "hatq_combine_rows": (_I, [_P, _I, _L, _L, _P, _P, _L, _I, _I, _P, _L, _P]),
+            "hatq_append_tokens": (_I, [ctypes.POINTER(TokenCacheStruct), _P, _L, _L, _P, _L, _L, _I, _L, _P, _L, _I, _P, _P,
+                                        _I, _P, _P, _P]),
+            "hatq_attend_workspace": (_I, [ctypes.POINTER(TokenCacheStruct), _I, _L, _I, _I, _I,
+                                           ctypes.POINTER(ctypes.c_size_t)]),
+            "hatq_attend_tokens": (_I, [_P, _I, _L, _L, _I, _L, ctypes.POINTER(TokenCacheStruct), _P, _L, _I, _P, _P, _I,
+                                        _F, _P, _L, _L, _P, ctypes.c_size_t, _P]),
             "hatq_version": (_I, []),
         }
         for name, (res, args) in sig.items():
@@ -1041,6 +1052,141 @@ def combine_rows(y, index, weights, out=None, stream=None):
     st = (_LIB or load()).hatq_combine_rows(y.data_ptr(), kind, pitch, rows, _flat(index, "index", torch.int32, shape, device),
                                             _flat(weights, "weights", torch.float32, shape, device), t, topk, c,
                                             out.data_ptr(), out_pitch, raw)
+    if st:
+        _check(st)
+    return out
+
+
+# ------------------------------------------------------------------ the 4-bit cache
+
+class TokenCache:
+    """The 4-bit keys and values of one attention layer (hatq_token_cache): `data` is a contiguous uint8 CUDA tensor
+    [pages][heads][page * (width + 8)] of the caller's, hb the block of the transform along a head."""
+
+    def __init__(self, data, page=64, hb=1):
+        torch = _token_torch()
+        if data.dtype != torch.uint8 or data.dim() != 3 or not data.is_contiguous():
+            raise ValueError("data: expected a contiguous uint8 tensor [pages][heads][page * (width + 8)]")
+        pages, heads, size = data.shape
+        if page not in (16, 32, 64) or size % page:
+            raise ValueError(f"data: {size} bytes per head and page are no {page} tokens (16, 32 or 64 a page)")
+        self.device = data.get_device()
+        if self.device < 0:
+            raise ValueError(f"expected CUDA tensors, got {data.device}")
+        self.data, self.pages, self.page, self.heads, self.width, self.hb = data, pages, page, heads, size // page - 8, hb
+        self.struct = TokenCacheStruct(data.data_ptr(), pages, page, heads, self.width, hb, 0)
+        self.ref = ctypes.byref(self.struct)
+        self.scale = self.width ** -0.5 if self.width > 0 else 1.0
+        size = ctypes.c_size_t()                    # the library looks the sizes over
+        _check(load().hatq_attend_workspace(self.ref, heads, 0, 0, 0, 0, ctypes.byref(size)))
+
+    @staticmethod
+    def bytes_of(pages, heads, width, page=64):
+        """Bytes of `data`: half a byte a value, and 8 bytes of scales per token and head."""
+        return pages * heads * page * (width + 8)
+
+    @classmethod
+    def empty(cls, pages, heads, width, page=64, hb=None, device="cuda"):
+        """A cache of its own memory; hb: by default the largest power of two that divides width."""
+        torch = _torch()
+        data = torch.empty(pages, heads, page * (width + 8), dtype=torch.uint8, device=device)
+        return cls(data, page, (width & -width) if hb is None else hb)
+
+
+def _heads_of(t, name, heads, width, device):
+    """Checks a [rows][heads][width] tensor on `device` whose values are contiguous; returns its type code, its rows and
+    the pitches of rows and heads in elements."""
+    code = _TOKEN_TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: dtype {t.dtype} is none of {[str(d) for d in _TOKEN_TYPES]}")
+    if t.dim() != 3 or heads and t.shape[1] != heads or t.shape[2] != width:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [rows][{heads or 'heads'}][{width}]")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
+    pitch, head_pitch, inner = t.stride()
+    if inner != 1:
+        raise ValueError(f"{name}: the values of a head must be contiguous")
+    return code, t.shape[0], pitch, head_pitch
+
+
+def _sequences_of(table, lengths, starts, rows, device):
+    """Checks the table [seqs][pages], lengths [seqs] and starts [seqs + 1] or None; returns what the library takes."""
+    i32 = _TORCH.int32
+    if table.dtype != i32 or table.dim() != 2 or table.get_device() != device:
+        raise ValueError(f"table: expected an int32 tensor [sequences][pages] on cuda:{device}, got {table.dtype} "
+                         f"{tuple(table.shape)} on {table.device}")
+    seqs, width = table.shape
+    pitch, inner = table.stride()
+    if inner != 1 and width > 1:
+        raise ValueError("table: the pages of a sequence must be contiguous")
+    p = _flat(lengths, "lengths", i32, (seqs,), device)
+    if starts is None:
+        if rows != seqs:
+            raise ValueError(f"{rows} rows for {seqs} sequences need starts")
+        return table.data_ptr(), pitch, width, p, None, seqs
+    return table.data_ptr(), pitch, width, p, _flat(starts, "starts", i32, (seqs + 1,), device), seqs
+
+
+def append_tokens(cache, k, v, table, lengths, starts=None, kept=False, stream=None):
+    """hatq_append_tokens: the newest tokens of every sequence into the cache.
+
+    k, v [rows][heads][width]: sequence b has rows starts[b] .. starts[b + 1] - 1
+    (starts int32 [sequences + 1]; None: one row each), its tokens up to
+    lengths[b] - 1 (int32 [sequences], the new ones counted). table int32
+    [sequences][pages]: token j lies in page table[b][j // cache.page]. All on the
+    device and read there only. kept: also return (k, v) as the cache holds them
+    now, in the inputs' type (rows that no sequence holds are not written)."""
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(k, stream)
+    if cache.device != device:
+        raise ValueError(f"the cache is on cuda:{cache.device}, k on cuda:{device}")
+    heads, width = cache.heads, cache.width
+    kind, rows, ldk, hk = _heads_of(k, "k", heads, width, device)
+    v_kind, v_rows, ldv, hv = _heads_of(v, "v", heads, width, device)
+    if v_kind != kind or v_rows != rows:
+        raise ValueError(f"k and v differ: {k.dtype} {tuple(k.shape)}, {v.dtype} {tuple(v.shape)}")
+    pt, ldt, pages, pl, ps, seqs = _sequences_of(table, lengths, starts, rows, device)
+    out, pk, pv = None, None, None
+    if kept:
+        both = _empty(k, (2, rows, heads, width), k.dtype, stream)
+        out = both.unbind(0)
+        pk = both.data_ptr()
+        pv = pk + both.element_size() * rows * heads * width
+    st = (_LIB or load()).hatq_append_tokens(cache.ref, k.data_ptr(), ldk, hk, v.data_ptr(), ldv, hv, kind, rows, pt, ldt,
+                                             pages, pl, ps, seqs, pk, pv, raw)
+    if st:
+        _check(st)
+    return out
+
+
+def attend_tokens(q, cache, table, lengths, starts=None, scale=None, out=None, stream=None):
+    """hatq_attend_tokens: causal softmax attention of q [rows][heads][width] (float16 or bfloat16) over the cache.
+
+    Rows, table, lengths and starts as append_tokens takes them: a row sees its own
+    token and those before it. The heads of q are a multiple of the cache's, those
+    of one cache head next to each other. scale: width ** -0.5 unless given."""
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(q, stream)
+    if cache.device != device:
+        raise ValueError(f"the cache is on cuda:{cache.device}, q on cuda:{device}")
+    kind, rows, ldq, hq = _heads_of(q, "q", 0, cache.width, device)
+    heads = q.shape[1]
+    pt, ldt, pages, pl, ps, seqs = _sequences_of(table, lengths, starts, rows, device)
+    if out is None:
+        out = _empty(q, q.shape, q.dtype, stream)
+        ldo, ho = heads * cache.width, cache.width
+    else:
+        if out.dtype != q.dtype or out.shape != q.shape:
+            raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {q.dtype} {tuple(q.shape)}")
+        _, _, ldo, ho = _heads_of(out, "out", heads, cache.width, device)
+    lib, size = _LIB or load(), ctypes.c_size_t()
+    st = lib.hatq_attend_workspace(cache.ref, heads, rows, seqs, 0 if starts is None else 1, pages, ctypes.byref(size))
+    if st:
+        _check(st)
+    scratch = _empty(q, (size.value,), torch.uint8, stream)
+    st = lib.hatq_attend_tokens(q.data_ptr(), kind, ldq, hq, heads, rows, cache.ref, pt, ldt, pages, pl, ps, seqs,
+                                cache.scale if scale is None else scale, out.data_ptr(), ldo, ho, scratch.data_ptr(),
+                                size.value, raw)
     if st:
         _check(st)
     return out
