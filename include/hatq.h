@@ -721,6 +721,52 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
                                const int32_t *lengths, const int32_t *starts, int seqs, float scale, void *out,
                                long long ldo, long long ho, void *workspace, size_t workspace_bytes, hatq_stream stream);
 
+/*
+ * Products with 4-bit weights that have one scale per group of inputs: the next
+ * step below hatq_linear's INT8 for what reads every weight for a few rows.
+ */
+typedef struct {
+    int n, k;             /* output channels (n <= 2^27), inputs (k <= 2^20) */
+    int group;            /* inputs that share a scale: a multiple of 32; the last group may be cut */
+    int reserved;
+    uint8_t *codes;       /* device, 16-byte aligned; hatq_linear4_sizes bytes, written by hatq_linear4_layout */
+    float *scales;        /* device, 16-byte aligned; likewise */
+    float *bias;          /* device [n] or NULL; the caller's */
+} hatq_linear4_weights;
+
+/* Bytes of hatq_linear4_weights.codes (half a byte a code, n padded to 16, k to 64) and .scales. */
+hatq_status hatq_linear4_sizes(int n, int k, int group, size_t *code_bytes, size_t *scale_bytes);
+
+/* Eq. symmetric_q with 4 bits on groups of a weight matrix's rows, in the Hadamard
+ * domain: t = H~_hb w (unnormalized, fp32, shortest distances first), and per row
+ * and group a = max|t|, codes = rint(7 t / a), scale = a / 7 / sqrt(hb); zeros get
+ * codes 0 and scale 1 / sqrt(hb), a group with 7 a not finite codes 0 and scale NaN.
+ *   w        device, hatq_type type, n rows of k <= 32768 values at a pitch of ldw
+ *   hb       a power of two <= 256 that divides k (1: no transform)
+ *   codes    device int8 [n] rows at a pitch of ldc; scales device float [n] rows of
+ *            ceil(k / group) at a pitch of lds. The three share no element */
+hatq_status hatq_quantize_groups(const void *w, int type, long long ldw, int n, int k, int hb, int group, int8_t *codes,
+                                 long long ldc, float *scales, long long lds, hatq_stream stream);
+
+/* Lays out codes w (device int8 [n] rows of k at a pitch of ldw; clamped to [-8, 7])
+ * and their scales (device float [n] rows of ceil(k / group) at a pitch of lds) into
+ * L->codes and L->scales. Stream-ordered. */
+hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *scales, long long lds,
+                                const hatq_linear4_weights *L, hatq_stream stream);
+
+/* y[r][n] = s_x[r] sum_g s[n][g] sum_{k in g} c[n][k] x[r][k] + bias[n]: products
+ * are exact, a group's sum is fp32 as the tensor cores add, everything else rounded
+ * fp32, then y_type once.
+ *   x        device, hatq_type x_type (16-bit x enter the products as they are, fp32
+ *            x as the exact sum of three bf16 numbers), pitch ldx >= k; codes of
+ *            hatq_quantize_tokens (F16 format, same hb as the weights) among them
+ *   s_x      device float [rows], or NULL: 1
+ *   y        device, hatq_type y_type, pitch ldy >= n; shares no element with x
+ *   rows     at most 2^20; the weights are read once for every 64 rows or fewer.
+ *            Made for few rows: hatq_linear is the faster from about 100 on */
+hatq_status hatq_linear4(const void *x, int x_type, long long ldx, const float *s_x, long long rows,
+                         const hatq_linear4_weights *L, int y_type, void *y, long long ldy, hatq_stream stream);
+
 /* Failure-detection self test (the paper has no counterpart): launches one
  * thread that waits, through the same bounded mbarrier wait the convolution
  * pipeline uses, on a barrier nothing arrives at. The wait expires after

@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "hatq_cache.h"
+#include "hatq_mma4.h"
 #include "hatq_tc.h"
 
 namespace hatq {
@@ -48,11 +49,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  "r"(bytes), "r"(bar)
                  : "memory");
 }
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -91,19 +87,6 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ float low_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x & 0xffff))); }
 __device__ __forceinline__ float high_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x >> 16))); }
-
-// The codes of a word at bits 0-3 (ODD: 4-7) of its halves, as A operands: bare, subnormal numbers (code + 8) 2^-24 and
-// 2^-20, or (WHOLE) the codes themselves: 1024 + x and 1024 + 16 x are fp16 numbers whose last bits are x.
-template <bool WHOLE, bool ODD>
-__device__ __forceinline__ uint32_t codes_of(uint32_t w) {
-    if constexpr (!WHOLE) return w & (ODD ? 0x00f000f0u : 0x000f000fu);
-    uint32_t x = (w & (ODD ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
-    if constexpr (ODD)
-        asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x) : "r"(0x2c002c00u), "r"(0xd480d480u));      // x / 16 - 72
-    else
-        asm("add.rn.f16x2 %0, %0, %1;" : "+r"(x) : "r"(0xe408e408u));                            // x - 1032
-    return x;
-}
 
 // The row of chunks: sequence after sequence, in it head after head, in it tile after tile of the columns.
 struct Sequence {
@@ -440,10 +423,10 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
 #pragma unroll
                 for (int x = 0; x < WORDS; ++x) {
                     const uint32_t u0 = w0[x] >> 8, u1 = w1[x] >> 8;
-                    const uint32_t A[4] = {codes_of<kTwo, false>(w0[x]), codes_of<kTwo, false>(w1[x]), codes_of<kTwo, true>(w0[x]),
-                                           codes_of<kTwo, true>(w1[x])};
-                    const uint32_t B[4] = {codes_of<kTwo, false>(u0), codes_of<kTwo, false>(u1), codes_of<kTwo, true>(u0),
-                                           codes_of<kTwo, true>(u1)};
+                    const uint32_t A[4] = {codes_f16<kTwo, false>(w0[x]), codes_f16<kTwo, false>(w1[x]), codes_f16<kTwo, true>(w0[x]),
+                                           codes_f16<kTwo, true>(w1[x])};
+                    const uint32_t B[4] = {codes_f16<kTwo, false>(u0), codes_f16<kTwo, false>(u1), codes_f16<kTwo, true>(u0),
+                                           codes_f16<kTwo, true>(u1)};
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -563,10 +546,10 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
                     const uint32_t n0 = __byte_perm(w[0][x], w[1][x], half ? 0x7632 : 0x5410);
                     const uint32_t n1 = __byte_perm(w[2][x], w[3][x], half ? 0x7632 : 0x5410);
                     const uint32_t u0 = n0 >> 8, u1 = n1 >> 8;
-                    const uint32_t A[4] = {codes_of<kTwo, false>(n0), codes_of<kTwo, true>(n0), codes_of<kTwo, false>(n1),
-                                           codes_of<kTwo, true>(n1)};
-                    const uint32_t B[4] = {codes_of<kTwo, false>(u0), codes_of<kTwo, true>(u0), codes_of<kTwo, false>(u1),
-                                           codes_of<kTwo, true>(u1)};
+                    const uint32_t A[4] = {codes_f16<kTwo, false>(n0), codes_f16<kTwo, true>(n0), codes_f16<kTwo, false>(n1),
+                                           codes_f16<kTwo, true>(n1)};
+                    const uint32_t B[4] = {codes_f16<kTwo, false>(u0), codes_f16<kTwo, true>(u0), codes_f16<kTwo, false>(u1),
+                                           codes_f16<kTwo, true>(u1)};
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

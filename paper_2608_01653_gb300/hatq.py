@@ -77,6 +77,11 @@ class TokenCacheStruct(ctypes.Structure):
                 ("width", ctypes.c_int), ("hb", ctypes.c_int), ("reserved", ctypes.c_int)]
 
 
+class Linear4WeightsStruct(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("k", ctypes.c_int), ("group", ctypes.c_int), ("reserved", ctypes.c_int),
+                ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -153,6 +158,10 @@ def load(build: bool = True) -> ctypes.CDLL:
                                            ctypes.POINTER(ctypes.c_size_t)]),
             "hatq_attend_tokens": (_I, [_P, _I, _L, _L, _I, _L, ctypes.POINTER(TokenCacheStruct), _P, _L, _I, _P, _P, _I,
                                         _F, _P, _L, _L, _P, ctypes.c_size_t, _P]),
+            "hatq_linear4_sizes": (_I, [_I, _I, _I, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]),
+            "hatq_quantize_groups": (_I, [_P, _I, _L, _I, _I, _I, _I, _P, _L, _P, _L, _P]),
+            "hatq_linear4_layout": (_I, [_P, _L, _P, _L, ctypes.POINTER(Linear4WeightsStruct), _P]),
+            "hatq_linear4": (_I, [_P, _I, _L, _P, _L, ctypes.POINTER(Linear4WeightsStruct), _I, _P, _L, _P]),
             "hatq_version": (_I, []),
         }
         for name, (res, args) in sig.items():
@@ -1187,6 +1196,101 @@ def attend_tokens(q, cache, table, lengths, starts=None, scale=None, out=None, s
     st = lib.hatq_attend_tokens(q.data_ptr(), kind, ldq, hq, heads, rows, cache.ref, pt, ldt, pages, pl, ps, seqs,
                                 cache.scale if scale is None else scale, out.data_ptr(), ldo, ho, scratch.data_ptr(),
                                 size.value, raw)
+    if st:
+        _check(st)
+    return out
+
+
+# ------------------------------------------------------------------ 4-bit weights
+
+class Linear4Weights:
+    """4-bit weights with one scale per group of inputs (hatq_linear4_weights): device buffers and the C struct."""
+
+    def __init__(self, n, k, group, codes, scales, bias):
+        self.n, self.k, self.group = n, k, group
+        self.codes, self.scales, self.bias = codes, scales, bias
+        self.device = codes.get_device()
+        self.struct = Linear4WeightsStruct(n, k, group, 0, codes.data_ptr(), scales.data_ptr(),
+                                           None if bias is None else bias.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+
+
+def quantize_groups(w, group=128, hb=1, stream=None):
+    """hatq_quantize_groups: (codes int8 [n][k] in -7 .. 7, scales [n][groups]) of a floating-point matrix [n][k]."""
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(w, stream)
+    kind, n, k, pitch = _rows_of(w, "w", _TOKEN_TYPES, device)
+    if pitch < k:
+        w, pitch = _apart(w, stream), k
+    groups = -(-k // group) if group > 0 else 0
+    codes, scales = _empty(w, (n, k), torch.int8, stream), _empty(w, (n, groups), torch.float32, stream)
+    _check((_LIB or load()).hatq_quantize_groups(w.data_ptr(), kind, pitch, n, k, hb, group, codes.data_ptr(), k,
+                                                 scales.data_ptr(), groups, raw))
+    return codes, scales
+
+
+def prepare_linear4(w, group=128, hb=1, scales=None, bias=None, stream=None) -> Linear4Weights:
+    """The weights of linear4 (w [n][k]), on the device.
+
+    w in float32 / float16 / bfloat16 (k <= 32768) is transformed along k in blocks
+    of hb and quantized to 4 bits with one scale per output channel and `group`
+    inputs (a multiple of 32; the last may be cut), as hatq_quantize_groups does;
+    x must be transformed with the same hb (quantize_tokens does). w in int8 (-8 .. 7)
+    is taken as it is, with `scales` [n][groups]. bias: [n], any floating type."""
+    torch = _token_torch()
+    _torch()
+    if w.dim() != 2:
+        raise ValueError(f"w: shape {tuple(w.shape)}, expected [n, k]")
+    n, k = w.shape
+    code_bytes, scale_bytes = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().hatq_linear4_sizes(n, k, group, ctypes.byref(code_bytes), ctypes.byref(scale_bytes)))
+    device, raw = _launch_stream(w, stream)
+    groups = -(-k // group)
+    with torch.cuda.stream(stream):                 # None: the current one
+        if w.dtype == torch.int8:
+            if scales is None or hb != 1:
+                raise ValueError("int8 weights need their scales, and are not transformed")
+            if tuple(scales.shape) != (n, groups):
+                raise ValueError(f"scales: shape {tuple(scales.shape)}, expected {(n, groups)}")
+            codes, scales = w.contiguous(), scales.to(device=w.device, dtype=torch.float32).contiguous()
+        else:
+            if scales is not None:
+                raise ValueError("scales belong to int8 weights")
+            codes, scales = quantize_groups(w, group, hb, stream)
+        if bias is not None:
+            if bias.numel() != n:
+                raise ValueError(f"bias: shape {tuple(bias.shape)}, expected {n} values")
+            bias = bias.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
+        L = Linear4Weights(n, k, group, torch.empty(code_bytes.value, dtype=torch.uint8, device=w.device),
+                           torch.empty(scale_bytes.value // 4, dtype=torch.float32, device=w.device), bias)
+        _check(load().hatq_linear4_layout(codes.data_ptr(), k, scales.data_ptr(), groups, L.ref, raw))
+    return L
+
+
+def linear4(x, layer, scales=None, dtype=None, out=None, stream=None):
+    """hatq_linear4: y [rows][n] of x [rows][k] (float32, float16, bfloat16), in `dtype` (by default x's) or into `out`.
+
+    scales: float32 [rows], a factor of each row: with x the "f16" codes of
+    quantize_tokens, their scales."""
+    torch = _TORCH or _token_torch()
+    device, raw = _launch_stream(x, stream)
+    x_kind, n, k, pitch = _rows_of(x, "x", _TOKEN_TYPES, device)
+    if k != layer.k:
+        raise ValueError(f"x: rows of {k} values, the weights take {layer.k}")
+    if pitch < k:
+        x, pitch = _apart(x, stream), k
+    if layer.device != device:
+        raise ValueError(f"the weights are on cuda:{layer.device}, x on cuda:{device}")
+    s_x = None if scales is None else _flat(scales, "scales", torch.float32, (n,), device)
+    if out is None:
+        dtype = dtype or x.dtype
+        kind, out_pitch = _TOKEN_TYPES.get(dtype), layer.n
+        if kind is None:
+            raise ValueError(f"dtype {dtype} is none of {[str(d) for d in _TOKEN_TYPES]}")
+        out = _empty(x, (n, out_pitch), dtype, stream)
+    else:
+        kind, out_pitch = _out_of(out, _TOKEN_TYPES, n, layer.n, device)
+    st = (_LIB or load()).hatq_linear4(x.data_ptr(), x_kind, pitch, s_x, n, layer.ref, kind, out.data_ptr(), out_pitch, raw)
     if st:
         _check(st)
     return out
