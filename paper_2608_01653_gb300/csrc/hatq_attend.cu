@@ -60,26 +60,29 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t at, uint32_t (&w)[N]) {
+__device__ __forceinline__ void load_words(const uint8_t *at, uint32_t (&w)[N]) {
     if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < N; i += 4)
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
-                         : "r"(at + 4 * i));
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(at + 4 * i);
+            w[i] = v.x;
+            w[i + 1] = v.y;
+            w[i + 2] = v.z;
+            w[i + 3] = v.w;
+        }
     } else if constexpr (N % 2 == 0) {
 #pragma unroll
-        for (int i = 0; i < N; i += 2)
-            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[i]), "=r"(w[i + 1]) : "r"(at + 4 * i));
+        for (int i = 0; i < N; i += 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(at + 4 * i);
+            w[i] = v.x;
+            w[i + 1] = v.y;
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i));
+        for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const uint32_t *>(at + 4 * i);
     }
 }
-__device__ __forceinline__ float load_float(uint32_t at) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
-    return v;
-}
+__device__ __forceinline__ float load_float(const uint8_t *at) { return *reinterpret_cast<const float *>(at); }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -116,50 +119,133 @@ __device__ __forceinline__ long long scan_add(long long v, int lane) {
     }
     return v;
 }
-
-// All units, or, where `unit` is one of them, the sequence that holds it. A whole warp calls this.
-template <int COLS>
-__device__ __forceinline__ long long find_unit(const CacheArgs &c, int group, int lane, long long unit, Sequence &found) {
-    long long units = 0, segments = 0;
-    int most = 0;                                            // of the offsets so far
-    for (int b0 = 0; b0 < c.seqs; b0 += 32) {
-        const int b = b0 + lane;
-        Sequence s{};
-        if (c.starts) {
-            int here = b < c.seqs ? c.starts[b] : 0, next = b < c.seqs ? c.starts[b + 1] : 0;
-            here = max(here, most);
+__device__ __forceinline__ int scan_max(int v) {
 #pragma unroll
-            for (int h = 1; h < 32; h *= 2) here = max(here, __shfl_up_sync(0xffffffffu, here, h));   // (lane < h: its own)
-            next = max(next, here);
-            if (b < c.seqs) measure<COLS>(c, group, s, b, here, next);
-            most = __shfl_sync(0xffffffffu, next, 31);
-        } else if (b < c.seqs) {
+    for (int h = 1; h < 32; h *= 2) v = max(v, __shfl_up_sync(0xffffffffu, v, h));     // (lane < h: its own)
+    return v;
+}
+// quotients are of numbers below 2^32 nearly always
+__device__ __forceinline__ long long divide(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// All sequences as one warp holds them: every lane a run of `per` of them, and what lies before it.
+template <int COLS>
+struct Row {
+    int per, most;                     // most: of the offsets before the lane's run
+    long long units, segments;         // before the lane's run
+    long long total;
+    Sequence own;                      // per == 1: the lane's sequence
+
+    // the sequence at place j of the lane's run
+    __device__ __forceinline__ void take(const CacheArgs &c, int group, Sequence &s, int b, int &most) const {
+        if (c.starts) {
+            const int here = max(c.starts[b], most), next = max(c.starts[b + 1], here);
+            measure<COLS>(c, group, s, b, here, next);
+            most = next;
+        } else {
             measure<COLS>(c, group, s, b, b, b + 1);
         }
-        const long long mine = s.units(c.heads), segs = s.segments(c.heads);
-        const long long up_to = scan_add(mine, lane);
-        if (unit >= 0) {
-            const bool here = unit < units + up_to;
-            const unsigned who = __ballot_sync(0xffffffffu, here);
-            if (who) {
-                const int from = __ffs(who) - 1;
-                const long long before = units + up_to - mine, before_segs = segments + scan_add(segs, lane) - segs;
-                found.b = __shfl_sync(0xffffffffu, s.b, from);
-                found.begin = __shfl_sync(0xffffffffu, s.begin, from);
-                found.m = __shfl_sync(0xffffffffu, s.m, from);
-                found.len = __shfl_sync(0xffffffffu, s.len, from);
-                found.tiles = __shfl_sync(0xffffffffu, s.tiles, from);
-                found.chunks = __shfl_sync(0xffffffffu, s.chunks, from);
-                found.unit = __shfl_sync(0xffffffffu, before, from);
-                found.segment = __shfl_sync(0xffffffffu, before_segs, from);
-                return 0;
-            }
-            segments += __shfl_sync(0xffffffffu, scan_add(segs, lane), 31);
-        }
-        units += __shfl_sync(0xffffffffu, up_to, 31);
     }
-    return units;
-}
+    __device__ __forceinline__ void read(const CacheArgs &c, int group, int lane) {
+        per = (c.seqs + 31) / 32;
+        const int from = min(lane * per, c.seqs), to = min(from + per, c.seqs);
+        most = 0;
+        if (c.starts) {
+            int mine = 0;
+            for (int b = from; b < to; ++b) mine = max(mine, c.starts[b]);
+            const int before = __shfl_up_sync(0xffffffffu, scan_max(mine), 1);
+            most = lane ? max(before, 0) : 0;
+        }
+        long long u = 0, sg = 0;
+        int m = most;
+        for (int b = from; b < to; ++b) {
+            Sequence s{};
+            take(c, group, s, b, m);
+            u += s.units(c.heads);
+            sg += s.segments(c.heads);
+            own = s;
+        }
+        const long long up_to = scan_add(u, lane);
+        units = up_to - u;
+        segments = scan_add(sg, lane) - sg;
+        total = __shfl_sync(0xffffffffu, up_to, 31);
+    }
+    __device__ __forceinline__ static void copy(Sequence &to, const Sequence &s, long long unit, long long segment, int from) {
+        to.b = __shfl_sync(0xffffffffu, s.b, from);
+        to.begin = __shfl_sync(0xffffffffu, s.begin, from);
+        to.m = __shfl_sync(0xffffffffu, s.m, from);
+        to.len = __shfl_sync(0xffffffffu, s.len, from);
+        to.tiles = __shfl_sync(0xffffffffu, s.tiles, from);
+        to.chunks = __shfl_sync(0xffffffffu, s.chunks, from);
+        to.unit = __shfl_sync(0xffffffffu, unit, from);
+        to.segment = __shfl_sync(0xffffffffu, segment, from);
+    }
+    // the sequence that holds a unit (0 <= unit < total)
+    __device__ __forceinline__ void find_unit(const CacheArgs &c, int group, int lane, long long unit, Sequence &found) const {
+        // the last lane whose run begins at or before it: those behind the last sequence begin at total
+        const int who = 31 - __clz(__ballot_sync(0xffffffffu, units <= unit));
+        if (per == 1) {
+            copy(found, own, units, segments, who);
+            return;
+        }
+        const int from = who * per, to = min(from + per, c.seqs);
+        int m = __shfl_sync(0xffffffffu, most, who);
+        long long u = __shfl_sync(0xffffffffu, units, who), sg = __shfl_sync(0xffffffffu, segments, who);
+        for (int b0 = from;; b0 += 32) {
+            const int b = b0 + lane;
+            Sequence s{};
+            if (c.starts) {
+                const int here = scan_max(max(b < to ? c.starts[b] : 0, m)), next = max(b < to ? c.starts[b + 1] : 0, here);
+                if (b < to) measure<COLS>(c, group, s, b, here, next);
+                m = __shfl_sync(0xffffffffu, next, 31);
+            } else if (b < to) {
+                measure<COLS>(c, group, s, b, b, b + 1);
+            }
+            const long long n = s.units(c.heads), up_to = u + scan_add(n, lane);
+            const long long segs = sg + scan_add(s.segments(c.heads), lane);
+            const unsigned here = __ballot_sync(0xffffffffu, unit < up_to);
+            if (here || b0 + 32 >= to) {
+                copy(found, s, up_to - n, segs - s.segments(c.heads), here ? __ffs(here) - 1 : 31);
+                return;
+            }
+            u = __shfl_sync(0xffffffffu, up_to, 31);
+            sg = __shfl_sync(0xffffffffu, segs, 31);
+        }
+    }
+    // what lies before sequence b, whose own sizes are s
+    __device__ __forceinline__ void before(const CacheArgs &c, int group, int lane, int b, long long &u, long long &sg) const {
+        const int who = b / per, from = who * per;
+        u = __shfl_sync(0xffffffffu, units, who);
+        sg = __shfl_sync(0xffffffffu, segments, who);
+        int m = __shfl_sync(0xffffffffu, most, who);
+        for (int b0 = from; b0 < b; b0 += 32) {
+            const int x = b0 + lane;
+            Sequence s{};
+            if (c.starts) {
+                const int here = scan_max(max(x < b ? c.starts[x] : 0, m)), next = max(x < b ? c.starts[x + 1] : 0, here);
+                if (x < b) measure<COLS>(c, group, s, x, here, next);
+                m = __shfl_sync(0xffffffffu, next, 31);
+            } else if (x < b) {
+                measure<COLS>(c, group, s, x, x, x + 1);
+            }
+            u += __shfl_sync(0xffffffffu, scan_add(s.units(c.heads), lane), 31);
+            sg += __shfl_sync(0xffffffffu, scan_add(s.segments(c.heads), lane), 31);
+        }
+    }
+};
+
+// Equal parts for the warps: of `active` ones in every CTA, as few as give every CTA a unit.
+struct Parts {
+    int active;
+    long long units;                   // of a worker
+    __device__ Parts(long long total, int ctas, int warps) {
+        const long long each = divide(total + ctas - 1, ctas);
+        active = each < warps ? (int)max(each, 1LL) : warps;
+        const long long workers = (long long)ctas * active;
+        units = max(divide(total + workers - 1, workers), 1LL);
+    }
+};
 
 // What a warp knows of a chunk between asking for it and working on it.
 struct alignas(16) Chunk {
@@ -196,16 +282,21 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
 
     // ---- this warp's part
-    Sequence seq{};
-    const long long total = find_unit<COLS>(c, a.group, lane, -1, seq);
-    const long long workers = (long long)gridDim.x * WARPS, worker = (long long)blockIdx.x * WARPS + warp;
-    const long long cta_from = blockIdx.x * WARPS * total / workers, cta_to = (blockIdx.x + 1LL) * WARPS * total / workers;
-    const long long from = worker * total / workers, to = (worker + 1) * total / workers;
+    Row<COLS> row;
+    row.read(c, a.group, lane);
+    const long long total = row.total;
+    const Parts parts(total, gridDim.x, WARPS);
+    const long long cta_from = min(blockIdx.x * (parts.active * parts.units), total);
+    const long long cta_to = min((blockIdx.x + 1LL) * (parts.active * parts.units), total);
+    const long long from = warp < parts.active ? min(cta_from + warp * parts.units, total) : cta_to, to = min(from + parts.units, cta_to);
     if (cta_from == cta_to) return;
-    find_unit<COLS>(c, a.group, lane, cta_from, seq);
-    const long long in_cta = (cta_from - seq.unit) / seq.chunks;
-    const bool joined = cta_to <= seq.unit + (in_cta + 1) * seq.chunks;      // the CTA's part lies in one segment
-    if (from < to && from >= seq.unit + seq.units(c.heads)) find_unit<COLS>(c, a.group, lane, from, seq);
+    Sequence seq{};
+    row.find_unit(c, a.group, lane, cta_from, seq);
+    const long long first_segment = divide(cta_from - seq.unit, seq.chunks);
+    const bool joined = cta_to <= seq.unit + (first_segment + 1) * seq.chunks;      // the CTA's part lies in one segment
+    const long long joined_place = cta_from == seq.unit + first_segment * seq.chunks ? seq.segment + first_segment
+                                                                                   : a.segments + blockIdx.x * (long long)WARPS;
+    if (from < to && from >= seq.unit + seq.units(c.heads)) row.find_unit(c, a.group, lane, from, seq);
     const int size = 1 << c.page_bits, pages_of_chunk = kChunk >> c.page_bits;
     const uint32_t record = (uint32_t)size * (D + 8);
 
@@ -213,8 +304,8 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     long long unit = from;                                   // the next one to ask for
     int segment = 0, chunk = 0, asked = 0;                   // segment within the sequence
     if (from < to) {
-        segment = (int)((from - seq.unit) / seq.chunks);
-        chunk = (int)((from - seq.unit) % seq.chunks);
+        segment = (int)divide(from - seq.unit, seq.chunks);
+        chunk = (int)(from - seq.unit - (long long)segment * seq.chunks);
     }
     int entry = -1, entries_from = -1;                       // 32 entries of the sequence's row of the table, one a lane
     auto ask = [&]() {
@@ -268,10 +359,11 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
         }
     };
     // Where the pieces go: one that begins its segment has the segment's place, any other (a worker has at most one, its
-    // first) the worker's.
+    // first) the warp's.
     long long piece = 0;
     if (from < to)
-        piece = from == seq.unit + (long long)segment * seq.chunks ? seq.segment + segment : a.segments + worker;
+        piece = from == seq.unit + (long long)segment * seq.chunks ? seq.segment + segment
+                    : a.segments + blockIdx.x * (long long)WARPS + warp;
     long long next_piece = from < to ? seq.segment + segment + 1 : 0;
     for (int i = 0; i < STAGES; ++i) ask();
 
@@ -297,17 +389,28 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float v[8][E];
+                // (columns in order: a token, and a head of its group)
+                int token = (k.tile * COLS + nt * 8) / a.group, h = k.tile * COLS + nt * 8 - token * a.group, live = 0;
 #pragma unroll
                 for (int col = 0; col < 8; ++col) {
-                    const int x = k.tile * COLS + nt * 8 + col, token = x / a.group, h = x - token * a.group;
                     const T *p = static_cast<const T *>(a.q) + (long long)(k.begin + token) * a.ldq +
                                  (long long)(k.head * a.group + h) * a.hq + lane;
-                    const bool live = token < k.m;
+                    if (token < k.m) live = col + 1;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) v[col][e] = live ? to_f32<T>(p[32 * e]) : 0.0f;
+                    for (int e = 0; e < E; ++e) v[col][e] = token < k.m ? to_f32<T>(p[32 * e]) : 0.0f;
+                    if (++h == a.group) {
+                        h = 0;
+                        ++token;
+                    }
                 }
 #pragma unroll
                 for (int col = 0; col < 8; ++col) {
+                    if (col >= live) {                       // zeros, which give logits of 0
+#pragma unroll
+                        for (int e = 0; e < E; ++e) q_smem[col * D + 32 * e + lane] = __float2half_rn(0.0f);
+                        if (lane == 0) factors[col] = factors[8 + col] = 0.0f;
+                        continue;
+                    }
 #pragma unroll
                     for (int h = 1; h < 32; h *= 2)
                         if (h < c.hb)
@@ -369,7 +472,7 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
 #pragma unroll
                     for (int j = 0; j < WORDS; ++j) {
                         uint32_t w[4];
-                        load_words<4>(smem_addr(q_smem + g * D + (t * WORDS + j) * 8), w);
+                        load_words<4>(reinterpret_cast<const uint8_t *>(q_smem + g * D + (t * WORDS + j) * 8), w);
                         qf[part][nt][2 * j][0] = w[0];
                         qf[part][nt][2 * j][1] = w[1];
                         qf[part][nt][2 * j + 1][0] = w[2];
@@ -396,78 +499,86 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
             rinv = 0x1p100f;
         }
 
-        // ---- S^T of the chunk's 64 keys
-        const uint32_t base = ring + stage * STAGE;
-        const int key0 = k.chunk * kChunk, left = min(k.len - key0, kChunk);
+        // ---- S^T of the chunk's 64 keys (what lies behind the last one is computed from whatever is there, and masked)
+        const uint8_t *base = mine + stage * STAGE;
+        const int key0 = k.chunk * kChunk;
         const bool whole = key0 + kChunk <= k.len - k.m + k.tile * COLS / a.group + 1 && k.pages == (1 << pages_of_chunk) - 1;
-        float s[NT][4][4], vs[4][2], most[NT][2], largest = 0.0f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) most[nt][0] = most[nt][1] = -1e30f;
+        float s[NT][4][4], vs[4][2], ks[4][2], most[NT][2], largest = 0.0f;
+        const uint8_t *rec[4];
+        int token[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int in_page = (16 * j) >> c.page_bits, token = (16 * j) & (size - 1);
-            const uint32_t rec = base + in_page * record, krow = rec + (token + near) * (D / 2);
-            if (16 * j < left) {
-                uint32_t w0[WORDS], w1[WORDS];
-                load_words<WORDS>(krow + t * (WORDS * 4), w0);
-                load_words<WORDS>(krow + 8 * (D / 2) + t * (WORDS * 4), w1);
-                const uint32_t sc = rec + size * D + 4 * (token + near);
-                float k0 = load_float(sc), k1 = load_float(sc + 32);
-                vs[j][0] = load_float(sc + 4 * size);
-                vs[j][1] = load_float(sc + 4 * size + 32);
+            rec[j] = base + ((16 * j) >> c.page_bits) * record;
+            token[j] = (16 * j) & (size - 1);
+            const uint8_t *sc = rec[j] + size * D + 4 * (token[j] + near);
+            ks[j][0] = load_float(sc);
+            ks[j][1] = load_float(sc + 32);
+            vs[j][0] = load_float(sc + 4 * size);
+            vs[j][1] = load_float(sc + 4 * size + 32);
+        }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    s[nt][j][0] = s[nt][j][2] = q_off[nt][0];
-                    s[nt][j][1] = s[nt][j][3] = q_off[nt][1];
-                }
-#pragma unroll
-                for (int x = 0; x < WORDS; ++x) {
-                    const uint32_t u0 = w0[x] >> 8, u1 = w1[x] >> 8;
-                    const uint32_t A[4] = {codes_f16<kTwo, false>(w0[x]), codes_f16<kTwo, false>(w1[x]), codes_f16<kTwo, true>(w0[x]),
-                                           codes_f16<kTwo, true>(w1[x])};
-                    const uint32_t B[4] = {codes_f16<kTwo, false>(u0), codes_f16<kTwo, false>(u1), codes_f16<kTwo, true>(u0),
-                                           codes_f16<kTwo, true>(u1)};
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int part = 0; part < PARTS; ++part) {
-                            mma(s[nt][j], A, qf[part][nt][2 * x][0], qf[part][nt][2 * x][1]);
-                            mma(s[nt][j], B, qf[part][nt][2 * x + 1][0], qf[part][nt][2 * x + 1][1]);
-                        }
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    s[nt][j][0] *= k0 * q_f[nt][0];
-                    s[nt][j][1] *= k0 * q_f[nt][1];
-                    s[nt][j][2] *= k1 * q_f[nt][0];
-                    s[nt][j][3] *= k1 * q_f[nt][1];
-                }
-                if (!whole) {
-                    const int key = key0 + 16 * j + near;
-                    const bool held = (k.pages >> in_page) & 1;
-                    const bool in0 = held && key < k.len, in1 = held && key + 8 < k.len;
-                    if (!in0) vs[j][0] = 0.0f;
-                    if (!in1) vs[j][1] = 0.0f;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            if (!in0 || key > lim[nt][y]) s[nt][j][y] = -INFINITY;
-                            if (!in1 || key + 8 > lim[nt][y]) s[nt][j][2 + y] = -INFINITY;
-                        }
-                }
-            } else {
-                vs[j][0] = vs[j][1] = 0.0f;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[nt][j][0] = s[nt][j][1] = s[nt][j][2] = s[nt][j][3] = -INFINITY;
-            }
-            largest = fmaxf(largest, fmaxf(vs[j][0], vs[j][1]));
+        for (int j = 0; j < 4; ++j) {
+            const uint8_t *krow = rec[j] + (token[j] + near) * (D / 2);
+            uint32_t w0[WORDS], w1[WORDS];
+            load_words<WORDS>(krow + t * (WORDS * 4), w0);
+            load_words<WORDS>(krow + 8 * (D / 2) + t * (WORDS * 4), w1);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                most[nt][0] = fmaxf(most[nt][0], fmaxf(s[nt][j][0], s[nt][j][2]));
-                most[nt][1] = fmaxf(most[nt][1], fmaxf(s[nt][j][1], s[nt][j][3]));
+                s[nt][j][0] = s[nt][j][2] = q_off[nt][0];
+                s[nt][j][1] = s[nt][j][3] = q_off[nt][1];
+            }
+#pragma unroll
+            for (int x = 0; x < WORDS; ++x) {
+                const uint32_t u0 = w0[x] >> 8, u1 = w1[x] >> 8;
+                const uint32_t A[4] = {codes_f16<kTwo, false>(w0[x]), codes_f16<kTwo, false>(w1[x]), codes_f16<kTwo, true>(w0[x]),
+                                       codes_f16<kTwo, true>(w1[x])};
+                const uint32_t B[4] = {codes_f16<kTwo, false>(u0), codes_f16<kTwo, false>(u1), codes_f16<kTwo, true>(u0),
+                                       codes_f16<kTwo, true>(u1)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        mma(s[nt][j], A, qf[part][nt][2 * x][0], qf[part][nt][2 * x][1]);
+                        mma(s[nt][j], B, qf[part][nt][2 * x + 1][0], qf[part][nt][2 * x + 1][1]);
+                    }
             }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                s[nt][j][0] *= ks[j][0] * q_f[nt][0];
+                s[nt][j][1] *= ks[j][0] * q_f[nt][1];
+                s[nt][j][2] *= ks[j][1] * q_f[nt][0];
+                s[nt][j][3] *= ks[j][1] * q_f[nt][1];
+            }
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = key0 + 16 * j + near;
+                const bool held = (k.pages >> ((16 * j) >> c.page_bits)) & 1;
+                const bool in0 = held && key < k.len, in1 = held && key + 8 < k.len;
+                if (!in0) vs[j][0] = 0.0f;
+                if (!in1) vs[j][1] = 0.0f;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        if (!in0 || key > lim[nt][y]) s[nt][j][y] = -INFINITY;
+                        if (!in1 || key + 8 > lim[nt][y]) s[nt][j][2 + y] = -INFINITY;
+                    }
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                most[nt][y] = -1e30f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most[nt][y] = fmaxf(most[nt][y], fmaxf(s[nt][j][y], s[nt][j][2 + y]));
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) largest = fmaxf(largest, fmaxf(vs[j][0], vs[j][1]));
 
         // ---- raise the maxima where a weight would leave the range
         bool raise = largest * rinv > 128.0f;
@@ -510,7 +621,6 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
         // ---- weights, and O^T
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (16 * j >= left) break;
             uint32_t pf[PARTS][NT][2];
             const float v0 = vs[j][0] * rinv, v1 = vs[j][1] * rinv;
 #pragma unroll
@@ -532,8 +642,7 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
                 }
                 if constexpr (!kTwo) mma(off[nt], ones, pf[0][nt][0], pf[0][nt][1]);
             }
-            const int in_page = (16 * j) >> c.page_bits, token = (16 * j) & (size - 1);
-            const uint32_t row = base + in_page * record + (size + token) * (D / 2) + g * (VW * 4);
+            const uint8_t *row = rec[j] + (size + token[j]) * (D / 2) + g * (VW * 4);
             uint32_t w[4][VW];
             load_words<VW>(row + t * (D / 2), w[0]);
             load_words<VW>(row + (7 - t) * (D / 2), w[1]);
@@ -607,11 +716,7 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     }
     __syncthreads();
     if (s_abort) return;
-    Sequence first{};
-    find_unit<COLS>(c, a.group, lane, cta_from, first);
-    const long long seg = (cta_from - first.unit) / first.chunks;
-    float *out = a.pieces + (cta_from == first.unit + seg * first.chunks ? first.segment + seg
-                                                                         : a.segments + blockIdx.x * (long long)WARPS) * piece_floats(D, COLS);
+    float *out = a.pieces + joined_place * piece_floats(D, COLS);
     for (int x = threadIdx.x; x < COLS * D; x += WARPS * 32) {
         const int col = x / D;
         float most = -1e30f;
@@ -648,40 +753,15 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas)
     const int r = (int)(blockIdx.x / c.heads), head = (int)(blockIdx.x % c.heads);
     int b, begin, end;
     if (!sequence_of(c, r, lane, b, begin, end)) return;
-    // units and segments of the sequences before, and all units
-    long long before = 0, total = 0, segs = 0;
-    int most = 0;
-    for (int b0 = 0; b0 < c.seqs; b0 += 32) {
-        const int x = b0 + lane;
-        Sequence s{};
-        if (c.starts) {
-            int here = x < c.seqs ? c.starts[x] : 0, next = x < c.seqs ? c.starts[x + 1] : 0;
-            here = max(here, most);
-#pragma unroll
-            for (int h = 1; h < 32; h *= 2) here = max(here, __shfl_up_sync(0xffffffffu, here, h));
-            next = max(next, here);
-            if (x < c.seqs) measure<COLS>(c, a.group, s, x, here, next);
-            most = __shfl_sync(0xffffffffu, next, 31);
-        } else if (x < c.seqs) {
-            measure<COLS>(c, a.group, s, x, x, x + 1);
-        }
-        const long long u = s.units(c.heads);
-        total += u;
-        if (x < b) {
-            before += u;
-            segs += s.segments(c.heads);
-        }
-    }
-#pragma unroll
-    for (int h = 1; h < 32; h *= 2) {
-        total += __shfl_xor_sync(0xffffffffu, total, h);
-        before += __shfl_xor_sync(0xffffffffu, before, h);
-        segs += __shfl_xor_sync(0xffffffffu, segs, h);
-    }
+    Row<COLS> row;
+    row.read(c, a.group, lane);
     Sequence s{};
     measure<COLS>(c, a.group, s, b, begin, end);
+    long long before, segs;
+    row.before(c, a.group, lane, b, before, segs);
+    const Parts parts(row.total, ctas, WARPS);
+    const long long cta_units = parts.active * parts.units;
     const int token = r - begin, ways = a.group >= 8 ? 1 : 8 / a.group;       // warps that share a head
-    const long long workers = (long long)ctas * WARPS;
     for (int h0 = 0; h0 < a.group; h0 += 8) {
         const int h = h0 + (ways > 1 ? warp % a.group : warp), way = ways > 1 ? warp / a.group : 0;
         const bool live = h < a.group && way < ways;
@@ -690,29 +770,49 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas)
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = 0.0f;
         if (live && s.chunks > 0) {
+            // The segment's pieces: those of its first CTA (one if that lies in the segment, else its warps'), one of each
+            // CTA between, those of its last.
             const long long seg = (long long)head * s.tiles + tile, u0 = before + seg * s.chunks, u1 = u0 + s.chunks;
-            long long at = u0;
-            for (int i = 0; at < u1; ++i) {
-                const long long w = ((at + 1) * workers - 1) / total;         // the worker that has unit `at`
-                const long long cta = w / WARPS, from = cta * WARPS * total / workers, to = (cta + 1) * WARPS * total / workers;
-                long long place, next;
-                if (from >= u0 && to <= u1) {
-                    place = from == u0 ? segs + seg : a.segments + cta * WARPS;
-                    next = to;
-                } else {
-                    place = at == u0 ? segs + seg : a.segments + w;
-                    next = (w + 1) * total / workers;
+            const long long c0 = divide(u0, cta_units), c1 = divide(u1 - 1, cta_units);
+            const long long from0 = c0 * cta_units, to0 = min(row.total, from0 + cta_units), from1 = c1 * cta_units;
+            const bool one0 = from0 == u0 && to0 <= u1, one1 = min(row.total, from1 + cta_units) <= u1;
+            const int w0 = (int)divide(u0 - from0, parts.units);
+            const int n0 = one0 ? 1 : (int)divide(min(u1, to0) - 1 - from0, parts.units) - w0 + 1;
+            const int n1 = c1 == c0 ? 0 : one1 ? 1 : (int)divide(u1 - 1 - from1, parts.units) + 1;
+            const int between = (int)max(c1 - c0 - 1, 0LL), n = n0 + between + n1;
+            // 32 pieces at a time: a lane each for their maxima, then all lanes along the head
+            for (int i0 = 0; i0 < n; i0 += 32 * ways) {
+                const int i = i0 + lane * ways + way;
+                long long place = 0;
+                if (i == 0) place = segs + seg;
+                else if (i < n0) place = a.segments + c0 * WARPS + w0 + i;
+                else if (i < n0 + between) place = a.segments + (c0 + 1 + i - n0) * WARPS;
+                else place = a.segments + c1 * WARPS + i - n0 - between;
+                float pm = -1e30f, pl = 0.0f;
+                if (i < n) {
+                    pm = a.pieces[place * piece_floats(D, COLS) + col];
+                    pl = a.pieces[place * piece_floats(D, COLS) + COLS + col];
                 }
-                at = next;
-                if (i % ways != way) continue;
-                const float *p = a.pieces + place * piece_floats(D, COLS);
-                const float pm = p[col], pl = p[COLS + col];
-                if (pl == 0.0f) continue;
-                const float now = fmaxf(mx, pm), by = exp2_fast(mx - now), add = exp2_fast(pm - now);
-                mx = now;
-                l = l * by + pl * add;
+                if (pl == 0.0f) pm = -1e30f;
+                float now = fmaxf(mx, pm);
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = o[e] * by + p[2 * COLS + col * D + 32 * e + lane] * add;
+                for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, d));
+                const float by = exp2_fast(mx - now), add = pl == 0.0f ? 0.0f : exp2_fast(pm - now);
+                mx = now;
+                float sum = pl * add;
+#pragma unroll
+                for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                l = l * by + sum;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] *= by;
+                const int here = min(32, (n - i0 - way + ways - 1) / ways);
+#pragma unroll 4
+                for (int y = 0; y < here; ++y) {
+                    const float f = __shfl_sync(0xffffffffu, add, y);
+                    const float *p = a.pieces + __shfl_sync(0xffffffffu, place, y) * piece_floats(D, COLS) + 2 * COLS + col * D + lane;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(f, p[32 * e], o[e]);
+                }
             }
         }
         if (ways > 1) {
@@ -789,7 +889,8 @@ cudaError_t launch_type(const AttendArgs &a, cudaStream_t s) {
 
 }  // namespace
 
-int attend_columns(int width, int group, bool one_each) { return width <= 128 && (group > 8 || !one_each) ? 16 : 8; }
+// 16 columns where most sequences have more than 8 (queries times heads of a group)
+int attend_columns(int width, int group, long long rows, int seqs) { return width <= 128 && rows * group > 8LL * seqs ? 16 : 8; }
 int attend_workers(int width, int sms) { return sms * kWarps(width); }
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s) {
     return type == HATQ_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);

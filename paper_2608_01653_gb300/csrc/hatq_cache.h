@@ -46,7 +46,7 @@ struct AttendArgs {
     int sms;
     int *err;
 };
-int attend_columns(int width, int group, bool one_each);
+int attend_columns(int width, int group, long long rows, int seqs);
 int attend_workers(int width, int sms);
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s);
 

@@ -98,7 +98,7 @@ hatq_status attend_args(const hatq_token_cache *c, int q_heads, long long rows, 
     if (rows * q_heads > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows x heads per call");
     a.q_heads = q_heads;
     a.group = q_heads / c->heads;
-    a.columns = hatq::attend_columns(c->width, a.group, !starts);
+    a.columns = hatq::attend_columns(c->width, a.group, rows, seqs);
     // tiles of columns: no more than whole tiles of all rows, and one cut tile a sequence
     a.segments = c->heads * (rows * a.group / a.columns + (seqs < rows ? seqs : rows));
     return HATQ_OK;
