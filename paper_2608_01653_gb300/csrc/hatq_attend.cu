@@ -36,12 +36,12 @@ using tc::smem_addr;
 // column tile) goes to a piece in memory, and a second kernel joins the pieces. Where a CTA's whole part lies in one
 // (sequence, head, tile) its warps are joined first.
 
-__host__ __device__ constexpr int kWarps(int d) { return d == 256 ? 6 : 8; }
-__host__ __device__ constexpr int kStages(int d) { return d == 64 ? 4 : d == 128 ? 3 : 2; }
+__host__ __device__ constexpr int kWarps(int d, int nt) { return d == 256 ? 6 : d == 192 || nt == 2 ? 8 : 12; }
+__host__ __device__ constexpr int kStages(int d, int nt) { return (d == 64 ? 3 : 2) + (d <= 128 && nt == 2); }
 __host__ __device__ constexpr int stage_bytes(int d) { return kChunk * (d + 8); }
 __host__ __device__ constexpr int piece_floats(int d, int cols) { return cols * (d + 2); }
-__host__ __device__ constexpr int warp_smem(int d) {       // ring, chunk descriptions, barriers, q, factors; in whole 128 bytes, as bulk copies take 16
-    return (kStages(d) * (stage_bytes(d) + 32 + 8) + 8 * d * 2 + 64 + 127) / 128 * 128;
+__host__ __device__ constexpr int warp_smem(int d, int nt) {   // ring, chunk descriptions, barriers; in whole 128 bytes, as bulk copies take 16
+    return (kStages(d, nt) * (stage_bytes(d) + 32 + 8) + 127) / 128 * 128;
 }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
@@ -111,7 +111,17 @@ __device__ __forceinline__ void measure(const CacheArgs &c, int group, Sequence 
     s.chunks = (s.len + kChunk - 1) / kChunk;
 }
 
-__device__ __forceinline__ long long scan_add(long long v, int lane) {
+// (small: the sum of all is below 2^31)
+__device__ __forceinline__ long long scan_add(long long v, int lane, bool small) {
+    if (small) {
+        int u = (int)v;
+#pragma unroll
+        for (int h = 1; h < 32; h *= 2) {
+            const int o = __shfl_up_sync(0xffffffffu, u, h);
+            if (lane >= h) u += o;
+        }
+        return u;
+    }
 #pragma unroll
     for (int h = 1; h < 32; h *= 2) {
         const long long o = __shfl_up_sync(0xffffffffu, v, h);
@@ -132,12 +142,16 @@ __device__ __forceinline__ long long divide(long long a, long long b) {
 // All sequences as one warp holds them: every lane a run of `per` of them, and what lies before it.
 template <int COLS>
 struct Row {
+    bool flat;                         // units are segments, those of sequences without tokens among them
     int per, most;                     // most: of the offsets before the lane's run
     long long units, segments;         // before the lane's run
     long long total;
     Sequence own;                      // per == 1: the lane's sequence
 
-    // the sequence at place j of the lane's run
+    __device__ __forceinline__ long long units_of(const Sequence &s, int heads) const {
+        return flat ? (long long)heads * s.tiles : s.units(heads);
+    }
+    // the next sequence of the lane's run
     __device__ __forceinline__ void take(const CacheArgs &c, int group, Sequence &s, int b, int &most) const {
         if (c.starts) {
             const int here = max(c.starts[b], most), next = max(c.starts[b + 1], here);
@@ -147,7 +161,8 @@ struct Row {
             measure<COLS>(c, group, s, b, b, b + 1);
         }
     }
-    __device__ __forceinline__ void read(const CacheArgs &c, int group, int lane) {
+    __device__ __forceinline__ void read(const CacheArgs &c, int group, int lane, bool flat_) {
+        flat = flat_;
         per = (c.seqs + 31) / 32;
         const int from = min(lane * per, c.seqs), to = min(from + per, c.seqs);
         most = 0;
@@ -162,13 +177,13 @@ struct Row {
         for (int b = from; b < to; ++b) {
             Sequence s{};
             take(c, group, s, b, m);
-            u += s.units(c.heads);
+            u += units_of(s, c.heads);
             sg += s.segments(c.heads);
             own = s;
         }
-        const long long up_to = scan_add(u, lane);
+        const long long up_to = scan_add(u, lane, c.small);
         units = up_to - u;
-        segments = scan_add(sg, lane) - sg;
+        segments = scan_add(sg, lane, c.small) - sg;
         total = __shfl_sync(0xffffffffu, up_to, 31);
     }
     __device__ __forceinline__ static void copy(Sequence &to, const Sequence &s, long long unit, long long segment, int from) {
@@ -202,8 +217,8 @@ struct Row {
             } else if (b < to) {
                 measure<COLS>(c, group, s, b, b, b + 1);
             }
-            const long long n = s.units(c.heads), up_to = u + scan_add(n, lane);
-            const long long segs = sg + scan_add(s.segments(c.heads), lane);
+            const long long n = units_of(s, c.heads), up_to = u + scan_add(n, lane, c.small);
+            const long long segs = sg + scan_add(s.segments(c.heads), lane, c.small);
             const unsigned here = __ballot_sync(0xffffffffu, unit < up_to);
             if (here || b0 + 32 >= to) {
                 copy(found, s, up_to - n, segs - s.segments(c.heads), here ? __ffs(here) - 1 : 31);
@@ -229,8 +244,8 @@ struct Row {
             } else if (x < b) {
                 measure<COLS>(c, group, s, x, x, x + 1);
             }
-            u += __shfl_sync(0xffffffffu, scan_add(s.units(c.heads), lane), 31);
-            sg += __shfl_sync(0xffffffffu, scan_add(s.segments(c.heads), lane), 31);
+            u += __shfl_sync(0xffffffffu, scan_add(s.units(c.heads), lane, c.small), 31);
+            sg += __shfl_sync(0xffffffffu, scan_add(s.segments(c.heads), lane, c.small), 31);
         }
     }
 };
@@ -256,9 +271,154 @@ struct alignas(16) Chunk {
 };
 static_assert(sizeof(Chunk) == 32, "two 16-byte loads");
 
+// A head's E values a lane (32 e + lane), transformed in place, unnormalized.
+template <int E>
+__device__ __forceinline__ void transform(float (&v)[E], int hb, int lane) {
+#pragma unroll
+    for (int h = 1; h < 32; h *= 2)
+        if (h < hb)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float other = __shfl_xor_sync(0xffffffffu, v[e], h);
+                v[e] = lane & h ? other - v[e] : v[e] + other;
+            }
+#pragma unroll
+    for (int h = 1; h < E; h *= 2)
+        if (32 * h < hb)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (!(e & h) && e + h < E) {
+                    const float x = v[e], y = v[e + h];
+                    v[e] = x + y;
+                    v[e + h] = x - y;
+                }
+}
+
+// 8 columns of queries from column x0 on as B operands of the steps over keys, qf[part][step][2]: transformed, brought
+// below 2^10 by a power of two per column, rounded to fp16 (part 0; part 1 is what that left). off: the accumulators' first
+// values, f: the factors of logits, both of columns 2 t and 2 t + 1.
+//
+// The transform is a product with a matrix of signs: exact operands, fp32 sums, all columns at once. Lane (g, t) reads the
+// values 32 J + 8 t .. + 7 of column g as they lie; step s of J has + 4 s .. 4 s + 3. Result rows may come in any order,
+// so that of tile (x, p) row r < 8 is value ((r / 2) WORDS + x) 8 + 2 p + 4 (r % 2) and row r + 8 the next one: transposed,
+// rows 2 t and 2 t + 1 are the pair that lane t multiplies with the codes at bits 0-3 (r + 8: 4-7) of its word x. A sign is
+// the parity of row & column & (hb - 1), zero where they are in different blocks; the two lowest bits of both make a
+// pattern of 4 words, the others flip it or clear it.
+template <int D, typename T, bool TWO, int PARTS, int STEPS>
+__device__ __forceinline__ void stage_queries(const AttendArgs &a, const Chunk &k, int x0, int lane, uint32_t (&qf)[PARTS][STEPS][2],
+                                              float (&off)[2], float (&f)[2]) {
+    constexpr int WORDS = D / 32;
+    constexpr uint32_t kOne = std::is_same<T, __half>::value ? 0x3c00u : 0x3f80u;
+    constexpr float kOdd = TWO ? 1.0f : 0.0625f, kUnit = TWO ? 1.0f : 0x1p24f;
+    const int g = lane >> 2, t = lane & 3, x = x0 + g, token = x / a.group, h = x - token * a.group;
+    uint32_t b[WORDS][4];
+    if (token < k.m) {
+        const T *p = static_cast<const T *>(a.q) + (long long)(k.begin + token) * a.ldq + (long long)(k.head * a.group + h) * a.hq + 8 * t;
+        if (a.vec) {
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p + 32 * j));
+                b[j][0] = v.x;
+                b[j][1] = v.y;
+                b[j][2] = v.z;
+                b[j][3] = v.w;
+            }
+        } else {
+            const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[j][i] = u[32 * j + 2 * i] | (uint32_t)u[32 * j + 2 * i + 1] << 16;
+        }
+    } else {                                                 // zeros, which give logits of 0
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) b[j][0] = b[j][1] = b[j][2] = b[j][3] = 0;
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __vmaxu2(most, b[j][i] & 0x7fff7fffu);
+    most = max(most & 0xffffu, most >> 16);
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    union { unsigned short u; T v; } m;
+    m.u = (unsigned short)most;
+    const uint32_t log_hb = 31 - __clz(a.c.hb), own = max(__float_as_uint(to_f32<T>(m.v)) >> 23, 10u);
+    float by[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        // a sum is below hb 2^(ex - 126); an infinity or a NaN makes the whole column NaN
+        const uint32_t ex = __shfl_sync(0xffffffffu, own, 8 * t + 4 * y);
+        by[y] = ex == 255u ? __int_as_float(0x7fffffff) : __uint_as_float((263u - log_hb - ex) << 23);
+        f[y] = a.scale * a.c.inv_norm * kUnit * __uint_as_float((min(ex, 254u) + log_hb - 9u) << 23);
+    }
+    // patterns of the lowest bits: rows 2 p and 2 p + 1, columns 0, 1 and 2, 3
+    const int low = (a.c.hb - 1) & 3, high = (a.c.hb - 1) >> 2;
+    uint32_t pattern[2][4];
+    auto sign = [&](int row, int col) { return ((row ^ col) & 3 & ~low) ? 0u : kOne ^ (uint32_t)(__popc(row & col & low) & 1) << 15; };
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pattern[p][i] = sign(2 * p + (i & 1), i & 2) | sign(2 * p + (i & 1), (i & 2) + 1) << 16;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        float c[2][4] = {};
+        const int row = (g >> 1) * (2 * WORDS) + 2 * w + (g & 1);
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int col = 8 * j + 2 * t + s;
+                const uint32_t keep = ((row ^ col) & ~high) ? 0u : 0xffffffffu, flip = (__popc(row & col & high) & 1) ? 0x80008000u : 0u;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    uint32_t A[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) A[i] = (pattern[p][i] ^ flip) & keep;
+                    if constexpr (std::is_same<T, __half>::value)
+                        mma(c[p], A, b[j][2 * s], b[j][2 * s + 1]);
+                    else
+                        mma_bf16(c[p], A, b[j][2 * s], b[j][2 * s + 1]);
+                }
+            }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {                    // values at odd places meet codes of 16-fold value
+                const float u = c[p][2 * o] * by[0] * (o ? kOdd : 1.0f), v = c[p][2 * o + 1] * by[1] * (o ? kOdd : 1.0f);
+                const uint32_t r = pack_half(u, v);
+                qf[0][2 * w + p][o] = transposed(r);
+                if constexpr (TWO) qf[1][2 * w + p][o] = transposed(pack_half(u - low_half(r), v - high_half(r)));
+            }
+    }
+    if constexpr (!TWO) {
+        // 8 * 2^-24 of every value, as the codes' offset meets them
+        const uint32_t A[4] = {0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u};
+        float c[4] = {};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) mma(c, A, qf[0][s][0], qf[0][s][1]);
+        sum[0] = -c[0];
+        sum[1] = -c[1];
+    }
+    off[0] = sum[0];
+    off[1] = sum[1];
+}
+
+// Writes a head of a row: o / l (zeros where no key was seen) transformed back.
+template <int D, typename T>
+__device__ __forceinline__ void finish(const AttendArgs &a, int r, int head, int lane, float (&o)[D / 32], float l) {
+    transform<D / 32>(o, a.c.hb, lane);
+    const float by = l == 0.0f ? 0.0f : a.c.inv_norm / l;
+    T *out = static_cast<T *>(a.out) + (long long)r * a.ldo + (long long)head * a.ho + lane;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) out[32 * e] = from_f32<T>(o[e] * by);
+}
+
 template <int D, typename T, int NT>
-__global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendArgs a) {
-    constexpr int COLS = 8 * NT, WARPS = kWarps(D), STAGES = kStages(D), STAGE = stage_bytes(D);
+__global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const AttendArgs a) {
+    constexpr int COLS = 8 * NT, WARPS = kWarps(D, NT), STAGES = kStages(D, NT), STAGE = stage_bytes(D);
     constexpr int WORDS = D / 32, VW = D / 64, STEPS = D / 16, E = D / 32;
     constexpr bool kTwo = std::is_same<T, __half>::value;      // q and p in two parts
     constexpr int PARTS = kTwo ? 2 : 1;
@@ -267,11 +427,9 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     __shared__ int s_abort;
     const CacheArgs &c = a.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    uint8_t *mine = smem + warp * warp_smem(D);
+    uint8_t *mine = smem + warp * warp_smem(D, NT);
     Chunk *chunks = reinterpret_cast<Chunk *>(mine + STAGES * STAGE);
-    __half *q_smem = reinterpret_cast<__half *>(mine + STAGES * (STAGE + 32));
-    float *factors = reinterpret_cast<float *>(mine + STAGES * (STAGE + 32) + 16 * D);      // 8 offsets, 8 factors
-    const uint32_t ring = smem_addr(mine), bars = smem_addr(mine + STAGES * (STAGE + 32) + 16 * D + 64);
+    const uint32_t ring = smem_addr(mine), bars = smem_addr(mine + STAGES * (STAGE + 32));
     volatile int *abort_flag = &s_abort;
 
     if (lane < STAGES) mbar_init(bars + 8 * lane, 1);
@@ -279,23 +437,41 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     if (threadIdx.x == 0) s_abort = 0;
     __syncthreads();
     after_prior_kernels();
-    if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
+    const int err = *reinterpret_cast<volatile int *>(a.err);
 
     // ---- this warp's part
     Row<COLS> row;
-    row.read(c, a.group, lane);
+    row.read(c, a.group, lane, a.direct);
     const long long total = row.total;
-    const Parts parts(total, gridDim.x, WARPS);
-    const long long cta_from = min(blockIdx.x * (parts.active * parts.units), total);
-    const long long cta_to = min((blockIdx.x + 1LL) * (parts.active * parts.units), total);
-    const long long from = warp < parts.active ? min(cta_from + warp * parts.units, total) : cta_to, to = min(from + parts.units, cta_to);
-    if (cta_from == cta_to) return;
+    long long cta_from, cta_to, from, to, joined_place = 0;
+    bool joined = true;                                      // the CTA's part lies in one segment
     Sequence seq{};
-    row.find_unit(c, a.group, lane, cta_from, seq);
-    const long long first_segment = divide(cta_from - seq.unit, seq.chunks);
-    const bool joined = cta_to <= seq.unit + (first_segment + 1) * seq.chunks;      // the CTA's part lies in one segment
-    const long long joined_place = cta_from == seq.unit + first_segment * seq.chunks ? seq.segment + first_segment
-                                                                                   : a.segments + blockIdx.x * (long long)WARPS;
+    if (a.direct) {
+        // a segment per CTA, all of it
+        if (blockIdx.x >= total) return;
+        row.find_unit(c, a.group, lane, blockIdx.x, seq);
+        const long long segment = blockIdx.x - seq.unit;
+        const int each = (seq.chunks + WARPS - 1) / WARPS;
+        seq.unit = -segment * seq.chunks;                    // units count from the segment's first
+        cta_from = 0;
+        cta_to = seq.chunks;
+        joined_place = segment;
+        from = min(warp * each, seq.chunks);
+        to = min(from + each, cta_to);
+    } else {
+        const Parts parts(total, gridDim.x, WARPS);
+        cta_from = min(blockIdx.x * (parts.active * parts.units), total);
+        cta_to = min((blockIdx.x + 1LL) * (parts.active * parts.units), total);
+        from = warp < parts.active ? min(cta_from + warp * parts.units, total) : cta_to;
+        to = min(from + parts.units, cta_to);
+        if (cta_from == cta_to) return;
+        row.find_unit(c, a.group, lane, cta_from, seq);
+        const long long segment = divide(cta_from - seq.unit, seq.chunks);
+        joined = cta_to <= seq.unit + (segment + 1) * seq.chunks;
+        joined_place = cta_from == seq.unit + segment * seq.chunks ? seq.segment + segment : a.segments + blockIdx.x * (long long)WARPS;
+    }
+    const Sequence first = seq;
+    if (err != 0) return;
     if (from < to && from >= seq.unit + seq.units(c.heads)) row.find_unit(c, a.group, lane, from, seq);
     const int size = 1 << c.page_bits, pages_of_chunk = kChunk >> c.page_bits;
     const uint32_t record = (uint32_t)size * (D + 8);
@@ -368,7 +544,7 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     for (int i = 0; i < STAGES; ++i) ask();
 
     float o[NT][STEPS][4], off[NT][4], m[NT][2], l[NT][2];
-    uint32_t qf[PARTS][NT][STEPS][2];
+    uint32_t qf[NT][PARTS][STEPS][2];
     float q_off[NT][2], q_f[NT][2];
     int lim[NT][2];
     float rinv = 0x1p100f;
@@ -388,107 +564,14 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
             // ---- a new segment: its queries, 8 columns at a time
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float v[8][E];
-                // (columns in order: a token, and a head of its group)
-                int token = (k.tile * COLS + nt * 8) / a.group, h = k.tile * COLS + nt * 8 - token * a.group, live = 0;
-#pragma unroll
-                for (int col = 0; col < 8; ++col) {
-                    const T *p = static_cast<const T *>(a.q) + (long long)(k.begin + token) * a.ldq +
-                                 (long long)(k.head * a.group + h) * a.hq + lane;
-                    if (token < k.m) live = col + 1;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[col][e] = token < k.m ? to_f32<T>(p[32 * e]) : 0.0f;
-                    if (++h == a.group) {
-                        h = 0;
-                        ++token;
-                    }
-                }
-#pragma unroll
-                for (int col = 0; col < 8; ++col) {
-                    if (col >= live) {                       // zeros, which give logits of 0
-#pragma unroll
-                        for (int e = 0; e < E; ++e) q_smem[col * D + 32 * e + lane] = __float2half_rn(0.0f);
-                        if (lane == 0) factors[col] = factors[8 + col] = 0.0f;
-                        continue;
-                    }
-#pragma unroll
-                    for (int h = 1; h < 32; h *= 2)
-                        if (h < c.hb)
-#pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                const float other = __shfl_xor_sync(0xffffffffu, v[col][e], h);
-                                v[col][e] = lane & h ? other - v[col][e] : v[col][e] + other;
-                            }
-#pragma unroll
-                    for (int h = 1; h < E; h *= 2)
-                        if (32 * h < c.hb)
-#pragma unroll
-                            for (int e = 0; e < E; ++e)
-                                if (!(e & h) && e + h < E) {
-                                    const float x = v[col][e], y = v[col][e + h];
-                                    v[col][e] = x + y;
-                                    v[col][e + h] = x - y;
-                                }
-                    unsigned bits = 0;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) bits = max(bits, __float_as_uint(v[col][e]) & 0x7fffffffu);
-                    bits = __reduce_max_sync(0xffffffffu, bits);
-                    // |q| below 2^10, by a power of two; an infinity or a NaN makes the whole column NaN
-                    const unsigned ex = max(bits >> 23, 10u);
-                    const float by = ex == 255u ? __int_as_float(0x7fffffff) : __uint_as_float((263u - ex) << 23);
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[col][e] *= by;
-                    // values at odd places meet codes of 16-fold value
-                    const float part = lane & 1 ? kOdd : 1.0f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const __half h = __float2half_rn(v[col][e] * part);
-                        q_smem[col * D + 32 * e + (lane & 24) + ((lane & 3) << 1) + ((lane >> 2) & 1)] = h;
-                        const float back = __half2float(h) * (lane & 1 ? 1.0f / kOdd : 1.0f);
-                        sum += back;
-                        v[col][e] -= back;
-                    }
-#pragma unroll
-                    for (int h = 1; h < 32; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
-                    if (lane == 0) {
-                        factors[col] = kTwo ? 0.0f : -0x1p-21f * sum;
-                        factors[8 + col] = a.scale * c.inv_norm * kUnit * __uint_as_float((min(ex, 254u) - 9u) << 23);
-                    }
-                }
-                __syncwarp();
-#pragma unroll
-                for (int part = 0; part < PARTS; ++part) {
-                    if (part) {
-                        __syncwarp();
-#pragma unroll
-                        for (int col = 0; col < 8; ++col)
-#pragma unroll
-                            for (int e = 0; e < E; ++e)
-                                q_smem[col * D + 32 * e + (lane & 24) + ((lane & 3) << 1) + ((lane >> 2) & 1)] =
-                                    __float2half_rn(v[col][e]);
-                        __syncwarp();
-                    }
-#pragma unroll
-                    for (int j = 0; j < WORDS; ++j) {
-                        uint32_t w[4];
-                        load_words<4>(reinterpret_cast<const uint8_t *>(q_smem + g * D + (t * WORDS + j) * 8), w);
-                        qf[part][nt][2 * j][0] = w[0];
-                        qf[part][nt][2 * j][1] = w[1];
-                        qf[part][nt][2 * j + 1][0] = w[2];
-                        qf[part][nt][2 * j + 1][1] = w[3];
-                    }
-                }
+                stage_queries<D, T, kTwo>(a, k, k.tile * COLS + nt * 8, lane, qf[nt], q_off[nt], q_f[nt]);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const int x = k.tile * COLS + nt * 8 + 2 * t + y, token = x / a.group;
-                    q_off[nt][y] = factors[2 * t + y];
-                    q_f[nt][y] = factors[8 + 2 * t + y];
                     lim[nt][y] = token < k.m ? k.len - k.m + token : -1;
                     m[nt][y] = -1e30f;
                     l[nt][y] = 0.0f;
                 }
-                __syncwarp();
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s)
 #pragma unroll
@@ -538,8 +621,8 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part) {
-                        mma(s[nt][j], A, qf[part][nt][2 * x][0], qf[part][nt][2 * x][1]);
-                        mma(s[nt][j], B, qf[part][nt][2 * x + 1][0], qf[part][nt][2 * x + 1][1]);
+                        mma(s[nt][j], A, qf[nt][part][2 * x][0], qf[nt][part][2 * x][1]);
+                        mma(s[nt][j], B, qf[nt][part][2 * x + 1][0], qf[nt][part][2 * x + 1][1]);
                     }
             }
         }
@@ -716,26 +799,40 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
     }
     __syncthreads();
     if (s_abort) return;
-    float *out = a.pieces + joined_place * piece_floats(D, COLS);
-    for (int x = threadIdx.x; x < COLS * D; x += WARPS * 32) {
-        const int col = x / D;
-        float most = -1e30f;
+    // a warp per column: a lane each for the warps' maxima, then all lanes along the head
+    const int head = (int)divide(joined_place, first.tiles), x0 = ((int)joined_place - head * first.tiles) * COLS;      // (direct)
+    for (int col = warp; col < COLS; col += WARPS) {
+        const int token = a.direct ? (x0 + col) / a.group : 0;
+        if (a.direct && token >= first.m) break;
+        const uint8_t *part = smem + min(lane, WARPS - 1) * warp_smem(D, NT) + 4 * col;
+        const float pm = load_float(part), pl = lane < WARPS ? load_float(part + 4 * COLS) : 0.0f;
+        float most = pl == 0.0f ? -1e30f : pm;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) most = fmaxf(most, reinterpret_cast<const float *>(smem + w * warp_smem(D))[col]);
-        float sum = 0.0f, o_sum = 0.0f;
+        for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const float by = pl == 0.0f ? 0.0f : exp2_fast(pm - most);
+        float sum = pl * by, v[E];
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 0.0f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const float *p = reinterpret_cast<const float *>(smem + w * warp_smem(D));
-            if (p[COLS + col] != 0.0f) {
-                const float by = exp2_fast(p[col] - most);
-                sum += by * p[COLS + col];
-                o_sum += by * p[2 * COLS + x];
-            }
+            const float f = __shfl_sync(0xffffffffu, by, w);
+            const uint8_t *p = smem + w * warp_smem(D, NT) + 4 * (2 * COLS + col * D + lane);
+            if (f != 0.0f)
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = fmaf(f, load_float(p + 128 * e), v[e]);
         }
-        out[2 * COLS + x] = o_sum;
-        if (x % D == 0) {
-            out[col] = most;
-            out[COLS + col] = sum;
+        if (a.direct) {
+            finish<D, T>(a, first.begin + token, head * a.group + x0 + col - token * a.group, lane, v, sum);
+        } else {
+            float *out = a.pieces + joined_place * piece_floats(D, COLS);
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[2 * COLS + col * D + 32 * e + lane] = v[e];
+            if (lane == 0) {
+                out[col] = most;
+                out[COLS + col] = sum;
+            }
         }
     }
 }
@@ -744,7 +841,7 @@ __global__ void __launch_bounds__(kWarps(D) * 32, 1) attend_kernel(const AttendA
 // one row and the heads of one kv head; where these are fewer than its warps, several warps share a head's pieces.
 template <int D, typename T, int NT>
 __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas) {
-    constexpr int COLS = 8 * NT, WARPS = kWarps(D), E = D / 32;
+    constexpr int COLS = 8 * NT, WARPS = kWarps(D, NT), E = D / 32;
     __shared__ float s_m[8], s_l[8], s_o[8][D];
     after_prior_kernels();
     if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
@@ -754,7 +851,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas)
     int b, begin, end;
     if (!sequence_of(c, r, lane, b, begin, end)) return;
     Row<COLS> row;
-    row.read(c, a.group, lane);
+    row.read(c, a.group, lane, false);
     Sequence s{};
     measure<COLS>(c, a.group, s, b, begin, end);
     long long before, segs;
@@ -837,38 +934,20 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas)
             __syncthreads();
         }
         if (!live || way) continue;
-        const float by = l == 0.0f ? 0.0f : c.inv_norm / l;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2)
-            if (d < c.hb)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float other = __shfl_xor_sync(0xffffffffu, o[e], d);
-                    o[e] = lane & d ? other - o[e] : o[e] + other;
-                }
-#pragma unroll
-        for (int d = 1; d < E; d *= 2)
-            if (32 * d < c.hb)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (!(e & d) && e + d < E) {
-                        const float x = o[e], y = o[e + d];
-                        o[e] = x + y;
-                        o[e + d] = x - y;
-                    }
-        T *out = static_cast<T *>(a.out) + (long long)r * a.ldo + (long long)(head * a.group + h) * a.ho + lane;
-#pragma unroll
-        for (int e = 0; e < E; ++e) out[32 * e] = from_f32<T>(o[e] * by);
+        finish<D, T>(a, r, head * a.group + h, lane, o, l);
     }
 }
 
 template <int D, typename T, int NT>
 cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
     static std::atomic<int> allowed[64];
-    const int bytes = kWarps(D) * warp_smem(D);
+    constexpr int bytes = kWarps(D, NT) * warp_smem(D, NT);
+    static_assert(bytes <= 227 * 1024 - 256, "shared memory of a CTA");
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(attend_kernel<D, T, NT>), bytes, allowed);
     if (e != cudaSuccess) return e;
-    if ((e = launch_early(attend_kernel<D, T, NT>, dim3((unsigned)a.sms), kWarps(D) * 32, bytes, s, a)) != cudaSuccess) return e;
+    if ((e = launch_early(attend_kernel<D, T, NT>, dim3((unsigned)(a.direct ? a.segments : a.sms)), kWarps(D, NT) * 32, bytes, s, a)) != cudaSuccess ||
+        a.direct)
+        return e;
     return launch_early(join_kernel<D, T, NT>, dim3((unsigned)((long long)a.c.rows * a.c.heads)), 256, 0, s, a, a.sms);
 }
 template <int D, typename T>
@@ -891,7 +970,11 @@ cudaError_t launch_type(const AttendArgs &a, cudaStream_t s) {
 
 // 16 columns where most sequences have more than 8 (queries times heads of a group)
 int attend_columns(int width, int group, long long rows, int seqs) { return width <= 128 && rows * group > 8LL * seqs ? 16 : 8; }
-int attend_workers(int width, int sms) { return sms * kWarps(width); }
+int attend_workers(int width, int sms) { return sms * kWarps(width, 1); }
+bool attend_direct(int width, long long segments, int capacity, int sms) {
+    const long long waves = (segments + sms - 1) / sms, chunks = (capacity + kChunk - 1) / kChunk, warps = kWarps(width, 1);
+    return segments < (1LL << 31) && waves * ((chunks + warps - 1) / warps) * 2 <= segments * chunks / (sms * warps) * 2 + 5;
+}
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s) {
     return type == HATQ_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);
 }

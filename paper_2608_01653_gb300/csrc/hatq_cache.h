@@ -21,6 +21,7 @@ struct CacheArgs {
     int seqs;
     const int32_t *lengths, *starts;
     int rows;
+    bool small;                        // all (sequence, head, tile, chunk) are fewer than 2^31
 };
 
 struct AppendArgs {
@@ -40,14 +41,19 @@ struct AttendArgs {
     long long ldo, ho;
     int q_heads, group;                // group = q_heads / heads
     int columns;                       // of a tile
+    bool vec;                          // rows of q lie on 16-byte boundaries
     float scale;                       // times log2(e): weights are powers of two
     float *pieces;
-    long long segments;                // upper bound
+    long long segments;                // (sequence, head, tile): upper bound
+    bool direct;
     int sms;
     int *err;
 };
 int attend_columns(int width, int group, long long rows, int seqs);
 int attend_workers(int width, int sms);
+// whether a CTA takes a whole segment and writes its outputs (rather than equal parts of all segments, which a second kernel
+// joins)
+bool attend_direct(int width, long long segments, int capacity, int sms);
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s);
 
 #ifdef __CUDACC__

@@ -101,10 +101,13 @@ hatq_status attend_args(const hatq_token_cache *c, int q_heads, long long rows, 
     a.columns = hatq::attend_columns(c->width, a.group, rows, seqs);
     // tiles of columns: no more than whole tiles of all rows, and one cut tile a sequence
     a.segments = c->heads * (rows * a.group / a.columns + (seqs < rows ? seqs : rows));
+    a.c.small = a.segments * ((a.c.capacity + hatq::kChunk - 1) / hatq::kChunk) < INT_MAX;
     return HATQ_OK;
 }
-size_t attend_bytes(const hatq::AttendArgs &a) {
-    return ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
+// once a.sms is set
+size_t attend_bytes(hatq::AttendArgs &a) {
+    a.direct = hatq::attend_direct(a.c.width, a.segments, a.c.capacity, a.sms);
+    return a.direct ? 0 : ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
 }
 
 }  // namespace
@@ -177,13 +180,15 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     if (overlap(in, to)) return fail(HATQ_ERR_INVALID_ARG, "q and out overlap");
     if (overlap(to, whole(cache))) return fail(HATQ_ERR_INVALID_ARG, "out and the cache overlap");
     if (!(a.sms = sm_count())) return fail(HATQ_ERR_CUDA, "no CUDA device");
-    if (!workspace || !aligned(workspace, 16)) return fail(HATQ_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
-    if (workspace_bytes < attend_bytes(a)) return fail(HATQ_ERR_INVALID_ARG, "the workspace is too small");
+    const size_t bytes = attend_bytes(a);
+    if (bytes && (!workspace || !aligned(workspace, 16))) return fail(HATQ_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
+    if (workspace_bytes < bytes) return fail(HATQ_ERR_INVALID_ARG, "the workspace is too small");
     a.err = hatq::device_error_word();
     if (!a.err) return fail(HATQ_ERR_CUDA, "no CUDA device");
     a.q = q;
     a.ldq = ldq;
     a.hq = hq;
+    a.vec = aligned(q, 16) && ldq % 8 == 0 && hq % 8 == 0;
     a.out = out;
     a.ldo = ldo;
     a.ho = ho;
