@@ -294,9 +294,8 @@ __device__ __forceinline__ void transform(float (&v)[E], int hb, int lane) {
                 }
 }
 
-// 8 columns of queries from column x0 on as B operands of the steps over keys, qf[part][step][2]: transformed, brought
-// below 2^10 by a power of two per column, rounded to fp16 (part 0; part 1 is what that left). off: the accumulators' first
-// values, f: the factors of logits, both of columns 2 t and 2 t + 1.
+// 8 columns of queries from column x0 on as B operands of the steps over keys: transformed, brought below 2^10 by a power
+// of two per column, rounded to fp16 (part 0; part 1 is what that left). f: the factors of logits of columns 2 t and 2 t + 1.
 //
 // The transform is a product with a matrix of signs: exact operands, fp32 sums, all columns at once. Lane (g, t) reads the
 // values 32 J + 8 t .. + 7 of column g as they lie; step s of J has + 4 s .. 4 s + 3. Result rows may come in any order,
@@ -304,68 +303,71 @@ __device__ __forceinline__ void transform(float (&v)[E], int hb, int lane) {
 // rows 2 t and 2 t + 1 are the pair that lane t multiplies with the codes at bits 0-3 (r + 8: 4-7) of its word x. A sign is
 // the parity of row & column & (hb - 1), zero where they are in different blocks; the two lowest bits of both make a
 // pattern of 4 words, the others flip it or clear it.
-template <int D, typename T, bool TWO, int PARTS, int STEPS>
-__device__ __forceinline__ void stage_queries(const AttendArgs &a, const Chunk &k, int x0, int lane, uint32_t (&qf)[PARTS][STEPS][2],
-                                              float (&off)[2], float (&f)[2]) {
-    constexpr int WORDS = D / 32;
-    constexpr uint32_t kOne = std::is_same<T, __half>::value ? 0x3c00u : 0x3f80u;
-    constexpr float kOdd = TWO ? 1.0f : 0.0625f, kUnit = TWO ? 1.0f : 0x1p24f;
-    const int g = lane >> 2, t = lane & 3, x = x0 + g, token = x / a.group, h = x - token * a.group;
-    uint32_t b[WORDS][4];
-    if (token < k.m) {
-        const T *p = static_cast<const T *>(a.q) + (long long)(k.begin + token) * a.ldq + (long long)(k.head * a.group + h) * a.hq + 8 * t;
-        if (a.vec) {
+template <int D, typename T, bool TWO>
+struct Queries {
+    static constexpr int WORDS = D / 32, PARTS = TWO ? 2 : 1;
+    static constexpr uint32_t kOne = std::is_same<T, __half>::value ? 0x3c00u : 0x3f80u;
+    static constexpr float kOdd = TWO ? 1.0f : 0.0625f, kUnit = TWO ? 1.0f : 0x1p24f;
+    uint32_t b[WORDS][4], pattern[2][4];
+    float by[2], f[2];
+
+    __device__ __forceinline__ void load(const AttendArgs &a, int begin, int m, int kv_head, int x0, int lane) {
+        const int g = lane >> 2, t = lane & 3, x = x0 + g, token = x / a.group, h = x - token * a.group;
+        if (token < m) {
+            const T *p = static_cast<const T *>(a.q) + (long long)(begin + token) * a.ldq + (long long)(kv_head * a.group + h) * a.hq + 8 * t;
+            if (a.vec) {
 #pragma unroll
-            for (int j = 0; j < WORDS; ++j) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p + 32 * j));
-                b[j][0] = v.x;
-                b[j][1] = v.y;
-                b[j][2] = v.z;
-                b[j][3] = v.w;
+                for (int j = 0; j < WORDS; ++j) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p + 32 * j));
+                    b[j][0] = v.x;
+                    b[j][1] = v.y;
+                    b[j][2] = v.z;
+                    b[j][3] = v.w;
+                }
+            } else {
+                const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+                for (int j = 0; j < WORDS; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[j][i] = u[32 * j + 2 * i] | (uint32_t)u[32 * j + 2 * i + 1] << 16;
             }
-        } else {
-            const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
+        } else {                                             // zeros, which give logits of 0
 #pragma unroll
-            for (int j = 0; j < WORDS; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[j][i] = u[32 * j + 2 * i] | (uint32_t)u[32 * j + 2 * i + 1] << 16;
+            for (int j = 0; j < WORDS; ++j) b[j][0] = b[j][1] = b[j][2] = b[j][3] = 0;
         }
-    } else {                                                 // zeros, which give logits of 0
-#pragma unroll
-        for (int j = 0; j < WORDS; ++j) b[j][0] = b[j][1] = b[j][2] = b[j][3] = 0;
     }
-    uint32_t most = 0;
+    __device__ __forceinline__ void measure(const AttendArgs &a, int lane) {
+        const int t = lane & 3;
+        uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < WORDS; ++j)
+        for (int j = 0; j < WORDS; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = __vmaxu2(most, b[j][i] & 0x7fff7fffu);
-    most = max(most & 0xffffu, most >> 16);
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    union { unsigned short u; T v; } m;
-    m.u = (unsigned short)most;
-    const uint32_t log_hb = 31 - __clz(a.c.hb), own = max(__float_as_uint(to_f32<T>(m.v)) >> 23, 10u);
-    float by[2];
+            for (int i = 0; i < 4; ++i) most = __vmaxu2(most, b[j][i] & 0x7fff7fffu);
+        most = max(most & 0xffffu, most >> 16);
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        union { unsigned short u; T v; } m;
+        m.u = (unsigned short)most;
+        const uint32_t log_hb = 31 - __clz(a.c.hb), own = max(__float_as_uint(to_f32<T>(m.v)) >> 23, 10u);
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        // a sum is below hb 2^(ex - 126); an infinity or a NaN makes the whole column NaN
-        const uint32_t ex = __shfl_sync(0xffffffffu, own, 8 * t + 4 * y);
-        by[y] = ex == 255u ? __int_as_float(0x7fffffff) : __uint_as_float((263u - log_hb - ex) << 23);
-        f[y] = a.scale * a.c.inv_norm * kUnit * __uint_as_float((min(ex, 254u) + log_hb - 9u) << 23);
+        for (int y = 0; y < 2; ++y) {
+            // a sum is below hb 2^(ex - 126); an infinity or a NaN makes the whole column NaN
+            const uint32_t ex = __shfl_sync(0xffffffffu, own, 8 * t + 4 * y);
+            by[y] = ex == 255u ? __int_as_float(0x7fffffff) : __uint_as_float((263u - log_hb - ex) << 23);
+            f[y] = a.scale * a.c.inv_norm * kUnit * __uint_as_float((min(ex, 254u) + log_hb - 9u) << 23);
+        }
+        // patterns of the lowest bits: rows 2 p and 2 p + 1, columns 0, 1 and 2, 3
+        const int low = (a.c.hb - 1) & 3;
+        auto sign = [&](int row, int col) { return ((row ^ col) & 3 & ~low) ? 0u : kOne ^ (uint32_t)(__popc(row & col & low) & 1) << 15; };
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pattern[p][i] = sign(2 * p + (i & 1), i & 2) | sign(2 * p + (i & 1), (i & 2) + 1) << 16;
     }
-    // patterns of the lowest bits: rows 2 p and 2 p + 1, columns 0, 1 and 2, 3
-    const int low = (a.c.hb - 1) & 3, high = (a.c.hb - 1) >> 2;
-    uint32_t pattern[2][4];
-    auto sign = [&](int row, int col) { return ((row ^ col) & 3 & ~low) ? 0u : kOne ^ (uint32_t)(__popc(row & col & low) & 1) << 15; };
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pattern[p][i] = sign(2 * p + (i & 1), i & 2) | sign(2 * p + (i & 1), (i & 2) + 1) << 16;
-    float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < WORDS; ++w) {
+    // the operands of steps 2 w and 2 w + 1: q[part][p][2]
+    __device__ __forceinline__ void tile(const AttendArgs &a, int w, int lane, uint32_t (&q)[PARTS][2][2]) const {
+        const int g = lane >> 2, t = lane & 3, high = (a.c.hb - 1) >> 2, row = (g >> 1) * (2 * WORDS) + 2 * w + (g & 1);
         float c[2][4] = {};
-        const int row = (g >> 1) * (2 * WORDS) + 2 * w + (g & 1);
 #pragma unroll
         for (int j = 0; j < WORDS; ++j)
 #pragma unroll
@@ -389,21 +391,20 @@ __device__ __forceinline__ void stage_queries(const AttendArgs &a, const Chunk &
             for (int o = 0; o < 2; ++o) {                    // values at odd places meet codes of 16-fold value
                 const float u = c[p][2 * o] * by[0] * (o ? kOdd : 1.0f), v = c[p][2 * o + 1] * by[1] * (o ? kOdd : 1.0f);
                 const uint32_t r = pack_half(u, v);
-                qf[0][2 * w + p][o] = transposed(r);
-                if constexpr (TWO) qf[1][2 * w + p][o] = transposed(pack_half(u - low_half(r), v - high_half(r)));
+                q[0][p][o] = transposed(r);
+                if constexpr (TWO) q[1][p][o] = transposed(pack_half(u - low_half(r), v - high_half(r)));
             }
     }
-    if constexpr (!TWO) {
-        // 8 * 2^-24 of every value, as the codes' offset meets them
-        const uint32_t A[4] = {0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u};
-        float c[4] = {};
+};
+// the accumulators' first values: 8 * 2^-24 of every value, as the codes' offset meets them
+template <int STEPS>
+__device__ __forceinline__ void offsets_of(const uint32_t (&qf)[STEPS][2], float (&off)[2]) {
+    const uint32_t A[4] = {0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u};
+    float c[4] = {};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) mma(c, A, qf[0][s][0], qf[0][s][1]);
-        sum[0] = -c[0];
-        sum[1] = -c[1];
-    }
-    off[0] = sum[0];
-    off[1] = sum[1];
+    for (int s = 0; s < STEPS; ++s) mma(c, A, qf[s][0], qf[s][1]);
+    off[0] = -c[0];
+    off[1] = -c[1];
 }
 
 // Writes a head of a row: o / l (zeros where no key was seen) transformed back.
@@ -444,18 +445,18 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
     row.read(c, a.group, lane, a.direct);
     const long long total = row.total;
     long long cta_from, cta_to, from, to, joined_place = 0;
-    bool joined = true;                                      // the CTA's part lies in one segment
+    bool joined = true;                                      // the CTA's part lies in one segment:
+    long long first_segment;                                 // this one of its sequence
     Sequence seq{};
     if (a.direct) {
         // a segment per CTA, all of it
         if (blockIdx.x >= total) return;
         row.find_unit(c, a.group, lane, blockIdx.x, seq);
-        const long long segment = blockIdx.x - seq.unit;
+        first_segment = blockIdx.x - seq.unit;
         const int each = (seq.chunks + WARPS - 1) / WARPS;
-        seq.unit = -segment * seq.chunks;                    // units count from the segment's first
+        seq.unit = -first_segment * seq.chunks;                    // units count from the segment's first
         cta_from = 0;
         cta_to = seq.chunks;
-        joined_place = segment;
         from = min(warp * each, seq.chunks);
         to = min(from + each, cta_to);
     } else {
@@ -466,9 +467,9 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
         to = min(from + parts.units, cta_to);
         if (cta_from == cta_to) return;
         row.find_unit(c, a.group, lane, cta_from, seq);
-        const long long segment = divide(cta_from - seq.unit, seq.chunks);
-        joined = cta_to <= seq.unit + (segment + 1) * seq.chunks;
-        joined_place = cta_from == seq.unit + segment * seq.chunks ? seq.segment + segment : a.segments + blockIdx.x * (long long)WARPS;
+        first_segment = divide(cta_from - seq.unit, seq.chunks);
+        joined = cta_to <= seq.unit + (first_segment + 1) * seq.chunks;
+        joined_place = cta_from == seq.unit + first_segment * seq.chunks ? seq.segment + first_segment : a.segments + blockIdx.x * (long long)WARPS;
     }
     const Sequence first = seq;
     if (err != 0) return;
@@ -513,6 +514,14 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
         __syncwarp();
         if (take)
             bulk_load(ring + stage * STAGE + lane * record, c.data + ((long long)page * c.heads + head) * record, record, bars + 8 * stage);
+        if (!joined && chunk == 0) {                         // a new segment: its queries on their way to L2
+            const int x = (segment - head * seq.tiles) * COLS + lane, at = x / a.group;
+            if (lane < COLS && at < seq.m) {
+                const T *p = static_cast<const T *>(a.q) + (long long)(seq.begin + at) * a.ldq + (long long)(head * a.group + x - at * a.group) * a.hq;
+#pragma unroll
+                for (int e = 0; e < D; e += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + e));
+            }
+        }
         ++asked;
         ++unit;
         if (++chunk == seq.chunks) {
@@ -541,7 +550,28 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
         piece = from == seq.unit + (long long)segment * seq.chunks ? seq.segment + segment
                     : a.segments + blockIdx.x * (long long)WARPS + warp;
     long long next_piece = from < to ? seq.segment + segment + 1 : 0;
+    // Where the CTA has one segment, its warps transform the queries together, a word of the codes each; the loads go out
+    // before those of keys, which would hold them up.
+    uint8_t *shared_q = smem + WARPS * warp_smem(D, NT);     // [tile of 8 columns][word][lane][part][2][2], then factors
+    constexpr int kQ = PARTS * 16, SHARERS = NT * WORDS;
+    Queries<D, T, kTwo> own;
+    const int first_head = (int)divide(first_segment, first.tiles), first_x = ((int)first_segment - first_head * first.tiles) * COLS;
+    if (joined && warp < SHARERS) own.load(a, first.begin, first.m, first_head, first_x + warp / WORDS * 8, lane);
     for (int i = 0; i < STAGES; ++i) ask();
+    if (joined) {
+        for (int x = warp; x < SHARERS; x += WARPS) {
+            if (x != warp) own.load(a, first.begin, first.m, first_head, first_x + x / WORDS * 8, lane);
+            own.measure(a, lane);
+            uint32_t q[PARTS][2][2];
+            own.tile(a, x % WORDS, lane, q);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part)
+                *reinterpret_cast<uint4 *>(shared_q + (x * 32 + lane) * kQ + 16 * part) = make_uint4(q[part][0][0], q[part][0][1], q[part][1][0], q[part][1][1]);
+            if (x % WORDS == 0 && lane < 4)
+                *reinterpret_cast<float2 *>(shared_q + SHARERS * 32 * kQ + 32 * (x / WORDS) + 8 * lane) = make_float2(own.f[0], own.f[1]);
+        }
+        __syncthreads();
+    }
 
     float o[NT][STEPS][4], off[NT][4], m[NT][2], l[NT][2];
     uint32_t qf[NT][PARTS][STEPS][2];
@@ -564,7 +594,41 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
             // ---- a new segment: its queries, 8 columns at a time
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                stage_queries<D, T, kTwo>(a, k, k.tile * COLS + nt * 8, lane, qf[nt], q_off[nt], q_f[nt]);
+                if (joined) {
+#pragma unroll
+                    for (int w = 0; w < WORDS; ++w)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) {
+                            const uint4 q = *reinterpret_cast<const uint4 *>(shared_q + ((nt * WORDS + w) * 32 + lane) * kQ + 16 * part);
+                            qf[nt][part][2 * w][0] = q.x;
+                            qf[nt][part][2 * w][1] = q.y;
+                            qf[nt][part][2 * w + 1][0] = q.z;
+                            qf[nt][part][2 * w + 1][1] = q.w;
+                        }
+                    const float2 f = *reinterpret_cast<const float2 *>(shared_q + SHARERS * 32 * kQ + 32 * nt + 8 * t);
+                    q_f[nt][0] = f.x;
+                    q_f[nt][1] = f.y;
+                } else {
+                    Queries<D, T, kTwo> own;
+                    own.load(a, k.begin, k.m, k.head, k.tile * COLS + nt * 8, lane);
+                    own.measure(a, lane);
+#pragma unroll
+                    for (int w = 0; w < WORDS; ++w) {
+                        uint32_t q[PARTS][2][2];
+                        own.tile(a, w, lane, q);
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                            for (int p = 0; p < 2; ++p) {
+                                qf[nt][part][2 * w + p][0] = q[part][p][0];
+                                qf[nt][part][2 * w + p][1] = q[part][p][1];
+                            }
+                    }
+                    q_f[nt][0] = own.f[0];
+                    q_f[nt][1] = own.f[1];
+                }
+                q_off[nt][0] = q_off[nt][1] = 0.0f;
+                if constexpr (!kTwo) offsets_of<STEPS>(qf[nt][0], q_off[nt]);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const int x = k.tile * COLS + nt * 8 + 2 * t + y, token = x / a.group;
@@ -800,9 +864,8 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
     __syncthreads();
     if (s_abort) return;
     // a warp per column: a lane each for the warps' maxima, then all lanes along the head
-    const int head = (int)divide(joined_place, first.tiles), x0 = ((int)joined_place - head * first.tiles) * COLS;      // (direct)
     for (int col = warp; col < COLS; col += WARPS) {
-        const int token = a.direct ? (x0 + col) / a.group : 0;
+        const int token = a.direct ? (first_x + col) / a.group : 0;
         if (a.direct && token >= first.m) break;
         const uint8_t *part = smem + min(lane, WARPS - 1) * warp_smem(D, NT) + 4 * col;
         const float pm = load_float(part), pl = lane < WARPS ? load_float(part + 4 * COLS) : 0.0f;
@@ -819,12 +882,14 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
         for (int w = 0; w < WARPS; ++w) {
             const float f = __shfl_sync(0xffffffffu, by, w);
             const uint8_t *p = smem + w * warp_smem(D, NT) + 4 * (2 * COLS + col * D + lane);
-            if (f != 0.0f)
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[e] = fmaf(f, load_float(p + 128 * e), v[e]);
+            for (int e = 0; e < E; ++e) {
+                const float x = load_float(p + 128 * e);     // (anything, where the warp had no keys)
+                v[e] = f == 0.0f ? v[e] : fmaf(f, x, v[e]);
+            }
         }
         if (a.direct) {
-            finish<D, T>(a, first.begin + token, head * a.group + x0 + col - token * a.group, lane, v, sum);
+            finish<D, T>(a, first.begin + token, first_head * a.group + first_x + col - token * a.group, lane, v, sum);
         } else {
             float *out = a.pieces + joined_place * piece_floats(D, COLS);
 #pragma unroll
@@ -837,17 +902,19 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
     }
 }
 
-// Joins the pieces of every row and head: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p, transformed back. A CTA has
-// one row and the heads of one kv head; where these are fewer than its warps, several warps share a head's pieces.
+// Joins the pieces of every row and head: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p, transformed back. A warp has
+// a row and a head, or `ways` warps next to each other share one's pieces.
 template <int D, typename T, int NT>
-__global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas) {
+__global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas, int ways) {
     constexpr int COLS = 8 * NT, WARPS = kWarps(D, NT), E = D / 32;
     __shared__ float s_m[8], s_l[8], s_o[8][D];
     after_prior_kernels();
     if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int r = (int)(blockIdx.x / c.heads), head = (int)(blockIdx.x % c.heads);
+    const int per_row = (a.q_heads * ways + 7) / 8;          // CTAs
+    const int r = (int)(blockIdx.x / per_row), way = warp % ways, q_head = (int)(blockIdx.x % per_row) * (8 / ways) + warp / ways;
+    const int head = q_head / a.group, h = q_head - head * a.group;
     int b, begin, end;
     if (!sequence_of(c, r, lane, b, begin, end)) return;
     Row<COLS> row;
@@ -858,97 +925,100 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas)
     row.before(c, a.group, lane, b, before, segs);
     const Parts parts(row.total, ctas, WARPS);
     const long long cta_units = parts.active * parts.units;
-    const int token = r - begin, ways = a.group >= 8 ? 1 : 8 / a.group;       // warps that share a head
-    for (int h0 = 0; h0 < a.group; h0 += 8) {
-        const int h = h0 + (ways > 1 ? warp % a.group : warp), way = ways > 1 ? warp / a.group : 0;
-        const bool live = h < a.group && way < ways;
-        const int x = token * a.group + h, tile = x / COLS, col = x % COLS;
-        float mx = -1e30f, l = 0.0f, o[E];
+    const int x = (r - begin) * a.group + h, tile = x / COLS, col = x % COLS;
+    float mx = -1e30f, l = 0.0f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    if (q_head < a.q_heads && s.chunks > 0) {
+        // The segment's pieces: those of its first CTA (one if that lies in the segment, else its warps'), one of each
+        // CTA between, those of its last.
+        const long long seg = (long long)head * s.tiles + tile, u0 = before + seg * s.chunks, u1 = u0 + s.chunks;
+        const long long c0 = divide(u0, cta_units), c1 = divide(u1 - 1, cta_units);
+        const long long from0 = c0 * cta_units, to0 = min(row.total, from0 + cta_units), from1 = c1 * cta_units;
+        const bool one0 = from0 == u0 && to0 <= u1, one1 = min(row.total, from1 + cta_units) <= u1;
+        const int w0 = (int)divide(u0 - from0, parts.units);
+        const int n0 = one0 ? 1 : (int)divide(min(u1, to0) - 1 - from0, parts.units) - w0 + 1;
+        const int n1 = c1 == c0 ? 0 : one1 ? 1 : (int)divide(u1 - 1 - from1, parts.units) + 1;
+        const int between = (int)max(c1 - c0 - 1, 0LL), n = n0 + between + n1;
+        // 32 pieces at a time: a lane each for their maxima, then all lanes along the head
+        for (int i0 = 0; i0 < n; i0 += 32 * ways) {
+            const int i = i0 + lane * ways + way;
+            long long place = 0;
+            if (i == 0) place = segs + seg;
+            else if (i < n0) place = a.segments + c0 * WARPS + w0 + i;
+            else if (i < n0 + between) place = a.segments + (c0 + 1 + i - n0) * WARPS;
+            else place = a.segments + c1 * WARPS + i - n0 - between;
+            float pm = -1e30f, pl = 0.0f;
+            if (i < n) {
+                pm = a.pieces[place * piece_floats(D, COLS) + col];
+                pl = a.pieces[place * piece_floats(D, COLS) + COLS + col];
+            }
+            if (pl == 0.0f) pm = -1e30f;
+            float now = fmaxf(mx, pm);
+#pragma unroll
+            for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, d));
+            const float by = exp2_fast(mx - now), add = pl == 0.0f ? 0.0f : exp2_fast(pm - now);
+            mx = now;
+            float sum = pl * add;
+#pragma unroll
+            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            l = l * by + sum;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= by;
+            const int here = min(32, (n - i0 - way + ways - 1) / ways);
+#pragma unroll 4
+            for (int y = 0; y < here; ++y) {
+                const float f = __shfl_sync(0xffffffffu, add, y);
+                const float *p = a.pieces + __shfl_sync(0xffffffffu, place, y) * piece_floats(D, COLS) + 2 * COLS + col * D + lane;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = fmaf(f, p[32 * e], o[e]);
+            }
+        }
+    }
+    if (ways > 1) {
+        if (lane == 0) {
+            s_m[warp] = mx;
+            s_l[warp] = l;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[warp][32 * e + lane] = o[e];
+        __syncthreads();
+        if (way) return;
+        const float pm = lane < ways ? s_m[warp + lane] : -1e30f, pl = lane < ways ? s_l[warp + lane] : 0.0f;
+        mx = pl == 0.0f ? -1e30f : pm;
+#pragma unroll
+        for (int d = 4; d; d /= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float by = pl == 0.0f ? 0.0f : exp2_fast(pm - mx);
+        l = pl * by;
+#pragma unroll
+        for (int d = 4; d; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+        l = __shfl_sync(0xffffffffu, l, 0);
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = 0.0f;
-        if (live && s.chunks > 0) {
-            // The segment's pieces: those of its first CTA (one if that lies in the segment, else its warps'), one of each
-            // CTA between, those of its last.
-            const long long seg = (long long)head * s.tiles + tile, u0 = before + seg * s.chunks, u1 = u0 + s.chunks;
-            const long long c0 = divide(u0, cta_units), c1 = divide(u1 - 1, cta_units);
-            const long long from0 = c0 * cta_units, to0 = min(row.total, from0 + cta_units), from1 = c1 * cta_units;
-            const bool one0 = from0 == u0 && to0 <= u1, one1 = min(row.total, from1 + cta_units) <= u1;
-            const int w0 = (int)divide(u0 - from0, parts.units);
-            const int n0 = one0 ? 1 : (int)divide(min(u1, to0) - 1 - from0, parts.units) - w0 + 1;
-            const int n1 = c1 == c0 ? 0 : one1 ? 1 : (int)divide(u1 - 1 - from1, parts.units) + 1;
-            const int between = (int)max(c1 - c0 - 1, 0LL), n = n0 + between + n1;
-            // 32 pieces at a time: a lane each for their maxima, then all lanes along the head
-            for (int i0 = 0; i0 < n; i0 += 32 * ways) {
-                const int i = i0 + lane * ways + way;
-                long long place = 0;
-                if (i == 0) place = segs + seg;
-                else if (i < n0) place = a.segments + c0 * WARPS + w0 + i;
-                else if (i < n0 + between) place = a.segments + (c0 + 1 + i - n0) * WARPS;
-                else place = a.segments + c1 * WARPS + i - n0 - between;
-                float pm = -1e30f, pl = 0.0f;
-                if (i < n) {
-                    pm = a.pieces[place * piece_floats(D, COLS) + col];
-                    pl = a.pieces[place * piece_floats(D, COLS) + COLS + col];
-                }
-                if (pl == 0.0f) pm = -1e30f;
-                float now = fmaxf(mx, pm);
+        for (int y = 0; y < ways; ++y) {
+            const float f = __shfl_sync(0xffffffffu, by, y);
 #pragma unroll
-                for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, d));
-                const float by = exp2_fast(mx - now), add = pl == 0.0f ? 0.0f : exp2_fast(pm - now);
-                mx = now;
-                float sum = pl * add;
-#pragma unroll
-                for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                l = l * by + sum;
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] *= by;
-                const int here = min(32, (n - i0 - way + ways - 1) / ways);
-#pragma unroll 4
-                for (int y = 0; y < here; ++y) {
-                    const float f = __shfl_sync(0xffffffffu, add, y);
-                    const float *p = a.pieces + __shfl_sync(0xffffffffu, place, y) * piece_floats(D, COLS) + 2 * COLS + col * D + lane;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = fmaf(f, p[32 * e], o[e]);
-                }
-            }
+            for (int e = 0; e < E; ++e) o[e] = fmaf(f, s_o[warp + y][32 * e + lane], o[e]);
         }
-        if (ways > 1) {
-            if (lane == 0) {
-                s_m[warp] = mx;
-                s_l[warp] = l;
-            }
-#pragma unroll
-            for (int e = 0; e < E; ++e) s_o[warp][32 * e + lane] = o[e];
-            __syncthreads();
-            if (live && way == 0)
-                for (int y = 1; y < ways; ++y) {
-                    const int other = warp + y * a.group;
-                    const float pm = s_m[other], pl = s_l[other];
-                    if (pl == 0.0f) continue;
-                    const float now = fmaxf(mx, pm), by = exp2_fast(mx - now), add = exp2_fast(pm - now);
-                    mx = now;
-                    l = l * by + pl * add;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = o[e] * by + s_o[other][32 * e + lane] * add;
-                }
-            __syncthreads();
-        }
-        if (!live || way) continue;
-        finish<D, T>(a, r, head * a.group + h, lane, o, l);
     }
+    if (q_head < a.q_heads) finish<D, T>(a, r, q_head, lane, o, l);
 }
 
 template <int D, typename T, int NT>
 cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
     static std::atomic<int> allowed[64];
-    constexpr int bytes = kWarps(D, NT) * warp_smem(D, NT);
+    constexpr int bytes = kWarps(D, NT) * warp_smem(D, NT) + NT * (D / 32) * 512 * (std::is_same<T, __half>::value ? 2 : 1) + 32 * NT;
     static_assert(bytes <= 227 * 1024 - 256, "shared memory of a CTA");
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(attend_kernel<D, T, NT>), bytes, allowed);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(attend_kernel<D, T, NT>, dim3((unsigned)(a.direct ? a.segments : a.sms)), kWarps(D, NT) * 32, bytes, s, a)) != cudaSuccess ||
         a.direct)
         return e;
-    return launch_early(join_kernel<D, T, NT>, dim3((unsigned)((long long)a.c.rows * a.c.heads)), 256, 0, s, a, a.sms);
+    // warps: no fewer than two for every SM's four schedulers
+    int ways = 1;
+    while (ways < 8 && (long long)a.c.rows * a.q_heads * ways < 8 * a.sms) ways *= 2;
+    const long long joiners = (long long)a.c.rows * ((a.q_heads * ways + 7) / 8);
+    return launch_early(join_kernel<D, T, NT>, dim3((unsigned)joiners), 256, 0, s, a, a.sms, ways);
 }
 template <int D, typename T>
 cudaError_t launch_columns(const AttendArgs &a, cudaStream_t s) {
