@@ -729,13 +729,14 @@ typedef struct {
     int n, k;             /* output channels (n <= 2^27), inputs (k <= 2^20) */
     int group;            /* inputs that share a scale: a multiple of 32; the last group may be cut */
     int reserved;
-    uint8_t *codes;       /* device, 16-byte aligned; hatq_linear4_sizes bytes, written by hatq_linear4_layout */
-    float *scales;        /* device, 16-byte aligned; likewise */
+    uint8_t *data;        /* device, 16-byte aligned; hatq_linear4_sizes bytes, written by hatq_linear4_layout */
     float *bias;          /* device [n] or NULL; the caller's */
 } hatq_linear4_weights;
 
-/* Bytes of hatq_linear4_weights.codes (half a byte a code, n padded to 16, k to 64) and .scales. */
-hatq_status hatq_linear4_sizes(int n, int k, int group, size_t *code_bytes, size_t *scale_bytes);
+/* Bytes of hatq_linear4_weights.data: half a byte a code, n padded to 16 and k to 64
+ * (128 where group is a multiple of it), and a float32 scale per channel and group
+ * (of more than 128 inputs: per 128; of a multiple of 32 only: per 32). */
+hatq_status hatq_linear4_sizes(int n, int k, int group, size_t *bytes);
 
 /* Eq. symmetric_q with 4 bits on groups of a weight matrix's rows, in the Hadamard
  * domain: t = H~_hb w (unnormalized, fp32, shortest distances first), and per row
@@ -750,7 +751,7 @@ hatq_status hatq_quantize_groups(const void *w, int type, long long ldw, int n, 
 
 /* Lays out codes w (device int8 [n] rows of k at a pitch of ldw; clamped to [-8, 7])
  * and their scales (device float [n] rows of ceil(k / group) at a pitch of lds) into
- * L->codes and L->scales. Stream-ordered. */
+ * L->data. Stream-ordered. */
 hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *scales, long long lds,
                                 const hatq_linear4_weights *L, hatq_stream stream);
 
@@ -763,7 +764,8 @@ hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *sca
  *   s_x      device float [rows], or NULL: 1
  *   y        device, hatq_type y_type, pitch ldy >= n; shares no element with x
  *   rows     at most 2^20; the weights are read once for every 64 rows or fewer.
- *            Made for few rows: hatq_linear is the faster from about 100 on */
+ *            Made for few rows: hatq_linear is the faster from about 100 on
+ * Stream-ordered; an expired device wait surfaces through hatq_sync_status(). */
 hatq_status hatq_linear4(const void *x, int x_type, long long ldx, const float *s_x, long long rows,
                          const hatq_linear4_weights *L, int y_type, void *y, long long ldy, hatq_stream stream);
 

@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const Att
         joined_place = cta_from == seq.unit + first_segment * seq.chunks ? seq.segment + first_segment : a.segments + blockIdx.x * (long long)WARPS;
     }
     const Sequence first = seq;
-    if (err != 0) return;
+    if (__syncthreads_or(err != 0)) return;
     if (from < to && from >= seq.unit + seq.units(c.heads)) row.find_unit(c, a.group, lane, from, seq);
     const int size = 1 << c.page_bits, pages_of_chunk = kChunk >> c.page_bits;
     const uint32_t record = (uint32_t)size * (D + 8);
@@ -909,7 +909,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
     constexpr int COLS = 8 * NT, WARPS = kWarps(D, NT), E = D / 32;
     __shared__ float s_m[8], s_l[8], s_o[8][D];
     after_prior_kernels();
-    if (*reinterpret_cast<volatile int *>(a.err) != 0) return;
+    if (__syncthreads_or(*reinterpret_cast<volatile int *>(a.err) != 0)) return;
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_row = (a.q_heads * ways + 7) / 8;          // CTAs

@@ -4,6 +4,7 @@
 
 #include "hatq_linear4.h"
 #include "hatq_mma4.h"
+#include "hatq_tc.h"
 
 namespace hatq {
 namespace {
@@ -14,58 +15,21 @@ namespace {
 // both 16-bit types, so 16-bit x go in as they are and fp32 x as the sum of three bf16 numbers, which is exact. A
 // group's sum is scaled in fp32 and added to the total.
 //
-// Memory-bound by the weights for few rows. Every lane reads its codes of 16 channels x 64 inputs as 16 bytes, whole
-// lines in order; the CTA's warps take every so many of these blocks, and their sums are added in shared memory.
-// x is read as it lies, 16 bytes a lane and 32 inputs (the order of inputs within a step is free: lane t of four has
-// inputs 8 t .. 8 t + 7 of each 32, the first four in the first step).
+// Layout: strips of 16 channels, in each units of 128 inputs (64 where a group is no multiple of 128) one after the
+// other: 16 bytes of codes a lane and 64 inputs, then the unit's 16 or 2 x 16 scales, so that one bulk copy brings in a
+// warp's next units whole. The order of inputs within a step is free: lane t of four has inputs 8 t .. 8 t + 7 of each
+// 32, the first four in the first step, so that x is read 16 bytes a lane from rows as they lie.
+//
+// Two kernels. A few rows (linear4_few): memory-bound by the weights. x lies in shared memory whole; a CTA's warps share
+// the inputs of a strip, each with its own ring of bulk copies that runs on from strip to strip, and add up at the
+// strip's end. More rows, or x too large for that (linear4_many): a strip a warp, x streamed through shared memory for
+// all of a CTA's strips; CTAs of a cluster share the inputs where there are few strips.
 
 constexpr int kCtaWarps = 8;
+constexpr int kStageBytes = 2560;      // of a warp's ring: two units of 128 (1088 bytes each), four of 64 (576 or 640)
+constexpr int kFewStages = 3;
 
 template <typename T> constexpr int kParts = std::is_same<T, float>::value ? 3 : 1;
-
-// 8 inputs of a row as B operands of two steps: b[part][step][2]
-template <typename T>
-__device__ __forceinline__ void load_x(const Linear4Args &a, const T *row, bool live, int k, uint32_t (&b)[kParts<T>][2][2]) {
-    if constexpr (std::is_same<T, float>::value) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        if (live && a.vec && k + 8 <= a.k) {
-            const float4 x = __ldg(reinterpret_cast<const float4 *>(row + k)), y = __ldg(reinterpret_cast<const float4 *>(row + k) + 1);
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-            v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-        } else if (live) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < a.k) v[i] = row[k + i];
-        }
-        // the upper 16 bits are a bf16 number, and what is left has 16, then 8 bits; nothing is left of an infinity
-#pragma unroll
-        for (int part = 0; part < 3; ++part)
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const uint32_t x = __float_as_uint(v[i]), y = __float_as_uint(v[i + 1]);
-                b[part][i / 4][i / 2 % 2] = __byte_perm(x, y, 0x7632);
-                v[i] = (x & 0x7f800000u) == 0x7f800000u ? 0.0f : v[i] - __uint_as_float(x & 0xffff0000u);
-                v[i + 1] = (y & 0x7f800000u) == 0x7f800000u ? 0.0f : v[i + 1] - __uint_as_float(y & 0xffff0000u);
-            }
-    } else {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (live && a.vec && k + 8 <= a.k) {
-            x = __ldg(reinterpret_cast<const uint4 *>(row + k));
-        } else if (live) {
-            const unsigned short *p = reinterpret_cast<const unsigned short *>(row) + k;
-            unsigned short v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < a.k ? p[i] : 0;
-            x = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-        }
-        b[0][0][0] = x.x;
-        b[0][0][1] = x.y;
-        b[0][1][0] = x.z;
-        b[0][1][1] = x.w;
-    }
-}
 
 // a word's codes as the A operand of a step
 template <typename T>
@@ -82,152 +46,411 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t (&A)[4]) {
     }
 }
 
-// NT tiles of 8 rows, MS strips a warp. `ways` warps of the CTA share a strip's inputs.
-template <typename T, typename Y, int NT, int MS>
-__global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_kernel(const Linear4Args a, int ways) {
-    constexpr int ROWS = 8 * NT, C = kStrip * MS;
-    extern __shared__ float sums[];                          // [warp][row][channel + 4]
-    after_prior_kernels();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int sets = kCtaWarps / ways, way = warp % ways;
-    const int blocks = (a.k + kStep - 1) / kStep, strips = (a.n + kStrip - 1) / kStrip;
-    const int strip0 = (blockIdx.x * sets + warp / ways) * MS, row0 = blockIdx.y * ROWS;
-
-    float total[MS][NT][4];
+// 8 inputs of a row in 16-bit parts: the upper 16 bits of a fp32 number are a bf16 number, and what is left has 16, then
+// 8 bits; nothing is left of an infinity
+template <typename T>
+__device__ __forceinline__ void load8(const Linear4Args &a, const T *row, bool live, int k, uint4 (&out)[kParts<T>]) {
+    if constexpr (std::is_same<T, float>::value) {
+        float v[8];
 #pragma unroll
-    for (int m = 0; m < MS; ++m)
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (live && a.vec && k + 8 <= a.k) {
+            const float4 x = __ldg(reinterpret_cast<const float4 *>(row + k)), y = __ldg(reinterpret_cast<const float4 *>(row + k) + 1);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else if (live) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int i = 0; i < 8; ++i)
+                if (k + i < a.k) v[i] = row[k + i];
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) total[m][nt][i] = 0.0f;
-    const uint4 *w[MS];
-    const float *scales[MS];
+        for (int part = 0; part < 3; ++part) {
+            uint32_t w[4];
 #pragma unroll
-    for (int m = 0; m < MS; ++m) {
-        const int strip = min(strip0 + m, strips - 1);       // (what lies behind the last is computed twice and not written)
-        w[m] = reinterpret_cast<const uint4 *>(a.w) + (long long)strip * blocks * 32 + lane;
-        scales[m] = a.scales + (long long)strip * a.groups * kStrip + g;
+            for (int i = 0; i < 8; i += 2) {
+                const uint32_t x = __float_as_uint(v[i]), y = __float_as_uint(v[i + 1]);
+                w[i / 2] = __byte_perm(x, y, 0x7632);
+                v[i] = (x & 0x7f800000u) == 0x7f800000u ? 0.0f : v[i] - __uint_as_float(x & 0xffff0000u);
+                v[i + 1] = (y & 0x7f800000u) == 0x7f800000u ? 0.0f : v[i + 1] - __uint_as_float(y & 0xffff0000u);
+            }
+            out[part] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    } else {
+        out[0] = make_uint4(0, 0, 0, 0);
+        if (live && a.vec && k + 8 <= a.k) {
+            out[0] = __ldg(reinterpret_cast<const uint4 *>(row + k));
+        } else if (live) {
+            const unsigned short *p = reinterpret_cast<const unsigned short *>(row) + k;
+            unsigned short v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < a.k ? p[i] : 0;
+            out[0] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+        }
     }
-    const T *x[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) x[nt] = static_cast<const T *>(a.x) + (long long)min(row0 + 8 * nt + g, a.rows - 1) * a.ldx;
-    const bool fine = a.group % kStep != 0;                  // a block holds two groups
+}
 
-    uint4 next[MS];
-    if (way < blocks)
-#pragma unroll
-        for (int m = 0; m < MS; ++m) next[m] = __ldcs(w[m] + (long long)way * 32);
-    for (int block = way; block < blocks; block += ways) {
-        uint4 now[MS];
-#pragma unroll
-        for (int m = 0; m < MS; ++m) now[m] = next[m];
-        if (block + ways < blocks)
-#pragma unroll
-            for (int m = 0; m < MS; ++m) next[m] = __ldcs(w[m] + (long long)(block + ways) * 32);
-        float sum[MS][NT][4];
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+// 16 bytes, the first `bytes` of them from src (16-byte aligned, unless bytes is 0), zeros behind
+__device__ __forceinline__ void async_copy(uint32_t dst, const void *src, int bytes) {
+    const void *from = bytes ? src : reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15);
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void store_y(const Linear4Args &a, int row, int n, float v) {
+    if (a.s_x) v *= __ldg(a.s_x + row);
+    if (a.bias) v += __ldg(a.bias + n);
+    const long long at = (long long)row * a.ldy + n;
+    if (a.y_type == HATQ_F32) static_cast<float *>(a.y)[at] = v;
+    else if (a.y_type == HATQ_F16) static_cast<__half *>(a.y)[at] = from_f32<__half>(v);
+    else static_cast<__nv_bfloat16 *>(a.y)[at] = from_f32<__nv_bfloat16>(v);
+}
+
+// A unit's products with NT tiles of 8 rows, added to the totals. x: lane (g, t)'s row g of the first tile at the unit's
+// first input (8 t on), the next tile 8 rows on, the next part part_pitch bytes on; rows from `live` on are zeros.
+template <typename T, int NT>
+__device__ __forceinline__ void unit_products(const Linear4Args &a, const uint8_t *unit, const uint8_t *x, int row_pitch, int part_pitch,
+                                              int live, int lane, float (&total)[NT][4]) {
+    const int g = lane >> 2;
+    const float *scales = reinterpret_cast<const float *>(unit + 512 * a.unit_blocks) + g;
+    float sum[NT][4];
+    for (int block = 0; block < a.unit_blocks; ++block) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(unit + 512 * block + 16 * lane);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int k = block * kStep + 32 * j;
-            if (j == 0 || fine)
+            if (block + j == 0 || a.unit_scales == 2)
 #pragma unroll
-                for (int m = 0; m < MS; ++m)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int i = 0; i < 4; ++i) sum[nt][i] = 0.0f;
+            uint32_t A[2][4];
+            widen<T>(j ? w.z : w.x, A[0]);
+            widen<T>(j ? w.w : w.y, A[1]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[m][nt][i] = 0.0f;
-            uint32_t A[MS][2][4];
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int m = 0; m < MS; ++m) {
-                widen<T>(j ? now[m].z : now[m].x, A[m][0]);
-                widen<T>(j ? now[m].w : now[m].y, A[m][1]);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                uint32_t b[kParts<T>][2][2];
-                load_x<T>(a, x[nt], row0 + 8 * nt + g < a.rows, k + 8 * t, b);
-#pragma unroll
-                for (int part = kParts<T> - 1; part >= 0; --part)
-#pragma unroll
-                    for (int m = 0; m < MS; ++m)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if constexpr (std::is_same<T, __half>::value)
-                                mma(sum[m][nt], A[m][h], b[part][h][0], b[part][h][1]);
-                            else
-                                mma_bf16(sum[m][nt], A[m][h], b[part][h][0], b[part][h][1]);
-                        }
-            }
-            if (j == 1 || fine) {
-                const int group = min(k / a.group, a.groups - 1);        // (behind the last input: sums are 0)
-#pragma unroll
-                for (int m = 0; m < MS; ++m) {
-                    const float s0 = __ldg(scales[m] + group * kStrip), s1 = __ldg(scales[m] + group * kStrip + 8);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        total[m][nt][0] = fmaf(s0, sum[m][nt][0], total[m][nt][0]);
-                        total[m][nt][1] = fmaf(s0, sum[m][nt][1], total[m][nt][1]);
-                        total[m][nt][2] = fmaf(s1, sum[m][nt][2], total[m][nt][2]);
-                        total[m][nt][3] = fmaf(s1, sum[m][nt][3], total[m][nt][3]);
+                for (int part = kParts<T> - 1; part >= 0; --part) {
+                    uint4 b = make_uint4(0, 0, 0, 0);
+                    if (8 * nt + g < live)
+                        b = *reinterpret_cast<const uint4 *>(x + 8 * nt * row_pitch + part * part_pitch + 128 * block + 64 * j);
+                    if constexpr (std::is_same<T, __half>::value) {
+                        mma(sum[nt], A[0], b.x, b.y);
+                        mma(sum[nt], A[1], b.z, b.w);
+                    } else {
+                        mma_bf16(sum[nt], A[0], b.x, b.y);
+                        mma_bf16(sum[nt], A[1], b.z, b.w);
                     }
+                }
+            if (a.unit_scales == 2 || (j == 1 && block + 1 == a.unit_blocks)) {
+                const float *s = scales + (a.unit_scales == 2 ? kStrip * j : 0);
+                const float s0 = s[0], s1 = s[8];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    total[nt][0] = fmaf(s0, sum[nt][0], total[nt][0]);
+                    total[nt][1] = fmaf(s0, sum[nt][1], total[nt][1]);
+                    total[nt][2] = fmaf(s1, sum[nt][2], total[nt][2]);
+                    total[nt][3] = fmaf(s1, sum[nt][3], total[nt][3]);
                 }
             }
         }
     }
-    // ---- the warps' sums, then scale, bias and the output type
-    constexpr int PITCH = C + 4;
-    float *mine = sums + warp * ROWS * PITCH;
+}
+
+// `ways` warps of the CTA share a strip's units; a CTA takes every gridDim.x-th set of strips.
+template <typename T, int NT>
+__global__ void __launch_bounds__(kCtaWarps * 32, NT == 1 ? 3 : 2) linear4_few(const Linear4Args a, int ways) {
+    constexpr int ROWS = 8 * NT, PITCH = kStrip + 4;
+    extern __shared__ __align__(128) uint8_t smem[];         // rings, sums of two strips, x
+    __shared__ __align__(8) uint64_t bars[kCtaWarps][kFewStages];
+    __shared__ int s_abort;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const uint8_t *ring = smem + warp * kFewStages * kStageBytes;
+    float *sums = reinterpret_cast<float *>(smem + kCtaWarps * kFewStages * kStageBytes);
+    uint8_t *xs = smem + kCtaWarps * kFewStages * kStageBytes + 2 * kCtaWarps * ROWS * PITCH * 4;
+    const uint32_t bar = tc::smem_addr(bars[warp]);
+    volatile int *abort_flag = &s_abort;
+    if (lane < kFewStages) tc::mbar_init(bar + 8 * lane, 1);
+    tc::fence_barrier_init();
+    if (threadIdx.x == 0) s_abort = 0;
+    __syncthreads();
+    after_prior_kernels();
+    const int err = *reinterpret_cast<volatile int *>(a.err);
+
+    const int sets = kCtaWarps / ways, way = warp % ways, set = warp / ways;
+    const int from = a.units * way / ways, to = a.units * (way + 1) / ways, per = (to - from + a.stage_units - 1) / a.stage_units;
+    const int step = gridDim.x * sets;
+    // ---- this warp's copies: `per` a strip
+    int asked = 0, strip = blockIdx.x * sets + set, chunk = 0;
+    auto ask = [&]() {
+        if (strip >= a.strips) return;
+        if (lane == 0) {
+            const int first = from + chunk * a.stage_units, n = min(a.stage_units, to - first), stage = asked % kFewStages;
+            tc::mbar_expect_tx(bar + 8 * stage, n * a.unit_bytes);
+            bulk_load(tc::smem_addr(ring + stage * kStageBytes), a.w + ((long long)strip * a.units + first) * a.unit_bytes, n * a.unit_bytes,
+                      bar + 8 * stage);
+        }
+        ++asked;
+        if (++chunk == per) {
+            chunk = 0;
+            strip += step;
+        }
+    };
+    for (int i = 0; i < kFewStages; ++i) ask();
+
+    // ---- x, behind its last input zeros
+    const int k_pad = a.units * a.unit_blocks * kStep, row_pitch = 2 * k_pad + 64, part_pitch = a.rows * row_pitch;
+    for (int row = warp; row < a.rows; row += kCtaWarps) {
+        const T *p = static_cast<const T *>(a.x) + (long long)row * a.ldx;
+        uint8_t *to_x = xs + row * row_pitch;
+        if (a.vec && kParts<T> == 1) {
+#pragma unroll 4
+            for (int k = 8 * lane; k < k_pad; k += 256) async_copy(tc::smem_addr(to_x + 2 * k), p + min(k, a.k - 1), min(max(2 * (a.k - k), 0), 16));
+        } else {
+#pragma unroll 2
+            for (int k = 8 * lane; k < k_pad; k += 256) {
+                uint4 v[kParts<T>];
+                load8<T>(a, p, true, k, v);
 #pragma unroll
-    for (int m = 0; m < MS; ++m)
+                for (int part = 0; part < kParts<T>; ++part) *reinterpret_cast<uint4 *>(to_x + part * part_pitch + 2 * k) = v[part];
+            }
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    bool sound = !__syncthreads_or(err != 0);
+
+    int done = 0, buffer = 0;
+    const int rounds = (a.strips + step - 1) / step;
+    const uint8_t *x = xs + min(g, a.rows - 1) * row_pitch + 16 * t;
+    for (int round = 0; round < rounds && sound; ++round) {
+        const int here = (round * (int)gridDim.x + (int)blockIdx.x) * sets + set;
+        float total[NT][4] = {};
+        if (here < a.strips)
+            for (int c = 0; c < per; ++c) {
+                const int stage = done % kFewStages, first = from + c * a.stage_units, n = min(a.stage_units, to - first);
+                sound = __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * stage, (uint32_t)(done / kFewStages) & 1u, abort_flag, a.err));
+                if (!sound) break;
+                for (int i = 0; i < n; ++i)
+                    unit_products<T, NT>(a, ring + stage * kStageBytes + i * a.unit_bytes, x + (first + i) * a.unit_blocks * (2 * kStep),
+                                         row_pitch, part_pitch, a.rows, lane, total);
+                __syncwarp();
+                ++done;
+                ask();
+            }
+        // ---- the warps' sums
+        float *mine = sums + (buffer * kCtaWarps + warp) * ROWS * PITCH;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(8 * nt + 2 * t + (i & 1)) * PITCH + 16 * m + g + (i >> 1) * 8] = total[m][nt][i];
-    __syncthreads();
-    const int live = min(ROWS, a.rows - row0);
-    for (int i = threadIdx.x; i < live * C * sets; i += kCtaWarps * 32) {
-        const int ch = i % C, set = i / C % sets, row = i / (C * sets), n = (blockIdx.x * sets + set) * C + ch;
-        if (n >= a.n) continue;
-        float v = 0.0f;
-        for (int j = 0; j < ways; ++j) v += sums[((set * ways + j) * ROWS + row) * PITCH + ch];
-        if (a.s_x) v *= __ldg(a.s_x + row0 + row);
-        if (a.bias) v += __ldg(a.bias + n);
-        static_cast<Y *>(a.y)[(long long)(row0 + row) * a.ldy + n] = from_f32<Y>(v);
+            for (int i = 0; i < 4; ++i) mine[(8 * nt + 2 * t + (i & 1)) * PITCH + g + (i >> 1) * 8] = total[nt][i];
+        sound = !__syncthreads_or(!sound);
+        for (int i = threadIdx.x; sound && i < a.rows * kStrip * sets; i += kCtaWarps * 32) {
+            const int ch = i % kStrip, of = i / kStrip % sets, row = i / (kStrip * sets);
+            const int n = ((round * (int)gridDim.x + (int)blockIdx.x) * sets + of) * kStrip + ch;
+            if (n >= a.n) continue;
+            const float *p = sums + (buffer * kCtaWarps + of * ways) * ROWS * PITCH + row * PITCH + ch;
+            float v = 0.0f;
+            for (int j = 0; j < ways; ++j) v += p[j * ROWS * PITCH];
+            store_y(a, row, n, v);
+        }
+        buffer ^= 1;
     }
+    // copies still on their way (where a wait gave up) have to land before the CTA leaves
+    const long long t0 = clock64();
+    for (int i = done; i < asked; ++i)
+        while (!tc::mbar_try_wait(bar + 8 * (i % kFewStages), (uint32_t)(i / kFewStages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
 }
 
-template <typename T, typename Y, int NT, int MS>
-cudaError_t launch(const Linear4Args &a, int ways, cudaStream_t s) {
-    static std::atomic<int> allowed[64];
-    constexpr int bytes = kCtaWarps * 8 * NT * (kStrip * MS + 4) * 4;
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_kernel<T, Y, NT, MS>), bytes, allowed);
-    if (e != cudaSuccess) return e;
-    const int channels = kStrip * MS * (kCtaWarps / ways);
-    return launch_early(linear4_kernel<T, Y, NT, MS>, dim3((unsigned)((a.n + channels - 1) / channels), (unsigned)((a.rows + 8 * NT - 1) / (8 * NT))),
-                        kCtaWarps * 32, bytes, s, a, ways);
+constexpr int kManyDepth = 128;        // inputs of a piece of x
+constexpr int kManyPitch = 2 * kManyDepth + 64;
+constexpr int kManyRing = 1280;        // bytes of a warp's weights for a piece: a unit of 128, or two of 64
+constexpr int kManyStages = 4;
+template <typename T> constexpr int kXStages = std::is_same<T, float>::value ? 2 : 3;
+
+// A warp per strip, 8 strips a CTA, NT tiles of 8 rows; the CTAs of a cluster (along z) have a part of the inputs each.
+template <typename T, int NT>
+__global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(const Linear4Args a, int split) {
+    constexpr int ROWS = 8 * NT, PARTS = kParts<T>, XS = kXStages<T>, PART = ROWS * kManyPitch, XSTAGE = PARTS * PART;
+    constexpr int PITCH = kCtaWarps * kStrip + 4;
+    extern __shared__ __align__(128) uint8_t smem[];         // rings, x; in the end the CTA's sums
+    __shared__ __align__(8) uint64_t bars[kCtaWarps][kManyStages];
+    __shared__ int s_abort;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const uint8_t *ring = smem + warp * kManyStages * kManyRing;
+    uint8_t *xs = smem + kCtaWarps * kManyStages * kManyRing;
+    const uint32_t bar = tc::smem_addr(bars[warp]);
+    volatile int *abort_flag = &s_abort;
+    if (lane < kManyStages) tc::mbar_init(bar + 8 * lane, 1);
+    tc::fence_barrier_init();
+    if (threadIdx.x == 0) s_abort = 0;
+    __syncthreads();
+    after_prior_kernels();
+    bool sound = !__syncthreads_or(*reinterpret_cast<volatile int *>(a.err) != 0);
+
+    const int strip = min((int)blockIdx.x * kCtaWarps + warp, a.strips - 1), row0 = blockIdx.y * ROWS, live = min(ROWS, a.rows - row0);
+    const int pieces = (a.k + kManyDepth - 1) / kManyDepth, from = pieces * (int)blockIdx.z / split, to = pieces * ((int)blockIdx.z + 1) / split;
+    const int piece_units = kManyDepth / (kStep * a.unit_blocks);
+    auto ask = [&](int i) {
+        if (i >= to - from || lane) return;
+        const int first = (from + i) * piece_units, n = min(piece_units, a.units - first), stage = i % kManyStages;
+        tc::mbar_expect_tx(bar + 8 * stage, n * a.unit_bytes);
+        bulk_load(tc::smem_addr(ring + stage * kManyRing), a.w + ((long long)strip * a.units + first) * a.unit_bytes, n * a.unit_bytes,
+                  bar + 8 * stage);
+    };
+    // Pieces of x, zeros behind the last row and input. As they lie, by asynchronous copies; otherwise through registers.
+    const bool direct = a.vec && PARTS == 1;
+    auto bring = [&](int i) {
+        if (i < to - from) {
+            const int k0 = (from + i) * kManyDepth;
+            uint8_t *stage = xs + i % XS * XSTAGE;
+            for (int j = threadIdx.x; j < ROWS * (kManyDepth / 8); j += kCtaWarps * 32) {
+                const int row = j / (kManyDepth / 8), k = j % (kManyDepth / 8) * 8;
+                uint8_t *to_x = stage + row * kManyPitch + 2 * k;
+                const T *p = static_cast<const T *>(a.x) + (long long)(row0 + min(row, live - 1)) * a.ldx;
+                if (direct) {
+                    const int bytes = row < live ? min(max(2 * (a.k - k0 - k), 0), 16) : 0;
+                    async_copy(tc::smem_addr(to_x), p + (bytes ? k0 + k : 0), bytes);
+                } else {
+                    uint4 v[PARTS];
+                    load8<T>(a, p, row < live, k0 + k, v);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<uint4 *>(to_x + part * PART) = v[part];
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (sound) {
+        for (int i = 0; i < kManyStages; ++i) ask(i);
+#pragma unroll
+        for (int i = 0; i < XS - 1; ++i) bring(i);
+    }
+    float total[NT][4] = {};
+    int done = 0;
+    for (; sound && done < to - from; ++done) {
+        const int stage = done % kManyStages, n = min(piece_units, a.units - (from + done) * piece_units);
+        asm volatile("cp.async.wait_group %0;" ::"n"(XS - 2) : "memory");
+        const bool here = tc::mbar_wait(bar + 8 * stage, (uint32_t)(done / kManyStages) & 1u, abort_flag, a.err);
+        sound = !__syncthreads_or(!here);
+        if (!sound) break;
+        bring(done + XS - 1);
+        const uint8_t *x = xs + done % XS * XSTAGE + g * kManyPitch + 16 * t;
+        for (int i = 0; i < n; ++i)
+            unit_products<T, NT>(a, ring + stage * kManyRing + i * a.unit_bytes, x + i * a.unit_blocks * (2 * kStep), kManyPitch, PART, ROWS, lane, total);
+        __syncwarp();
+        ask(done + kManyStages);
+    }
+    if (!sound) {                                            // (copies on their way have to land before the CTA leaves)
+        const long long t0 = clock64();
+        const int asked = min(done + kManyStages, to - from);
+        for (int i = done; i < asked; ++i)
+            while (!tc::mbar_try_wait(bar + 8 * (i % kManyStages), (uint32_t)(i / kManyStages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    // ---- the CTA's sums, added up over the cluster, a share of the rows each
+    float *sums = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sums[(8 * nt + 2 * t + (i & 1)) * PITCH + kStrip * warp + g + (i >> 1) * 8] = total[nt][i];
+    if (split > 1) {
+        asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+    if (*abort_flag) sound = false;
+    const int each = (live + split - 1) / split, row_from = (int)blockIdx.z * each, row_to = min(row_from + each, live);
+    // 4 channels a thread: a warp has a row, and its store is of whole lines
+    for (int row = row_from + warp; sound && row < row_to; row += kCtaWarps) {
+        const uint32_t at = tc::smem_addr(sums + row * PITCH + 4 * lane);
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int z = 0; z < 8; ++z)
+            if (z < split) {
+                uint32_t there = at;
+                float4 u;
+                if (split > 1) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(z));
+                if (split > 1)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(u.x), "=f"(u.y), "=f"(u.z), "=f"(u.w) : "r"(there) : "memory");
+                else
+                    u = *reinterpret_cast<const float4 *>(sums + row * PITCH + 4 * lane);
+                v.x += u.x;
+                v.y += u.y;
+                v.z += u.z;
+                v.w += u.w;
+            }
+        const int n = blockIdx.x * kCtaWarps * kStrip + 4 * lane;
+        const float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < a.n) store_y(a, row0 + row, n + i, o[i]);
+    }
+    if (split > 1) asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
-template <typename T, typename Y>
-cudaError_t launch_rows(const Linear4Args &a, cudaStream_t s) {
-    const int blocks = (a.k + kStep - 1) / kStep, ways = blocks >= 8 ? 8 : blocks >= 4 ? 4 : blocks >= 2 ? 2 : 1;
-    if (a.rows <= 8) return launch<T, Y, 1, 1>(a, ways, s);
-    if (a.rows <= 16) return launch<T, Y, 2, 2>(a, ways, s);
-    return launch<T, Y, 4, 2>(a, ways, s);
+
+template <typename T, int NT>
+cudaError_t launch_few(const Linear4Args &a, int x_bytes, int sms, cudaStream_t s) {
+    static std::atomic<int> allowed[64];
+    const int bytes = kCtaWarps * kFewStages * kStageBytes + 2 * kCtaWarps * 8 * NT * (kStrip + 4) * 4 + x_bytes;
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_few<T, NT>), bytes, allowed);
+    if (e != cudaSuccess) return e;
+    const int ways = a.units >= 8 ? 8 : a.units >= 4 ? 4 : a.units >= 2 ? 2 : 1, sets = kCtaWarps / ways;
+    const int resident = max(1, min(3, 220 * 1024 / (bytes + 1024))), all = (a.strips + sets - 1) / sets;
+    return launch_early(linear4_few<T, NT>, dim3((unsigned)min(all, sms * resident)), kCtaWarps * 32, bytes, s, a, ways);
+}
+template <typename T, int NT>
+cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
+    static std::atomic<int> allowed[64];
+    constexpr int x_bytes = kXStages<T> * kParts<T> * 8 * NT * kManyPitch, sum_bytes = 8 * NT * (kCtaWarps * kStrip + 4) * 4;
+    constexpr int ring = kCtaWarps * kManyStages * kManyRing, bytes = ring + x_bytes > sum_bytes ? ring + x_bytes : sum_bytes;
+    static_assert(bytes <= 226 * 1024, "shared memory of a CTA");
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_many<T, NT>), bytes, allowed);
+    if (e != cudaSuccess) return e;
+    const int tiles = (a.strips + kCtaWarps - 1) / kCtaWarps, row_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
+    const int pieces = (a.k + kManyDepth - 1) / kManyDepth;
+    // the split of the inputs that takes the fewest steps: waves x pieces, and about three for joining
+    int split = 1;
+    long long best = LLONG_MAX;
+    for (int x = 1; x <= 8 && x <= pieces; x *= 2) {
+        const long long ctas = (long long)tiles * row_tiles * x, cost = (ctas + sms - 1) / sms * ((pieces + x - 1) / x) + (x > 1 ? 3 : 0);
+        if (cost < best) {
+            best = cost;
+            split = x;
+        }
+    }
+    cudaLaunchAttribute attr[2] = {early_start(), {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = (unsigned)split;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)tiles, (unsigned)row_tiles, (unsigned)split);
+    cfg.blockDim = dim3(kCtaWarps * 32);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, linear4_many<T, NT>, a, split);
 }
 template <typename T>
-cudaError_t launch_type(const Linear4Args &a, cudaStream_t s) {
-    switch (a.y_type) {
-        case HATQ_F32: return launch_rows<T, float>(a, s);
-        case HATQ_F16: return launch_rows<T, __half>(a, s);
-        default: return launch_rows<T, __nv_bfloat16>(a, s);
-    }
+cudaError_t launch_type(const Linear4Args &a, int sms, cudaStream_t s) {
+    const long long x_bytes = (long long)kParts<T> * a.rows * (2LL * a.units * a.unit_blocks * kStep + 64);
+    if (a.rows <= 16 && x_bytes <= 140 * 1024)
+        return a.rows <= 8 ? launch_few<T, 1>(a, (int)x_bytes, sms, s) : launch_few<T, 2>(a, (int)x_bytes, sms, s);
+    return a.rows <= 16 ? launch_many<T, 2>(a, sms, s) : a.rows <= 32 ? launch_many<T, 4>(a, sms, s) : launch_many<T, 8>(a, sms, s);
 }
 
-// A warp per strip and block: lane (g, t) packs channels g and g + 8 (the first in the lower of two nibbles) at inputs
-// 8 t .. 8 t + 7 of each half of the block; a word has four inputs, their pairs 16 bits apart.
-__global__ void __launch_bounds__(256) layout_kernel(const int8_t *w, long long ldw, int n, int k, int strips, int blocks, uint4 *out) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (unit >= (long long)strips * blocks) return;
-    const int strip = (int)(unit / blocks), block = (int)(unit % blocks);
+// A warp per strip and 64 inputs: lane (g, t) packs channels g and g + 8 (the first in the lower of two nibbles) at inputs
+// 8 t .. 8 t + 7 of each half of them; a word has four inputs, their pairs 16 bits apart.
+__global__ void __launch_bounds__(256) layout_kernel(const int8_t *w, long long ldw, const float *scales, long long lds, const Linear4Args a,
+                                                     uint8_t *out) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, blocks = a.units * a.unit_blocks;
+    const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (at >= (long long)a.strips * blocks) return;
+    const int strip = (int)(at / blocks), block = (int)(at % blocks), in_unit = block % a.unit_blocks;
+    uint8_t *unit = out + ((long long)strip * a.units + block / a.unit_blocks) * a.unit_bytes;
     uint32_t words[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -235,18 +458,15 @@ __global__ void __launch_bounds__(256) layout_kernel(const int8_t *w, long long 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {                        // input j & 3 of the word, channel g + 8 (j >> 2)
             const int row = strip * kStrip + g + (j >> 2) * 8, col = block * kStep + (i >> 1) * 32 + 8 * t + (i & 1) * 4 + (j & 3);
-            const int code = row < n && col < k ? min(max((int)w[row * ldw + col], -8), 7) : 0;
+            const int code = row < a.n && col < a.k ? min(max((int)w[row * ldw + col], -8), 7) : 0;
             const int nibble = (j & 1) * 4 + ((j >> 1) & 1) * 2 + (j >> 2);
             words[i] |= (uint32_t)(code + 8) << (4 * nibble);
         }
     }
-    out[unit * 32 + lane] = make_uint4(words[0], words[1], words[2], words[3]);
-}
-__global__ void __launch_bounds__(256) scales_kernel(const float *scales, long long lds, int n, int groups, long long total, float *out) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int ch = (int)(i % kStrip), group = (int)(i / kStrip % groups), row = (int)(i / ((long long)kStrip * groups)) * kStrip + ch;
-    out[i] = row < n ? scales[row * lds + group] : 0.0f;
+    reinterpret_cast<uint4 *>(unit + 512 * in_unit)[lane] = make_uint4(words[0], words[1], words[2], words[3]);
+    const int row = strip * kStrip + (lane & 15), k = block * kStep + 32 * (lane >> 4);
+    if (in_unit == 0 && lane < kStrip * a.unit_scales)
+        reinterpret_cast<float *>(unit + 512 * a.unit_blocks)[lane] = row < a.n && k < a.k ? scales[row * lds + k / a.group] : 0.0f;
 }
 
 // A CTA per row: transformed in shared memory, then a warp per group.
@@ -297,14 +517,12 @@ cudaError_t quantize_type(const void *w, long long ldw, int n, int k, int hb, in
 }  // namespace
 
 cudaError_t launch_linear4(const Linear4Args &a, int x_type, int sms, cudaStream_t s) {
-    return x_type == HATQ_F32 ? launch_type<float>(a, s) : x_type == HATQ_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);
+    return x_type == HATQ_F32 ? launch_type<float>(a, sms, s) : x_type == HATQ_F16 ? launch_type<__half>(a, sms, s) : launch_type<__nv_bfloat16>(a, sms, s);
 }
-cudaError_t launch_linear4_layout(const int8_t *w, long long ldw, const float *scales, long long lds, int n, int k, int groups,
-                                  uint8_t *codes, float *out_scales, cudaStream_t s) {
-    const int strips = (n + kStrip - 1) / kStrip, blocks = (k + kStep - 1) / kStep;
-    const long long units = (long long)strips * blocks, total = (long long)strips * kStrip * groups;
-    layout_kernel<<<(unsigned)((units + 7) / 8), 256, 0, s>>>(w, ldw, n, k, strips, blocks, reinterpret_cast<uint4 *>(codes));
-    scales_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(scales, lds, n, groups, total, out_scales);
+cudaError_t launch_linear4_layout(const int8_t *w, long long ldw, const float *scales, long long lds, const Linear4Args &a, uint8_t *out,
+                                  cudaStream_t s) {
+    const long long blocks = (long long)a.strips * a.units * a.unit_blocks;
+    layout_kernel<<<(unsigned)((blocks + 7) / 8), 256, 0, s>>>(w, ldw, scales, lds, a, out);
     return cudaGetLastError();
 }
 cudaError_t launch_quantize_groups(const void *w, int type, long long ldw, int n, int k, int hb, int group, int8_t *codes,

@@ -17,28 +17,28 @@ hatq_status check_weights(const hatq_linear4_weights *L) {
     return HATQ_OK;
 }
 hatq_status check_buffers(const hatq_linear4_weights *L) {
-    if (!L->codes || !L->scales) return fail(HATQ_ERR_INVALID_ARG, "null weights");
-    if (!aligned(L->codes, 16) || !aligned(L->scales, 16) || !aligned(L->bias, 4))
-        return fail(HATQ_ERR_INVALID_ARG, "weight codes and scales must be 16-byte aligned, the bias to its elements");
+    if (!L->data) return fail(HATQ_ERR_INVALID_ARG, "null weights");
+    if (!aligned(L->data, 16) || !aligned(L->bias, 4))
+        return fail(HATQ_ERR_INVALID_ARG, "weights must be 16-byte aligned, the bias to its elements");
     return HATQ_OK;
 }
 long long groups_of(const hatq_linear4_weights *L) { return ((long long)L->k + L->group - 1) / L->group; }
-size_t strips_of(int n) { return ((size_t)n + hatq::kStrip - 1) / hatq::kStrip; }
 
 }  // namespace
 
 extern "C" {
 
-hatq_status hatq_linear4_sizes(int n, int k, int group, size_t *code_bytes, size_t *scale_bytes) {
+hatq_status hatq_linear4_sizes(int n, int k, int group, size_t *bytes) {
     hatq_linear4_weights L{};
     L.n = n;
     L.k = k;
     L.group = group;
     const hatq_status st = check_weights(&L);
     if (st != HATQ_OK) return st;
-    if (!code_bytes || !scale_bytes) return fail(HATQ_ERR_INVALID_ARG, "null output");
-    *code_bytes = strips_of(n) * (size_t)((k + hatq::kStep - 1) / hatq::kStep) * 512;
-    *scale_bytes = strips_of(n) * hatq::kStrip * (size_t)groups_of(&L) * 4;
+    if (!bytes) return fail(HATQ_ERR_INVALID_ARG, "null output");
+    hatq::Linear4Args a{};
+    hatq::linear4_units(n, k, group, a);
+    *bytes = (size_t)a.strips * (size_t)a.units * (size_t)a.unit_bytes;
     return HATQ_OK;
 }
 
@@ -73,8 +73,9 @@ hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *sca
     if (ldw > kMaxPitch || lds > kMaxPitch) return fail(HATQ_ERR_UNSUPPORTED, "a pitch is larger than 2^32 elements");
     if (!w || !scales) return fail(HATQ_ERR_INVALID_ARG, "null tensor");
     if (!aligned(scales, 4)) return fail(HATQ_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
-    const cudaError_t e = hatq::launch_linear4_layout(w, ldw, scales, lds, L->n, L->k, (int)groups_of(L), L->codes, L->scales,
-                                                      reinterpret_cast<cudaStream_t>(stream));
+    hatq::Linear4Args a{};
+    hatq::linear4_units(L->n, L->k, L->group, a);
+    const cudaError_t e = hatq::launch_linear4_layout(w, ldw, scales, lds, a, L->data, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "weight layout launch");
 }
 
@@ -95,19 +96,16 @@ hatq_status hatq_linear4(const void *x, int x_type, long long ldx, const float *
     if (overlap(x, rows, ldx, L->k, type_size(x_type), y, rows, ldy, L->n, type_size(y_type)))
         return fail(HATQ_ERR_INVALID_ARG, "x and y overlap");
     const int sms = sm_count();
-    if (!sms) return fail(HATQ_ERR_CUDA, "no CUDA device");
     hatq::Linear4Args a{};
+    a.err = hatq::device_error_word();
+    if (!sms || !a.err) return fail(HATQ_ERR_CUDA, "no CUDA device");
     a.x = x;
     a.ldx = ldx;
     a.vec = aligned(x, 16) && ldx * type_size(x_type) % 16 == 0;
     a.s_x = s_x;
     a.rows = (int)rows;
-    a.n = L->n;
-    a.k = L->k;
-    a.group = L->group;
-    a.groups = (int)groups_of(L);
-    a.w = L->codes;
-    a.scales = L->scales;
+    hatq::linear4_units(L->n, L->k, L->group, a);
+    a.w = L->data;
     a.bias = L->bias;
     a.y = y;
     a.ldy = ldy;

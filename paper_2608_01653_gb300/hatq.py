@@ -79,7 +79,7 @@ class TokenCacheStruct(ctypes.Structure):
 
 class Linear4WeightsStruct(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int), ("k", ctypes.c_int), ("group", ctypes.c_int), ("reserved", ctypes.c_int),
-                ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+                ("data", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
 _LIB = None
@@ -158,7 +158,7 @@ def load(build: bool = True) -> ctypes.CDLL:
                                            ctypes.POINTER(ctypes.c_size_t)]),
             "hatq_attend_tokens": (_I, [_P, _I, _L, _L, _I, _L, ctypes.POINTER(TokenCacheStruct), _P, _L, _I, _P, _P, _I,
                                         _F, _P, _L, _L, _P, ctypes.c_size_t, _P]),
-            "hatq_linear4_sizes": (_I, [_I, _I, _I, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]),
+            "hatq_linear4_sizes": (_I, [_I, _I, _I, ctypes.POINTER(ctypes.c_size_t)]),
             "hatq_quantize_groups": (_I, [_P, _I, _L, _I, _I, _I, _I, _P, _L, _P, _L, _P]),
             "hatq_linear4_layout": (_I, [_P, _L, _P, _L, ctypes.POINTER(Linear4WeightsStruct), _P]),
             "hatq_linear4": (_I, [_P, _I, _L, _P, _L, ctypes.POINTER(Linear4WeightsStruct), _I, _P, _L, _P]),
@@ -1086,6 +1086,7 @@ class TokenCache:
         self.struct = TokenCacheStruct(data.data_ptr(), pages, page, heads, self.width, hb, 0)
         self.ref = ctypes.byref(self.struct)
         self.scale = self.width ** -0.5 if self.width > 0 else 1.0
+        self.workspaces = {}                        # bytes of attend_tokens' workspace, by the sizes of a call
         size = ctypes.c_size_t()                    # the library looks the sizes over
         _check(load().hatq_attend_workspace(self.ref, heads, 0, 0, 0, 0, ctypes.byref(size)))
 
@@ -1157,10 +1158,11 @@ def append_tokens(cache, k, v, table, lengths, starts=None, kept=False, stream=N
     pt, ldt, pages, pl, ps, seqs = _sequences_of(table, lengths, starts, rows, device)
     out, pk, pv = None, None, None
     if kept:
-        both = _empty(k, (2, rows, heads, width), k.dtype, stream)
-        out = both.unbind(0)
-        pk = both.data_ptr()
-        pv = pk + both.element_size() * rows * heads * width
+        if stream is None and k.is_contiguous():
+            out = torch.empty_like(k), torch.empty_like(k)
+        else:
+            out = _empty(k, k.shape, k.dtype, stream), _empty(k, k.shape, k.dtype, stream)
+        pk, pv = out[0].data_ptr(), out[1].data_ptr()
     st = (_LIB or load()).hatq_append_tokens(cache.ref, k.data_ptr(), ldk, hk, v.data_ptr(), ldv, hv, kind, rows, pt, ldt,
                                              pages, pl, ps, seqs, pk, pv, raw)
     if st:
@@ -1182,20 +1184,24 @@ def attend_tokens(q, cache, table, lengths, starts=None, scale=None, out=None, s
     heads = q.shape[1]
     pt, ldt, pages, pl, ps, seqs = _sequences_of(table, lengths, starts, rows, device)
     if out is None:
-        out = _empty(q, q.shape, q.dtype, stream)
+        out = torch.empty_like(q) if stream is None and q.is_contiguous() else _empty(q, q.shape, q.dtype, stream)
         ldo, ho = heads * cache.width, cache.width
     else:
         if out.dtype != q.dtype or out.shape != q.shape:
             raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {q.dtype} {tuple(q.shape)}")
         _, _, ldo, ho = _heads_of(out, "out", heads, cache.width, device)
-    lib, size = _LIB or load(), ctypes.c_size_t()
-    st = lib.hatq_attend_workspace(cache.ref, heads, rows, seqs, 0 if starts is None else 1, pages, ctypes.byref(size))
-    if st:
-        _check(st)
-    scratch = _empty(q, (size.value,), torch.uint8, stream)
+    lib, sizes = _LIB or load(), (heads, rows, seqs, pages, starts is None)
+    size = cache.workspaces.get(sizes)
+    if size is None:
+        need = ctypes.c_size_t()
+        _check(lib.hatq_attend_workspace(cache.ref, heads, rows, seqs, 0 if starts is None else 1, pages, ctypes.byref(need)))
+        if len(cache.workspaces) >= 256:
+            cache.workspaces.clear()
+        size = cache.workspaces[sizes] = need.value
+    scratch = _empty(q, (size,), torch.uint8, stream) if size else None
     st = lib.hatq_attend_tokens(q.data_ptr(), kind, ldq, hq, heads, rows, cache.ref, pt, ldt, pages, pl, ps, seqs,
-                                cache.scale if scale is None else scale, out.data_ptr(), ldo, ho, scratch.data_ptr(),
-                                size.value, raw)
+                                cache.scale if scale is None else scale, out.data_ptr(), ldo, ho,
+                                scratch.data_ptr() if size else None, size, raw)
     if st:
         _check(st)
     return out
@@ -1206,12 +1212,10 @@ def attend_tokens(q, cache, table, lengths, starts=None, scale=None, out=None, s
 class Linear4Weights:
     """4-bit weights with one scale per group of inputs (hatq_linear4_weights): device buffers and the C struct."""
 
-    def __init__(self, n, k, group, codes, scales, bias):
-        self.n, self.k, self.group = n, k, group
-        self.codes, self.scales, self.bias = codes, scales, bias
-        self.device = codes.get_device()
-        self.struct = Linear4WeightsStruct(n, k, group, 0, codes.data_ptr(), scales.data_ptr(),
-                                           None if bias is None else bias.data_ptr())
+    def __init__(self, n, k, group, data, bias):
+        self.n, self.k, self.group, self.data, self.bias = n, k, group, data, bias
+        self.device = data.get_device()
+        self.struct = Linear4WeightsStruct(n, k, group, 0, data.data_ptr(), None if bias is None else bias.data_ptr())
         self.ref = ctypes.byref(self.struct)
 
 
@@ -1242,8 +1246,8 @@ def prepare_linear4(w, group=128, hb=1, scales=None, bias=None, stream=None) -> 
     if w.dim() != 2:
         raise ValueError(f"w: shape {tuple(w.shape)}, expected [n, k]")
     n, k = w.shape
-    code_bytes, scale_bytes = ctypes.c_size_t(), ctypes.c_size_t()
-    _check(load().hatq_linear4_sizes(n, k, group, ctypes.byref(code_bytes), ctypes.byref(scale_bytes)))
+    size = ctypes.c_size_t()
+    _check(load().hatq_linear4_sizes(n, k, group, ctypes.byref(size)))
     device, raw = _launch_stream(w, stream)
     groups = -(-k // group)
     with torch.cuda.stream(stream):                 # None: the current one
@@ -1261,8 +1265,7 @@ def prepare_linear4(w, group=128, hb=1, scales=None, bias=None, stream=None) -> 
             if bias.numel() != n:
                 raise ValueError(f"bias: shape {tuple(bias.shape)}, expected {n} values")
             bias = bias.to(device=w.device, dtype=torch.float32).reshape(-1).clone()
-        L = Linear4Weights(n, k, group, torch.empty(code_bytes.value, dtype=torch.uint8, device=w.device),
-                           torch.empty(scale_bytes.value // 4, dtype=torch.float32, device=w.device), bias)
+        L = Linear4Weights(n, k, group, torch.empty(size.value, dtype=torch.uint8, device=w.device), bias)
         _check(load().hatq_linear4_layout(codes.data_ptr(), k, scales.data_ptr(), groups, L.ref, raw))
     return L
 

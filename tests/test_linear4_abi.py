@@ -13,8 +13,8 @@ def lib():
     return H.load()
 
 
-def weights(n=64, k=130, group=32, codes=P, scales=2 * P, bias=None):
-    return H.Linear4WeightsStruct(n, k, group, 0, codes, scales, bias)
+def weights(n=64, k=130, group=32, data=P, bias=None):
+    return H.Linear4WeightsStruct(n, k, group, 0, data, bias)
 
 
 def product(lib, L=None, **kw):
@@ -28,7 +28,7 @@ def product(lib, L=None, **kw):
 WEIGHTS = [(dict(n=0), H.ERR_INVALID_ARG), (dict(k=0), H.ERR_INVALID_ARG), (dict(k=(1 << 20) + 1), H.ERR_UNSUPPORTED),
            (dict(n=(1 << 27) + 1), H.ERR_UNSUPPORTED), (dict(group=0), H.ERR_INVALID_ARG), (dict(group=16), H.ERR_INVALID_ARG),
            (dict(group=48), H.ERR_INVALID_ARG), (dict(group=-32), H.ERR_INVALID_ARG)]
-BUFFERS = [dict(codes=None), dict(scales=None), dict(codes=P + 8), dict(scales=2 * P + 4), dict(bias=P + 2)]
+BUFFERS = [dict(data=None), dict(data=P + 8), dict(bias=P + 2)]
 
 
 @pytest.mark.parametrize("kw,status", WEIGHTS + [(b, H.ERR_INVALID_ARG) for b in BUFFERS])
@@ -48,20 +48,20 @@ def test_linear4_refuses(lib, kw, status):
 
 
 def test_no_rows_is_no_work(lib):
-    assert product(lib, weights(codes=None, scales=None), x=None, y=None, rows=0) == H.OK
+    assert product(lib, weights(data=None), x=None, y=None, rows=0) == H.OK
     assert lib.hatq_quantize_groups(None, 0, 64, 0, 64, 1, 32, None, 64, None, 2, None) == H.OK
     assert lib.hatq_linear4(3 * P, 0, 130, None, 4, None, 0, 4 * P, 64, None) == H.ERR_INVALID_ARG
 
 
 def test_sizes(lib):
-    a, b = ctypes.c_size_t(), ctypes.c_size_t()
-    for n, k, group, codes, scales in ((1, 1, 32, 512, 64), (17, 65, 64, 2 * 2 * 512, 32 * 2 * 4), (4096, 4096, 128, 1 << 23, 4096 * 32 * 4)):
-        assert lib.hatq_linear4_sizes(n, k, group, ctypes.byref(a), ctypes.byref(b)) == H.OK
-        assert (a.value, b.value) == (codes, scales)
+    a = ctypes.c_size_t()
+    for n, k, group, size in ((1, 1, 32, 512 + 128), (17, 65, 64, 2 * 2 * (512 + 64)), (17, 65, 128, 2 * (1024 + 64)),
+                              (4096, 4096, 128, 4096 * 2048 + 4096 * 32 * 4), (16, 300, 96, 5 * (512 + 128))):
+        assert lib.hatq_linear4_sizes(n, k, group, ctypes.byref(a)) == H.OK and a.value == size
     for kw, status in WEIGHTS:
         L = weights(**kw)
-        assert lib.hatq_linear4_sizes(L.n, L.k, L.group, ctypes.byref(a), ctypes.byref(b)) == status
-    assert lib.hatq_linear4_sizes(1, 1, 32, None, ctypes.byref(b)) == H.ERR_INVALID_ARG
+        assert lib.hatq_linear4_sizes(L.n, L.k, L.group, ctypes.byref(a)) == status
+    assert lib.hatq_linear4_sizes(1, 1, 32, None) == H.ERR_INVALID_ARG
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -90,13 +90,13 @@ def test_struct_matches_the_header():
     import os
     import subprocess
     import tempfile
-    src = ('#include <stdio.h>\n#include <stddef.h>\n#include "hatq.h"\nint main(void) { printf("%zu %zu %zu %zu %zu",'
-           ' sizeof(hatq_linear4_weights), offsetof(hatq_linear4_weights, group), offsetof(hatq_linear4_weights, codes),'
-           ' offsetof(hatq_linear4_weights, scales), offsetof(hatq_linear4_weights, bias)); return 0; }\n')
+    src = ('#include <stdio.h>\n#include <stddef.h>\n#include "hatq.h"\nint main(void) { printf("%zu %zu %zu %zu",'
+           ' sizeof(hatq_linear4_weights), offsetof(hatq_linear4_weights, group), offsetof(hatq_linear4_weights, data),'
+           ' offsetof(hatq_linear4_weights, bias)); return 0; }\n')
     include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
     with tempfile.TemporaryDirectory() as d:
         open(os.path.join(d, "t.c"), "w").write(src)
         subprocess.run(["gcc", "-I", include, os.path.join(d, "t.c"), "-o", os.path.join(d, "t")], check=True)
         got = [int(v) for v in subprocess.run([os.path.join(d, "t")], capture_output=True, text=True).stdout.split()]
     S = H.Linear4WeightsStruct
-    assert got == [ctypes.sizeof(S), S.group.offset, S.codes.offset, S.scales.offset, S.bias.offset]
+    assert got == [ctypes.sizeof(S), S.group.offset, S.data.offset, S.bias.offset]
