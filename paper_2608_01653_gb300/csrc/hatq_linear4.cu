@@ -25,9 +25,8 @@ namespace {
 // strip's end. More rows, or x too large for that (linear4_many): a strip a warp, x streamed through shared memory for
 // all of a CTA's strips; CTAs of a cluster share the inputs where there are few strips.
 
-constexpr int kCtaWarps = 8;
-constexpr int kStageBytes = 2560;      // of a warp's ring: two units of 128 (1088 bytes each), four of 64 (576 or 640)
-constexpr int kFewStages = 3;
+constexpr int kCtaWarps = 8, kMostWarps = 16;
+constexpr int kFewStages = 3;          // of a warp's ring, at most; each two units of 128, or four of 64
 
 template <typename T> constexpr int kParts = std::is_same<T, float>::value ? 3 : 1;
 
@@ -108,100 +107,102 @@ __device__ __forceinline__ void store_y(const Linear4Args &a, int row, int n, fl
     else static_cast<__nv_bfloat16 *>(a.y)[at] = from_f32<__nv_bfloat16>(v);
 }
 
-// A unit's products with NT tiles of 8 rows, added to the totals. x: lane (g, t)'s row g of the first tile at the unit's
-// first input (8 t on), the next tile 8 rows on, the next part part_pitch bytes on; rows from `live` on are zeros.
-template <typename T, int NT>
-__device__ __forceinline__ void unit_products(const Linear4Args &a, const uint8_t *unit, const uint8_t *x, int row_pitch, int part_pitch,
-                                              int live, int lane, float (&total)[NT][4]) {
-    const int g = lane >> 2;
-    const float *scales = reinterpret_cast<const float *>(unit + 512 * a.unit_blocks) + g;
-    float sum[NT][4];
-    for (int block = 0; block < a.unit_blocks; ++block) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(unit + 512 * block + 16 * lane);
+// A unit's products with NT tiles of 8 rows, added to the totals: BLOCKS x 64 inputs, SCALES scales a channel. x: lane
+// (g, t)'s row of the first tile at the unit's first input (8 t on); `next` bytes on the row of the next tile, part_pitch
+// on the next part. (Columns of rows that are none may hold anything.) Two sums at a time where tiles are few: steps
+// that add to one wait for each other.
+template <typename T, int NT, int BLOCKS, int SCALES>
+__device__ __forceinline__ void unit_products(const uint8_t *unit, const uint8_t *x, int next, int part_pitch, int lane, float (&total)[NT][4]) {
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr int SUMS = SCALES == 2 || NT <= 2 ? 2 : 1;
+    uint4 w[BLOCKS];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (block + j == 0 || a.unit_scales == 2)
+    for (int i = 0; i < BLOCKS; ++i) w[i] = *reinterpret_cast<const uint4 *>(unit + 512 * i + 16 * lane);
+    const float *scales = reinterpret_cast<const float *>(unit + 512 * BLOCKS) + (lane >> 2);
+    float s[SCALES][2], sum[SUMS][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+    for (int i = 0; i < SCALES; ++i) {
+        s[i][0] = scales[kStrip * i];
+        s[i][1] = scales[kStrip * i + 8];
+    }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[nt][i] = 0.0f;
-            uint32_t A[2][4];
-            widen<T>(j ? w.z : w.x, A[0]);
-            widen<T>(j ? w.w : w.y, A[1]);
+    for (int h = 0; h < 2 * BLOCKS; ++h) {                   // 32 inputs
+        const int of = SUMS == 1 ? 0 : BLOCKS == 2 ? h >> 1 : h;
+        const bool first = SUMS == 1 || BLOCKS == 1 ? h == 0 || SUMS == 2 : (h & 1) == 0;
+        uint32_t A[2][4];
+        widen<T>(h & 1 ? w[h >> 1].z : w[h >> 1].x, A[0]);
+        widen<T>(h & 1 ? w[h >> 1].w : w[h >> 1].y, A[1]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+        for (int part = kParts<T> - 1; part >= 0; --part) {
+            uint4 b[NT];
 #pragma unroll
-                for (int part = kParts<T> - 1; part >= 0; --part) {
-                    uint4 b = make_uint4(0, 0, 0, 0);
-                    if (8 * nt + g < live)
-                        b = *reinterpret_cast<const uint4 *>(x + 8 * nt * row_pitch + part * part_pitch + 128 * block + 64 * j);
-                    if constexpr (std::is_same<T, __half>::value) {
-                        mma(sum[nt], A[0], b.x, b.y);
-                        mma(sum[nt], A[1], b.z, b.w);
-                    } else {
-                        mma_bf16(sum[nt], A[0], b.x, b.y);
-                        mma_bf16(sum[nt], A[1], b.z, b.w);
-                    }
-                }
-            if (a.unit_scales == 2 || (j == 1 && block + 1 == a.unit_blocks)) {
-                const float *s = scales + (a.unit_scales == 2 ? kStrip * j : 0);
-                const float s0 = s[0], s1 = s[8];
+            for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4 *>(x + nt * next + part * part_pitch + 64 * h);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    total[nt][0] = fmaf(s0, sum[nt][0], total[nt][0]);
-                    total[nt][1] = fmaf(s0, sum[nt][1], total[nt][1]);
-                    total[nt][2] = fmaf(s1, sum[nt][2], total[nt][2]);
-                    total[nt][3] = fmaf(s1, sum[nt][3], total[nt][3]);
-                }
+            for (int nt = 0; nt < NT; ++nt) {
+                if (first && part == kParts<T> - 1) mma_first<kHalf>(sum[of][nt], A[0], b[nt].x, b[nt].y);
+                else mma_more<kHalf>(sum[of][nt], A[0], b[nt].x, b[nt].y);
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_more<kHalf>(sum[of][nt], A[1], b[nt].z, b[nt].w);
         }
     }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (SCALES == 2)
+                total[nt][i] = fmaf(s[SCALES - 1][i >> 1], sum[SUMS - 1][nt][i], fmaf(s[0][i >> 1], sum[0][nt][i], total[nt][i]));
+            else
+                total[nt][i] = fmaf(s[0][i >> 1], SUMS == 2 ? sum[0][nt][i] + sum[SUMS - 1][nt][i] : sum[0][nt][i], total[nt][i]);
+        }
 }
 
 // `ways` warps of the CTA share a strip's units; a CTA takes every gridDim.x-th set of strips.
-template <typename T, int NT>
-__global__ void __launch_bounds__(kCtaWarps * 32, NT == 1 ? 3 : 2) linear4_few(const Linear4Args a, int ways) {
-    constexpr int ROWS = 8 * NT, PITCH = kStrip + 4;
-    extern __shared__ __align__(128) uint8_t smem[];         // rings, sums of two strips, x
-    __shared__ __align__(8) uint64_t bars[kCtaWarps][kFewStages];
+template <typename T, int NT, int BLOCKS, int SCALES>
+__global__ void __launch_bounds__(kMostWarps * 32, 1) linear4_few(const Linear4Args a, int ways, int stages) {
+    constexpr int ROWS = 8 * NT, PITCH = kStrip + 4, UNIT = 512 * BLOCKS + 4 * kStrip * SCALES, STAGE_UNITS = 4 / BLOCKS;
+    constexpr int STAGE = STAGE_UNITS * UNIT;
+    const int warps = blockDim.x >> 5;
+    extern __shared__ __align__(128) uint8_t smem[];         // rings, sums of a strip, x
+    __shared__ __align__(8) uint64_t bars[kMostWarps][kFewStages];
     __shared__ int s_abort;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint8_t *ring = smem + warp * kFewStages * kStageBytes;
-    float *sums = reinterpret_cast<float *>(smem + kCtaWarps * kFewStages * kStageBytes);
-    uint8_t *xs = smem + kCtaWarps * kFewStages * kStageBytes + 2 * kCtaWarps * ROWS * PITCH * 4;
+    const uint8_t *ring = smem + warp * stages * STAGE;
+    float *sums = reinterpret_cast<float *>(smem + warps * stages * STAGE);
+    uint8_t *xs = smem + warps * stages * STAGE + warps * ROWS * PITCH * 4;
     const uint32_t bar = tc::smem_addr(bars[warp]);
     volatile int *abort_flag = &s_abort;
-    if (lane < kFewStages) tc::mbar_init(bar + 8 * lane, 1);
+    if (lane < stages) tc::mbar_init(bar + 8 * lane, 1);
     tc::fence_barrier_init();
     if (threadIdx.x == 0) s_abort = 0;
     __syncthreads();
     after_prior_kernels();
     const int err = *reinterpret_cast<volatile int *>(a.err);
 
-    const int sets = kCtaWarps / ways, way = warp % ways, set = warp / ways;
-    const int from = a.units * way / ways, to = a.units * (way + 1) / ways, per = (to - from + a.stage_units - 1) / a.stage_units;
+    const int sets = warps / ways, way = warp % ways, set = warp / ways;
+    const int from = a.units * way / ways, to = a.units * (way + 1) / ways, per = (to - from + STAGE_UNITS - 1) / STAGE_UNITS;
     const int step = gridDim.x * sets;
     // ---- this warp's copies: `per` a strip
-    int asked = 0, strip = blockIdx.x * sets + set, chunk = 0;
+    int asked = 0, ask_stage = 0, strip = blockIdx.x * sets + set, chunk = 0;
     auto ask = [&]() {
         if (strip >= a.strips) return;
         if (lane == 0) {
-            const int first = from + chunk * a.stage_units, n = min(a.stage_units, to - first), stage = asked % kFewStages;
-            tc::mbar_expect_tx(bar + 8 * stage, n * a.unit_bytes);
-            bulk_load(tc::smem_addr(ring + stage * kStageBytes), a.w + ((long long)strip * a.units + first) * a.unit_bytes, n * a.unit_bytes,
-                      bar + 8 * stage);
+            const int first = from + chunk * STAGE_UNITS, bytes = min(STAGE_UNITS, to - first) * UNIT;
+            tc::mbar_expect_tx(bar + 8 * ask_stage, bytes);
+            bulk_load(tc::smem_addr(ring + ask_stage * STAGE), a.w + ((long long)strip * a.units + first) * UNIT, bytes, bar + 8 * ask_stage);
         }
         ++asked;
+        if (++ask_stage == stages) ask_stage = 0;
         if (++chunk == per) {
             chunk = 0;
             strip += step;
         }
     };
-    for (int i = 0; i < kFewStages; ++i) ask();
+    for (int i = 0; i < stages; ++i) ask();
 
     // ---- x, behind its last input zeros
-    const int k_pad = a.units * a.unit_blocks * kStep, row_pitch = 2 * k_pad + 64, part_pitch = a.rows * row_pitch;
-    for (int row = warp; row < a.rows; row += kCtaWarps) {
+    const int k_pad = a.units * BLOCKS * kStep, row_pitch = 2 * k_pad + 64, part_pitch = a.rows * row_pitch;
+    for (int row = warp; row < a.rows; row += warps) {
         const T *p = static_cast<const T *>(a.x) + (long long)row * a.ldx;
         uint8_t *to_x = xs + row * row_pitch;
         if (a.vec && kParts<T> == 1) {
@@ -220,46 +221,51 @@ __global__ void __launch_bounds__(kCtaWarps * 32, NT == 1 ? 3 : 2) linear4_few(c
     asm volatile("cp.async.wait_all;" ::: "memory");
     bool sound = !__syncthreads_or(err != 0);
 
-    int done = 0, buffer = 0;
-    const int rounds = (a.strips + step - 1) / step;
-    const uint8_t *x = xs + min(g, a.rows - 1) * row_pitch + 16 * t;
+    int done = 0, stage = 0;
+    uint32_t parity = 0;
+    const int rounds = (a.strips + step - 1) / step, row = min(g, a.rows - 1), next = (min(g + 8, a.rows - 1) - row) * row_pitch;
+    const uint8_t *x = xs + row * row_pitch + 16 * t;
     for (int round = 0; round < rounds && sound; ++round) {
-        const int here = (round * (int)gridDim.x + (int)blockIdx.x) * sets + set;
+        const int strip_set = (round * (int)gridDim.x + (int)blockIdx.x) * sets;
         float total[NT][4] = {};
-        if (here < a.strips)
+        if (strip_set + set < a.strips)
             for (int c = 0; c < per; ++c) {
-                const int stage = done % kFewStages, first = from + c * a.stage_units, n = min(a.stage_units, to - first);
-                sound = __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * stage, (uint32_t)(done / kFewStages) & 1u, abort_flag, a.err));
+                const int first = from + c * STAGE_UNITS, n = min(STAGE_UNITS, to - first);
+                sound = __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * stage, parity, abort_flag, a.err));
                 if (!sound) break;
                 for (int i = 0; i < n; ++i)
-                    unit_products<T, NT>(a, ring + stage * kStageBytes + i * a.unit_bytes, x + (first + i) * a.unit_blocks * (2 * kStep),
-                                         row_pitch, part_pitch, a.rows, lane, total);
+                    unit_products<T, NT, BLOCKS, SCALES>(ring + stage * STAGE + i * UNIT, x + (first + i) * (BLOCKS * 2 * kStep), next, part_pitch,
+                                                         lane, total);
                 __syncwarp();
                 ++done;
+                if (++stage == stages) {
+                    stage = 0;
+                    parity ^= 1;
+                }
                 ask();
             }
         // ---- the warps' sums
-        float *mine = sums + (buffer * kCtaWarps + warp) * ROWS * PITCH;
+        float *mine = sums + warp * ROWS * PITCH;
+        if (round) __syncthreads();                          // (the last ones are read)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) mine[(8 * nt + 2 * t + (i & 1)) * PITCH + g + (i >> 1) * 8] = total[nt][i];
         sound = !__syncthreads_or(!sound);
-        for (int i = threadIdx.x; sound && i < a.rows * kStrip * sets; i += kCtaWarps * 32) {
-            const int ch = i % kStrip, of = i / kStrip % sets, row = i / (kStrip * sets);
-            const int n = ((round * (int)gridDim.x + (int)blockIdx.x) * sets + of) * kStrip + ch;
+        for (int i = threadIdx.x; sound && i < a.rows * kStrip * sets; i += blockDim.x) {
+            const int ch = i % kStrip, r = i / kStrip % a.rows, of = i / (kStrip * a.rows), n = (strip_set + of) * kStrip + ch;
             if (n >= a.n) continue;
-            const float *p = sums + (buffer * kCtaWarps + of * ways) * ROWS * PITCH + row * PITCH + ch;
+            const float *p = sums + of * ways * ROWS * PITCH + r * PITCH + ch;
             float v = 0.0f;
+#pragma unroll 8
             for (int j = 0; j < ways; ++j) v += p[j * ROWS * PITCH];
-            store_y(a, row, n, v);
+            store_y(a, r, n, v);
         }
-        buffer ^= 1;
     }
     // copies still on their way (where a wait gave up) have to land before the CTA leaves
     const long long t0 = clock64();
     for (int i = done; i < asked; ++i)
-        while (!tc::mbar_try_wait(bar + 8 * (i % kFewStages), (uint32_t)(i / kFewStages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
+        while (!tc::mbar_try_wait(bar + 8 * (i % stages), (uint32_t)(i / stages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
 }
 
 constexpr int kManyDepth = 128;        // inputs of a piece of x
@@ -269,10 +275,10 @@ constexpr int kManyStages = 4;
 template <typename T> constexpr int kXStages = std::is_same<T, float>::value ? 2 : 3;
 
 // A warp per strip, 8 strips a CTA, NT tiles of 8 rows; the CTAs of a cluster (along z) have a part of the inputs each.
-template <typename T, int NT>
-__global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(const Linear4Args a, int split) {
+template <typename T, int NT, int BLOCKS, int SCALES>
+__global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4Args a, int split) {
     constexpr int ROWS = 8 * NT, PARTS = kParts<T>, XS = kXStages<T>, PART = ROWS * kManyPitch, XSTAGE = PARTS * PART;
-    constexpr int PITCH = kCtaWarps * kStrip + 4;
+    constexpr int PITCH = kCtaWarps * kStrip + 4, UNIT = 512 * BLOCKS + 4 * kStrip * SCALES, PIECE_UNITS = 2 / BLOCKS;
     extern __shared__ __align__(128) uint8_t smem[];         // rings, x; in the end the CTA's sums
     __shared__ __align__(8) uint64_t bars[kCtaWarps][kManyStages];
     __shared__ int s_abort;
@@ -290,12 +296,11 @@ __global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(
 
     const int strip = min((int)blockIdx.x * kCtaWarps + warp, a.strips - 1), row0 = blockIdx.y * ROWS, live = min(ROWS, a.rows - row0);
     const int pieces = (a.k + kManyDepth - 1) / kManyDepth, from = pieces * (int)blockIdx.z / split, to = pieces * ((int)blockIdx.z + 1) / split;
-    const int piece_units = kManyDepth / (kStep * a.unit_blocks);
     auto ask = [&](int i) {
         if (i >= to - from || lane) return;
-        const int first = (from + i) * piece_units, n = min(piece_units, a.units - first), stage = i % kManyStages;
-        tc::mbar_expect_tx(bar + 8 * stage, n * a.unit_bytes);
-        bulk_load(tc::smem_addr(ring + stage * kManyRing), a.w + ((long long)strip * a.units + first) * a.unit_bytes, n * a.unit_bytes,
+        const int first = (from + i) * PIECE_UNITS, n = min(PIECE_UNITS, a.units - first), stage = i % kManyStages;
+        tc::mbar_expect_tx(bar + 8 * stage, n * UNIT);
+        bulk_load(tc::smem_addr(ring + stage * kManyRing), a.w + ((long long)strip * a.units + first) * UNIT, n * UNIT,
                   bar + 8 * stage);
     };
     // Pieces of x, zeros behind the last row and input. As they lie, by asynchronous copies; otherwise through registers.
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(
     float total[NT][4] = {};
     int done = 0;
     for (; sound && done < to - from; ++done) {
-        const int stage = done % kManyStages, n = min(piece_units, a.units - (from + done) * piece_units);
+        const int stage = done % kManyStages, n = min(PIECE_UNITS, a.units - (from + done) * PIECE_UNITS);
         asm volatile("cp.async.wait_group %0;" ::"n"(XS - 2) : "memory");
         const bool here = tc::mbar_wait(bar + 8 * stage, (uint32_t)(done / kManyStages) & 1u, abort_flag, a.err);
         sound = !__syncthreads_or(!here);
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(
         bring(done + XS - 1);
         const uint8_t *x = xs + done % XS * XSTAGE + g * kManyPitch + 16 * t;
         for (int i = 0; i < n; ++i)
-            unit_products<T, NT>(a, ring + stage * kManyRing + i * a.unit_bytes, x + i * a.unit_blocks * (2 * kStep), kManyPitch, PART, ROWS, lane, total);
+            unit_products<T, NT, BLOCKS, SCALES>(ring + stage * kManyRing + i * UNIT, x + i * (BLOCKS * 2 * kStep), 8 * kManyPitch, PART, lane, total);
         __syncwarp();
         ask(done + kManyStages);
     }
@@ -391,23 +396,51 @@ __global__ void __launch_bounds__(kCtaWarps * 32, NT == 8 ? 1 : 2) linear4_many(
     if (split > 1) asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
 
-template <typename T, int NT>
-cudaError_t launch_few(const Linear4Args &a, int x_bytes, int sms, cudaStream_t s) {
-    static std::atomic<int> allowed[64];
-    const int bytes = kCtaWarps * kFewStages * kStageBytes + 2 * kCtaWarps * 8 * NT * (kStrip + 4) * 4 + x_bytes;
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_few<T, NT>), bytes, allowed);
-    if (e != cudaSuccess) return e;
-    const int ways = a.units >= 8 ? 8 : a.units >= 4 ? 4 : a.units >= 2 ? 2 : 1, sets = kCtaWarps / ways;
-    const int resident = max(1, min(3, 220 * 1024 / (bytes + 1024))), all = (a.strips + sets - 1) / sets;
-    return launch_early(linear4_few<T, NT>, dim3((unsigned)min(all, sms * resident)), kCtaWarps * 32, bytes, s, a, ways);
+// What a CTA of the few-row kernel has: warps, stages, bytes of shared memory.
+struct FewPlan {
+    int warps, ways, stages, bytes, ctas;
+};
+bool plan_few(const Linear4Args &a, long long x_bytes, int tiles, int sms, FewPlan &p) {
+    const int stage = a.stage_units * a.unit_bytes;
+    auto bytes = [&](int warps, int stages) { return warps * stages * stage + warps * 8 * tiles * (kStrip + 4) * 4 + x_bytes; };
+    constexpr long long most = 226 * 1024;
+    // two CTAs of 8 warps on an SM, or one of 16, or of 8
+    p.stages = kFewStages;
+    if (bytes(8, 3) <= most / 2) p.warps = 8;
+    else if (bytes(16, 3) <= most) p.warps = 16;
+    else if (bytes(16, 2) <= most) p.warps = 16, p.stages = 2;
+    else if (bytes(8, 3) <= most) p.warps = 8;
+    else return false;
+    p.bytes = (int)bytes(p.warps, p.stages);
+    // how many warps share a strip: the least time, in units: rounds over the strips, each with about one and a half for
+    // the sums and the barrier (16 rows of 4096 x 16384: XXX)
+    const int resident = p.warps == 16 ? 1 : max(1, min(3, 227 * 1024 / (p.bytes + 1024)));
+    long long best = LLONG_MAX;
+    for (int ways = 1; ways <= p.warps && ways <= a.units; ways *= 2) {
+        const long long sets = p.warps / ways, ctas = (a.strips + sets - 1) / sets, room = (long long)sms * resident;
+        const long long cost = (ctas + room - 1) / room * (2 * ((a.units + ways - 1) / ways) + 3);
+        if (cost < best) {
+            best = cost;
+            p.ways = ways;
+            p.ctas = (int)min(ctas, room);
+        }
+    }
+    return true;
 }
-template <typename T, int NT>
+template <typename T, int NT, int BLOCKS, int SCALES>
+cudaError_t launch_few(const Linear4Args &a, const FewPlan &p, cudaStream_t s) {
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_few<T, NT, BLOCKS, SCALES>), p.bytes, allowed);
+    if (e != cudaSuccess) return e;
+    return launch_early(linear4_few<T, NT, BLOCKS, SCALES>, dim3((unsigned)p.ctas), p.warps * 32, p.bytes, s, a, p.ways, p.stages);
+}
+template <typename T, int NT, int BLOCKS, int SCALES>
 cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     static std::atomic<int> allowed[64];
     constexpr int x_bytes = kXStages<T> * kParts<T> * 8 * NT * kManyPitch, sum_bytes = 8 * NT * (kCtaWarps * kStrip + 4) * 4;
     constexpr int ring = kCtaWarps * kManyStages * kManyRing, bytes = ring + x_bytes > sum_bytes ? ring + x_bytes : sum_bytes;
     static_assert(bytes <= 226 * 1024, "shared memory of a CTA");
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_many<T, NT>), bytes, allowed);
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_many<T, NT, BLOCKS, SCALES>), bytes, allowed);
     if (e != cudaSuccess) return e;
     const int tiles = (a.strips + kCtaWarps - 1) / kCtaWarps, row_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
     const int pieces = (a.k + kManyDepth - 1) / kManyDepth;
@@ -415,7 +448,7 @@ cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     int split = 1;
     long long best = LLONG_MAX;
     for (int x = 1; x <= 8 && x <= pieces; x *= 2) {
-        const long long ctas = (long long)tiles * row_tiles * x, cost = (ctas + sms - 1) / sms * ((pieces + x - 1) / x) + (x > 1 ? 3 : 0);
+        const long long ctas = (long long)tiles * row_tiles * x, room = 2LL * sms, cost = (ctas + room - 1) / room * ((pieces + x - 1) / x) + (x > 1 ? 3 : 0);
         if (cost < best) {
             best = cost;
             split = x;
@@ -432,14 +465,21 @@ cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, linear4_many<T, NT>, a, split);
+    return cudaLaunchKernelEx(&cfg, linear4_many<T, NT, BLOCKS, SCALES>, a, split);
+}
+template <typename T, int BLOCKS, int SCALES>
+cudaError_t launch_units(const Linear4Args &a, int sms, cudaStream_t s) {
+    const long long x_bytes = (long long)kParts<T> * a.rows * (2LL * a.units * BLOCKS * kStep + 64);
+    FewPlan p;
+    if (a.rows <= 16 && plan_few(a, x_bytes, a.rows <= 8 ? 1 : 2, sms, p))
+        return a.rows <= 8 ? launch_few<T, 1, BLOCKS, SCALES>(a, p, s) : launch_few<T, 2, BLOCKS, SCALES>(a, p, s);
+    return a.rows <= 16   ? launch_many<T, 2, BLOCKS, SCALES>(a, sms, s)
+           : a.rows <= 32 ? launch_many<T, 4, BLOCKS, SCALES>(a, sms, s)
+                          : launch_many<T, 8, BLOCKS, SCALES>(a, sms, s);
 }
 template <typename T>
 cudaError_t launch_type(const Linear4Args &a, int sms, cudaStream_t s) {
-    const long long x_bytes = (long long)kParts<T> * a.rows * (2LL * a.units * a.unit_blocks * kStep + 64);
-    if (a.rows <= 16 && x_bytes <= 140 * 1024)
-        return a.rows <= 8 ? launch_few<T, 1>(a, (int)x_bytes, sms, s) : launch_few<T, 2>(a, (int)x_bytes, sms, s);
-    return a.rows <= 16 ? launch_many<T, 2>(a, sms, s) : a.rows <= 32 ? launch_many<T, 4>(a, sms, s) : launch_many<T, 8>(a, sms, s);
+    return a.unit_blocks == 2 ? launch_units<T, 2, 1>(a, sms, s) : a.unit_scales == 1 ? launch_units<T, 1, 1>(a, sms, s) : launch_units<T, 1, 2>(a, sms, s);
 }
 
 // A warp per strip and 64 inputs: lane (g, t) packs channels g and g + 8 (the first in the lower of two nibbles) at inputs
