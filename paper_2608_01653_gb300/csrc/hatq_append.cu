@@ -1,4 +1,6 @@
 // Keys and values of new tokens into the 4-bit cache.
+#include <type_traits>
+
 #include "hatq_cache.h"
 
 namespace hatq {
@@ -8,130 +10,208 @@ namespace {
 //
 // The code is the rounding of the correctly rounded quotient (7 t) / a, so that whoever computes t alike gets the same
 // codes. A multiplication by 7 / a gives the same but near the middle of two codes: both lie within 7 * 4 * 2^-24 <
-// 2^-19 of 7 t / a, so only what comes within 2^-18 of a middle is divided.
+// 2^-19 of 7 t / a, so where a value of the lane comes within 2^-18 of a middle the lane divides.
 //
-// Memory-bound: the values' bytes. A lane owns 8 neighbouring values (16 bytes of a 16-bit type in, one word of codes
-// out), LANES lanes a head; blocks wider than 8 cost one lane exchange per doubling.
-__device__ __forceinline__ float code_of(float t, float a, float inv) {
-    const float c = t * inv;
-    float r = rintf(c);
-    if (fabsf(fabsf(c - r) - 0.5f) < 0x1p-18f) r = rintf(__fdiv_rn(7.0f * t, a));
-    return r;
-}
-
+// The values' bytes are the floor, but instructions come first: about 25 a value, of which the transform takes 9. A warp
+// has 8 heads, lane (g, t) of head g the values 64 c + 16 t .. + 15, so that 4 of 6 doublings (distances 16 and 32 are the
+// exceptions) stay within a lane. What the cache now stands for is transformed back in pairs of fp16: sums of codes are
+// whole numbers below 2^11, exact.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, float (&v)[8]) {
+__device__ __forceinline__ void load16(const T *p, bool vec, float *v) {
     if (vec) {
-        union { uint4 u[sizeof(T) / 2]; T t[8]; } x;
+        union { uint4 u[sizeof(T)]; T t[16]; } x;
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) x.u[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+        for (int i = 0; i < (int)sizeof(T); ++i) x.u[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(x.t[i]);
+        for (int i = 0; i < 16; ++i) v[i] = to_f32<T>(x.t[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(p[i]);
+        for (int i = 0; i < 16; ++i) v[i] = to_f32<T>(p[i]);
     }
 }
 
-// neighbours first: distances 1, 2, 4 within the lane, then 8, 16, ... between lanes
-template <int LANES>
-__device__ __forceinline__ void transform(float (&v)[8], int hb, int lane) {
+// neighbours first: distances 1 .. 8 within the lane, 16 and 32 between lanes, 64 and 128 between a lane's runs of 16
+template <int N>
+__device__ __forceinline__ void transform(float (&v)[N], int hb, int t) {
 #pragma unroll
-    for (int h = 1; h < 8; h *= 2)
+    for (int h = 1; h < 16; h *= 2)
         if (h < hb)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < N; ++i)
                 if (!(i & h)) {
                     const float a = v[i], b = v[i + h];
                     v[i] = a + b;
                     v[i + h] = a - b;
                 }
 #pragma unroll
-    for (int h = 1; h < LANES; h *= 2)
-        if (8 * h < hb)
+    for (int h = 1; h < 4; h *= 2)
+        if (16 * h < hb) {
+            const float sign = t & h ? -1.0f : 1.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float o = __shfl_xor_sync(0xffffffffu, v[i], h);
-                v[i] = lane & h ? o - v[i] : v[i] + o;
-            }
+            for (int i = 0; i < N; ++i) v[i] = fmaf(sign, v[i], __shfl_xor_sync(0xffffffffu, v[i], h));
+        }
+#pragma unroll
+    for (int h = 16; h < N; h *= 2)
+        if (4 * h < hb)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (!(i & h) && i + h < N) {
+                    const float a = v[i], b = v[i + h];
+                    v[i] = a + b;
+                    v[i + h] = a - b;
+                }
 }
 
-template <typename T, int LANES>
+// the same of whole numbers in pairs (2 i, 2 i + 1)
+template <int N>
+__device__ __forceinline__ void transform_pairs(__half2 (&v)[N / 2], int hb, int t) {
+    if (hb > 1) {
+        const __half2 sign = __halves2half2(__float2half_rn(1.0f), __float2half_rn(-1.0f));
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v[i] = __hfma2(v[i], sign, __lowhigh2highlow(v[i]));
+    }
+#pragma unroll
+    for (int h = 1; h < 8; h *= 2)
+        if (2 * h < hb)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                if (!(i & h)) {
+                    const __half2 a = v[i], b = v[i + h];
+                    v[i] = __hadd2(a, b);
+                    v[i + h] = __hsub2(a, b);
+                }
+#pragma unroll
+    for (int h = 1; h < 4; h *= 2)
+        if (16 * h < hb) {
+            const __half2 sign = __float2half2_rn(t & h ? -1.0f : 1.0f);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) v[i] = __hfma2(sign, v[i], __shfl_xor_sync(0xffffffffu, v[i], h));
+        }
+#pragma unroll
+    for (int h = 8; h < N / 2; h *= 2)
+        if (8 * h < hb)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+                if (!(i & h) && i + h < N / 2) {
+                    const __half2 a = v[i], b = v[i + h];
+                    v[i] = __hadd2(a, b);
+                    v[i + h] = __hsub2(a, b);
+                }
+}
+
+// C runs of 16 values a lane: heads of 64 C. Keys where blockIdx.y is 0, values where it is 1.
+template <typename T, int C>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
-    constexpr int kUnits = 32 / LANES;                       // (head, key or value) pairs of a warp
+    constexpr int N = 16 * C;
     after_prior_kernels();
     const CacheArgs &c = a.c;
-    const int lane = threadIdx.x & 31, mine = lane % LANES;
-    const int per_row = (2 * c.heads + kUnits - 1) / kUnits; // warps of a row
-    const long long warp = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int r = (int)(warp / per_row);
-    if (r >= c.rows) return;
-    const int unit = (int)(warp % per_row) * kUnits + lane / LANES;
-    const bool live = unit < 2 * c.heads && 8 * mine < c.width;
-    const int part = unit & 1, head = unit >> 1;
-    float v[8];
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, part = blockIdx.y;
+    const long long heads = (long long)c.rows * c.heads, first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 8;
+    if (first >= heads) return;
+    const bool live = first + g < heads;
+    const uint32_t unit = (uint32_t)(live ? first + g : heads - 1);
+    const int r = (int)(unit / (uint32_t)c.heads), head = (int)(unit - (uint32_t)r * c.heads);
+    float v[N];
+    const T *x = static_cast<const T *>(a.x[part]) + r * a.ldx[part] + head * a.hx[part] + 16 * t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    if (live) load8(static_cast<const T *>(a.x[part]) + r * a.ldx[part] + head * a.hx[part] + 8 * mine, a.vec, v);
-    int b, begin, end;
-    if (!sequence_of(c, r, lane, b, begin, end)) return;
-    const int at = length_of(c, b) - end + r;
-    int page = -1;
-    if (at >= 0) page = c.table[b * c.ldt + (at >> c.page_bits)];      // at < length <= capacity
+    for (int i = 0; i < C; ++i) load16(x + 64 * i, a.vec, v + 16 * i);
+    // ---- the row's place: at in its sequence, and the page there
+    int b = r, at = -1, page = -1;
+    bool held = live;
+    if (c.starts) {
+        held = false;
+        const int last = __shfl_sync(0xffffffffu, r, 31);
+        for (int row = __shfl_sync(0xffffffffu, r, 0); row <= last; ++row) {
+            int of, begin, end;
+            if (sequence_of(c, row, lane, of, begin, end) && row == r && live) {
+                held = true;
+                b = of;
+                at = row - end;
+            }
+        }
+    }
+    if (held) {
+        at += length_of(c, b);
+        if (at >= 0) page = c.table[b * c.ldt + (at >> c.page_bits)];            // at < length <= capacity
+    }
 
-    transform<LANES>(v, c.hb, lane);
+    transform<N>(v, c.hb, t);
     float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
         most = fmaxf(most, fabsf(v[i]));
         if (v[i] != v[i]) most = __int_as_float(0x7f800000);
     }
 #pragma unroll
-    for (int h = 1; h < LANES; h *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, h));
+    for (int h = 1; h < 4; h *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, h));
     const bool sound = 7.0f * most < __int_as_float(0x7f800000), some = sound && most > 0.0f;
     // (7 / a overflows where a is subnormal: every value is then divided)
-    const float inv = 7.0f / most;
-    const bool fast = inv < __int_as_float(0x7f800000);
-    uint32_t word = 0x88888888u;
-    float n[8];
+    const float inv = some ? 7.0f / most : 0.0f;
+    float worst = inv < __int_as_float(0x7f800000) ? 0.0f : 1.0f;
+    float n[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) n[i] = 0.0f;
-    if (some) {
-        word = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            n[i] = fast ? code_of(v[i], most, inv) : rintf(__fdiv_rn(7.0f * v[i], most));
-            word |= (uint32_t)((int)n[i] + 8) << (4 * i);
-        }
+    for (int i = 0; i < N; ++i) {
+        const float q = v[i] * inv;
+        n[i] = rintf(q);
+        worst = fmaxf(worst, fabsf(q - n[i]));
     }
+    if (some && worst > 0.5f - 0x1p-18f)
+#pragma unroll
+        for (int i = 0; i < N; ++i) n[i] = rintf(__fdiv_rn(7.0f * v[i], most));
+    if (!some)
+#pragma unroll
+        for (int i = 0; i < N; ++i) n[i] = 0.0f;
     const float step = !sound ? __int_as_float(0x7fffffff) : some ? __fdiv_rn(most, 7.0f) * c.inv_norm : c.inv_norm;
-    if (live && page >= 0 && page < c.pages) {
-        const int size = 1 << c.page_bits, slot = at & (size - 1), half = c.width / 2;
-        uint8_t *rec = c.data + ((long long)page * c.heads + head) * size * (c.width + 8);
-        *reinterpret_cast<uint32_t *>(rec + (part * size + slot) * half + 4 * mine) = word;
-        if (mine == 0) *reinterpret_cast<float *>(rec + size * c.width + 4 * (part * size + slot)) = step;
+    if (held && page >= 0 && page < c.pages) {
+        const int size = 1 << c.page_bits, slot = at & (size - 1);
+        uint8_t *rec = c.data + ((long long)page * c.heads + head) * size * (64 * C + 8);
+        uint2 *words = reinterpret_cast<uint2 *>(rec + (part * size + slot) * (32 * C) + 8 * t);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            // four codes + 8 at a time as a number below 2^16, exact in fp32
+            uint32_t q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float *m = n + 16 * i + 4 * j;
+                q[j] = (uint32_t)fmaf(m[3], 4096.0f, fmaf(m[2], 256.0f, fmaf(m[1], 16.0f, m[0] + 34952.0f)));
+            }
+            words[4 * i] = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+        }
+        if (t == 0) *reinterpret_cast<float *>(rec + size * (64 * C) + 4 * (part * size + slot)) = step;
     }
     if (!a.kept[part]) return;
-    // what the cache now stands for: the codes' transform is an integer, exact
-    transform<LANES>(n, c.hb, lane);
-    if (!live) return;
+    // ---- what the cache now stands for
+    __half2 pairs[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) pairs[i] = __floats2half2_rn(n[2 * i], n[2 * i + 1]);
+    transform_pairs<N>(pairs, c.hb, t);
+    if (!held) return;
     const float back = step * c.inv_norm;
-    T *kept = static_cast<T *>(a.kept[part]) + ((long long)r * c.heads + head) * c.width + 8 * mine;
-    union { uint4 u[sizeof(T) / 2]; T t[8]; } y;
+    T *kept = static_cast<T *>(a.kept[part]) + ((long long)r * c.heads + head) * (64 * C) + 16 * t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y.t[i] = from_f32<T>(n[i] * back);
+    for (int i = 0; i < C; ++i) {
+        union { uint4 u[sizeof(T)]; T t[16]; } y;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(kept)[i] = y.u[i];
+        for (int j = 0; j < 8; ++j) {
+            const float2 f = __half22float2(pairs[8 * i + j]);
+            y.t[2 * j] = from_f32<T>(f.x * back);
+            y.t[2 * j + 1] = from_f32<T>(f.y * back);
+        }
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4 *>(kept + 64 * i)[j] = y.u[j];
+    }
 }
 
-template <typename T, int LANES>
+template <typename T, int C>
 cudaError_t launch(const AppendArgs &a, cudaStream_t s) {
-    const long long warps = (long long)a.c.rows * ((2 * a.c.heads + 32 / LANES - 1) / (32 / LANES));
-    return launch_early(append_kernel<T, LANES>, dim3((unsigned)((warps + 7) / 8)), 256, 0, s, a);
+    return launch_early(append_kernel<T, C>, dim3((unsigned)(((long long)a.c.rows * a.c.heads + 63) / 64), 2), 256, 0, s, a);
 }
 template <typename T>
 cudaError_t launch_type(const AppendArgs &a, cudaStream_t s) {
-    return a.c.width <= 64 ? launch<T, 8>(a, s) : a.c.width <= 128 ? launch<T, 16>(a, s) : launch<T, 32>(a, s);
+    return a.c.width == 64    ? launch<T, 1>(a, s)
+           : a.c.width == 128 ? launch<T, 2>(a, s)
+           : a.c.width == 192 ? launch<T, 3>(a, s)
+                              : launch<T, 4>(a, s);
 }
 
 }  // namespace
