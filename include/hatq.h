@@ -714,7 +714,7 @@ hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, lon
  * Results do not depend on timing; they may differ in the last bits with the
  * number of SMs and with what else is in the call. Stream-ordered; an expired
  * device wait surfaces through hatq_sync_status(). */
-hatq_status hatq_attend_workspace(const hatq_token_cache *cache, int q_heads, long long rows, int seqs, int starts,
+hatq_status hatq_attend_workspace(const hatq_token_cache *cache, int type, int q_heads, long long rows, int seqs, int starts,
                                   int table_width, size_t *bytes);
 hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long hq, int q_heads, long long rows,
                                const hatq_token_cache *cache, const int32_t *table, long long ldt, int table_width,

@@ -21,10 +21,10 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libhatq.so")
 SOURCES = ["hatq_api.cu", "hatq_fwht.cu", "hatq_conv.cu", "hatq_conv_pieces.cu", "hatq_gdn.cu", "hatq_noalloc.cu",
            "hatq_profile.cu", "hatq_tokens.cu", "hatq_linear.cu", "hatq_tokens_api.cu", "hatq_append.cu",
-           "hatq_attend.cu", "hatq_cache_api.cu", "hatq_linear4.cu", "hatq_linear4_api.cu"]
+           "hatq_attend.cu", "hatq_prompt.cu", "hatq_cache_api.cu", "hatq_linear4.cu", "hatq_linear4_api.cu"]
 HEADERS = [os.path.join(CSRC, "hatq_internal.h"), os.path.join(CSRC, "hatq_tc.h"),
            os.path.join(CSRC, "hatq_tokens.h"), os.path.join(CSRC, "hatq_host.h"),
-           os.path.join(CSRC, "hatq_cache.h"), os.path.join(CSRC, "hatq_mma4.h"), os.path.join(CSRC, "hatq_linear4.h"),
+           os.path.join(CSRC, "hatq_cache.h"), os.path.join(CSRC, "hatq_mma4.h"), os.path.join(CSRC, "hatq_sequences.h"), os.path.join(CSRC, "hatq_linear4.h"),
            os.path.join(INCLUDE, "hatq.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -45,7 +45,8 @@ struct AttendArgs {
     float scale;                       // times log2(e): weights are powers of two
     float *pieces;
     long long segments;                // (sequence, head, tile): upper bound
-    bool direct;
+    bool direct, prompt;
+    bool vec_out;                      // rows of out lie on 16-byte boundaries
     int sms;
     int *err;
 };
@@ -55,6 +56,10 @@ int attend_workers(int width, int sms);
 // joins)
 bool attend_direct(int width, long long segments, int capacity, int sms);
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s);
+
+constexpr int kPromptColumns = 256;    // of a CTA of the kernel for many queries per sequence
+bool attend_prompt(int type, int width, int heads, int group, long long rows, int seqs, int sms);
+cudaError_t launch_prompt(const AttendArgs &a, cudaStream_t s);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ int length_of(const CacheArgs &c, int b) {

@@ -89,10 +89,11 @@ Heads whole(const hatq_token_cache *c) {
     return {c->data, c->pages, (long long)c->heads * c->page * (c->width + 8), 1, 0, (long long)c->heads * c->page * (c->width + 8), 1};
 }
 
-hatq_status attend_args(const hatq_token_cache *c, int q_heads, long long rows, int table_width, int seqs, bool starts,
+hatq_status attend_args(const hatq_token_cache *c, int type, int q_heads, long long rows, int table_width, int seqs, bool starts,
                         hatq::AttendArgs &a) {
     hatq_status st = check_cache(c);
     if (st != HATQ_OK || (st = check_sizes(c, rows, table_width, seqs, starts, a.c)) != HATQ_OK) return st;
+    if (type != HATQ_F16 && type != HATQ_BF16) return fail(HATQ_ERR_INVALID_ARG, "queries are fp16 or bf16, not type %d", type);
     if (q_heads < 1 || q_heads % c->heads) return fail(HATQ_ERR_INVALID_ARG, "the query heads are no multiple of the cache's");
     if (q_heads > 16 * kMaxHeads) return fail(HATQ_ERR_UNSUPPORTED, "at most %d query heads", 16 * kMaxHeads);
     if (rows * q_heads > kMaxRows) return fail(HATQ_ERR_UNSUPPORTED, "at most 2^31 - 1024 rows x heads per call");
@@ -105,9 +106,10 @@ hatq_status attend_args(const hatq_token_cache *c, int q_heads, long long rows, 
     return HATQ_OK;
 }
 // once a.sms is set
-size_t attend_bytes(hatq::AttendArgs &a) {
+size_t attend_bytes(hatq::AttendArgs &a, int type) {
+    a.prompt = hatq::attend_prompt(type, a.c.width, a.c.heads, a.group, a.c.rows, a.c.seqs, a.sms);
     a.direct = hatq::attend_direct(a.c.width, a.segments, a.c.capacity, a.sms);
-    return a.direct ? 0 : ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
+    return a.prompt || a.direct ? 0 : ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
 }
 
 }  // namespace
@@ -151,16 +153,16 @@ hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, lon
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "append launch");
 }
 
-hatq_status hatq_attend_workspace(const hatq_token_cache *cache, int q_heads, long long rows, int seqs, int starts,
+hatq_status hatq_attend_workspace(const hatq_token_cache *cache, int type, int q_heads, long long rows, int seqs, int starts,
                                   int table_width, size_t *bytes) {
     hatq::AttendArgs a{};
     if (!bytes) return fail(HATQ_ERR_INVALID_ARG, "null output");
-    const hatq_status st = attend_args(cache, q_heads, rows, table_width, seqs, starts != 0, a);
+    const hatq_status st = attend_args(cache, type, q_heads, rows, table_width, seqs, starts != 0, a);
     if (st != HATQ_OK) return st;
     *bytes = 0;
     if (rows == 0 || seqs == 0) return HATQ_OK;
     if (!(a.sms = sm_count())) return fail(HATQ_ERR_CUDA, "no CUDA device");
-    *bytes = attend_bytes(a);
+    *bytes = attend_bytes(a, type);
     return HATQ_OK;
 }
 
@@ -169,9 +171,8 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
                                const int32_t *lengths, const int32_t *starts, int seqs, float scale, void *out,
                                long long ldo, long long ho, void *workspace, size_t workspace_bytes, hatq_stream stream) {
     hatq::AttendArgs a{};
-    hatq_status st = attend_args(cache, q_heads, rows, table_width, seqs, starts != nullptr, a);
+    hatq_status st = attend_args(cache, type, q_heads, rows, table_width, seqs, starts != nullptr, a);
     if (st != HATQ_OK) return st;
-    if (type != HATQ_F16 && type != HATQ_BF16) return fail(HATQ_ERR_INVALID_ARG, "queries are fp16 or bf16, not type %d", type);
     if (!std::isfinite(scale)) return fail(HATQ_ERR_INVALID_ARG, "the scale is not finite");
     if (rows == 0 || seqs == 0) return HATQ_OK;
     if ((st = check_sequences(table, ldt, lengths, starts, a.c)) != HATQ_OK) return st;
@@ -180,7 +181,7 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     if (overlap(in, to)) return fail(HATQ_ERR_INVALID_ARG, "q and out overlap");
     if (overlap(to, whole(cache))) return fail(HATQ_ERR_INVALID_ARG, "out and the cache overlap");
     if (!(a.sms = sm_count())) return fail(HATQ_ERR_CUDA, "no CUDA device");
-    const size_t bytes = attend_bytes(a);
+    const size_t bytes = attend_bytes(a, type);
     if (bytes && (!workspace || !aligned(workspace, 16))) return fail(HATQ_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
     if (workspace_bytes < bytes) return fail(HATQ_ERR_INVALID_ARG, "the workspace is too small");
     a.err = hatq::device_error_word();
@@ -192,9 +193,11 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     a.out = out;
     a.ldo = ldo;
     a.ho = ho;
+    a.vec_out = aligned(out, 16) && ldo % 8 == 0 && ho % 8 == 0;
     a.scale = scale * 1.44269504088896340736f;
     a.pieces = static_cast<float *>(workspace);
-    const cudaError_t e = hatq::launch_attend(a, type, reinterpret_cast<cudaStream_t>(stream));
+    const cudaStream_t on = reinterpret_cast<cudaStream_t>(stream);
+    const cudaError_t e = a.prompt ? hatq::launch_prompt(a, on) : hatq::launch_attend(a, type, on);
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "attention launch");
 }
 

@@ -1,0 +1,522 @@
+// Attention over the 4-bit cache for many queries per sequence, on the fifth-generation tensor cores.
+#include "hatq_cache.h"
+#include "hatq_mma4.h"
+#include "hatq_sequences.h"
+#include "hatq_tc.h"
+
+namespace hatq {
+namespace {
+
+using tc::mbar_arrive;
+using tc::mbar_expect_tx;
+using tc::mbar_init;
+using tc::mbar_wait;
+using tc::smem_addr;
+
+// The formulas of hatq_attend.cu for two tiles of 128 query columns of a kv head at a time: S = Q K^T (128 x 64 keys),
+// O += P V (128 x D), Q and P in tensor memory, codes widened once for both tiles into shared memory. bf16 queries only:
+// rounded to fp16 are q and p as there, and here also code times scale of keys and of values (an error of 2^-12 each,
+// against 2^-9 of the output), so that a logit costs one instruction less than it would with a factor of its key.
+//
+// Scales are brought into fp16's range by powers of two: those of a chunk's keys by the largest of them, whose exponent
+// goes into the logits' factor; those of values by the largest so far, and O is scaled where that grows. A token whose
+// scales are not finite gets values of 0 and keys of NaN, so that it makes NaN exactly of the rows that see it (0 times NaN
+// in a masked place would do so of all).
+//
+// Roles: 4 warps per tile have a row a thread (transform of the query, softmax, transform back), 4 warps widen chunks of 64
+// keys, one brings them in, one issues the MMAs: PV of a tile, then S of its next chunk, which may overwrite P. While one
+// tile's rows are at their softmax, the tensor cores are at the other's.
+//
+// Bound by instructions and the tensor cores about alike: per chunk and two tiles 1024 cycles of MMA, 820 issue slots of
+// each scheduler.
+constexpr int kRaw = 4;                // chunks on their way or being widened
+constexpr int kPromptThreads = 14 * 32;
+
+template <int D>
+struct Shape {
+    static constexpr int kChunkBytes = kChunk * (D + 8), kK = kChunk * D * 2, kKV = 2 * kK;
+    static constexpr int kO = 0, kQ = 2 * D, kS = 3 * D;     // columns of tensor memory: two tiles each of D, D / 2, 64
+    static constexpr int kBytes = 1024 + 2 * kKV + kRaw * kChunkBytes;
+};
+
+struct Info {                          // of a widened chunk, for the rows
+    float k_factor, v_ratio;           // 2^(exponent of the keys' scales); what O is multiplied by before
+    int v_exponent;                    // of the values' scales, as a float's
+    unsigned held[2];                  // keys that are there
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float power(int exponent) { return __int_as_float(exponent << 23); }      // 1 .. 254
+__device__ __forceinline__ void butterflies(float (&v)[64], int hb) {
+#pragma unroll
+    for (int h = 1; h < 64; h *= 2)
+        if (h < hb)
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+                if (!(i & h)) {
+                    const float x = v[i], y = v[i + h];
+                    v[i] = x + y;
+                    v[i + h] = x - y;
+                }
+}
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!tc::mbar_try_wait(bar, parity) && clock64() - t0 < tc::kWaitLimitCycles) {}
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendArgs a) {
+    using S = Shape<D>;
+    constexpr int GROUPS = D / 8;                            // of 8 neighbouring values
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_bars[2 * kRaw + 13];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort, s_pages[kRaw];
+    __shared__ Info s_info[2];
+    uint8_t *smem = smem_raw + (-smem_addr(smem_raw) & 1023u);
+    uint8_t *raw = smem + 2 * S::kKV;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CacheArgs &c = a.c;
+    volatile int *abort_flag = &s_abort;
+    const uint32_t bars = smem_addr(s_bars);
+    auto raw_full = [&](int i) { return bars + 8 * i; };
+    auto raw_free = [&](int i) { return bars + 8 * (kRaw + i); };
+    auto kv_full = [&](int i) { return bars + 8 * (2 * kRaw + i); };
+    auto kv_free = [&](int i) { return bars + 8 * (2 * kRaw + 2 + i); };
+    auto s_full = [&](int i) { return bars + 8 * (2 * kRaw + 4 + i); };
+    auto p_full = [&](int i) { return bars + 8 * (2 * kRaw + 6 + i); };
+    auto o_full = [&](int i) { return bars + 8 * (2 * kRaw + 8 + i); };
+    const uint32_t q_full = bars + 8 * (2 * kRaw + 10), tail = bars + 8 * (2 * kRaw + 11);
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int i = 0; i < kRaw; ++i) {
+            mbar_init(raw_full(i), 1);
+            mbar_init(raw_free(i), 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(kv_full(i), 4);
+            mbar_init(kv_free(i), 1);
+            mbar_init(s_full(i), 1);
+            mbar_init(p_full(i), 4);
+            mbar_init(o_full(i), 1);
+        }
+        mbar_init(q_full, 8);
+        mbar_init(tail, 1);
+        tc::fence_barrier_init();
+    }
+    if (warp == 13) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    after_prior_kernels();
+    const int err = *reinterpret_cast<volatile int *>(a.err);
+    // ---- the CTA's sequence, head and columns; of a sequence the last columns, which see most, come first
+    Row<kPromptColumns> row;
+    row.read(c, a.group, lane, true);
+    const bool work = blockIdx.x < row.total;
+    Sequence seq{};
+    if (work) row.find_unit(c, a.group, lane, blockIdx.x, seq);
+    const int rank = work ? (int)(blockIdx.x - seq.unit) : 0, head = rank % c.heads, x0 = (seq.tiles - 1 - rank / c.heads) * kPromptColumns;
+    const int columns = min((long long)seq.m * a.group - x0, (long long)kPromptColumns), last_token = (x0 + columns - 1) / a.group;
+    const int tiles = columns > 128 ? 2 : 1;
+    tc::tc_fence_before();
+    const bool skip = __syncthreads_or(err != 0) || !work;
+    tc::tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    // chunks that some column sees
+    const int chunks = skip ? 0 : max(0, (seq.len - seq.m + last_token) / kChunk + (seq.len - seq.m + last_token >= 0 ? 1 : 0));
+    const int size = 1 << c.page_bits, pages_of_chunk = kChunk >> c.page_bits;
+    const uint32_t record = (uint32_t)size * (D + 8);
+    bool ok = true;
+
+    if (warp == 12) {
+        // ---- chunks from the cache
+        int issued = 0;
+        for (; issued < chunks; ++issued) {
+            const int stage = issued % kRaw, first = issued * pages_of_chunk;
+            const int page = lane < pages_of_chunk && first + lane < c.table_width ? c.table[seq.b * c.ldt + first + lane] : -1;
+            const bool take = issued * kChunk + lane * size < seq.len && page >= 0 && page < c.pages;
+            const unsigned pages = __ballot_sync(0xffffffffu, take);
+            if (issued >= kRaw) ok = mbar_wait(raw_free(stage), (uint32_t)(issued / kRaw - 1) & 1u, abort_flag, a.err);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            if (lane == 0) {
+                s_pages[stage] = (int)pages;
+                mbar_expect_tx(raw_full(stage), (uint32_t)__popc(pages) * record);
+            }
+            __syncwarp();
+            if (take)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 smem_addr(raw + stage * S::kChunkBytes + lane * record)),
+                             "l"(c.data + ((long long)page * c.heads + head) * record), "r"(record), "r"(raw_full(stage))
+                             : "memory");
+        }
+        // copies land before the CTA leaves, whoever gave up
+        for (int i = max(0, issued - kRaw); i < issued; ++i) drain(raw_full(i % kRaw), (uint32_t)(i / kRaw) & 1u);
+    } else if (warp == 13) {
+        // ---- MMAs
+        const uint32_t s_idesc = tc::idesc_f16(kChunk), o_idesc = tc::idesc_f16(D);
+        auto issue_s = [&](int tile, int buf) {
+            const uint64_t k0 = tc::sdesc_sw128(smem_addr(smem + buf * S::kKV));
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+                tc::umma_f16_ts(tmem + S::kS + 64 * tile, tmem + S::kQ + D / 2 * tile + 8 * j, k0 + (uint64_t)((j / 4) * 512 + 2 * (j % 4)), s_idesc, j > 0);
+            tc::umma_commit(s_full(tile));
+        };
+        if (chunks) {
+            ok = mbar_wait(q_full, 0, abort_flag, a.err) && mbar_wait(kv_full(0), 0, abort_flag, a.err);
+            ok = __all_sync(0xffffffffu, ok);
+            tc::tc_fence_after();
+            if (ok && lane == 0)
+                for (int tile = 0; tile < tiles; ++tile) issue_s(tile, 0);
+        }
+        for (int i = 0; i < chunks && ok; ++i) {
+            const int buf = i & 1;
+            for (int tile = 0; tile < tiles && ok; ++tile) {
+                ok = mbar_wait(p_full(tile), (uint32_t)i & 1u, abort_flag, a.err);
+                if (ok && tile == 0 && i + 1 < chunks) ok = mbar_wait(kv_full(buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u, abort_flag, a.err);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc::tc_fence_after();
+                if (lane == 0) {
+                    const uint64_t v0 = tc::sdesc_sw128(smem_addr(smem + buf * S::kKV + S::kK));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        tc::umma_f16_ts(tmem + S::kO + D * tile, tmem + S::kS + 64 * tile + 8 * j, v0 + (uint64_t)(2 * j), o_idesc, i > 0 || j > 0);
+                    if (tile + 1 == tiles) tc::umma_commit(kv_free(buf));
+                    if (i + 1 < chunks) issue_s(tile, buf ^ 1);
+                    else tc::umma_commit(o_full(tile));
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) tc::umma_commit(tail);
+        __syncwarp();
+        drain(tail, 0);
+    } else if (warp >= 8) {
+        // ---- widening
+        const int tid = threadIdx.x - 256, part = tid >> 6, key = tid & 63;
+        const int dg = lane % GROUPS, tg = (tid >> 5) * 2 + (lane / GROUPS & 1);
+        const bool has_v = GROUPS == 16 || lane < 16;
+        int v_exponent = 1;
+        for (int i = 0; i < chunks; ++i) {
+            const int stage = i % kRaw, buf = i & 1;
+            ok = mbar_wait(raw_full(stage), (uint32_t)(i / kRaw) & 1u, abort_flag, a.err);
+            if (ok && i >= 2) ok = mbar_wait(kv_free(buf), (uint32_t)((i >> 1) - 1) & 1u, abort_flag, a.err);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            const uint8_t *chunk = raw + stage * S::kChunkBytes;
+            const int pages = s_pages[stage], left = seq.len - i * kChunk;
+            // scales of token j, 0 where it is none; NaN of the keys' where either is not finite
+            auto scales = [&](int j, float &ks, float &vs) {
+                const int in_page = j >> c.page_bits;
+                const uint8_t *at = chunk + in_page * record + size * D + 4 * (j & (size - 1));
+                const bool there = (pages >> in_page & 1) && j < left;
+                const float k = *reinterpret_cast<const float *>(at), v = *reinterpret_cast<const float *>(at + 4 * size);
+                const bool sound = fabsf(k) < __int_as_float(0x7f800000) && fabsf(v) < __int_as_float(0x7f800000);
+                ks = !there ? 0.0f : sound ? k : __int_as_float(0x7fffffff);
+                vs = there && sound ? v : 0.0f;
+                return there;
+            };
+            float k0, v0, k1, v1;
+            const unsigned held0 = __ballot_sync(0xffffffffu, scales(lane, k0, v0)), held1 = __ballot_sync(0xffffffffu, scales(lane + 32, k1, v1));
+            // (a NaN is larger than any number: left out)
+            auto bits = [](float x) { return x == x ? __float_as_uint(x) & 0x7fffffffu : 0u; };
+            const int k_exponent = min(max((int)(__reduce_max_sync(0xffffffffu, max(bits(k0), bits(k1))) >> 23), 1), 253);
+            const int v_most = min(max((int)(__reduce_max_sync(0xffffffffu, max(bits(v0), bits(v1))) >> 23), 1), 253);
+            const int v_last = v_exponent;
+            v_exponent = max(v_exponent, v_most);
+            if (tid == 0) {
+                Info info;
+                info.k_factor = power(k_exponent);
+                info.v_ratio = v_exponent - v_last > 126 ? 0.0f : power(127 - (v_exponent - v_last));
+                info.v_exponent = v_exponent;
+                info.held[0] = held0;
+                info.held[1] = held1;
+                s_info[buf] = info;
+            }
+            uint8_t *K = smem + buf * S::kKV, *V = K + S::kK;
+            {
+                // keys: row = key, values in the order 0 4 1 5 2 6 3 7 of each 8, as the queries have them
+                const float of = __shfl_sync(0xffffffffu, key & 32 ? k1 : k0, lane);   // (key = lane or lane + 32)
+                const float by = of * power(254 - k_exponent);
+                const uint32_t scale = pack_half(by, by);
+                const uint8_t *at = chunk + (key >> c.page_bits) * record + (key & (size - 1)) * (D / 2) + part * (D / 4);
+                uint32_t w[D / 16];
+#pragma unroll
+                for (int j = 0; j < D / 16; j += 4) *reinterpret_cast<uint4 *>(w + j) = *reinterpret_cast<const uint4 *>(at + 4 * j);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    const uint32_t u = w[j] >> 8;
+                    const int word = part * (D / 16) + j;
+                    const uint4 o = make_uint4(mul2(codes_f16<true, false>(w[j]), scale), mul2(codes_f16<true, true>(w[j]), scale),
+                                               mul2(codes_f16<true, false>(u), scale), mul2(codes_f16<true, true>(u), scale));
+                    *reinterpret_cast<uint4 *>(K + (word >> 3) * 8192 + key * 128 + (((word & 7) ^ (key & 7)) << 4)) = o;
+                }
+            }
+            if (has_v) {
+                // values, transposed: 8 tokens of 8 values; value 8 dg + j is row j GROUPS + dg
+                uint32_t w[8], scale[4];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int token = tg * 8 + j;
+                    w[j] = *reinterpret_cast<const uint32_t *>(chunk + (token >> c.page_bits) * record + (size + (token & (size - 1))) * (D / 2) + 4 * dg);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float ka, va, kb, vb;
+                    scales(tg * 8 + 2 * j, ka, va);
+                    scales(tg * 8 + 2 * j + 1, kb, vb);
+                    scale[j] = pack_half(va * power(254 - v_exponent), vb * power(254 - v_exponent));
+                }
+                uint32_t o[8][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t n = __byte_perm(w[2 * j], w[2 * j + 1], half ? 0x7632 : 0x5410), u = n >> 8;
+                        o[4 * half][j] = mul2(codes_f16<true, false>(n), scale[j]);
+                        o[4 * half + 1][j] = mul2(codes_f16<true, true>(n), scale[j]);
+                        o[4 * half + 2][j] = mul2(codes_f16<true, false>(u), scale[j]);
+                        o[4 * half + 3][j] = mul2(codes_f16<true, true>(u), scale[j]);
+                    }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int n = j * GROUPS + dg;
+                    *reinterpret_cast<uint4 *>(V + n * 128 + ((tg ^ (n & 7)) << 4)) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(kv_full(buf));
+                mbar_arrive(raw_free(stage));
+            }
+        }
+    } else {
+        // ---- a row a thread
+        const int tile = warp >> 2, x = x0 + threadIdx.x, token = x / a.group, q_head = head * a.group + x - token * a.group;
+        const bool live = !skip && token < seq.m;
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        float f = 0.0f;
+        const bool here = !skip && tile < tiles;
+        if (here && chunks) {
+            // The query, transformed; its halves of 64 one after the other (of 128 in a block: sums, then differences).
+            const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.q) + (long long)(seq.begin + (live ? token : 0)) * a.ldq +
+                                     (long long)(live ? q_head : 0) * a.hq;
+            auto load8 = [&](int i, uint32_t (&w)[4]) {
+                if (a.vec) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                } else {
+                    const unsigned short *u = reinterpret_cast<const unsigned short *>(p) + 8 * i;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = u[2 * j] | (uint32_t)u[2 * j + 1] << 16;
+                }
+            };
+            uint32_t most = 0;
+#pragma unroll 4
+            for (int i = 0; i < GROUPS; ++i) {
+                uint32_t w[4];
+                load8(i, w);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = __vmaxu2(most, w[j] & 0x7fff7fffu);
+            }
+            // below 2^10 by a power of two; an infinity or a NaN makes the row NaN
+            const int log_hb = 31 - __clz(c.hb), ex = max((int)(max(most & 0xffffu, most >> 16) >> 7), 10);
+            const float by = !live ? 0.0f : ex == 255 ? __int_as_float(0x7fffffff) : copysignf(power(263 - log_hb - ex), a.scale);
+            f = fabsf(a.scale) * c.inv_norm * power(min(ex, 254) + log_hb - 9);
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half) {
+                float v[64];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t w[4], u[4];
+                    load8(D == 128 && c.hb <= 64 ? 8 * half + i : i, w);
+                    if (D == 128 && c.hb == 128) load8(8 + i, u);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+                        v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                        if (D == 128 && c.hb == 128) {
+                            const float y = __uint_as_float(u[j] << 16), z = __uint_as_float(u[j] & 0xffff0000u);
+                            v[8 * i + 2 * j] += half ? -y : y;
+                            v[8 * i + 2 * j + 1] += half ? -z : z;
+                        }
+                    }
+                }
+                butterflies(v, c.hb);
+                uint32_t r[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int d = (i >> 2) * 8 + (i & 3);
+                    r[i] = pack_half(live ? v[d] * by : 0.0f, live ? v[d + 4] * by : 0.0f);
+                }
+                tc::tmem_st32(at + S::kQ + D / 2 * tile + 32 * half, r);
+            }
+            tc::tmem_wait_st();
+            tc::tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full);
+        // ---- softmax
+        const int position = live ? seq.len - seq.m + token : 0x7fffffff;          // (rows that are none: nothing to mask)
+        const int lowest = __reduce_min_sync(0xffffffffu, position);
+        float m = -1e30f, l = 0.0f;
+        int v_exponent = 127;
+        for (int i = 0; i < (here ? chunks : 0); ++i) {
+            ok = mbar_wait(s_full(tile), (uint32_t)i & 1u, abort_flag, a.err);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc::tc_fence_after();
+            const Info info = s_info[i & 1];
+            v_exponent = info.v_exponent;
+            const float fs = f * info.k_factor;
+            uint32_t s[64];
+            tc::tmem_ld32(at + S::kS + 64 * tile, *reinterpret_cast<uint32_t (*)[32]>(s));
+            tc::tmem_ld32(at + S::kS + 64 * tile + 32, *reinterpret_cast<uint32_t (*)[32]>(s + 32));
+            tc::tmem_wait_ld();
+            const bool whole = i * kChunk + kChunk - 1 <= lowest && (info.held[0] & info.held[1]) == 0xffffffffu;
+            unsigned seen[2] = {0xffffffffu, 0xffffffffu};
+            if (!whole) {
+                const int ends = min(max(position - i * kChunk, -1), kChunk - 1) + 1;                // keys before it
+                seen[0] = info.held[0] & (ends >= 32 ? 0xffffffffu : (1u << ends) - 1u);
+                seen[1] = info.held[1] & (ends >= 64 ? 0xffffffffu : ends <= 32 ? 0u : (1u << (ends - 32)) - 1u);
+#pragma unroll
+                for (int j = 0; j < 64; ++j)
+                    if (!(seen[j >> 5] >> (j & 31) & 1)) s[j] = __float_as_uint(-3e38f);
+            }
+            float most = -3e38f;
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) most = max3(most, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+            const float top = (whole || (seen[0] | seen[1])) ? most * fs : -1e30f;
+            const bool raise = top > m + 8.0f;
+            if (__any_sync(0xffffffffu, raise || info.v_ratio != 1.0f)) {
+                const float now = raise ? top : m, by = exp2_fast(m - now);
+                m = now;
+                l *= by;
+                if (i > 0) {
+                    const float o_by = by * info.v_ratio;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        tc::tmem_ld32(at + S::kO + D * tile + d, o);
+                        tc::tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * o_by);
+                        tc::tmem_st32(at + S::kO + D * tile + d, o);
+                    }
+                    tc::tmem_wait_st();
+                }
+            }
+            float sum[4] = {};
+            uint32_t p[32];
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) {
+                float u = exp2_fast(fmaf(__uint_as_float(s[j]), fs, -m)), v = exp2_fast(fmaf(__uint_as_float(s[j + 1]), fs, -m));
+                if (!whole) {
+                    if (!(seen[j >> 5] >> (j & 31) & 1)) u = 0.0f;
+                    if (!(seen[j >> 5] >> ((j + 1) & 31) & 1)) v = 0.0f;
+                }
+                sum[j & 2] += u;
+                sum[(j & 2) + 1] += v;
+                p[j / 2] = pack_half(u, v);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tc::tmem_st32(at + S::kS + 64 * tile, p);
+            tc::tmem_wait_st();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full(tile));
+        }
+        // ---- the row's output
+        ok = __all_sync(0xffffffffu, ok);
+        if (here && chunks && ok) {
+            ok = __all_sync(0xffffffffu, mbar_wait(o_full(tile), 0, abort_flag, a.err));
+            tc::tc_fence_after();
+        }
+        if (here && ok) {
+            const float by = l == 0.0f ? 0.0f : c.inv_norm / l, unit = power(v_exponent);
+            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + (long long)(seq.begin + (live ? token : 0)) * a.ldo +
+                                 (long long)(live ? q_head : 0) * a.ho;
+#pragma unroll 1
+            for (int half = 0; half < D / 64; ++half) {
+                float v[64];
+                constexpr int PER = 32 / GROUPS;             // values j of each group in 32 columns
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    uint32_t o[32];
+                    if (chunks) {
+                        tc::tmem_ld32(at + S::kO + D * tile + 32 * j, o);
+                        tc::tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int y = 0; y < PER; ++y)
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            float u = __uint_as_float(o[y * GROUPS + g]);
+                            if (D == 128) {
+                                const float z = __uint_as_float(o[y * GROUPS + (GROUPS - 8) + g]);
+                                u = c.hb == 128 ? (half ? u - z : u + z) : half ? z : u;
+                            }
+                            v[8 * g + PER * j + y] = chunks ? u : 0.0f;
+                        }
+                }
+                butterflies(v, c.hb);
+                if (live) {
+                    union { uint4 u[8]; __nv_bfloat16 t[64]; } y;
+#pragma unroll
+                    for (int d = 0; d < 64; ++d) y.t[d] = from_f32<__nv_bfloat16>(v[d] * by * unit);
+                    if (a.vec_out) {
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) reinterpret_cast<uint4 *>(out + 64 * half)[d] = y.u[d];
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < 64; ++d) out[64 * half + d] = y.t[d];
+                    }
+                }
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 13)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+template <int D>
+cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
+    static std::atomic<int> allowed[64];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(prompt_kernel<D>), Shape<D>::kBytes, allowed);
+    if (e != cudaSuccess) return e;
+    const long long tasks = a.c.heads * ((long long)a.c.rows * a.group / kPromptColumns + min(a.c.seqs, a.c.rows));
+    return launch_early(prompt_kernel<D>, dim3((unsigned)tasks), kPromptThreads, Shape<D>::kBytes, s, a);
+}
+
+}  // namespace
+
+// Where a CTA's waves of 256 columns take less time than the few-column kernel's 16 columns at a time.
+bool attend_prompt(int type, int width, int heads, int group, long long rows, int seqs, int sms) {
+    if (type != HATQ_BF16 || width > 128 || seqs == 0) return false;
+    const long long columns = (rows * group + seqs - 1) / seqs, tasks = (long long)heads * seqs * ((columns + kPromptColumns - 1) / kPromptColumns);
+    return (tasks + sms - 1) / sms * 1400 < (long long)heads * seqs * ((columns + 15) / 16) * 750 / sms;
+}
+cudaError_t launch_prompt(const AttendArgs &a, cudaStream_t s) { return a.c.width == 64 ? launch<64>(a, s) : launch<128>(a, s); }
+
+}  // namespace hatq

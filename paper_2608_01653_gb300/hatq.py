@@ -154,7 +154,7 @@ def load(build: bool = True) -> ctypes.CDLL:
             "hatq_combine_rows": (_I, [_P, _I, _L, _L, _P, _P, _L, _I, _I, _P, _L, _P]),
             "hatq_append_tokens": (_I, [ctypes.POINTER(TokenCacheStruct), _P, _L, _L, _P, _L, _L, _I, _L, _P, _L, _I, _P, _P,
                                         _I, _P, _P, _P]),
-            "hatq_attend_workspace": (_I, [ctypes.POINTER(TokenCacheStruct), _I, _L, _I, _I, _I,
+            "hatq_attend_workspace": (_I, [ctypes.POINTER(TokenCacheStruct), _I, _I, _L, _I, _I, _I,
                                            ctypes.POINTER(ctypes.c_size_t)]),
             "hatq_attend_tokens": (_I, [_P, _I, _L, _L, _I, _L, ctypes.POINTER(TokenCacheStruct), _P, _L, _I, _P, _P, _I,
                                         _F, _P, _L, _L, _P, ctypes.c_size_t, _P]),
@@ -1088,7 +1088,7 @@ class TokenCache:
         self.scale = self.width ** -0.5 if self.width > 0 else 1.0
         self.workspaces = {}                        # bytes of attend_tokens' workspace, by the sizes of a call
         size = ctypes.c_size_t()                    # the library looks the sizes over
-        _check(load().hatq_attend_workspace(self.ref, heads, 0, 0, 0, 0, ctypes.byref(size)))
+        _check(load().hatq_attend_workspace(self.ref, BF16, heads, 0, 0, 0, 0, ctypes.byref(size)))
 
     @staticmethod
     def bytes_of(pages, heads, width, page=64):
@@ -1190,11 +1190,11 @@ def attend_tokens(q, cache, table, lengths, starts=None, scale=None, out=None, s
         if out.dtype != q.dtype or out.shape != q.shape:
             raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {q.dtype} {tuple(q.shape)}")
         _, _, ldo, ho = _heads_of(out, "out", heads, cache.width, device)
-    lib, sizes = _LIB or load(), (heads, rows, seqs, pages, starts is None)
+    lib, sizes = _LIB or load(), (kind, heads, rows, seqs, pages, starts is None)
     size = cache.workspaces.get(sizes)
     if size is None:
         need = ctypes.c_size_t()
-        _check(lib.hatq_attend_workspace(cache.ref, heads, rows, seqs, 0 if starts is None else 1, pages, ctypes.byref(need)))
+        _check(lib.hatq_attend_workspace(cache.ref, kind, heads, rows, seqs, 0 if starts is None else 1, pages, ctypes.byref(need)))
         if len(cache.workspaces) >= 256:
             cache.workspaces.clear()
         size = cache.workspaces[sizes] = need.value

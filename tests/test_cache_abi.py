@@ -43,7 +43,7 @@ def test_caches_that_are_refused(lib, kw, status):
     assert append(lib, cache(**kw)) == status and H.last_error()
     assert attend(lib, cache(**kw)) == status and H.last_error()
     size = ctypes.c_size_t(7)
-    assert lib.hatq_attend_workspace(ctypes.byref(cache(**kw)), 4, 4, 2, 1, 3, ctypes.byref(size)) == status
+    assert lib.hatq_attend_workspace(ctypes.byref(cache(**kw)), H.BF16, 4, 4, 2, 1, 3, ctypes.byref(size)) == status
     assert size.value == 7
 
 
@@ -86,7 +86,7 @@ def test_no_rows_is_no_work(lib):
     assert append(lib, seqs=0, lengths=None) == H.OK                    # rows of no sequence
     assert attend(lib, q=None, out=None, ws=None, size=0, **none) == H.OK
     size = ctypes.c_size_t(7)
-    assert lib.hatq_attend_workspace(ctypes.byref(cache()), 4, 0, 0, 0, 3, ctypes.byref(size)) == H.OK and size.value == 0
+    assert lib.hatq_attend_workspace(ctypes.byref(cache()), H.BF16, 4, 0, 0, 0, 3, ctypes.byref(size)) == H.OK and size.value == 0
 
 
 def test_struct_matches_the_header():

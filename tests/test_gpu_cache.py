@@ -251,8 +251,8 @@ def turned(x, hb):
     return (x.reshape(*x.shape[:-1], -1, hb) @ basis(hb)).reshape(x.shape)
 
 
-def reference(run, q, scale=None):
-    """Outputs in 64 bits and the standard deviation of the kernel's roundings.
+def reference(run, q, scale=None, rows=None):
+    """Outputs in 64 bits and the standard deviation of the kernel's roundings (rows: of some rows only, zeros elsewhere).
 
     Every rounding is an independent error of zero mean, at most half a step, so of a standard deviation of at most
     h / sqrt(3), h = 2^-11 (bf16: q and w v once to fp16) or 2^-21 (fp16: twice). With n keys and width D:
@@ -272,7 +272,7 @@ def reference(run, q, scale=None):
         kc, ks, vc, vs, there = held(run, b, n) if n else (None,) * 5
         for i in range(m):
             p = n - m + i
-            if p >= 0 and bool(there[:p + 1].any()):
+            if p >= 0 and (rows is None or r in rows) and bool(there[:p + 1].any()):
                 keep = torch.nonzero(there[:p + 1])[:, 0]
                 K, V, sv = kc[:, keep] * ks[:, keep, None], vc[:, keep] * vs[:, keep, None], vs[:, keep]
                 s = scale * torch.einsum("hgd,hnd->hgn", t[r], K)
@@ -290,11 +290,12 @@ def reference(run, q, scale=None):
     return out, sd
 
 
-def check_attend(run, q, y, scale=None, rows=None):
-    ref, sd = reference(run, q, scale)
-    n = sum(run.new) if rows is None else rows
-    err = (y.double().cpu() - ref)[:n].abs()
-    tol = (8 * sd + torch.finfo(q.dtype).eps / 2 * 1.01 * ref.abs() + 2.0 ** -24)[:n]
+def check_attend(run, q, y, scale=None, rows=None, more=1.0):
+    """rows: of these only; more: times the deviation."""
+    ref, sd = reference(run, q, scale, rows)
+    of = list(range(sum(run.new))) if rows is None else sorted(rows)
+    err = (y.double().cpu() - ref)[of].abs()
+    tol = (8 * more * sd + torch.finfo(q.dtype).eps / 2 * 1.01 * ref.abs() + 2.0 ** -24)[of]
     assert y.dtype == q.dtype
     worst = float((err / tol).nan_to_num(nan=INF).max())
     assert worst <= 1
@@ -462,6 +463,141 @@ def test_attend_strides():
     assert bool((wide[:, 2] == 0).all()) and torch.equal(wide[:, 0], q)
     first = q[:1].expand(run.rows, -1, -1)
     assert torch.equal(attend(run, first), attend(run, first.contiguous()))
+
+
+# Many queries per sequence and bf16: another kernel. It rounds code times scale to fp16 as well, of keys (as q is) and of
+# values (as w v is): variances twice as large, deviations sqrt(2) times.
+MANY = 2 ** 0.5
+
+
+def some(run, n, seed=0):
+    """Rows to compare: the first and last of every sequence, and n others."""
+    ends, at = set(), 0
+    for m in run.new:
+        if m:
+            ends |= {at, at + m - 1}
+        at += m
+    return ends | set(np.random.default_rng(seed).integers(0, at, n).tolist())
+
+
+@pytest.mark.parametrize("width,hb,page", [(64, 64, 16), (64, 1, 64), (64, 8, 32), (128, 128, 64), (128, 64, 16), (128, 2, 32), (128, 1, 64)])
+@pytest.mark.parametrize("kv,group", [(16, 2), (12, 7), (40, 1)])
+def test_attend_many_columns(width, hb, page, kv, group):
+    """Columns below, at and above a tile's, last tiles cut, sequences without tokens, without keys, with more rows than tokens."""
+    lengths = [64, 40, 130, 0, 5, 260, 127, 65, 700]
+    run = Run(lengths, [64, 3, 130, 0, 9, 1, 127, 64, 37], kv=kv, width=width, page=page, hb=hb)
+    q = run.random(kv * group, 5)
+    check_attend(run, q, attend(run, q), rows=some(run, 60), more=MANY)
+
+
+@pytest.mark.parametrize("width", [64, 128])
+def test_attend_long_prompts(width):
+    run = Run([1900, 1111], [1500, 1111], kv=8, width=width)
+    q = run.random(32, 5)
+    check_attend(run, q, attend(run, q), rows=some(run, 30), more=MANY)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-3, 0.7, -0.3, 8.0])
+def test_attend_many_columns_scales(scale):
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=64)
+    q = run.random(64, 5)
+    check_attend(run, q, attend(run, q, scale=scale), scale, rows=some(run, 40), more=MANY)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-4, 1e4, 1e30])
+def test_attend_many_columns_scales_of_any_size(size):
+    """Of values times size; of both growing from token to token, so that later ones raise what the first were brought to."""
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=128)
+    at = run.page * run.width
+    scales = run.cache.data[:, :, at:].contiguous().view(torch.float32).reshape(-1, 16, 2, run.page)
+    scales[:, :, 1] *= size
+    for b, n in enumerate(run.len):
+        for j in range(n):
+            scales[run.table[b, j // run.page], :, 1, j % run.page] *= 1.05 ** (j - n)
+    run.cache.data[:, :, at:] = scales.reshape(-1, 16, 2 * run.page).view(torch.uint8)
+    q = run.random(64, 5)
+    y = attend(run, q)
+    rows = some(run, 40)
+    ref, sd = reference(run, q, rows=rows)
+    tol = 8 * MANY * sd + 2.0 ** -8 * 1.01 * ref.abs() + 2.0 ** -130
+    assert float(((y.double().cpu() - ref).abs() / tol)[sorted(rows)].max()) <= 1
+
+
+def test_attend_many_columns_pages_that_are_none():
+    run = Run([200, 333, 90, 40], [60, 40, 90, 48], kv=16, width=64, page=16)
+    run.table[0, 3], run.table[1, 0], run.table[1, 20] = -1, 1 << 30, run.cache.pages
+    run.table[2, :] = -1
+    q = run.random(64, 5)
+    y = attend(run, q)
+    check_attend(run, q, y, rows=some(run, 60), more=MANY)
+    assert bool((y[100:190] == 0).all()) and bool((y[190:198] == 0).all()) and bool((y[198:] != 0).any())
+
+
+def test_attend_many_columns_what_a_row_does_not_see():
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=64, page=32)
+    page, width = run.page, run.width
+    q = run.random(64, 5)
+    want = attend(run, q)
+    scales = run.cache.data[:, :, page * width:].contiguous().view(torch.float32).reshape(-1, 16, 2, page)
+    first = {0: 150, 1: 332, 2: 1, 3: 64}                               # the first token that is NaN, by sequence (3: none)
+    for b, n in enumerate(run.len):
+        for part, j in ((0, first[b]), (1, first[b] + 1), (1, n), (0, n + 1)):
+            if j >= first[b] and j // page < run.table.shape[1] and run.table[b, j // page] >= 0:
+                scales[run.table[b, j // page], :, part, j % page] = NAN
+    run.cache.data[:, :, page * width:] = scales.reshape(-1, 16, 2 * page).view(torch.uint8)
+    y = attend(run, q)
+    for r, b, p in run.places():
+        if p >= first[b]:
+            assert bool(y[r].isnan().all())
+        else:
+            assert torch.equal(y[r], want[r])
+
+
+def test_attend_many_columns_queries_with_an_infinity_or_a_nan():
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=128)
+    q = run.random(64, 5)
+    want = attend(run, q)
+    bad = torch.zeros(254, 64, dtype=torch.bool, device="cuda")
+    for r, h, d, v in ((1, 2, 5, INF), (100, 0, 0, NAN), (253, 63, 127, -INF)):
+        q[r, h, d], bad[r, h] = v, True
+    y = attend(run, q)
+    assert bool(y[bad].isnan().all()) and torch.equal(y[~bad], want[~bad])
+
+
+def test_attend_many_columns_strides_and_rows_of_no_sequence():
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=64)
+    q = run.random(32, 5)
+    want = attend(run, q)
+    odd, out = torch.zeros(260, 32, 67, dtype=torch.bfloat16, device="cuda"), torch.full((260, 32, 67), 7.0, dtype=torch.bfloat16, device="cuda")
+    odd[3:257, :, 1:65] = q
+    H.attend_tokens(odd[:, :, 1:65], run.cache, run.table, run.lengths, run.starts + 3, out=out[:, :, 2:66])
+    outside = q.transpose(0, 1).contiguous().transpose(0, 1)
+    y = torch.empty_like(outside)
+    H.attend_tokens(outside, run.cache, run.table, run.lengths, run.starts, out=y)
+    finish()
+    assert torch.equal(out[3:257, :, 2:66], want) and torch.equal(y, want)
+    out[3:257, :, 2:66] = 7
+    assert bool((out == 7).all())
+
+
+def test_attend_many_columns_twice_and_in_a_graph():
+    run = Run([200, 333, 90, 64], [60, 40, 90, 64], kv=16, width=128)
+    q, p = run.random(64, 5), run.random(64, 6)
+    want = attend(run, q), attend(run, p)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [(H.attend_tokens(q, run.cache, run.table, run.lengths, run.starts, stream=a),
+            H.attend_tokens(p, run.cache, run.table, run.lengths, run.starts, stream=b)) for _ in range(10)]
+    finish()
+    assert all(torch.equal(x, want[0]) and torch.equal(y, want[1]) for x, y in got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = H.attend_tokens(q, run.cache, run.table, run.lengths, run.starts)
+    for src, ref in ((p, want[1]), (q.clone(), want[0])):
+        q.copy_(src)
+        graph.replay()
+        finish()
+        assert torch.equal(y, ref)
 
 
 def test_attend_twice_and_on_two_streams():
