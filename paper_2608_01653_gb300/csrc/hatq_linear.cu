@@ -68,11 +68,6 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 // One lane of the warp. The issuing warps run their loops with all lanes and pick the lane only around the
 // asynchronous instructions: their operands then stay warp-uniform for the compiler (with the loops under a
 // lane == 0 branch a 64-code block cost about 800 cycles of issue, whatever the tile).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
-    return p != 0;
-}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }

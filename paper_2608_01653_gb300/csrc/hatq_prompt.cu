@@ -7,6 +7,7 @@
 namespace hatq {
 namespace {
 
+using tc::elect_one;
 using tc::mbar_arrive;
 using tc::mbar_expect_tx;
 using tc::mbar_init;
@@ -18,29 +19,33 @@ using tc::smem_addr;
 // rounded to fp16 are q and p as there, and here also code times scale of keys and of values (an error of 2^-12 each,
 // against 2^-9 of the output), so that a logit costs one instruction less than it would with a factor of its key.
 //
-// Scales are brought into fp16's range by powers of two: those of a chunk's keys by the largest of them, whose exponent
-// goes into the logits' factor; those of values by the largest so far, and O is scaled where that grows. A token whose
+// Scales are brought into fp16's range by powers of two, a chunk's by the largest of them: that of keys goes into the
+// logits' factor, that of values, relative to the largest chunk's so far, into the weights; O is scaled where that
+// grows. A token whose
 // scales are not finite gets values of 0 and keys of NaN, so that it makes NaN exactly of the rows that see it (0 times NaN
 // in a masked place would do so of all).
 //
-// Roles: 4 warps per tile have a row a thread (transform of the query, softmax, transform back), 4 warps widen chunks of 64
-// keys, one brings them in, one issues the MMAs: PV of a tile, then S of its next chunk, which may overwrite P. While one
+// Roles: 4 warps per tile have a row a thread (transform of the query, softmax, transform back), twice 4 warps widen chunks
+// of 64 keys in turn, one brings them in, one issues the MMAs: PV of a tile, then S of its next chunk, which may overwrite P. While one
 // tile's rows are at their softmax, the tensor cores are at the other's.
 //
 // Bound by instructions and the tensor cores about alike: per chunk and two tiles 1024 cycles of MMA, 820 issue slots of
 // each scheduler.
 constexpr int kRaw = 4;                // chunks on their way or being widened
-constexpr int kPromptThreads = 14 * 32;
+constexpr int kWide = 4;               // widened chunks
+// Five groups of four warps; the last has two that rest. Registers are handed on between them: 640 x 96 at launch.
+constexpr int kPromptThreads = 20 * 32, kRegsLaunch = 96, kRegsRows = 144, kRegsWiden = 72, kRegsRest = 40;
+static_assert(256 * kRegsRows + 256 * kRegsWiden + 128 * kRegsRest <= kPromptThreads * kRegsLaunch, "setmaxnreg waits for registers that there are");
 
 template <int D>
 struct Shape {
     static constexpr int kChunkBytes = kChunk * (D + 8), kK = kChunk * D * 2, kKV = 2 * kK;
     static constexpr int kO = 0, kQ = 2 * D, kS = 3 * D;     // columns of tensor memory: two tiles each of D, D / 2, 64
-    static constexpr int kBytes = 1024 + 2 * kKV + kRaw * kChunkBytes;
+    static constexpr int kBytes = 1024 + kWide * kKV + kRaw * kChunkBytes;
 };
 
 struct Info {                          // of a widened chunk, for the rows
-    float k_factor, v_ratio;           // 2^(exponent of the keys' scales); what O is multiplied by before
+    float k_factor;                    // 2^(exponent of the keys' scales)
     int v_exponent;                    // of the values' scales, as a float's
     unsigned held[2];                  // keys that are there
 };
@@ -65,6 +70,11 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
 __device__ __forceinline__ float power(int exponent) { return __int_as_float(exponent << 23); }      // 1 .. 254
 __device__ __forceinline__ void butterflies(float (&v)[64], int hb) {
 #pragma unroll
@@ -83,17 +93,23 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
     while (!tc::mbar_try_wait(bar, parity) && clock64() - t0 < tc::kWaitLimitCycles) {}
 }
 
+template <int N, bool MORE>
+__device__ __forceinline__ void set_regs() {
+    if constexpr (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendArgs a) {
     using S = Shape<D>;
     constexpr int GROUPS = D / 8;                            // of 8 neighbouring values
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_bars[2 * kRaw + 13];
+    __shared__ __align__(8) uint64_t s_bars[2 * kRaw + 2 * kWide + 8];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_pages[kRaw];
-    __shared__ Info s_info[2];
+    __shared__ Info s_info[kWide];
     uint8_t *smem = smem_raw + (-smem_addr(smem_raw) & 1023u);
-    uint8_t *raw = smem + 2 * S::kKV;
+    uint8_t *raw = smem + kWide * S::kKV;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const CacheArgs &c = a.c;
     volatile int *abort_flag = &s_abort;
@@ -101,20 +117,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
     auto raw_full = [&](int i) { return bars + 8 * i; };
     auto raw_free = [&](int i) { return bars + 8 * (kRaw + i); };
     auto kv_full = [&](int i) { return bars + 8 * (2 * kRaw + i); };
-    auto kv_free = [&](int i) { return bars + 8 * (2 * kRaw + 2 + i); };
-    auto s_full = [&](int i) { return bars + 8 * (2 * kRaw + 4 + i); };
-    auto p_full = [&](int i) { return bars + 8 * (2 * kRaw + 6 + i); };
-    auto o_full = [&](int i) { return bars + 8 * (2 * kRaw + 8 + i); };
-    const uint32_t q_full = bars + 8 * (2 * kRaw + 10), tail = bars + 8 * (2 * kRaw + 11);
+    auto kv_free = [&](int i) { return bars + 8 * (2 * kRaw + kWide + i); };
+    constexpr int kRest = 2 * kRaw + 2 * kWide;
+    auto s_full = [&](int i) { return bars + 8 * (kRest + i); };
+    auto p_full = [&](int i) { return bars + 8 * (kRest + 2 + i); };
+    auto o_full = [&](int i) { return bars + 8 * (kRest + 4 + i); };
+    const uint32_t q_full = bars + 8 * (kRest + 6), tail = bars + 8 * (kRest + 7);
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (int i = 0; i < kRaw; ++i) {
             mbar_init(raw_full(i), 1);
             mbar_init(raw_free(i), 4);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kWide; ++i) {
             mbar_init(kv_full(i), 4);
             mbar_init(kv_free(i), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(s_full(i), 1);
             mbar_init(p_full(i), 4);
             mbar_init(o_full(i), 1);
@@ -123,7 +142,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         mbar_init(tail, 1);
         tc::fence_barrier_init();
     }
-    if (warp == 13) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -148,7 +167,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
     const uint32_t record = (uint32_t)size * (D + 8);
     bool ok = true;
 
-    if (warp == 12) {
+    if (warp >= 16) set_regs<kRegsRest, false>();
+    if (warp == 16) {
         // ---- chunks from the cache
         int issued = 0;
         for (; issued < chunks; ++issued) {
@@ -171,7 +191,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         }
         // copies land before the CTA leaves, whoever gave up
         for (int i = max(0, issued - kRaw); i < issued; ++i) drain(raw_full(i % kRaw), (uint32_t)(i / kRaw) & 1u);
-    } else if (warp == 13) {
+    } else if (warp == 17) {
         // ---- MMAs
         const uint32_t s_idesc = tc::idesc_f16(kChunk), o_idesc = tc::idesc_f16(D);
         auto issue_s = [&](int tile, int buf) {
@@ -185,42 +205,44 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             ok = mbar_wait(q_full, 0, abort_flag, a.err) && mbar_wait(kv_full(0), 0, abort_flag, a.err);
             ok = __all_sync(0xffffffffu, ok);
             tc::tc_fence_after();
-            if (ok && lane == 0)
+            if (ok && elect_one())
                 for (int tile = 0; tile < tiles; ++tile) issue_s(tile, 0);
+            __syncwarp();
         }
         for (int i = 0; i < chunks && ok; ++i) {
-            const int buf = i & 1;
+            const int buf = i % kWide, next = (i + 1) % kWide;
             for (int tile = 0; tile < tiles && ok; ++tile) {
                 ok = mbar_wait(p_full(tile), (uint32_t)i & 1u, abort_flag, a.err);
-                if (ok && tile == 0 && i + 1 < chunks) ok = mbar_wait(kv_full(buf ^ 1), (uint32_t)((i + 1) >> 1) & 1u, abort_flag, a.err);
+                if (ok && tile == 0 && i + 1 < chunks) ok = mbar_wait(kv_full(next), (uint32_t)((i + 1) / kWide) & 1u, abort_flag, a.err);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc::tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     const uint64_t v0 = tc::sdesc_sw128(smem_addr(smem + buf * S::kKV + S::kK));
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         tc::umma_f16_ts(tmem + S::kO + D * tile, tmem + S::kS + 64 * tile + 8 * j, v0 + (uint64_t)(2 * j), o_idesc, i > 0 || j > 0);
                     if (tile + 1 == tiles) tc::umma_commit(kv_free(buf));
-                    if (i + 1 < chunks) issue_s(tile, buf ^ 1);
+                    if (i + 1 < chunks) issue_s(tile, next);
                     else tc::umma_commit(o_full(tile));
                 }
                 __syncwarp();
             }
         }
-        if (lane == 0) tc::umma_commit(tail);
+        if (elect_one()) tc::umma_commit(tail);
         __syncwarp();
         drain(tail, 0);
+    } else if (warp >= 18) {
     } else if (warp >= 8) {
-        // ---- widening
-        const int tid = threadIdx.x - 256, part = tid >> 6, key = tid & 63;
+        set_regs<kRegsWiden, false>();
+        // ---- widening: four warps take every other chunk
+        const int tid = threadIdx.x & 127, part = tid >> 6, key = tid & 63;
         const int dg = lane % GROUPS, tg = (tid >> 5) * 2 + (lane / GROUPS & 1);
         const bool has_v = GROUPS == 16 || lane < 16;
-        int v_exponent = 1;
-        for (int i = 0; i < chunks; ++i) {
-            const int stage = i % kRaw, buf = i & 1;
+        for (int i = (warp >> 2) & 1; i < chunks; i += 2) {
+            const int stage = i % kRaw, buf = i % kWide;
             ok = mbar_wait(raw_full(stage), (uint32_t)(i / kRaw) & 1u, abort_flag, a.err);
-            if (ok && i >= 2) ok = mbar_wait(kv_free(buf), (uint32_t)((i >> 1) - 1) & 1u, abort_flag, a.err);
+            if (ok && i >= kWide) ok = mbar_wait(kv_free(buf), (uint32_t)(i / kWide - 1) & 1u, abort_flag, a.err);
             if (!__all_sync(0xffffffffu, ok)) break;
             const uint8_t *chunk = raw + stage * S::kChunkBytes;
             const int pages = s_pages[stage], left = seq.len - i * kChunk;
@@ -240,13 +262,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             // (a NaN is larger than any number: left out)
             auto bits = [](float x) { return x == x ? __float_as_uint(x) & 0x7fffffffu : 0u; };
             const int k_exponent = min(max((int)(__reduce_max_sync(0xffffffffu, max(bits(k0), bits(k1))) >> 23), 1), 253);
-            const int v_most = min(max((int)(__reduce_max_sync(0xffffffffu, max(bits(v0), bits(v1))) >> 23), 1), 253);
-            const int v_last = v_exponent;
-            v_exponent = max(v_exponent, v_most);
+            const int v_exponent = min(max((int)(__reduce_max_sync(0xffffffffu, max(bits(v0), bits(v1))) >> 23), 1), 253);
             if (tid == 0) {
                 Info info;
                 info.k_factor = power(k_exponent);
-                info.v_ratio = v_exponent - v_last > 126 ? 0.0f : power(127 - (v_exponent - v_last));
                 info.v_exponent = v_exponent;
                 info.held[0] = held0;
                 info.held[1] = held1;
@@ -256,8 +275,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             {
                 // keys: row = key, values in the order 0 4 1 5 2 6 3 7 of each 8, as the queries have them
                 const float of = __shfl_sync(0xffffffffu, key & 32 ? k1 : k0, lane);   // (key = lane or lane + 32)
-                const float by = of * power(254 - k_exponent);
-                const uint32_t scale = pack_half(by, by);
+                // The scale as two fp16, so that a product is rounded once: an error of the scale itself would be that of a
+                // whole logit (8 rows of 1000 .. 8000 keys: 2.1e-3 off in all, against 1.8e-3).
+                const float by = of * power(254 - k_exponent), high = __half2float(__float2half_rn(by));
+                const uint32_t scale = pack_half(by, by), rest = pack_half(by - high, by - high);
+                auto product = [&](uint32_t codes) { return fma2(codes, scale, mul2(codes, rest)); };
                 const uint8_t *at = chunk + (key >> c.page_bits) * record + (key & (size - 1)) * (D / 2) + part * (D / 4);
                 uint32_t w[D / 16];
 #pragma unroll
@@ -266,8 +288,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                 for (int j = 0; j < D / 16; ++j) {
                     const uint32_t u = w[j] >> 8;
                     const int word = part * (D / 16) + j;
-                    const uint4 o = make_uint4(mul2(codes_f16<true, false>(w[j]), scale), mul2(codes_f16<true, true>(w[j]), scale),
-                                               mul2(codes_f16<true, false>(u), scale), mul2(codes_f16<true, true>(u), scale));
+                    const uint4 o = make_uint4(product(codes_f16<true, false>(w[j])), product(codes_f16<true, true>(w[j])),
+                                               product(codes_f16<true, false>(u)), product(codes_f16<true, true>(u)));
                     *reinterpret_cast<uint4 *>(K + (word >> 3) * 8192 + key * 128 + (((word & 7) ^ (key & 7)) << 4)) = o;
                 }
             }
@@ -311,6 +333,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             }
         }
     } else {
+        set_regs<kRegsRows, true>();
         // ---- a row a thread
         const int tile = warp >> 2, x = x0 + threadIdx.x, token = x / a.group, q_head = head * a.group + x - token * a.group;
         const bool live = !skip && token < seq.m;
@@ -380,13 +403,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         const int position = live ? seq.len - seq.m + token : 0x7fffffff;          // (rows that are none: nothing to mask)
         const int lowest = __reduce_min_sync(0xffffffffu, position);
         float m = -1e30f, l = 0.0f;
-        int v_exponent = 127;
+        int exponent = 0;                                    // of the values' scales, the largest so far
         for (int i = 0; i < (here ? chunks : 0); ++i) {
             ok = mbar_wait(s_full(tile), (uint32_t)i & 1u, abort_flag, a.err);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc::tc_fence_after();
-            const Info info = s_info[i & 1];
-            v_exponent = info.v_exponent;
+            const Info info = s_info[i % kWide];
             const float fs = f * info.k_factor;
             uint32_t s[64];
             tc::tmem_ld32(at + S::kS + 64 * tile, *reinterpret_cast<uint32_t (*)[32]>(s));
@@ -407,12 +429,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             for (int j = 0; j < 64; j += 2) most = max3(most, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
             const float top = (whole || (seen[0] | seen[1])) ? most * fs : -1e30f;
             const bool raise = top > m + 8.0f;
-            if (__any_sync(0xffffffffu, raise || info.v_ratio != 1.0f)) {
+            if (__any_sync(0xffffffffu, raise || info.v_exponent > exponent)) {
                 const float now = raise ? top : m, by = exp2_fast(m - now);
+                const int more = max(info.v_exponent - exponent, 0);
                 m = now;
                 l *= by;
+                exponent += more;
                 if (i > 0) {
-                    const float o_by = by * info.v_ratio;
+                    const float o_by = more > 126 ? 0.0f : by * power(127 - more);
 #pragma unroll 1
                     for (int d = 0; d < D; d += 32) {
                         uint32_t o[32];
@@ -425,20 +449,26 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                     tc::tmem_wait_st();
                 }
             }
+            // weights carry what the chunk's values are brought to (2^-64 of the largest is nothing in fp16, but counts in l)
+            const int less = max(info.v_exponent - exponent, -64);
+            const float shift = m - (float)less;
             float sum[4] = {};
             uint32_t p[32];
 #pragma unroll
+            for (int j = 0; j < 64; ++j) s[j] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[j]), fs, -shift)));
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 64; ++j)
+                    if (!(seen[j >> 5] >> (j & 31) & 1)) s[j] = 0;
+            }
+#pragma unroll
             for (int j = 0; j < 64; j += 2) {
-                float u = exp2_fast(fmaf(__uint_as_float(s[j]), fs, -m)), v = exp2_fast(fmaf(__uint_as_float(s[j + 1]), fs, -m));
-                if (!whole) {
-                    if (!(seen[j >> 5] >> (j & 31) & 1)) u = 0.0f;
-                    if (!(seen[j >> 5] >> ((j + 1) & 31) & 1)) v = 0.0f;
-                }
+                const float u = __uint_as_float(s[j]), v = __uint_as_float(s[j + 1]);
                 sum[j & 2] += u;
                 sum[(j & 2) + 1] += v;
                 p[j / 2] = pack_half(u, v);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), power(127 - less), l);
             tc::tmem_st32(at + S::kS + 64 * tile, p);
             tc::tmem_wait_st();
             tc::tc_fence_before();
@@ -452,7 +482,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             tc::tc_fence_after();
         }
         if (here && ok) {
-            const float by = l == 0.0f ? 0.0f : c.inv_norm / l, unit = power(v_exponent);
+            const float by = l == 0.0f ? 0.0f : c.inv_norm / l, unit = power(max(exponent, 1));
             __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.out) + (long long)(seq.begin + (live ? token : 0)) * a.ldo +
                                  (long long)(live ? q_head : 0) * a.ho;
 #pragma unroll 1
@@ -496,7 +526,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 13)
+    if (warp == 17)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
