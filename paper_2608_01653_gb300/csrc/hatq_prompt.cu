@@ -15,7 +15,8 @@ using tc::mbar_wait;
 using tc::smem_addr;
 
 // The formulas of hatq_attend.cu for two tiles of 128 query columns of a kv head at a time: S = Q K^T (128 x 64 keys),
-// O += P V (128 x D), Q and P in tensor memory, codes widened once for both tiles into shared memory. bf16 queries only:
+// O += P V (128 x D), Q and P in tensor memory (of heads of 128 the second tile's Q has no room there and is in shared
+// memory), codes widened once for both tiles into shared memory. bf16 queries only:
 // rounded to fp16 are q and p as there, and here also code times scale of keys and of values (an error of 2^-12 each,
 // against 2^-9 of the output), so that a logit costs one instruction less than it would with a factor of its key.
 //
@@ -33,15 +34,18 @@ using tc::smem_addr;
 // each scheduler.
 constexpr int kRaw = 4;                // chunks on their way or being widened
 constexpr int kWide = 4;               // widened chunks
-// Five groups of four warps; the last has two that rest. Registers are handed on between them: 640 x 96 at launch.
+// Five groups of four warps; the last has one that rests. Registers are handed on between them: 640 x 96 at launch.
 constexpr int kPromptThreads = 20 * 32, kRegsLaunch = 96, kRegsRows = 144, kRegsWiden = 72, kRegsRest = 40;
 static_assert(256 * kRegsRows + 256 * kRegsWiden + 128 * kRegsRest <= kPromptThreads * kRegsLaunch, "setmaxnreg waits for registers that there are");
 
 template <int D>
 struct Shape {
     static constexpr int kChunkBytes = kChunk * (D + 8), kK = kChunk * D * 2, kKV = 2 * kK;
-    static constexpr int kO = 0, kQ = 2 * D, kS = 3 * D;     // columns of tensor memory: two tiles each of D, D / 2, 64
-    static constexpr int kBytes = 1024 + kWide * kKV + kRaw * kChunkBytes;
+    // columns of tensor memory: two tiles each of D, 64, 32; then Q, D / 2 a tile, of the second where that is left
+    static constexpr int kO = 0, kS = 2 * D, kP = kS + 128, kQ = kP + 64;
+    static constexpr bool kSecond = kQ + D <= 512;
+    static constexpr int kQBytes = kSecond ? 0 : 128 * D * 2;
+    static constexpr int kBytes = 1024 + kQBytes + kWide * kKV + kRaw * kChunkBytes;
 };
 
 struct Info {                          // of a widened chunk, for the rows
@@ -104,12 +108,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
     using S = Shape<D>;
     constexpr int GROUPS = D / 8;                            // of 8 neighbouring values
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_bars[2 * kRaw + 2 * kWide + 8];
+    __shared__ __align__(8) uint64_t s_bars[2 * kRaw + 2 * kWide + 11];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_pages[kRaw];
     __shared__ Info s_info[kWide];
     uint8_t *smem = smem_raw + (-smem_addr(smem_raw) & 1023u);
-    uint8_t *raw = smem + kWide * S::kKV;
+    uint8_t *wide = smem + S::kQBytes, *raw = wide + kWide * S::kKV;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const CacheArgs &c = a.c;
     volatile int *abort_flag = &s_abort;
@@ -122,7 +126,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
     auto s_full = [&](int i) { return bars + 8 * (kRest + i); };
     auto p_full = [&](int i) { return bars + 8 * (kRest + 2 + i); };
     auto o_full = [&](int i) { return bars + 8 * (kRest + 4 + i); };
-    const uint32_t q_full = bars + 8 * (kRest + 6), tail = bars + 8 * (kRest + 7);
+    auto s_free = [&](int i) { return bars + 8 * (kRest + 6 + i); };
+    auto tail = [&](int i) { return bars + 8 * (kRest + 8 + i); };
+    const uint32_t q_full = bars + 8 * (kRest + 10);
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (int i = 0; i < kRaw; ++i) {
@@ -131,15 +137,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         }
         for (int i = 0; i < kWide; ++i) {
             mbar_init(kv_full(i), 4);
-            mbar_init(kv_free(i), 1);
+            mbar_init(kv_free(i), 2);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full(i), 1);
+            mbar_init(s_free(i), 4);
             mbar_init(p_full(i), 4);
             mbar_init(o_full(i), 1);
+            mbar_init(tail(i), 1);
         }
         mbar_init(q_full, 8);
-        mbar_init(tail, 1);
         tc::fence_barrier_init();
     }
     if (warp == 17) {
@@ -191,48 +198,63 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         }
         // copies land before the CTA leaves, whoever gave up
         for (int i = max(0, issued - kRaw); i < issued; ++i) drain(raw_full(i % kRaw), (uint32_t)(i / kRaw) & 1u);
-    } else if (warp == 17) {
-        // ---- MMAs
+    } else if (warp == 17 || warp == 18) {
+        // ---- MMAs of a tile. (One warp for both took 1750 cycles a chunk: a wait, a fence and a commit cost it about 300.)
+        const int tile = warp - 17;
         const uint32_t s_idesc = tc::idesc_f16(kChunk), o_idesc = tc::idesc_f16(D);
-        auto issue_s = [&](int tile, int buf) {
-            const uint64_t k0 = tc::sdesc_sw128(smem_addr(smem + buf * S::kKV));
+        const uint64_t q0 = tc::sdesc_sw128(smem_addr(smem)), wide0 = tc::sdesc_sw128(smem_addr(wide));
+        auto issue_s = [&](int i) {
+            if (elect_one()) {
+                const uint64_t k0 = wide0 + (uint64_t)(i % kWide * (S::kKV >> 4));
+                const uint32_t d = tmem + S::kS + 64 * tile;
+                if (tile == 0 || S::kSecond) {
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j)
-                tc::umma_f16_ts(tmem + S::kS + 64 * tile, tmem + S::kQ + D / 2 * tile + 8 * j, k0 + (uint64_t)((j / 4) * 512 + 2 * (j % 4)), s_idesc, j > 0);
-            tc::umma_commit(s_full(tile));
+                    for (int j = 0; j < D / 16; ++j)
+                        tc::umma_f16_ts(d, tmem + S::kQ + D / 2 * tile + 8 * j, k0 + (uint64_t)((j / 4) * 512 + 2 * (j % 4)), s_idesc, j > 0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j)
+                        tc::umma_f16_ss(d, q0 + (uint64_t)((j / 4) * 1024 + 2 * (j % 4)), k0 + (uint64_t)((j / 4) * 512 + 2 * (j % 4)), s_idesc, j > 0);
+                }
+                tc::umma_commit(s_full(tile));
+            }
+            __syncwarp();
         };
-        if (chunks) {
+        const int mine = tile < tiles ? chunks : 0;
+        if (mine) {
             ok = mbar_wait(q_full, 0, abort_flag, a.err) && mbar_wait(kv_full(0), 0, abort_flag, a.err);
             ok = __all_sync(0xffffffffu, ok);
             tc::tc_fence_after();
-            if (ok && elect_one())
-                for (int tile = 0; tile < tiles; ++tile) issue_s(tile, 0);
-            __syncwarp();
+            if (ok) issue_s(0);
         }
-        for (int i = 0; i < chunks && ok; ++i) {
-            const int buf = i % kWide, next = (i + 1) % kWide;
-            for (int tile = 0; tile < tiles && ok; ++tile) {
-                ok = mbar_wait(p_full(tile), (uint32_t)i & 1u, abort_flag, a.err);
-                if (ok && tile == 0 && i + 1 < chunks) ok = mbar_wait(kv_full(next), (uint32_t)((i + 1) / kWide) & 1u, abort_flag, a.err);
+        for (int i = 0; i < mine && ok; ++i) {
+            if (i + 1 < chunks) {
+                // S of the next chunk as soon as the rows have read this one's
+                ok = mbar_wait(s_free(tile), (uint32_t)i & 1u, abort_flag, a.err) &&
+                     mbar_wait(kv_full((i + 1) % kWide), (uint32_t)((i + 1) / kWide) & 1u, abort_flag, a.err);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc::tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t v0 = tc::sdesc_sw128(smem_addr(smem + buf * S::kKV + S::kK));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        tc::umma_f16_ts(tmem + S::kO + D * tile, tmem + S::kS + 64 * tile + 8 * j, v0 + (uint64_t)(2 * j), o_idesc, i > 0 || j > 0);
-                    if (tile + 1 == tiles) tc::umma_commit(kv_free(buf));
-                    if (i + 1 < chunks) issue_s(tile, next);
-                    else tc::umma_commit(o_full(tile));
-                }
-                __syncwarp();
+                issue_s(i + 1);
             }
+            ok = __all_sync(0xffffffffu, mbar_wait(p_full(tile), (uint32_t)i & 1u, abort_flag, a.err));
+            if (!ok) break;
+            tc::tc_fence_after();
+            if (elect_one()) {
+                const uint64_t v0 = wide0 + (uint64_t)(i % kWide * (S::kKV >> 4) + (S::kK >> 4));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    tc::umma_f16_ts(tmem + S::kO + D * tile, tmem + S::kP + 32 * tile + 8 * j, v0 + (uint64_t)(2 * j), o_idesc, i > 0 || j > 0);
+                tc::umma_commit(o_full(tile));
+                tc::umma_commit(kv_free(i % kWide));
+                if (tiles == 1) mbar_arrive(kv_free(i % kWide));          // (no other tile's)
+            }
+            __syncwarp();
         }
-        if (elect_one()) tc::umma_commit(tail);
+        if (elect_one()) tc::umma_commit(tail(tile));
         __syncwarp();
-        drain(tail, 0);
-    } else if (warp >= 18) {
+        drain(tail(tile), 0);
+    } else if (warp == 19) {
     } else if (warp >= 8) {
         set_regs<kRegsWiden, false>();
         // ---- widening: four warps take every other chunk
@@ -271,7 +293,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                 info.held[1] = held1;
                 s_info[buf] = info;
             }
-            uint8_t *K = smem + buf * S::kKV, *V = K + S::kK;
+            uint8_t *K = wide + buf * S::kKV, *V = K + S::kK;
             {
                 // keys: row = key, values in the order 0 4 1 5 2 6 3 7 of each 8, as the queries have them
                 const float of = __shfl_sync(0xffffffffu, key & 32 ? k1 : k0, lane);   // (key = lane or lane + 32)
@@ -392,10 +414,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                     const int d = (i >> 2) * 8 + (i & 3);
                     r[i] = pack_half(live ? v[d] * by : 0.0f, live ? v[d + 4] * by : 0.0f);
                 }
-                tc::tmem_st32(at + S::kQ + D / 2 * tile + 32 * half, r);
+                if (tile == 0 || S::kSecond) {
+                    tc::tmem_st32(at + S::kQ + D / 2 * tile + 32 * half, r);
+                } else {
+                    // a panel of 64 values: rows of 128 bytes, 16-byte pieces exchanged by the row
+                    const int of = threadIdx.x & 127;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4 *>(smem + half * 16384 + of * 128 + ((i ^ (of & 7)) << 4)) =
+                            make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                }
             }
             tc::tmem_wait_st();
             tc::tc_fence_before();
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full);
@@ -414,6 +446,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             tc::tmem_ld32(at + S::kS + 64 * tile, *reinterpret_cast<uint32_t (*)[32]>(s));
             tc::tmem_ld32(at + S::kS + 64 * tile + 32, *reinterpret_cast<uint32_t (*)[32]>(s + 32));
             tc::tmem_wait_ld();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(s_free(tile));
             const bool whole = i * kChunk + kChunk - 1 <= lowest && (info.held[0] & info.held[1]) == 0xffffffffu;
             unsigned seen[2] = {0xffffffffu, 0xffffffffu};
             if (!whole) {
@@ -429,7 +464,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             for (int j = 0; j < 64; j += 2) most = max3(most, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
             const float top = (whole || (seen[0] | seen[1])) ? most * fs : -1e30f;
             const bool raise = top > m + 8.0f;
+            // the last chunk's weights are used, and O is there
+            auto wait_used = [&]() {
+                if (i > 0) ok = __all_sync(0xffffffffu, mbar_wait(o_full(tile), (uint32_t)(i - 1) & 1u, abort_flag, a.err));
+                tc::tc_fence_after();
+            };
             if (__any_sync(0xffffffffu, raise || info.v_exponent > exponent)) {
+                wait_used();
+                if (!ok) break;
                 const float now = raise ? top : m, by = exp2_fast(m - now);
                 const int more = max(info.v_exponent - exponent, 0);
                 m = now;
@@ -469,7 +511,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                 p[j / 2] = pack_half(u, v);
             }
             l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), power(127 - less), l);
-            tc::tmem_st32(at + S::kS + 64 * tile, p);
+            wait_used();
+            if (!ok) break;
+            tc::tmem_st32(at + S::kP + 32 * tile, p);
             tc::tmem_wait_st();
             tc::tc_fence_before();
             __syncwarp();
@@ -478,7 +522,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         // ---- the row's output
         ok = __all_sync(0xffffffffu, ok);
         if (here && chunks && ok) {
-            ok = __all_sync(0xffffffffu, mbar_wait(o_full(tile), 0, abort_flag, a.err));
+            ok = __all_sync(0xffffffffu, mbar_wait(o_full(tile), (uint32_t)(chunks - 1) & 1u, abort_flag, a.err));
             tc::tc_fence_after();
         }
         if (here && ok) {
