@@ -305,22 +305,31 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     };
     // Pieces of x, zeros behind the last row and input. As they lie, by asynchronous copies; otherwise through registers.
     const bool direct = a.vec && PARTS == 1;
-    auto bring = [&](int i) {
+    // A thread has the same 8 inputs of every 16th row.
+    const int x_row = threadIdx.x >> 4, x_k = (threadIdx.x & 15) * 8;
+    const T *x_first = static_cast<const T *>(a.x) + (long long)row0 * a.ldx, *x_mine = x_first + (long long)min(x_row, live - 1) * a.ldx + x_k;
+    uint8_t *x_to = xs + x_row * kManyPitch + 2 * x_k;
+    auto bring = [&](int i, int stage) {
         if (i < to - from) {
             const int k0 = (from + i) * kManyDepth;
-            uint8_t *stage = xs + i % XS * XSTAGE;
-            for (int j = threadIdx.x; j < ROWS * (kManyDepth / 8); j += kCtaWarps * 32) {
-                const int row = j / (kManyDepth / 8), k = j % (kManyDepth / 8) * 8;
-                uint8_t *to_x = stage + row * kManyPitch + 2 * k;
-                const T *p = static_cast<const T *>(a.x) + (long long)(row0 + min(row, live - 1)) * a.ldx;
-                if (direct) {
-                    const int bytes = row < live ? min(max(2 * (a.k - k0 - k), 0), 16) : 0;
-                    async_copy(tc::smem_addr(to_x), p + (bytes ? k0 + k : 0), bytes);
-                } else {
-                    uint4 v[PARTS];
-                    load8<T>(a, p, row < live, k0 + k, v);
+            uint8_t *to_x = x_to + stage * XSTAGE;
+            if (direct) {
+                const int there = min(max(2 * (a.k - k0 - x_k), 0), 16);
+                const uint32_t dst = tc::smem_addr(to_x);
+                const T *p = x_mine + k0;
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<uint4 *>(to_x + part * PART) = v[part];
+                for (int j = 0; j < ROWS / 16; ++j) {
+                    const int bytes = x_row + 16 * j < live ? there : 0;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst + 16 * j * kManyPitch),
+                                 "l"(bytes ? p + j * 16 * a.ldx : x_first), "r"(bytes)
+                                 : "memory");
+                }
+            } else {
+                for (int j = 0; j < ROWS / 16; ++j) {
+                    uint4 v[PARTS];
+                    load8<T>(a, x_first + (long long)min(x_row + 16 * j, live - 1) * a.ldx, x_row + 16 * j < live, k0 + x_k, v);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<uint4 *>(to_x + 16 * j * kManyPitch + part * PART) = v[part];
                 }
             }
         }
@@ -329,22 +338,23 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     if (sound) {
         for (int i = 0; i < kManyStages; ++i) ask(i);
 #pragma unroll
-        for (int i = 0; i < XS - 1; ++i) bring(i);
+        for (int i = 0; i < XS - 1; ++i) bring(i, i);
     }
     float total[NT][4] = {};
-    int done = 0;
+    int done = 0, x_stage = 0;
     for (; sound && done < to - from; ++done) {
         const int stage = done % kManyStages, n = min(PIECE_UNITS, a.units - (from + done) * PIECE_UNITS);
         asm volatile("cp.async.wait_group %0;" ::"n"(XS - 2) : "memory");
         const bool here = tc::mbar_wait(bar + 8 * stage, (uint32_t)(done / kManyStages) & 1u, abort_flag, a.err);
         sound = !__syncthreads_or(!here);
         if (!sound) break;
-        bring(done + XS - 1);
-        const uint8_t *x = xs + done % XS * XSTAGE + g * kManyPitch + 16 * t;
+        bring(done + XS - 1, x_stage == 0 ? XS - 1 : x_stage - 1);
+        const uint8_t *x = xs + x_stage * XSTAGE + g * kManyPitch + 16 * t;
         for (int i = 0; i < n; ++i)
             unit_products<T, NT, BLOCKS, SCALES>(ring + stage * kManyRing + i * UNIT, x + i * (BLOCKS * 2 * kStep), 8 * kManyPitch, PART, lane, total);
         __syncwarp();
         ask(done + kManyStages);
+        if (++x_stage == XS) x_stage = 0;
     }
     if (!sound) {                                            // (copies on their way have to land before the CTA leaves)
         const long long t0 = clock64();

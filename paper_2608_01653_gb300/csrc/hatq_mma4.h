@@ -36,12 +36,18 @@ __device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4],
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
+// (w & mask) | bits in one instruction, which has room for one constant: the other is in a register
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask, uint32_t bits) {
+    uint32_t x;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(w), "r"(mask), "r"(bits));
+    return x;
+}
 // The codes of a word at bits 0-3 (ODD: 4-7) of its halves, as A operands: bare, subnormal numbers (code + 8) 2^-24 and
 // 2^-20, or (WHOLE) the codes themselves: 1024 + x and 1024 + 16 x are fp16 numbers whose last bits are x.
 template <bool WHOLE, bool ODD>
 __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
     if constexpr (!WHOLE) return w & (ODD ? 0x00f000f0u : 0x000f000fu);
-    uint32_t x = (w & (ODD ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    uint32_t x = masked(w, ODD ? 0x00f000f0u : 0x000f000fu, 0x64006400u);
     if constexpr (ODD)
         asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(x) : "r"(0x2c002c00u), "r"(0xd480d480u));      // x / 16 - 72
     else
@@ -51,7 +57,7 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
 
 // The codes at bits 0-3 of a word's halves as bf16: 128 + x has x in its last bits.
 __device__ __forceinline__ uint32_t codes_bf16(uint32_t w) {
-    uint32_t x = (w & 0x000f000fu) | 0x43004300u;
+    uint32_t x = masked(w, 0x000f000fu, 0x43004300u);
     asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(x) : "r"(0xc308c308u));                               // x - 136
     return x;
 }
