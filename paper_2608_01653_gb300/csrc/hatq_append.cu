@@ -101,7 +101,7 @@ __device__ __forceinline__ void transform_pairs(__half2 (&v)[N / 2], int hb, int
 
 // C runs of 16 values a lane: heads of 64 C. Keys where blockIdx.y is 0, values where it is 1.
 template <typename T, int C>
-__global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(256, C <= 2 ? 3 : 1) append_kernel(const AppendArgs a) {
     constexpr int N = 16 * C;
     after_prior_kernels();
     const CacheArgs &c = a.c;

@@ -315,21 +315,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                     *reinterpret_cast<uint4 *>(K + (word >> 3) * 8192 + key * 128 + (((word & 7) ^ (key & 7)) << 4)) = o;
                 }
             }
+            // tokens 2 lane and 2 lane + 1 of the half of the chunk that this warp's groups lie in, in lanes 0 .. 15
+            const float v_own = (tg < 4 ? v0 : v1) * power(254 - v_exponent);
+            const uint32_t v_pairs = pack_half(__shfl_sync(0xffffffffu, v_own, 2 * lane & 31), __shfl_sync(0xffffffffu, v_own, (2 * lane + 1) & 31));
+            const unsigned has_v_mask = GROUPS == 16 ? 0xffffffffu : 0x0000ffffu;
             if (has_v) {
                 // values, transposed: 8 tokens of 8 values; value 8 dg + j is row j GROUPS + dg
-                uint32_t w[8], scale[4];
+                uint32_t w[8], scale[4];                     // (these tokens' scales: of lanes' first keys, or of their second)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int token = tg * 8 + j;
                     w[j] = *reinterpret_cast<const uint32_t *>(chunk + (token >> c.page_bits) * record + (size + (token & (size - 1))) * (D / 2) + 4 * dg);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float ka, va, kb, vb;
-                    scales(tg * 8 + 2 * j, ka, va);
-                    scales(tg * 8 + 2 * j + 1, kb, vb);
-                    scale[j] = pack_half(va * power(254 - v_exponent), vb * power(254 - v_exponent));
-                }
+                for (int j = 0; j < 4; ++j) scale[j] = __shfl_sync(has_v_mask, v_pairs, (tg & 3) * 4 + j);
                 uint32_t o[8][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
