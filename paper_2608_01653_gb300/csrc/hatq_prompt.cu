@@ -35,7 +35,7 @@ using tc::smem_addr;
 constexpr int kRaw = 4;                // chunks on their way or being widened
 constexpr int kWide = 4;               // widened chunks
 // Five groups of four warps; the last has one that rests. Registers are handed on between them: 640 x 96 at launch.
-constexpr int kPromptThreads = 20 * 32, kRegsLaunch = 96, kRegsRows = 144, kRegsWiden = 72, kRegsRest = 40;
+constexpr int kPromptThreads = 20 * 32, kRegsLaunch = 96, kRegsRows = 136, kRegsWiden = 72, kRegsRest = 56;
 static_assert(256 * kRegsRows + 256 * kRegsWiden + 128 * kRegsRest <= kPromptThreads * kRegsLaunch, "setmaxnreg waits for registers that there are");
 
 template <int D>
@@ -575,6 +575,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
 
 template <int D>
 cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
+    // shares of registers that the launch does not bring would be waited for forever
+    static const int regs = [] {
+        cudaFuncAttributes fa{};
+        return cudaFuncGetAttributes(&fa, prompt_kernel<D>) == cudaSuccess ? fa.numRegs : 0;
+    }();
+    if (regs != kRegsLaunch) return cudaErrorInvalidConfiguration;
     static std::atomic<int> allowed[64];
     const cudaError_t e = allow_shared(reinterpret_cast<const void *>(prompt_kernel<D>), Shape<D>::kBytes, allowed);
     if (e != cudaSuccess) return e;
