@@ -30,12 +30,14 @@ __device__ __forceinline__ void load16(const T *p, bool vec, float *v) {
     }
 }
 
-// neighbours first: distances 1 .. 8 within the lane, 16 and 32 between lanes, 64 and 128 between a lane's runs of 16
-template <int N>
+// Neighbours first: distances 1 .. 8 within the lane, 16 and 32 between lanes, 64 and 128 between a lane's runs of 16.
+// FULL: hb is all of it, known to the compiler, which then need not bring results back to where they were for a stage that
+// may be left out (a seventh of all instructions).
+template <int N, bool FULL>
 __device__ __forceinline__ void transform(float (&v)[N], int hb, int t) {
 #pragma unroll
     for (int h = 1; h < 16; h *= 2)
-        if (h < hb)
+        if (FULL || h < hb)
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (!(i & h)) {
@@ -45,14 +47,14 @@ __device__ __forceinline__ void transform(float (&v)[N], int hb, int t) {
                 }
 #pragma unroll
     for (int h = 1; h < 4; h *= 2)
-        if (16 * h < hb) {
+        if (FULL || 16 * h < hb) {
             const float sign = t & h ? -1.0f : 1.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = fmaf(sign, v[i], __shfl_xor_sync(0xffffffffu, v[i], h));
         }
 #pragma unroll
-    for (int h = 16; h < N; h *= 2)
-        if (4 * h < hb)
+    for (int h = 16; h < (FULL ? N & -N : N); h *= 2)
+        if (FULL || 4 * h < hb)
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (!(i & h) && i + h < N) {
@@ -63,16 +65,16 @@ __device__ __forceinline__ void transform(float (&v)[N], int hb, int t) {
 }
 
 // the same of whole numbers in pairs (2 i, 2 i + 1)
-template <int N>
+template <int N, bool FULL>
 __device__ __forceinline__ void transform_pairs(__half2 (&v)[N / 2], int hb, int t) {
-    if (hb > 1) {
+    if (FULL || hb > 1) {
         const __half2 sign = __halves2half2(__float2half_rn(1.0f), __float2half_rn(-1.0f));
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) v[i] = __hfma2(v[i], sign, __lowhigh2highlow(v[i]));
     }
 #pragma unroll
     for (int h = 1; h < 8; h *= 2)
-        if (2 * h < hb)
+        if (FULL || 2 * h < hb)
 #pragma unroll
             for (int i = 0; i < N / 2; ++i)
                 if (!(i & h)) {
@@ -82,14 +84,14 @@ __device__ __forceinline__ void transform_pairs(__half2 (&v)[N / 2], int hb, int
                 }
 #pragma unroll
     for (int h = 1; h < 4; h *= 2)
-        if (16 * h < hb) {
+        if (FULL || 16 * h < hb) {
             const __half2 sign = __float2half2_rn(t & h ? -1.0f : 1.0f);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) v[i] = __hfma2(sign, v[i], __shfl_xor_sync(0xffffffffu, v[i], h));
         }
 #pragma unroll
-    for (int h = 8; h < N / 2; h *= 2)
-        if (8 * h < hb)
+    for (int h = 8; h < (FULL ? (N & -N) / 2 : N / 2); h *= 2)
+        if (FULL || 8 * h < hb)
 #pragma unroll
             for (int i = 0; i < N / 2; ++i)
                 if (!(i & h) && i + h < N / 2) {
@@ -99,8 +101,14 @@ __device__ __forceinline__ void transform_pairs(__half2 (&v)[N / 2], int hb, int
                 }
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // C runs of 16 values a lane: heads of 64 C. Keys where blockIdx.y is 0, values where it is 1.
-template <typename T, int C>
+template <typename T, int C, bool FULL>
 __global__ void __launch_bounds__(256, C <= 2 ? 3 : 1) append_kernel(const AppendArgs a) {
     constexpr int N = 16 * C;
     after_prior_kernels();
@@ -135,15 +143,14 @@ __global__ void __launch_bounds__(256, C <= 2 ? 3 : 1) append_kernel(const Appen
         if (at >= 0) page = c.table[b * c.ldt + (at >> c.page_bits)];            // at < length <= capacity
     }
 
-    transform<N>(v, c.hb, t);
+    transform<N, FULL>(v, c.hb, t);
     float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        most = fmaxf(most, fabsf(v[i]));
-        if (v[i] != v[i]) most = __int_as_float(0x7f800000);
+        most = max_nan(most, fabsf(v[i]));
     }
 #pragma unroll
-    for (int h = 1; h < 4; h *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, h));
+    for (int h = 1; h < 4; h *= 2) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, h));
     const bool sound = 7.0f * most < __int_as_float(0x7f800000), some = sound && most > 0.0f;
     // (7 / a overflows where a is subnormal: every value is then divided)
     const float inv = some ? 7.0f / most : 0.0f;
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 3 : 1) append_kernel(const Appen
     __half2 pairs[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) pairs[i] = __floats2half2_rn(n[2 * i], n[2 * i + 1]);
-    transform_pairs<N>(pairs, c.hb, t);
+    transform_pairs<N, FULL>(pairs, c.hb, t);
     if (!held) return;
     const float back = step * c.inv_norm;
     T *kept = static_cast<T *>(a.kept[part]) + ((long long)r * c.heads + head) * (64 * C) + 16 * t;
@@ -204,7 +211,9 @@ __global__ void __launch_bounds__(256, C <= 2 ? 3 : 1) append_kernel(const Appen
 
 template <typename T, int C>
 cudaError_t launch(const AppendArgs &a, cudaStream_t s) {
-    return launch_early(append_kernel<T, C>, dim3((unsigned)(((long long)a.c.rows * a.c.heads + 63) / 64), 2), 256, 0, s, a);
+    const dim3 grid((unsigned)(((long long)a.c.rows * a.c.heads + 63) / 64), 2);
+    constexpr int all = 64 * C & -(64 * C);
+    return a.c.hb == all ? launch_early(append_kernel<T, C, true>, grid, 256, 0, s, a) : launch_early(append_kernel<T, C, false>, grid, 256, 0, s, a);
 }
 template <typename T>
 cudaError_t launch_type(const AppendArgs &a, cudaStream_t s) {

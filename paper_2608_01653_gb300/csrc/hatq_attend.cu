@@ -1,4 +1,6 @@
 // Attention over the 4-bit cache.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "hatq_cache.h"
@@ -259,9 +261,9 @@ __device__ __forceinline__ void finish(const AttendArgs &a, int r, int head, int
     for (int e = 0; e < D / 32; ++e) out[32 * e] = from_f32<T>(o[e] * by);
 }
 
-template <int D, typename T, int NT>
-__global__ void __launch_bounds__(kWarps(D, NT) * 32, 1) attend_kernel(const AttendArgs a) {
-    constexpr int COLS = 8 * NT, WARPS = kWarps(D, NT), STAGES = kStages(D, NT), STAGE = stage_bytes(D);
+template <int D, typename T, int NT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kernel(const AttendArgs a) {
+    constexpr int COLS = 8 * NT, STAGES = kStages(D, NT), STAGE = stage_bytes(D);
     constexpr int WORDS = D / 32, VW = D / 64, STEPS = D / 16, E = D / 32;
     constexpr bool kTwo = std::is_same<T, __half>::value;      // q and p in two parts
     constexpr int PARTS = kTwo ? 2 : 1;
@@ -846,14 +848,14 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
     if (q_head < a.q_heads) finish<D, T>(a, r, q_head, lane, o, l);
 }
 
-template <int D, typename T, int NT>
-cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
+template <int D, typename T, int NT, int WARPS>
+cudaError_t launch_warps(const AttendArgs &a, cudaStream_t s) {
     static std::atomic<int> allowed[64];
-    constexpr int bytes = kWarps(D, NT) * warp_smem(D, NT) + NT * (D / 32) * 512 * (std::is_same<T, __half>::value ? 2 : 1) + 32 * NT;
+    constexpr int bytes = WARPS * warp_smem(D, NT) + NT * (D / 32) * 512 * (std::is_same<T, __half>::value ? 2 : 1) + 32 * NT;
     static_assert(bytes <= 227 * 1024 - 256, "shared memory of a CTA");
-    cudaError_t e = allow_shared(reinterpret_cast<const void *>(attend_kernel<D, T, NT>), bytes, allowed);
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(attend_kernel<D, T, NT, WARPS>), bytes, allowed);
     if (e != cudaSuccess) return e;
-    if ((e = launch_early(attend_kernel<D, T, NT>, dim3((unsigned)(a.direct ? a.segments : a.sms)), kWarps(D, NT) * 32, bytes, s, a)) != cudaSuccess ||
+    if ((e = launch_early(attend_kernel<D, T, NT, WARPS>, dim3((unsigned)(a.direct ? a.segments : a.sms)), WARPS * 32, bytes, s, a)) != cudaSuccess ||
         a.direct)
         return e;
     // warps: no fewer than two for every SM's four schedulers
@@ -861,6 +863,10 @@ cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
     while (ways < 8 && (long long)a.c.rows * a.q_heads * ways < 8 * a.sms) ways *= 2;
     const long long joiners = (long long)a.c.rows * ((a.q_heads * ways + 7) / 8);
     return launch_early(join_kernel<D, T, NT>, dim3((unsigned)joiners), 256, 0, s, a, a.sms, ways);
+}
+template <int D, typename T, int NT>
+cudaError_t launch(const AttendArgs &a, cudaStream_t s) {
+    return a.direct == 2 ? launch_warps<D, T, NT, kWarps(D, NT) / 2>(a, s) : launch_warps<D, T, NT, kWarps(D, NT)>(a, s);
 }
 template <int D, typename T>
 cudaError_t launch_columns(const AttendArgs &a, cudaStream_t s) {
@@ -883,9 +889,20 @@ cudaError_t launch_type(const AttendArgs &a, cudaStream_t s) {
 // 16 columns where most sequences have more than 8 (queries times heads of a group)
 int attend_columns(int width, int group, long long rows, int seqs) { return width <= 128 && rows * group > 8LL * seqs ? 16 : 8; }
 int attend_workers(int width, int sms) { return sms * kWarps(width, 1); }
-bool attend_direct(int width, long long segments, int capacity, int sms) {
-    const long long waves = (segments + sms - 1) / sms, chunks = (capacity + kChunk - 1) / kChunk, warps = kWarps(width, 1);
-    return segments < (1LL << 31) && waves * ((chunks + warps - 1) / warps) * 2 <= segments * chunks / (sms * warps) * 2 + 5;
+int attend_direct(int width, int columns, long long segments, int capacity, int sms) {
+    if (segments >= 1LL << 31) return 0;
+    // All the host knows of lengths is the table's width. Measured: a CTA takes about 4 us to set out and end, a warp 1.2 us
+    // for a chunk, or what the memory takes where all SMs are at work (2.4 us for 12 warps' chunks of heads of 128); equal
+    // parts and the second kernel 18 us for both, and about 4.5 us (heads of 128) for the queries of every segment a warp
+    // comes to. Two CTAs of half the warps an SM where there are more segments than SMs: one sets out while the other reads.
+    // Direct against parts: 256 segments of 2050 keys, 64 wide, 18.9 us against 24; 328 of 320, 192 wide, 25 against 38;
+    // 512 of 8192 and fewer, 128 wide, 94 against 78; 2048 of one key, 192 wide, 62 against 45.
+    const int per_sm = segments > sms ? 2 : 1, full = kWarps(width, columns / 8), warps = full / per_sm;
+    const double slots = (double)sms * per_sm, chunks = (double)((capacity + kChunk - 1) / kChunk), workers = (double)sms * full;
+    const double memory = 2.4 * width / 128, waves = std::ceil((double)segments / slots), steps = std::ceil(chunks / warps);
+    const double direct = waves * (4 + std::max(1.2, memory * std::min(1.0, (double)segments / slots)) * steps);
+    const double parts = 18 + (double)segments * chunks / workers * memory + (double)segments / workers * 4.5 * (width / 128.0) * (width / 128.0);
+    return direct <= parts ? per_sm : 0;
 }
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s) {
     return type == HATQ_F16 ? launch_type<__half>(a, s) : launch_type<__nv_bfloat16>(a, s);

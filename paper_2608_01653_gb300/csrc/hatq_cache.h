@@ -45,16 +45,17 @@ struct AttendArgs {
     float scale;                       // times log2(e): weights are powers of two
     float *pieces;
     long long segments;                // (sequence, head, tile): upper bound
-    bool direct, prompt;
+    int direct;                        // see attend_direct
+    bool prompt;
     bool vec_out;                      // rows of out lie on 16-byte boundaries
     int sms;
     int *err;
 };
 int attend_columns(int width, int group, long long rows, int seqs);
 int attend_workers(int width, int sms);
-// whether a CTA takes a whole segment and writes its outputs (rather than equal parts of all segments, which a second kernel
-// joins)
-bool attend_direct(int width, long long segments, int capacity, int sms);
+// CTAs an SM where one takes a whole segment and writes its outputs, or 0: equal parts of all segments, which a second
+// kernel joins
+int attend_direct(int width, int columns, long long segments, int capacity, int sms);
 cudaError_t launch_attend(const AttendArgs &a, int type, cudaStream_t s);
 
 constexpr int kPromptColumns = 256;    // of a CTA of the kernel for many queries per sequence

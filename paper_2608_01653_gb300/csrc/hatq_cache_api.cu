@@ -108,7 +108,10 @@ hatq_status attend_args(const hatq_token_cache *c, int type, int q_heads, long l
 // once a.sms is set
 size_t attend_bytes(hatq::AttendArgs &a, int type) {
     a.prompt = hatq::attend_prompt(type, a.c.width, a.c.heads, a.group, a.c.rows, a.c.seqs, a.sms);
-    a.direct = hatq::attend_direct(a.c.width, a.segments, a.c.capacity, a.sms);
+    // as many segments as there are if all sequences have as many rows
+    const long long seqs = a.c.seqs < a.c.rows ? a.c.seqs : a.c.rows, columns = ((long long)a.c.rows * a.group + seqs - 1) / seqs;
+    const long long segments = a.c.heads * seqs * ((columns + a.columns - 1) / a.columns);
+    a.direct = hatq::attend_direct(a.c.width, a.columns, segments, a.c.capacity, a.sms);
     return a.prompt || a.direct ? 0 : ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
 }
 
