@@ -304,6 +304,8 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         from = min(warp * each, seq.chunks);
         to = min(from + each, cta_to);
     } else {
+        // for the second kernel (by a warp of the last part, which may be a short one)
+        if (blockIdx.x + 1 == gridDim.x && warp + 1 == WARPS) row.write(c, a.group, lane, a.before);
         const Parts parts(total, gridDim.x, WARPS);
         cta_from = min(blockIdx.x * (parts.active * parts.units), total);
         cta_to = min((blockIdx.x + 1LL) * (parts.active * parts.units), total);
@@ -761,13 +763,10 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
     const int head = q_head / a.group, h = q_head - head * a.group;
     int b, begin, end;
     if (!sequence_of(c, r, lane, b, begin, end)) return;
-    Row<COLS> row;
-    row.read(c, a.group, lane, false);
     Sequence s{};
     measure<COLS>(c, a.group, s, b, begin, end);
-    long long before, segs;
-    row.before(c, a.group, lane, b, before, segs);
-    const Parts parts(row.total, ctas, WARPS);
+    const long long before = a.before[2 * b], segs = a.before[2 * b + 1], total = a.before[2 * c.seqs];
+    const Parts parts(total, ctas, WARPS);
     const long long cta_units = parts.active * parts.units;
     const int x = (r - begin) * a.group + h, tile = x / COLS, col = x % COLS;
     float mx = -1e30f, l = 0.0f, o[E];
@@ -778,8 +777,8 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
         // CTA between, those of its last.
         const long long seg = (long long)head * s.tiles + tile, u0 = before + seg * s.chunks, u1 = u0 + s.chunks;
         const long long c0 = divide(u0, cta_units), c1 = divide(u1 - 1, cta_units);
-        const long long from0 = c0 * cta_units, to0 = min(row.total, from0 + cta_units), from1 = c1 * cta_units;
-        const bool one0 = from0 == u0 && to0 <= u1, one1 = min(row.total, from1 + cta_units) <= u1;
+        const long long from0 = c0 * cta_units, to0 = min(total, from0 + cta_units), from1 = c1 * cta_units;
+        const bool one0 = from0 == u0 && to0 <= u1, one1 = min(total, from1 + cta_units) <= u1;
         const int w0 = (int)divide(u0 - from0, parts.units);
         const int n0 = one0 ? 1 : (int)divide(min(u1, to0) - 1 - from0, parts.units) - w0 + 1;
         const int n1 = c1 == c0 ? 0 : one1 ? 1 : (int)divide(u1 - 1 - from1, parts.units) + 1;

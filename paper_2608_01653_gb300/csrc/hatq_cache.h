@@ -43,6 +43,7 @@ struct AttendArgs {
     int columns;                       // of a tile
     bool vec;                          // rows of q lie on 16-byte boundaries
     float scale;                       // times log2(e): weights are powers of two
+    long long *before;                 // [2 seqs + 2]: units and segments before every sequence; all units (parts only)
     float *pieces;
     long long segments;                // (sequence, head, tile): upper bound
     int direct;                        // see attend_direct

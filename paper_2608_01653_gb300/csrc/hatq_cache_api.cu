@@ -105,6 +105,7 @@ hatq_status attend_args(const hatq_token_cache *c, int type, int q_heads, long l
     a.c.small = a.segments * ((a.c.capacity + hatq::kChunk - 1) / hatq::kChunk) < INT_MAX;
     return HATQ_OK;
 }
+size_t before_bytes(const hatq::AttendArgs &a) { return ((size_t)a.c.seqs + 1) * 16; }
 // once a.sms is set
 size_t attend_bytes(hatq::AttendArgs &a, int type) {
     a.prompt = hatq::attend_prompt(type, a.c.width, a.c.heads, a.group, a.c.rows, a.c.seqs, a.sms);
@@ -112,7 +113,7 @@ size_t attend_bytes(hatq::AttendArgs &a, int type) {
     const long long seqs = a.c.seqs < a.c.rows ? a.c.seqs : a.c.rows, columns = ((long long)a.c.rows * a.group + seqs - 1) / seqs;
     const long long segments = a.c.heads * seqs * ((columns + a.columns - 1) / a.columns);
     a.direct = hatq::attend_direct(a.c.width, a.columns, segments, a.c.capacity, a.sms);
-    return a.prompt || a.direct ? 0 : ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
+    return a.prompt || a.direct ? 0 : before_bytes(a) + ((size_t)a.segments + (size_t)hatq::attend_workers(a.c.width, a.sms)) * a.columns * (a.c.width + 2) * 4;
 }
 
 }  // namespace
@@ -198,7 +199,10 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     a.ho = ho;
     a.vec_out = aligned(out, 16) && ldo % 8 == 0 && ho % 8 == 0;
     a.scale = scale * 1.44269504088896340736f;
-    a.pieces = static_cast<float *>(workspace);
+    if (bytes) {
+        a.before = static_cast<long long *>(workspace);
+        a.pieces = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + before_bytes(a));
+    }
     const cudaStream_t on = reinterpret_cast<cudaStream_t>(stream);
     const cudaError_t e = a.prompt ? hatq::launch_prompt(a, on) : hatq::launch_attend(a, type, on);
     return e == cudaSuccess ? HATQ_OK : cuda_fail(e, "attention launch");

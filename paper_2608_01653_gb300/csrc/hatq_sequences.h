@@ -143,25 +143,20 @@ struct Row {
             sg = __shfl_sync(0xffffffffu, segs, 31);
         }
     }
-    // what lies before sequence b, whose own sizes are s
-    __device__ __forceinline__ void before(const CacheArgs &c, int group, int lane, int b, long long &u, long long &sg) const {
-        const int who = b / per, from = who * per;
-        u = __shfl_sync(0xffffffffu, units, who);
-        sg = __shfl_sync(0xffffffffu, segments, who);
-        int m = __shfl_sync(0xffffffffu, most, who);
-        for (int b0 = from; b0 < b; b0 += 32) {
-            const int x = b0 + lane;
+    // units and segments before every sequence, and all units, to memory
+    __device__ __forceinline__ void write(const CacheArgs &c, int group, int lane, long long *to) const {
+        const int from = min(lane * per, c.seqs), end = min(from + per, c.seqs);
+        long long u = units, sg = segments;
+        int m = most;
+        for (int b = from; b < end; ++b) {
+            to[2 * b] = u;
+            to[2 * b + 1] = sg;
             Sequence s{};
-            if (c.starts) {
-                const int here = scan_max(max(x < b ? c.starts[x] : 0, m)), next = max(x < b ? c.starts[x + 1] : 0, here);
-                if (x < b) measure<COLS>(c, group, s, x, here, next);
-                m = __shfl_sync(0xffffffffu, next, 31);
-            } else if (x < b) {
-                measure<COLS>(c, group, s, x, x, x + 1);
-            }
-            u += __shfl_sync(0xffffffffu, scan_add(s.units(c.heads), lane, c.small), 31);
-            sg += __shfl_sync(0xffffffffu, scan_add(s.segments(c.heads), lane, c.small), 31);
+            take(c, group, s, b, m);
+            u += units_of(s, c.heads);
+            sg += s.segments(c.heads);
         }
+        if (lane == 0) to[2 * c.seqs] = total;
     }
 };
 

@@ -683,3 +683,23 @@ def test_refusals():
         with pytest.raises((ValueError, H.HatqError)):
             bad()
     finish()
+
+
+def test_attend_many_sequences():
+    """More sequences than a warp has lanes, several a lane, of all lengths down to none."""
+    lengths = [(37 * i) % 190 for i in range(700)]
+    run = Run(lengths, [1] * 700, kv=2, width=64, page=16, one_each=True)
+    q = run.random(10, 5)
+    check_attend(run, q, attend(run, q), rows=some(run, 100))
+    new = [min(n, i % 3) for i, n in enumerate(lengths)]
+    run = Run(lengths, new, kv=2, width=64, page=16)
+    q = run.random(4, 5)
+    check_attend(run, q, attend(run, q), rows=some(run, 100))
+
+
+def test_attend_parts_of_many_sequences():
+    """The same in equal parts: more segments than a CTA each would be worth, some sequences much longer."""
+    lengths = [700 if i % 50 == 3 else (7 * i) % 30 for i in range(500)]
+    run = Run(lengths, [1] * 500, kv=8, width=128, page=64, one_each=True)
+    q = run.random(16, 5)
+    check_attend(run, q, attend(run, q), rows=some(run, 60) | {3, 53, 103})
