@@ -268,6 +268,39 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) linear4_few(const Linear4A
         while (!tc::mbar_try_wait(bar + 8 * (i % stages), (uint32_t)(i / stages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
 }
 
+// Rows from, from + 8, .. of a CTA's sums and those of the other CTAs of its cluster, added up and written. All of a row's
+// (two rows') loads are on their way at once: each takes about 400 cycles.
+template <int SPLIT>
+__device__ __forceinline__ void join_rows(const Linear4Args &a, const float *sums, int pitch, int row0, int from, int to, int lane) {
+    const int n = blockIdx.x * kCtaWarps * kStrip + 4 * lane;
+#pragma unroll 2
+    for (int row = from; row < to; row += kCtaWarps) {
+        const float *own = sums + row * pitch + 4 * lane;
+        float4 u[SPLIT];
+        if constexpr (SPLIT == 1) {
+            u[0] = *reinterpret_cast<const float4 *>(own);
+        } else {
+#pragma unroll
+            for (int z = 0; z < SPLIT; ++z) {
+                uint32_t there;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(tc::smem_addr(own)), "r"(z));
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(u[z].x), "=f"(u[z].y), "=f"(u[z].z), "=f"(u[z].w) : "r"(there) : "memory");
+            }
+        }
+        float v[4] = {};
+#pragma unroll
+        for (int z = 0; z < SPLIT; ++z) {
+            v[0] += u[z].x;
+            v[1] += u[z].y;
+            v[2] += u[z].z;
+            v[3] += u[z].w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < a.n) store_y(a, row0 + row, n + i, v[i]);
+    }
+}
+
 constexpr int kManyDepth = 128;        // inputs of a piece of x
 constexpr int kManyPitch = 2 * kManyDepth + 64;
 constexpr int kManyRing = 1280;        // bytes of a warp's weights for a piece: a unit of 128, or two of 64
@@ -379,29 +412,11 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     if (*abort_flag) sound = false;
     const int each = (live + split - 1) / split, row_from = (int)blockIdx.z * each, row_to = min(row_from + each, live);
     // 4 channels a thread: a warp has a row, and its store is of whole lines
-    for (int row = row_from + warp; sound && row < row_to; row += kCtaWarps) {
-        const uint32_t at = tc::smem_addr(sums + row * PITCH + 4 * lane);
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int z = 0; z < 8; ++z)
-            if (z < split) {
-                uint32_t there = at;
-                float4 u;
-                if (split > 1) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(z));
-                if (split > 1)
-                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(u.x), "=f"(u.y), "=f"(u.z), "=f"(u.w) : "r"(there) : "memory");
-                else
-                    u = *reinterpret_cast<const float4 *>(sums + row * PITCH + 4 * lane);
-                v.x += u.x;
-                v.y += u.y;
-                v.z += u.z;
-                v.w += u.w;
-            }
-        const int n = blockIdx.x * kCtaWarps * kStrip + 4 * lane;
-        const float o[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < a.n) store_y(a, row0 + row, n + i, o[i]);
+    if (sound) {
+        if (split == 1) join_rows<1>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else if (split == 2) join_rows<2>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else if (split == 4) join_rows<4>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else join_rows<8>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
     }
     if (split > 1) asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
