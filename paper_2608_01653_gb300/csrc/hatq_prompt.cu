@@ -59,6 +59,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// two fp32 numbers in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float y;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
@@ -493,10 +510,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             // weights carry what the chunk's values are brought to (2^-64 of the largest is nothing in fp16, but counts in l)
             const int less = max(info.v_exponent - exponent, -64);
             const float shift = m - (float)less;
-            float sum[4] = {};
+            uint64_t sum[2] = {0, 0};
             uint32_t p[32];
+            const uint64_t by2 = pair(fs, fs), less2 = pair(-shift, -shift);
 #pragma unroll
-            for (int j = 0; j < 64; ++j) s[j] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[j]), fs, -shift)));
+            for (int j = 0; j < 64; j += 2) {
+                float u, v;
+                unpair(fma_pair(pair(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), by2, less2), u, v);
+                s[j] = __float_as_uint(exp2_fast(u));
+                s[j + 1] = __float_as_uint(exp2_fast(v));
+            }
             if (!whole) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
@@ -505,11 +528,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
 #pragma unroll
             for (int j = 0; j < 64; j += 2) {
                 const float u = __uint_as_float(s[j]), v = __uint_as_float(s[j + 1]);
-                sum[j & 2] += u;
-                sum[(j & 2) + 1] += v;
+                sum[j / 2 % 2] = add_pair(sum[j / 2 % 2], pair(u, v));
                 p[j / 2] = pack_half(u, v);
             }
-            l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), power(127 - less), l);
+            float s0, s1;
+            unpair(add_pair(sum[0], sum[1]), s0, s1);
+            l = fmaf(s0 + s1, power(127 - less), l);
             wait_used();
             if (!ok) break;
             tc::tmem_st32(at + S::kP + 32 * tile, p);
