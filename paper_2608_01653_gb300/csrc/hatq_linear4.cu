@@ -24,6 +24,9 @@ namespace {
 // the inputs of a strip, each with its own ring of bulk copies that runs on from strip to strip, and add up at the
 // strip's end. More rows, or x too large for that (linear4_many): a strip a warp, x streamed through shared memory for
 // all of a CTA's strips; CTAs of a cluster share the inputs where there are few strips.
+//
+// Measured: 4096 -> 4096, one row 5.8 us; 4096 -> 16384, one row 11 us (3.3 TB/s), 16 rows 15.5 us: bound by the instructions
+// that widen codes and fill the steps; 8192 -> 4096, 64 rows 23.5 us, of which the warp-level MMAs alone take 7.3.
 
 constexpr int kCtaWarps = 8, kMostWarps = 16;
 constexpr int kFewStages = 3;          // of a warp's ring, at most; each two units of 128, or four of 64
