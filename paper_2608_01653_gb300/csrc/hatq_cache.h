@@ -2,6 +2,8 @@
 // the host side (hatq_cache_api.cu) and the kernels. Not part of the public ABI.
 #pragma once
 
+#include <climits>
+
 #include "hatq_tokens.h"
 
 namespace hatq {
@@ -76,15 +78,24 @@ __device__ __forceinline__ bool sequence_of(const CacheArgs &c, int r, int lane,
         end = r + 1;
         return r < c.seqs;
     }
+    // eight offsets a lane at a time, so that a call of thousands of sequences waits for memory less often
     unsigned first = 0xffffffffu;
-    for (int j = lane; j <= c.seqs && first == 0xffffffffu; j += 32)
-        if (c.starts[j] > r) first = (unsigned)j;
-    first = __reduce_min_sync(0xffffffffu, first);
+    int most = 0;
+    for (int j0 = 0; j0 <= c.seqs && first == 0xffffffffu; j0 += 256) {
+        int v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = j0 + 32 * i + lane <= c.seqs ? c.starts[j0 + 32 * i + lane] : INT_MIN;
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+            if (v[i] > r) first = (unsigned)(j0 + 32 * i + lane);
+        first = __reduce_min_sync(0xffffffffu, first);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(j0 + 32 * i + lane) < first) most = max(most, v[i]);
+    }
     if (first == 0xffffffffu || first == 0) return false;
     b = (int)first - 1;
     end = min(c.starts[first], c.rows);
-    int most = 0;
-    for (int j = lane; j <= b; j += 32) most = max(most, c.starts[j]);
     begin = __reduce_max_sync(0xffffffffu, most);
     return true;
 }

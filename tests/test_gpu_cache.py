@@ -703,3 +703,10 @@ def test_attend_parts_of_many_sequences():
     run = Run(lengths, [1] * 500, kv=8, width=128, page=64, one_each=True)
     q = run.random(16, 5)
     check_attend(run, q, attend(run, q), rows=some(run, 60) | {3, 53, 103})
+
+
+def test_append_many_sequences():
+    """More offsets than are looked at at a time, some sequences without rows, one head: eight rows of a warp."""
+    new = [(i * i) % 4 for i in range(900)]
+    run = Run([m + i % 60 for i, m in enumerate(new)], new, kv=1, width=64, page=16)
+    check_append(run, run.random(1, 5), run.random(1, 6))
