@@ -670,7 +670,7 @@ typedef struct {
  *            - 1, its newest tokens in order, so that the last row is token
  *            lengths[b] - 1. NULL: one row each (rows == seqs). Offsets are clamped to
  *            [0, rows], one below an earlier one counts as the earlier one; rows that
- *            no sequence holds are neither read nor written
+ *            no sequence holds go nowhere, and no output of theirs is written
  *   seqs     at most 65536
  *
  * hatq_append_tokens writes the new tokens' keys and values, all in fp32: per row
@@ -708,6 +708,7 @@ hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, lon
  *   q, out   device, both HATQ_F16 or HATQ_BF16, [rows][q_heads][width] at pitches
  *            of rows and heads; they share no element, and out none with the cache
  *   q_heads  a multiple of the cache's heads, rows * q_heads < 2^31 - 1024
+ *   scale    of either sign or zero; scale * log2(e) is finite in fp32
  *   workspace  device scratch of the bytes that hatq_attend_workspace returns for
  *            the same sizes (starts: whether there are any), 16-byte aligned.
  *            Calls in flight at the same time need one each

@@ -40,7 +40,8 @@ class AttentionBlock:
 
     def forward(self, x, cache, table, lengths, starts=None, turn=None):
         """x [rows][C], the newest tokens of every sequence (table, lengths, starts as hatq.append_tokens takes them; they
-        go into the cache). turn(q, k), if given, returns both with their positions. Returns [rows][C] in x's type."""
+        go into the cache). turn(q, k), if given, returns both with their positions. Returns [rows][C] in x's type; what it
+        holds for rows of no sequence (padding behind the last) means nothing."""
         rows, h, kv, d = x.shape[0], self.heads, self.kv_heads, self.width
         c, s = hatq.quantize_tokens(x, hb=self.hb, codes="f16")
         y = hatq.linear4(c, self.qkv, scales=s, dtype=x.dtype).view(rows, h + 2 * kv, d)

@@ -177,7 +177,8 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     hatq::AttendArgs a{};
     hatq_status st = attend_args(cache, type, q_heads, rows, table_width, seqs, starts != nullptr, a);
     if (st != HATQ_OK) return st;
-    if (!std::isfinite(scale)) return fail(HATQ_ERR_INVALID_ARG, "the scale is not finite");
+    a.scale = scale * 1.44269504088896340736f;
+    if (!std::isfinite(a.scale)) return fail(HATQ_ERR_INVALID_ARG, "the scale, or scale * log2(e), is not finite");
     if (rows == 0 || seqs == 0) return HATQ_OK;
     if ((st = check_sequences(table, ldt, lengths, starts, a.c)) != HATQ_OK) return st;
     const Heads in{q, rows, ldq, q_heads, hq, cache->width, 2}, to{out, rows, ldo, q_heads, ho, cache->width, 2};
@@ -198,7 +199,6 @@ hatq_status hatq_attend_tokens(const void *q, int type, long long ldq, long long
     a.ldo = ldo;
     a.ho = ho;
     a.vec_out = aligned(out, 16) && ldo % 8 == 0 && ho % 8 == 0;
-    a.scale = scale * 1.44269504088896340736f;
     if (bytes) {
         a.before = static_cast<long long *>(workspace);
         a.pieces = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + before_bytes(a));

@@ -79,6 +79,11 @@ def test_attend_refuses(lib, kw, status):
     assert attend(lib, **kw) == status and H.last_error()
 
 
+@pytest.mark.parametrize("scale", [2.5e38, -3.4e38])                    # times log2(e): above the largest fp32
+def test_attend_refuses_scales_that_overflow(lib, scale):
+    assert attend(lib, scale=scale) == H.ERR_INVALID_ARG and b"finite" in H.last_error().encode()
+
+
 def test_no_rows_is_no_work(lib):
     none = dict(rows=0, seqs=0, table=None, lengths=None, starts=None)
     assert append(lib, k=None, v=None, kept_k=None, kept_v=None, **none) == H.OK
