@@ -28,7 +28,7 @@ namespace {
 // Measured: 4096 -> 4096, one row 5.8 us; 4096 -> 16384, one row 11 us (3.3 TB/s), 16 rows 15.5 us: bound by the instructions
 // that widen codes and fill the steps; 8192 -> 4096, 64 rows 23.5 us, of which the warp-level MMAs alone take 7.3.
 
-constexpr int kCtaWarps = 8, kMostWarps = 16;
+constexpr int kCtaStrips = 8, kMostWarps = 16;
 constexpr int kFewStages = 3;          // of a warp's ring, at most; each two units of 128, or four of 64
 
 template <typename T> constexpr int kParts = std::is_same<T, float>::value ? 3 : 1;
@@ -110,54 +110,70 @@ __device__ __forceinline__ void store_y(const Linear4Args &a, int row, int n, fl
     else static_cast<__nv_bfloat16 *>(a.y)[at] = from_f32<__nv_bfloat16>(v);
 }
 
-// A unit's products with NT tiles of 8 rows, added to the totals: BLOCKS x 64 inputs, SCALES scales a channel. x: lane
+// A unit's products with NT tiles of 8 rows, added to the totals: BLOCKS x 64 inputs, SCALES scales a channel, of STRIPS
+// strips (strip_pitch bytes on) that share what is read of x. x: lane
 // (g, t)'s row of the first tile at the unit's first input (8 t on); `next` bytes on the row of the next tile, part_pitch
 // on the next part. (Columns of rows that are none may hold anything.) Two sums at a time where tiles are few: steps
 // that add to one wait for each other.
-template <typename T, int NT, int BLOCKS, int SCALES>
-__device__ __forceinline__ void unit_products(const uint8_t *unit, const uint8_t *x, int next, int part_pitch, int lane, float (&total)[NT][4]) {
+template <typename T, int NT, int BLOCKS, int SCALES, int STRIPS>
+__device__ __forceinline__ void unit_products(const uint8_t *unit, int strip_pitch, const uint8_t *x, int next, int part_pitch, int lane,
+                                              float (&total)[STRIPS][NT][4]) {
     constexpr bool kHalf = std::is_same<T, __half>::value;
     constexpr int SUMS = SCALES == 2 || NT <= 2 ? 2 : 1;
-    uint4 w[BLOCKS];
+    uint4 w[STRIPS][BLOCKS];
+    float s[STRIPS][SCALES][2], sum[SUMS][STRIPS][NT][4];
 #pragma unroll
-    for (int i = 0; i < BLOCKS; ++i) w[i] = *reinterpret_cast<const uint4 *>(unit + 512 * i + 16 * lane);
-    const float *scales = reinterpret_cast<const float *>(unit + 512 * BLOCKS) + (lane >> 2);
-    float s[SCALES][2], sum[SUMS][NT][4];
+    for (int z = 0; z < STRIPS; ++z) {
+        const uint8_t *of = unit + z * strip_pitch;
 #pragma unroll
-    for (int i = 0; i < SCALES; ++i) {
-        s[i][0] = scales[kStrip * i];
-        s[i][1] = scales[kStrip * i + 8];
+        for (int i = 0; i < BLOCKS; ++i) w[z][i] = *reinterpret_cast<const uint4 *>(of + 512 * i + 16 * lane);
+        const float *scales = reinterpret_cast<const float *>(of + 512 * BLOCKS) + (lane >> 2);
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            s[z][i][0] = scales[kStrip * i];
+            s[z][i][1] = scales[kStrip * i + 8];
+        }
     }
 #pragma unroll
     for (int h = 0; h < 2 * BLOCKS; ++h) {                   // 32 inputs
         const int of = SUMS == 1 ? 0 : BLOCKS == 2 ? h >> 1 : h;
         const bool first = SUMS == 1 || BLOCKS == 1 ? h == 0 || SUMS == 2 : (h & 1) == 0;
-        uint32_t A[2][4];
-        widen<T>(h & 1 ? w[h >> 1].z : w[h >> 1].x, A[0]);
-        widen<T>(h & 1 ? w[h >> 1].w : w[h >> 1].y, A[1]);
+        uint32_t A[STRIPS][2][4];
+#pragma unroll
+        for (int z = 0; z < STRIPS; ++z) {
+            widen<T>(h & 1 ? w[z][h >> 1].z : w[z][h >> 1].x, A[z][0]);
+            widen<T>(h & 1 ? w[z][h >> 1].w : w[z][h >> 1].y, A[z][1]);
+        }
 #pragma unroll
         for (int part = kParts<T> - 1; part >= 0; --part) {
             uint4 b[NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4 *>(x + nt * next + part * part_pitch + 64 * h);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (first && part == kParts<T> - 1) mma_first<kHalf>(sum[of][nt], A[0], b[nt].x, b[nt].y);
-                else mma_more<kHalf>(sum[of][nt], A[0], b[nt].x, b[nt].y);
-            }
+            for (int z = 0; z < STRIPS; ++z)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_more<kHalf>(sum[of][nt], A[1], b[nt].z, b[nt].w);
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (first && part == kParts<T> - 1) mma_first<kHalf>(sum[of][z][nt], A[z][0], b[nt].x, b[nt].y);
+                    else mma_more<kHalf>(sum[of][z][nt], A[z][0], b[nt].x, b[nt].y);
+                }
+#pragma unroll
+            for (int z = 0; z < STRIPS; ++z)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_more<kHalf>(sum[of][z][nt], A[z][1], b[nt].z, b[nt].w);
         }
     }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int z = 0; z < STRIPS; ++z)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (SCALES == 2)
-                total[nt][i] = fmaf(s[SCALES - 1][i >> 1], sum[SUMS - 1][nt][i], fmaf(s[0][i >> 1], sum[0][nt][i], total[nt][i]));
-            else
-                total[nt][i] = fmaf(s[0][i >> 1], SUMS == 2 ? sum[0][nt][i] + sum[SUMS - 1][nt][i] : sum[0][nt][i], total[nt][i]);
-        }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float &to = total[z][nt][i];
+                if constexpr (SCALES == 2)
+                    to = fmaf(s[z][SCALES - 1][i >> 1], sum[SUMS - 1][z][nt][i], fmaf(s[z][0][i >> 1], sum[0][z][nt][i], to));
+                else
+                    to = fmaf(s[z][0][i >> 1], SUMS == 2 ? sum[0][z][nt][i] + sum[SUMS - 1][z][nt][i] : sum[0][z][nt][i], to);
+            }
 }
 
 // `ways` warps of the CTA share a strip's units; a CTA takes every gridDim.x-th set of strips.
@@ -230,14 +246,14 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) linear4_few(const Linear4A
     const uint8_t *x = xs + row * row_pitch + 16 * t;
     for (int round = 0; round < rounds && sound; ++round) {
         const int strip_set = (round * (int)gridDim.x + (int)blockIdx.x) * sets;
-        float total[NT][4] = {};
+        float total[1][NT][4] = {};
         if (strip_set + set < a.strips)
             for (int c = 0; c < per; ++c) {
                 const int first = from + c * STAGE_UNITS, n = min(STAGE_UNITS, to - first);
                 sound = __all_sync(0xffffffffu, tc::mbar_wait(bar + 8 * stage, parity, abort_flag, a.err));
                 if (!sound) break;
                 for (int i = 0; i < n; ++i)
-                    unit_products<T, NT, BLOCKS, SCALES>(ring + stage * STAGE + i * UNIT, x + (first + i) * (BLOCKS * 2 * kStep), next, part_pitch,
+                    unit_products<T, NT, BLOCKS, SCALES, 1>(ring + stage * STAGE + i * UNIT, 0, x + (first + i) * (BLOCKS * 2 * kStep), next, part_pitch,
                                                          lane, total);
                 __syncwarp();
                 ++done;
@@ -253,7 +269,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) linear4_few(const Linear4A
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(8 * nt + 2 * t + (i & 1)) * PITCH + g + (i >> 1) * 8] = total[nt][i];
+            for (int i = 0; i < 4; ++i) mine[(8 * nt + 2 * t + (i & 1)) * PITCH + g + (i >> 1) * 8] = total[0][nt][i];
         sound = !__syncthreads_or(!sound);
         for (int i = threadIdx.x; sound && i < a.rows * kStrip * sets; i += blockDim.x) {
             const int ch = i % kStrip, r = i / kStrip % a.rows, of = i / (kStrip * a.rows), n = (strip_set + of) * kStrip + ch;
@@ -271,13 +287,13 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) linear4_few(const Linear4A
         while (!tc::mbar_try_wait(bar + 8 * (i % stages), (uint32_t)(i / stages) & 1u) && clock64() - t0 < tc::kWaitLimitCycles) {}
 }
 
-// Rows from, from + 8, .. of a CTA's sums and those of the other CTAs of its cluster, added up and written. All of a row's
+// Rows from, from + WARPS, .. of a CTA's sums and those of the other CTAs of its cluster, added up and written. All of a row's
 // (two rows') loads are on their way at once: each takes about 400 cycles.
-template <int SPLIT>
+template <int WARPS, int SPLIT>
 __device__ __forceinline__ void join_rows(const Linear4Args &a, const float *sums, int pitch, int row0, int from, int to, int lane) {
-    const int n = blockIdx.x * kCtaWarps * kStrip + 4 * lane;
+    const int n = blockIdx.x * kCtaStrips * kStrip + 4 * lane;
 #pragma unroll 2
-    for (int row = from; row < to; row += kCtaWarps) {
+    for (int row = from; row < to; row += WARPS) {
         const float *own = sums + row * pitch + 4 * lane;
         float4 u[SPLIT];
         if constexpr (SPLIT == 1) {
@@ -310,17 +326,24 @@ constexpr int kManyRing = 1280;        // bytes of a warp's weights for a piece:
 constexpr int kManyStages = 4;
 template <typename T> constexpr int kXStages = std::is_same<T, float>::value ? 2 : 3;
 
-// A warp per strip, 8 strips a CTA, NT tiles of 8 rows; the CTAs of a cluster (along z) have a part of the inputs each.
+// Strips a warp: what is read of x is read once for all of them, in return a CTA has fewer warps. Two for eight tiles of
+// 16-bit x (64 rows of 8192 -> 4096: 21.6 us against 23.8); with four tiles (32 rows: 16.9 against 15.1) or fp32 x (64 rows:
+// 125 against 109), where registers hold the warps of an SM down, one.
+template <typename T, int NT, int SCALES> constexpr int kManyStrips = sizeof(T) == 2 && NT == 8 && SCALES == 1 ? 2 : 1;
+
+// 8 strips a CTA, kManyStrips of them a warp, NT tiles of 8 rows; the CTAs of a cluster (along z) have a part of the
+// inputs each.
 template <typename T, int NT, int BLOCKS, int SCALES>
-__global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4Args a, int split) {
+__global__ void __launch_bounds__(kCtaStrips / kManyStrips<T, NT, SCALES> * 32, 2) linear4_many(const Linear4Args a, int split) {
+    constexpr int STRIPS = kManyStrips<T, NT, SCALES>, WARPS = kCtaStrips / STRIPS, RING = STRIPS * kManyRing;
     constexpr int ROWS = 8 * NT, PARTS = kParts<T>, XS = kXStages<T>, PART = ROWS * kManyPitch, XSTAGE = PARTS * PART;
-    constexpr int PITCH = kCtaWarps * kStrip + 4, UNIT = 512 * BLOCKS + 4 * kStrip * SCALES, PIECE_UNITS = 2 / BLOCKS;
+    constexpr int PITCH = kCtaStrips * kStrip + 4, UNIT = 512 * BLOCKS + 4 * kStrip * SCALES, PIECE_UNITS = 2 / BLOCKS;
     extern __shared__ __align__(128) uint8_t smem[];         // rings, x; in the end the CTA's sums
-    __shared__ __align__(8) uint64_t bars[kCtaWarps][kManyStages];
+    __shared__ __align__(8) uint64_t bars[WARPS][kManyStages];
     __shared__ int s_abort;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint8_t *ring = smem + warp * kManyStages * kManyRing;
-    uint8_t *xs = smem + kCtaWarps * kManyStages * kManyRing;
+    const uint8_t *ring = smem + warp * kManyStages * RING;
+    uint8_t *xs = smem + kCtaStrips * kManyStages * kManyRing;
     const uint32_t bar = tc::smem_addr(bars[warp]);
     volatile int *abort_flag = &s_abort;
     if (lane < kManyStages) tc::mbar_init(bar + 8 * lane, 1);
@@ -330,18 +353,21 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     after_prior_kernels();
     bool sound = !__syncthreads_or(*reinterpret_cast<volatile int *>(a.err) != 0);
 
-    const int strip = min((int)blockIdx.x * kCtaWarps + warp, a.strips - 1), row0 = blockIdx.y * ROWS, live = min(ROWS, a.rows - row0);
+    const int strip = (int)blockIdx.x * kCtaStrips + warp * STRIPS, row0 = blockIdx.y * ROWS, live = min(ROWS, a.rows - row0);
     const int pieces = (a.k + kManyDepth - 1) / kManyDepth, from = pieces * (int)blockIdx.z / split, to = pieces * ((int)blockIdx.z + 1) / split;
     auto ask = [&](int i) {
         if (i >= to - from || lane) return;
         const int first = (from + i) * PIECE_UNITS, n = min(PIECE_UNITS, a.units - first), stage = i % kManyStages;
-        tc::mbar_expect_tx(bar + 8 * stage, n * UNIT);
-        bulk_load(tc::smem_addr(ring + stage * kManyRing), a.w + ((long long)strip * a.units + first) * UNIT, n * UNIT,
-                  bar + 8 * stage);
+        tc::mbar_expect_tx(bar + 8 * stage, STRIPS * n * UNIT);
+#pragma unroll
+        for (int z = 0; z < STRIPS; ++z)
+            bulk_load(tc::smem_addr(ring + stage * RING + z * kManyRing), a.w + ((long long)min(strip + z, a.strips - 1) * a.units + first) * UNIT,
+                      n * UNIT, bar + 8 * stage);
     };
     // Pieces of x, zeros behind the last row and input. As they lie, by asynchronous copies; otherwise through registers.
     const bool direct = a.vec && PARTS == 1;
-    // A thread has the same 8 inputs of every 16th row.
+    // A thread has the same 8 inputs of every APARTth row.
+    constexpr int APART = WARPS * 2;
     const int x_row = threadIdx.x >> 4, x_k = (threadIdx.x & 15) * 8;
     const T *x_first = static_cast<const T *>(a.x) + (long long)row0 * a.ldx, *x_mine = x_first + (long long)min(x_row, live - 1) * a.ldx + x_k;
     uint8_t *x_to = xs + x_row * kManyPitch + 2 * x_k;
@@ -354,18 +380,18 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
                 const uint32_t dst = tc::smem_addr(to_x);
                 const T *p = x_mine + k0;
 #pragma unroll
-                for (int j = 0; j < ROWS / 16; ++j) {
-                    const int bytes = x_row + 16 * j < live ? there : 0;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst + 16 * j * kManyPitch),
-                                 "l"(bytes ? p + j * 16 * a.ldx : x_first), "r"(bytes)
+                for (int j = 0; j < ROWS / APART; ++j) {
+                    const int bytes = x_row + APART * j < live ? there : 0;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst + APART * j * kManyPitch),
+                                 "l"(bytes ? p + j * APART * a.ldx : x_first), "r"(bytes)
                                  : "memory");
                 }
             } else {
-                for (int j = 0; j < ROWS / 16; ++j) {
+                for (int j = 0; j < ROWS / APART; ++j) {
                     uint4 v[PARTS];
-                    load8<T>(a, x_first + (long long)min(x_row + 16 * j, live - 1) * a.ldx, x_row + 16 * j < live, k0 + x_k, v);
+                    load8<T>(a, x_first + (long long)min(x_row + APART * j, live - 1) * a.ldx, x_row + APART * j < live, k0 + x_k, v);
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<uint4 *>(to_x + 16 * j * kManyPitch + part * PART) = v[part];
+                    for (int part = 0; part < PARTS; ++part) *reinterpret_cast<uint4 *>(to_x + APART * j * kManyPitch + part * PART) = v[part];
                 }
             }
         }
@@ -376,7 +402,7 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
 #pragma unroll
         for (int i = 0; i < XS - 1; ++i) bring(i, i);
     }
-    float total[NT][4] = {};
+    float total[STRIPS][NT][4] = {};
     int done = 0, x_stage = 0;
     for (; sound && done < to - from; ++done) {
         const int stage = done % kManyStages, n = min(PIECE_UNITS, a.units - (from + done) * PIECE_UNITS);
@@ -387,7 +413,8 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
         bring(done + XS - 1, x_stage == 0 ? XS - 1 : x_stage - 1);
         const uint8_t *x = xs + x_stage * XSTAGE + g * kManyPitch + 16 * t;
         for (int i = 0; i < n; ++i)
-            unit_products<T, NT, BLOCKS, SCALES>(ring + stage * kManyRing + i * UNIT, x + i * (BLOCKS * 2 * kStep), 8 * kManyPitch, PART, lane, total);
+            unit_products<T, NT, BLOCKS, SCALES, STRIPS>(ring + stage * RING + i * UNIT, kManyRing, x + i * (BLOCKS * 2 * kStep), 8 * kManyPitch, PART,
+                                                         lane, total);
         __syncwarp();
         ask(done + kManyStages);
         if (++x_stage == XS) x_stage = 0;
@@ -403,10 +430,12 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     // ---- the CTA's sums, added up over the cluster, a share of the rows each
     float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int z = 0; z < STRIPS; ++z)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sums[(8 * nt + 2 * t + (i & 1)) * PITCH + kStrip * warp + g + (i >> 1) * 8] = total[nt][i];
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sums[(8 * nt + 2 * t + (i & 1)) * PITCH + kStrip * (warp * STRIPS + z) + g + (i >> 1) * 8] = total[z][nt][i];
     if (split > 1) {
         asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
     } else {
@@ -416,10 +445,10 @@ __global__ void __launch_bounds__(kCtaWarps * 32, 2) linear4_many(const Linear4A
     const int each = (live + split - 1) / split, row_from = (int)blockIdx.z * each, row_to = min(row_from + each, live);
     // 4 channels a thread: a warp has a row, and its store is of whole lines
     if (sound) {
-        if (split == 1) join_rows<1>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
-        else if (split == 2) join_rows<2>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
-        else if (split == 4) join_rows<4>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
-        else join_rows<8>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        if (split == 1) join_rows<WARPS, 1>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else if (split == 2) join_rows<WARPS, 2>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else if (split == 4) join_rows<WARPS, 4>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
+        else join_rows<WARPS, 8>(a, sums, PITCH, row0, row_from + warp, row_to, lane);
     }
     if (split > 1) asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -465,12 +494,12 @@ cudaError_t launch_few(const Linear4Args &a, const FewPlan &p, cudaStream_t s) {
 template <typename T, int NT, int BLOCKS, int SCALES>
 cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     static std::atomic<int> allowed[64];
-    constexpr int x_bytes = kXStages<T> * kParts<T> * 8 * NT * kManyPitch, sum_bytes = 8 * NT * (kCtaWarps * kStrip + 4) * 4;
-    constexpr int ring = kCtaWarps * kManyStages * kManyRing, bytes = ring + x_bytes > sum_bytes ? ring + x_bytes : sum_bytes;
+    constexpr int x_bytes = kXStages<T> * kParts<T> * 8 * NT * kManyPitch, sum_bytes = 8 * NT * (kCtaStrips * kStrip + 4) * 4;
+    constexpr int ring = kCtaStrips * kManyStages * kManyRing, bytes = ring + x_bytes > sum_bytes ? ring + x_bytes : sum_bytes;
     static_assert(bytes <= 226 * 1024, "shared memory of a CTA");
     const cudaError_t e = allow_shared(reinterpret_cast<const void *>(linear4_many<T, NT, BLOCKS, SCALES>), bytes, allowed);
     if (e != cudaSuccess) return e;
-    const int tiles = (a.strips + kCtaWarps - 1) / kCtaWarps, row_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
+    const int tiles = (a.strips + kCtaStrips - 1) / kCtaStrips, row_tiles = (a.rows + 8 * NT - 1) / (8 * NT);
     const int pieces = (a.k + kManyDepth - 1) / kManyDepth;
     // the split of the inputs that takes the fewest steps: waves x pieces, and about three for joining
     int split = 1;
@@ -488,7 +517,7 @@ cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     attr[1].val.clusterDim.z = (unsigned)split;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)tiles, (unsigned)row_tiles, (unsigned)split);
-    cfg.blockDim = dim3(kCtaWarps * 32);
+    cfg.blockDim = dim3(kCtaStrips / kManyStrips<T, NT, SCALES> * 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cfg.attrs = attr;
