@@ -764,7 +764,7 @@ hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *sca
  *            hatq_quantize_tokens (F16 format, same hb as the weights) among them
  *   s_x      device float [rows], or NULL: 1
  *   y        device, hatq_type y_type, pitch ldy >= n; shares no element with x
- *   rows     at most 2^20; the weights are read once for every 64 rows or fewer.
+ *   rows     at most 2^20; the weights are read once for every 64 rows (fp32 x: 32) or fewer.
  *            Made for few rows: hatq_linear is the faster from about 100 on
  * Stream-ordered; an expired device wait surfaces through hatq_sync_status(). */
 hatq_status hatq_linear4(const void *x, int x_type, long long ldx, const float *s_x, long long rows,

@@ -26,7 +26,7 @@ namespace {
 // all of a CTA's strips; CTAs of a cluster share the inputs where there are few strips.
 //
 // Measured: 4096 -> 4096, one row 5.8 us; 4096 -> 16384, one row 11 us (3.3 TB/s), 16 rows 15.5 us: bound by the instructions
-// that widen codes and fill the steps; 8192 -> 4096, 64 rows 23.5 us, of which the warp-level MMAs alone take 7.3.
+// that widen codes and fill the steps; 8192 -> 4096, 64 rows 21.4 us, of which the warp-level MMAs alone take 7.3.
 
 constexpr int kCtaStrips = 8, kMostWarps = 16;
 constexpr int kFewStages = 3;          // of a warp's ring, at most; each two units of 128, or four of 64
@@ -326,16 +326,16 @@ constexpr int kManyRing = 1280;        // bytes of a warp's weights for a piece:
 constexpr int kManyStages = 4;
 template <typename T> constexpr int kXStages = std::is_same<T, float>::value ? 2 : 3;
 
-// Strips a warp: what is read of x is read once for all of them, in return a CTA has fewer warps. Two for eight tiles of
-// 16-bit x (64 rows of 8192 -> 4096: 21.6 us against 23.8); with four tiles (32 rows: 16.9 against 15.1) or fp32 x (64 rows:
-// 125 against 109), where registers hold the warps of an SM down, one.
-template <typename T, int NT, int SCALES> constexpr int kManyStrips = sizeof(T) == 2 && NT == 8 && SCALES == 1 ? 2 : 1;
+// Strips a warp: what is read of x is read once for all of them, in return a CTA has fewer warps. Two with eight tiles of
+// rows (64 rows of 8192 -> 4096: 21.4 us against 23.6), one with four (32 rows: 15.1 against 16.9) and where registers
+// hold two scales a unit.
+template <int NT, int SCALES> constexpr int kManyStrips = NT == 8 && SCALES == 1 ? 2 : 1;
 
 // 8 strips a CTA, kManyStrips of them a warp, NT tiles of 8 rows; the CTAs of a cluster (along z) have a part of the
 // inputs each.
 template <typename T, int NT, int BLOCKS, int SCALES>
-__global__ void __launch_bounds__(kCtaStrips / kManyStrips<T, NT, SCALES> * 32, 2) linear4_many(const Linear4Args a, int split) {
-    constexpr int STRIPS = kManyStrips<T, NT, SCALES>, WARPS = kCtaStrips / STRIPS, RING = STRIPS * kManyRing;
+__global__ void __launch_bounds__(kCtaStrips / kManyStrips<NT, SCALES> * 32, 2) linear4_many(const Linear4Args a, int split) {
+    constexpr int STRIPS = kManyStrips<NT, SCALES>, WARPS = kCtaStrips / STRIPS, RING = STRIPS * kManyRing;
     constexpr int ROWS = 8 * NT, PARTS = kParts<T>, XS = kXStages<T>, PART = ROWS * kManyPitch, XSTAGE = PARTS * PART;
     constexpr int PITCH = kCtaStrips * kStrip + 4, UNIT = 512 * BLOCKS + 4 * kStrip * SCALES, PIECE_UNITS = 2 / BLOCKS;
     extern __shared__ __align__(128) uint8_t smem[];         // rings, x; in the end the CTA's sums
@@ -517,7 +517,7 @@ cudaError_t launch_many(const Linear4Args &a, int sms, cudaStream_t s) {
     attr[1].val.clusterDim.z = (unsigned)split;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)tiles, (unsigned)row_tiles, (unsigned)split);
-    cfg.blockDim = dim3(kCtaStrips / kManyStrips<T, NT, SCALES> * 32);
+    cfg.blockDim = dim3(kCtaStrips / kManyStrips<NT, SCALES> * 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cfg.attrs = attr;
@@ -530,9 +530,12 @@ cudaError_t launch_units(const Linear4Args &a, int sms, cudaStream_t s) {
     FewPlan p;
     if (a.rows <= 16 && plan_few(a, x_bytes, a.rows <= 8 ? 1 : 2, sms, p))
         return a.rows <= 8 ? launch_few<T, 1, BLOCKS, SCALES>(a, p, s) : launch_few<T, 2, BLOCKS, SCALES>(a, p, s);
-    return a.rows <= 16   ? launch_many<T, 2, BLOCKS, SCALES>(a, sms, s)
-           : a.rows <= 32 ? launch_many<T, 4, BLOCKS, SCALES>(a, sms, s)
-                          : launch_many<T, 8, BLOCKS, SCALES>(a, sms, s);
+    // At most 64 rows a CTA, or 32 of fp32 x: their three parts of more leave an SM one CTA (64 rows of 8192 -> 4096: 54 us
+    // against 109)
+    if (a.rows <= 16) return launch_many<T, 2, BLOCKS, SCALES>(a, sms, s);
+    if constexpr (kParts<T> == 1)
+        if (a.rows > 32) return launch_many<T, 8, BLOCKS, SCALES>(a, sms, s);
+    return launch_many<T, 4, BLOCKS, SCALES>(a, sms, s);
 }
 template <typename T>
 cudaError_t launch_type(const Linear4Args &a, int sms, cudaStream_t s) {
