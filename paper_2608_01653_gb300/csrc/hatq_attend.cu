@@ -27,11 +27,16 @@ using tc::smem_addr;
 // sum_d q_d as the accumulators' first value, 8 * 2^-24 sum_j p_j by one step with constant A. The scales of keys
 // multiply s, those of values p: no code is ever multiplied by a scale.
 //
-// Rounded to fewer than 32 bits: q and p v, to fp16, both brought into its range by powers of two (q per column, p v
-// by the largest v so far). For fp16 queries, whose outputs would show it, both go through in two parts, high and low,
+// Rounded to fewer than 32 bits: q and p v, to fp16. q is brought into its range by a power of two per column, p v by the
+// choice of m_c, so that what it keeps is relative to the largest term of the column's own sum: a token that the column does
+// not see has no part in that, whatever its scale, nor has one whose codes are all 0 (append gives rows of zeros a scale like
+// any other). For fp16 queries, whose outputs would show it, both go through in two parts, high and low,
 // and codes are widened whole: the tensor cores align a subnormal's product as if it were a normal one's, and what they
 // then drop left sums off by up to 2^-14 of their terms.
-// m_c is raised only when some s_j exceeds it by 8: p stays below 2^8, sums are in fp32.
+// m_c is raised only where some p v would exceed 2^15, to where it is just below 2^8 (what is dropped of subnormal products
+// goes by the power of two of p v, so that it is least there). Sums are in fp32, and so is that of p, which
+// may be large or small as the scales are: p stays below 2^103, so that scales of 2^-109 and more have all their bits, and
+// those up to 2^110 leave room for weights of 2^-23 of the heaviest.
 //
 // Memory-bound for few queries. A warp works by itself: its own ring of chunks (64 keys of one head, brought in by one
 // bulk copy per page), its own maxima and sums; no barrier between warps. The chunks of all sequences and heads are
@@ -96,6 +101,21 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ float low_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x & 0xffff))); }
 __device__ __forceinline__ float high_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x >> 16))); }
+
+// A scale's logarithm. Those below 2^-88 count as that, so that weights stay below 2^103; an infinity has one of no NaN.
+__device__ __forceinline__ float log2_of(float v) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fminf(fmaxf(v, 0x1p-88f), 0x1p127f)));
+    return y;
+}
+
+// Sums of weights below a maximum that is raised: by 2^less, which may be below what fp32 holds when the sum itself is not.
+// Returns 2^less (or 0), for sums of products.
+__device__ __forceinline__ float lowered(float &l, float less) {
+    const float half = exp2_fast(0.5f * less);
+    l = l * half * half;
+    return half * half;
+}
 
 // Equal parts for the warps: of `active` ones in every CTA, as few as give every CTA a unit.
 struct Parts {
@@ -426,7 +446,6 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
     uint32_t qf[NT][PARTS][STEPS][2];
     float q_off[NT][2], q_f[NT][2];
     int lim[NT][2];
-    float rinv = 0x1p100f;
     bool sound = true;
     const int units = (int)(to - from);
     const int near = (g & 1) ? 7 - (g >> 1) : g >> 1;        // the key of the tile that row g of A is; row g + 8: + 8
@@ -492,14 +511,13 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
                 for (int y = 0; y < 4; ++y) off[nt][y] = 0.0f;
             }
-            rinv = 0x1p100f;
         }
 
         // ---- S^T of the chunk's 64 keys (what lies behind the last one is computed from whatever is there, and masked)
         const uint8_t *base = mine + stage * STAGE;
         const int key0 = k.chunk * kChunk;
         const bool whole = key0 + kChunk <= k.len - k.m + k.tile * COLS / a.group + 1 && k.pages == (1 << pages_of_chunk) - 1;
-        float s[NT][4][4], vs[4][2], ks[4][2], most[NT][2], largest = 0.0f;
+        float s[NT][4][4], vs[4][2], ks[4][2], most[NT][2];
         const uint8_t *rec[4];
         int token[4];
 #pragma unroll
@@ -573,35 +591,53 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most[nt][y] = fmaxf(most[nt][y], fmaxf(s[nt][j][y], s[nt][j][2 + y]));
             }
+
+        // how far a logit of these keys may exceed m
+        float largest = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) largest = fmaxf(largest, fmaxf(vs[j][0], vs[j][1]));
-
-        // ---- raise the maxima where a weight would leave the range
-        bool raise = largest * rinv > 128.0f;
+        const float room = 15.0f - log2_of(largest);
+        // ---- raise the maxima where a weight, or its product with a scale, may leave the range
+        bool high = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) raise |= most[nt][0] > m[nt][0] + 8.0f || most[nt][1] > m[nt][1] + 8.0f;
-        if (__any_sync(0xffffffffu, raise)) {
-            float ratio = 1.0f;
-            largest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));
-            if (largest * rinv > 128.0f) {
-                const int ex = (int)(__float_as_uint(largest) >> 23);
-                const float now = __uint_as_float((uint32_t)min(max(260 - ex, 1), 247) << 23);      // largest * now in [2^6, 2^7)
-                ratio = now / rinv;
-                rinv = now;
+        for (int nt = 0; nt < NT; ++nt) high |= most[nt][0] > m[nt][0] + room || most[nt][1] > m[nt][1] + room;
+        if (__any_sync(0xffffffffu, high)) {
+            // Tokens whose codes are all 0: nothing of them, whatever their scale. Two a lane. (Every warp comes here once, and
+            // code that runs once is waited for: loops, not unrolled.)
+            unsigned none[2] = {0, 0};
+#pragma unroll 1
+            for (int i = 0; i < kChunk; i += 32) {
+                const int at = i + lane;
+                const uint4 *row = reinterpret_cast<const uint4 *>(base + (at >> c.page_bits) * record + (size + (at & (size - 1))) * (D / 2));
+                uint32_t z = 0;
+#pragma unroll 1
+                for (int x = 0; x < D / 32; ++x) {
+                    const uint4 w = row[x];
+                    z |= (w.x ^ 0x88888888u) | (w.y ^ 0x88888888u) | (w.z ^ 0x88888888u) | (w.w ^ 0x88888888u);
+                }
+                none[0] = none[1];
+                none[1] = __ballot_sync(0xffffffffu, z == 0);
             }
+            if (none[0] | none[1])
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if ((none[j >> 1] >> (16 * (j & 1) + 8 * h + near) & 1) && vs[j][h] < INFINITY) vs[j][h] = 0.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float by[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float x = most[nt][y];
+                    float x = -1e30f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x = fmaxf(x, fmaxf(s[nt][j][y] + log2_of(vs[j][0]), s[nt][j][2 + y] + log2_of(vs[j][1])));
 #pragma unroll
                     for (int h = 4; h < 32; h *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, h));
-                    x = fmaxf(x, m[nt][y]);
-                    by[y] = exp2_fast(m[nt][y] - x);
+                    // (each column by what it sees alone)
+                    x = x > m[nt][y] + 15.0f ? x - 7.9f : m[nt][y];
+                    by[y] = lowered(l[nt][y], m[nt][y] - x);
                     m[nt][y] = x;
-                    l[nt][y] *= by[y];
-                    by[y] *= ratio;
                     off[nt][y] *= by[y];
                 }
 #pragma unroll
@@ -618,7 +654,6 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t pf[PARTS][NT][2];
-            const float v0 = vs[j][0] * rinv, v1 = vs[j][1] * rinv;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float p[4];
@@ -626,9 +661,9 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
                 for (int y = 0; y < 4; ++y) p[y] = exp2_fast(s[nt][j][y] - m[nt][y & 1]);
                 l[nt][0] += p[0] + p[2];
                 l[nt][1] += p[1] + p[3];
-                // (a weight of 0 stays 0, whatever the scale of a value that this query does not see)
+                // (nothing of a value that this query does not see, whatever its scale)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) p[y] = whole || p[y] != 0.0f ? p[y] * (y < 2 ? v0 : v1) : 0.0f;
+                for (int y = 0; y < 4; ++y) p[y] = whole || p[y] != 0.0f ? p[y] * vs[j][y >> 1] : 0.0f;
                 const uint32_t x = pack_half(p[0], p[1]), y = pack_half(p[2], p[3]);
                 pf[0][nt][0] = transposed(x);
                 pf[0][nt][1] = transposed(y);
@@ -669,7 +704,6 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         if (k.first_last & 2) {
             // ---- the warp's part of the segment is done: m, l and o of every column to its piece
             float *to_piece = joined ? reinterpret_cast<float *>(mine) : a.pieces + piece * piece_floats(D, COLS);
-            const float up = 1.0f / rinv;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -686,8 +720,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
                     for (int x = 0; x < STEPS; ++x)
                         *reinterpret_cast<float2 *>(p + 2 * x) =
-                            make_float2((o[nt][x][y] - off[nt][y]) * kUnit * up,
-                                        (o[nt][x][2 + y] * kOdd - off[nt][y]) * kUnit * up);
+                            make_float2((o[nt][x][y] - off[nt][y]) * kUnit, (o[nt][x][2 + y] * kOdd - off[nt][y]) * kUnit);
                 }
             piece = next_piece++;
         }
@@ -721,8 +754,8 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         float most = pl == 0.0f ? -1e30f : pm;
 #pragma unroll
         for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const float by = pl == 0.0f ? 0.0f : exp2_fast(pm - most);
-        float sum = pl * by, v[E];
+        float sum = pl, v[E];
+        const float by = pl == 0.0f ? 0.0f : lowered(sum, pm - most);
 #pragma unroll
         for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
 #pragma unroll
@@ -803,12 +836,12 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
             float now = fmaxf(mx, pm);
 #pragma unroll
             for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, d));
-            const float by = exp2_fast(mx - now), add = pl == 0.0f ? 0.0f : exp2_fast(pm - now);
+            const float by = lowered(l, mx - now), add = pl == 0.0f ? 0.0f : lowered(pl, pm - now);
             mx = now;
-            float sum = pl * add;
+            float sum = pl;
 #pragma unroll
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            l = l * by + sum;
+            l += sum;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] *= by;
             const int here = min(32, (n - i0 - way + ways - 1) / ways);
@@ -830,12 +863,13 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
         for (int e = 0; e < E; ++e) s_o[warp][32 * e + lane] = o[e];
         __syncthreads();
         if (way) return;
-        const float pm = lane < ways ? s_m[warp + lane] : -1e30f, pl = lane < ways ? s_l[warp + lane] : 0.0f;
+        const float pm = lane < ways ? s_m[warp + lane] : -1e30f;
+        float pl = lane < ways ? s_l[warp + lane] : 0.0f;
         mx = pl == 0.0f ? -1e30f : pm;
 #pragma unroll
         for (int d = 4; d; d /= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        const float by = pl == 0.0f ? 0.0f : exp2_fast(pm - mx);
-        l = pl * by;
+        const float by = pl == 0.0f ? 0.0f : lowered(pl, pm - mx);
+        l = pl;
 #pragma unroll
         for (int d = 4; d; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
         l = __shfl_sync(0xffffffffu, l, 0);

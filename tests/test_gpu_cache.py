@@ -710,3 +710,148 @@ def test_append_many_sequences():
     new = [(i * i) % 4 for i in range(900)]
     run = Run([m + i % 60 for i, m in enumerate(new)], new, kv=1, width=64, page=16)
     check_append(run, run.random(1, 5), run.random(1, 6))
+
+
+# ------------------------------------------------------------------ scales far from one another
+
+# A few queries per sequence; many, which bf16 queries take to the other kernel.
+FEW = dict(lengths=[200, 333], new=[3, 1], kv=2, width=64)
+MANY_COLUMNS = dict(lengths=[200, 333, 90, 64], new=[60, 40, 90, 64], kv=16, width=64)
+SHAPES = [(FEW, 4, "bf16"), (FEW, 4, "f16"), (dict(FEW, width=128), 6, "bf16"), (MANY_COLUMNS, 64, "f16")]
+
+
+def scales_of(run):
+    """Scales of the cache [pages][kv][2][page]: keys', values'."""
+    return run.cache.data[:, :, run.page * run.width:].contiguous().view(torch.float32).reshape(-1, run.kv, 2, run.page)
+
+
+def put_scales(run, scales):
+    run.cache.data[:, :, run.page * run.width:] = scales.reshape(-1, run.kv, 2 * run.page).view(torch.uint8)
+
+
+def put_codes(run, part, b, j, code):
+    """One code for all of a token's keys (part 0) or values."""
+    at = (part * run.page + j % run.page) * run.width // 2
+    run.cache.data[run.table[b, j // run.page], :, at:at + run.width // 2] = 17 * (code + 8)
+
+
+def some_rows(run):
+    return list(range(run.rows)) if run.rows < 20 else sorted(some(run, 25))
+
+
+def check_within(run, q, y, ref, sd, rows):
+    """As check_attend does, with nothing added to the bound but what the type itself cannot hold (bf16: outputs of any
+    size count). The other kernel's deviations for all."""
+    tol = 8 * MANY * sd + torch.finfo(q.dtype).eps / 2 * 1.01 * ref.abs() + (2.0 ** -24 if q.dtype == torch.float16 else 2.0 ** -130)
+    assert len(rows) and float(((y.double().cpu() - ref).abs() / tol)[rows].nan_to_num(nan=INF).max()) <= 1
+
+
+@pytest.mark.parametrize("part", ["keys", "values"])
+@pytest.mark.parametrize("size", [2.0 ** 9, 2.0 ** 13, 2.0 ** 20, 2.0 ** 33, 2.0 ** 90, INF])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_a_large_scale_that_a_row_does_not_see(shape, heads, dtype, size, part):
+    """The newest token of every sequence, which only the last row sees."""
+    run = Run(**shape, dtype=dtype)
+    q = run.random(heads, 5)
+    last = set((np.cumsum(run.new) - 1).tolist())
+    rows = [r for r in some_rows(run) if r not in last]
+    ref, sd = reference(run, q, rows=rows)
+    scales = scales_of(run)
+    for b, n in enumerate(run.len):
+        scales[run.table[b, (n - 1) // run.page], :, 0 if part == "keys" else 1, (n - 1) % run.page] *= size
+    put_scales(run, scales)
+    check_within(run, q, attend(run, q), ref, sd, rows)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 40, 2.0 ** 100])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_values_of_nothing_say_nothing(shape, heads, dtype, size):
+    """Tokens whose value codes are all 0, single ones and the whole first chunk, whatever their scale: as with a scale of 0."""
+    run = Run(**shape, dtype=dtype)
+    q = run.random(heads, 5)
+    rows = some_rows(run)
+    scales = scales_of(run)
+    for b, n in enumerate(run.len):
+        for j in {0, 40, n - 1} | set(range(64) if b == 1 else ()):
+            put_codes(run, 1, b, j, 0)
+            scales[run.table[b, j // run.page], :, 1, j % run.page] = 0
+    put_scales(run, scales)
+    ref, sd = reference(run, q, rows=rows)
+    put_scales(run, torch.where(scales == 0, size, scales))
+    check_within(run, q, attend(run, q), ref, sd, rows)
+
+
+@pytest.mark.parametrize("shape,heads", [(FEW, 4)])
+def test_attend_zeros_appended_among_small_values(shape, heads):
+    """Append gives a row of zeros a scale of 1 / sqrt(hb): the values of 1e-12 beside it stay what they are."""
+    run = Run(**shape)
+    new = dict(shape, new=shape["lengths"])                             # all tokens go in at once
+    fill = Run(**new)
+    k, v = fill.random(run.kv, 5), fill.random(run.kv, 6) * 1e-12
+    at = 0
+    for n in run.len:
+        v[at + 7], v[at + n - 1] = 0, 0
+        at += n
+    H.append_tokens(run.cache, k, v, run.table, run.lengths, fill.starts)
+    q = run.random(heads, 8)
+    rows = some_rows(run)
+    y = attend(run, q)
+    scales = scales_of(run)
+    scales[:, :, 1] = torch.where(scales[:, :, 1] == 1 / math.sqrt(run.hb), 0.0, scales[:, :, 1])
+    put_scales(run, scales)
+    ref, sd = reference(run, q, rows=rows)
+    check_within(run, q, y, ref, sd, rows)
+
+
+@pytest.mark.parametrize("part", ["keys", "values"])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_scales_of_many_sizes_that_rows_see(shape, heads, dtype, part):
+    """Value scales spread over 2^60 (fp16: up to 2^10, what its outputs hold), key scales over 2^40 down from 1."""
+    run = Run(**shape, dtype=dtype)
+    q = run.random(heads, 5)
+    scales = scales_of(run)
+    u = torch.rand(scales.shape[:2] + scales.shape[3:], generator=gen(9), device="cuda")
+    if part == "keys":
+        scales[:, :, 0] *= 2.0 ** (-40 * u)
+    else:
+        scales[:, :, 1] *= 2.0 ** (60 * u - (30 if dtype == "bf16" else 50))
+    put_scales(run, scales)
+    rows = some_rows(run)
+    ref, sd = reference(run, q, rows=rows)
+    check_within(run, q, attend(run, q), ref, sd, rows)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -105, 2.0 ** 107])
+@pytest.mark.parametrize("shape,heads,dtype", [x for x in SHAPES if x[2] == "bf16"])
+def test_attend_value_scales_at_the_ends_of_their_range(shape, heads, dtype, size):
+    run = Run(**shape, dtype=dtype)
+    q = run.random(heads, 5)
+    scales = scales_of(run)
+    scales[:, :, 1] *= size
+    put_scales(run, scales)
+    rows = some_rows(run)
+    ref, sd = reference(run, q, rows=rows)
+    check_within(run, q, attend(run, q), ref, sd, rows)
+
+
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_large_values_of_no_weight(shape, heads, dtype, first):
+    """Half of the tokens weigh 2^-80 of the others, each, and have values of 2^40 (fp16: 2^12) times theirs: nothing of
+    them is in the output, and what there is of the others is whole. Equal keys, so that a common error of their logits
+    cancels; the light half comes first or last, or in turns of 5."""
+    for turns in (False, True):
+        run = Run(**shape, hb=1, dtype=dtype)
+        q = torch.ones_like(run.random(heads, 5))
+        scales = scales_of(run)
+        scales[:, :, 0] = 4 / run.width ** 0.5                           # logits of +-28
+        for b, n in enumerate(run.len):
+            for j in range(n):
+                light = (j // 5 % 2 == 0) if turns else (j < n // 2) == first
+                put_codes(run, 0, b, j, -7 if light else 7)
+                if light:
+                    scales[run.table[b, j // run.page], :, 1, j % run.page] *= 2.0 ** (40 if dtype == "bf16" else 12)
+        put_scales(run, scales)
+        rows = some_rows(run)
+        ref, sd = reference(run, q, rows=rows)
+        check_within(run, q, attend(run, q), ref, sd, rows)
