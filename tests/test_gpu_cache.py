@@ -717,7 +717,8 @@ def test_append_many_sequences():
 # A few queries per sequence; many, which bf16 queries take to the other kernel.
 FEW = dict(lengths=[200, 333], new=[3, 1], kv=2, width=64)
 MANY_COLUMNS = dict(lengths=[200, 333, 90, 64], new=[60, 40, 90, 64], kv=16, width=64)
-SHAPES = [(FEW, 4, "bf16"), (FEW, 4, "f16"), (dict(FEW, width=128), 6, "bf16"), (MANY_COLUMNS, 64, "f16")]
+SHAPES = [(FEW, 4, "bf16"), (FEW, 4, "f16"), (dict(FEW, width=128), 6, "bf16"), (MANY_COLUMNS, 64, "f16"), (MANY_COLUMNS, 64, "bf16"),
+          (dict(MANY_COLUMNS, width=128, page=16), 64, "bf16")]
 
 
 def scales_of(run):
@@ -781,7 +782,7 @@ def test_attend_values_of_nothing_say_nothing(shape, heads, dtype, size):
     check_within(run, q, attend(run, q), ref, sd, rows)
 
 
-@pytest.mark.parametrize("shape,heads", [(FEW, 4)])
+@pytest.mark.parametrize("shape,heads", [(FEW, 4), (MANY_COLUMNS, 64)])
 def test_attend_zeros_appended_among_small_values(shape, heads):
     """Append gives a row of zeros a scale of 1 / sqrt(hb): the values of 1e-12 beside it stay what they are."""
     run = Run(**shape)
