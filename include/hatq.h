@@ -706,8 +706,9 @@ hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, lon
  * own sum, to which tokens whose value codes are all 0 do not belong (for fp16
  * queries as two fp16 each, about 22 bits); sums, maxima and norms are fp32. Value
  * scales of seen tokens may be anything from 2^-109 to 2^110; beyond, terms lose
- * bits. Rows that see a token with an infinite scale may become NaN. An infinity
- * or a NaN in a query makes that head of that row NaN.
+ * bits. Logits may be of any size up to about 1e30. Rows that see a token with an
+ * infinite scale may become NaN. An infinity or a NaN in a query makes that head of
+ * that row NaN.
  *   q, out   device, both HATQ_F16 or HATQ_BF16, [rows][q_heads][width] at pitches
  *            of rows and heads; they share no element, and out none with the cache
  *   q_heads  a multiple of the cache's heads, rows * q_heads < 2^31 - 1024

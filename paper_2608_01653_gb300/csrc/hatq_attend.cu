@@ -36,7 +36,8 @@ using tc::smem_addr;
 // m_c is raised only where some p v would exceed 2^15, to where it is just below 2^8 (what is dropped of subnormal products
 // goes by the power of two of p v, so that it is least there). Sums are in fp32, and so is that of p, which
 // may be large or small as the scales are: p stays below 2^103, so that scales of 2^-109 and more have all their bits, and
-// those up to 2^110 leave room for weights of 2^-23 of the heaviest.
+// those up to 2^110 leave room for weights of 2^-23 of the heaviest. Logits count from a base per column, 0 unless they are
+// beyond 2^13, so that m_c has bits for all that whatever their size.
 //
 // Memory-bound for few queries. A warp works by itself: its own ring of chunks (64 keys of one head, brought in by one
 // bulk copy per page), its own maxima and sums; no barrier between warps. The chunks of all sequences and heads are
@@ -101,6 +102,11 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ float low_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x & 0xffff))); }
 __device__ __forceinline__ float high_half(uint32_t x) { return __half2float(__ushort_as_half((unsigned short)(x >> 16))); }
+
+constexpr float kLowest = -3.402823466e38f;  // below every logit
+
+// A logit from its column's base on: not fused with the product that it is, so that equal ones stay equal.
+__device__ __forceinline__ float below(float s, float base) { return __fsub_rn(s, base); }
 
 // A scale's logarithm. Those below 2^-88 count as that, so that weights stay below 2^103; an infinity has one of no NaN.
 __device__ __forceinline__ float log2_of(float v) {
@@ -442,7 +448,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         __syncthreads();
     }
 
-    float o[NT][STEPS][4], off[NT][4], m[NT][2], l[NT][2];
+    float o[NT][STEPS][4], off[NT][4], base[NT][2], m[NT][2], l[NT][2];      // m from base on
     uint32_t qf[NT][PARTS][STEPS][2];
     float q_off[NT][2], q_f[NT][2];
     int lim[NT][2];
@@ -501,7 +507,8 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
                 for (int y = 0; y < 2; ++y) {
                     const int x = k.tile * COLS + nt * 8 + 2 * t + y, token = x / a.group;
                     lim[nt][y] = token < k.m ? k.len - k.m + token : -1;
-                    m[nt][y] = -1e30f;
+                    base[nt][y] = 0.0f;
+                    m[nt][y] = kLowest;
                     l[nt][y] = 0.0f;
                 }
 #pragma unroll
@@ -514,7 +521,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         }
 
         // ---- S^T of the chunk's 64 keys (what lies behind the last one is computed from whatever is there, and masked)
-        const uint8_t *base = mine + stage * STAGE;
+        const uint8_t *keys = mine + stage * STAGE;
         const int key0 = k.chunk * kChunk;
         const bool whole = key0 + kChunk <= k.len - k.m + k.tile * COLS / a.group + 1 && k.pages == (1 << pages_of_chunk) - 1;
         float s[NT][4][4], vs[4][2], ks[4][2], most[NT][2];
@@ -522,7 +529,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         int token[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            rec[j] = base + ((16 * j) >> c.page_bits) * record;
+            rec[j] = keys + ((16 * j) >> c.page_bits) * record;
             token[j] = (16 * j) & (size - 1);
             const uint8_t *sc = rec[j] + size * D + 4 * (token[j] + near);
             ks[j][0] = load_float(sc);
@@ -587,7 +594,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                most[nt][y] = -1e30f;
+                most[nt][y] = kLowest;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most[nt][y] = fmaxf(most[nt][y], fmaxf(s[nt][j][y], s[nt][j][2 + y]));
             }
@@ -600,7 +607,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         // ---- raise the maxima where a weight, or its product with a scale, may leave the range
         bool high = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) high |= most[nt][0] > m[nt][0] + room || most[nt][1] > m[nt][1] + room;
+        for (int nt = 0; nt < NT; ++nt) high |= most[nt][0] - base[nt][0] > m[nt][0] + room || most[nt][1] - base[nt][1] > m[nt][1] + room;
         if (__any_sync(0xffffffffu, high)) {
             // Tokens whose codes are all 0: nothing of them, whatever their scale. Two a lane. (Every warp comes here once, and
             // code that runs once is waited for: loops, not unrolled.)
@@ -608,7 +615,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll 1
             for (int i = 0; i < kChunk; i += 32) {
                 const int at = i + lane;
-                const uint4 *row = reinterpret_cast<const uint4 *>(base + (at >> c.page_bits) * record + (size + (at & (size - 1))) * (D / 2));
+                const uint4 *row = reinterpret_cast<const uint4 *>(keys + (at >> c.page_bits) * record + (size + (at & (size - 1))) * (D / 2));
                 uint32_t z = 0;
 #pragma unroll 1
                 for (int x = 0; x < D / 32; ++x) {
@@ -624,20 +631,44 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
                         if ((none[j >> 1] >> (16 * (j & 1) + 8 * h + near) & 1) && vs[j][h] < INFINITY) vs[j][h] = 0.0f;
+            // the largest product of every column, by what it sees alone
+            auto largest = [&](int nt, int y) {
+                float u = kLowest;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u = fmaxf(u, fmaxf(below(s[nt][j][y], base[nt][y]) + log2_of(vs[j][0]), below(s[nt][j][2 + y], base[nt][y]) + log2_of(vs[j][1])));
+#pragma unroll
+                for (int h = 4; h < 32; h *= 2) u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, h));
+                return u;
+            };
+            float x[NT][2];
+            bool move = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    x[nt][y] = largest(nt, y);
+                    move |= x[nt][y] > m[nt][y] + 15.0f && fabsf(x[nt][y]) > 8192.0f;
+                }
+            if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const bool own = x[nt][y] > m[nt][y] + 15.0f && fabsf(x[nt][y]) > 8192.0f;
+                        const float to = base[nt][y] + (own ? x[nt][y] : 0.0f), up = to - base[nt][y];
+                        base[nt][y] = to;
+                        m[nt][y] = fmaxf(m[nt][y] - up, kLowest);
+                        x[nt][y] = largest(nt, y);
+                    }
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float by[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float x = -1e30f;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x = fmaxf(x, fmaxf(s[nt][j][y] + log2_of(vs[j][0]), s[nt][j][2 + y] + log2_of(vs[j][1])));
-#pragma unroll
-                    for (int h = 4; h < 32; h *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, h));
-                    // (each column by what it sees alone)
-                    x = x > m[nt][y] + 15.0f ? x - 7.9f : m[nt][y];
-                    by[y] = lowered(l[nt][y], m[nt][y] - x);
-                    m[nt][y] = x;
+                    const float to = x[nt][y] > m[nt][y] + 15.0f ? x[nt][y] - 7.9f : m[nt][y];
+                    by[y] = lowered(l[nt][y], m[nt][y] - to);
+                    m[nt][y] = to;
                     off[nt][y] *= by[y];
                 }
 #pragma unroll
@@ -658,7 +689,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
             for (int nt = 0; nt < NT; ++nt) {
                 float p[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) p[y] = exp2_fast(s[nt][j][y] - m[nt][y & 1]);
+                for (int y = 0; y < 4; ++y) p[y] = exp2_fast(below(s[nt][j][y], base[nt][y & 1]) - m[nt][y & 1]);
                 l[nt][0] += p[0] + p[2];
                 l[nt][1] += p[1] + p[3];
                 // (nothing of a value that this query does not see, whatever its scale)
@@ -703,6 +734,24 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 
         if (k.first_last & 2) {
             // ---- the warp's part of the segment is done: m, l and o of every column to its piece
+            bool based = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) based |= base[nt][0] != 0.0f || base[nt][1] != 0.0f;
+            if (__any_sync(0xffffffffu, based)) {            // what base + m loses of m goes into l and o
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float rest = exp2_fast(base[nt][y] - (base[nt][y] + m[nt][y]) + m[nt][y]);
+                        l[nt][y] *= rest;
+                        off[nt][y] *= rest;
+#pragma unroll
+                        for (int x = 0; x < STEPS; ++x) {
+                            o[nt][x][y] *= rest;
+                            o[nt][x][2 + y] *= rest;
+                        }
+                    }
+            }
             float *to_piece = joined ? reinterpret_cast<float *>(mine) : a.pieces + piece * piece_floats(D, COLS);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -713,7 +762,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
                     for (int h = 4; h < 32; h *= 2) x += __shfl_xor_sync(0xffffffffu, x, h);
                     const int col = nt * 8 + 2 * t + y;
                     if (g == 0) {
-                        to_piece[col] = m[nt][y];
+                        to_piece[col] = base[nt][y] + m[nt][y];
                         to_piece[COLS + col] = x;
                     }
                     float *p = to_piece + 2 * COLS + col * D + g * (D / 8);
@@ -740,7 +789,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
     // ---- one segment: the warps' parts become one piece
     if (from == to && lane < COLS) {
         float *p = reinterpret_cast<float *>(mine);
-        p[lane] = -1e30f;
+        p[lane] = kLowest;
         p[COLS + lane] = 0.0f;
     }
     __syncthreads();
@@ -751,7 +800,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         if (a.direct && token >= first.m) break;
         const uint8_t *part = smem + min(lane, WARPS - 1) * warp_smem(D, NT) + 4 * col;
         const float pm = load_float(part), pl = lane < WARPS ? load_float(part + 4 * COLS) : 0.0f;
-        float most = pl == 0.0f ? -1e30f : pm;
+        float most = pl == 0.0f ? kLowest : pm;
 #pragma unroll
         for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         float sum = pl, v[E];
@@ -805,7 +854,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
     const Parts parts(total, ctas, WARPS);
     const long long cta_units = parts.active * parts.units;
     const int x = (r - begin) * a.group + h, tile = x / COLS, col = x % COLS;
-    float mx = -1e30f, l = 0.0f, o[E];
+    float mx = kLowest, l = 0.0f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
     if (q_head < a.q_heads && s.chunks > 0) {
@@ -827,12 +876,12 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
             else if (i < n0) place = a.segments + c0 * WARPS + w0 + i;
             else if (i < n0 + between) place = a.segments + (c0 + 1 + i - n0) * WARPS;
             else place = a.segments + c1 * WARPS + i - n0 - between;
-            float pm = -1e30f, pl = 0.0f;
+            float pm = kLowest, pl = 0.0f;
             if (i < n) {
                 pm = a.pieces[place * piece_floats(D, COLS) + col];
                 pl = a.pieces[place * piece_floats(D, COLS) + COLS + col];
             }
-            if (pl == 0.0f) pm = -1e30f;
+            if (pl == 0.0f) pm = kLowest;
             float now = fmaxf(mx, pm);
 #pragma unroll
             for (int d = 16; d; d /= 2) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, d));
@@ -863,9 +912,9 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs a, int ctas,
         for (int e = 0; e < E; ++e) s_o[warp][32 * e + lane] = o[e];
         __syncthreads();
         if (way) return;
-        const float pm = lane < ways ? s_m[warp + lane] : -1e30f;
+        const float pm = lane < ways ? s_m[warp + lane] : kLowest;
         float pl = lane < ways ? s_l[warp + lane] : 0.0f;
-        mx = pl == 0.0f ? -1e30f : pm;
+        mx = pl == 0.0f ? kLowest : pm;
 #pragma unroll
         for (int d = 4; d; d /= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
         const float by = pl == 0.0f ? 0.0f : lowered(pl, pm - mx);

@@ -24,7 +24,7 @@ using tc::smem_addr;
 // scales of those lie within 2^10 of the largest (a scale in two parts then keeps 15 bits), and one for its values, a factor of
 // the weights, where those do within 2^13 (code times scale is then a normal number, and what a row's own largest term is
 // rounded by at most 2^-18 of it). Otherwise every token has its own
-// two, which the rows apply one by one, to this chunk and those behind it. A row has two references: m for the sum of its weights, and
+// two, which the rows apply one by one, to this chunk and those behind it, as where logits are beyond 2^13. A row has two references: m for the sum of its weights, and
 // m + vm for their products with the values' powers, which it raises by what it sees alone, to where they are below 2^8: what
 // they keep is relative to the largest term of the row's own sum, whatever the scales of tokens that it does not see. A token
 // whose value codes are all 0 has no power (append gives rows of zeros a scale like any other).
@@ -68,6 +68,7 @@ struct alignas(16) Scaled {            // what the powers leave of the scales, f
 };
 constexpr int kKeysApart = 10, kValuesApart = 13, kNoOne = 1 << 20;
 constexpr float kNoPower = -10000.0f;  // of values of 0
+constexpr float kLowest = -3.402823466e38f;  // below every logit
 constexpr int kLeastV = -1000;         // below any product's power
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -513,7 +514,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
         // ---- softmax
         const int position = live ? seq.len - seq.m + token : 0x7fffffff;          // (rows that are none: nothing to mask)
         const int lowest = __reduce_min_sync(0xffffffffu, position);
-        float m = -1e30f, l = 0.0f;
+        float m = kLowest, l = 0.0f;
         int vm = kLeastV;
         // A row's keys of a chunk: all of them (true), or the ones that it sees.
         auto look = [&](int i, const Info &info, unsigned (&seen)[2]) {
@@ -556,7 +557,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             __syncwarp();
             if (lane == 0) mbar_arrive(p_full(tile));
         };
-        // A chunk whose scales have a power together. False where they have not, and nothing done, or where a wait gave up.
+        // A chunk whose scales have a power together. False where they have not or logits are too large, and nothing done, or where
+        // a wait gave up.
         auto together = [&](int i) {
             ok = __all_sync(0xffffffffu, mbar_wait(s_full(tile), (uint32_t)i & 1u, abort_flag, a.err));
             if (!ok) return false;
@@ -577,12 +579,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             float most = -3e38f;
 #pragma unroll
             for (int j = 0; j < 64; j += 2) most = max3(most, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
-            const float top = (whole || (seen[0] | seen[1])) ? most * fs : -1e30f;
+            const float top = (whole || (seen[0] | seen[1])) ? most * fs : kLowest;
             if (__any_sync(0xffffffffu, top > m + (float)min(8, vm + 15 - info.v_exponent) || info.v_exponent == kNoOne)) {
-                if (info.v_exponent == kNoOne) return false;
+                const float now = top > m + 8.0f ? top : m;
+                // (beyond 2^13 m has no bits for what weights carry beside it)
+                if (info.v_exponent == kNoOne || __any_sync(0xffffffffu, fabsf(now) > 8192.0f && now != kLowest)) return false;
                 wait_used(i);
                 if (!ok) return false;
-                const float now = top > m + 8.0f ? top : m;
                 raise(i, now, top - now + (float)info.v_exponent);
             }
             tc::tc_fence_before();
@@ -638,11 +641,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
                     tc::tmem_ld8(at + S::kS + 64 * tile + from, s);
                     tc::tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * (f * powers.k_factor[from + j]));
+                    for (int j = 0; j < 8; ++j) s[j] = __float_as_uint(__fmul_rn(__uint_as_float(s[j]), f * powers.k_factor[from + j]));      // (rounded: equal ones stay equal)
                     use(from, (from < 32 ? seen[0] : seen[1]) >> (from & 31));
                 }
             };
-            float top = -1e30f, more = -1e30f, now = m, sum = 0.0f;
+            float top = kLowest, more = kLowest, now = m, sum = 0.0f;
             auto largest = [&](int from, unsigned mask) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -654,7 +657,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             pass(largest);
             if (top > m + 8.0f) {
                 now = top;
-                more = -1e30f;
+                more = kLowest;
             }
             if (__any_sync(0xffffffffu, now != m)) pass(largest);
             wait_used(i);

@@ -856,3 +856,41 @@ def test_attend_large_values_of_no_weight(shape, heads, dtype, first):
         rows = some_rows(run)
         ref, sd = reference(run, q, rows=rows)
         check_within(run, q, attend(run, q), ref, sd, rows)
+
+
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -60, 2.0 ** 60])
+@pytest.mark.parametrize("scale", [1e31, -1e31])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_logits_far_from_zero(shape, heads, dtype, scale, size):
+    """A row that sees one token has its value, however low or high the logit: no magnitude stands for "no token"."""
+    if dtype == "f16" and size != 1:
+        pytest.skip("values that fp16 does not hold")
+    run = Run(**dict(shape, lengths=[max(m, 1) for m in shape["new"]]), dtype=dtype)
+    scales = scales_of(run)
+    scales[:, :, 1] *= size
+    put_scales(run, scales)
+    q = run.random(heads, 5)
+    rows = [r for r, _, p in run.places() if p == 0]
+    ref, sd = reference(run, q, rows=rows)                              # (one weight of 1: of any scale)
+    check_within(run, q, attend(run, q, scale=scale), ref, sd, rows)
+
+
+@pytest.mark.parametrize("spread", [0, 20])
+@pytest.mark.parametrize("logit", [3e3, -2e4, 3e6, -1e9, 1e20, -1e30])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_equal_logits_of_any_size(shape, heads, dtype, logit, spread):
+    """Equal keys: the average of the values that a row sees, as with a scale of 0. (fp16: spread by 2^10, as its outputs are.)"""
+    run = Run(**shape, hb=1, dtype=dtype)
+    q = torch.ones_like(run.random(heads, 5))
+    for b, n in enumerate(run.len):
+        for j in range(n):
+            put_codes(run, 0, b, j, 7)
+    scales = scales_of(run)
+    scales[:, :, 0] = 1 / 7
+    if spread:
+        u = torch.rand(scales.shape[:2] + scales.shape[3:], generator=gen(9), device="cuda")
+        scales[:, :, 1] *= 2.0 ** ((2 * u - 1) * (spread if dtype == "bf16" else 5))
+    put_scales(run, scales)
+    rows = some_rows(run)
+    ref, sd = reference(run, q, 0.0, rows=rows)
+    check_within(run, q, attend(run, q, scale=logit / run.width), ref, sd, rows)
