@@ -185,3 +185,19 @@ def test_refusals():
                 lambda: block().forward(rand(3, C, seed=1), block().cache(4), ints([[0], [1]]), ints([1, 1]))):
         with pytest.raises((ValueError, H.HatqError)):
             bad()
+
+
+@pytest.mark.parametrize("x", [torch.float32, torch.float64])
+def test_inputs_that_cannot_be_attended_leave_the_cache(x):
+    B = block()
+    table, pages = tables([3], 16)
+    cache = B.cache(pages, page=16)
+    before = cache.data.clone()
+    good = rand(3, C, seed=8)
+    for bad in (lambda: B.forward(good.to(x), cache, table, ints([3]), ints([0, 3])),
+                lambda: B.forward(good, cache, table, ints([3]), ints([0, 3]), turn=lambda q, k: (q.to(x), k)),
+                lambda: B.forward(good, cache, table, ints([3]), ints([0, 3]), turn=lambda q, k: (q[:, :, 1:], k))):
+        with pytest.raises(ValueError):
+            bad()
+    torch.cuda.synchronize()
+    assert torch.equal(cache.data, before)
