@@ -586,9 +586,9 @@ __global__ void __launch_bounds__(256) quantize_groups_kernel(const T *w, long l
         }
         __syncthreads();
     }
-    const int lane = threadIdx.x & 31, groups = (k + group - 1) / group;
+    const int lane = threadIdx.x & 31, groups = (k - 1) / group + 1;              // (k + group may be beyond an int)
     for (int g = threadIdx.x >> 5; g < groups; g += 8) {
-        const int from = g * group, to = min(k, from + group);
+        const int from = g * group, to = k - from > group ? from + group : k;
         float most = 0.0f;
         for (int i = from + lane; i < to; i += 32) {
             const float v = fabsf(t[i]);

@@ -224,3 +224,17 @@ def test_refusals():
         with pytest.raises((ValueError, H.HatqError)):
             bad()
     finish()
+
+
+@pytest.mark.parametrize("group", [2 ** 31 - 32, 2 ** 31 - 128])
+def test_the_largest_groups(group):
+    """One scale a channel, the group's size as large as an int allows: as with a group of all inputs."""
+    w = torch.randn(37, 320, generator=gen(1), device="cuda")
+    c, s = H.quantize_groups(w, group, 64)
+    want = H.quantize_groups(w, 320, 64)
+    x = whole(3, 320, 2, torch.bfloat16)
+    y = H.linear4(x, H.prepare_linear4(w, group, 64), dtype=torch.float32)
+    finish()
+    assert c.shape == (37, 320) and s.shape == (37, 1) and torch.equal(c, want[0]) and torch.equal(s, want[1])
+    ref, terms = formula(x, c, s, 320)
+    assert bool(((y.double() - ref).abs() <= U * (17 * 4 + 2 * 5 / 8 + 12) * terms + U * ref.abs()).all())
