@@ -238,3 +238,19 @@ def test_the_largest_groups(group):
     assert c.shape == (37, 320) and s.shape == (37, 1) and torch.equal(c, want[0]) and torch.equal(s, want[1])
     ref, terms = formula(x, c, s, 320)
     assert bool(((y.double() - ref).abs() <= U * (17 * 4 + 2 * 5 / 8 + 12) * terms + U * ref.abs()).all())
+
+
+@pytest.mark.parametrize("rows", [5, 40])
+def test_any_nan_in_single_precision_is_one(rows):
+    """NaNs whose upper 16 bits are those of an infinity among them."""
+    x = whole(rows, 200, 1, torch.float32)
+    w = codes(40, 200, 2)
+    w[w == 0] = 1
+    L = H.prepare_linear4(w, 32, scales=torch.ones(40, 7, device="cuda"))
+    want = H.linear4(x, L)
+    bits = torch.tensor([0x7f800001, 0x7f80ffff, -0x7fffff, 0x7fffffff], dtype=torch.int32, device="cuda").view(torch.float32)
+    for r in range(4):
+        x[r, 50 * r] = bits[r]
+    y = H.linear4(x, L)
+    finish()
+    assert bool(y[:4].isnan().all()) and torch.equal(y[4:], want[4:])
