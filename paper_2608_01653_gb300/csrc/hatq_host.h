@@ -41,6 +41,7 @@ bool overlap(const void *p, long long p_rows, long long p_pitch, long long p_wid
     if (!(p0 < q1 && q0 < p1)) return false;
     if (p_rows > 1 && q_rows > 1 ? p_step != q_step : p_rows == 1 && q_rows == 1) return true;
     const uintptr_t step = p_rows > 1 ? p_step : q_step;
+    if (step == 0) return true;                              // (all of its rows are one)
     const uintptr_t at = q0 >= p0 ? (q0 - p0) % step : (step - (p0 - q0) % step) % step;   // q's place, p's is 0
     return at < p_bytes || at + q_bytes > step;
 }

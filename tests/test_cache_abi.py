@@ -58,6 +58,13 @@ def test_append_refuses(lib, kw, status):
     assert append(lib, **kw) == status and H.last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(k=P + 512, ldk=0), dict(v=P + 512, ldv=0), dict(k=P + 512, ldk=0, ldv=0)])
+def test_append_refuses_one_row_for_all_within_the_cache(lib, kw):
+    """Keys or values expanded over the rows (a pitch of 0) that lie in a cache of one page."""
+    assert append(lib, cache(pages=1), **kw) == H.ERR_INVALID_ARG and "overlap" in H.last_error()
+    assert append(lib, cache(pages=1), **dict(kw, rows=1, seqs=1)) == H.ERR_INVALID_ARG
+
+
 def attend(lib, c=None, **kw):
     a = dict(q=2 * P, type=H.BF16, ldq=512, hq=128, heads=4, rows=4, table=4 * P, ldt=3, width=3, lengths=5 * P, starts=6 * P,
              seqs=2, scale=0.1, out=7 * P, ldo=512, ho=128, ws=8 * P, size=1 << 40)
