@@ -5,12 +5,14 @@ side of a code's border would otherwise be carried on); then prompts, pieces, si
 another.
 """
 import math
+from types import SimpleNamespace
 
 import pytest
 import torch
 
 from paper_2608_01653_gb300 import hatq as H
 from paper_2608_01653_gb300.attention import AttentionBlock
+from tests.test_gpu_cache import reference
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +203,27 @@ def test_inputs_that_cannot_be_attended_leave_the_cache(x):
             bad()
     torch.cuda.synchronize()
     assert torch.equal(cache.data, before)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lengths,new", [([70, 5, 33], [70, 5, 33]), ([300, 1, 129], [1, 1, 1])])
+def test_attention_of_the_block_within_its_deviations(dtype, lengths, new):
+    """What the block attends to, with a bound that an output of zeros does not meet.
+
+    A logit's terms are rounded to fp16 once, 2^-11 / sqrt(3) of sqrt(sum q^2 k^2) / 8, which is about 1 here: weights are off by
+    some 4e-4 of themselves and rounded by as much; deviations of the output are below 2^0.5 times that of its own size (both
+    are sums of terms of random signs), eight of them times sqrt(2) below 2 %, and half a step of the type 0.4 %: 5 % in all."""
+    B = block()
+    table, pages = tables(lengths, 16)
+    cache = B.cache(pages, page=16)
+    n = sum(lengths)
+    B.forward(rand(n, C, seed=7, dtype=dtype), cache, table, ints(lengths), ints([0] + torch.tensor(lengths).cumsum(0).tolist()))
+    q = rand(sum(new), HEADS, D, seed=8, dtype=dtype)
+    y = H.attend_tokens(q, cache, table, ints(lengths), ints([0] + torch.tensor(new).cumsum(0).tolist()))
+    torch.cuda.synchronize()
+    H.sync_status()
+    run = SimpleNamespace(kv=KV, width=D, page=16, hb=cache.hb, cache=cache, table=table, len=lengths, new=new)
+    ref, sd = reference(run, q)
+    tol = 8 * 2 ** 0.5 * sd + torch.finfo(dtype).eps / 2 * 1.01 * ref.abs() + 2.0 ** -24
+    assert bool(((y.double().cpu() - ref).abs() <= tol).all())
+    assert bool((tol.norm(dim=-1) < 0.05 * ref.norm(dim=-1)).all())
