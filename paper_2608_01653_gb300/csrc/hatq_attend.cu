@@ -609,17 +609,18 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) high |= most[nt][0] - base[nt][0] > m[nt][0] + room || most[nt][1] - base[nt][1] > m[nt][1] + room;
         if (__any_sync(0xffffffffu, high)) {
-            // Tokens whose codes are all 0: nothing of them, whatever their scale. Two a lane. (Every warp comes here once, and
-            // code that runs once is waited for: loops, not unrolled.)
+            // Tokens whose codes are all 0: nothing of them, whatever their scale. A lane has two, one after the other: every warp
+            // comes here once, and code that runs once is waited for (131072 keys 42.6 us, both at once 43.7).
             unsigned none[2] = {0, 0};
 #pragma unroll 1
             for (int i = 0; i < kChunk; i += 32) {
                 const int at = i + lane;
                 const uint4 *row = reinterpret_cast<const uint4 *>(keys + (at >> c.page_bits) * record + (size + (at & (size - 1))) * (D / 2));
                 uint32_t z = 0;
-#pragma unroll 1
-                for (int x = 0; x < D / 32; ++x) {
-                    const uint4 w = row[x];
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {           // (from a piece on that leaves no two lanes the same banks)
+                    const int piece = x + (lane >> (D == 128 ? 1 : D == 256 ? 0 : 2)) % (D / 32);
+                    const uint4 w = row[piece < D / 32 ? piece : piece - D / 32];
                     z |= (w.x ^ 0x88888888u) | (w.y ^ 0x88888888u) | (w.z ^ 0x88888888u) | (w.w ^ 0x88888888u);
                 }
                 none[0] = none[1];
