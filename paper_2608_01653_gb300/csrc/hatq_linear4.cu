@@ -65,10 +65,9 @@ __device__ __forceinline__ void load8(const Linear4Args &a, const T *row, bool l
             for (int i = 0; i < 8; ++i)
                 if (k + i < a.k) v[i] = row[k + i];
         }
-        // (a NaN may have no bit of it in its upper half, which would be an infinity)
+        // (a NaN may have no bit of it in its upper half, which would be an infinity; a sum's has all)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (v[i] != v[i]) v[i] = __int_as_float(0x7fffffff);
+        for (int i = 0; i < 8; ++i) v[i] = __fadd_rn(v[i], 0.0f);
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
             uint32_t w[4];
