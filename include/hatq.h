@@ -764,7 +764,8 @@ hatq_status hatq_linear4_layout(const int8_t *w, long long ldw, const float *sca
  * are exact, a group's sum is fp32 as the tensor cores add, everything else rounded
  * fp32, then y_type once.
  *   x        device, hatq_type x_type (16-bit x enter the products as they are, fp32
- *            x as the exact sum of three bf16 numbers), pitch ldx >= k; codes of
+ *            x as the sum of three bf16 numbers, exact for magnitudes from 2^-102
+ *            on), pitch ldx >= k; codes of
  *            hatq_quantize_tokens (F16 format, same hb as the weights) among them
  *   s_x      device float [rows], or NULL: 1
  *   y        device, hatq_type y_type, pitch ldy >= n; shares no element with x

@@ -46,7 +46,7 @@ using tc::smem_addr;
 // (sequence, head, tile) its warps are joined first; where such segments are short a CTA takes one each and no second
 // kernel is needed. 12 warps (heads of 128) are what 227 KB of rings and 168 registers allow. Measured: one query behind
 // 131072 keys, 32 heads over 8: 42 us (3.4 TB/s; 0.9 of the memory's rate once all warps are under way, 12 us to set out
-// and to join); 64 ragged sequences up to 8192 keys 72 us (4.2 TB/s).
+// and to join); 64 ragged sequences up to 8192 keys 73 us (4.2 TB/s).
 
 __host__ __device__ constexpr int kWarps(int d, int nt) { return d == 256 ? 6 : d == 192 || nt == 2 ? 8 : 12; }
 __host__ __device__ constexpr int kStages(int d, int nt) { return (d == 64 ? 3 : 2) + (d <= 128 && nt == 2); }

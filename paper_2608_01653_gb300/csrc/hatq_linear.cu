@@ -65,9 +65,6 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-// One lane of the warp. The issuing warps run their loops with all lanes and pick the lane only around the
-// asynchronous instructions: their operands then stay warp-uniform for the compiler (with the loops under a
-// lane == 0 branch a 64-code block cost about 800 cycles of issue, whatever the tile).
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }

@@ -36,7 +36,7 @@ using tc::smem_addr;
 // chunk as soon as the rows have read this one's, PV when the weights are there. Two tiles share what is widened.
 //
 // Bound by the rows' softmax: per chunk and two tiles the tensor cores have 1200 cycles of work, a chunk takes 2500 (2048
-// queries, the last of 8192 tokens, and 889 of 3445, 32 heads over 8: 325 us, 872 TFLOP/s, tensor pipe 0.41, issue 0.53).
+// queries, the last of 8192 tokens, and 889 of 3445, 32 heads over 8: 326 us, 870 TFLOP/s, tensor pipe 0.41, issue 0.53).
 constexpr int kRaw = 4;                // chunks on their way or being widened
 constexpr int kWide = 4;               // widened chunks
 constexpr int kInfo = kRaw + kWide;    // a chunk is brought in when the one this many before has been multiplied

@@ -782,6 +782,20 @@ def test_attend_values_of_nothing_say_nothing(shape, heads, dtype, size):
     check_within(run, q, attend(run, q), ref, sd, rows)
 
 
+@pytest.mark.parametrize("size", [0.0, 2.0 ** -100, 1.0, 2.0 ** 100])
+@pytest.mark.parametrize("shape,heads,dtype", SHAPES)
+def test_attend_values_of_nothing_alone(shape, heads, dtype, size):
+    """All value codes are 0, or (size 0) all value scales: zeros."""
+    run = Run(**shape, dtype=dtype)
+    half = run.page * run.width // 2
+    if size:
+        run.cache.data[:, :, half:2 * half] = 0x88
+    scales = scales_of(run)
+    scales[:, :, 1] *= size
+    put_scales(run, scales)
+    assert bool((attend(run, run.random(heads, 5)) == 0).all())
+
+
 @pytest.mark.parametrize("shape,heads", [(FEW, 4), (MANY_COLUMNS, 64)])
 def test_attend_zeros_appended_among_small_values(shape, heads):
     """Append gives a row of zeros a scale of 1 / sqrt(hb): the values of 1e-12 beside it stay what they are."""
