@@ -40,10 +40,11 @@ class AttentionBlock:
 
     def forward(self, x, cache, table, lengths, starts=None, turn=None):
         """x [rows][C] in float16 or bfloat16, the newest tokens of every sequence (table, lengths, starts as hatq.append_tokens
-        takes them; they go into the cache). turn(q, k), if given, returns both with their positions, as they were given.
+        takes them; they go into the cache). turn(q, k), if given, returns both with their positions (k as it was given).
         Returns [rows][C] in x's type; what it holds for rows of no sequence (padding behind the last) means nothing."""
         torch = hatq._token_torch()
-        if x.dtype != torch.bfloat16 and x.dtype != torch.float16:          # (append would take it, attention would not)
+        types = torch.float16, torch.bfloat16
+        if x.dtype not in types:                                            # (append would take it, attention would not)
             raise ValueError(f"x: dtype {x.dtype}, expected float16 or bfloat16")
         rows, h, kv, d = x.shape[0], self.heads, self.kv_heads, self.width
         c, s = hatq.quantize_tokens(x, hb=self.hb, codes="f16")
@@ -51,9 +52,9 @@ class AttentionBlock:
         q, k, v = y[:, :h], y[:, h:h + kv], y[:, h + kv:]
         if turn is not None:
             q, k = turn(q, k)
-            if q.dtype != x.dtype or tuple(q.shape) != (rows, h, d) or q.device != x.device or q.stride(2) != 1:
-                raise ValueError(f"turn: q is {q.dtype} {tuple(q.shape)} on {q.device} with strides {q.stride()}, expected {x.dtype} "
-                                 f"{(rows, h, d)} on {x.device} with contiguous heads")
+            if q.dtype not in types or tuple(q.shape) != (rows, h, d) or q.device != x.device or q.stride(2) != 1:
+                raise ValueError(f"turn: q is {q.dtype} {tuple(q.shape)} on {q.device} with strides {q.stride()}, expected float16 or "
+                                 f"bfloat16 {(rows, h, d)} on {x.device} with contiguous heads")
         hatq.append_tokens(cache, k, v, table, lengths, starts)
         y = hatq.attend_tokens(q, cache, table, lengths, starts)
         c, s = hatq.quantize_tokens(y.reshape(rows, h * d), hb=self.hb, codes="f16")

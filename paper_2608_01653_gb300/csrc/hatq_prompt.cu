@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(const AttendA
             float most = -3e38f;
 #pragma unroll
             for (int j = 0; j < 64; j += 2) most = max3(most, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
-            const float top = (whole || (seen[0] | seen[1])) ? most * fs : kLowest;
+            const float top = most > -3e38f ? most * fs : kLowest;           // (none seen that is a number)
             if (__any_sync(0xffffffffu, top > m + (float)min(8, vm + 15 - info.v_exponent) || info.v_exponent == kNoOne)) {
                 const float now = top > m + 8.0f ? top : m;
                 // (beyond 2^13 m has no bits for what weights carry beside it)

@@ -227,3 +227,18 @@ def test_attention_of_the_block_within_its_deviations(dtype, lengths, new):
     tol = 8 * 2 ** 0.5 * sd + torch.finfo(dtype).eps / 2 * 1.01 * ref.abs() + 2.0 ** -24
     assert bool(((y.double().cpu() - ref).abs() <= tol).all())
     assert bool((tol.norm(dim=-1) < 0.05 * ref.norm(dim=-1)).all())
+
+
+@pytest.mark.parametrize("queries", [torch.bfloat16, torch.float16])
+def test_queries_may_be_turned_in_either_type(queries):
+    B = block()
+    table, pages = tables([40], 16)
+    out = []
+    for turn in (None, lambda q, k: (q.to(queries), k)):
+        cache = B.cache(pages, page=16)
+        out.append(B.forward(rand(40, C, seed=8), cache, table, ints([40]), ints([0, 40]), turn=turn))
+    torch.cuda.synchronize()
+    H.sync_status()
+    # (bf16 queries are fp16's, but for their range; the second attention rounds to 11 bits where the first does to 8, 2^-9 of a
+    # value: a code of its 8-bit quantization in 4, 1/127 of the largest or about 3 / 127 of the rest each, changes)
+    assert float((out[0] - out[1]).float().norm() / out[0].float().norm()) < 0.05
