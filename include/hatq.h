@@ -702,13 +702,13 @@ hatq_status hatq_append_tokens(const hatq_token_cache *cache, const void *k, lon
  * A row that sees no token (before the sequence's first, or none of its pages is
  * one) gets zeros. Tokens that a row does not see do not reach it, whatever their
  * scales are. q and the weights times the value scales enter the products as fp16
- * brought into range by powers of two, the latter by the largest term of the row's
- * own sum, to which tokens whose value codes are all 0 do not belong (for fp16
- * queries as two fp16 each, about 22 bits); sums, maxima and norms are fp32. Value
- * scales of seen tokens may be anything from 2^-109 to 2^110; beyond, terms lose
- * bits. Logits may be of any size up to about 1e30. Rows that see a token with an
- * infinite scale may become NaN. An infinity or a NaN in a query makes that head of
- * that row NaN.
+ * brought into range by powers of two, the latter by the largest that the row sees:
+ * terms below 2^-20 of it lose bits, below 2^-31 all. (Tokens whose value codes are all
+ * 0 count there by their weight at most, not by their scale. For fp16 queries both go
+ * in as two fp16 each, about 22 bits.) Sums, maxima and norms are fp32. Value scales
+ * of seen tokens may be anything from 2^-109 to 2^110; beyond, terms lose bits. Logits
+ * may be of any size up to about 1e30. Rows that see a token with an infinite scale
+ * may become NaN. An infinity or a NaN in a query makes that head of that row NaN.
  *   q, out   device, both HATQ_F16 or HATQ_BF16, [rows][q_heads][width] at pitches
  *            of rows and heads; they share no element, and out none with the cache
  *   q_heads  a multiple of the cache's heads, rows * q_heads < 2^31 - 1024
