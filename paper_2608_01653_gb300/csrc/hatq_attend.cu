@@ -33,8 +33,10 @@ using tc::smem_addr;
 // any other). For fp16 queries, whose outputs would show it, both go through in two parts, high and low,
 // and codes are widened whole: the tensor cores align a subnormal's product as if it were a normal one's, and what they
 // then drop left sums off by up to 2^-14 of their terms.
-// m_c is raised only where some p v would exceed 2^15, to where it is just below 2^8 (what is dropped of subnormal products
-// goes by the power of two of p v, so that it is least there). Sums are in fp32, and so is that of p, which
+// m_c is raised only where some p v would exceed 2^15 (bf16: 2^12), to where it is just below 2^8. (What is dropped of
+// subnormal products goes by the power of two of the largest p v: it is least there, and codes of 0, which are looked for
+// where m_c may be raised alone, cost the others 2^-14 of at most 2^4 times the largest of them. 64 ragged sequences 73.3 us, with 2^15
+// 72.7.) Sums are in fp32, and so is that of p, which
 // may be large or small as the scales are: p stays below 2^103, so that scales of 2^-109 and more have all their bits, and
 // those up to 2^110 leave room for weights of 2^-23 of the heaviest. Logits count from a base per column, 0 unless they are
 // beyond 2^13, so that m_c has bits for all that whatever their size.
@@ -297,6 +299,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
     constexpr bool kTwo = std::is_same<T, __half>::value;      // q and p in two parts
     constexpr int PARTS = kTwo ? 2 : 1;
     constexpr float kOdd = kTwo ? 1.0f : 0.0625f, kUnit = kTwo ? 1.0f : 0x1p24f;     // of a code at an odd place; of a sum
+    constexpr float kMost = kTwo ? 15.0f : 12.0f;              // logarithm of what p v may be before m is raised
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ int s_abort;
     const CacheArgs &c = a.c;
@@ -603,7 +606,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
         float largest = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) largest = fmaxf(largest, fmaxf(vs[j][0], vs[j][1]));
-        const float room = 15.0f - log2_of(largest);
+        const float room = kMost - log2_of(largest);
         // ---- raise the maxima where a weight, or its product with a scale, may leave the range
         bool high = false;
 #pragma unroll
@@ -648,14 +651,14 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     x[nt][y] = largest(nt, y);
-                    move |= x[nt][y] > m[nt][y] + 15.0f && fabsf(x[nt][y]) > 8192.0f;
+                    move |= x[nt][y] > m[nt][y] + kMost && fabsf(x[nt][y]) > 8192.0f;
                 }
             if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const bool own = x[nt][y] > m[nt][y] + 15.0f && fabsf(x[nt][y]) > 8192.0f;
+                        const bool own = x[nt][y] > m[nt][y] + kMost && fabsf(x[nt][y]) > 8192.0f;
                         const float to = base[nt][y] + (own ? x[nt][y] : 0.0f), up = to - base[nt][y];
                         base[nt][y] = to;
                         m[nt][y] = fmaxf(m[nt][y] - up, kLowest);
@@ -667,7 +670,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWarps(D, NT) / WARPS) attend_kern
                 float by[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float to = x[nt][y] > m[nt][y] + 15.0f ? x[nt][y] - 7.9f : m[nt][y];
+                    const float to = x[nt][y] > m[nt][y] + kMost ? x[nt][y] - 7.9f : m[nt][y];
                     by[y] = lowered(l[nt][y], m[nt][y] - to);
                     m[nt][y] = to;
                     off[nt][y] *= by[y];

@@ -782,6 +782,27 @@ def test_attend_values_of_nothing_say_nothing(shape, heads, dtype, size):
     check_within(run, q, attend(run, q), ref, sd, rows)
 
 
+@pytest.mark.parametrize("size", [4.0, 10.0, 20.0, 40.0, 100.0])
+@pytest.mark.parametrize("width,hb,page,group", [(64, 1, 16, 4), (128, 128, 64, 1), (256, 1, 16, 4), (256, 256, 16, 1)])
+@pytest.mark.parametrize("seed", [3, 26, 34, 56])
+def test_attend_values_of_nothing_among_the_others(width, hb, page, group, seed, size):
+    """Two in five tokens have value codes of 0 and scales some times those of the others: too near them to raise a maximum."""
+    lengths = [559, 60, 132, 490, 32, 400, 375, 68]
+    run = Run(lengths, [1] * 8, kv=2, width=width, page=page, hb=hb, seed=seed, one_each=True)
+    pick = np.random.default_rng(seed)
+    scales = scales_of(run)
+    for b, n in enumerate(lengths):
+        for j in range(1, n):
+            if pick.random() < 0.4:
+                put_codes(run, 1, b, j, 0)
+                scales[run.table[b, j // page], :, 1, j % page] = 0
+    put_scales(run, scales)
+    q = run.random(2 * group, 5)
+    ref, sd = reference(run, q, 0.05)                                   # (small logits: the others keep weights of their own)
+    put_scales(run, torch.where(scales == 0, size, scales))
+    check_within(run, q, attend(run, q, scale=0.05), ref, sd, list(range(8)))
+
+
 @pytest.mark.parametrize("size", [0.0, 2.0 ** -100, 1.0, 2.0 ** 100])
 @pytest.mark.parametrize("shape,heads,dtype", SHAPES)
 def test_attend_values_of_nothing_alone(shape, heads, dtype, size):
